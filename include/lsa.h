@@ -292,6 +292,117 @@ size_t lsa_hfa_attn_workspace_size(const lsa_attn_params* p, int64_t n_rows);
 lsa_status lsa_hfa_attn(const lsa_attn_params* p, int64_t n_rows, const void* q, const void* kv, int64_t n_kv_rows,
                         const int32_t* idx, const int32_t* count, int32_t k_cap, int64_t q_start, int32_t k_swa,
                         void* out, float* lse, void* workspace, size_t ws_bytes, void* stream);
+/*
+ * Appending new tokens to a paged cache, with the position rotation applied on the way: the step of a
+ * serving program before the indexer and the attention of every layer. Per token, in one launch:
+ *   - dims [rot_start, rot_start + rot_dim) of each query and key head are rotated by the angles of the
+ *     token's position p: for pair i (0 <= i < rot_dim / 2) of values (a, b),
+ *       a' = a cos(p, i) - b sin(p, i),  b' = b cos(p, i) + a sin(p, i),
+ *     where the pair is dims (i, i + rot_dim / 2) of the rotated part, or (2 i, 2 i + 1) when interleaved;
+ *   - keys and values are written to the token's row of the caches, in bf16, or as e4m3 codes with one
+ *     fp32 scale per token and head (scale = max |x| / 448 over the rotated row, at least 2^-126; 1 for a
+ *     row of zeros; code = x / scale, both rounded to nearest even); the products are fp32 and each stored
+ *     value is rounded once;
+ *   - queries are written to q_out, rotated.
+ * It serves the cache of MQA and grouped heads (keys and values), the MLA latent cache (d_v = 0, the
+ * latent and its rotated part given apart) and the indexer's key cache (d_v = 0, fp8).
+ */
+typedef struct lsa_append_params {
+  int32_t n_heads;     /* query heads rotated in the same call; 0: no queries                    */
+  int32_t n_kv_heads;  /* key (and value) heads of a token, >= 1                                 */
+  int32_t d_k;         /* width of a query or key head, multiple of 16, <= 1024                  */
+  int32_t d_v;         /* width of a value head, multiple of 16, <= 1024; 0: no values           */
+  int32_t rot_start;   /* first rotated dim, multiple of 16                                      */
+  int32_t rot_dim;     /* rotated dims, multiple of 16; 0: no rotation                           */
+  int32_t interleaved; /* 1: pairs (2 i, 2 i + 1); 0: pairs (i, i + rot_dim / 2)                 */
+  int32_t key_dtype;   /* lsa_key_dtype of the caches                                            */
+} lsa_append_params;
+
+/* Device tensors of one append. Strides are elements from one token to the next (a token's heads lie one
+ * after the other), multiples of 8, so that the slices of a fused projection are taken as they are; bf16
+ * inputs are 16-byte aligned. P = kv_page_size. */
+typedef struct lsa_append_tensors {
+  const void* q;             /* [n_tok, n_heads, d_k] bf16, or without the rotated dims (q_rot given)    */
+  const void* q_rot;         /* NULL, or [n_tok, n_heads, rot_dim] bf16; then rot_start = d_k - rot_dim > 0 */
+  const void* k;             /* [n_tok, n_kv_heads, d_k] bf16, or without the rotated dims (k_rot given) */
+  const void* k_rot;         /* NULL, or [n_tok, n_kv_heads, rot_dim] bf16                               */
+  const void* v;             /* [n_tok, n_kv_heads, d_v] bf16; NULL when d_v = 0                         */
+  int64_t q_stride, q_rot_stride, k_stride, k_rot_stride, v_stride;
+  const float* rope;         /* [rope_rows, rot_dim]: rot_dim / 2 cosines, then as many sines, of each
+                                position; NULL when rot_dim = 0                                          */
+  int64_t rope_rows;
+  const int32_t* seq;        /* [n_tok] sequence of each token; NULL: token i is of sequence
+                                i / rows_per_seq                                                         */
+  const int32_t* pos;        /* [n_tok] position of each token; NULL: the tokens are the last ones of
+                                their sequences by ctx_len, as in lsa_decode_attn: token i of sequence b
+                                is at ctx_len[b] - rows_per_seq + i % rows_per_seq                       */
+  const int32_t* ctx_len;    /* [n_seq] tokens of each sequence, the new ones included; only without pos */
+  const int32_t* page_table; /* [n_seq, max_pages] physical pages; NULL: sequence b has page b alone     */
+  void* q_out;               /* [n_tok, n_heads, d_k] bf16, contiguous; may be q itself when q is
+                                contiguous and q_rot NULL                                                */
+  void* k_cache;             /* [n_phys, n_kv_heads, P, d_k]                                             */
+  float* k_scale;            /* [n_phys, n_kv_heads, P]; NULL for bf16                                   */
+  void* v_cache;             /* [n_phys, n_kv_heads, P, d_v]; NULL when d_v = 0                          */
+  float* v_scale;            /* [n_phys, n_kv_heads, P]; NULL for bf16 or when d_v = 0                   */
+  int64_t* rows;             /* NULL, or [n_tok]: physical page * P + offset of each token, -1 where it
+                                was skipped: what lsa_block_keys_update takes                            */
+} lsa_append_tensors;
+
+/*
+ * A token is skipped (nothing is cached, rows = -1) when its sequence is outside [0, n_seq), its position
+ * is negative, beyond max_pages * P or (with a rotation) beyond rope_rows, or its page-table entry is
+ * outside [0, n_phys). The queries of a token without a valid sequence and position are zeros. Two tokens
+ * of one call must not share a sequence and position.
+ */
+lsa_status lsa_cache_append(const lsa_append_params* p, const lsa_append_tensors* t, int64_t n_tok,
+                            int32_t n_seq, int32_t rows_per_seq, int32_t max_pages, int32_t kv_page_size,
+                            int64_t n_phys, void* stream);
+
+/*
+ * Attention of new tokens over the whole of a paged cache (decode of layers, or of contexts, that have no
+ * index list): grouped query heads over keys and values, or the MLA latent cache.
+ */
+typedef struct lsa_decode_attn_params {
+  int32_t n_heads;    /* query heads, a multiple of n_kv_heads, <= 1024                                */
+  int32_t n_kv_heads; /* key/value heads; 1 with a latent cache                                        */
+  int32_t d_qk, d_v;  /* (64, 64) or (128, 128); (576, 512) with a latent cache                        */
+  int32_t latent;     /* 1: MLA latent cache, V = first d_v columns of the same row (Eq. 3)            */
+  int32_t key_dtype;  /* lsa_key_dtype of the caches; LSA_KEY_BF16 with a latent cache                 */
+  int32_t k_sink;     /* with k_swa > 0: the first k_sink positions are attended as well               */
+  int32_t k_swa;      /* 0: every position up to the query's; else only the last k_swa (and the sink)  */
+  float sm_scale;     /* softmax scale applied to q . k                                                */
+} lsa_decode_attn_params;
+
+/* Workspace bytes for lsa_decode_attn; 0 when no call of these sizes cuts a sequence into parts. */
+size_t lsa_decode_attn_workspace_size(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq,
+                                      int32_t max_pages, int32_t kv_page_size);
+
+/*
+ * The rows_per_seq (>= 1) newest tokens of each sequence, whose keys and values are in the cache already:
+ * row j of sequence b is its token at t = ctx_len[b] - rows_per_seq + j and attends to
+ *   A = { s <= t : k_swa = 0 or s > t - k_swa or s < k_sink, and the page of s is mapped },
+ *   o = sum_{s in A} softmax_s(sm_scale * q . k_s) v_s,   lse = log sum_{s in A} exp(sm_scale * q . k_s).
+ * Head h reads key/value head h / (n_heads / n_kv_heads). Where A is empty (t < 0, an idle slot of a
+ * batch with ctx_len = 0, no mapped page, or ctx_len outside [0, max_pages * P]), and where every score is
+ * -inf, o = 0 and lse = -inf. What the cache holds outside A, NaN and infinities among it, has no effect.
+ *   q           [n_seq * rows_per_seq, n_heads, d_qk] bf16 (already rotated, e.g. by lsa_cache_append)
+ *   k_cache     [n_phys, n_kv_heads, P, d_qk] with P = kv_page_size, as lsa_cache_append writes it;
+ *               latent: [n_phys, P, d_qk]
+ *   k_scale     [n_phys, n_kv_heads, P] fp32 for fp8 caches (k = scale * code), else NULL
+ *   v_cache     [n_phys, n_kv_heads, P, d_v], v_scale as k_scale; both NULL with a latent cache
+ *   ctx_len     [n_seq] int32, the new tokens included
+ *   page_table  [n_seq, max_pages] int32 physical pages, entries outside [0, n_phys) are unmapped; NULL:
+ *               sequence b has page b alone (max_pages = 1, n_phys >= n_seq)
+ *   out         [n_seq * rows_per_seq, n_heads, d_v] bf16; lse [n_seq * rows_per_seq, n_heads] fp32 or NULL
+ *   workspace   >= lsa_decode_attn_workspace_size(...) bytes, 256-byte aligned
+ * The same call gives the same bits; the same sequence in another batch agrees within rounding.
+ */
+lsa_status lsa_decode_attn(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq, const void* q,
+                           const void* k_cache, const float* k_scale, const void* v_cache,
+                           const float* v_scale, const int32_t* ctx_len, const int32_t* page_table,
+                           int32_t max_pages, int32_t kv_page_size, int64_t n_phys, void* out, float* lse,
+                           void* workspace, size_t ws_bytes, void* stream);
+
 /* Human-readable name of a status code (static string). */
 const char* lsa_status_string(int32_t status);
 

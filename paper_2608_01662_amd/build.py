@@ -14,7 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "liblsa.so")
-SOURCES = ["indexer.hip", "attention.hip", "lsa_api.cpp"]
+SOURCES = ["indexer.hip", "attention.hip", "append.hip", "decode_attn.hip", "lsa_api.cpp", "serve_api.cpp"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [

@@ -1,0 +1,190 @@
+// Cache append with position rotation (lsa_cache_append) for gfx950: queries and keys rotated, keys and
+// values written to their rows of a paged cache in bf16 or e4m3 with a scale per row.
+//
+// A thread takes 16 values of one head of one token: eight pairs of the rotated part (both halves of each
+// pair, so that every input is loaded once), or 16 neighbours elsewhere. Nothing is shared between threads
+// but the maximum of an fp8 row, an exchange within the lanes that hold the row.
+#include "device.hpp"
+#include "launch.hpp"
+
+namespace lsa {
+
+constexpr int kAppendThreads = 256;
+
+// What a token is: its sequence and position (pos < 0: none), and the page offset of its row.
+struct AppendToken {
+  int seq, pos;
+};
+__device__ __forceinline__ AppendToken append_token(const AppendGeom& g, int64_t t) {
+  AppendToken r;
+  r.seq = g.seq ? g.seq[t] : (int)(t / g.rows_per_seq);
+  if (r.seq < 0 || r.seq >= g.n_seq) return AppendToken{0, -1};
+  const int64_t p = g.pos ? g.pos[t] : (int64_t)g.ctx_len[r.seq] - g.rows_per_seq + (int)(t - (int64_t)r.seq * g.rows_per_seq);
+  const bool ok = p >= 0 && p < (int64_t)g.max_pages * g.P && (g.rot_dim == 0 || p < g.rope_rows);
+  r.pos = ok ? (int)p : -1;
+  return r;
+}
+// Physical page of a token, -1 when it has none.
+__device__ __forceinline__ int64_t append_page(const AppendGeom& g, const AppendToken& t) {
+  if (t.pos < 0) return -1;
+  const int64_t ph = g.page_table ? g.page_table[(int64_t)t.seq * g.max_pages + t.pos / g.P] : t.seq;
+  return ph >= 0 && ph < g.n_phys ? ph : -1;
+}
+
+__device__ __forceinline__ void unpack8(u32x4 v, float* x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(v[i] << 16);
+    x[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ u32x4 pack8(const float* x) {
+  return u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+}
+
+// The 16 values of unit u of a head: dims `lo` .. + 7 and `hi` .. + 7.
+struct Unit {
+  int lo, hi, pair;  // pair: first pair of the rotated part, -1 outside it
+};
+__device__ __forceinline__ Unit unit_of(const AppendGeom& g, int u) {
+  const int c = u - g.rot_start / 16;
+  if (c < 0 || c >= g.rot_dim / 16) return Unit{16 * u, 16 * u + 8, -1};
+  if (g.interleaved) return Unit{16 * u, 16 * u + 8, 8 * c};
+  return Unit{g.rot_start + 8 * c, g.rot_start + g.rot_dim / 2 + 8 * c, 8 * c};
+}
+
+// x[0..8) and x[8..16): the values at dims lo and hi, rotated where the unit is.
+__device__ __forceinline__ void load_unit(const AppendGeom& g, const uint16_t* x, int64_t stride, const uint16_t* part,
+                                          int64_t part_stride, int64_t t, int head, const Unit& u, int pos, float* y) {
+  const uint16_t* p;
+  int lo = u.lo, hi = u.hi;
+  if (part == nullptr) {
+    p = x + t * stride + (int64_t)head * g.d_k;
+  } else if (u.pair < 0) {
+    p = x + t * stride + (int64_t)head * (g.d_k - g.rot_dim);
+  } else {
+    p = part + t * part_stride + (int64_t)head * g.rot_dim;
+    lo -= g.rot_start;
+    hi -= g.rot_start;
+  }
+  unpack8(*reinterpret_cast<const u32x4*>(p + lo), y);
+  unpack8(*reinterpret_cast<const u32x4*>(p + hi), y + 8);
+  if (u.pair < 0 || pos < 0) return;
+  const f32x4* cs = reinterpret_cast<const f32x4*>(g.rope + (int64_t)pos * g.rot_dim + u.pair);
+  const f32x4* sn = reinterpret_cast<const f32x4*>(g.rope + (int64_t)pos * g.rot_dim + g.rot_dim / 2 + u.pair);
+  const f32x4 c0 = cs[0], c1 = cs[1], s0 = sn[0], s1 = sn[1];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float c = i < 4 ? c0[i & 3] : c1[i & 3], s = i < 4 ? s0[i & 3] : s1[i & 3];
+    const float a = g.interleaved ? y[2 * i] : y[i], b = g.interleaved ? y[2 * i + 1] : y[i + 8];
+    const float ra = a * c - b * s, rb = b * c + a * s;
+    if (g.interleaved) {
+      y[2 * i] = ra;
+      y[2 * i + 1] = rb;
+    } else {
+      y[i] = ra;
+      y[i + 8] = rb;
+    }
+  }
+}
+
+// Eight values as e4m3 codes (round to nearest even; NaN stays NaN; |x| < 464).
+__device__ __forceinline__ u32x2 pack_fp8x8(const float* x) {
+  int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], lo, true);
+  int hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[4], x[5], 0, false);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[6], x[7], hi, true);
+  return u32x2{(uint32_t)lo, (uint32_t)hi};
+}
+
+// Blocks [0, bq) rotate queries, [bq, bq + bk) append keys, the rest values. A head's units are dealt to
+// `lanes` neighbouring threads: as many as it has, or for fp8 rows the next power of two, so that the lanes
+// of a row exchange their maximum within one wave.
+__global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendGeom g, int64_t bq, int64_t bk, int k_lanes, int v_lanes) {
+  const int64_t blk = blockIdx.x;
+  if (blk < bq) {
+    const int units = g.d_k / 16;
+    const int64_t item = blk * kAppendThreads + threadIdx.x, vec = item / units;
+    if (vec >= g.n_tok * g.H) return;
+    const int64_t t = vec / g.H;
+    const AppendToken tok = append_token(g, t);
+    const Unit u = unit_of(g, (int)(item - vec * units));
+    float y[16];
+    load_unit(g, g.q, g.q_stride, g.q_rot, g.q_rot_stride, t, (int)(vec - t * g.H), u, tok.pos, y);
+    if (tok.pos < 0) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) y[i] = 0.f;
+    }
+    uint16_t* o = g.q_out + vec * g.d_k;
+    *reinterpret_cast<u32x4*>(o + u.lo) = pack8(y);
+    *reinterpret_cast<u32x4*>(o + u.hi) = pack8(y + 8);
+    return;
+  }
+  const bool key = blk < bq + bk;
+  const int lanes = key ? k_lanes : v_lanes, d = key ? g.d_k : g.d_v, units = d / 16;
+  const int64_t item = (key ? blk - bq : blk - bq - bk) * kAppendThreads + threadIdx.x;
+  const int64_t vec = item / lanes;
+  if (vec >= g.n_tok * g.Hkv) return;  // (whole groups of lanes leave)
+  const int64_t t = vec / g.Hkv;
+  const int head = (int)(vec - t * g.Hkv), ui = (int)(item - vec * lanes);
+  const AppendToken tok = append_token(g, t);
+  const int64_t page = append_page(g, tok);
+  const int off = tok.pos < 0 ? 0 : tok.pos % g.P;
+  if (key && head == 0 && ui == 0 && g.rows) g.rows[t] = page < 0 ? -1 : page * g.P + off;
+  float y[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) y[i] = 0.f;
+  Unit u{16 * ui, 16 * ui + 8, -1};
+  if (ui < units) {
+    if (key) {
+      u = unit_of(g, ui);
+      load_unit(g, g.k, g.k_stride, g.k_rot, g.k_rot_stride, t, head, u, tok.pos, y);
+    } else {
+      const uint16_t* p = g.v + t * g.v_stride + (int64_t)head * d;
+      unpack8(*reinterpret_cast<const u32x4*>(p + u.lo), y);
+      unpack8(*reinterpret_cast<const u32x4*>(p + u.hi), y + 8);
+    }
+  }
+  const int64_t row = (page * g.Hkv + head) * g.P + off;
+  if (!g.fp8) {
+    if (page < 0 || ui >= units) return;
+    uint16_t* o = static_cast<uint16_t*>(key ? g.k_cache : g.v_cache) + row * d;
+    *reinterpret_cast<u32x4*>(o + u.lo) = pack8(y);
+    *reinterpret_cast<u32x4*>(o + u.hi) = pack8(y + 8);
+    return;
+  }
+  // the row's largest magnitude, on the bits, so that a NaN or infinity counts
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(y[i]) & 0x7FFFFFFFu);
+  for (int o = 1; o < lanes; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+  float scale = __uint_as_float(top) / 448.f;
+  scale = top == 0 ? 1.f : scale < 1.17549435e-38f ? 1.17549435e-38f : scale;
+  if (page < 0) return;
+  float* sc = key ? g.k_scale : g.v_scale;
+  if (ui == 0) sc[row] = scale;
+  if (ui >= units) return;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) y[i] = y[i] / scale;
+  uint8_t* o = static_cast<uint8_t*>(key ? g.k_cache : g.v_cache) + row * d;
+  *reinterpret_cast<u32x2*>(o + u.lo) = pack_fp8x8(y);
+  *reinterpret_cast<u32x2*>(o + u.hi) = pack_fp8x8(y + 8);
+}
+
+static int append_lanes(int units, bool fp8) {
+  if (!fp8) return units;
+  int l = 1;
+  while (l < units) l *= 2;
+  return l;
+}
+
+hipError_t launch_append(const AppendGeom& g, hipStream_t st) {
+  const int k_lanes = append_lanes(g.d_k / 16, g.fp8), v_lanes = g.d_v ? append_lanes(g.d_v / 16, g.fp8) : 1;
+  auto blocks = [](int64_t items) { return (items + kAppendThreads - 1) / kAppendThreads; };
+  const int64_t bq = blocks(g.n_tok * g.H * (g.d_k / 16)), bk = blocks(g.n_tok * g.Hkv * k_lanes);
+  const int64_t bv = g.d_v ? blocks(g.n_tok * g.Hkv * v_lanes) : 0;
+  hipLaunchKernelGGL(append_kernel, dim3((unsigned)(bq + bk + bv)), dim3(kAppendThreads), 0, st, g, bq, bk, k_lanes, v_lanes);
+  return hipGetLastError();
+}
+
+}  // namespace lsa

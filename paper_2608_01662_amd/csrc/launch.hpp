@@ -98,4 +98,50 @@ hipError_t launch_mla_attn(const AttnGeom& a, hipStream_t st);
 hipError_t launch_mqa_attn(const AttnGeom& a, hipStream_t st);
 hipError_t launch_attn_combine(const AttnGeom& a, hipStream_t st);  // MLA: 64 heads x 512
 
+// Exact division of 0 <= n < 2^31 by d >= 1: n / d = (n * mul) >> shift with mul = floor(2^shift / d) + 1,
+// shift = 31 + ceil(log2 d), so that the error n (mul d - 2^shift) / (d 2^shift) stays below 1 / d.
+struct FastDiv {
+  uint32_t d, shift;
+  uint64_t mul;
+};
+inline FastDiv fast_div(uint32_t d) {
+  uint32_t l = 0;
+  while (l < 32 && (uint64_t(1) << l) < d) ++l;
+  const uint32_t shift = 31 + l;
+  return FastDiv{d, shift, (uint64_t(1) << shift) / d + 1};
+}
+
+// One cache append (lsa_append_tensors, checked).
+struct AppendGeom {
+  const uint16_t *q, *q_rot, *k, *k_rot, *v;
+  int64_t q_stride, q_rot_stride, k_stride, k_rot_stride, v_stride;
+  const float* rope;
+  int64_t rope_rows;
+  const int32_t *seq, *pos, *ctx_len, *page_table;
+  uint16_t* q_out;
+  void *k_cache, *v_cache;
+  float *k_scale, *v_scale;
+  int64_t* rows;
+  int64_t n_tok, n_phys;
+  int H, Hkv, d_k, d_v, rot_start, rot_dim, interleaved, fp8;
+  int n_seq, rows_per_seq, max_pages, P;
+};
+hipError_t launch_append(const AppendGeom& g, hipStream_t st);
+
+// One call of the attention over the whole cache (lsa_decode_attn, checked).
+struct DecodeGeom {
+  const uint16_t* q;  // [n_seq * R, H, d_qk]
+  const void *k, *v;  // [n_phys, Hkv, P, d]; v unused with a latent cache
+  const float *k_scale, *v_scale;
+  const int32_t *ctx_len, *page_table;
+  uint16_t* out;
+  float* lse;  // or nullptr
+  int64_t n_phys;
+  int n_seq, R, H, Hkv, d_qk, d_v, latent, fp8;
+  int max_pages, P;
+  int k_sink, k_swa;
+  float scale_log2;  // sm_scale * log2(e)
+};
+hipError_t launch_decode_attn(const DecodeGeom& g, hipStream_t st);
+
 }  // namespace lsa

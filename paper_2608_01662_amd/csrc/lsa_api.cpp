@@ -1,43 +1,26 @@
 // C-ABI front end of the LSA library: argument checks (host only, before any HIP call),
 // workspace layout, kernel selection and error reporting. See include/lsa.h.
-#include "../../include/lsa.h"
+#include "api_common.hpp"
 
-#include <hip/hip_runtime.h>
-
-#include <cstdarg>
-#include <cstdio>
 #include <cstring>
 #include <mutex>
 
 #include "launch.hpp"
 
+thread_local char lsa::g_err[512] = "";
+
+using lsa::aligned;
+using lsa::cdiv;
+using lsa::fail;
+using lsa::g_err;
+using lsa::hip_fail;
+using lsa::pow2;
+using lsa::round_up;
+
 namespace {
 
-thread_local char g_err[512] = "";
 constexpr size_t kMaxLds = 160 * 1024;        // gfx950 LDS per workgroup
 constexpr size_t kSelectStaticLds = 8 * 1024;  // static LDS of the page selection (upper bound)
-
-lsa_status fail(lsa_status st, const char* fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_err, sizeof(g_err), fmt, ap);
-  va_end(ap);
-  return st;
-}
-
-lsa_status hip_fail(hipError_t e, const char* where) {
-  return fail(LSA_ERR_HIP, "%s: %s", where, hipGetErrorString(e));
-}
-
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-bool pow2(int64_t x) { return x > 0 && (x & (x - 1)) == 0; }
-size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-#define LSA_REQUIRE(cond, st, ...) \
-  do {                             \
-    if (!(cond)) return fail(st, __VA_ARGS__); \
-  } while (0)
 
 lsa_status check_index_params(const lsa_index_params* p) {
   LSA_REQUIRE(p != nullptr, LSA_ERR_INVALID_ARG, "params is NULL");

@@ -1,0 +1,237 @@
+// C-ABI front end of the serving operators: the cache append and the attention of new tokens over the
+// whole cache. Argument checks (host only, before any HIP call) and launches. See include/lsa.h.
+#include "api_common.hpp"
+#include "launch.hpp"
+
+using lsa::aligned;
+using lsa::cdiv;
+using lsa::fail;
+using lsa::g_err;
+using lsa::hip_fail;
+
+namespace {
+
+lsa_status check_append_params(const lsa_append_params* p) {
+  LSA_REQUIRE(p != nullptr, LSA_ERR_INVALID_ARG, "params is NULL");
+  LSA_REQUIRE(p->n_heads >= 0 && p->n_heads <= 4096, LSA_ERR_INVALID_ARG, "n_heads=%d not in [0, 4096]", p->n_heads);
+  LSA_REQUIRE(p->n_kv_heads >= 1 && p->n_kv_heads <= 4096, LSA_ERR_INVALID_ARG, "n_kv_heads=%d not in [1, 4096]",
+              p->n_kv_heads);
+  LSA_REQUIRE(p->d_k >= 16 && p->d_k <= 1024 && p->d_k % 16 == 0, LSA_ERR_UNSUPPORTED,
+              "d_k=%d must be a multiple of 16 in [16, 1024]", p->d_k);
+  LSA_REQUIRE(p->d_v >= 0 && p->d_v <= 1024 && p->d_v % 16 == 0, LSA_ERR_UNSUPPORTED,
+              "d_v=%d must be a multiple of 16 in [0, 1024]", p->d_v);
+  LSA_REQUIRE(p->rot_start >= 0 && p->rot_dim >= 0 && p->rot_start <= p->d_k && p->rot_dim <= p->d_k - p->rot_start,
+              LSA_ERR_INVALID_ARG, "rotated dims [%d, +%d) exceed d_k=%d", p->rot_start, p->rot_dim, p->d_k);
+  LSA_REQUIRE(p->rot_start % 16 == 0 && p->rot_dim % 16 == 0, LSA_ERR_UNSUPPORTED,
+              "rot_start=%d and rot_dim=%d must be multiples of 16", p->rot_start, p->rot_dim);
+  LSA_REQUIRE(p->interleaved == 0 || p->interleaved == 1, LSA_ERR_INVALID_ARG, "interleaved=%d must be 0 or 1",
+              p->interleaved);
+  LSA_REQUIRE(p->key_dtype == LSA_KEY_BF16 || p->key_dtype == LSA_KEY_FP8_E4M3FN, LSA_ERR_INVALID_ARG,
+              "key_dtype=%d unknown", p->key_dtype);
+  return LSA_OK;
+}
+
+// An input [n_tok, heads, width] whose tokens lie `stride` elements apart.
+lsa_status check_tokens(const char* name, const void* x, int64_t stride, int64_t heads, int64_t width) {
+  LSA_REQUIRE(x != nullptr, LSA_ERR_INVALID_ARG, "%s is NULL", name);
+  LSA_REQUIRE(aligned(x, 16) && stride % 8 == 0, LSA_ERR_INVALID_ARG,
+              "%s must be 16-byte aligned and its stride (%lld) a multiple of 8", name, (long long)stride);
+  LSA_REQUIRE(stride >= heads * width, LSA_ERR_INVALID_ARG, "%s: a stride of %lld is less than a token's %lld elements",
+              name, (long long)stride, (long long)(heads * width));
+  return LSA_OK;
+}
+
+lsa_status check_decode_params(const lsa_decode_attn_params* p) {
+  LSA_REQUIRE(p != nullptr, LSA_ERR_INVALID_ARG, "params is NULL");
+  LSA_REQUIRE(p->latent == 0 || p->latent == 1, LSA_ERR_INVALID_ARG, "latent=%d must be 0 or 1", p->latent);
+  LSA_REQUIRE(p->n_heads >= 1 && p->n_heads <= 1024 && p->n_kv_heads >= 1 && p->n_heads % p->n_kv_heads == 0,
+              LSA_ERR_INVALID_ARG, "n_heads=%d must be a multiple of n_kv_heads=%d and at most 1024", p->n_heads,
+              p->n_kv_heads);
+  LSA_REQUIRE(p->key_dtype == LSA_KEY_BF16 || p->key_dtype == LSA_KEY_FP8_E4M3FN, LSA_ERR_INVALID_ARG,
+              "key_dtype=%d unknown", p->key_dtype);
+  const bool mla = p->latent == 1 && p->n_kv_heads == 1 && p->d_qk == 576 && p->d_v == 512 && p->key_dtype == LSA_KEY_BF16;
+  const bool gqa = p->latent == 0 && (p->d_qk == 64 || p->d_qk == 128) && p->d_v == p->d_qk;
+  LSA_REQUIRE(mla || gqa, LSA_ERR_UNSUPPORTED,
+              "attention shape (n_kv_heads=%d, d_qk=%d, d_v=%d, latent=%d, key_dtype=%d) not supported; use widths "
+              "(64,64) or (128,128), or a bf16 latent cache of (576,512) with one head",
+              p->n_kv_heads, p->d_qk, p->d_v, p->latent, p->key_dtype);
+  LSA_REQUIRE(p->k_sink >= 0 && p->k_swa >= 0, LSA_ERR_INVALID_ARG, "k_sink=%d / k_swa=%d must be >= 0", p->k_sink,
+              p->k_swa);
+  LSA_REQUIRE(p->sm_scale > 0.f && p->sm_scale < 1e30f, LSA_ERR_INVALID_ARG, "sm_scale must be positive and finite");
+  return LSA_OK;
+}
+
+lsa_status check_decode_sizes(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq, int32_t max_pages,
+                              int32_t kv_page_size) {
+  LSA_REQUIRE(n_seq >= 0, LSA_ERR_INVALID_ARG, "n_seq=%d < 0", n_seq);
+  LSA_REQUIRE(rows_per_seq >= 1 && max_pages >= 1 && kv_page_size >= 1, LSA_ERR_INVALID_ARG,
+              "rows_per_seq, max_pages and kv_page_size must be >= 1");
+  LSA_REQUIRE((int64_t)max_pages * kv_page_size < (1LL << 31), LSA_ERR_UNSUPPORTED, "positions must fit in int32");
+  LSA_REQUIRE(rows_per_seq <= 1024 && (int64_t)n_seq * rows_per_seq * p->n_heads < (1LL << 30), LSA_ERR_UNSUPPORTED,
+              "rows_per_seq must be <= 1024 and the call have < 2^30 rows of all heads");
+  return LSA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+lsa_status lsa_cache_append(const lsa_append_params* p, const lsa_append_tensors* t, int64_t n_tok, int32_t n_seq,
+                            int32_t rows_per_seq, int32_t max_pages, int32_t kv_page_size, int64_t n_phys,
+                            void* stream) {
+  g_err[0] = 0;
+  lsa_status s = check_append_params(p);
+  if (s != LSA_OK) return s;
+  LSA_REQUIRE(t != nullptr, LSA_ERR_INVALID_ARG, "tensors is NULL");
+  LSA_REQUIRE(n_tok >= 0 && n_seq >= 0, LSA_ERR_INVALID_ARG, "n_tok=%lld / n_seq=%d < 0", (long long)n_tok, n_seq);
+  if (n_tok == 0) return LSA_OK;  // nothing to read or write
+  LSA_REQUIRE(n_tok < (1LL << 28), LSA_ERR_UNSUPPORTED, "n_tok must be < 2^28 per call");
+  LSA_REQUIRE(n_seq >= 1 && rows_per_seq >= 1 && max_pages >= 1 && kv_page_size >= 1 && n_phys >= 1,
+              LSA_ERR_INVALID_ARG, "n_seq, rows_per_seq, max_pages, kv_page_size and n_phys must be >= 1");
+  LSA_REQUIRE((int64_t)max_pages * kv_page_size < (1LL << 31), LSA_ERR_UNSUPPORTED, "positions must fit in int32");
+  LSA_REQUIRE(n_phys < (1LL << 31) && n_phys * kv_page_size < (1LL << 31) / p->n_kv_heads, LSA_ERR_UNSUPPORTED,
+              "n_phys * kv_page_size * n_kv_heads must be < 2^31");
+  LSA_REQUIRE(t->page_table != nullptr || (max_pages == 1 && n_phys >= n_seq), LSA_ERR_INVALID_ARG,
+              "without a page table each sequence has one page: max_pages must be 1 and n_phys >= n_seq");
+  LSA_REQUIRE((t->pos != nullptr) != (t->ctx_len != nullptr), LSA_ERR_INVALID_ARG,
+              "exactly one of pos and ctx_len must be given");
+  LSA_REQUIRE(t->pos != nullptr || (t->seq == nullptr && n_tok == (int64_t)n_seq * rows_per_seq), LSA_ERR_INVALID_ARG,
+              "with ctx_len the tokens are rows_per_seq of every sequence: n_tok must be n_seq * rows_per_seq, seq NULL");
+  const bool fp8 = p->key_dtype == LSA_KEY_FP8_E4M3FN, rot = p->rot_dim > 0;
+  LSA_REQUIRE(rot == (t->rope != nullptr) && t->rope_rows >= 0, LSA_ERR_INVALID_ARG,
+              "rope must be given exactly when rot_dim > 0, rope_rows must be >= 0");
+  LSA_REQUIRE((t->k_rot == nullptr && t->q_rot == nullptr) || (rot && p->rot_start > 0 && p->rot_start + p->rot_dim == p->d_k),
+              LSA_ERR_INVALID_ARG, "k_rot / q_rot need a rotation of the last rot_dim dims, fewer than d_k");
+  LSA_REQUIRE((t->q != nullptr) == (p->n_heads > 0) && (t->q_out != nullptr) == (p->n_heads > 0) &&
+                  (t->q_rot == nullptr || p->n_heads > 0),
+              LSA_ERR_INVALID_ARG, "q and q_out must be given exactly when n_heads > 0, q_rot only then");
+  LSA_REQUIRE((t->v != nullptr) == (p->d_v > 0) && (t->v_cache != nullptr) == (p->d_v > 0), LSA_ERR_INVALID_ARG,
+              "v and v_cache must be given exactly when d_v > 0");
+  LSA_REQUIRE(t->k_cache != nullptr, LSA_ERR_INVALID_ARG, "k_cache is NULL");
+  LSA_REQUIRE((t->k_scale != nullptr) == fp8 && (t->v_scale != nullptr) == (fp8 && p->d_v > 0), LSA_ERR_INVALID_ARG,
+              "k_scale / v_scale must be given exactly for fp8 caches");
+  const int64_t k_width = t->k_rot ? p->d_k - p->rot_dim : p->d_k, q_width = t->q_rot ? p->d_k - p->rot_dim : p->d_k;
+  s = check_tokens("k", t->k, t->k_stride, p->n_kv_heads, k_width);
+  if (s == LSA_OK && t->k_rot) s = check_tokens("k_rot", t->k_rot, t->k_rot_stride, p->n_kv_heads, p->rot_dim);
+  if (s == LSA_OK && t->v) s = check_tokens("v", t->v, t->v_stride, p->n_kv_heads, p->d_v);
+  if (s == LSA_OK && t->q) s = check_tokens("q", t->q, t->q_stride, p->n_heads, q_width);
+  if (s == LSA_OK && t->q_rot) s = check_tokens("q_rot", t->q_rot, t->q_rot_stride, p->n_heads, p->rot_dim);
+  if (s != LSA_OK) return s;
+  LSA_REQUIRE(t->q == nullptr || t->q_out != t->q || (t->q_rot == nullptr && t->q_stride == (int64_t)p->n_heads * p->d_k),
+              LSA_ERR_INVALID_ARG, "q_out may be q only when q is contiguous and whole");
+  LSA_REQUIRE(aligned(t->q_out, 16) && aligned(t->k_cache, 16) && aligned(t->v_cache, 16) && aligned(t->rope, 16),
+              LSA_ERR_INVALID_ARG, "q_out, k_cache, v_cache and rope must be 16-byte aligned");
+  LSA_REQUIRE(aligned(t->seq, 4) && aligned(t->pos, 4) && aligned(t->ctx_len, 4) && aligned(t->page_table, 4) &&
+                  aligned(t->k_scale, 4) && aligned(t->v_scale, 4) && aligned(t->rows, 8),
+              LSA_ERR_INVALID_ARG, "seq, pos, ctx_len, page_table and scales must be 4-byte aligned, rows 8-byte");
+  // a thread per 16 values, in one launch
+  const int64_t threads = n_tok * ((int64_t)p->n_heads * (p->d_k / 16) + (int64_t)p->n_kv_heads * 128);
+  LSA_REQUIRE(threads < (1LL << 38), LSA_ERR_UNSUPPORTED, "the call is too large; append in parts");
+
+  lsa::AppendGeom g{};
+  g.q = static_cast<const uint16_t*>(t->q);
+  g.q_rot = static_cast<const uint16_t*>(t->q_rot);
+  g.k = static_cast<const uint16_t*>(t->k);
+  g.k_rot = static_cast<const uint16_t*>(t->k_rot);
+  g.v = static_cast<const uint16_t*>(t->v);
+  g.q_stride = t->q_stride;
+  g.q_rot_stride = t->q_rot_stride;
+  g.k_stride = t->k_stride;
+  g.k_rot_stride = t->k_rot_stride;
+  g.v_stride = t->v_stride;
+  g.rope = t->rope;
+  g.rope_rows = t->rope_rows;
+  g.seq = t->seq;
+  g.pos = t->pos;
+  g.ctx_len = t->ctx_len;
+  g.page_table = t->page_table;
+  g.q_out = static_cast<uint16_t*>(t->q_out);
+  g.k_cache = t->k_cache;
+  g.v_cache = t->v_cache;
+  g.k_scale = t->k_scale;
+  g.v_scale = t->v_scale;
+  g.rows = t->rows;
+  g.n_tok = n_tok;
+  g.n_phys = n_phys;
+  g.H = p->n_heads;
+  g.Hkv = p->n_kv_heads;
+  g.d_k = p->d_k;
+  g.d_v = p->d_v;
+  g.rot_start = p->rot_start;
+  g.rot_dim = p->rot_dim;
+  g.interleaved = p->interleaved;
+  g.fp8 = fp8;
+  g.n_seq = n_seq;
+  g.rows_per_seq = rows_per_seq;
+  g.max_pages = max_pages;
+  g.P = kv_page_size;
+  const hipError_t e = lsa::launch_append(g, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "cache append");
+  return LSA_OK;
+}
+
+size_t lsa_decode_attn_workspace_size(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq,
+                                      int32_t max_pages, int32_t kv_page_size) {
+  if (check_decode_params(p) != LSA_OK || check_decode_sizes(p, n_seq, rows_per_seq, max_pages, kv_page_size) != LSA_OK) return 0;
+  return 0;
+}
+
+lsa_status lsa_decode_attn(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq, const void* q,
+                           const void* k_cache, const float* k_scale, const void* v_cache, const float* v_scale,
+                           const int32_t* ctx_len, const int32_t* page_table, int32_t max_pages, int32_t kv_page_size,
+                           int64_t n_phys, void* out, float* lse, void* workspace, size_t ws_bytes, void* stream) {
+  g_err[0] = 0;
+  lsa_status s = check_decode_params(p);
+  if (s != LSA_OK) return s;
+  s = check_decode_sizes(p, n_seq, rows_per_seq, max_pages, kv_page_size);
+  if (s != LSA_OK) return s;
+  if (n_seq == 0) return LSA_OK;  // nothing to read or write
+  LSA_REQUIRE(n_phys >= 1 && n_phys < (1LL << 31) && n_phys * kv_page_size < (1LL << 31) / p->n_kv_heads,
+              LSA_ERR_UNSUPPORTED, "n_phys must be >= 1 and n_phys * kv_page_size * n_kv_heads < 2^31");
+  LSA_REQUIRE(page_table != nullptr || (max_pages == 1 && n_phys >= n_seq), LSA_ERR_INVALID_ARG,
+              "without a page table each sequence has one page: max_pages must be 1 and n_phys >= n_seq");
+  const bool fp8 = p->key_dtype == LSA_KEY_FP8_E4M3FN, latent = p->latent != 0;
+  LSA_REQUIRE(q && k_cache && ctx_len && out, LSA_ERR_INVALID_ARG, "q, k_cache, ctx_len and out must be non-NULL");
+  LSA_REQUIRE(latent == (v_cache == nullptr), LSA_ERR_INVALID_ARG,
+              latent ? "v_cache must be NULL for a latent cache" : "v_cache is NULL");
+  LSA_REQUIRE(fp8 == (k_scale != nullptr) && fp8 == (v_scale != nullptr), LSA_ERR_INVALID_ARG,
+              "k_scale and v_scale must be given exactly for fp8 caches");
+  LSA_REQUIRE(aligned(q, 16) && aligned(k_cache, 16) && aligned(v_cache, 16) && aligned(out, 16), LSA_ERR_INVALID_ARG,
+              "q, k_cache, v_cache and out must be 16-byte aligned");
+  LSA_REQUIRE(aligned(k_scale, 4) && aligned(v_scale, 4) && aligned(ctx_len, 4) && aligned(page_table, 4) && aligned(lse, 4),
+              LSA_ERR_INVALID_ARG, "scales, ctx_len, page_table and lse must be 4-byte aligned");
+  const size_t need = lsa_decode_attn_workspace_size(p, n_seq, rows_per_seq, max_pages, kv_page_size);
+  LSA_REQUIRE(need == 0 || (workspace != nullptr && aligned(workspace, 256)), LSA_ERR_WORKSPACE,
+              "workspace must be non-NULL and 256-byte aligned");
+  LSA_REQUIRE(ws_bytes >= need, LSA_ERR_WORKSPACE, "workspace of %zu bytes < %zu needed", ws_bytes, need);
+  lsa::DecodeGeom g{};
+  g.q = static_cast<const uint16_t*>(q);
+  g.k = k_cache;
+  g.v = v_cache;
+  g.k_scale = k_scale;
+  g.v_scale = v_scale;
+  g.ctx_len = ctx_len;
+  g.page_table = page_table;
+  g.out = static_cast<uint16_t*>(out);
+  g.lse = lse;
+  g.n_phys = n_phys;
+  g.n_seq = n_seq;
+  g.R = rows_per_seq;
+  g.H = p->n_heads;
+  g.Hkv = p->n_kv_heads;
+  g.d_qk = p->d_qk;
+  g.d_v = p->d_v;
+  g.latent = latent;
+  g.fp8 = fp8;
+  g.max_pages = max_pages;
+  g.P = kv_page_size;
+  // (without a window there is no separate sink)
+  g.k_swa = p->k_swa;
+  g.k_sink = p->k_swa > 0 ? p->k_sink : 0;
+  g.scale_log2 = p->sm_scale * 1.4426950408889634f;
+  const hipError_t e = lsa::launch_decode_attn(g, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "decode attention");
+  return LSA_OK;
+}
+
+}  // extern "C"

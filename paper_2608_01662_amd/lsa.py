@@ -37,6 +37,25 @@ class _AttnParams(ctypes.Structure):
                 ("latent", ctypes.c_int32), ("sm_scale", ctypes.c_float)]
 
 
+class _AppendParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "n_heads", "n_kv_heads", "d_k", "d_v", "rot_start", "rot_dim", "interleaved", "key_dtype")]
+
+
+class _AppendTensors(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "q_rot", "k", "k_rot", "v")] + \
+               [(n, ctypes.c_int64) for n in ("q_stride", "q_rot_stride", "k_stride", "k_rot_stride", "v_stride")] + \
+               [("rope", ctypes.c_void_p), ("rope_rows", ctypes.c_int64)] + \
+               [(n, ctypes.c_void_p) for n in ("seq", "pos", "ctx_len", "page_table", "q_out", "k_cache", "k_scale",
+                                               "v_cache", "v_scale", "rows")]
+
+
+class _DecodeAttnParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "n_heads", "n_kv_heads", "d_qk", "d_v", "latent", "key_dtype", "k_sink", "k_swa")] + \
+               [("sm_scale", ctypes.c_float)]
+
+
 @dataclass(frozen=True)
 class IndexParams:
     """Indexer hyper-parameters (Sec. 3.1 and 3.3 of the paper); see lsa_index_params."""
@@ -78,6 +97,42 @@ class AttnParams:
 
     def c(self) -> _AttnParams:
         return _AttnParams(self.n_heads, self.d_qk, self.d_v, int(self.latent), self.sm_scale)
+
+
+@dataclass(frozen=True)
+class AppendParams:
+    """What an append to a paged cache rotates and writes; see lsa_append_params."""
+    n_heads: int             # query heads rotated in the same call; 0: none
+    n_kv_heads: int
+    d_k: int
+    d_v: int = 0             # 0: no values (latent cache, indexer keys)
+    rot_start: int = 0
+    rot_dim: int = 0         # 0: no rotation
+    interleaved: bool = False
+    fp8: bool = False
+
+    def c(self) -> _AppendParams:
+        return _AppendParams(self.n_heads, self.n_kv_heads, self.d_k, self.d_v, self.rot_start, self.rot_dim,
+                             int(self.interleaved), LSA_KEY_FP8_E4M3FN if self.fp8 else LSA_KEY_BF16)
+
+
+@dataclass(frozen=True)
+class DecodeAttnParams:
+    """Attention of new tokens over a whole paged cache; see lsa_decode_attn_params."""
+    n_heads: int
+    n_kv_heads: int
+    d_qk: int
+    d_v: int
+    latent: bool
+    sm_scale: float
+    fp8: bool = False
+    k_sink: int = 0          # with k_swa > 0: the first positions are attended as well
+    k_swa: int = 0           # 0: every position up to the query's; else the last k_swa
+
+    def c(self) -> _DecodeAttnParams:
+        return _DecodeAttnParams(self.n_heads, self.n_kv_heads, self.d_qk, self.d_v, int(self.latent),
+                                 LSA_KEY_FP8_E4M3FN if self.fp8 else LSA_KEY_BF16, self.k_sink, self.k_swa,
+                                 self.sm_scale)
 
 
 MLA = dict(n_heads=64, d_qk=576, d_v=512, latent=True)
@@ -129,6 +184,15 @@ def lib() -> ctypes.CDLL:
         L.lsa_hfa_attn_workspace_size.restype = _sz
         L.lsa_hfa_attn.argtypes = [A, _i64, _vp, _vp, _i64, _vp, _vp, _i32, _i64, _i32, _vp, _vp, _vp, _sz, _vp]
         L.lsa_hfa_attn.restype = _i32
+        D = ctypes.POINTER(_DecodeAttnParams)
+        L.lsa_cache_append.argtypes = [ctypes.POINTER(_AppendParams), ctypes.POINTER(_AppendTensors), _i64, _i32, _i32,
+                                       _i32, _i32, _i64, _vp]
+        L.lsa_cache_append.restype = _i32
+        L.lsa_decode_attn_workspace_size.argtypes = [D, _i32, _i32, _i32, _i32]
+        L.lsa_decode_attn_workspace_size.restype = _sz
+        L.lsa_decode_attn.argtypes = [D, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i64, _vp, _vp, _vp,
+                                      _sz, _vp]
+        L.lsa_decode_attn.restype = _i32
         L.lsa_status_string.argtypes = [_i32]
         L.lsa_status_string.restype = ctypes.c_char_p
         L.lsa_last_error.argtypes = []
@@ -479,6 +543,184 @@ def hfa_attn(prm: AttnParams, q: torch.Tensor, kv: torch.Tensor, idx: torch.Tens
     ws, wsb = _workspace(hfa_workspace_size(prm, n_rows), q.device, workspace)
     _check(lib().lsa_hfa_attn(_ref(prm), n_rows, _p(q), _p(kv), n_kv_rows, _p(idx), _p(count), k_cap,
                               q_start, k_swa, _p(out), _p(lse), _p(ws), wsb, _stream(q.device)), "lsa_hfa_attn")
+    return out, lse
+
+
+# ---------------------------------------------------------------- serving: appends and dense decode
+def _tokens(name: str, t, n_tok, heads: int, width: int, device):
+    """A bf16 tensor [n_tok, heads, width] whose tokens may lie any stride apart (a slice of a fused
+    projection), their heads one after the other. Returns that stride in elements."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a torch tensor")
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{name} must be a CUDA tensor on {device or 'a GPU'} (got {t.device})")
+    if t.dtype != torch.bfloat16:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {torch.bfloat16}")
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != width or (n_tok is not None and shape[0] != n_tok):
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected {('*' if n_tok is None else n_tok, heads, width)}")
+    s0, s1, s2 = t.stride()
+    if (s2 != 1 and width > 1) or (s1 != width and heads > 1):
+        raise ValueError(f"{name}: the heads of a token must be contiguous (strides {t.stride()})")
+    return s0 if shape[0] > 1 else heads * width
+
+
+def _paged_cache(name: str, t, fp8: bool, heads: int, width: int, device, like=None):
+    """A cache [n_phys, heads, page, width], or without the head dimension when there is one head. Returns
+    (n_phys, page); `like`: the (n_phys, page) it must have."""
+    if isinstance(t, torch.Tensor) and t.dtype == torch.float8_e4m3fn:
+        t = t.view(torch.uint8)
+    if heads == 1 and isinstance(t, torch.Tensor) and t.dim() == 3:
+        _need(name, t, _U8 if fp8 else _BF16, (None, None, width), device)
+        got = (t.shape[0], t.shape[1])
+    else:
+        _need(name, t, _U8 if fp8 else _BF16, (None, heads, None, width), device)
+        got = (t.shape[0], t.shape[2])
+    if like is not None and got != like:
+        raise ValueError(f"{name} has {got[0]} pages of {got[1]} rows, expected {like[0]} of {like[1]}")
+    return got
+
+
+def _cache_scale(name: str, t, fp8: bool, n_phys: int, heads: int, page: int, device):
+    if not fp8:
+        if t is not None:
+            raise ValueError(f"{name} must be None for bf16 caches")
+        return
+    if heads == 1 and isinstance(t, torch.Tensor) and t.dim() == 2:
+        _need(name, t, _F32, (n_phys, page), device)
+    else:
+        _need(name, t, _F32, (n_phys, heads, page), device)
+
+
+def cache_append(prm: AppendParams, k: torch.Tensor, k_cache: torch.Tensor, *, page_table: torch.Tensor | None = None,
+                 ctx_len: torch.Tensor | None = None, pos: torch.Tensor | None = None, seq: torch.Tensor | None = None,
+                 rows_per_seq: int = 1, n_seq: int | None = None, rope: torch.Tensor | None = None,
+                 k_rot: torch.Tensor | None = None, v: torch.Tensor | None = None,
+                 v_cache: torch.Tensor | None = None, k_scale: torch.Tensor | None = None,
+                 v_scale: torch.Tensor | None = None, q: torch.Tensor | None = None,
+                 q_rot: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
+                 rows: torch.Tensor | bool = False):
+    """Rotate new tokens' queries and keys by position and write keys and values to a paged cache
+    (lsa_cache_append). Returns (q_out or None, rows or None).
+
+    The tokens are the last rows_per_seq of every sequence (ctx_len, the new ones counted), or lie at `pos`
+    of sequence `seq` (seq None: token i is of sequence i // rows_per_seq). k, v, q: [n_tok, heads, d] bf16
+    with any token stride; with k_rot / q_rot, their last rot_dim dims apart. Caches [n_phys, heads, page, d]
+    (or [n_phys, page, d] of one head), bf16 or fp8 codes with scales [n_phys, heads, page]. rope:
+    [positions, rot_dim] fp32, cosines then sines. page_table None: sequence b has page b alone. rows: True, or an
+    int64 tensor [n_tok], for the physical cache rows (block_keys_update takes them)."""
+    nk, nq = prm.n_kv_heads, prm.n_heads
+    dev = k.device if isinstance(k, torch.Tensor) else None
+    cut = prm.rot_dim if k_rot is not None else 0
+    ks = _tokens("k", k, None, nk, prm.d_k - cut, dev)
+    n = k.shape[0]
+    krs = _tokens("k_rot", k_rot, n, nk, prm.rot_dim, dev) if k_rot is not None else 0
+    n_phys, page = _paged_cache("k_cache", k_cache, prm.fp8, nk, prm.d_k, dev)
+    _cache_scale("k_scale", k_scale, prm.fp8, n_phys, nk, page, dev)
+    vs = 0
+    if prm.d_v:
+        vs = _tokens("v", v, n, nk, prm.d_v, dev)
+        _paged_cache("v_cache", v_cache, prm.fp8, nk, prm.d_v, dev, (n_phys, page))
+        _cache_scale("v_scale", v_scale, prm.fp8, n_phys, nk, page, dev)
+    elif v is not None or v_cache is not None or v_scale is not None:
+        raise ValueError("v, v_cache and v_scale must be None with d_v = 0")
+    qs = qrs = 0
+    if nq:
+        qs = _tokens("q", q, n, nq, prm.d_k - (prm.rot_dim if q_rot is not None else 0), dev)
+        if q_rot is not None:
+            qrs = _tokens("q_rot", q_rot, n, nq, prm.rot_dim, dev)
+        if q_out is None:
+            q_out = torch.empty((n, nq, prm.d_k), dtype=torch.bfloat16, device=dev)
+        else:
+            _need("q_out", q_out, _BF16, (n, nq, prm.d_k), dev)
+    elif q is not None or q_rot is not None or q_out is not None:
+        raise ValueError("q, q_rot and q_out must be None with n_heads = 0")
+    rope_rows = 0
+    if prm.rot_dim:
+        rope_rows = _need("rope", rope, _F32, (None, prm.rot_dim), dev).shape[0]
+    elif rope is not None:
+        raise ValueError("rope must be None with rot_dim = 0")
+    if (pos is None) == (ctx_len is None):
+        raise ValueError("exactly one of pos and ctx_len must be given")
+    if page_table is not None:
+        _need("page_table", page_table, _I32, (None, None), dev)
+        seqs, max_pages = page_table.shape
+    else:
+        seqs, max_pages = ctx_len.shape[0] if ctx_len is not None else n_phys, 1
+    if n_seq is not None and n_seq != seqs:
+        if page_table is not None or ctx_len is not None or not 0 <= n_seq <= seqs:
+            raise ValueError(f"n_seq is {n_seq}, the page table, ctx_len or cache hold {seqs} sequences")
+        seqs = n_seq
+    if ctx_len is not None:
+        _need("ctx_len", ctx_len, _I32, (seqs,), dev)
+        if seq is not None:
+            raise ValueError("seq must be None with ctx_len")
+        if n != seqs * rows_per_seq:
+            raise ValueError(f"{n} tokens, but {seqs} sequences of rows_per_seq = {rows_per_seq}")
+    else:
+        _need("pos", pos, _I32, (n,), dev)
+        _need_opt("seq", seq, _I32, (n,), dev)
+    if rows is True:
+        rows = torch.empty((n,), dtype=torch.int64, device=dev)
+    elif rows is False or rows is None:
+        rows = None
+    else:
+        _need("rows", rows, _I64, (n,), dev)
+    t = _AppendTensors(_p(q), _p(q_rot), _p(k), _p(k_rot), _p(v), qs, qrs, ks, krs, vs, _p(rope), rope_rows, _p(seq),
+                       _p(pos), _p(ctx_len), _p(page_table), _p(q_out), _p(k_cache), _p(k_scale), _p(v_cache),
+                       _p(v_scale), _p(rows))
+    _check(lib().lsa_cache_append(_ref(prm), ctypes.byref(t), n, seqs, rows_per_seq, max_pages, page, n_phys,
+                                  _stream(dev)), "lsa_cache_append")
+    return q_out, rows
+
+
+def decode_attn_workspace_size(prm: DecodeAttnParams, n_seq: int, rows_per_seq: int, max_pages: int,
+                               kv_page_size: int) -> int:
+    return lib().lsa_decode_attn_workspace_size(_ref(prm), n_seq, rows_per_seq, max_pages, kv_page_size)
+
+
+def decode_attn(prm: DecodeAttnParams, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor | None,
+                ctx_len: torch.Tensor, page_table: torch.Tensor | None = None, rows_per_seq: int = 1,
+                k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None,
+                out: torch.Tensor | None = None, lse: torch.Tensor | bool | None = True,
+                workspace: torch.Tensor | None = None):
+    """Attention of each sequence's rows_per_seq newest tokens over its whole cached context, or the sink and
+    sliding window of prm (lsa_decode_attn). Returns (out [n_seq * rows_per_seq, H, d_v] bf16, lse or None).
+
+    Caches as cache_append writes them; v_cache None with a latent cache. page_table None: sequence b has
+    page b alone."""
+    _need("q", q, _BF16, (None, prm.n_heads, prm.d_qk))
+    n_rows, dev = q.shape[0], q.device
+    n_phys, page = _paged_cache("k_cache", k_cache, prm.fp8, prm.n_kv_heads, prm.d_qk, dev)
+    _cache_scale("k_scale", k_scale, prm.fp8, n_phys, prm.n_kv_heads, page, dev)
+    if prm.latent:
+        if v_cache is not None:
+            raise ValueError("v_cache must be None with a latent cache (V is the first d_v columns of k_cache)")
+    else:
+        _paged_cache("v_cache", v_cache, prm.fp8, prm.n_kv_heads, prm.d_v, dev, (n_phys, page))
+        _cache_scale("v_scale", v_scale, prm.fp8, n_phys, prm.n_kv_heads, page, dev)
+    _need("ctx_len", ctx_len, _I32, (None,), dev)
+    n_seq = ctx_len.shape[0]
+    if n_rows != n_seq * rows_per_seq:
+        raise ValueError(f"q has {n_rows} rows, {n_seq} sequences of rows_per_seq = {rows_per_seq} need {n_seq * rows_per_seq}")
+    max_pages = 1
+    if page_table is not None:
+        max_pages = _need("page_table", page_table, _I32, (n_seq, None), dev).shape[1]
+    if out is None:
+        out = torch.empty((n_rows, prm.n_heads, prm.d_v), dtype=torch.bfloat16, device=dev)
+    else:
+        _need("out", out, _BF16, (n_rows, prm.n_heads, prm.d_v), dev)
+    if lse is True:
+        lse = torch.empty((n_rows, prm.n_heads), dtype=torch.float32, device=dev)
+    elif lse is False:
+        lse = None
+    else:
+        _need_opt("lse", lse, _F32, (n_rows, prm.n_heads), dev)
+    L, ref = lib(), _ref(prm)
+    ws, wsb = _workspace(L.lsa_decode_attn_workspace_size(ref, n_seq, rows_per_seq, max_pages, page), dev, workspace)
+    _check(L.lsa_decode_attn(ref, n_seq, rows_per_seq, _p(q), _p(k_cache), _p(k_scale), _p(v_cache), _p(v_scale),
+                             _p(ctx_len), _p(page_table), max_pages, page, n_phys, _p(out), _p(lse), _p(ws), wsb,
+                             _stream(dev)), "lsa_decode_attn")
     return out, lse
 
 

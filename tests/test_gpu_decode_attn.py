@@ -1,0 +1,355 @@
+"""lsa_decode_attn against the float64 oracle: new tokens over a whole paged cache.
+
+Tolerances, from the arithmetic. A score is an fp32 sum of d exact products: off by at most
+e = (d + 2) 2^-23 scale sum |q_i k_i| (2^-23: a product may be added with truncation), taken at its largest
+over the row's positions, which moves a weight by a factor exp(+-e) and the lse by e; base-2 exponentials and
+the sum of the weights in fp32 add 2^-18. A weight is rounded to bf16 once or, where a tile's halves or parts
+are brought to one maximum, twice (8 significant bits, 2^-8 each), the output once: every output is within
+(3 * 2^-8 + 2 e + 2^-18) sum p |v| of the exact one, where the sum also bounds the output."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+import oracle.serve_oracle as orc
+from paper_2608_01662_amd import lsa
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+GQA, MLA = "gqa", "latent"
+
+
+def _params(kind, H, Hkv, d, fp8=False, k_sink=0, k_swa=0):
+    if kind == MLA:
+        return lsa.DecodeAttnParams(H, 1, 576, 512, True, 192 ** -0.5, False, k_sink, k_swa)
+    return lsa.DecodeAttnParams(H, Hkv, d, d, False, d ** -0.5, fp8, k_sink, k_swa)
+
+
+def _batch(prm, ctx, R, page, seed, q_scale=2.0, width=None, slack=1):
+    """Device inputs of a batch of contexts `ctx` (host list) over permuted pages."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    h = torch.Generator().manual_seed(seed)
+    pages = [max(0, -(-c // page)) for c in ctx]
+    n_phys = sum(pages) + slack
+    width = width or max(pages + [1])
+    table = torch.full((len(ctx), width), -1, dtype=torch.int64)
+    perm = torch.randperm(n_phys, generator=h)
+    at = 0
+    for b, p in enumerate(pages):
+        table[b, :p] = perm[at:at + p]
+        at += p
+    rn = lambda *s: torch.randn(s, generator=g, device=DEV)
+    q = (rn(len(ctx) * R, prm.n_heads, prm.d_qk) * (1.0 if prm.latent else q_scale)).to(torch.bfloat16)
+    shape = (n_phys, page) if prm.latent else (n_phys, prm.n_kv_heads, page)
+    x = dict(q=q, ctx=torch.tensor(ctx, dtype=torch.int32, device=DEV), table=table.to(torch.int32).to(DEV), R=R, page=page)
+    for name, d in [("k", prm.d_qk)] + ([] if prm.latent else [("v", prm.d_v)]):
+        c = rn(*shape, d)
+        if prm.fp8:
+            s = c.abs().amax(-1) / 448
+            x[name + "_scale"] = s
+            c = (c / s[..., None]).to(torch.float8_e4m3fn)
+        else:
+            c = c.to(torch.bfloat16)
+        x[name + "_cache"] = c
+    return x
+
+
+def _run(prm, x, **kw):
+    return lsa.decode_attn(prm, x["q"], x["k_cache"], x.get("v_cache"), x["ctx"], page_table=x["table"],
+                           rows_per_seq=x["R"], k_scale=x.get("k_scale"), v_scale=x.get("v_scale"), **kw)
+
+
+def _check(prm, x, out, lse, rows=None):
+    page, R = x["page"], x["R"]
+    ctx, table = x["ctx"].tolist(), x["table"].cpu().tolist() if x["table"] is not None else None
+    n_phys = x["k_cache"].shape[0]
+    group = prm.n_heads // prm.n_kv_heads
+    q, got, gl = x["q"].cpu().double(), out.cpu().double(), lse.cpu().double()
+    cap = (len(table[0]) if table is not None else 1) * page
+
+    def cached(name, head, rowids):
+        c = x[name + "_cache"]
+        c = c.view(torch.uint8) if prm.fp8 else c
+        c = (c.reshape(n_phys * page, -1) if prm.latent or c.dim() == 3 else c[:, head].reshape(n_phys * page, -1))[rowids]
+        if prm.fp8:
+            sc = x[name + "_scale"]
+            sc = (sc if sc.dim() == 2 else sc[:, head]).reshape(-1)[rowids]
+            return (c.view(torch.float8_e4m3fn).double() * sc.double()[:, None]).cpu()
+        return c.double().cpu()
+    for b, c in enumerate(ctx):
+        n = c if 0 <= c <= cap else 0
+        ids = [orc.cache_row(b, s, table, page, len(ctx), n_phys) for s in range(n)]
+        mapped = torch.tensor([i >= 0 for i in ids], dtype=torch.bool)
+        rid = torch.tensor([max(0, i) for i in ids], dtype=torch.int64, device=DEV)
+        at = torch.arange(n)
+        for head in range(prm.n_kv_heads):
+            k = cached("k", head, rid)
+            v = k[:, :prm.d_v] if prm.latent else cached("v", head, rid)
+            for j in range(R):
+                row = b * R + j
+                if rows is not None and row not in rows:
+                    continue
+                t = n - R + j if n else -1
+                seen = (at <= t) & mapped
+                if prm.k_swa:
+                    seen &= (at > t - prm.k_swa) | (at < prm.k_sink)
+                hs = slice(head * group, (head + 1) * group)
+                o, l, spread, reach = orc.decode_attention(q[row, hs], k, v, seen, prm.sm_scale)
+                e = (prm.d_qk + 2) * 2.0 ** -23 * reach
+                if not bool(seen.any()):
+                    assert (got[row, hs] == 0).all() and (gl[row, hs] == float("-inf")).all(), (b, j)
+                    continue
+                bad = (got[row, hs] - o).abs() - (3 * 2.0 ** -8 + 2 * e + 2.0 ** -18) * spread
+                assert float(bad.max()) <= 0, (b, j, head, c, float(bad.max()))
+                assert ((gl[row, hs] - l).abs() <= e + 2.0 ** -18 * (1 + l.abs())).all(), (b, j, head, c)
+
+
+EDGES = [0, 1, 2, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 257, 1000]
+FORMS = [(GQA, 32, 8, 128, False), (GQA, 32, 8, 128, True), (GQA, 16, 1, 128, False), (GQA, 4, 4, 64, False),
+         (GQA, 4, 4, 64, True), (GQA, 28, 4, 64, True), (GQA, 40, 5, 128, False), (GQA, 24, 1, 128, True),
+         (GQA, 64, 1, 64, False), (GQA, 100, 1, 128, False), (GQA, 1, 1, 128, False), (GQA, 96, 2, 64, True),
+         (MLA, 64, 1, 576, False), (MLA, 16, 1, 576, False), (MLA, 7, 1, 576, False), (MLA, 128, 1, 576, False)]
+
+
+@pytest.mark.parametrize("form", FORMS, ids=str)
+@pytest.mark.parametrize("R,page", [(1, 64), (2, 37), (3, 128)])
+def test_forms_and_short_contexts(form, R, page):
+    """Every head layout and type at contexts from none to a thousand, at and around the tile sizes."""
+    prm = _params(*form)
+    x = _batch(prm, EDGES, R, page, seed=R)
+    out, lse = _run(prm, x)
+    _check(prm, x, out, lse)
+
+
+@pytest.mark.parametrize("form", [(GQA, 32, 8, 128, False), (GQA, 8, 8, 64, True), (MLA, 64, 1, 576, False)], ids=str)
+@pytest.mark.parametrize("page", [1, 3, 16, 20, 32, 100, 256, 1000])
+def test_page_sizes(form, page):
+    prm = _params(*form)
+    x = _batch(prm, [1, 999, 2000, 97], 1, page, seed=page)
+    out, lse = _run(prm, x)
+    _check(prm, x, out, lse)
+
+
+@pytest.mark.parametrize("form", [(GQA, 32, 8, 128, False), (GQA, 12, 12, 64, False), (GQA, 16, 2, 128, True), (MLA, 64, 1, 576, False),
+                                  (MLA, 16, 1, 576, False)], ids=str)
+@pytest.mark.parametrize("sink,swa,R", [(0, 1, 1), (0, 1, 3), (4, 128, 1), (4, 100, 4), (100, 33, 2), (0, 4000, 1), (64, 64, 1),
+                                        (2000, 64, 1), (33, 700, 2)])
+def test_windows(form, sink, swa, R):
+    """Sink and sliding window, apart and meeting, smaller than the new tokens, larger than the context."""
+    prm = _params(*form, k_sink=sink, k_swa=swa)
+    x = _batch(prm, [0, 1, 5, 64, 130, 777, 2050], R, 64, seed=sink + swa)
+    out, lse = _run(prm, x)
+    _check(prm, x, out, lse)
+
+
+@pytest.mark.parametrize("form,ctx,R", [((GQA, 16, 1, 128, False), [40001], 1), ((GQA, 32, 8, 128, True), [9000, 20], 2),
+                                        ((MLA, 64, 1, 576, False), [20001], 1), ((MLA, 128, 1, 576, False), [5000, 1], 2),
+                                        ((GQA, 64, 8, 64, False), [12345, 0, 7], 1)], ids=str)
+def test_long_contexts_of_few_sequences(form, ctx, R):
+    """A long axis split among many workgroups and joined."""
+    prm = _params(*form)
+    x = _batch(prm, ctx, R, 64, seed=11)
+    out, lse = _run(prm, x)
+    _check(prm, x, out, lse)
+
+
+@pytest.mark.parametrize("form", [(GQA, 8, 2, 128, False), (GQA, 8, 8, 64, True), (MLA, 64, 1, 576, False)], ids=str)
+def test_large_ragged_batches(form):
+    """More sequences than a wave has lanes, most of them short or idle, a few long."""
+    prm = _params(*form)
+    g = torch.Generator().manual_seed(5)
+    ctx = [int(x) for x in torch.randint(0, 150, (331,), generator=g)]
+    ctx[0], ctx[100], ctx[330], ctx[64], ctx[63] = 3001, 2500, 4100, 0, 0
+    x = _batch(prm, ctx, 1, 64, seed=6)
+    out, lse = _run(prm, x)
+    _check(prm, x, out, lse)
+
+
+@pytest.mark.parametrize("form", [(GQA, 32, 8, 128, False), (GQA, 8, 8, 64, True), (GQA, 6, 2, 128, True), (MLA, 64, 1, 576, False),
+                                  (MLA, 16, 1, 576, False)], ids=str)
+def test_unmapped_pages_and_bad_lengths(form):
+    """Unmapped pages are left out wherever they lie; lengths out of range and rows before the first token are empty."""
+    prm = _params(*form)
+    x = _batch(prm, [500, 300, 64, 200, 129, 1, 400], 2, 16, seed=7)
+    t = x["table"]
+    t[0, 3], t[0, 4], t[0, 31] = -1, x["k_cache"].shape[0], -7       # holes and the newest page
+    t[1, :] = -1                                                     # nothing mapped
+    t[2, :3] = 2 ** 31 - 1
+    x["ctx"][3], x["ctx"][4] = -3, t.shape[1] * 16 + 1
+    out, lse = _run(prm, x)
+    _check(prm, x, out, lse)
+    assert (out[2:4] == 0).all() and (out[6:10] == 0).all() and (out[10] == 0).all() and not (out[11] == 0).all()
+
+
+@pytest.mark.parametrize("form", [(GQA, 32, 8, 128, False), (GQA, 16, 16, 64, True), (GQA, 64, 1, 128, True), (MLA, 64, 1, 576, False),
+                                  (MLA, 20, 1, 576, False)], ids=str)
+@pytest.mark.parametrize("sink,swa,R,bad", [(0, 0, 1, float("nan")), (5, 100, 1, float("inf")), (5, 100, 3, float("nan")), (0, 0, 4, float("-inf"))])
+def test_what_is_masked_has_no_effect(form, sink, swa, R, bad):
+    """NaN and infinities in every place that no row attends to (behind the context, between sink and window, in
+    pages of nobody) leave every bit as it is; in a place that only later rows attend to, they leave earlier rows."""
+    prm = _params(*form, k_sink=sink, k_swa=swa)
+    page, ctx = 48, [0, 3, 47, 100, 330, 1001]
+    x = _batch(prm, ctx, R, page, seed=13, slack=3)
+    ref, ref_l = (y.clone() for y in _run(prm, x))
+    live = torch.zeros((x["k_cache"].shape[0], page), dtype=torch.bool)
+    for b, c in enumerate(ctx):
+        lo = max(0, c - R - swa + 1) if swa else 0
+        for s in range(c):
+            if s < sink or s >= lo:
+                live[int(x["table"][b, s // page]), s % page] = True
+    dead = ~live.to(DEV)
+    for name in ("k", "v"):
+        c = x.get(name + "_cache")
+        if c is None:
+            continue
+        m = dead if c.dim() == 3 else dead[:, None].expand(c.shape[:3])
+        if prm.fp8:
+            c.view(torch.uint8)[m] = 0x7F
+            x[name + "_scale"][m] = bad
+        else:
+            c[m] = bad
+    out, lse = _run(prm, x)
+    assert torch.equal(out, ref) and torch.equal(lse, ref_l)
+    if R > 1:       # the newest token of the longest sequence is seen by its last row alone
+        b, c = len(ctx) - 1, ctx[-1]
+        ph, off = int(x["table"][b, (c - 1) // page]), (c - 1) % page
+        for name in ("k", "v"):
+            cc = x.get(name + "_cache")
+            if cc is not None:
+                if prm.fp8:
+                    x[name + "_scale"][ph, ..., off] = float("nan")
+                else:
+                    cc[ph, ..., off, :] = float("nan")
+        out, lse = _run(prm, x)
+        n = len(ctx) * R
+        assert torch.equal(out[:n - 1], ref[:n - 1]) and torch.equal(lse[:n - 1], ref_l[:n - 1])
+        assert torch.isnan(out[n - 1]).all() and torch.isnan(lse[n - 1]).all()
+
+
+@pytest.mark.parametrize("form", [(GQA, 16, 2, 128, False), (GQA, 16, 2, 64, True), (MLA, 64, 1, 576, False)], ids=str)
+def test_extreme_scores(form):
+    """One position far above the rest, in each tile in turn (the running maximum moves late and early), scores of
+    thousands, and keys of all -inf products: finite and within bounds, or empty."""
+    prm = _params(*form)
+    for at in (0, 17, 40, 500, 998):
+        x = _batch(prm, [999], 1, 64, seed=at)
+        x["q"].abs_()
+        page = int(x["table"][0, at // 64])
+        if prm.fp8:
+            x["k_cache"].view(torch.uint8)[page, ..., at % 64, :] = torch.tensor(120.0).to(torch.float8_e4m3fn).view(torch.uint8).item()
+            x["k_scale"][page, ..., at % 64] = 1.0
+        else:
+            x["k_cache"][page, ..., at % 64, :] = 60.0
+        out, lse = _run(prm, x)
+        _check(prm, x, out, lse)
+    if not prm.fp8:
+        x = _batch(prm, [100], 1, 64, seed=1)
+        x["q"].abs_().add_(0.5)
+        x["k_cache"].fill_(float("-inf"))
+        if prm.latent:                     # values are columns of the same rows: only the rope dims score
+            x["k_cache"][..., :512] = 1.0
+        out, lse = _run(prm, x)
+        assert (out == 0).all() and (lse == float("-inf")).all()
+
+
+def test_contiguous_cache_matches_paged():
+    """Without a page table sequence b's rows are page b."""
+    prm = _params(GQA, 8, 2, 128, False)
+    x = _batch(prm, [70, 0, 300, 299], 1, 300, seed=3, slack=0)
+    x["k_cache"], x["v_cache"] = x["k_cache"].repeat(2, 1, 1, 1), x["v_cache"].repeat(2, 1, 1, 1)
+    x["table"] = torch.arange(4, dtype=torch.int32, device=DEV)[:, None].contiguous()
+    a, la = (y.clone() for y in _run(prm, x))
+    x["table"] = None
+    b, lb = _run(prm, x)
+    assert torch.equal(a, b) and torch.equal(la, lb)
+    _check(prm, x, b, lb)
+
+
+@pytest.mark.parametrize("form", [(GQA, 8, 1, 128, False), (GQA, 8, 1, 64, True), (MLA, 64, 1, 576, False)], ids=str)
+def test_rows_past_4_gib(form):
+    """Pages that lie beyond 2^32 bytes of the cache."""
+    prm = _params(*form)
+    row = prm.d_qk * (1 if prm.fp8 else 2)
+    page, n_phys = 64, (1 << 32) // (64 * row) + 9
+    x = _batch(prm, [200, 70], 1, page, seed=2)
+    small = x["k_cache"].shape[0]
+    for name in ("k_cache", "v_cache", "k_scale", "v_scale"):
+        if name in x:
+            old = x[name]
+            big = torch.zeros((n_phys,) + tuple(old.shape[1:]), dtype=torch.uint8 if prm.fp8 and "cache" in name else old.dtype, device=DEV)
+            big[n_phys - small:] = old.view(torch.uint8) if prm.fp8 and "cache" in name else old
+            x[name] = big
+    x["table"] = torch.where(x["table"] >= 0, x["table"] + n_phys - small, x["table"])
+    out, lse = _run(prm, x)
+    _check(prm, x, out, lse)
+
+
+def test_same_call_same_bits_on_any_stream_and_workspace():
+    """The same inputs twice, on another stream and with a larger workspace full of NaN: the same bits."""
+    for form in ((GQA, 32, 8, 128, False), (GQA, 32, 8, 128, True), (MLA, 64, 1, 576, False)):
+        prm = _params(*form)
+        x = _batch(prm, [5000, 1, 300, 0, 77], 1, 64, seed=21)
+        ref, ref_l = (y.clone() for y in _run(prm, x))
+        need = lsa.decode_attn_workspace_size(prm, 5, 1, x["table"].shape[1], 64)
+        ws = torch.full((need // 4 + 1000,), float("nan"), device=DEV)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            out, lse = _run(prm, x, workspace=ws)
+        side.synchronize()
+        assert torch.equal(out, ref) and torch.equal(lse, ref_l)
+        out, none = _run(prm, x, lse=False)
+        assert none is None and torch.equal(out, ref)
+
+
+def test_graph_replays_match_eager():
+    """An append and the attention captured into a graph: every replay, with eager work between, as eager."""
+    prm = _params(GQA, 16, 2, 128, True)
+    ap = lsa.AppendParams(16, 2, 128, 128, 0, 128, False, True)
+    x = _batch(prm, [3000, 17, 0, 400], 1, 64, seed=5)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    k, v, q = (torch.randn((4, h, 128), generator=g, device=DEV).to(torch.bfloat16) for h in (2, 2, 16))
+    rope = torch.randn((3000, 128), generator=g, device=DEV)
+    out, lse = torch.empty_like(x["q"]), torch.empty((4, 16), device=DEV)
+    ws = torch.empty(max(1, lsa.decode_attn_workspace_size(prm, 4, 1, x["table"].shape[1], 64)), dtype=torch.uint8, device=DEV)
+
+    def step():
+        lsa.cache_append(ap, k, x["k_cache"], page_table=x["table"], ctx_len=x["ctx"], rope=rope, v=v, v_cache=x["v_cache"],
+                         k_scale=x["k_scale"], v_scale=x["v_scale"], q=q, q_out=x["q"])
+        _run(prm, x, out=out, lse=lse, workspace=ws)
+    step()
+    torch.cuda.synchronize()
+    ref, ref_l = out.clone(), lse.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        out.fill_(float("nan"))
+        lse.zero_()
+        x["q"].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref) and torch.equal(lse, ref_l), i
+        ws.fill_(0xFF)
+
+
+def test_refusals():
+    prm = _params(GQA, 8, 2, 64)
+    x = _batch(prm, [10, 20], 1, 16, seed=1)
+    for kw, word in [(dict(q=x["q"][:1]), "rows"), (dict(q=x["q"].float()), "dtype"), (dict(table=x["table"][:1]), "shape"),
+                     (dict(k_cache=x["k_cache"][..., :32]), "contiguous|shape"), (dict(v_cache=None), "v_cache"),
+                     (dict(v_cache=x["v_cache"][:1]), "pages"), (dict(k_scale=torch.zeros(1, device=DEV)), "None"),
+                     (dict(ctx=x["ctx"].long()), "dtype"), (dict(q=x["q"].cpu()), "CUDA")]:
+        with pytest.raises(ValueError, match=word):
+            _run(prm, {**x, **kw})
+    with pytest.raises(ValueError, match="lse"):
+        _run(prm, x, lse=torch.zeros((2, 4), device=DEV))
+    for bad in (lsa.DecodeAttnParams(8, 2, 64, 64, False, 0.0), lsa.DecodeAttnParams(8, 2, 64, 64, False, float("nan"))):
+        with pytest.raises(lsa.LSAError, match="sm_scale"):
+            _run(bad, x)
