@@ -36,7 +36,7 @@ BF16_PEAK_TFLOPS = 2500.0
 
 
 TRAFFIC_FILE = os.path.join(ROOT, "profiles", "mla_attn_kernel_L131072_hbm_traffic.txt")
-KERNEL_SOURCES = [os.path.join(ROOT, "paper_2608_01662_amd", "csrc", f) for f in ("attention.hip", "device.hpp")]
+KERNEL_SOURCES = [os.path.join(ROOT, "paper_2608_01662_amd", "csrc", f) for f in ("attention.hip", "attn_tile.hpp", "device.hpp")]
 
 
 def log(*a):
