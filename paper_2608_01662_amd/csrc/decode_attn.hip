@@ -1,29 +1,609 @@
 // Attention of new tokens over the whole of a paged cache (lsa_decode_attn) for gfx950.
+//
+// A call is bound by reading the cache once: 4 flops per byte with 32 query heads on 8 bf16 key heads, 121
+// with 64 heads on an MLA latent row, where the card has about 250. So the work is dealt out by cache tiles, not by sequences: the
+// tiles (32 positions of one key/value head) of all sequences stand in one line, sequence after sequence, and
+// every workgroup takes an equal stretch of it, whatever the lengths are. A stretch that covers a (sequence,
+// head) whole writes its output; the others leave a partial (running maximum, sum and unnormalised fp32
+// accumulators of the online softmax) and a second kernel joins the partials. The lengths are on the device, so
+// every workgroup finds its stretch by itself from the lengths.
+#include "attn_tile.hpp"
 #include "device.hpp"
 #include "launch.hpp"
 
 namespace lsa {
 
-constexpr float kLn2 = 0.69314718055994530942f;
+constexpr int kTile = 32;  // positions of a tile
 
+// What loads of positions that nobody attends to read instead (behind the context, in unmapped pages): zeros,
+// since a weight of zero does not silence a NaN or an infinity in V.
+__device__ __attribute__((aligned(256))) const uint8_t zero_row[1152] = {};
+
+__device__ __forceinline__ int fdiv(const FastDiv& f, int n) { return (int)(((uint64_t)(uint32_t)n * f.mul) >> f.shift); }
+
+// The tiles of a sequence that any of its new tokens attends to: 0 .. ns - 1 (the sink) and then ns + skip ..
+struct Span {
+  int c;         // cached positions, 0 where the length is out of range
+  int lo;        // first position of the window of the first new token
+  int ns, skip;  // tile i of the span is tile i of the sequence, from ns on tile i + skip
+  int nt;        // tiles in all
+};
+__device__ __forceinline__ Span span_of(const DecodeGeom& g, int ctx) {
+  Span s;
+  s.c = ctx < 0 || ctx > g.cap ? 0 : ctx;
+  const int t1 = s.c - g.R + 1;  // (first new token) + 1
+  s.lo = g.k_swa > 0 && t1 > g.k_swa ? t1 - g.k_swa : 0;
+  const int sink = g.k_sink < s.c ? g.k_sink : s.c, total = (int)(((uint32_t)s.c + kTile - 1) / kTile);
+  const int st = (int)(((uint32_t)sink + kTile - 1) / kTile), first = s.lo / kTile;
+  s.ns = first <= st ? total : st;
+  s.skip = first <= st ? 0 : first - st;
+  s.nt = total - s.skip;
+  return s;
+}
+
+// Tiles of all sequences (one key/value head), the same in every lane.
+__device__ __forceinline__ int64_t all_tiles(const DecodeGeom& g) {
+  const int lane = threadIdx.x & 63;
+  int64_t sum = 0;
+  for (int b0 = 0; b0 < g.n_seq; b0 += 64)
+    if (b0 + lane < g.n_seq) sum += span_of(g, g.ctx_len[b0 + lane]).nt;
+  for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
+  return sum;
+}
+// Tiles a workgroup takes: an equal share of the `total` tiles of all (sequence, head)s, but no fewer than
+// pay for a workgroup.
+__device__ __forceinline__ int64_t share_of(const DecodeGeom& g, int64_t total) {
+  const int64_t s = (total + g.grid - 1) / g.grid;
+  return s < g.min_tiles ? g.min_tiles : s;
+}
+// The sequence that tile `at` (of one head) is in, and the tiles before it. at < all_tiles.
+__device__ __forceinline__ int find_seq(const DecodeGeom& g, int64_t at, int64_t& before) {
+  const int lane = threadIdx.x & 63;
+  before = 0;
+  for (int b0 = 0; b0 < g.n_seq; b0 += 64) {
+    const int nt = b0 + lane < g.n_seq ? span_of(g, g.ctx_len[b0 + lane]).nt : 0;
+    int64_t inc = nt;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t x = __shfl_up(inc, o);
+      if (lane >= o) inc += x;
+    }
+    const uint64_t past = __ballot(before + inc > at);
+    if (past) {
+      const int first = __ffsll((unsigned long long)past) - 1;
+      before += __shfl(inc - nt, first);
+      return b0 + first;
+    }
+    before += __shfl(inc, 63);
+  }
+  return g.n_seq;
+}
+
+// ---------------------------------------------------------------- direct global -> LDS loads
+// 16 (4) bytes per lane from `src` to LDS bytes lds + 16 (4) lane. The compiler does not see these loads, so
+// that it does not drain them before every LDS read; callers wait with explicit vmcnt counts. M0 holds the LDS
+// address and is restored; the s_nop is the wait state before a load may read it.
+__device__ __forceinline__ void lds_dma16(const uint8_t* src, uint32_t lds) {
+  uint32_t save;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
+               : "=&s"(save) : "v"(src), "s"(lds) : "memory");
+}
+__device__ __forceinline__ void lds_dma4(const uint8_t* src, uint32_t lds) {
+  uint32_t save;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %1, off\n\ts_mov_b32 m0, %0"
+               : "=&s"(save) : "v"(src), "s"(lds) : "memory");
+}
+
+// eight e4m3 codes -> eight bf16 (exact)
+__device__ __forceinline__ u32x4 fp8x8_bf16(uint32_t lo, uint32_t hi) {
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true))};
+}
+typedef __attribute__((ext_vector_type(2))) int i32x2;
+// Transposed read of 8-bit values: in a 16-lane group, source lane s supplies 8 bytes of row s / 2 (columns
+// 8 (s % 2) ..), and lane i receives column i of the 8 rows.
+__device__ __forceinline__ u32x2 tr8(const uint8_t* p) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(p)));
+}
+
+// ============================================================================ grouped heads, 64 or 128 wide
+// One workgroup = four waves that share no tiles: wave w streams tiles w, w + 4, .. of the stretch through a
+// ring in LDS of its own, K and V apart, by direct loads of whole rows, and refills a tile's K as soon as it is
+// scored and its V as soon as it is multiplied, so that about 24 KB per wave are on their way at any time. (A step of the
+// ring needs no barrier, only a count of the wave's own loads.) At the stretch's end the waves' results are
+// merged through LDS.
+//
+// The rows of the products are query rows: the heads of the group of all new tokens, in blocks of 16 (NB
+// blocks per wave); S^T = K Q^T on 16x16x32 products with tokens on the rows, in an order that gives lane
+// (g = lane / 16) the scores of tokens 8 g .. + 7 of its column, which is the layout of the B operand of
+// O^T += V^T P^T: P never leaves the registers.
+constexpr int kGqaWaves = 4;
+constexpr int kGqaRing = 32 * 1024;   // LDS ring bytes per wave
+constexpr int kPageSlots = 2048;      // page-table entries staged in LDS at a time
+
+template <int D, bool FP8>
+struct GqaTile {
+  static constexpr int kRow = D * (FP8 ? 1 : 2);          // bytes of a cache row
+  static constexpr int kBytes = kTile * kRow;             // of a K or V tile
+  static constexpr int kChunks = kRow / 16;               // 16-byte chunks of a row
+  static constexpr int kLoads = kBytes / 1024;            // direct loads of a K or V tile
+  static constexpr int kStages = kGqaRing / (2 * kBytes); // tiles in the ring
+  static constexpr int kK = kLoads + (FP8 ? 1 : 0);       // loads issued with K: its rows, and both scales
+  static constexpr int kPair = kK + kLoads;
+  // Chunk c of token t lies in 16-byte slot c ^ swz(t) of its row. The K reads (16 tokens of one chunk per 16
+  // lanes) and the transposed V reads (per 32 lanes 8 or 16 tokens x 32 or 16 bytes) then fall on all
+  // banks alike: with t = 16 a1 + 8 a0 + 4 b + 2 k1 + k0, a K read varies a1, a0, k1, k0, a V read of 32 lanes a0, k1, k0
+  // (fp8: and b), and rows of less than 256 bytes spread by their own low token bits.
+  static __device__ __forceinline__ int swz(int t) {
+    const int a1 = (t >> 4) & 1, a0 = (t >> 3) & 1, b = (t >> 2) & 1;
+    if constexpr (kChunks == 16) return a1 | (t & 3) << 1 | a0 << 3;
+    if constexpr (kChunks == 8) return (a1 ^ b) | (t & 2) | a0 << 2;
+    return a0 | (a1 ^ b) << 1;
+  }
+};
+
+template <int D, bool FP8, int NB>
+__global__ __launch_bounds__(64 * kGqaWaves) __attribute__((amdgpu_waves_per_eu(1, 1)))
+void gqa_decode_kernel(DecodeGeom g) {
+  using T = GqaTile<D, FP8>;
+  constexpr int NS = T::kStages, KS = D / 32, CD = D / 16, COLS = 16 * NB;
+  constexpr int OS = D + 4;  // floats per column of a merged accumulator
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[kGqaWaves][kGqaRing];
+  __shared__ __attribute__((aligned(16))) float scales[FP8 ? kGqaWaves : 1][FP8 ? NS : 1][64];
+  __shared__ int pages[kPageSlots];
+  __shared__ float pm[kGqaWaves][16], pl[kGqaWaves][16];
+  static_assert(16 * OS * 4 <= kGqaRing, "the accumulators are merged in the ring");
+  const int lane = threadIdx.x & 63, q4 = lane >> 4, i16 = lane & 15;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint8_t* const lk = ring[wv];                    // K tiles, then V tiles
+  uint8_t* const lv = ring[wv] + NS * T::kBytes;
+  const int group = g.H / g.Hkv, cols = g.R * group;
+  const int cb_n = (cols + COLS - 1) / COLS, M = g.Hkv * cb_n;  // (head, column block)s of a sequence
+
+  // LDS offsets of this lane's operands: K of token block mt at chunk 4 s + q4, V of value block c
+  int k_off[2], k_swz[2];
+#pragma unroll
+  for (int mt = 0; mt < 2; ++mt) {
+    const int t = 8 * (i16 >> 2) + 4 * mt + (i16 & 3);
+    k_off[mt] = t * T::kRow;
+    k_swz[mt] = T::swz(t);
+  }
+  const int v_t0 = FP8 ? 8 * q4 + (i16 >> 1) : 8 * q4 + (i16 >> 2), v_t1 = v_t0 + 4;  // (bf16: rows of both reads)
+  // direct load j: tokens j * 64 / chunks .., lane -> token lane / chunks of them, slot lane % chunks
+  constexpr int LT = 64 / T::kChunks;  // tokens per load
+  const int ld_t = lane / T::kChunks, ld_slot = lane % T::kChunks;
+
+  auto segment = [&](int b, int r, const Span& sp, int t0, int t1, bool whole, int64_t slot) {
+    const int kvh = r / cb_n, col0 = (r - kvh * cb_n) * COLS;
+    const int ncols = cols - col0 < COLS ? cols - col0 : COLS;
+    // ---- Q as the B operand: column 16 nb + i16 = (new token j, head of the group), dims of k-step s
+    u32x4 qb[NB][KS];
+    int tcol[NB];  // position of the column's token
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int col = col0 + 16 * nb + i16;
+      const bool ok = 16 * nb + i16 < ncols;
+      const int j = ok ? col / group : 0, hh = ok ? col - j * group : 0;
+      tcol[nb] = sp.c - g.R + j;
+      const uint8_t* qp = reinterpret_cast<const uint8_t*>(g.q + (((int64_t)b * g.R + j) * g.H + kvh * group + hh) * D);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        // bf16: chunk 4 s + q4 of the row; fp8: a 16-byte K chunk 4 (s / 2) + q4 holds the dims of two k-steps
+        const int dim = FP8 ? 64 * (s >> 1) + 16 * q4 + 8 * (s & 1) : 32 * s + 8 * q4;
+        qb[nb][s] = ok ? *reinterpret_cast<const u32x4*>(qp + 2 * dim) : u32x4{};
+      }
+    }
+    f32x4 o[NB][CD];
+    float m[NB], l[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      m[nb] = kNoRef;
+      l[nb] = 0.f;
+#pragma unroll
+      for (int c = 0; c < CD; ++c) o[nb][c] = f32x4{};
+    }
+    for (int p0 = t0; p0 < t1; p0 += g.pass_tiles) {
+      const int p1 = t1 - p0 < g.pass_tiles ? t1 : p0 + g.pass_tiles;
+      // ---- page-table entries of tiles [p0, p1): those before the skipped ones, then the others
+      const int e1 = p1 < sp.ns ? p1 : sp.ns, b2 = p0 > sp.ns ? p0 : sp.ns;
+      int f1 = 0, n1 = 0, f2 = 0, n2 = 0;  // first page and pages of both parts
+      if (p0 < e1) {
+        f1 = fdiv(g.by_page, p0 * kTile);
+        const int last = e1 * kTile - 1 < sp.c ? e1 * kTile - 1 : sp.c - 1;
+        n1 = fdiv(g.by_page, last) - f1 + 1;
+      }
+      if (b2 < p1) {
+        f2 = fdiv(g.by_page, (b2 + sp.skip) * kTile);
+        const int64_t end = (int64_t)(p1 + sp.skip) * kTile - 1;
+        n2 = fdiv(g.by_page, end < sp.c ? (int)end : sp.c - 1) - f2 + 1;
+      }
+      for (int i = (int)threadIdx.x; i < n1 + n2; i += 64 * kGqaWaves) {
+        const int pg = i < n1 ? f1 + i : f2 + i - n1;
+        const int ph = g.page_table ? g.page_table[(int64_t)b * g.max_pages + pg] : b;
+        pages[i] = ph >= 0 && ph < g.n_phys ? ph : -1;
+      }
+      // Q (and everything else on its way) has arrived before the first direct load: the compiler, which does
+      // not know of those, would wait for all of them together with Q
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      const int nw = p1 - p0 > wv ? (p1 - p0 - wv + kGqaWaves - 1) / kGqaWaves : 0;  // this wave's tiles
+      // cache row of token lane % 32 of this wave's tile i, -1 where nobody attends to it
+      auto tile_pos = [&](int i) {
+        const int t = p0 + wv + kGqaWaves * i;
+        return (t < sp.ns ? t : t + sp.skip) * kTile;
+      };
+      auto tile_rows = [&](int i) {
+        const int s = tile_pos(i) + (lane & 31), t = p0 + wv + kGqaWaves * i;
+        const bool seen = s >= 0 && s < sp.c && (s >= sp.lo || s < g.k_sink);
+        if (!seen) return -1;
+        const int pg = fdiv(g.by_page, s);
+        const int ph = pages[t < sp.ns ? pg - f1 : n1 + pg - f2];
+        return ph >= 0 ? (int)(((uint32_t)ph * (uint32_t)g.Hkv + (uint32_t)kvh) * (uint32_t)g.P + (uint32_t)(s - pg * g.P)) : -1;
+      };
+      auto issue = [&](const void* base, uint8_t* dst, int rows) {
+#pragma unroll
+        for (int j = 0; j < T::kLoads; ++j) {
+          const int t = j * LT + ld_t, row = __shfl(rows, t);
+          const uint8_t* src = row >= 0 ? static_cast<const uint8_t*>(base) + (int64_t)row * T::kRow : zero_row;
+          lds_dma16(src + (ld_slot ^ T::swz(t)) * 16, lds_addr(dst + j * 1024));
+        }
+      };
+      auto issue_k = [&](int i, int rows) {
+        const int st = i % NS;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage's last reads are done
+        if constexpr (FP8) {
+          const float* sc = lane < 32 ? g.k_scale : g.v_scale;
+          lds_dma4(rows >= 0 ? reinterpret_cast<const uint8_t*>(sc + rows) : zero_row, lds_addr(scales[wv][st]));
+        }
+        issue(g.k, lk + st * T::kBytes, rows);
+      };
+      auto issue_v = [&](int i, int rows) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        issue(g.v, lv + (i % NS) * T::kBytes, rows);
+      };
+      uint32_t seen_bits[NS];
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        seen_bits[i] = 0;
+        if (i < nw) {
+          const int rows = tile_rows(i);
+          seen_bits[i] = (uint32_t)__ballot(rows >= 0);
+          issue_k(i, rows);
+          issue_v(i, rows);
+        }
+      }
+      for (int i0 = 0; i0 < nw; i0 += NS) {
+#pragma unroll
+        for (int st = 0; st < NS; ++st) {
+          const int i = i0 + st;
+          if (i >= nw) break;
+          const bool more = i + NS < nw;  // tile i + NS takes this one's place
+          const int rows = more ? tile_rows(i + NS) : -1;
+          const uint32_t bits = seen_bits[st];
+          // K of tile i has landed: behind it are its V and the other stages' tiles (fewer at the stretch's end)
+          if (i + NS <= nw) vm_wait<T::kLoads + (NS - 1) * T::kPair>();
+          else vm_wait<0>();
+          // ---- S^T = K Q^T
+          const uint8_t* kt = lk + st * T::kBytes;
+          f32x4 s4[2][NB];
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) s4[mt][nb] = f32x4{};
+            if constexpr (FP8) {
+#pragma unroll
+              for (int s = 0; s < KS; s += 2) {
+                const u32x4 x = *reinterpret_cast<const u32x4*>(kt + k_off[mt] + ((2 * s + q4) ^ k_swz[mt]) * 16);
+                const u32x4 a = fp8x8_bf16(x.x, x.y), b = fp8x8_bf16(x.z, x.w);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                  s4[mt][nb] = mfma16(a, qb[nb][s], s4[mt][nb]);
+                  s4[mt][nb] = mfma16(b, qb[nb][s + 1], s4[mt][nb]);
+                }
+              }
+            } else {
+#pragma unroll
+              for (int s = 0; s < KS; ++s) {
+                const u32x4 a = *reinterpret_cast<const u32x4*>(kt + k_off[mt] + ((4 * s + q4) ^ k_swz[mt]) * 16);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) s4[mt][nb] = mfma16(a, qb[nb][s], s4[mt][nb]);
+              }
+            }
+          }
+          // scores of tokens 8 q4 .. + 7 of the columns, in units of log2
+          float z[NB][8], vs[8];
+          if constexpr (FP8) {
+            const f32x4* sk = reinterpret_cast<const f32x4*>(&scales[wv][st][8 * q4]);
+            const f32x4* sv = reinterpret_cast<const f32x4*>(&scales[wv][st][32 + 8 * q4]);
+            const f32x4 a = sk[0], b = sk[1], c = sv[0], d = sv[1];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const float ks = (k < 4 ? a[k & 3] : b[k & 3]) * g.scale_log2;
+              vs[k] = k < 4 ? c[k & 3] : d[k & 3];
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) z[nb][k] = s4[k >> 2][nb][k & 3] * ks;
+            }
+          } else {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int k = 0; k < 8; ++k) z[nb][k] = s4[k >> 2][nb][k & 3] * g.scale_log2;
+          }
+          if (more) issue_k(i + NS, rows);
+          const int s0 = tile_pos(i);
+          // several new tokens: does the tile reach to where they see different positions?
+          const bool uneven = g.R > 1 && (s0 + kTile > sp.c - g.R + 1 || (g.k_swa > 0 && s0 < sp.c - g.k_swa));
+          if (bits != 0xFFFFFFFFu || uneven) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const int s = s0 + 8 * q4 + k;
+              const bool live = (bits >> (8 * q4 + k)) & 1u;
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) {
+                const bool own = !uneven || (s <= tcol[nb] && (g.k_swa == 0 || tcol[nb] - s < g.k_swa || s < g.k_sink));
+                z[nb][k] = live && own ? z[nb][k] : -INFINITY;
+              }
+            }
+          }
+          // ---- online softmax; the reference maximum moves when it grows by more than 2^8
+          u32x4 pb[NB];
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            float mx = z[nb][0];
+#pragma unroll
+            for (int k = 1; k < 8; ++k) mx = fmaxf(mx, z[nb][k]);
+            mx = max4_xor16_32(mx);
+            const bool need = mx > m[nb] + kLazy;
+            if (__ballot(need)) {
+              const float alpha = need ? fast_exp2(m[nb] - mx) : 1.f;
+#pragma unroll
+              for (int c = 0; c < CD; ++c) o[nb][c] *= alpha;
+              l[nb] *= alpha;
+              m[nb] = need ? mx : m[nb];
+            }
+            float p[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              p[k] = fast_exp2(z[nb][k] - m[nb]);  // -inf -> 0
+              l[nb] += p[k];
+              if constexpr (FP8) p[k] = z[nb][k] == -INFINITY ? 0.f : p[k] * vs[k];  // (masked: also from a NaN scale)
+            }
+            pb[nb] = u32x4{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])};
+          }
+          // V of tile i has landed: behind it are the other stages' tiles and the K just requested
+          if (more) vm_wait<(NS - 1) * T::kPair + T::kK>();
+          else if (i + NS == nw) vm_wait<(NS - 1) * T::kPair>();
+          else vm_wait<0>();
+          // ---- O^T += V^T P^T
+          const uint8_t* vt = lv + st * T::kBytes;
+          auto value = [&](int c) {
+            if constexpr (FP8) {
+              const u32x2 x = tr8(vt + v_t0 * T::kRow + (c ^ T::swz(v_t0)) * 16 + (i16 & 1) * 8);
+              return fp8x8_bf16(x.x, x.y);
+            } else {
+              const int ch = 2 * c + ((i16 >> 1) & 1), half = (i16 & 1) * 8;
+              return tr16_pair(vt + v_t0 * T::kRow + (ch ^ T::swz(v_t0)) * 16 + half,
+                               vt + v_t1 * T::kRow + (ch ^ T::swz(v_t1)) * 16 + half);
+            }
+          };
+          if (!uneven) {
+#pragma unroll
+            for (int c = 0; c < CD; ++c) {
+              const u32x4 a = value(c);
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) o[nb][c] = mfma16(a, pb[nb], o[nb][c]);
+            }
+          } else {
+            // a token's row of V reaches only the columns that see it, also if it holds a NaN: one product per new
+            // token, its unseen rows of V zeroed, taken by its own columns
+            for (int j = col0 / group; j <= (col0 + ncols - 1) / group; ++j) {
+              const int t = sp.c - g.R + j;
+              u32x4 keep;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const int s = s0 + 8 * q4 + 2 * k;
+                auto sees = [&](int x) { return x <= t && (g.k_swa == 0 || t - x < g.k_swa || x < g.k_sink); };
+                keep[k] = (sees(s) ? 0xFFFFu : 0u) | (sees(s + 1) ? 0xFFFF0000u : 0u);
+              }
+#pragma unroll
+              for (int c = 0; c < CD; ++c) {
+                const u32x4 a = value(c) & keep;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                  const f32x4 x = mfma16(a, pb[nb], f32x4{});
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) o[nb][c][k] += tcol[nb] == t ? x[k] : 0.f;
+                }
+              }
+            }
+          }
+          if (more) {
+            seen_bits[st] = (uint32_t)__ballot(rows >= 0);
+            issue_v(i + NS, rows);
+          }
+        }
+      }
+      __syncthreads();  // every wave is done with `pages` and its ring
+    }
+    // ---- the waves' results, 16 columns at a time: weighted by 2^(m_w - M) and summed
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      if (16 * nb >= ncols) break;
+      float* po = reinterpret_cast<float*>(ring[wv]);
+#pragma unroll
+      for (int c = 0; c < CD; ++c) *reinterpret_cast<f32x4*>(po + i16 * OS + 16 * c + 4 * q4) = o[nb][c];
+      const float lt = sum4_xor16_32(l[nb]);
+      if (q4 == 0) {
+        pm[wv][i16] = m[nb];
+        pl[wv][i16] = lt;
+      }
+      __syncthreads();
+      for (int u = (int)threadIdx.x; u < 16 * (D / 4); u += 64 * kGqaWaves) {
+        const int col = u / (D / 4), d = 4 * (u % (D / 4));
+        if (16 * nb + col >= ncols) break;
+        float mx = pm[0][col];
+#pragma unroll
+        for (int x = 1; x < kGqaWaves; ++x) mx = fmaxf(mx, pm[x][col]);
+        float sum = 0.f;
+        f32x4 acc = {};
+#pragma unroll
+        for (int x = 0; x < kGqaWaves; ++x) {
+          const float w = fast_exp2(pm[x][col] - mx);
+          sum += pl[x][col] * w;
+          acc += w * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(ring[x]) + col * OS + d);
+        }
+        const int at = col0 + 16 * nb + col;
+        if (whole) {
+          const int j = at / group;
+          const int64_t row = ((int64_t)b * g.R + j) * g.H + kvh * group + at - j * group;
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+          *reinterpret_cast<u32x2*>(g.out + row * D + d) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+          if (g.lse && d == 0) g.lse[row] = sum == 0.f ? -INFINITY : (mx + __log2f(sum)) * kLn2;
+        } else {
+          const int64_t pc = slot * COLS + 16 * nb + col;
+          *reinterpret_cast<f32x4*>(g.part_o + pc * D + d) = acc;
+          if (d == 0) *reinterpret_cast<f32x2*>(g.part_ml + 2 * pc) = f32x2{mx, sum};
+        }
+      }
+      __syncthreads();
+    }
+  };
+
+  const int64_t total = all_tiles(g) * M, share = share_of(g, total);
+  int64_t at = blockIdx.x * share;
+  const int64_t start = at, end = at + share < total ? at + share : total;
+  if (at < end) {
+    int64_t before;
+    int b = find_seq(g, at / M, before);
+    while (at < end) {
+      const Span sp = span_of(g, g.ctx_len[b]);
+      if (sp.nt == 0) {
+        ++b;
+        continue;
+      }
+      const int64_t rel = at - before * M;
+      const int r = (int)(rel / sp.nt), t0 = (int)(rel - (int64_t)r * sp.nt);
+      const int n = end - at < sp.nt - t0 ? (int)(end - at) : sp.nt - t0;
+      segment(b, r, sp, t0, t0 + n, n == sp.nt, 2 * (int64_t)blockIdx.x + (at != start));
+      at += n;
+      if (r == M - 1 && t0 + n == sp.nt) {
+        before += sp.nt;
+        ++b;
+      }
+    }
+  }
+  // sequences without a tile: empty rows, dealt to the workgroups
+  const int64_t row_elems = (int64_t)g.R * g.H * D;
+  for (int b = blockIdx.x; b < g.n_seq; b += g.grid) {
+    if (span_of(g, g.ctx_len[b]).nt != 0) continue;
+    for (int64_t i = 8 * (int64_t)threadIdx.x; i < row_elems; i += 8 * 64 * kGqaWaves) *reinterpret_cast<u32x4*>(g.out + b * row_elems + i) = u32x4{};
+    if (g.lse)
+      for (int i = (int)threadIdx.x; i < g.R * g.H; i += 64 * kGqaWaves) g.lse[(int64_t)b * g.R * g.H + i] = -INFINITY;
+  }
+}
+
+// ============================================================================ joining the partials
+// One workgroup per (sequence, head, column): nothing to do where one stretch covered it whole. The threads
+// take four dims each, in groups that share the partials and keep a running maximum of their own.
+template <int D, int COLS>
+__global__ __launch_bounds__(256) void decode_join_kernel(DecodeGeom g) {
+  constexpr int Q = D / 4, SUBS = 256 / Q, U = 4;
+  __shared__ __attribute__((aligned(16))) float acc_s[SUBS][D];
+  __shared__ float m_s[SUBS], l_s[SUBS];
+  const int group = g.H / g.Hkv, cols = g.R * group, cb_n = (cols + COLS - 1) / COLS, M = g.Hkv * cb_n;
+  const int64_t pair = blockIdx.x / cols;  // (sequence, key/value head)
+  const int col = (int)(blockIdx.x - pair * cols);
+  const int b = (int)(pair / g.Hkv), kvh = (int)(pair - (int64_t)b * g.Hkv), r = kvh * cb_n + col / COLS;
+  int64_t before = 0, all = 0;  // tiles of the sequences before b, and of all
+  {
+    const int lane = threadIdx.x & 63;
+    for (int b0 = 0; b0 < g.n_seq; b0 += 64)
+      if (b0 + lane < g.n_seq) {
+        const int nt = span_of(g, g.ctx_len[b0 + lane]).nt;
+        all += nt;
+        before += b0 + lane < b ? nt : 0;
+      }
+    for (int o = 32; o >= 1; o >>= 1) {
+      all += __shfl_xor(all, o);
+      before += __shfl_xor(before, o);
+    }
+  }
+  const int nt = span_of(g, g.ctx_len[b]).nt;
+  const int64_t share = share_of(g, all * M), first = before * M + (int64_t)r * nt;
+  const int64_t w0 = first / share, w1 = (first + nt - 1) / share;
+  if (nt == 0 || w0 == w1) return;  // (uniform)
+  const int sub = threadIdx.x / Q, d = 4 * (threadIdx.x % Q), cc = col % COLS;
+  // the first stretch may have begun with another head: then this one's partial is its second
+  auto slot = [&](int64_t w) { return (2 * w + (w == w0 && first != w0 * share)) * COLS + cc; };
+  float m = kNoRef, l = 0.f;
+  f32x4 acc = {};
+  for (int64_t w = w0 + sub; w <= w1; w += SUBS * U) {
+    f32x2 ml[U];
+    f32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t v = w + (int64_t)u * SUBS <= w1 ? w + (int64_t)u * SUBS : w;
+      ml[u] = *reinterpret_cast<const f32x2*>(g.part_ml + 2 * slot(v));
+      x[u] = *reinterpret_cast<const f32x4*>(g.part_o + slot(v) * D + d);
+    }
+    float mx = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) mx = fmaxf(mx, ml[u][0]);
+    const float a = fast_exp2(m - mx);
+    l *= a;
+    acc *= a;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (w + (int64_t)u * SUBS > w1) break;
+      const float f = fast_exp2(ml[u][0] - mx);
+      l += ml[u][1] * f;
+      acc += f * x[u];
+    }
+    m = mx;
+  }
+  *reinterpret_cast<f32x4*>(&acc_s[sub][d]) = acc;
+  if (d == 0) {
+    m_s[sub] = m;
+    l_s[sub] = l;
+  }
+  __syncthreads();
+  if (sub != 0) return;
+  float mx = m_s[0];
+  for (int s = 1; s < SUBS; ++s) mx = fmaxf(mx, m_s[s]);
+  float sum = 0.f;
+  f32x4 o = {};
+  for (int s = 0; s < SUBS; ++s) {
+    const float f = fast_exp2(m_s[s] - mx);
+    sum += l_s[s] * f;
+    o += f * *reinterpret_cast<const f32x4*>(&acc_s[s][d]);
+  }
+  const int j = col / group;
+  const int64_t row = ((int64_t)b * g.R + j) * g.H + kvh * group + col - j * group;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  *reinterpret_cast<u32x2*>(g.out + row * D + d) = u32x2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
+  if (g.lse && d == 0) g.lse[row] = sum == 0.f ? -INFINITY : (mx + __log2f(sum)) * kLn2;
+}
+
+// ============================================================================ latent cache
 // One wave per (row, head), 64 positions at a time: a lane scores one position, then holds d_v / 64 columns
 // of the output. The plain form of the operator: every head reads its rows by itself.
-__global__ __launch_bounds__(64) void decode_attn_kernel(DecodeGeom g) {
+__global__ __launch_bounds__(64) void latent_decode_kernel(DecodeGeom g) {
   __shared__ float qs[576];
   __shared__ float ps[64];
   __shared__ int rows[64];
   const int lane = threadIdx.x;
   const int64_t r = blockIdx.x / g.H;
-  const int h = (int)(blockIdx.x - r * g.H), kvh = h / (g.H / g.Hkv);
+  const int h = (int)(blockIdx.x - r * g.H);
   const int b = (int)(r / g.R), j = (int)(r - (int64_t)b * g.R);
   for (int i = lane; i < g.d_qk; i += 64) qs[i] = __uint_as_float((uint32_t)g.q[(r * g.H + h) * g.d_qk + i] << 16);
   const int ctx = g.ctx_len[b];
   const int t = ctx < 0 || ctx > g.max_pages * g.P ? -1 : ctx - g.R + j;
   const int cols = g.d_v / 64;
   float o[8] = {}, m = -INFINITY, l = 0.f;
-  auto value = [&](const void* base, const float* scale, int64_t row, int d, int i) {
-    if (!g.fp8) return __uint_as_float((uint32_t) static_cast<const uint16_t*>(base)[row * d + i] << 16);
-    return __builtin_amdgcn_cvt_f32_fp8((int) static_cast<const uint8_t*>(base)[row * d + i], 0) * scale[row];
+  auto value = [&](const void* base, int64_t row, int d, int i) {
+    return __uint_as_float((uint32_t) static_cast<const uint16_t*>(base)[row * d + i] << 16);
   };
   __syncthreads();
   for (int s0 = 0; s0 <= t; s0 += 64) {
@@ -32,11 +612,11 @@ __global__ __launch_bounds__(64) void decode_attn_kernel(DecodeGeom g) {
     int64_t ph = -1;
     if (seen) ph = g.page_table ? g.page_table[(int64_t)b * g.max_pages + s / g.P] : b;
     seen = seen && ph >= 0 && ph < g.n_phys;
-    const int64_t row = (ph * g.Hkv + kvh) * g.P + s % g.P;
+    const int64_t row = ph * g.P + s % g.P;
     float z = -INFINITY;
     if (seen) {
       float acc = 0.f;
-      for (int i = 0; i < g.d_qk; ++i) acc += qs[i] * value(g.k, g.k_scale, row, g.d_qk, i);
+      for (int i = 0; i < g.d_qk; ++i) acc += qs[i] * value(g.k, row, g.d_qk, i);
       z = acc * g.scale_log2;
     }
     const float mx = fmaxf(wave_max(z), m);
@@ -52,9 +632,7 @@ __global__ __launch_bounds__(64) void decode_attn_kernel(DecodeGeom g) {
     for (int c = 0; c < cols; ++c) o[c] *= alpha;
     for (int k = 0; k < 64; ++k) {
       if (rows[k] < 0) continue;
-      for (int c = 0; c < cols; ++c)
-        o[c] += ps[k] * (g.latent ? value(g.k, nullptr, rows[k], g.d_qk, 64 * c + lane)
-                                  : value(g.v, g.v_scale, rows[k], g.d_v, 64 * c + lane));
+      for (int c = 0; c < cols; ++c) o[c] += ps[k] * value(g.k, rows[k], g.d_qk, 64 * c + lane);
     }
     __syncthreads();
   }
@@ -64,9 +642,29 @@ __global__ __launch_bounds__(64) void decode_attn_kernel(DecodeGeom g) {
   if (g.lse && lane == 0) g.lse[r * g.H + h] = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
-hipError_t launch_decode_attn(const DecodeGeom& g, hipStream_t st) {
-  hipLaunchKernelGGL(decode_attn_kernel, dim3((unsigned)(g.n_seq * g.R * g.H)), dim3(64), 0, st, g);
+// ============================================================================ host launchers
+template <int D, bool FP8, int NB>
+static hipError_t launch_gqa(const DecodeGeom& g, hipStream_t st) {
+  hipLaunchKernelGGL((gqa_decode_kernel<D, FP8, NB>), dim3((unsigned)g.grid), dim3(64 * kGqaWaves), 0, st, g);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || g.part_o == nullptr) return e;
+  const int64_t blocks = (int64_t)g.n_seq * g.R * g.H;
+  hipLaunchKernelGGL((decode_join_kernel<D, 16 * NB>), dim3((unsigned)blocks), dim3(256), 0, st, g);
   return hipGetLastError();
+}
+template <int D, bool FP8>
+static hipError_t launch_gqa(const DecodeGeom& g, hipStream_t st) {
+  const int nb = g.block_cols / 16;
+  return nb == 1 ? launch_gqa<D, FP8, 1>(g, st) : nb == 2 ? launch_gqa<D, FP8, 2>(g, st) : launch_gqa<D, FP8, 4>(g, st);
+}
+
+hipError_t launch_decode_attn(const DecodeGeom& g, hipStream_t st) {
+  if (g.latent) {
+    hipLaunchKernelGGL(latent_decode_kernel, dim3((unsigned)(g.n_seq * g.R * g.H)), dim3(64), 0, st, g);
+    return hipGetLastError();
+  }
+  if (g.d_qk == 64) return g.fp8 ? launch_gqa<64, true>(g, st) : launch_gqa<64, false>(g, st);
+  return g.fp8 ? launch_gqa<128, true>(g, st) : launch_gqa<128, false>(g, st);
 }
 
 }  // namespace lsa

@@ -139,8 +139,16 @@ struct DecodeGeom {
   int64_t n_phys;
   int n_seq, R, H, Hkv, d_qk, d_v, latent, fp8;
   int max_pages, P;
-  int k_sink, k_swa;
-  float scale_log2;  // sm_scale * log2(e)
+  int k_sink, k_swa;  // both below cap, or 0
+  float scale_log2;   // sm_scale * log2(e)
+  // the plan
+  int cap;            // positions a sequence can have: max_pages * P
+  FastDiv by_page;    // division by P
+  int pass_tiles;     // tiles whose page-table entries fit the LDS area
+  int block_cols;     // query rows of one key/value head that a workgroup takes together
+  int grid;           // workgroups
+  int min_tiles;      // tiles that pay for a workgroup
+  float *part_o, *part_ml;  // two partials per workgroup: [block_cols, d_v], [block_cols, 2]; nullptr: none is cut
 };
 hipError_t launch_decode_attn(const DecodeGeom& g, hipStream_t st);
 

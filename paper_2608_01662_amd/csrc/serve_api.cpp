@@ -72,6 +72,40 @@ lsa_status check_decode_sizes(const lsa_decode_attn_params* p, int32_t n_seq, in
   return LSA_OK;
 }
 
+// How a call is dealt out (decode_attn.hip): `grid` workgroups take equal stretches of all tiles.
+struct DecodePlan {
+  int grid, min_tiles, block_cols, pass_tiles;
+  bool cut;  // may a stretch end inside a (sequence, head)?
+  size_t off_ml, total;
+};
+constexpr int kTile = 32;          // positions of a tile
+constexpr int kPageSlots = 2048;   // page-table entries a workgroup stages at a time
+
+DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq, int32_t max_pages,
+                       int32_t kv_page_size) {
+  DecodePlan pl{};
+  const int64_t cols = (int64_t)rows_per_seq * (p->n_heads / p->n_kv_heads);
+  pl.block_cols = cols <= 16 ? 16 : cols <= 32 ? 32 : 64;
+  const int64_t pairs = (int64_t)n_seq * p->n_kv_heads * cdiv(cols, pl.block_cols);
+  const int64_t cap = (int64_t)max_pages * kv_page_size;
+  int64_t tiles = cdiv(cap, kTile);  // of one (sequence, head), at most
+  if (p->k_swa > 0) {
+    const int64_t window = cdiv(p->k_sink, kTile) + cdiv((int64_t)p->k_swa + rows_per_seq, kTile) + 1;
+    tiles = window < tiles ? window : tiles;
+  }
+  pl.min_tiles = 4;  // one per wave
+  const int64_t most = cdiv(pairs * tiles, pl.min_tiles);
+  pl.grid = (int)(most < 256 ? most : 256);
+  pl.cut = true;
+  // pages of a pass: tiles * 32 / P, and two more at the ends of each of two parts
+  const int64_t pass = (int64_t)(kPageSlots - 4) * kv_page_size / kTile;
+  pl.pass_tiles = (int)(pass < (1 << 26) ? pass : (1 << 26));
+  const size_t parts = pl.cut ? (size_t)2 * pl.grid * pl.block_cols : 0;
+  pl.off_ml = lsa::round_up(parts * p->d_v * 4, 256);
+  pl.total = pl.off_ml + lsa::round_up(parts * 2 * 4, 256);
+  return pl;
+}
+
 }  // namespace
 
 extern "C" {
@@ -173,7 +207,7 @@ lsa_status lsa_cache_append(const lsa_append_params* p, const lsa_append_tensors
 size_t lsa_decode_attn_workspace_size(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq,
                                       int32_t max_pages, int32_t kv_page_size) {
   if (check_decode_params(p) != LSA_OK || check_decode_sizes(p, n_seq, rows_per_seq, max_pages, kv_page_size) != LSA_OK) return 0;
-  return 0;
+  return n_seq == 0 || p->latent ? 0 : plan_decode(p, n_seq, rows_per_seq, max_pages, kv_page_size).total;
 }
 
 lsa_status lsa_decode_attn(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq, const void* q,
@@ -225,10 +259,21 @@ lsa_status lsa_decode_attn(const lsa_decode_attn_params* p, int32_t n_seq, int32
   g.fp8 = fp8;
   g.max_pages = max_pages;
   g.P = kv_page_size;
-  // (without a window there is no separate sink)
-  g.k_swa = p->k_swa;
-  g.k_sink = p->k_swa > 0 ? p->k_sink : 0;
+  g.cap = max_pages * kv_page_size;
+  // (a window of all positions is none, and without a window there is no separate sink)
+  g.k_swa = p->k_swa < g.cap ? p->k_swa : 0;
+  g.k_sink = g.k_swa == 0 ? 0 : p->k_sink < g.cap ? p->k_sink : g.cap;
   g.scale_log2 = p->sm_scale * 1.4426950408889634f;
+  const DecodePlan pl = plan_decode(p, n_seq, rows_per_seq, max_pages, kv_page_size);
+  g.by_page = lsa::fast_div((uint32_t)kv_page_size);
+  g.pass_tiles = pl.pass_tiles;
+  g.block_cols = pl.block_cols;
+  g.grid = pl.grid;
+  g.min_tiles = pl.min_tiles;
+  if (pl.cut) {
+    g.part_o = static_cast<float*>(workspace);
+    g.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + pl.off_ml);
+  }
   const hipError_t e = lsa::launch_decode_attn(g, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "decode attention");
   return LSA_OK;
