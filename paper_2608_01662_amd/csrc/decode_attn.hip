@@ -41,14 +41,19 @@ __device__ __forceinline__ Span span_of(const DecodeGeom& g, int ctx) {
   return s;
 }
 
-// Tiles of all sequences (one key/value head), the same in every lane.
+// (wave-uniform values that the compiler cannot know to be: kept in scalar registers)
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+}
+// Tiles of all sequences (one key/value head).
 __device__ __forceinline__ int64_t all_tiles(const DecodeGeom& g) {
   const int lane = threadIdx.x & 63;
   int64_t sum = 0;
   for (int b0 = 0; b0 < g.n_seq; b0 += 64)
     if (b0 + lane < g.n_seq) sum += span_of(g, g.ctx_len[b0 + lane]).nt;
   for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
-  return sum;
+  return uniform(sum);
 }
 // Tiles a workgroup takes: an equal share of the `total` tiles of all (sequence, head)s, but no fewer than
 // pay for a workgroup.
@@ -71,12 +76,50 @@ __device__ __forceinline__ int find_seq(const DecodeGeom& g, int64_t at, int64_t
     const uint64_t past = __ballot(before + inc > at);
     if (past) {
       const int first = __ffsll((unsigned long long)past) - 1;
-      before += __shfl(inc - nt, first);
+      before += uniform((int64_t)__shfl(inc - nt, first));
       return b0 + first;
     }
-    before += __shfl(inc, 63);
+    before += uniform((int64_t)__shfl(inc, 63));
   }
   return g.n_seq;
+}
+
+// Deals this workgroup its stretch of the tiles of all sequences, M (head, query row block)s each, one
+// (sequence, head) after the other: segment(sequence, r in [0, M), span, first tile, last tile + 1, whole, slot
+// of the partial). Then the rows of sequences without a tile, dealt to the workgroups. d: width of an output row.
+template <class F>
+__device__ __forceinline__ void deal(const DecodeGeom& g, int M, int d, F&& segment) {
+  const int64_t total = all_tiles(g) * M, share = share_of(g, total);
+  int64_t at = blockIdx.x * share;
+  const int64_t start = at, end = at + share < total ? at + share : total;
+  if (at < end) {
+    int64_t before;
+    int b = find_seq(g, at / M, before);
+    while (at < end) {
+      const Span sp = span_of(g, uniform(g.ctx_len[b]));
+      if (sp.nt == 0) {
+        ++b;
+        continue;
+      }
+      const int64_t rel = at - before * M;
+      const int r = (int)(rel / sp.nt), t0 = (int)(rel - (int64_t)r * sp.nt);
+      const int n = end - at < sp.nt - t0 ? (int)(end - at) : sp.nt - t0;
+      segment(b, r, sp, t0, t0 + n, n == sp.nt, 2 * (int64_t)blockIdx.x + (at != start));
+      at += n;
+      if (r == M - 1 && t0 + n == sp.nt) {
+        before += sp.nt;
+        ++b;
+      }
+    }
+  }
+  const int64_t row_elems = (int64_t)g.R * g.H * d;
+  for (int b = blockIdx.x; b < g.n_seq; b += g.grid) {
+    if (span_of(g, g.ctx_len[b]).nt != 0) continue;
+    for (int64_t i = 8 * (int64_t)threadIdx.x; i < row_elems; i += 8 * (int64_t)blockDim.x)
+      *reinterpret_cast<u32x4*>(g.out + b * row_elems + i) = u32x4{};
+    if (g.lse)
+      for (int i = (int)threadIdx.x; i < g.R * g.H; i += (int)blockDim.x) g.lse[(int64_t)b * g.R * g.H + i] = -INFINITY;
+  }
 }
 
 // ---------------------------------------------------------------- direct global -> LDS loads
@@ -156,7 +199,7 @@ void gqa_decode_kernel(DecodeGeom g) {
   __shared__ float pm[kGqaWaves][16], pl[kGqaWaves][16];
   static_assert(16 * OS * 4 <= kGqaRing, "the accumulators are merged in the ring");
   const int lane = threadIdx.x & 63, q4 = lane >> 4, i16 = lane & 15;
-  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wv = uniform((int)(threadIdx.x >> 6));
   uint8_t* const lk = ring[wv];                    // K tiles, then V tiles
   uint8_t* const lv = ring[wv] + NS * T::kBytes;
   const int group = g.H / g.Hkv, cols = g.R * group;
@@ -471,51 +514,352 @@ void gqa_decode_kernel(DecodeGeom g) {
     }
   };
 
-  const int64_t total = all_tiles(g) * M, share = share_of(g, total);
-  int64_t at = blockIdx.x * share;
-  const int64_t start = at, end = at + share < total ? at + share : total;
-  if (at < end) {
-    int64_t before;
-    int b = find_seq(g, at / M, before);
-    while (at < end) {
-      const Span sp = span_of(g, g.ctx_len[b]);
-      if (sp.nt == 0) {
-        ++b;
-        continue;
+  deal(g, M, D, segment);
+}
+
+// ============================================================================ latent cache
+// One workgroup = eight waves = up to 64 heads of one new token. Two waves per SIMD, split by role as in the
+// sparse attention (attention.hip, whose tile and operand layouts these are): four scorers compute S^T = K Q^T of 16 tokens x 32 heads each, do the online
+// softmax and leave P (bf16) and the reference maximum of their token half in an LDS slot; four value waves,
+// one tile behind, accumulate O^T += V^T P^T for all heads and 128 value columns each, from V operands read a
+// tile ahead. One barrier per tile.
+//
+// Here the tiles are whole stretches of cache rows, so nothing is gathered through a list: a value wave's lane finds
+// the row of its token from the staged page-table entries. A call is bound by the cache's bytes, not by the
+// products, so kLatBufs tile buffers keep kLatBufs - 1 tiles on their way while one is scored (at barrier `it`
+// the buffer of tile it - 1 is free: its V operands are in registers).
+constexpr int kLatBufs = 4;
+constexpr int kLatPages = 1024;  // page-table entries staged in LDS at a time
+
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void latent_decode_kernel(DecodeGeom g) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kLatBufs * kMlaTile + 2 * kMlaPSlot];
+  __shared__ int pages[kLatPages];
+  __shared__ float fin[2 * 2 * 64];  // per (token half, head): reference maximum and sum
+  const int lane = threadIdx.x & 63, wv = uniform((int)(threadIdx.x >> 6));
+  const int i16 = lane & 15, q4 = lane >> 4, w4 = wv & 3;
+  const bool scorer = wv < 4;
+  uint8_t* const pslots = lds + kLatBufs * kMlaTile;
+  const uint8_t* kvb = static_cast<const uint8_t*>(g.k);
+  const int hb_n = (g.H + 63) / 64, M = g.R * hb_n;  // (new token, 64 heads)s of a sequence
+
+  auto segment = [&](int b, int r, const Span& sp, int t0, int t1, bool whole, int64_t slot) {
+    const int j = r / hb_n, h0 = (r - j * hb_n) * 64, nh = g.H - h0 < 64 ? g.H - h0 : 64;
+    const int tq = sp.c - g.R + j;  // this token's position
+    const int64_t row0 = ((int64_t)b * g.R + j) * g.H + h0;  // output row of head h0
+    // page-table entries of tiles [p0, p1): those before the skipped ones, then the others
+    int f1 = 0, n1 = 0, f2 = 0;
+    auto stage = [&](int p0, int p1) {
+      const int e1 = p1 < sp.ns ? p1 : sp.ns, b2 = p0 > sp.ns ? p0 : sp.ns;
+      int n2 = 0;
+      f1 = n1 = f2 = 0;
+      if (p0 < e1) {
+        f1 = fdiv(g.by_page, p0 * kTile);
+        const int last = e1 * kTile - 1 < sp.c ? e1 * kTile - 1 : sp.c - 1;
+        n1 = fdiv(g.by_page, last) - f1 + 1;
       }
-      const int64_t rel = at - before * M;
-      const int r = (int)(rel / sp.nt), t0 = (int)(rel - (int64_t)r * sp.nt);
-      const int n = end - at < sp.nt - t0 ? (int)(end - at) : sp.nt - t0;
-      segment(b, r, sp, t0, t0 + n, n == sp.nt, 2 * (int64_t)blockIdx.x + (at != start));
-      at += n;
-      if (r == M - 1 && t0 + n == sp.nt) {
-        before += sp.nt;
-        ++b;
+      if (b2 < p1) {
+        f2 = fdiv(g.by_page, (b2 + sp.skip) * kTile);
+        const int64_t end = (int64_t)(p1 + sp.skip) * kTile - 1;
+        n2 = fdiv(g.by_page, end < sp.c ? (int)end : sp.c - 1) - f2 + 1;
+      }
+      __syncthreads();  // the previous entries' readers are done
+      for (int i = (int)threadIdx.x; i < n1 + n2; i += 512) {
+        const int pg = i < n1 ? f1 + i : f2 + i - n1;
+        const int ph = g.page_table ? g.page_table[(int64_t)b * g.max_pages + pg] : b;
+        pages[i] = ph >= 0 && ph < g.n_phys ? ph : -1;
+      }
+      __syncthreads();
+    };
+    // cache row of token `tok` of tile t, -1 where this query does not attend to it
+    auto row_of = [&](int t, int tok) {
+      const int s = (t < sp.ns ? t : t + sp.skip) * kTile + tok;
+      if (s < 0 || s > tq || !(g.k_swa == 0 || tq - s < g.k_swa || s < g.k_sink)) return -1;
+      const int pg = fdiv(g.by_page, s);
+      const int ph = pages[t < sp.ns ? pg - f1 : n1 + pg - f2];
+      return ph >= 0 ? ph * g.P + (s - pg * g.P) : -1;
+    };
+    if (scorer) {
+      const int th = w4 & 1, pair = w4 >> 1;  // tokens 16 th .. + 15, heads 32 pair .. + 31
+      u32x4 qb[2][18];
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb) {
+        const int h = 32 * pair + 16 * nb + i16;
+        const u32x4* qp = reinterpret_cast<const u32x4*>(g.q + (row0 + (h < nh ? h : 0)) * 576 + 8 * q4);
+#pragma unroll
+        for (int s = 0; s < 18; ++s) qb[nb][s] = h < nh ? qp[4 * s] : u32x4{};
+      }
+      const int ksw = mla_swz(i16 >> 3, i16 & 7);
+      const int k_row = th * kMlaHalf + 9 * (i16 >> 3) * 1024 + 8 * (i16 & 7) * 16;
+      const int k_even = k_row + ((0 + q4) ^ ksw) * 16, k_odd = k_row + ((4 + q4) ^ ksw) * 16;
+      float m[2] = {kNoRef, kNoRef}, l[2] = {0.f, 0.f};
+      for (int p0 = t0; p0 < t1; p0 += g.pass_tiles) {
+        const int nt = t1 - p0 < g.pass_tiles ? t1 - p0 : g.pass_tiles;
+        stage(p0, p0 + nt);
+        uint32_t cur = 0;
+        for (int it = 0; it <= nt; ++it) {
+          // tile it has landed; this scorer's P of tile it - 1 is written
+          asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          const uint8_t* tb = lds + __builtin_amdgcn_readfirstlane(cur);
+          cur = cur + kMlaTile == kLatBufs * kMlaTile ? 0 : cur + kMlaTile;
+          if (it == nt) continue;  // (the value waves' last tile)
+          const uint32_t vmask = (uint32_t)__ballot(row_of(p0 + it, lane & 31) >= 0);
+          float mp[2] = {-INFINITY, -INFINITY};  // the other token half's reference of tile it - 1
+          if (it > 0) {
+            const uint8_t* pr = pslots + ((it - 1) & 1) * kMlaPSlot + 64 * kMlaPHead + (1 - th) * 256;
+#pragma unroll
+            for (int nb = 0; nb < 2; ++nb) mp[nb] = *reinterpret_cast<const float*>(pr + 4 * (32 * pair + 16 * nb + i16));
+          }
+          constexpr int KB = 3;  // K operands requested ahead of the products
+          f32x4 sacc[2] = {f32x4{}, f32x4{}};
+          u32x4 ka[2][KB];
+#pragma unroll
+          for (int s6 = 0; s6 < KB; ++s6) ka[0][s6] = *reinterpret_cast<const u32x4*>(tb + ((s6 & 1) ? k_odd : k_even) + (s6 >> 1) * 1024);
+#pragma unroll
+          for (int bt = 0; bt < 18 / KB; ++bt) {
+            if (bt + 1 < 18 / KB) {
+#pragma unroll
+              for (int s6 = 0; s6 < KB; ++s6) {
+                const int s = KB * (bt + 1) + s6;
+                ka[(bt + 1) & 1][s6] = *reinterpret_cast<const u32x4*>(tb + ((s & 1) ? k_odd : k_even) + (s >> 1) * 1024);
+              }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int s6 = 0; s6 < KB; ++s6)
+#pragma unroll
+              for (int nb = 0; nb < 2; ++nb) sacc[nb] = mfma16(ka[bt & 1][s6], qb[nb][KB * bt + s6], sacc[nb]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          const uint32_t hmask = (vmask >> (16 * th)) & 0xFFFFu;
+          if (hmask != 0xFFFFu) {
+#pragma unroll
+            for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) sacc[nb][k] = ((hmask >> (4 * q4 + k)) & 1u) ? sacc[nb][k] : -INFINITY;
+          }
+          uint8_t* ps = pslots + (it & 1) * kMlaPSlot;
+          float smx[2];
+#pragma unroll
+          for (int nb = 0; nb < 2; ++nb) smx[nb] = fmaxf(fmaxf(sacc[nb][0], sacc[nb][1]), fmaxf(sacc[nb][2], sacc[nb][3]));
+          max4_xor16_32_pair(smx[0], smx[1]);
+#pragma unroll
+          for (int nb = 0; nb < 2; ++nb) {
+            const float mx = smx[nb] * g.scale_log2;
+            // the reference moves when the maximum grows by more than 2^8, or to the other half's when that is larger
+            float tgt = mx > m[nb] + kLazy ? mx : m[nb];
+            tgt = fmaxf(tgt, mp[nb]);
+            const bool up = tgt > m[nb];
+            if (__ballot(up)) {
+              l[nb] = up ? l[nb] * fast_exp2(m[nb] - tgt) : l[nb];
+              m[nb] = up ? tgt : m[nb];
+            }
+            float p[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              p[k] = fast_exp2(fmaf(sacc[nb][k], g.scale_log2, -m[nb]));  // -inf -> 0
+              l[nb] += p[k];
+            }
+            const int lh = 32 * pair + 16 * nb + i16;
+            *reinterpret_cast<u32x2*>(ps + lh * kMlaPHead + 32 * th + 8 * q4) = u32x2{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])};
+            if (q4 == 0) *reinterpret_cast<float*>(ps + 64 * kMlaPHead + th * 256 + 4 * lh) = m[nb];
+          }
+        }
+      }
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb) {
+        const float lt = sum4_xor16_32(l[nb]);
+        if (q4 == 0) {
+          const int lh = 32 * pair + 16 * nb + i16;
+          fin[2 * (64 * th + lh)] = m[nb];
+          fin[2 * (64 * th + lh) + 1] = lt;
+        }
+      }
+      __syncthreads();
+      return;
+    }
+    // ---- value wave w4: columns 128 w4 .. + 127 of all heads
+    const int G = lane >> 4, sl = lane & 15;
+    int v_off[2][2];
+#pragma unroll
+    for (int rd = 0; rd < 2; ++rd)
+#pragma unroll
+      for (int par = 0; par < 2; ++par) {
+        const int tk = 8 * (G >> 1) + 4 * rd + (sl >> 2), o8 = tk >> 3, j8 = tk & 7;
+        const int ch = 4 * par + 2 * (G & 1) + ((sl >> 1) & 1);
+        v_off[rd][par] = (9 * o8 + 2 * w4) * 1024 + (8 * j8 + (ch ^ mla_swz(o8, j8))) * 16 + (sl & 1) * 8;
+      }
+    const int oj = lane & 31;
+    f32x16 o[8];  // block 4 hb + c: heads 32 hb .., dims 128 w4 + 32 c ..
+#pragma unroll
+    for (int c = 0; c < 8; ++c) o[c] = f32x16{};
+    float m_o[2] = {-INFINITY, -INFINITY};  // reference maxima of the accumulators
+    // this wave loads tokens 8 w4 .. of a tile: lane 8 jj + u takes chunk u ^ swz of token jj of them, nine times
+    const int dj = lane >> 3, dma_tok = 8 * w4 + dj;
+    const int64_t dma_col = ((lane & 7) ^ mla_swz(w4, dj)) * 16;
+    for (int p0 = t0; p0 < t1; p0 += g.pass_tiles) {
+      const int nt = t1 - p0 < g.pass_tiles ? t1 - p0 : g.pass_tiles;
+      stage(p0, p0 + nt);
+      auto issue = [&](int it, uint32_t buf) {
+        const int row = row_of(p0 + it, dma_tok);
+        lds_dma_row9((row >= 0 ? kvb + (int64_t)row * 1152 : zero_row) + dma_col, lds_addr(lds + buf + w4 * (kMlaLoads * 1024)));
+      };
+      uint32_t cur = 0, next = 0;  // buffers of tile it, and of the next tile to load
+#pragma unroll
+      for (int i = 0; i < kLatBufs - 1; ++i)
+        if (i < nt) {
+          issue(i, next);
+          next += kMlaTile;
+        }
+      u32x4 va[4][2];  // V operands of tile it - 1
+      for (int it = 0; it <= nt; ++it) {
+        // tile it has landed (behind it are the kLatBufs - 2 next ones, fewer at the end); the scorers' P of tile
+        // it - 1 is in its slot; the buffer of tile it - 1 is free
+        if (it + kLatBufs - 2 < nt) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kMlaLoads * (kLatBufs - 2)) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (it + kLatBufs - 1 < nt) {
+          issue(it + kLatBufs - 1, next = next == kLatBufs * kMlaTile ? 0 : next);
+          next += kMlaTile;
+        }
+        const uint32_t at = cur;
+        cur = cur + kMlaTile == kLatBufs * kMlaTile ? 0 : cur + kMlaTile;
+        auto read_v = [&]() {
+          const uint8_t* tp = lds + __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+              va[c][ks] = tr16_pair(tp + v_off[0][c & 1] + ks * kMlaHalf + (c >> 1) * 1024, tp + v_off[1][c & 1] + ks * kMlaHalf + (c >> 1) * 1024);
+        };
+        if (it == 0) {  // (nothing scored yet)
+          read_v();
+          continue;
+        }
+        const uint8_t* ps = pslots + ((it - 1) & 1) * kMlaPSlot;
+        float mA[2], mB[2];
+#pragma unroll
+        for (int hb = 0; hb < 2; ++hb) {
+          mA[hb] = *reinterpret_cast<const float*>(ps + 64 * kMlaPHead + 4 * (32 * hb + oj));
+          mB[hb] = *reinterpret_cast<const float*>(ps + 64 * kMlaPHead + 256 + 4 * (32 * hb + oj));
+        }
+        u32x4 pb[2][2];
+#pragma unroll
+        for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+          for (int ks = 0; ks < 2; ++ks)
+            pb[hb][ks] = *reinterpret_cast<const u32x4*>(ps + (32 * hb + oj) * kMlaPHead + 32 * ks + 16 * (lane >> 5));
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int hb = 0; hb < 2; ++hb) {
+          const float mn = fmaxf(mA[hb], mB[hb]);  // >= m_o: the references never decrease
+          if (__ballot(mA[hb] != mB[hb] || mn > m_o[hb])) {  // rare once the halves agree
+            const float alpha = mn > m_o[hb] ? fast_exp2(m_o[hb] - mn) : 1.f;  // m_o = -inf -> 0
+            m_o[hb] = mn;
+            if (__ballot(alpha != 1.f)) {
+#pragma unroll
+              for (int c = 0; c < 4; ++c) o[4 * hb + c] *= alpha;
+            }
+            const float fa = mA[hb] == mn ? 1.f : fast_exp2(mA[hb] - mn), fb = mB[hb] == mn ? 1.f : fast_exp2(mB[hb] - mn);
+            if (__ballot(fa != 1.f)) pb[hb][0] = scale_bf16x8(pb[hb][0], fa);
+            if (__ballot(fb != 1.f)) pb[hb][1] = scale_bf16x8(pb[hb][1], fb);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int hb = 0; hb < 2; ++hb) o[4 * hb + c] = mfma32(va[c][ks], pb[hb][ks], o[4 * hb + c]);
+        if (it < nt) {
+          __builtin_amdgcn_sched_barrier(0);
+          read_v();
+        }
       }
     }
-  }
-  // sequences without a tile: empty rows, dealt to the workgroups
-  const int64_t row_elems = (int64_t)g.R * g.H * D;
-  for (int b = blockIdx.x; b < g.n_seq; b += g.grid) {
-    if (span_of(g, g.ctx_len[b]).nt != 0) continue;
-    for (int64_t i = 8 * (int64_t)threadIdx.x; i < row_elems; i += 8 * 64 * kGqaWaves) *reinterpret_cast<u32x4*>(g.out + b * row_elems + i) = u32x4{};
-    if (g.lse)
-      for (int i = (int)threadIdx.x; i < g.R * g.H; i += 64 * kGqaWaves) g.lse[(int64_t)b * g.R * g.H + i] = -INFINITY;
-  }
+    __syncthreads();  // the scorers' reference maxima and sums
+    float mfin[2], lt[2];
+#pragma unroll
+    for (int hb = 0; hb < 2; ++hb) {
+      const int lh = 32 * hb + oj;
+      const float ma = fin[2 * lh], la = fin[2 * lh + 1], mb = fin[2 * (64 + lh)], lb = fin[2 * (64 + lh) + 1];
+      mfin[hb] = fmaxf(ma, mb);
+      lt[hb] = la * fast_exp2(ma - mfin[hb]) + lb * fast_exp2(mb - mfin[hb]);
+      if (w4 == 0 && lane < 32 && lh < nh) {
+        if (whole) {
+          if (g.lse) g.lse[row0 + lh] = lt[hb] == 0.f ? -INFINITY : (mfin[hb] + __log2f(lt[hb])) * kLn2;
+        } else {
+          *reinterpret_cast<f32x2*>(g.part_ml + 2 * (slot * 64 + lh)) = f32x2{mfin[hb], lt[hb]};
+        }
+      }
+    }
+    // This wave's accumulators (64 heads x 128 columns) go head by head through the tile buffers, idle since the
+    // barrier, so that a store instruction writes whole lines: 32 heads at a time in fp32 (a partial), or all in bf16.
+    // Lane l, register r of block 4 hb + c holds column 32 c + 8 (r / 4) + 4 (l / 32) + r % 4 of head 32 hb + l % 32.
+    // (the lane made opaque here, or these offsets are computed before the loop over stretches and spill)
+    int el = lane;
+    asm volatile("" : "+v"(el));
+    const int ej = el & 31;
+    if (whole) {
+      uint8_t* ost = lds + w4 * (64 * 272);
+#pragma unroll
+      for (int hb = 0; hb < 2; ++hb) {
+        const float inv = lt[hb] == 0.f ? 0.f : 1.f / lt[hb];
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x16& ob = o[4 * hb + c];
+            *reinterpret_cast<u32x2*>(ost + (32 * hb + ej) * 272 + (32 * c + 8 * q + 4 * (el >> 5)) * 2) =
+                u32x2{pack_bf16x2(ob[4 * q] * inv, ob[4 * q + 1] * inv), pack_bf16x2(ob[4 * q + 2] * inv, ob[4 * q + 3] * inv)};
+          }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (this wave's own writes)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const int hh = 4 * k + (el >> 4);
+        const u32x4 v = *reinterpret_cast<const u32x4*>(ost + hh * 272 + 16 * (el & 15));
+        if (hh < nh) *reinterpret_cast<u32x4*>(g.out + (row0 + hh) * 512 + 128 * w4 + 8 * (el & 15)) = v;
+      }
+    } else {
+      uint8_t* ost = lds + w4 * (32 * 528);
+#pragma unroll
+      for (int hb = 0; hb < 2; ++hb) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x16& ob = o[4 * hb + c];
+            *reinterpret_cast<f32x4*>(ost + ej * 528 + (32 * c + 8 * q + 4 * (el >> 5)) * 4) = f32x4{ob[4 * q], ob[4 * q + 1], ob[4 * q + 2], ob[4 * q + 3]};
+          }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          const int hh = 2 * k + (el >> 5);
+          const f32x4 v = *reinterpret_cast<const f32x4*>(ost + hh * 528 + 16 * (el & 31));
+          if (32 * hb + hh < nh) *reinterpret_cast<f32x4*>(g.part_o + (slot * 64 + 32 * hb + hh) * 512 + 128 * w4 + 4 * (el & 31)) = v;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      }
+    }
+  };
+  deal(g, M, 512, segment);
 }
 
 // ============================================================================ joining the partials
 // One workgroup per (sequence, head, column): nothing to do where one stretch covered it whole. The threads
 // take four dims each, in groups that share the partials and keep a running maximum of their own.
-template <int D, int COLS>
+template <int D, int COLS, bool LATENT>
 __global__ __launch_bounds__(256) void decode_join_kernel(DecodeGeom g) {
   constexpr int Q = D / 4, SUBS = 256 / Q, U = 4;
   __shared__ __attribute__((aligned(16))) float acc_s[SUBS][D];
   __shared__ float m_s[SUBS], l_s[SUBS];
-  const int group = g.H / g.Hkv, cols = g.R * group, cb_n = (cols + COLS - 1) / COLS, M = g.Hkv * cb_n;
-  const int64_t pair = blockIdx.x / cols;  // (sequence, key/value head)
-  const int col = (int)(blockIdx.x - pair * cols);
-  const int b = (int)(pair / g.Hkv), kvh = (int)(pair - (int64_t)b * g.Hkv), r = kvh * cb_n + col / COLS;
+  // columns of a unit: query rows of a (sequence, key/value head), or heads of a (sequence, new token)
+  const int group = g.H / g.Hkv, cols = LATENT ? g.H : g.R * group, units = LATENT ? g.R : g.Hkv;
+  const int cb_n = (cols + COLS - 1) / COLS, M = units * cb_n;
+  const int64_t unit = blockIdx.x / cols;
+  const int col = (int)(blockIdx.x - unit * cols);
+  const int b = (int)(unit / units), un = (int)(unit - (int64_t)b * units), r = un * cb_n + col / COLS;
   int64_t before = 0, all = 0;  // tiles of the sequences before b, and of all
   {
     const int lane = threadIdx.x & 63;
@@ -579,67 +923,11 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeGeom g) {
     sum += l_s[s] * f;
     o += f * *reinterpret_cast<const f32x4*>(&acc_s[s][d]);
   }
-  const int j = col / group;
-  const int64_t row = ((int64_t)b * g.R + j) * g.H + kvh * group + col - j * group;
+  const int j = LATENT ? un : col / group;
+  const int64_t row = ((int64_t)b * g.R + j) * g.H + (LATENT ? col : un * group + col - j * group);
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   *reinterpret_cast<u32x2*>(g.out + row * D + d) = u32x2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
   if (g.lse && d == 0) g.lse[row] = sum == 0.f ? -INFINITY : (mx + __log2f(sum)) * kLn2;
-}
-
-// ============================================================================ latent cache
-// One wave per (row, head), 64 positions at a time: a lane scores one position, then holds d_v / 64 columns
-// of the output. The plain form of the operator: every head reads its rows by itself.
-__global__ __launch_bounds__(64) void latent_decode_kernel(DecodeGeom g) {
-  __shared__ float qs[576];
-  __shared__ float ps[64];
-  __shared__ int rows[64];
-  const int lane = threadIdx.x;
-  const int64_t r = blockIdx.x / g.H;
-  const int h = (int)(blockIdx.x - r * g.H);
-  const int b = (int)(r / g.R), j = (int)(r - (int64_t)b * g.R);
-  for (int i = lane; i < g.d_qk; i += 64) qs[i] = __uint_as_float((uint32_t)g.q[(r * g.H + h) * g.d_qk + i] << 16);
-  const int ctx = g.ctx_len[b];
-  const int t = ctx < 0 || ctx > g.max_pages * g.P ? -1 : ctx - g.R + j;
-  const int cols = g.d_v / 64;
-  float o[8] = {}, m = -INFINITY, l = 0.f;
-  auto value = [&](const void* base, int64_t row, int d, int i) {
-    return __uint_as_float((uint32_t) static_cast<const uint16_t*>(base)[row * d + i] << 16);
-  };
-  __syncthreads();
-  for (int s0 = 0; s0 <= t; s0 += 64) {
-    const int s = s0 + lane;
-    bool seen = s <= t && (g.k_swa == 0 || s > t - g.k_swa || s < g.k_sink);
-    int64_t ph = -1;
-    if (seen) ph = g.page_table ? g.page_table[(int64_t)b * g.max_pages + s / g.P] : b;
-    seen = seen && ph >= 0 && ph < g.n_phys;
-    const int64_t row = ph * g.P + s % g.P;
-    float z = -INFINITY;
-    if (seen) {
-      float acc = 0.f;
-      for (int i = 0; i < g.d_qk; ++i) acc += qs[i] * value(g.k, row, g.d_qk, i);
-      z = acc * g.scale_log2;
-    }
-    const float mx = fmaxf(wave_max(z), m);
-    const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx);
-    const float p = seen && z != -INFINITY ? __builtin_amdgcn_exp2f(z - mx) : 0.f;
-    float sum = p;
-    for (int x = 32; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
-    l = l * alpha + sum;
-    m = mx;
-    ps[lane] = p;
-    rows[lane] = seen ? (int)row : -1;
-    __syncthreads();
-    for (int c = 0; c < cols; ++c) o[c] *= alpha;
-    for (int k = 0; k < 64; ++k) {
-      if (rows[k] < 0) continue;
-      for (int c = 0; c < cols; ++c) o[c] += ps[k] * value(g.k, rows[k], g.d_qk, 64 * c + lane);
-    }
-    __syncthreads();
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  for (int c = 0; c < cols; ++c)
-    g.out[(r * g.H + h) * g.d_v + 64 * c + lane] = (uint16_t)pack_bf16x2(l == 0.f ? 0.f : o[c] * inv, 0.f);
-  if (g.lse && lane == 0) g.lse[r * g.H + h] = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
 // ============================================================================ host launchers
@@ -649,7 +937,7 @@ static hipError_t launch_gqa(const DecodeGeom& g, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.part_o == nullptr) return e;
   const int64_t blocks = (int64_t)g.n_seq * g.R * g.H;
-  hipLaunchKernelGGL((decode_join_kernel<D, 16 * NB>), dim3((unsigned)blocks), dim3(256), 0, st, g);
+  hipLaunchKernelGGL((decode_join_kernel<D, 16 * NB, false>), dim3((unsigned)blocks), dim3(256), 0, st, g);
   return hipGetLastError();
 }
 template <int D, bool FP8>
@@ -660,7 +948,10 @@ static hipError_t launch_gqa(const DecodeGeom& g, hipStream_t st) {
 
 hipError_t launch_decode_attn(const DecodeGeom& g, hipStream_t st) {
   if (g.latent) {
-    hipLaunchKernelGGL(latent_decode_kernel, dim3((unsigned)(g.n_seq * g.R * g.H)), dim3(64), 0, st, g);
+    hipLaunchKernelGGL(latent_decode_kernel, dim3((unsigned)g.grid), dim3(512), 0, st, g);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || g.part_o == nullptr) return e;
+    hipLaunchKernelGGL((decode_join_kernel<512, 64, true>), dim3((unsigned)((int64_t)g.n_seq * g.R * g.H)), dim3(256), 0, st, g);
     return hipGetLastError();
   }
   if (g.d_qk == 64) return g.fp8 ? launch_gqa<64, true>(g, st) : launch_gqa<64, false>(g, st);

@@ -80,13 +80,16 @@ struct DecodePlan {
 };
 constexpr int kTile = 32;          // positions of a tile
 constexpr int kPageSlots = 2048;   // page-table entries a workgroup stages at a time
+constexpr int kLatentPages = 1024; // the same, latent cache
 
 DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq, int32_t max_pages,
                        int32_t kv_page_size) {
   DecodePlan pl{};
-  const int64_t cols = (int64_t)rows_per_seq * (p->n_heads / p->n_kv_heads);
-  pl.block_cols = cols <= 16 ? 16 : cols <= 32 ? 32 : 64;
-  const int64_t pairs = (int64_t)n_seq * p->n_kv_heads * cdiv(cols, pl.block_cols);
+  // grouped heads: the query rows of a key/value head, in blocks; latent: 64 heads of one new token
+  const bool latent = p->latent != 0;
+  const int64_t cols = latent ? p->n_heads : (int64_t)rows_per_seq * (p->n_heads / p->n_kv_heads);
+  pl.block_cols = latent ? 64 : cols <= 16 ? 16 : cols <= 32 ? 32 : 64;
+  const int64_t pairs = (int64_t)n_seq * (latent ? rows_per_seq : p->n_kv_heads) * cdiv(cols, pl.block_cols);
   const int64_t cap = (int64_t)max_pages * kv_page_size;
   int64_t tiles = cdiv(cap, kTile);  // of one (sequence, head), at most
   if (p->k_swa > 0) {
@@ -98,7 +101,7 @@ DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t r
   pl.grid = (int)(most < 256 ? most : 256);
   pl.cut = true;
   // pages of a pass: tiles * 32 / P, and two more at the ends of each of two parts
-  const int64_t pass = (int64_t)(kPageSlots - 4) * kv_page_size / kTile;
+  const int64_t pass = (int64_t)((latent ? kLatentPages : kPageSlots) - 4) * kv_page_size / kTile;
   pl.pass_tiles = (int)(pass < (1 << 26) ? pass : (1 << 26));
   const size_t parts = pl.cut ? (size_t)2 * pl.grid * pl.block_cols : 0;
   pl.off_ml = lsa::round_up(parts * p->d_v * 4, 256);
@@ -207,7 +210,7 @@ lsa_status lsa_cache_append(const lsa_append_params* p, const lsa_append_tensors
 size_t lsa_decode_attn_workspace_size(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq,
                                       int32_t max_pages, int32_t kv_page_size) {
   if (check_decode_params(p) != LSA_OK || check_decode_sizes(p, n_seq, rows_per_seq, max_pages, kv_page_size) != LSA_OK) return 0;
-  return n_seq == 0 || p->latent ? 0 : plan_decode(p, n_seq, rows_per_seq, max_pages, kv_page_size).total;
+  return n_seq == 0 ? 0 : plan_decode(p, n_seq, rows_per_seq, max_pages, kv_page_size).total;
 }
 
 lsa_status lsa_decode_attn(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq, const void* q,
