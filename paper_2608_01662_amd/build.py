@@ -30,7 +30,8 @@ HIPCC_FLAGS = [
 # The attention kernels never produce a NaN from finite inputs (masked scores are -inf and every
 # difference of two -inf is guarded): without NaN semantics the softmax maxima compile to plain
 # v_max_f32, without the canonicalising v_max_f32 x, x, x in front of each operand.
-EXTRA_FLAGS = {"indexer.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "attention.hip": ["-fno-honor-nans"]}
+EXTRA_FLAGS = {"indexer.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "attention.hip": ["-fno-honor-nans"],
+               "decode_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _hipcc() -> str:

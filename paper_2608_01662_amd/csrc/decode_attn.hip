@@ -163,16 +163,17 @@ __device__ __forceinline__ u32x2 tr8(const uint8_t* p) {
 // (g = lane / 16) the scores of tokens 8 g .. + 7 of its column, which is the layout of the B operand of
 // O^T += V^T P^T: P never leaves the registers.
 constexpr int kGqaWaves = 4;
-constexpr int kGqaRing = 32 * 1024;   // LDS ring bytes per wave
 constexpr int kPageSlots = 2048;      // page-table entries staged in LDS at a time
 
-template <int D, bool FP8>
+template <int D, bool FP8, int NB>
 struct GqaTile {
+  static constexpr int kPerCu = gqa_per_cu(D, NB);
+  static constexpr int kRing = 32 * 1024 / kPerCu;        // LDS ring bytes per wave
   static constexpr int kRow = D * (FP8 ? 1 : 2);          // bytes of a cache row
   static constexpr int kBytes = kTile * kRow;             // of a K or V tile
   static constexpr int kChunks = kRow / 16;               // 16-byte chunks of a row
   static constexpr int kLoads = kBytes / 1024;            // direct loads of a K or V tile
-  static constexpr int kStages = kGqaRing / (2 * kBytes); // tiles in the ring
+  static constexpr int kStages = kRing / (2 * kBytes); // tiles in the ring
   static constexpr int kK = kLoads + (FP8 ? 1 : 0);       // loads issued with K: its rows, and both scales
   static constexpr int kPair = kK + kLoads;
   // Chunk c of token t lies in 16-byte slot c ^ swz(t) of its row. The K reads (16 tokens of one chunk per 16
@@ -188,16 +189,16 @@ struct GqaTile {
 };
 
 template <int D, bool FP8, int NB>
-__global__ __launch_bounds__(64 * kGqaWaves) __attribute__((amdgpu_waves_per_eu(1, 1)))
+__global__ __launch_bounds__(64 * kGqaWaves) __attribute__((amdgpu_waves_per_eu(gqa_per_cu(D, NB), gqa_per_cu(D, NB))))
 void gqa_decode_kernel(DecodeGeom g) {
-  using T = GqaTile<D, FP8>;
+  using T = GqaTile<D, FP8, NB>;
   constexpr int NS = T::kStages, KS = D / 32, CD = D / 16, COLS = 16 * NB;
   constexpr int OS = D + 4;  // floats per column of a merged accumulator
-  __shared__ __attribute__((aligned(1024))) uint8_t ring[kGqaWaves][kGqaRing];
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[kGqaWaves][T::kRing];
   __shared__ __attribute__((aligned(16))) float scales[FP8 ? kGqaWaves : 1][FP8 ? NS : 1][64];
   __shared__ int pages[kPageSlots];
   __shared__ float pm[kGqaWaves][16], pl[kGqaWaves][16];
-  static_assert(16 * OS * 4 <= kGqaRing, "the accumulators are merged in the ring");
+  static_assert(16 * OS * 4 <= T::kRing, "the accumulators are merged in the ring");
   const int lane = threadIdx.x & 63, q4 = lane >> 4, i16 = lane & 15;
   const int wv = uniform((int)(threadIdx.x >> 6));
   uint8_t* const lk = ring[wv];                    // K tiles, then V tiles
@@ -470,20 +471,24 @@ void gqa_decode_kernel(DecodeGeom g) {
       }
       __syncthreads();  // every wave is done with `pages` and its ring
     }
-    // ---- the waves' results, 16 columns at a time: weighted by 2^(m_w - M) and summed
+    // ---- the waves' results, 16 columns at a time: weighted by 2^(m_w - M) and summed. (The lane is made
+    // opaque, or these offsets are computed before the loop over stretches and spill.)
+    int el = lane;
+    asm volatile("" : "+v"(el));
+    const int e16 = el & 15, e4 = el >> 4;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       if (16 * nb >= ncols) break;
       float* po = reinterpret_cast<float*>(ring[wv]);
 #pragma unroll
-      for (int c = 0; c < CD; ++c) *reinterpret_cast<f32x4*>(po + i16 * OS + 16 * c + 4 * q4) = o[nb][c];
+      for (int c = 0; c < CD; ++c) *reinterpret_cast<f32x4*>(po + e16 * OS + 16 * c + 4 * e4) = o[nb][c];
       const float lt = sum4_xor16_32(l[nb]);
-      if (q4 == 0) {
-        pm[wv][i16] = m[nb];
-        pl[wv][i16] = lt;
+      if (e4 == 0) {
+        pm[wv][e16] = m[nb];
+        pl[wv][e16] = lt;
       }
       __syncthreads();
-      for (int u = (int)threadIdx.x; u < 16 * (D / 4); u += 64 * kGqaWaves) {
+      for (int u = 64 * wv + el; u < 16 * (D / 4); u += 64 * kGqaWaves) {
         const int col = u / (D / 4), d = 4 * (u % (D / 4));
         if (16 * nb + col >= ncols) break;
         float mx = pm[0][col];
@@ -847,12 +852,15 @@ void latent_decode_kernel(DecodeGeom g) {
 }
 
 // ============================================================================ joining the partials
-// One workgroup per (sequence, head, column): nothing to do where one stretch covered it whole. The threads
-// take four dims each, in groups that share the partials and keep a running maximum of their own.
-template <int D, int COLS, bool LATENT>
+// One workgroup per output row and 4 Q of its dims: nothing to do where one stretch covered it whole. A thread
+// takes four dims, and 256 / Q groups of threads share the partials, with a running maximum each. Bound by the
+// round trips to partials that other XCDs have just written: calls of few rows, whose rows have many partials,
+// take few dims per workgroup, so that every thread has few of them.
+constexpr int64_t kJoinFew = 2048;  // workgroups of 32 dims
+template <int D, int COLS, bool LATENT, int Q>
 __global__ __launch_bounds__(256) void decode_join_kernel(DecodeGeom g) {
-  constexpr int Q = D / 4, SUBS = 256 / Q, U = 4;
-  __shared__ __attribute__((aligned(16))) float acc_s[SUBS][D];
+  constexpr int SUBS = 256 / Q, U = 4;
+  __shared__ __attribute__((aligned(16))) float acc_s[SUBS][4 * Q];
   __shared__ float m_s[SUBS], l_s[SUBS];
   // columns of a unit: query rows of a (sequence, key/value head), or heads of a (sequence, new token)
   const int group = g.H / g.Hkv, cols = LATENT ? g.H : g.R * group, units = LATENT ? g.R : g.Hkv;
@@ -878,7 +886,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeGeom g) {
   const int64_t share = share_of(g, all * M), first = before * M + (int64_t)r * nt;
   const int64_t w0 = first / share, w1 = (first + nt - 1) / share;
   if (nt == 0 || w0 == w1) return;  // (uniform)
-  const int sub = threadIdx.x / Q, d = 4 * (threadIdx.x % Q), cc = col % COLS;
+  const int sub = threadIdx.x / Q, dl = 4 * (threadIdx.x % Q), d = 4 * Q * (int)blockIdx.y + dl, cc = col % COLS;
   // the first stretch may have begun with another head: then this one's partial is its second
   auto slot = [&](int64_t w) { return (2 * w + (w == w0 && first != w0 * share)) * COLS + cc; };
   float m = kNoRef, l = 0.f;
@@ -907,8 +915,8 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeGeom g) {
     }
     m = mx;
   }
-  *reinterpret_cast<f32x4*>(&acc_s[sub][d]) = acc;
-  if (d == 0) {
+  *reinterpret_cast<f32x4*>(&acc_s[sub][dl]) = acc;
+  if (dl == 0) {
     m_s[sub] = m;
     l_s[sub] = l;
   }
@@ -921,7 +929,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeGeom g) {
   for (int s = 0; s < SUBS; ++s) {
     const float f = fast_exp2(m_s[s] - mx);
     sum += l_s[s] * f;
-    o += f * *reinterpret_cast<const f32x4*>(&acc_s[s][d]);
+    o += f * *reinterpret_cast<const f32x4*>(&acc_s[s][dl]);
   }
   const int j = LATENT ? un : col / group;
   const int64_t row = ((int64_t)b * g.R + j) * g.H + (LATENT ? col : un * group + col - j * group);
@@ -931,14 +939,21 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeGeom g) {
 }
 
 // ============================================================================ host launchers
+template <int D, int COLS, bool LATENT>
+static hipError_t launch_join(const DecodeGeom& g, hipStream_t st) {
+  const int64_t rows = (int64_t)g.n_seq * g.R * g.H;
+  if (rows * (D / 32) <= kJoinFew)
+    hipLaunchKernelGGL((decode_join_kernel<D, COLS, LATENT, 8>), dim3((unsigned)rows, D / 32), dim3(256), 0, st, g);
+  else
+    hipLaunchKernelGGL((decode_join_kernel<D, COLS, LATENT, D / 4>), dim3((unsigned)rows), dim3(256), 0, st, g);
+  return hipGetLastError();
+}
 template <int D, bool FP8, int NB>
 static hipError_t launch_gqa(const DecodeGeom& g, hipStream_t st) {
   hipLaunchKernelGGL((gqa_decode_kernel<D, FP8, NB>), dim3((unsigned)g.grid), dim3(64 * kGqaWaves), 0, st, g);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.part_o == nullptr) return e;
-  const int64_t blocks = (int64_t)g.n_seq * g.R * g.H;
-  hipLaunchKernelGGL((decode_join_kernel<D, 16 * NB, false>), dim3((unsigned)blocks), dim3(256), 0, st, g);
-  return hipGetLastError();
+  return launch_join<D, 16 * NB, false>(g, st);
 }
 template <int D, bool FP8>
 static hipError_t launch_gqa(const DecodeGeom& g, hipStream_t st) {
@@ -951,8 +966,7 @@ hipError_t launch_decode_attn(const DecodeGeom& g, hipStream_t st) {
     hipLaunchKernelGGL(latent_decode_kernel, dim3((unsigned)g.grid), dim3(512), 0, st, g);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || g.part_o == nullptr) return e;
-    hipLaunchKernelGGL((decode_join_kernel<512, 64, true>), dim3((unsigned)((int64_t)g.n_seq * g.R * g.H)), dim3(256), 0, st, g);
-    return hipGetLastError();
+    return launch_join<512, 64, true>(g, st);
   }
   if (g.d_qk == 64) return g.fp8 ? launch_gqa<64, true>(g, st) : launch_gqa<64, false>(g, st);
   return g.fp8 ? launch_gqa<128, true>(g, st) : launch_gqa<128, false>(g, st);

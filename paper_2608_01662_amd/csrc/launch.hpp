@@ -150,6 +150,8 @@ struct DecodeGeom {
   int min_tiles;      // tiles that pay for a workgroup
   float *part_o, *part_ml;  // two partials per workgroup: [block_cols, d_v], [block_cols, 2]; nullptr: none is cut
 };
+// Workgroups of the grouped-head kernel per CU: two where the registers of NB blocks of 16 query rows allow it.
+constexpr int gqa_per_cu(int d, int nb) { return nb * d <= 256 ? 2 : 1; }
 hipError_t launch_decode_attn(const DecodeGeom& g, hipStream_t st);
 
 }  // namespace lsa

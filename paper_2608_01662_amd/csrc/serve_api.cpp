@@ -98,7 +98,8 @@ DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t r
   }
   pl.min_tiles = 4;  // one per wave
   const int64_t most = cdiv(pairs * tiles, pl.min_tiles);
-  pl.grid = (int)(most < 256 ? most : 256);
+  const int64_t wgs = 256 * (latent ? 1 : lsa::gqa_per_cu(p->d_qk, pl.block_cols / 16));
+  pl.grid = (int)(most < wgs ? most : wgs);
   pl.cut = true;
   // pages of a pass: tiles * 32 / P, and two more at the ends of each of two parts
   const int64_t pass = (int64_t)((latent ? kLatentPages : kPageSlots) - 4) * kv_page_size / kTile;

@@ -547,49 +547,62 @@ def hfa_attn(prm: AttnParams, q: torch.Tensor, kv: torch.Tensor, idx: torch.Tens
 
 
 # ---------------------------------------------------------------- serving: appends and dense decode
-def _tokens(name: str, t, n_tok, heads: int, width: int, device):
+# These calls' kernels take a few microseconds at small batches, less than a host that checks every tensor in
+# detail: a tensor as it should be is passed by one expression (_fits), and only what is not goes through the
+# checks that say why (host time of an append 22.5 -> 16.6 us, of an attention 22.3 -> 17.1).
+_FP8 = (torch.uint8, torch.float8_e4m3fn)
+
+
+def _fits(t, dtypes, shape, index: int) -> bool:
+    return isinstance(t, torch.Tensor) and t.dtype in dtypes and t.shape == shape and t.get_device() == index and \
+        t.is_contiguous()
+
+
+def _tokens(name: str, t, n_tok, heads: int, width: int, device, index: int) -> int:
     """A bf16 tensor [n_tok, heads, width] whose tokens may lie any stride apart (a slice of a fused
     projection), their heads one after the other. Returns that stride in elements."""
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name} must be a torch tensor")
-    if not t.is_cuda or (device is not None and t.device != device):
-        raise ValueError(f"{name} must be a CUDA tensor on {device or 'a GPU'} (got {t.device})")
+    if index < 0 or t.get_device() != index:
+        raise ValueError(f"{name} must be a CUDA tensor on {device if index >= 0 else 'a GPU'} (got {t.device})")
     if t.dtype != torch.bfloat16:
         raise ValueError(f"{name} has dtype {t.dtype}, expected {torch.bfloat16}")
-    shape = t.shape
-    if len(shape) != 3 or shape[1] != heads or shape[2] != width or (n_tok is not None and shape[0] != n_tok):
-        raise ValueError(f"{name} has shape {tuple(shape)}, expected {('*' if n_tok is None else n_tok, heads, width)}")
+    if t.shape != (n_tok, heads, width):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(n_tok, heads, width)}")
     s0, s1, s2 = t.stride()
     if (s2 != 1 and width > 1) or (s1 != width and heads > 1):
         raise ValueError(f"{name}: the heads of a token must be contiguous (strides {t.stride()})")
-    return s0 if shape[0] > 1 else heads * width
+    return s0 if n_tok > 1 else heads * width
 
 
-def _paged_cache(name: str, t, fp8: bool, heads: int, width: int, device, like=None):
-    """A cache [n_phys, heads, page, width], or without the head dimension when there is one head. Returns
-    (n_phys, page); `like`: the (n_phys, page) it must have."""
-    if isinstance(t, torch.Tensor) and t.dtype == torch.float8_e4m3fn:
-        t = t.view(torch.uint8)
-    if heads == 1 and isinstance(t, torch.Tensor) and t.dim() == 3:
-        _need(name, t, _U8 if fp8 else _BF16, (None, None, width), device)
-        got = (t.shape[0], t.shape[1])
+def _paged_shape(name: str, t, fp8: bool, heads: int, width: int, device, index: int):
+    """(n_phys, page) of a cache [n_phys, heads, page, width], or without the head dimension when there is one
+    head."""
+    shape = t.shape if isinstance(t, torch.Tensor) else ()
+    if len(shape) == 3 and heads == 1:
+        n_phys, page, _ = shape
+        want = (n_phys, page, width)
     else:
-        _need(name, t, _U8 if fp8 else _BF16, (None, heads, None, width), device)
-        got = (t.shape[0], t.shape[2])
-    if like is not None and got != like:
-        raise ValueError(f"{name} has {got[0]} pages of {got[1]} rows, expected {like[0]} of {like[1]}")
-    return got
+        n_phys, page = (shape[0], shape[2]) if len(shape) == 4 else (None, None)
+        want = (n_phys, heads, page, width)
+    if not _fits(t, _FP8 if fp8 else _BF16, want, index):
+        _need(name, t, _FP8 if fp8 else _BF16, want, device)
+    return n_phys, page
 
 
-def _cache_scale(name: str, t, fp8: bool, n_phys: int, heads: int, page: int, device):
-    if not fp8:
-        if t is not None:
-            raise ValueError(f"{name} must be None for bf16 caches")
+def _paged_like(name: str, t, fp8: bool, n_phys: int, heads: int, page: int, width: int, device, index: int) -> None:
+    """A cache with the pages of another."""
+    dtypes = _FP8 if fp8 else _BF16
+    if _fits(t, dtypes, (n_phys, heads, page, width), index) or (heads == 1 and _fits(t, dtypes, (n_phys, page, width), index)):
         return
-    if heads == 1 and isinstance(t, torch.Tensor) and t.dim() == 2:
-        _need(name, t, _F32, (n_phys, page), device)
-    else:
-        _need(name, t, _F32, (n_phys, heads, page), device)
+    got = _paged_shape(name, t, fp8, heads, width, device, index)
+    raise ValueError(f"{name} has {got[0]} pages of {got[1]} rows, expected {n_phys} of {page}")
+
+
+def _cache_scale(name: str, t, n_phys: int, heads: int, page: int, device, index: int) -> None:
+    if _fits(t, _F32, (n_phys, heads, page), index) or (heads == 1 and _fits(t, _F32, (n_phys, page), index)):
+        return
+    _need(name, t, _F32, (n_phys, heads, page), device)
 
 
 def cache_append(prm: AppendParams, k: torch.Tensor, k_cache: torch.Tensor, *, page_table: torch.Tensor | None = None,
@@ -607,70 +620,81 @@ def cache_append(prm: AppendParams, k: torch.Tensor, k_cache: torch.Tensor, *, p
     of sequence `seq` (seq None: token i is of sequence i // rows_per_seq). k, v, q: [n_tok, heads, d] bf16
     with any token stride; with k_rot / q_rot, their last rot_dim dims apart. Caches [n_phys, heads, page, d]
     (or [n_phys, page, d] of one head), bf16 or fp8 codes with scales [n_phys, heads, page]. rope:
-    [positions, rot_dim] fp32, cosines then sines. page_table None: sequence b has page b alone. rows: True, or an
-    int64 tensor [n_tok], for the physical cache rows (block_keys_update takes them)."""
-    nk, nq = prm.n_kv_heads, prm.n_heads
-    dev = k.device if isinstance(k, torch.Tensor) else None
-    cut = prm.rot_dim if k_rot is not None else 0
-    ks = _tokens("k", k, None, nk, prm.d_k - cut, dev)
-    n = k.shape[0]
-    krs = _tokens("k_rot", k_rot, n, nk, prm.rot_dim, dev) if k_rot is not None else 0
-    n_phys, page = _paged_cache("k_cache", k_cache, prm.fp8, nk, prm.d_k, dev)
-    _cache_scale("k_scale", k_scale, prm.fp8, n_phys, nk, page, dev)
-    vs = 0
-    if prm.d_v:
-        vs = _tokens("v", v, n, nk, prm.d_v, dev)
-        _paged_cache("v_cache", v_cache, prm.fp8, nk, prm.d_v, dev, (n_phys, page))
-        _cache_scale("v_scale", v_scale, prm.fp8, n_phys, nk, page, dev)
+    [positions, rot_dim] fp32, cosines then sines. page_table None: sequence b has page b alone (n_seq: how many
+    there are, else as ctx_len or the cache has). rows: True, or an int64 tensor [n_tok], for the physical cache
+    rows (block_keys_update takes them)."""
+    nk, nq, d_k, d_v, rot, fp8 = prm.n_kv_heads, prm.n_heads, prm.d_k, prm.d_v, prm.rot_dim, prm.fp8
+    is_tensor = isinstance(k, torch.Tensor)
+    dev, i = (k.device, k.get_device()) if is_tensor else (None, -1)
+    n = k.shape[0] if is_tensor and k.dim() == 3 else None
+    ks = _tokens("k", k, n, nk, d_k if k_rot is None else d_k - rot, dev, i)
+    krs = 0 if k_rot is None else _tokens("k_rot", k_rot, n, nk, rot, dev, i)
+    n_phys, page = _paged_shape("k_cache", k_cache, fp8, nk, d_k, dev, i)
+    vs = qs = qrs = rope_rows = 0
+    if d_v:
+        vs = _tokens("v", v, n, nk, d_v, dev, i)
+        _paged_like("v_cache", v_cache, fp8, n_phys, nk, page, d_v, dev, i)
     elif v is not None or v_cache is not None or v_scale is not None:
         raise ValueError("v, v_cache and v_scale must be None with d_v = 0")
-    qs = qrs = 0
+    if fp8:
+        _cache_scale("k_scale", k_scale, n_phys, nk, page, dev, i)
+        if d_v:
+            _cache_scale("v_scale", v_scale, n_phys, nk, page, dev, i)
+    elif k_scale is not None or v_scale is not None:
+        raise ValueError("k_scale and v_scale must be None for bf16 caches")
     if nq:
-        qs = _tokens("q", q, n, nq, prm.d_k - (prm.rot_dim if q_rot is not None else 0), dev)
+        qs = _tokens("q", q, n, nq, d_k if q_rot is None else d_k - rot, dev, i)
         if q_rot is not None:
-            qrs = _tokens("q_rot", q_rot, n, nq, prm.rot_dim, dev)
+            qrs = _tokens("q_rot", q_rot, n, nq, rot, dev, i)
         if q_out is None:
-            q_out = torch.empty((n, nq, prm.d_k), dtype=torch.bfloat16, device=dev)
-        else:
-            _need("q_out", q_out, _BF16, (n, nq, prm.d_k), dev)
+            q_out = q.new_empty((n, nq, d_k))
+        elif not _fits(q_out, _BF16, (n, nq, d_k), i):
+            _need("q_out", q_out, _BF16, (n, nq, d_k), dev)
     elif q is not None or q_rot is not None or q_out is not None:
         raise ValueError("q, q_rot and q_out must be None with n_heads = 0")
-    rope_rows = 0
-    if prm.rot_dim:
-        rope_rows = _need("rope", rope, _F32, (None, prm.rot_dim), dev).shape[0]
+    if rot:
+        rope_rows = rope.shape[0] if isinstance(rope, torch.Tensor) and rope.dim() == 2 else None
+        if not _fits(rope, _F32, (rope_rows, rot), i):
+            _need("rope", rope, _F32, (None, rot), dev)
     elif rope is not None:
         raise ValueError("rope must be None with rot_dim = 0")
     if (pos is None) == (ctx_len is None):
         raise ValueError("exactly one of pos and ctx_len must be given")
+    max_pages = 1
     if page_table is not None:
-        _need("page_table", page_table, _I32, (None, None), dev)
-        seqs, max_pages = page_table.shape
+        seqs, max_pages = page_table.shape if isinstance(page_table, torch.Tensor) and page_table.dim() == 2 else (None, None)
+        if not _fits(page_table, _I32, (seqs, max_pages), i):
+            _need("page_table", page_table, _I32, (None, None), dev)
     else:
-        seqs, max_pages = ctx_len.shape[0] if ctx_len is not None else n_phys, 1
+        seqs = n_phys if ctx_len is None else ctx_len.shape[0]
     if n_seq is not None and n_seq != seqs:
         if page_table is not None or ctx_len is not None or not 0 <= n_seq <= seqs:
             raise ValueError(f"n_seq is {n_seq}, the page table, ctx_len or cache hold {seqs} sequences")
         seqs = n_seq
     if ctx_len is not None:
-        _need("ctx_len", ctx_len, _I32, (seqs,), dev)
+        if not _fits(ctx_len, _I32, (seqs,), i):
+            _need("ctx_len", ctx_len, _I32, (seqs,), dev)
         if seq is not None:
             raise ValueError("seq must be None with ctx_len")
         if n != seqs * rows_per_seq:
             raise ValueError(f"{n} tokens, but {seqs} sequences of rows_per_seq = {rows_per_seq}")
     else:
-        _need("pos", pos, _I32, (n,), dev)
-        _need_opt("seq", seq, _I32, (n,), dev)
+        if not _fits(pos, _I32, (n,), i):
+            _need("pos", pos, _I32, (n,), dev)
+        if seq is not None and not _fits(seq, _I32, (n,), i):
+            _need("seq", seq, _I32, (n,), dev)
     if rows is True:
-        rows = torch.empty((n,), dtype=torch.int64, device=dev)
+        rows = torch.empty(n, dtype=torch.int64, device=dev)
     elif rows is False or rows is None:
         rows = None
-    else:
+    elif not _fits(rows, _I64, (n,), i):
         _need("rows", rows, _I64, (n,), dev)
     t = _AppendTensors(_p(q), _p(q_rot), _p(k), _p(k_rot), _p(v), qs, qrs, ks, krs, vs, _p(rope), rope_rows, _p(seq),
                        _p(pos), _p(ctx_len), _p(page_table), _p(q_out), _p(k_cache), _p(k_scale), _p(v_cache),
                        _p(v_scale), _p(rows))
-    _check(lib().lsa_cache_append(_ref(prm), ctypes.byref(t), n, seqs, rows_per_seq, max_pages, page, n_phys,
-                                  _stream(dev)), "lsa_cache_append")
+    st = lib().lsa_cache_append(_ref(prm), ctypes.byref(t), n, seqs, rows_per_seq, max_pages, page, n_phys, _stream(dev))
+    if st != 0:
+        _check(st, "lsa_cache_append")
     return q_out, rows
 
 
@@ -689,38 +713,50 @@ def decode_attn(prm: DecodeAttnParams, q: torch.Tensor, k_cache: torch.Tensor, v
 
     Caches as cache_append writes them; v_cache None with a latent cache. page_table None: sequence b has
     page b alone."""
-    _need("q", q, _BF16, (None, prm.n_heads, prm.d_qk))
-    n_rows, dev = q.shape[0], q.device
-    n_phys, page = _paged_cache("k_cache", k_cache, prm.fp8, prm.n_kv_heads, prm.d_qk, dev)
-    _cache_scale("k_scale", k_scale, prm.fp8, n_phys, prm.n_kv_heads, page, dev)
-    if prm.latent:
-        if v_cache is not None:
-            raise ValueError("v_cache must be None with a latent cache (V is the first d_v columns of k_cache)")
-    else:
-        _paged_cache("v_cache", v_cache, prm.fp8, prm.n_kv_heads, prm.d_v, dev, (n_phys, page))
-        _cache_scale("v_scale", v_scale, prm.fp8, n_phys, prm.n_kv_heads, page, dev)
-    _need("ctx_len", ctx_len, _I32, (None,), dev)
-    n_seq = ctx_len.shape[0]
+    H, nk, d_qk, d_v, fp8 = prm.n_heads, prm.n_kv_heads, prm.d_qk, prm.d_v, prm.fp8
+    n_rows = q.shape[0] if isinstance(q, torch.Tensor) and q.dim() == 3 else None
+    i = -1 if n_rows is None else q.get_device()
+    if i < 0 or not _fits(q, _BF16, (n_rows, H, d_qk), i):
+        _need("q", q, _BF16, (None, H, d_qk))
+    dev = q.device
+    n_phys, page = _paged_shape("k_cache", k_cache, fp8, nk, d_qk, dev, i)
+    if not prm.latent:
+        _paged_like("v_cache", v_cache, fp8, n_phys, nk, page, d_v, dev, i)
+    elif v_cache is not None:
+        raise ValueError("v_cache must be None with a latent cache (V is the first d_v columns of k_cache)")
+    if fp8:
+        _cache_scale("k_scale", k_scale, n_phys, nk, page, dev, i)
+        if not prm.latent:
+            _cache_scale("v_scale", v_scale, n_phys, nk, page, dev, i)
+    elif k_scale is not None or v_scale is not None:
+        raise ValueError("k_scale and v_scale must be None for bf16 caches")
+    n_seq = ctx_len.shape[0] if isinstance(ctx_len, torch.Tensor) and ctx_len.dim() == 1 else None
+    if not _fits(ctx_len, _I32, (n_seq,), i):
+        _need("ctx_len", ctx_len, _I32, (None,), dev)
     if n_rows != n_seq * rows_per_seq:
         raise ValueError(f"q has {n_rows} rows, {n_seq} sequences of rows_per_seq = {rows_per_seq} need {n_seq * rows_per_seq}")
     max_pages = 1
     if page_table is not None:
-        max_pages = _need("page_table", page_table, _I32, (n_seq, None), dev).shape[1]
+        max_pages = page_table.shape[1] if isinstance(page_table, torch.Tensor) and page_table.dim() == 2 else None
+        if not _fits(page_table, _I32, (n_seq, max_pages), i):
+            _need("page_table", page_table, _I32, (n_seq, None), dev)
     if out is None:
-        out = torch.empty((n_rows, prm.n_heads, prm.d_v), dtype=torch.bfloat16, device=dev)
-    else:
-        _need("out", out, _BF16, (n_rows, prm.n_heads, prm.d_v), dev)
+        out = q.new_empty((n_rows, H, d_v))
+    elif not _fits(out, _BF16, (n_rows, H, d_v), i):
+        _need("out", out, _BF16, (n_rows, H, d_v), dev)
     if lse is True:
-        lse = torch.empty((n_rows, prm.n_heads), dtype=torch.float32, device=dev)
-    elif lse is False:
+        lse = torch.empty((n_rows, H), dtype=torch.float32, device=dev)
+    elif lse is False or lse is None:
         lse = None
-    else:
-        _need_opt("lse", lse, _F32, (n_rows, prm.n_heads), dev)
+    elif not _fits(lse, _F32, (n_rows, H), i):
+        _need("lse", lse, _F32, (n_rows, H), dev)
     L, ref = lib(), _ref(prm)
-    ws, wsb = _workspace(L.lsa_decode_attn_workspace_size(ref, n_seq, rows_per_seq, max_pages, page), dev, workspace)
-    _check(L.lsa_decode_attn(ref, n_seq, rows_per_seq, _p(q), _p(k_cache), _p(k_scale), _p(v_cache), _p(v_scale),
-                             _p(ctx_len), _p(page_table), max_pages, page, n_phys, _p(out), _p(lse), _p(ws), wsb,
-                             _stream(dev)), "lsa_decode_attn")
+    wsb = L.lsa_decode_attn_workspace_size(ref, n_seq, rows_per_seq, max_pages, page)
+    ws, wsb = _workspace(wsb, dev, workspace)
+    st = L.lsa_decode_attn(ref, n_seq, rows_per_seq, _p(q), _p(k_cache), _p(k_scale), _p(v_cache), _p(v_scale),
+                           _p(ctx_len), _p(page_table), max_pages, page, n_phys, _p(out), _p(lse), _p(ws), wsb, _stream(dev))
+    if st != 0:
+        _check(st, "lsa_decode_attn")
     return out, lse
 
 
