@@ -41,70 +41,72 @@ __device__ __forceinline__ Span span_of(const DecodeGeom& g, int ctx) {
   return s;
 }
 
-// (wave-uniform values that the compiler cannot know to be: kept in scalar registers)
+// (a wave-uniform value that the compiler cannot know to be: kept in a scalar register)
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int64_t uniform(int64_t x) {
-  return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
-}
-// Tiles of all sequences (one key/value head).
-__device__ __forceinline__ int64_t all_tiles(const DecodeGeom& g) {
-  const int lane = threadIdx.x & 63;
-  int64_t sum = 0;
-  for (int b0 = 0; b0 < g.n_seq; b0 += 64)
-    if (b0 + lane < g.n_seq) sum += span_of(g, g.ctx_len[b0 + lane]).nt;
-  for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
-  return uniform(sum);
-}
-// Tiles a workgroup takes: an equal share of the `total` tiles of all (sequence, head)s, but no fewer than
-// pay for a workgroup.
-__device__ __forceinline__ int64_t share_of(const DecodeGeom& g, int64_t total) {
-  const int64_t s = (total + g.grid - 1) / g.grid;
-  return s < g.min_tiles ? g.min_tiles : s;
-}
-// The sequence that tile `at` (of one head) is in, and the tiles before it. at < all_tiles.
-__device__ __forceinline__ int find_seq(const DecodeGeom& g, int64_t at, int64_t& before) {
-  const int lane = threadIdx.x & 63;
-  before = 0;
-  for (int b0 = 0; b0 < g.n_seq; b0 += 64) {
-    const int nt = b0 + lane < g.n_seq ? span_of(g, g.ctx_len[b0 + lane]).nt : 0;
-    int64_t inc = nt;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t x = __shfl_up(inc, o);
-      if (lane >= o) inc += x;
-    }
-    const uint64_t past = __ballot(before + inc > at);
-    if (past) {
-      const int first = __ffsll((unsigned long long)past) - 1;
-      before += uniform((int64_t)__shfl(inc - nt, first));
-      return b0 + first;
-    }
-    before += uniform((int64_t)__shfl(inc, 63));
-  }
-  return g.n_seq;
+
+// Inclusive sum over the lanes of a wave.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr 1, 2, 4, 8: within rows of 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast 15: rows 0 and 2 into 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast 31: row 1 into 2 and 3
+  return x;
 }
 
 // Deals this workgroup its stretch of the tiles of all sequences, M (head, query row block)s each, one
-// (sequence, head) after the other: segment(sequence, r in [0, M), span, first tile, last tile + 1, whole, slot
-// of the partial). Then the rows of sequences without a tile, dealt to the workgroups. d: width of an output row.
+// (sequence, head) after the other: an equal share of all, but no fewer tiles than pay for a workgroup. Calls
+// segment(sequence, r in [0, M), span, first tile, last tile + 1, whole, slot of the partial), and tells the
+// join about every (sequence, head) whose first tile is here. Then the rows of sequences without a tile, dealt
+// to the workgroups. d: width of an output row. (Tiles of all in all fit 30 bits: the host refuses more.)
+//
+// What precedes the first load of a row is a chain of round trips, so the first 64 lengths are loaded once and
+// scanned in registers, and divisions by what the host knows are products.
 template <class F>
 __device__ __forceinline__ void deal(const DecodeGeom& g, int M, int d, F&& segment) {
-  const int64_t total = all_tiles(g) * M, share = share_of(g, total);
-  int64_t at = blockIdx.x * share;
-  const int64_t start = at, end = at + share < total ? at + share : total;
-  if (at < end) {
-    int64_t before;
-    int b = find_seq(g, at / M, before);
+  const int lane = threadIdx.x & 63;
+  auto length = [&](int b) { return b < g.n_seq ? g.ctx_len[b] : 0; };
+  const int ctx0 = length(lane), inc0 = wave_scan(span_of(g, ctx0).nt);
+  int total = __builtin_amdgcn_readlane(inc0, 63);
+  for (int b0 = 64; b0 < g.n_seq; b0 += 64) total += __builtin_amdgcn_readlane(wave_scan(span_of(g, length(b0 + lane)).nt), 63);
+  total *= M;
+  int share = fdiv(g.by_grid, total + g.grid - 1);
+  // (where workgroups are idle, one of fewer tiles rather than one for several short (sequence, head)s)
+  const int mean = fdiv(g.by_pairs, total + (int)g.by_pairs.d - 1), least = mean < g.min_tiles ? mean : g.min_tiles;
+  share = share < least ? least : share;
+  const int64_t start = (int64_t)blockIdx.x * share;
+  if (start < total) {
+    int at = (int)start;
+    const int end = total - at < share ? total : at + share;
+    // the sequence that tile `at` is in, and the tiles (of one head) before it
+    int b = 0, before = 0;
+    for (int inc = inc0, ctx = ctx0;;) {
+      const uint64_t past = __ballot((int64_t)(before + inc) * M > at);
+      if (past) {
+        const int first = __ffsll((unsigned long long)past) - 1;
+        before += __builtin_amdgcn_readlane(inc, first) - span_of(g, __builtin_amdgcn_readlane(ctx, first)).nt;
+        b += first;
+        break;
+      }
+      before += __builtin_amdgcn_readlane(inc, 63);
+      b += 64;
+      ctx = length(b + lane);
+      inc = wave_scan(span_of(g, ctx).nt);
+    }
     while (at < end) {
-      const Span sp = span_of(g, uniform(g.ctx_len[b]));
+      const Span sp = span_of(g, b < 64 ? __builtin_amdgcn_readlane(ctx0, b) : uniform(g.ctx_len[b]));
       if (sp.nt == 0) {
         ++b;
         continue;
       }
-      const int64_t rel = at - before * M;
-      const int r = (int)(rel / sp.nt), t0 = (int)(rel - (int64_t)r * sp.nt);
-      const int n = end - at < sp.nt - t0 ? (int)(end - at) : sp.nt - t0;
-      segment(b, r, sp, t0, t0 + n, n == sp.nt, 2 * (int64_t)blockIdx.x + (at != start));
+      const int rel = at - before * M;
+      const int r = M == 1 ? 0 : uniform((int)((uint32_t)rel / (uint32_t)sp.nt)), t0 = rel - r * sp.nt;
+      const int n = end - at < sp.nt - t0 ? end - at : sp.nt - t0;
+      const int slot = 2 * (int)blockIdx.x + (at != (int)start);
+      if (t0 == 0 && g.parts && threadIdx.x == 0)  // first workgroup, last one, and the first one's partial
+        g.parts[(int64_t)b * M + r] = int4{(int)blockIdx.x, (int)((uint32_t)(at + sp.nt - 1) / (uint32_t)share), slot, 0};
+      segment(b, r, sp, t0, t0 + n, n == sp.nt, slot);
       at += n;
       if (r == M - 1 && t0 + n == sp.nt) {
         before += sp.nt;
@@ -119,6 +121,8 @@ __device__ __forceinline__ void deal(const DecodeGeom& g, int M, int d, F&& segm
       *reinterpret_cast<u32x4*>(g.out + b * row_elems + i) = u32x4{};
     if (g.lse)
       for (int i = (int)threadIdx.x; i < g.R * g.H; i += (int)blockDim.x) g.lse[(int64_t)b * g.R * g.H + i] = -INFINITY;
+    if (g.parts)
+      for (int i = (int)threadIdx.x; i < M; i += (int)blockDim.x) g.parts[(int64_t)b * M + i] = int4{0, 0, 0, 0};
   }
 }
 
@@ -219,7 +223,7 @@ void gqa_decode_kernel(DecodeGeom g) {
   constexpr int LT = 64 / T::kChunks;  // tokens per load
   const int ld_t = lane / T::kChunks, ld_slot = lane % T::kChunks;
 
-  auto segment = [&](int b, int r, const Span& sp, int t0, int t1, bool whole, int64_t slot) {
+  auto segment = [&](int b, int r, const Span& sp, int t0, int t1, bool whole, int slot) {
     const int kvh = r / cb_n, col0 = (r - kvh * cb_n) * COLS;
     const int ncols = cols - col0 < COLS ? cols - col0 : COLS;
     // ---- Q as the B operand: column 16 nb + i16 = (new token j, head of the group), dims of k-step s
@@ -510,7 +514,7 @@ void gqa_decode_kernel(DecodeGeom g) {
           *reinterpret_cast<u32x2*>(g.out + row * D + d) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
           if (g.lse && d == 0) g.lse[row] = sum == 0.f ? -INFINITY : (mx + __log2f(sum)) * kLn2;
         } else {
-          const int64_t pc = slot * COLS + 16 * nb + col;
+          const int64_t pc = (int64_t)slot * COLS + 16 * nb + col;
           *reinterpret_cast<f32x4*>(g.part_o + pc * D + d) = acc;
           if (d == 0) *reinterpret_cast<f32x2*>(g.part_ml + 2 * pc) = f32x2{mx, sum};
         }
@@ -548,7 +552,7 @@ void latent_decode_kernel(DecodeGeom g) {
   const uint8_t* kvb = static_cast<const uint8_t*>(g.k);
   const int hb_n = (g.H + 63) / 64, M = g.R * hb_n;  // (new token, 64 heads)s of a sequence
 
-  auto segment = [&](int b, int r, const Span& sp, int t0, int t1, bool whole, int64_t slot) {
+  auto segment = [&](int b, int r, const Span& sp, int t0, int t1, bool whole, int slot) {
     const int j = r / hb_n, h0 = (r - j * hb_n) * 64, nh = g.H - h0 < 64 ? g.H - h0 : 64;
     const int tq = sp.c - g.R + j;  // this token's position
     const int64_t row0 = ((int64_t)b * g.R + j) * g.H + h0;  // output row of head h0
@@ -568,13 +572,15 @@ void latent_decode_kernel(DecodeGeom g) {
         const int64_t end = (int64_t)(p1 + sp.skip) * kTile - 1;
         n2 = fdiv(g.by_page, end < sp.c ? (int)end : sp.c - 1) - f2 + 1;
       }
-      __syncthreads();  // the previous entries' readers are done
-      for (int i = (int)threadIdx.x; i < n1 + n2; i += 512) {
-        const int pg = i < n1 ? f1 + i : f2 + i - n1;
-        const int ph = g.page_table ? g.page_table[(int64_t)b * g.max_pages + pg] : b;
-        pages[i] = ph >= 0 && ph < g.n_phys ? ph : -1;
-      }
-      __syncthreads();
+      // (barriers that wait for LDS alone, and no entries loaded by scorers: their Q may still be on its way)
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // the previous entries' readers are done
+      if (!scorer)
+        for (int i = (int)threadIdx.x - 256; i < n1 + n2; i += 256) {
+          const int pg = i < n1 ? f1 + i : f2 + i - n1;
+          const int ph = g.page_table ? g.page_table[(int64_t)b * g.max_pages + pg] : b;
+          pages[i] = ph >= 0 && ph < g.n_phys ? ph : -1;
+        }
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     };
     // cache row of token `tok` of tile t, -1 where this query does not attend to it
     auto row_of = [&](int t, int tok) {
@@ -798,8 +804,8 @@ void latent_decode_kernel(DecodeGeom g) {
         }
       }
     }
-    // This wave's accumulators (64 heads x 128 columns) go head by head through the tile buffers, idle since the
-    // barrier, so that a store instruction writes whole lines: 32 heads at a time in fp32 (a partial), or all in bf16.
+    // An output goes head by head through the tile buffers, idle since the barrier, so that a store instruction
+    // writes whole lines.
     // Lane l, register r of block 4 hb + c holds column 32 c + 8 (r / 4) + 4 (l / 32) + r % 4 of head 32 hb + l % 32.
     // (the lane made opaque here, or these offsets are computed before the loop over stretches and spill)
     int el = lane;
@@ -826,134 +832,140 @@ void latent_decode_kernel(DecodeGeom g) {
         const u32x4 v = *reinterpret_cast<const u32x4*>(ost + hh * 272 + 16 * (el & 15));
         if (hh < nh) *reinterpret_cast<u32x4*>(g.out + (row0 + hh) * 512 + 128 * w4 + 8 * (el & 15)) = v;
       }
-    } else {
-      uint8_t* ost = lds + w4 * (32 * 528);
+    } else {  // a partial in the accumulators' order, whole lines per store: [4 waves][8 blocks][4][64 lanes][4]
+      f32x4* dst = reinterpret_cast<f32x4*>(g.part_o) + (int64_t)slot * 8192 + w4 * 2048 + el;
 #pragma unroll
-      for (int hb = 0; hb < 2; ++hb) {
+      for (int c = 0; c < 8; ++c)
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const f32x16& ob = o[4 * hb + c];
-            *reinterpret_cast<f32x4*>(ost + ej * 528 + (32 * c + 8 * q + 4 * (el >> 5)) * 4) = f32x4{ob[4 * q], ob[4 * q + 1], ob[4 * q + 2], ob[4 * q + 3]};
-          }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const int hh = 2 * k + (el >> 5);
-          const f32x4 v = *reinterpret_cast<const f32x4*>(ost + hh * 528 + 16 * (el & 31));
-          if (32 * hb + hh < nh) *reinterpret_cast<f32x4*>(g.part_o + (slot * 64 + 32 * hb + hh) * 512 + 128 * w4 + 4 * (el & 31)) = v;
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      }
+        for (int q = 0; q < 4; ++q) dst[(4 * c + q) * 64] = f32x4{o[c][4 * q], o[c][4 * q + 1], o[c][4 * q + 2], o[c][4 * q + 3]};
     }
   };
   deal(g, M, 512, segment);
 }
 
 // ============================================================================ joining the partials
-// One workgroup per output row and 4 Q of its dims: nothing to do where one stretch covered it whole. A thread
-// takes four dims, and 256 / Q groups of threads share the partials, with a running maximum each. Bound by the
-// round trips to partials that other XCDs have just written: calls of few rows, whose rows have many partials,
-// take few dims per workgroup, so that every thread has few of them.
-constexpr int64_t kJoinFew = 2048;  // workgroups of 32 dims
-template <int D, int COLS, bool LATENT, int Q>
-__global__ __launch_bounds__(256) void decode_join_kernel(DecodeGeom g) {
-  constexpr int SUBS = 256 / Q, U = 4;
-  __shared__ __attribute__((aligned(16))) float acc_s[SUBS][4 * Q];
-  __shared__ float m_s[SUBS], l_s[SUBS];
-  // columns of a unit: query rows of a (sequence, key/value head), or heads of a (sequence, new token)
-  const int group = g.H / g.Hkv, cols = LATENT ? g.H : g.R * group, units = LATENT ? g.R : g.Hkv;
-  const int cb_n = (cols + COLS - 1) / COLS, M = units * cb_n;
-  const int64_t unit = blockIdx.x / cols;
-  const int col = (int)(blockIdx.x - unit * cols);
-  const int b = (int)(unit / units), un = (int)(unit - (int64_t)b * units), r = un * cb_n + col / COLS;
-  int64_t before = 0, all = 0;  // tiles of the sequences before b, and of all
-  {
-    const int lane = threadIdx.x & 63;
-    for (int b0 = 0; b0 < g.n_seq; b0 += 64)
-      if (b0 + lane < g.n_seq) {
-        const int nt = span_of(g, g.ctx_len[b0 + lane]).nt;
-        all += nt;
-        before += b0 + lane < b ? nt : 0;
-      }
-    for (int o = 32; o >= 1; o >>= 1) {
-      all += __shfl_xor(all, o);
-      before += __shfl_xor(before, o);
-    }
-  }
-  const int nt = span_of(g, g.ctx_len[b]).nt;
-  const int64_t share = share_of(g, all * M), first = before * M + (int64_t)r * nt;
-  const int64_t w0 = first / share, w1 = (first + nt - 1) / share;
-  if (nt == 0 || w0 == w1) return;  // (uniform)
-  const int sub = threadIdx.x / Q, dl = 4 * (threadIdx.x % Q), d = 4 * Q * (int)blockIdx.y + dl, cc = col % COLS;
-  // the first stretch may have begun with another head: then this one's partial is its second
-  auto slot = [&](int64_t w) { return (2 * w + (w == w0 && first != w0 * share)) * COLS + cc; };
-  float m = kNoRef, l = 0.f;
-  f32x4 acc = {};
-  for (int64_t w = w0 + sub; w <= w1; w += SUBS * U) {
+// A thread takes four dims of one output row and every S-th of the row's partials, with a running maximum; the
+// S threads of a row and dims meet in LDS. Bound by two round trips to what other XCDs have just written: which
+// workgroups have partials (left there by the first of them), and the partials. Nothing to do where one
+// stretch covered a (sequence, head) whole.
+struct Joined {
+  float m, l;
+  f32x4 acc;
+};
+// partial v of the parts p: slot of the first workgroup's, then the first slot of each following one
+__device__ __forceinline__ int part_slot(const int4& p, int v) { return v == 0 ? p.z : 2 * (p.x + v); }
+
+template <int S, int U, class ML, class O>  // U partials requested together
+__device__ __forceinline__ Joined join_parts(const int4& p, int sub, ML&& load_ml, O&& load_o) {
+  const int n = p.y - p.x + 1;
+  Joined r{kNoRef, 0.f, f32x4{}};
+  for (int v = sub; v < n; v += S * U) {
     f32x2 ml[U];
     f32x4 x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t v = w + (int64_t)u * SUBS <= w1 ? w + (int64_t)u * SUBS : w;
-      ml[u] = *reinterpret_cast<const f32x2*>(g.part_ml + 2 * slot(v));
-      x[u] = *reinterpret_cast<const f32x4*>(g.part_o + slot(v) * D + d);
+      const int slot = part_slot(p, v + u * S < n ? v + u * S : v);
+      ml[u] = load_ml(slot);
+      x[u] = load_o(slot);
     }
-    float mx = m;
+    float mx = r.m;
 #pragma unroll
     for (int u = 0; u < U; ++u) mx = fmaxf(mx, ml[u][0]);
-    const float a = fast_exp2(m - mx);
-    l *= a;
-    acc *= a;
+    const float a = fast_exp2(r.m - mx);
+    r.l *= a;
+    r.acc *= a;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (w + (int64_t)u * SUBS > w1) break;
+      if (v + u * S >= n) break;
       const float f = fast_exp2(ml[u][0] - mx);
-      l += ml[u][1] * f;
-      acc += f * x[u];
+      r.l += ml[u][1] * f;
+      r.acc += f * x[u];
     }
-    m = mx;
+    r.m = mx;
   }
-  *reinterpret_cast<f32x4*>(&acc_s[sub][dl]) = acc;
-  if (dl == 0) {
-    m_s[sub] = m;
-    l_s[sub] = l;
-  }
+  return r;
+}
+// The sum over the S threads x, x + T, .. of a workgroup of S T threads (in the first T); lds: S T entries.
+template <int S, int T>
+__device__ __forceinline__ Joined join_threads(const Joined& mine, Joined* lds) {
+  const int x = threadIdx.x % T, sub = threadIdx.x / T;
+  if (sub) lds[sub * T + x] = mine;
   __syncthreads();
-  if (sub != 0) return;
-  float mx = m_s[0];
-  for (int s = 1; s < SUBS; ++s) mx = fmaxf(mx, m_s[s]);
-  float sum = 0.f;
-  f32x4 o = {};
-  for (int s = 0; s < SUBS; ++s) {
-    const float f = fast_exp2(m_s[s] - mx);
-    sum += l_s[s] * f;
-    o += f * *reinterpret_cast<const f32x4*>(&acc_s[s][dl]);
+  Joined r = mine;
+  if (sub == 0) {
+    float mx = r.m;
+    for (int k = 1; k < S; ++k) mx = fmaxf(mx, lds[k * T + x].m);
+    const float a = fast_exp2(r.m - mx);
+    r.l *= a;
+    r.acc *= a;
+    for (int k = 1; k < S; ++k) {
+      const Joined& q = lds[k * T + x];
+      const float f = fast_exp2(q.m - mx);
+      r.l += q.l * f;
+      r.acc += f * q.acc;
+    }
+    r.m = mx;
   }
-  const int j = LATENT ? un : col / group;
-  const int64_t row = ((int64_t)b * g.R + j) * g.H + (LATENT ? col : un * group + col - j * group);
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  *reinterpret_cast<u32x2*>(g.out + row * D + d) = u32x2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
-  if (g.lse && d == 0) g.lse[row] = sum == 0.f ? -INFINITY : (mx + __log2f(sum)) * kLn2;
+  return r;
+}
+__device__ __forceinline__ void join_store(const DecodeGeom& g, const Joined& r, int64_t row, int width, int d) {
+  const float inv = r.l == 0.f ? 0.f : 1.f / r.l;
+  *reinterpret_cast<u32x2*>(g.out + row * width + d) = u32x2{pack_bf16x2(r.acc[0] * inv, r.acc[1] * inv), pack_bf16x2(r.acc[2] * inv, r.acc[3] * inv)};
+  if (g.lse && d == 0) g.lse[row] = r.l == 0.f ? -INFINITY : (r.m + __log2f(r.l)) * kLn2;
+}
+
+// Grouped heads: a workgroup per output row and 1024 / S of its dims.
+template <int D, int COLS, int S>
+__global__ __launch_bounds__(256) void gqa_join_kernel(DecodeGeom g) {
+  constexpr int T = 256 / S;
+  __shared__ Joined lds[256];
+  const int group = g.H / g.Hkv, cols = g.R * group, cb_n = (cols + COLS - 1) / COLS;
+  const int unit = (int)(blockIdx.x / (uint32_t)cols), col = (int)blockIdx.x - unit * cols;  // (sequence, key/value head)
+  const int4 p = g.parts[(int64_t)unit * cb_n + col / COLS];
+  if (p.x == p.y) return;
+  const int d = 4 * (T * (int)blockIdx.y + (int)threadIdx.x % T), cc = col % COLS;
+  Joined r = join_parts<S, 4>(p, threadIdx.x / T, [&](int slot) { return *reinterpret_cast<const f32x2*>(g.part_ml + 2 * ((int64_t)slot * COLS + cc)); },
+                           [&](int slot) { return *reinterpret_cast<const f32x4*>(g.part_o + ((int64_t)slot * COLS + cc) * D + d); });
+  r = join_threads<S, T>(r, lds);
+  if (threadIdx.x >= T) return;
+  const int b = unit / g.Hkv, kvh = unit - b * g.Hkv, j = col / group;
+  join_store(g, r, ((int64_t)b * g.R + j) * g.H + kvh * group + col - j * group, D, d);
+}
+
+// Latent: a workgroup per (new token, 64 heads) and T of the partial's 8192 vectors of four, 64 of which are 32 heads x 8
+// dims in the accumulators' order.
+template <int S, int T>
+__global__ __launch_bounds__(S * T) void latent_join_kernel(DecodeGeom g) {
+  static_assert(T % 64 == 0, "a wave's threads share their partials");
+  __shared__ Joined lds[S * T];
+  const int4 p = g.parts[blockIdx.x];
+  if (p.x == p.y) return;
+  const int vec = T * (int)blockIdx.y + (int)threadIdx.x % T;
+  const int lane = vec & 63, q = (vec >> 6) & 3, c = (vec >> 8) & 3, hb = (vec >> 10) & 1, w4 = vec >> 11;
+  const int lh = 32 * hb + (lane & 31), d = 128 * w4 + 32 * c + 8 * q + 4 * (lane >> 5);
+  Joined r = join_parts<S, (S > 1 ? 8 : 4)>(p, threadIdx.x / T, [&](int slot) { return *reinterpret_cast<const f32x2*>(g.part_ml + 2 * ((int64_t)slot * 64 + lh)); },
+                           [&](int slot) { return reinterpret_cast<const f32x4*>(g.part_o)[(int64_t)slot * 8192 + vec]; });
+  r = join_threads<S, T>(r, lds);
+  if (threadIdx.x >= T) return;
+  const int hb_n = (g.H + 63) / 64, row = (int)(blockIdx.x / (uint32_t)hb_n), h = 64 * ((int)blockIdx.x - row * hb_n) + lh;
+  if (h < g.H) join_store(g, r, (int64_t)row * g.H + h, 512, d);
 }
 
 // ============================================================================ host launchers
-template <int D, int COLS, bool LATENT>
-static hipError_t launch_join(const DecodeGeom& g, hipStream_t st) {
-  const int64_t rows = (int64_t)g.n_seq * g.R * g.H;
-  if (rows * (D / 32) <= kJoinFew)
-    hipLaunchKernelGGL((decode_join_kernel<D, COLS, LATENT, 8>), dim3((unsigned)rows, D / 32), dim3(256), 0, st, g);
-  else
-    hipLaunchKernelGGL((decode_join_kernel<D, COLS, LATENT, D / 4>), dim3((unsigned)rows), dim3(256), 0, st, g);
-  return hipGetLastError();
-}
+// Calls of few rows, whose rows have many partials, take few dims per workgroup and share the partials among
+// more threads.
+constexpr int64_t kJoinFew = 2048;  // workgroups
 template <int D, bool FP8, int NB>
 static hipError_t launch_gqa(const DecodeGeom& g, hipStream_t st) {
   hipLaunchKernelGGL((gqa_decode_kernel<D, FP8, NB>), dim3((unsigned)g.grid), dim3(64 * kGqaWaves), 0, st, g);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.part_o == nullptr) return e;
-  return launch_join<D, 16 * NB, false>(g, st);
+  const int64_t rows = (int64_t)g.n_seq * g.R * g.H;
+  if (rows * (D / 32) <= kJoinFew)
+    hipLaunchKernelGGL((gqa_join_kernel<D, 16 * NB, 32>), dim3((unsigned)rows, D / 32), dim3(256), 0, st, g);
+  else
+    hipLaunchKernelGGL((gqa_join_kernel<D, 16 * NB, 1024 / D>), dim3((unsigned)rows), dim3(256), 0, st, g);
+  return hipGetLastError();
 }
 template <int D, bool FP8>
 static hipError_t launch_gqa(const DecodeGeom& g, hipStream_t st) {
@@ -966,7 +978,10 @@ hipError_t launch_decode_attn(const DecodeGeom& g, hipStream_t st) {
     hipLaunchKernelGGL(latent_decode_kernel, dim3((unsigned)g.grid), dim3(512), 0, st, g);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || g.part_o == nullptr) return e;
-    return launch_join<512, 64, true>(g, st);
+    const int64_t units = (int64_t)g.n_seq * g.R * ((g.H + 63) / 64);
+    if (units * 128 <= kJoinFew) hipLaunchKernelGGL((latent_join_kernel<16, 64>), dim3((unsigned)units, 128), dim3(1024), 0, st, g);
+    else hipLaunchKernelGGL((latent_join_kernel<1, 256>), dim3((unsigned)units, 32), dim3(256), 0, st, g);
+    return hipGetLastError();
   }
   if (g.d_qk == 64) return g.fp8 ? launch_gqa<64, true>(g, st) : launch_gqa<64, false>(g, st);
   return g.fp8 ? launch_gqa<128, true>(g, st) : launch_gqa<128, false>(g, st);

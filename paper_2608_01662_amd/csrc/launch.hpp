@@ -147,8 +147,11 @@ struct DecodeGeom {
   int pass_tiles;     // tiles whose page-table entries fit the LDS area
   int block_cols;     // query rows of one key/value head that a workgroup takes together
   int grid;           // workgroups
+  FastDiv by_grid;    // division by it
+  FastDiv by_pairs;   // by the (sequence, head, query row block)s
   int min_tiles;      // tiles that pay for a workgroup
   float *part_o, *part_ml;  // two partials per workgroup: [block_cols, d_v], [block_cols, 2]; nullptr: none is cut
+  int4* parts;        // [n_seq, M]: first and last workgroup of each (sequence, head), slot of the first one's partial
 };
 // Workgroups of the grouped-head kernel per CU: two where the registers of NB blocks of 16 query rows allow it.
 constexpr int gqa_per_cu(int d, int nb) { return nb * d <= 256 ? 2 : 1; }

@@ -76,7 +76,8 @@ lsa_status check_decode_sizes(const lsa_decode_attn_params* p, int32_t n_seq, in
 struct DecodePlan {
   int grid, min_tiles, block_cols, pass_tiles;
   bool cut;  // may a stretch end inside a (sequence, head)?
-  size_t off_ml, total;
+  int64_t pairs, all_tiles;  // (sequence, head, query row block)s; their tiles at most
+  size_t off_ml, off_parts, total;
 };
 constexpr int kTile = 32;          // positions of a tile
 constexpr int kPageSlots = 2048;   // page-table entries a workgroup stages at a time
@@ -97,7 +98,9 @@ DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t r
     tiles = window < tiles ? window : tiles;
   }
   pl.min_tiles = 4;  // one per wave
-  const int64_t most = cdiv(pairs * tiles, pl.min_tiles);
+  pl.all_tiles = pairs * tiles;
+  pl.pairs = pairs;
+  const int64_t some = cdiv(pl.all_tiles, pl.min_tiles), most = some > pairs ? some : pairs;
   const int64_t wgs = 256 * (latent ? 1 : lsa::gqa_per_cu(p->d_qk, pl.block_cols / 16));
   pl.grid = (int)(most < wgs ? most : wgs);
   pl.cut = true;
@@ -106,7 +109,8 @@ DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t r
   pl.pass_tiles = (int)(pass < (1 << 26) ? pass : (1 << 26));
   const size_t parts = pl.cut ? (size_t)2 * pl.grid * pl.block_cols : 0;
   pl.off_ml = lsa::round_up(parts * p->d_v * 4, 256);
-  pl.total = pl.off_ml + lsa::round_up(parts * 2 * 4, 256);
+  pl.off_parts = pl.off_ml + lsa::round_up(parts * 2 * 4, 256);
+  pl.total = pl.off_parts + (pl.cut ? lsa::round_up((size_t)pairs * 16, 256) : 0);
   return pl;
 }
 
@@ -238,7 +242,10 @@ lsa_status lsa_decode_attn(const lsa_decode_attn_params* p, int32_t n_seq, int32
               "q, k_cache, v_cache and out must be 16-byte aligned");
   LSA_REQUIRE(aligned(k_scale, 4) && aligned(v_scale, 4) && aligned(ctx_len, 4) && aligned(page_table, 4) && aligned(lse, 4),
               LSA_ERR_INVALID_ARG, "scales, ctx_len, page_table and lse must be 4-byte aligned");
-  const size_t need = lsa_decode_attn_workspace_size(p, n_seq, rows_per_seq, max_pages, kv_page_size);
+  const DecodePlan pl = plan_decode(p, n_seq, rows_per_seq, max_pages, kv_page_size);
+  LSA_REQUIRE(pl.all_tiles <= (1LL << 30), LSA_ERR_UNSUPPORTED,
+              "n_seq * max_pages * kv_page_size / 32 * n_kv_heads must be <= 2^30");
+  const size_t need = pl.total;
   LSA_REQUIRE(need == 0 || (workspace != nullptr && aligned(workspace, 256)), LSA_ERR_WORKSPACE,
               "workspace must be non-NULL and 256-byte aligned");
   LSA_REQUIRE(ws_bytes >= need, LSA_ERR_WORKSPACE, "workspace of %zu bytes < %zu needed", ws_bytes, need);
@@ -268,15 +275,17 @@ lsa_status lsa_decode_attn(const lsa_decode_attn_params* p, int32_t n_seq, int32
   g.k_swa = p->k_swa < g.cap ? p->k_swa : 0;
   g.k_sink = g.k_swa == 0 ? 0 : p->k_sink < g.cap ? p->k_sink : g.cap;
   g.scale_log2 = p->sm_scale * 1.4426950408889634f;
-  const DecodePlan pl = plan_decode(p, n_seq, rows_per_seq, max_pages, kv_page_size);
   g.by_page = lsa::fast_div((uint32_t)kv_page_size);
   g.pass_tiles = pl.pass_tiles;
   g.block_cols = pl.block_cols;
   g.grid = pl.grid;
+  g.by_grid = lsa::fast_div((uint32_t)pl.grid);
+  g.by_pairs = lsa::fast_div((uint32_t)pl.pairs);
   g.min_tiles = pl.min_tiles;
   if (pl.cut) {
     g.part_o = static_cast<float*>(workspace);
     g.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + pl.off_ml);
+    g.parts = reinterpret_cast<int4*>(static_cast<uint8_t*>(workspace) + pl.off_parts);
   }
   const hipError_t e = lsa::launch_decode_attn(g, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "decode attention");
