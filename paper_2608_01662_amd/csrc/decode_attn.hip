@@ -226,21 +226,22 @@ void gqa_decode_kernel(DecodeGeom g) {
   auto segment = [&](int b, int r, const Span& sp, int t0, int t1, bool whole, int slot) {
     const int kvh = r / cb_n, col0 = (r - kvh * cb_n) * COLS;
     const int ncols = cols - col0 < COLS ? cols - col0 : COLS;
-    // ---- Q as the B operand: column 16 nb + i16 = (new token j, head of the group), dims of k-step s
+    // ---- Q as the B operand: column 16 nb + i16 = (new token j, head of the group), dims of k-step s. (Columns past the
+    // last query row repeat the first one's and are not stored.)
     u32x4 qb[NB][KS];
     int tcol[NB];  // position of the column's token
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       const int col = col0 + 16 * nb + i16;
       const bool ok = 16 * nb + i16 < ncols;
-      const int j = ok ? col / group : 0, hh = ok ? col - j * group : 0;
+      const int j = (ok ? col : col0) / group, hh = (ok ? col : col0) - j * group;
       tcol[nb] = sp.c - g.R + j;
       const uint8_t* qp = reinterpret_cast<const uint8_t*>(g.q + (((int64_t)b * g.R + j) * g.H + kvh * group + hh) * D);
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         // bf16: chunk 4 s + q4 of the row; fp8: a 16-byte K chunk 4 (s / 2) + q4 holds the dims of two k-steps
         const int dim = FP8 ? 64 * (s >> 1) + 16 * q4 + 8 * (s & 1) : 32 * s + 8 * q4;
-        qb[nb][s] = ok ? *reinterpret_cast<const u32x4*>(qp + 2 * dim) : u32x4{};
+        qb[nb][s] = *reinterpret_cast<const u32x4*>(qp + 2 * dim);
       }
     }
     f32x4 o[NB][CD];
@@ -538,6 +539,7 @@ void gqa_decode_kernel(DecodeGeom g) {
 // products, so kLatBufs tile buffers keep kLatBufs - 1 tiles on their way while one is scored (at barrier `it`
 // the buffer of tile it - 1 is free: its V operands are in registers).
 constexpr int kLatBufs = 4;
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 constexpr int kLatPages = 1024;  // page-table entries staged in LDS at a time
 
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
@@ -572,15 +574,16 @@ void latent_decode_kernel(DecodeGeom g) {
         const int64_t end = (int64_t)(p1 + sp.skip) * kTile - 1;
         n2 = fdiv(g.by_page, end < sp.c ? (int)end : sp.c - 1) - f2 + 1;
       }
-      // (barriers that wait for LDS alone, and no entries loaded by scorers: their Q may still be on its way)
-      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // the previous entries' readers are done
-      if (!scorer)
-        for (int i = (int)threadIdx.x - 256; i < n1 + n2; i += 256) {
+      // (barriers that wait for LDS alone, and no entries loaded by value waves: their direct loads of Q may still be on
+      // their way)
+      lds_barrier();  // the previous entries' readers are done
+      if (scorer)
+        for (int i = (int)threadIdx.x; i < n1 + n2; i += 256) {
           const int pg = i < n1 ? f1 + i : f2 + i - n1;
           const int ph = g.page_table ? g.page_table[(int64_t)b * g.max_pages + pg] : b;
           pages[i] = ph >= 0 && ph < g.n_phys ? ph : -1;
         }
-      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      lds_barrier();
     };
     // cache row of token `tok` of tile t, -1 where this query does not attend to it
     auto row_of = [&](int t, int tok) {
@@ -592,21 +595,23 @@ void latent_decode_kernel(DecodeGeom g) {
     };
     if (scorer) {
       const int th = w4 & 1, pair = w4 >> 1;  // tokens 16 th .. + 15, heads 32 pair .. + 31
-      u32x4 qb[2][18];
-#pragma unroll
-      for (int nb = 0; nb < 2; ++nb) {
-        const int h = 32 * pair + 16 * nb + i16;
-        const u32x4* qp = reinterpret_cast<const u32x4*>(g.q + (row0 + (h < nh ? h : 0)) * 576 + 8 * q4);
-#pragma unroll
-        for (int s = 0; s < 18; ++s) qb[nb][s] = h < nh ? qp[4 * s] : u32x4{};
-      }
       const int ksw = mla_swz(i16 >> 3, i16 & 7);
       const int k_row = th * kMlaHalf + 9 * (i16 >> 3) * 1024 + 8 * (i16 & 7) * 16;
       const int k_even = k_row + ((0 + q4) ^ ksw) * 16, k_odd = k_row + ((4 + q4) ^ ksw) * 16;
+      u32x4 qb[2][18];  // Q^T as the B operand: column = head 32 pair + 16 nb + i16, k-step s covers dims 32 s + 8 q4 ..
       float m[2] = {kNoRef, kNoRef}, l[2] = {0.f, 0.f};
       for (int p0 = t0; p0 < t1; p0 += g.pass_tiles) {
         const int nt = t1 - p0 < g.pass_tiles ? t1 - p0 : g.pass_tiles;
         stage(p0, p0 + nt);
+        if (p0 == t0) {  // Q has landed as two tiles of 32 heads, whose rows lie as a K tile's
+          lds_barrier();
+          const uint8_t* qt = lds + (kLatBufs - 2 + pair) * kMlaTile - th * kMlaHalf;
+#pragma unroll
+          for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+            for (int s = 0; s < 18; ++s) qb[nb][s] = *reinterpret_cast<const u32x4*>(qt + nb * kMlaHalf + ((s & 1) ? k_odd : k_even) + (s >> 1) * 1024);
+          lds_barrier();
+        }
         uint32_t cur = 0;
         for (int it = 0; it <= nt; ++it) {
           // tile it has landed; this scorer's P of tile it - 1 is written
@@ -708,6 +713,13 @@ void latent_decode_kernel(DecodeGeom g) {
     // this wave loads tokens 8 w4 .. of a tile: lane 8 jj + u takes chunk u ^ swz of token jj of them, nine times
     const int dj = lane >> 3, dma_tok = 8 * w4 + dj;
     const int64_t dma_col = ((lane & 7) ^ mla_swz(w4, dj)) * 16;
+    // Q goes through the last two tile buffers. (Columns past the heads repeat the first and are not stored.)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int h = 32 * t + dma_tok;
+      lds_dma_row9(reinterpret_cast<const uint8_t*>(g.q) + (row0 + (h < nh ? h : 0)) * 1152 + dma_col,
+                   lds_addr(lds + (kLatBufs - 2 + t) * kMlaTile + w4 * (kMlaLoads * 1024)));
+    }
     for (int p0 = t0; p0 < t1; p0 += g.pass_tiles) {
       const int nt = t1 - p0 < g.pass_tiles ? t1 - p0 : g.pass_tiles;
       stage(p0, p0 + nt);
@@ -716,12 +728,26 @@ void latent_decode_kernel(DecodeGeom g) {
         lds_dma_row9((row >= 0 ? kvb + (int64_t)row * 1152 : zero_row) + dma_col, lds_addr(lds + buf + w4 * (kMlaLoads * 1024)));
       };
       uint32_t cur = 0, next = 0;  // buffers of tile it, and of the next tile to load
-#pragma unroll
-      for (int i = 0; i < kLatBufs - 1; ++i)
+      auto fill = [&](int i) {
         if (i < nt) {
           issue(i, next);
           next += kMlaTile;
         }
+      };
+      if (p0 == t0) {
+        fill(0);
+        fill(1);
+        // Q has landed (behind it are one or two tiles), and the scorers have read it
+        if (nt > 1) vm_wait<2 * kMlaLoads>();
+        else vm_wait<kMlaLoads>();
+        lds_barrier();
+        lds_barrier();
+      } else {
+        fill(0);
+        fill(1);
+      }
+      fill(2);
+      static_assert(kLatBufs == 4, "two buffers for Q, two to fill meanwhile");
       u32x4 va[4][2];  // V operands of tile it - 1
       for (int it = 0; it <= nt; ++it) {
         // tile it has landed (behind it are the kLatBufs - 2 next ones, fewer at the end); the scorers' P of tile
