@@ -55,16 +55,17 @@ __device__ __forceinline__ int wave_scan(int x) {
   return x;
 }
 
-// Deals this workgroup its stretch of the tiles of all sequences, M (head, query row block)s each, one
+// Deals this workgroup its stretch of the tiles of all sequences, g.M (head, query row block)s each, one
 // (sequence, head) after the other: an equal share of all, but no fewer tiles than pay for a workgroup. Calls
-// segment(sequence, r in [0, M), span, first tile, last tile + 1, whole, slot of the partial), and tells the
+// segment(sequence, r in [0, g.M), span, first tile, last tile + 1, whole, slot of the partial), and tells the
 // join about every (sequence, head) whose first tile is here. Then the rows of sequences without a tile, dealt
 // to the workgroups. d: width of an output row. (Tiles of all in all fit 30 bits: the host refuses more.)
 //
 // What precedes the first load of a row is a chain of round trips, so the first 64 lengths are loaded once and
 // scanned in registers, and divisions by what the host knows are products.
 template <class F>
-__device__ __forceinline__ void deal(const DecodeGeom& g, int M, int d, F&& segment) {
+__device__ __forceinline__ void deal(const DecodeGeom& g, int d, F&& segment) {
+  const int M = g.M;
   const int lane = threadIdx.x & 63;
   auto length = [&](int b) { return b < g.n_seq ? g.ctx_len[b] : 0; };
   const int ctx0 = length(lane), inc0 = wave_scan(span_of(g, ctx0).nt);
@@ -82,7 +83,7 @@ __device__ __forceinline__ void deal(const DecodeGeom& g, int M, int d, F&& segm
     // the sequence that tile `at` is in, and the tiles (of one head) before it
     int b = 0, before = 0;
     for (int inc = inc0, ctx = ctx0;;) {
-      const uint64_t past = __ballot((int64_t)(before + inc) * M > at);
+      const uint64_t past = __ballot((before + inc) * M > at);
       if (past) {
         const int first = __ffsll((unsigned long long)past) - 1;
         before += __builtin_amdgcn_readlane(inc, first) - span_of(g, __builtin_amdgcn_readlane(ctx, first)).nt;
@@ -104,9 +105,9 @@ __device__ __forceinline__ void deal(const DecodeGeom& g, int M, int d, F&& segm
       const int r = M == 1 ? 0 : uniform((int)((uint32_t)rel / (uint32_t)sp.nt)), t0 = rel - r * sp.nt;
       const int n = end - at < sp.nt - t0 ? end - at : sp.nt - t0;
       const int slot = 2 * (int)blockIdx.x + (at != (int)start);
+      segment(b, r, sp, t0, t0 + n, n == sp.nt, slot);
       if (t0 == 0 && g.parts && threadIdx.x == 0)  // first workgroup, last one, and the first one's partial
         g.parts[(int64_t)b * M + r] = int4{(int)blockIdx.x, (int)((uint32_t)(at + sp.nt - 1) / (uint32_t)share), slot, 0};
-      segment(b, r, sp, t0, t0 + n, n == sp.nt, slot);
       at += n;
       if (r == M - 1 && t0 + n == sp.nt) {
         before += sp.nt;
@@ -134,6 +135,19 @@ __device__ __forceinline__ void lds_dma16(const uint8_t* src, uint32_t lds) {
   uint32_t save;
   asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
                : "=&s"(save) : "v"(src), "s"(lds) : "memory");
+}
+// N <= 4 KB of neighbouring cache rows from `base`: load j takes base + 1024 j + off[j] per lane to LDS bytes lds + 1024 j +
+// 16 lane. (The immediate offset counts for both addresses.)
+template <int N>
+__device__ __forceinline__ void lds_dma16_rows(const uint8_t* base, uint32_t off, uint32_t x1, uint32_t x2, uint32_t x3, uint32_t lds) {
+  uint32_t save;
+  if constexpr (N == 4)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024\n\t"
+                 "global_load_lds_dwordx4 %4, %1 offset:2048\n\tglobal_load_lds_dwordx4 %5, %1 offset:3072\n\ts_mov_b32 m0, %0"
+                 : "=&s"(save) : "s"(base), "v"(off), "v"(off ^ x1), "v"(off ^ x2), "v"(off ^ x3), "s"(lds) : "memory");
+  else
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024\n\ts_mov_b32 m0, %0"
+                 : "=&s"(save) : "s"(base), "v"(off), "v"(off ^ x1), "s"(lds) : "memory");
 }
 __device__ __forceinline__ void lds_dma4(const uint8_t* src, uint32_t lds) {
   uint32_t save;
@@ -184,7 +198,7 @@ struct GqaTile {
   // lanes) and the transposed V reads (per 32 lanes 8 or 16 tokens x 32 or 16 bytes) then fall on all
   // banks alike: with t = 16 a1 + 8 a0 + 4 b + 2 k1 + k0, a K read varies a1, a0, k1, k0, a V read of 32 lanes a0, k1, k0
   // (fp8: and b), and rows of less than 256 bytes spread by their own low token bits.
-  static __device__ __forceinline__ int swz(int t) {
+  static constexpr __host__ __device__ __forceinline__ int swz(int t) {
     const int a1 = (t >> 4) & 1, a0 = (t >> 3) & 1, b = (t >> 2) & 1;
     if constexpr (kChunks == 16) return a1 | (t & 3) << 1 | a0 << 3;
     if constexpr (kChunks == 8) return (a1 ^ b) | (t & 2) | a0 << 2;
@@ -207,8 +221,7 @@ void gqa_decode_kernel(DecodeGeom g) {
   const int wv = uniform((int)(threadIdx.x >> 6));
   uint8_t* const lk = ring[wv];                    // K tiles, then V tiles
   uint8_t* const lv = ring[wv] + NS * T::kBytes;
-  const int group = g.H / g.Hkv, cols = g.R * group;
-  const int cb_n = (cols + COLS - 1) / COLS, M = g.Hkv * cb_n;  // (head, column block)s of a sequence
+  const int group = (int)g.by_group.d, cols = g.R * group, cb_n = (int)g.by_blocks.d;  // query rows of a head, and their blocks
 
   // LDS offsets of this lane's operands: K of token block mt at chunk 4 s + q4, V of value block c
   int k_off[2], k_swz[2];
@@ -224,7 +237,7 @@ void gqa_decode_kernel(DecodeGeom g) {
   const int ld_t = lane / T::kChunks, ld_slot = lane % T::kChunks;
 
   auto segment = [&](int b, int r, const Span& sp, int t0, int t1, bool whole, int slot) {
-    const int kvh = r / cb_n, col0 = (r - kvh * cb_n) * COLS;
+    const int kvh = fdiv(g.by_blocks, r), col0 = (r - kvh * cb_n) * COLS;
     const int ncols = cols - col0 < COLS ? cols - col0 : COLS;
     // ---- Q as the B operand: column 16 nb + i16 = (new token j, head of the group), dims of k-step s. (Columns past the
     // last query row repeat the first one's and are not stored.)
@@ -234,7 +247,7 @@ void gqa_decode_kernel(DecodeGeom g) {
     for (int nb = 0; nb < NB; ++nb) {
       const int col = col0 + 16 * nb + i16;
       const bool ok = 16 * nb + i16 < ncols;
-      const int j = (ok ? col : col0) / group, hh = (ok ? col : col0) - j * group;
+      const int j = fdiv(g.by_group, ok ? col : col0), hh = (ok ? col : col0) - j * group;
       tcol[nb] = sp.c - g.R + j;
       const uint8_t* qp = reinterpret_cast<const uint8_t*>(g.q + (((int64_t)b * g.R + j) * g.H + kvh * group + hh) * D);
 #pragma unroll
@@ -278,49 +291,78 @@ void gqa_decode_kernel(DecodeGeom g) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
       const int nw = p1 - p0 > wv ? (p1 - p0 - wv + kGqaWaves - 1) / kGqaWaves : 0;  // this wave's tiles
-      // cache row of token lane % 32 of this wave's tile i, -1 where nobody attends to it
       auto tile_pos = [&](int i) {
         const int t = p0 + wv + kGqaWaves * i;
         return (t < sp.ns ? t : t + sp.skip) * kTile;
       };
-      auto tile_rows = [&](int i) {
-        const int s = tile_pos(i) + (lane & 31), t = p0 + wv + kGqaWaves * i;
-        const bool seen = s >= 0 && s < sp.c && (s >= sp.lo || s < g.k_sink);
-        if (!seen) return -1;
-        const int pg = fdiv(g.by_page, s);
-        const int ph = pages[t < sp.ns ? pg - f1 : n1 + pg - f2];
-        return ph >= 0 ? (int)(((uint32_t)ph * (uint32_t)g.Hkv + (uint32_t)kvh) * (uint32_t)g.P + (uint32_t)(s - pg * g.P)) : -1;
+      // Where this wave's tile i lies: the cache row of token lane % 32, -1 where nobody attends to it (bits: the tokens
+      // somebody attends to). A tile that lies whole in one page and is attended to whole needs its first row only.
+      struct Where {
+        int rows;
+        uint32_t row0, bits;
       };
-      auto issue = [&](const void* base, uint8_t* dst, int rows) {
+      auto locate = [&](int i) {
+        Where w{-1, 0u, 0u};
+        const int t = p0 + wv + kGqaWaves * i, s0 = tile_pos(i), s = s0 + (lane & 31);
+        const bool seen = s < sp.c && (s >= sp.lo || s < g.k_sink);
+        const int shift = t < sp.ns ? f1 : f2 - n1;
+        if (g.whole_tiles) {
+          const int pg = fdiv(g.by_page, s0), ph = uniform(pages[pg - shift]);
+          w.row0 = ((uint32_t)ph * (uint32_t)g.Hkv + (uint32_t)kvh) * (uint32_t)g.P + (uint32_t)(s0 - pg * g.P);
+          if (ph >= 0) {
+            w.bits = (uint32_t)__ballot(seen);
+            if (w.bits != ~0u) w.rows = seen ? (int)w.row0 + (lane & 31) : -1;
+          }
+          return w;
+        }
+        if (seen) {
+          const int pg = fdiv(g.by_page, s), ph = pages[pg - shift];
+          if (ph >= 0) w.rows = (int)(((uint32_t)ph * (uint32_t)g.Hkv + (uint32_t)kvh) * (uint32_t)g.P + (uint32_t)(s - pg * g.P));
+        }
+        w.bits = (uint32_t)__ballot(w.rows >= 0);
+        return w;
+      };
+      auto issue = [&](const void* base, uint8_t* dst, const Where& w) {
+        if (g.whole_tiles && w.bits == ~0u) {
+          constexpr int N = T::kLoads < 4 ? T::kLoads : 4;
+          // (swz(t + u) = swz(t) ^ swz(u) where the bits of t and u are apart)
+          constexpr uint32_t x1 = T::swz(LT) * 16, x2 = T::swz(2 * LT) * 16, x3 = T::swz(3 * LT) * 16;
+          const uint32_t off = (uint32_t)(ld_t * T::kRow + (ld_slot ^ T::swz(ld_t)) * 16);
+          const uint8_t* src = static_cast<const uint8_t*>(base) + (int64_t)w.row0 * T::kRow;
+#pragma unroll
+          for (int j = 0; j < T::kLoads; j += N) lds_dma16_rows<N>(src + j * 1024, off ^ (T::swz(j * LT) * 16), x1, x2, x3, lds_addr(dst + j * 1024));
+          return;
+        }
 #pragma unroll
         for (int j = 0; j < T::kLoads; ++j) {
-          const int t = j * LT + ld_t, row = __shfl(rows, t);
+          const int t = j * LT + ld_t, row = __shfl(w.rows, t);
           const uint8_t* src = row >= 0 ? static_cast<const uint8_t*>(base) + (int64_t)row * T::kRow : zero_row;
           lds_dma16(src + (ld_slot ^ T::swz(t)) * 16, lds_addr(dst + j * 1024));
         }
       };
-      auto issue_k = [&](int i, int rows) {
+      auto issue_k = [&](int i, const Where& w) {
         const int st = i % NS;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage's last reads are done
         if constexpr (FP8) {
           const float* sc = lane < 32 ? g.k_scale : g.v_scale;
-          lds_dma4(rows >= 0 ? reinterpret_cast<const uint8_t*>(sc + rows) : zero_row, lds_addr(scales[wv][st]));
+          const int row = g.whole_tiles && w.bits == ~0u ? (int)w.row0 + (lane & 31) : w.rows;
+          lds_dma4(row >= 0 ? reinterpret_cast<const uint8_t*>(sc + row) : zero_row, lds_addr(scales[wv][st]));
         }
-        issue(g.k, lk + st * T::kBytes, rows);
+        issue(g.k, lk + st * T::kBytes, w);
       };
-      auto issue_v = [&](int i, int rows) {
+      auto issue_v = [&](int i, const Where& w) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        issue(g.v, lv + (i % NS) * T::kBytes, rows);
+        issue(g.v, lv + (i % NS) * T::kBytes, w);
       };
       uint32_t seen_bits[NS];
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
         seen_bits[i] = 0;
         if (i < nw) {
-          const int rows = tile_rows(i);
-          seen_bits[i] = (uint32_t)__ballot(rows >= 0);
-          issue_k(i, rows);
-          issue_v(i, rows);
+          const Where w = locate(i);
+          seen_bits[i] = w.bits;
+          issue_k(i, w);
+          issue_v(i, w);
         }
       }
       for (int i0 = 0; i0 < nw; i0 += NS) {
@@ -329,7 +371,8 @@ void gqa_decode_kernel(DecodeGeom g) {
           const int i = i0 + st;
           if (i >= nw) break;
           const bool more = i + NS < nw;  // tile i + NS takes this one's place
-          const int rows = more ? tile_rows(i + NS) : -1;
+          Where w{};
+          if (more) w = locate(i + NS);
           const uint32_t bits = seen_bits[st];
           // K of tile i has landed: behind it are its V and the other stages' tiles (fewer at the stretch's end)
           if (i + NS <= nw) vm_wait<T::kLoads + (NS - 1) * T::kPair>();
@@ -380,7 +423,7 @@ void gqa_decode_kernel(DecodeGeom g) {
 #pragma unroll
               for (int k = 0; k < 8; ++k) z[nb][k] = s4[k >> 2][nb][k & 3] * g.scale_log2;
           }
-          if (more) issue_k(i + NS, rows);
+          if (more) issue_k(i + NS, w);
           const int s0 = tile_pos(i);
           // several new tokens: does the tile reach to where they see different positions?
           const bool uneven = g.R > 1 && (s0 + kTile > sp.c - g.R + 1 || (g.k_swa > 0 && s0 < sp.c - g.k_swa));
@@ -447,7 +490,7 @@ void gqa_decode_kernel(DecodeGeom g) {
           } else {
             // a token's row of V reaches only the columns that see it, also if it holds a NaN: one product per new
             // token, its unseen rows of V zeroed, taken by its own columns
-            for (int j = col0 / group; j <= (col0 + ncols - 1) / group; ++j) {
+            for (int j = fdiv(g.by_group, col0); j <= fdiv(g.by_group, col0 + ncols - 1); ++j) {
               const int t = sp.c - g.R + j;
               u32x4 keep;
 #pragma unroll
@@ -469,8 +512,8 @@ void gqa_decode_kernel(DecodeGeom g) {
             }
           }
           if (more) {
-            seen_bits[st] = (uint32_t)__ballot(rows >= 0);
-            issue_v(i + NS, rows);
+            seen_bits[st] = w.bits;
+            issue_v(i + NS, w);
           }
         }
       }
@@ -509,7 +552,7 @@ void gqa_decode_kernel(DecodeGeom g) {
         }
         const int at = col0 + 16 * nb + col;
         if (whole) {
-          const int j = at / group;
+          const int j = fdiv(g.by_group, at);
           const int64_t row = ((int64_t)b * g.R + j) * g.H + kvh * group + at - j * group;
           const float inv = sum == 0.f ? 0.f : 1.f / sum;
           *reinterpret_cast<u32x2*>(g.out + row * D + d) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
@@ -524,7 +567,7 @@ void gqa_decode_kernel(DecodeGeom g) {
     }
   };
 
-  deal(g, M, D, segment);
+  deal(g, D, segment);
 }
 
 // ============================================================================ latent cache
@@ -552,10 +595,10 @@ void latent_decode_kernel(DecodeGeom g) {
   const bool scorer = wv < 4;
   uint8_t* const pslots = lds + kLatBufs * kMlaTile;
   const uint8_t* kvb = static_cast<const uint8_t*>(g.k);
-  const int hb_n = (g.H + 63) / 64, M = g.R * hb_n;  // (new token, 64 heads)s of a sequence
+  const int hb_n = (int)g.by_blocks.d;  // 64 heads each, of one new token
 
   auto segment = [&](int b, int r, const Span& sp, int t0, int t1, bool whole, int slot) {
-    const int j = r / hb_n, h0 = (r - j * hb_n) * 64, nh = g.H - h0 < 64 ? g.H - h0 : 64;
+    const int j = fdiv(g.by_blocks, r), h0 = (r - j * hb_n) * 64, nh = g.H - h0 < 64 ? g.H - h0 : 64;
     const int tq = sp.c - g.R + j;  // this token's position
     const int64_t row0 = ((int64_t)b * g.R + j) * g.H + h0;  // output row of head h0
     // page-table entries of tiles [p0, p1): those before the skipped ones, then the others
@@ -866,7 +909,7 @@ void latent_decode_kernel(DecodeGeom g) {
         for (int q = 0; q < 4; ++q) dst[(4 * c + q) * 64] = f32x4{o[c][4 * q], o[c][4 * q + 1], o[c][4 * q + 2], o[c][4 * q + 3]};
     }
   };
-  deal(g, M, 512, segment);
+  deal(g, 512, segment);
 }
 
 // ============================================================================ joining the partials
@@ -911,26 +954,32 @@ __device__ __forceinline__ Joined join_parts(const int4& p, int sub, ML&& load_m
   }
   return r;
 }
-// The sum over the S threads x, x + T, .. of a workgroup of S T threads (in the first T); lds: S T entries.
+__device__ __forceinline__ void join_two(Joined& r, const Joined& q) {
+  const float mx = fmaxf(r.m, q.m), a = fast_exp2(r.m - mx), f = fast_exp2(q.m - mx);
+  r.l = r.l * a + q.l * f;
+  r.acc = r.acc * a + q.acc * f;
+  r.m = mx;
+}
+// The sum over the S threads x, x + T, .. of a workgroup of S T threads (in its first T), first within waves.
 template <int S, int T>
-__device__ __forceinline__ Joined join_threads(const Joined& mine, Joined* lds) {
-  const int x = threadIdx.x % T, sub = threadIdx.x / T;
-  if (sub) lds[sub * T + x] = mine;
-  __syncthreads();
-  Joined r = mine;
-  if (sub == 0) {
-    float mx = r.m;
-    for (int k = 1; k < S; ++k) mx = fmaxf(mx, lds[k * T + x].m);
-    const float a = fast_exp2(r.m - mx);
-    r.l *= a;
-    r.acc *= a;
-    for (int k = 1; k < S; ++k) {
-      const Joined& q = lds[k * T + x];
-      const float f = fast_exp2(q.m - mx);
-      r.l += q.l * f;
-      r.acc += f * q.acc;
-    }
-    r.m = mx;
+__device__ __forceinline__ Joined join_threads(Joined r, Joined* lds) {
+  constexpr int TW = T < 64 ? T : 64, W = S * T / 64, G = W * TW / T;  // threads of a wave apart, waves, entries per thread
+#pragma unroll
+  for (int o = TW; o < 64; o <<= 1) {
+    Joined q;
+    q.m = __shfl_xor(r.m, o);
+    q.l = __shfl_xor(r.l, o);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) q.acc[k] = __shfl_xor(r.acc[k], o);
+    join_two(r, q);
+  }
+  if constexpr (G > 1) {
+    const int wv = threadIdx.x >> 6, at = wv * TW + (threadIdx.x & 63);  // = group * T + x, T threads of neighbouring waves
+    if ((threadIdx.x & 63) < TW) lds[at] = r;
+    __syncthreads();
+    if ((int)threadIdx.x < T)
+#pragma unroll
+      for (int k = 1; k < G; ++k) join_two(r, lds[k * T + (int)threadIdx.x]);
   }
   return r;
 }
@@ -940,21 +989,20 @@ __device__ __forceinline__ void join_store(const DecodeGeom& g, const Joined& r,
   if (g.lse && d == 0) g.lse[row] = r.l == 0.f ? -INFINITY : (r.m + __log2f(r.l)) * kLn2;
 }
 
-// Grouped heads: a workgroup per output row and 1024 / S of its dims.
-template <int D, int COLS, int S>
-__global__ __launch_bounds__(256) void gqa_join_kernel(DecodeGeom g) {
-  constexpr int T = 256 / S;
-  __shared__ Joined lds[256];
-  const int group = g.H / g.Hkv, cols = g.R * group, cb_n = (cols + COLS - 1) / COLS;
+// Grouped heads: a workgroup per output row and 4 T of its dims.
+template <int D, int COLS, int S, int T>
+__global__ __launch_bounds__(S * T) void gqa_join_kernel(DecodeGeom g) {
+  __shared__ Joined lds[S * T < 64 ? 1 : S * T / 64 * (T < 64 ? T : 64)];
+  const int group = (int)g.by_group.d, cols = g.R * group, cb_n = (int)g.by_blocks.d;
   const int unit = (int)(blockIdx.x / (uint32_t)cols), col = (int)blockIdx.x - unit * cols;  // (sequence, key/value head)
   const int4 p = g.parts[(int64_t)unit * cb_n + col / COLS];
   if (p.x == p.y) return;
   const int d = 4 * (T * (int)blockIdx.y + (int)threadIdx.x % T), cc = col % COLS;
   Joined r = join_parts<S, 4>(p, threadIdx.x / T, [&](int slot) { return *reinterpret_cast<const f32x2*>(g.part_ml + 2 * ((int64_t)slot * COLS + cc)); },
-                           [&](int slot) { return *reinterpret_cast<const f32x4*>(g.part_o + ((int64_t)slot * COLS + cc) * D + d); });
+                              [&](int slot) { return *reinterpret_cast<const f32x4*>(g.part_o + ((int64_t)slot * COLS + cc) * D + d); });
   r = join_threads<S, T>(r, lds);
-  if (threadIdx.x >= T) return;
-  const int b = unit / g.Hkv, kvh = unit - b * g.Hkv, j = col / group;
+  if ((int)threadIdx.x >= T) return;
+  const int b = unit / g.Hkv, kvh = unit - b * g.Hkv, j = fdiv(g.by_group, col);
   join_store(g, r, ((int64_t)b * g.R + j) * g.H + kvh * group + col - j * group, D, d);
 }
 
@@ -963,7 +1011,7 @@ __global__ __launch_bounds__(256) void gqa_join_kernel(DecodeGeom g) {
 template <int S, int T>
 __global__ __launch_bounds__(S * T) void latent_join_kernel(DecodeGeom g) {
   static_assert(T % 64 == 0, "a wave's threads share their partials");
-  __shared__ Joined lds[S * T];
+  __shared__ Joined lds[S * T / 64 * 64];
   const int4 p = g.parts[blockIdx.x];
   if (p.x == p.y) return;
   const int vec = T * (int)blockIdx.y + (int)threadIdx.x % T;
@@ -973,7 +1021,7 @@ __global__ __launch_bounds__(S * T) void latent_join_kernel(DecodeGeom g) {
                            [&](int slot) { return reinterpret_cast<const f32x4*>(g.part_o)[(int64_t)slot * 8192 + vec]; });
   r = join_threads<S, T>(r, lds);
   if (threadIdx.x >= T) return;
-  const int hb_n = (g.H + 63) / 64, row = (int)(blockIdx.x / (uint32_t)hb_n), h = 64 * ((int)blockIdx.x - row * hb_n) + lh;
+  const int hb_n = (int)g.by_blocks.d, row = fdiv(g.by_blocks, (int)blockIdx.x), h = 64 * ((int)blockIdx.x - row * hb_n) + lh;
   if (h < g.H) join_store(g, r, (int64_t)row * g.H + h, 512, d);
 }
 
@@ -987,10 +1035,13 @@ static hipError_t launch_gqa(const DecodeGeom& g, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.part_o == nullptr) return e;
   const int64_t rows = (int64_t)g.n_seq * g.R * g.H;
-  if (rows * (D / 32) <= kJoinFew)
-    hipLaunchKernelGGL((gqa_join_kernel<D, 16 * NB, 32>), dim3((unsigned)rows, D / 32), dim3(256), 0, st, g);
-  else
-    hipLaunchKernelGGL((gqa_join_kernel<D, 16 * NB, 1024 / D>), dim3((unsigned)rows), dim3(256), 0, st, g);
+  if (rows * (D / 32) <= kJoinFew) {
+    // (at most that many partials of a row, if the sequences are alike)
+    if (g.grid / (int)g.by_pairs.d > 32) hipLaunchKernelGGL((gqa_join_kernel<D, 16 * NB, 128, 8>), dim3((unsigned)rows, D / 32), dim3(1024), 0, st, g);
+    else hipLaunchKernelGGL((gqa_join_kernel<D, 16 * NB, 32, 8>), dim3((unsigned)rows, D / 32), dim3(256), 0, st, g);
+  } else {
+    hipLaunchKernelGGL((gqa_join_kernel<D, 16 * NB, 1024 / D, D / 4>), dim3((unsigned)rows), dim3(256), 0, st, g);
+  }
   return hipGetLastError();
 }
 template <int D, bool FP8>
@@ -1004,7 +1055,7 @@ hipError_t launch_decode_attn(const DecodeGeom& g, hipStream_t st) {
     hipLaunchKernelGGL(latent_decode_kernel, dim3((unsigned)g.grid), dim3(512), 0, st, g);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || g.part_o == nullptr) return e;
-    const int64_t units = (int64_t)g.n_seq * g.R * ((g.H + 63) / 64);
+    const int64_t units = (int64_t)g.n_seq * g.M;
     if (units * 128 <= kJoinFew) hipLaunchKernelGGL((latent_join_kernel<16, 64>), dim3((unsigned)units, 128), dim3(1024), 0, st, g);
     else hipLaunchKernelGGL((latent_join_kernel<1, 256>), dim3((unsigned)units, 32), dim3(256), 0, st, g);
     return hipGetLastError();

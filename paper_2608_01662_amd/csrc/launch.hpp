@@ -144,8 +144,12 @@ struct DecodeGeom {
   // the plan
   int cap;            // positions a sequence can have: max_pages * P
   FastDiv by_page;    // division by P
+  int whole_tiles;    // no tile lies in two pages (P is a multiple of the tile)
   int pass_tiles;     // tiles whose page-table entries fit the LDS area
   int block_cols;     // query rows of one key/value head that a workgroup takes together
+  FastDiv by_group;   // division by H / Hkv
+  FastDiv by_blocks;  // by the blocks of block_cols of a head's query rows (latent: of a new token's heads)
+  int M;              // such blocks of a sequence
   int grid;           // workgroups
   FastDiv by_grid;    // division by it
   FastDiv by_pairs;   // by the (sequence, head, query row block)s

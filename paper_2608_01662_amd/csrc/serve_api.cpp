@@ -74,7 +74,7 @@ lsa_status check_decode_sizes(const lsa_decode_attn_params* p, int32_t n_seq, in
 
 // How a call is dealt out (decode_attn.hip): `grid` workgroups take equal stretches of all tiles.
 struct DecodePlan {
-  int grid, min_tiles, block_cols, pass_tiles;
+  int grid, min_tiles, block_cols, blocks, M, pass_tiles;  // (see DecodeGeom)
   bool cut;  // may a stretch end inside a (sequence, head)?
   int64_t pairs, all_tiles;  // (sequence, head, query row block)s; their tiles at most
   size_t off_ml, off_parts, total;
@@ -90,7 +90,9 @@ DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t r
   const bool latent = p->latent != 0;
   const int64_t cols = latent ? p->n_heads : (int64_t)rows_per_seq * (p->n_heads / p->n_kv_heads);
   pl.block_cols = latent ? 64 : cols <= 16 ? 16 : cols <= 32 ? 32 : 64;
-  const int64_t pairs = (int64_t)n_seq * (latent ? rows_per_seq : p->n_kv_heads) * cdiv(cols, pl.block_cols);
+  pl.blocks = (int)cdiv(cols, pl.block_cols);
+  pl.M = (latent ? rows_per_seq : p->n_kv_heads) * pl.blocks;
+  const int64_t pairs = (int64_t)n_seq * pl.M;
   const int64_t cap = (int64_t)max_pages * kv_page_size;
   int64_t tiles = cdiv(cap, kTile);  // of one (sequence, head), at most
   if (p->k_swa > 0) {
@@ -277,7 +279,11 @@ lsa_status lsa_decode_attn(const lsa_decode_attn_params* p, int32_t n_seq, int32
   g.scale_log2 = p->sm_scale * 1.4426950408889634f;
   g.by_page = lsa::fast_div((uint32_t)kv_page_size);
   g.pass_tiles = pl.pass_tiles;
+  g.whole_tiles = kv_page_size % kTile == 0;
   g.block_cols = pl.block_cols;
+  g.by_group = lsa::fast_div((uint32_t)(p->n_heads / p->n_kv_heads));
+  g.by_blocks = lsa::fast_div((uint32_t)pl.blocks);
+  g.M = pl.M;
   g.grid = pl.grid;
   g.by_grid = lsa::fast_div((uint32_t)pl.grid);
   g.by_pairs = lsa::fast_div((uint32_t)pl.pairs);
