@@ -55,6 +55,14 @@ __device__ __forceinline__ int wave_scan(int x) {
   return x;
 }
 
+// The rows of a sequence that attend to nothing (d: width of an output row).
+__device__ __forceinline__ void empty_rows(const DecodeGeom& g, int b, int d) {
+  const int64_t n = (int64_t)g.R * g.H * d;
+  for (int64_t i = 8 * (int64_t)threadIdx.x; i < n; i += 8 * (int64_t)blockDim.x) *reinterpret_cast<u32x4*>(g.out + b * n + i) = u32x4{};
+  if (g.lse)
+    for (int i = (int)threadIdx.x; i < g.R * g.H; i += (int)blockDim.x) g.lse[(int64_t)b * g.R * g.H + i] = -INFINITY;
+}
+
 // Deals this workgroup its stretch of the tiles of all sequences, g.M (head, query row block)s each, one
 // (sequence, head) after the other: an equal share of all, but no fewer tiles than pay for a workgroup. Calls
 // segment(sequence, r in [0, g.M), span, first tile, last tile + 1, whole, slot of the partial), and tells the
@@ -65,65 +73,75 @@ __device__ __forceinline__ int wave_scan(int x) {
 // scanned in registers, and divisions by what the host knows are products.
 template <class F>
 __device__ __forceinline__ void deal(const DecodeGeom& g, int d, F&& segment) {
-  const int M = g.M;
-  const int lane = threadIdx.x & 63;
+  const int M = g.M, lane = threadIdx.x & 63;
+  const bool cut = g.parts != nullptr;
   auto length = [&](int b) { return b < g.n_seq ? g.ctx_len[b] : 0; };
-  const int ctx0 = length(lane), inc0 = wave_scan(span_of(g, ctx0).nt);
-  int total = __builtin_amdgcn_readlane(inc0, 63);
-  for (int b0 = 64; b0 < g.n_seq; b0 += 64) total += __builtin_amdgcn_readlane(wave_scan(span_of(g, length(b0 + lane)).nt), 63);
-  total *= M;
-  int share = fdiv(g.by_grid, total + g.grid - 1);
-  // (where workgroups are idle, one of fewer tiles rather than one for several short (sequence, head)s)
-  const int mean = fdiv(g.by_pairs, total + (int)g.by_pairs.d - 1), least = mean < g.min_tiles ? mean : g.min_tiles;
-  share = share < least ? least : share;
-  const int64_t start = (int64_t)blockIdx.x * share;
-  if (start < total) {
-    int at = (int)start;
-    const int end = total - at < share ? total : at + share;
-    // the sequence that tile `at` is in, and the tiles (of one head) before it
-    int b = 0, before = 0;
-    for (int inc = inc0, ctx = ctx0;;) {
-      const uint64_t past = __ballot((before + inc) * M > at);
-      if (past) {
-        const int first = __ffsll((unsigned long long)past) - 1;
-        before += __builtin_amdgcn_readlane(inc, first) - span_of(g, __builtin_amdgcn_readlane(ctx, first)).nt;
-        b += first;
-        break;
-      }
-      before += __builtin_amdgcn_readlane(inc, 63);
-      b += 64;
-      ctx = length(b + lane);
-      inc = wave_scan(span_of(g, ctx).nt);
-    }
-    while (at < end) {
-      const Span sp = span_of(g, b < 64 ? __builtin_amdgcn_readlane(ctx0, b) : uniform(g.ctx_len[b]));
-      if (sp.nt == 0) {
-        ++b;
-        continue;
-      }
-      const int rel = at - before * M;
-      const int r = M == 1 ? 0 : uniform((int)((uint32_t)rel / (uint32_t)sp.nt)), t0 = rel - r * sp.nt;
-      const int n = end - at < sp.nt - t0 ? end - at : sp.nt - t0;
-      const int slot = 2 * (int)blockIdx.x + (at != (int)start);
-      segment(b, r, sp, t0, t0 + n, n == sp.nt, slot);
-      if (t0 == 0 && g.parts && threadIdx.x == 0)  // first workgroup, last one, and the first one's partial
-        g.parts[(int64_t)b * M + r] = int4{(int)blockIdx.x, (int)((uint32_t)(at + sp.nt - 1) / (uint32_t)share), slot, 0};
-      at += n;
-      if (r == M - 1 && t0 + n == sp.nt) {
-        before += sp.nt;
-        ++b;
+  int ctx0 = 0, share = 0;
+  int at = 0, end = 0, b = 0, before = 0;  // tiles [at, end), the sequence of `at`, tiles (of one head) before that sequence
+  if (!cut) {  // a workgroup per (sequence, head); `before` counts from its own sequence
+    b = fdiv(g.by_m, (int)blockIdx.x);
+    ctx0 = uniform(g.ctx_len[b]);
+    const int nt = span_of(g, ctx0).nt;
+    at = ((int)blockIdx.x - b * M) * nt;
+    end = at + nt;
+  } else {
+    ctx0 = length(lane);
+    const int inc0 = wave_scan(span_of(g, ctx0).nt);
+    int total = __builtin_amdgcn_readlane(inc0, 63);
+    for (int b0 = 64; b0 < g.n_seq; b0 += 64) total += __builtin_amdgcn_readlane(wave_scan(span_of(g, length(b0 + lane)).nt), 63);
+    total *= M;
+    share = fdiv(g.by_grid, total + g.grid - 1);
+    // (where workgroups are idle, one of fewer tiles rather than one for several short (sequence, head)s)
+    const int mean = fdiv(g.by_pairs, total + (int)g.by_pairs.d - 1), least = mean < g.min_tiles ? mean : g.min_tiles;
+    share = share < least ? least : share;
+    const int64_t first = (int64_t)blockIdx.x * share;
+    if (first < total) {
+      at = (int)first;
+      end = total - at < share ? total : at + share;
+      for (int inc = inc0, ctx = ctx0;;) {
+        const uint64_t past = __ballot((before + inc) * M > at);
+        if (past) {
+          const int i = __ffsll((unsigned long long)past) - 1;
+          before += __builtin_amdgcn_readlane(inc, i) - span_of(g, __builtin_amdgcn_readlane(ctx, i)).nt;
+          b += i;
+          break;
+        }
+        before += __builtin_amdgcn_readlane(inc, 63);
+        b += 64;
+        ctx = length(b + lane);
+        inc = wave_scan(span_of(g, ctx).nt);
       }
     }
   }
-  const int64_t row_elems = (int64_t)g.R * g.H * d;
-  for (int b = blockIdx.x; b < g.n_seq; b += g.grid) {
-    if (span_of(g, g.ctx_len[b]).nt != 0) continue;
-    for (int64_t i = 8 * (int64_t)threadIdx.x; i < row_elems; i += 8 * (int64_t)blockDim.x)
-      *reinterpret_cast<u32x4*>(g.out + b * row_elems + i) = u32x4{};
-    if (g.lse)
-      for (int i = (int)threadIdx.x; i < g.R * g.H; i += (int)blockDim.x) g.lse[(int64_t)b * g.R * g.H + i] = -INFINITY;
-    if (g.parts)
-      for (int i = (int)threadIdx.x; i < M; i += (int)blockDim.x) g.parts[(int64_t)b * M + i] = int4{0, 0, 0, 0};
+  const int start = at;
+  while (at < end) {
+    const Span sp = span_of(g, !cut ? ctx0 : b < 64 ? __builtin_amdgcn_readlane(ctx0, b) : uniform(g.ctx_len[b]));
+    if (sp.nt == 0) {
+      ++b;
+      continue;
+    }
+    const int rel = at - before * M;
+    const int r = M == 1 ? 0 : uniform((int)((uint32_t)rel / (uint32_t)sp.nt)), t0 = rel - r * sp.nt;
+    const int n = end - at < sp.nt - t0 ? end - at : sp.nt - t0;
+    const int slot = 2 * (int)blockIdx.x + (at != start);
+    segment(b, r, sp, t0, t0 + n, n == sp.nt, slot);
+    if (t0 == 0 && cut && threadIdx.x == 0)  // first workgroup, last one, and the first one's partial
+      g.parts[(int64_t)b * M + r] = int4{(int)blockIdx.x, (int)((uint32_t)(at + sp.nt - 1) / (uint32_t)share), slot, 0};
+    at += n;
+    if (r == M - 1 && t0 + n == sp.nt) {
+      before += sp.nt;
+      ++b;
+    }
+  }
+  // sequences without a tile
+  if (!cut) {
+    if (end == 0 && (int)blockIdx.x == b * M) empty_rows(g, b, d);
+    return;
+  }
+  for (int e = blockIdx.x; e < g.n_seq; e += g.grid) {
+    if (span_of(g, g.ctx_len[e]).nt != 0) continue;
+    empty_rows(g, e, d);
+    for (int i = (int)threadIdx.x; i < M; i += (int)blockDim.x) g.parts[(int64_t)e * M + i] = int4{0, 0, 0, 0};
   }
 }
 
@@ -328,7 +346,7 @@ void gqa_decode_kernel(DecodeGeom g) {
           // (swz(t + u) = swz(t) ^ swz(u) where the bits of t and u are apart)
           constexpr uint32_t x1 = T::swz(LT) * 16, x2 = T::swz(2 * LT) * 16, x3 = T::swz(3 * LT) * 16;
           const uint32_t off = (uint32_t)(ld_t * T::kRow + (ld_slot ^ T::swz(ld_t)) * 16);
-          const uint8_t* src = static_cast<const uint8_t*>(base) + (int64_t)w.row0 * T::kRow;
+          const uint8_t* src = static_cast<const uint8_t*>(base) + (int64_t)(uint32_t)uniform((int)w.row0) * T::kRow;
 #pragma unroll
           for (int j = 0; j < T::kLoads; j += N) lds_dma16_rows<N>(src + j * 1024, off ^ (T::swz(j * LT) * 16), x1, x2, x3, lds_addr(dst + j * 1024));
           return;

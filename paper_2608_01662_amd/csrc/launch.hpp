@@ -150,6 +150,7 @@ struct DecodeGeom {
   FastDiv by_group;   // division by H / Hkv
   FastDiv by_blocks;  // by the blocks of block_cols of a head's query rows (latent: of a new token's heads)
   int M;              // such blocks of a sequence
+  FastDiv by_m;       // by M
   int grid;           // workgroups
   FastDiv by_grid;    // division by it
   FastDiv by_pairs;   // by the (sequence, head, query row block)s

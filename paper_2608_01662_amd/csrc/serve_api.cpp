@@ -79,9 +79,23 @@ struct DecodePlan {
   int64_t pairs, all_tiles;  // (sequence, head, query row block)s; their tiles at most
   size_t off_ml, off_parts, total;
 };
+constexpr int64_t kCus = 256;
 constexpr int kTile = 32;          // positions of a tile
 constexpr int kPageSlots = 2048;   // page-table entries a workgroup stages at a time
 constexpr int kLatentPages = 1024; // the same, latent cache
+
+// A (sequence, head) of at most that many tiles is left whole: a workgroup each, no scan of the lengths, no partials and
+// no join. What the host knows is the tables' capacity, so the bound also limits what one long sequence among short
+// ones can cost. us of whole calls, cut / whole, sequences x positions:
+//   32 heads on 8 key heads (about 0.3 us a tile in a workgroup of its own; 128 pairs come near the memory's rate):
+//     1 x 128 7.6 / 5.6, 1 x 500 9.6 / 9.5, 1 x 1001 9.6 / 13.6, 4 x 500 10.3 / 9.6, 4 x 1001 11.6 / 14.8, 16 x 500 15.2 / 11.2,
+//     16 x 2000 34.6 / 30.4, 64 x 1000 53.8 / 51.2, 256 x 1000 196 / 187; a window of 1024 on 33 x 12 heads 27.6 / 22.7
+//   latent, 64 heads (0.95 us a tile): 1 x 128 13.3 / 11.1, 1 x 512 14.8 / 22.1, 16 x 500 25.5 / 22.9, 64 x 500 27.3 / 23.9,
+//     64 x 1000 33.1 / 38.6, 256 x 1000 74.4 / 68.2
+int64_t whole_tiles(bool latent, int64_t pairs) {
+  if (latent) return pairs >= 256 ? 40 : 5 + pairs * 2 / 3 < 20 ? 5 + pairs * 2 / 3 : 20;
+  return pairs >= 128 ? 64 : 16;
+}
 
 DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq, int32_t max_pages,
                        int32_t kv_page_size) {
@@ -103,9 +117,10 @@ DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t r
   pl.all_tiles = pairs * tiles;
   pl.pairs = pairs;
   const int64_t some = cdiv(pl.all_tiles, pl.min_tiles), most = some > pairs ? some : pairs;
-  const int64_t wgs = 256 * (latent ? 1 : lsa::gqa_per_cu(p->d_qk, pl.block_cols / 16));
+  const int64_t wgs = kCus * (latent ? 1 : lsa::gqa_per_cu(p->d_qk, pl.block_cols / 16));
   pl.grid = (int)(most < wgs ? most : wgs);
-  pl.cut = true;
+  pl.cut = tiles > whole_tiles(latent, pairs);
+  if (!pl.cut) pl.grid = (int)pairs;
   // pages of a pass: tiles * 32 / P, and two more at the ends of each of two parts
   const int64_t pass = (int64_t)((latent ? kLatentPages : kPageSlots) - 4) * kv_page_size / kTile;
   pl.pass_tiles = (int)(pass < (1 << 26) ? pass : (1 << 26));
@@ -284,6 +299,7 @@ lsa_status lsa_decode_attn(const lsa_decode_attn_params* p, int32_t n_seq, int32
   g.by_group = lsa::fast_div((uint32_t)(p->n_heads / p->n_kv_heads));
   g.by_blocks = lsa::fast_div((uint32_t)pl.blocks);
   g.M = pl.M;
+  g.by_m = lsa::fast_div((uint32_t)pl.M);
   g.grid = pl.grid;
   g.by_grid = lsa::fast_div((uint32_t)pl.grid);
   g.by_pairs = lsa::fast_div((uint32_t)pl.pairs);
