@@ -91,8 +91,10 @@ __device__ __forceinline__ void deal(const DecodeGeom& g, int d, F&& segment) {
     for (int b0 = 64; b0 < g.n_seq; b0 += 64) total += __builtin_amdgcn_readlane(wave_scan(span_of(g, length(b0 + lane)).nt), 63);
     total *= M;
     share = fdiv(g.by_grid, total + g.grid - 1);
+    int least = least_tiles(total, g.min_tiles);
     // (where workgroups are idle, one of fewer tiles rather than one for several short (sequence, head)s)
-    const int mean = fdiv(g.by_pairs, total + (int)g.by_pairs.d - 1), least = mean < g.min_tiles ? mean : g.min_tiles;
+    const int mean = fdiv(g.by_pairs, total + (int)g.by_pairs.d - 1);
+    least = mean < least ? mean : least;
     share = share < least ? least : share;
     const int64_t first = (int64_t)blockIdx.x * share;
     if (first < total) {

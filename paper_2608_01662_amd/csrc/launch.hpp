@@ -154,10 +154,18 @@ struct DecodeGeom {
   int grid;           // workgroups
   FastDiv by_grid;    // division by it
   FastDiv by_pairs;   // by the (sequence, head, query row block)s
-  int min_tiles;      // tiles that pay for a workgroup
+  int min_tiles;      // fewest tiles of a workgroup (see least_tiles)
   float *part_o, *part_ml;  // two partials per workgroup: [block_cols, d_v], [block_cols, 2]; nullptr: none is cut
   int4* parts;        // [n_seq, M]: first and last workgroup of each (sequence, head), slot of the first one's partial
 };
+// Tiles that pay for a workgroup in a call of `total` tiles: n workgroups take total / n tiles each and leave n partials
+// to be written and joined, and the sum of both is least at n ~ sqrt(total). In steps of `step` (grouped heads: four
+// waves). us at fixed tiles per workgroup: latent 1000 positions (32 tiles) 2 14.0, 4 15.1; 16K (512) 4 25.4, 6 23.9, 12 26.7; 64K
+// (2048) 8 34.0, 12 32.5, 16 33.7; MQA 16K (512) 4 11.8, 8 11.9; 128K (4096) 8 21.7, 16 20.5.
+__host__ __device__ inline int least_tiles(int64_t total, int step) {
+  const int t = (int)(__builtin_sqrtf((float)total) * 0.25f + 0.5f);
+  return t < step ? step : step == 4 ? t & -4 : t;
+}
 // Workgroups of the grouped-head kernel per CU: two where the registers of NB blocks of 16 query rows allow it.
 constexpr int gqa_per_cu(int d, int nb) { return nb * d <= 256 ? 2 : 1; }
 hipError_t launch_decode_attn(const DecodeGeom& g, hipStream_t st);

@@ -113,10 +113,10 @@ DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t r
     const int64_t window = cdiv(p->k_sink, kTile) + cdiv((int64_t)p->k_swa + rows_per_seq, kTile) + 1;
     tiles = window < tiles ? window : tiles;
   }
-  pl.min_tiles = 4;  // one per wave
+  pl.min_tiles = latent ? 2 : 4;  // (grouped heads: one per wave)
   pl.all_tiles = pairs * tiles;
   pl.pairs = pairs;
-  const int64_t some = cdiv(pl.all_tiles, pl.min_tiles), most = some > pairs ? some : pairs;
+  const int64_t some = cdiv(pl.all_tiles, lsa::least_tiles(pl.all_tiles, pl.min_tiles)), most = some > pairs ? some : pairs;
   const int64_t wgs = kCus * (latent ? 1 : lsa::gqa_per_cu(p->d_qk, pl.block_cols / 16));
   pl.grid = (int)(most < wgs ? most : wgs);
   pl.cut = tiles > whole_tiles(latent, pairs);
