@@ -301,8 +301,8 @@ lsa_status lsa_hfa_attn(const lsa_attn_params* p, int64_t n_rows, const void* q,
  *     where the pair is dims (i, i + rot_dim / 2) of the rotated part, or (2 i, 2 i + 1) when interleaved;
  *   - keys and values are written to the token's row of the caches, in bf16, or as e4m3 codes with one
  *     fp32 scale per token and head (scale = max |x| / 448 over the rotated row, at least 2^-126; 1 for a
- *     row of zeros; code = x / scale, both rounded to nearest even); the products are fp32 and each stored
- *     value is rounded once;
+ *     row of zeros; code = x / scale, rounded to nearest even); the products are fp32 and each stored value is
+ *     rounded once;
  *   - queries are written to q_out, rotated.
  * It serves the cache of MQA and grouped heads (keys and values), the MLA latent cache (d_v = 0, the
  * latent and its rotated part given apart) and the indexer's key cache (d_v = 0, fp8).

@@ -11,24 +11,22 @@ namespace lsa {
 
 constexpr int kAppendThreads = 256;
 
-// What a token is: its sequence and position (pos < 0: none), and the page offset of its row.
+__device__ __forceinline__ int fdiv(const FastDiv& f, int n) { return (int)(((uint64_t)(uint32_t)n * f.mul) >> f.shift); }
+
+// What token t of this launch is: its sequence and position (pos < 0: none).
 struct AppendToken {
   int seq, pos;
 };
-__device__ __forceinline__ AppendToken append_token(const AppendGeom& g, int64_t t) {
+__device__ __forceinline__ AppendToken append_token(const AppendGeom& g, int t) {
   AppendToken r;
-  r.seq = g.seq ? g.seq[t] : (int)(t / g.rows_per_seq);
+  const int nth = g.tok0 + t, by_rows = fdiv(g.by_rows, nth);
+  r.seq = g.seq ? g.seq[nth] : by_rows;
   if (r.seq < 0 || r.seq >= g.n_seq) return AppendToken{0, -1};
-  const int64_t p = g.pos ? g.pos[t] : (int64_t)g.ctx_len[r.seq] - g.rows_per_seq + (int)(t - (int64_t)r.seq * g.rows_per_seq);
+  const int rows = (int)g.by_rows.d;
+  const int64_t p = g.pos ? g.pos[nth] : (int64_t)g.ctx_len[r.seq] - rows + (nth - by_rows * rows);
   const bool ok = p >= 0 && p < (int64_t)g.max_pages * g.P && (g.rot_dim == 0 || p < g.rope_rows);
   r.pos = ok ? (int)p : -1;
   return r;
-}
-// Physical page of a token, -1 when it has none.
-__device__ __forceinline__ int64_t append_page(const AppendGeom& g, const AppendToken& t) {
-  if (t.pos < 0) return -1;
-  const int64_t ph = g.page_table ? g.page_table[(int64_t)t.seq * g.max_pages + t.pos / g.P] : t.seq;
-  return ph >= 0 && ph < g.n_phys ? ph : -1;
 }
 
 __device__ __forceinline__ void unpack8(u32x4 v, float* x) {
@@ -55,15 +53,15 @@ __device__ __forceinline__ Unit unit_of(const AppendGeom& g, int u) {
 
 // x[0..8) and x[8..16): the values at dims lo and hi, rotated where the unit is.
 __device__ __forceinline__ void load_unit(const AppendGeom& g, const uint16_t* x, int64_t stride, const uint16_t* part,
-                                          int64_t part_stride, int64_t t, int head, const Unit& u, int pos, float* y) {
+                                          int64_t part_stride, int t, int head, const Unit& u, int pos, float* y) {
   const uint16_t* p;
   int lo = u.lo, hi = u.hi;
   if (part == nullptr) {
-    p = x + t * stride + (int64_t)head * g.d_k;
+    p = x + (int64_t)t * stride + (int64_t)head * g.d_k;
   } else if (u.pair < 0) {
-    p = x + t * stride + (int64_t)head * (g.d_k - g.rot_dim);
+    p = x + (int64_t)t * stride + (int64_t)head * (g.d_k - g.rot_dim);
   } else {
-    p = part + t * part_stride + (int64_t)head * g.rot_dim;
+    p = part + (int64_t)t * part_stride + (int64_t)head * g.rot_dim;
     lo -= g.rot_start;
     hi -= g.rot_start;
   }
@@ -100,37 +98,37 @@ __device__ __forceinline__ u32x2 pack_fp8x8(const float* x) {
 // Blocks [0, bq) rotate queries, [bq, bq + bk) append keys, the rest values. A head's units are dealt to
 // `lanes` neighbouring threads: as many as it has, or for fp8 rows the next power of two, so that the lanes
 // of a row exchange their maximum within one wave.
-__global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendGeom g, int64_t bq, int64_t bk, int k_lanes, int v_lanes) {
-  const int64_t blk = blockIdx.x;
+__global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendGeom g, int bq, int bk) {
+  const int blk = (int)blockIdx.x;
   if (blk < bq) {
-    const int units = g.d_k / 16;
-    const int64_t item = blk * kAppendThreads + threadIdx.x, vec = item / units;
-    if (vec >= g.n_tok * g.H) return;
-    const int64_t t = vec / g.H;
+    const int item = blk * kAppendThreads + (int)threadIdx.x, vec = fdiv(g.by_q_units, item), t = fdiv(g.by_q_heads, vec);
+    if (t >= g.n_tok) return;
     const AppendToken tok = append_token(g, t);
-    const Unit u = unit_of(g, (int)(item - vec * units));
+    const Unit u = unit_of(g, item - vec * (int)g.by_q_units.d);
     float y[16];
-    load_unit(g, g.q, g.q_stride, g.q_rot, g.q_rot_stride, t, (int)(vec - t * g.H), u, tok.pos, y);
+    load_unit(g, g.q, g.q_stride, g.q_rot, g.q_rot_stride, t, vec - t * g.H, u, tok.pos, y);
     if (tok.pos < 0) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) y[i] = 0.f;
     }
-    uint16_t* o = g.q_out + vec * g.d_k;
+    uint16_t* o = g.q_out + (int64_t)vec * g.d_k;
     *reinterpret_cast<u32x4*>(o + u.lo) = pack8(y);
     *reinterpret_cast<u32x4*>(o + u.hi) = pack8(y + 8);
     return;
   }
   const bool key = blk < bq + bk;
-  const int lanes = key ? k_lanes : v_lanes, d = key ? g.d_k : g.d_v, units = d / 16;
-  const int64_t item = (key ? blk - bq : blk - bq - bk) * kAppendThreads + threadIdx.x;
-  const int64_t vec = item / lanes;
-  if (vec >= g.n_tok * g.Hkv) return;  // (whole groups of lanes leave)
-  const int64_t t = vec / g.Hkv;
-  const int head = (int)(vec - t * g.Hkv), ui = (int)(item - vec * lanes);
+  const FastDiv& by_lanes = key ? g.by_k_lanes : g.by_v_lanes;
+  const int d = key ? g.d_k : g.d_v, units = d / 16, lanes = (int)by_lanes.d;
+  const int item = (key ? blk - bq : blk - bq - bk) * kAppendThreads + (int)threadIdx.x;
+  const int vec = fdiv(by_lanes, item), t = fdiv(g.by_kv_heads, vec);
+  if (t >= g.n_tok) return;  // (whole groups of lanes leave)
+  const int head = vec - t * g.Hkv, ui = item - vec * lanes;
   const AppendToken tok = append_token(g, t);
-  const int64_t page = append_page(g, tok);
-  const int off = tok.pos < 0 ? 0 : tok.pos % g.P;
-  if (key && head == 0 && ui == 0 && g.rows) g.rows[t] = page < 0 ? -1 : page * g.P + off;
+  const int pg = tok.pos < 0 ? 0 : fdiv(g.by_page, tok.pos), off = tok.pos < 0 ? 0 : tok.pos - pg * g.P;
+  int64_t page = -1;
+  if (tok.pos >= 0) page = g.page_table ? g.page_table[(int64_t)tok.seq * g.max_pages + pg] : tok.seq;
+  if (page >= g.n_phys) page = -1;
+  if (key && head == 0 && ui == 0 && g.rows) g.rows[g.tok0 + t] = page < 0 ? -1 : page * g.P + off;
   float y[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) y[i] = 0.f;
@@ -140,7 +138,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendGeom g, in
       u = unit_of(g, ui);
       load_unit(g, g.k, g.k_stride, g.k_rot, g.k_rot_stride, t, head, u, tok.pos, y);
     } else {
-      const uint16_t* p = g.v + t * g.v_stride + (int64_t)head * d;
+      const uint16_t* p = g.v + (int64_t)t * g.v_stride + head * d;
       unpack8(*reinterpret_cast<const u32x4*>(p + u.lo), y);
       unpack8(*reinterpret_cast<const u32x4*>(p + u.hi), y + 8);
     }
@@ -164,8 +162,12 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendGeom g, in
   float* sc = key ? g.k_scale : g.v_scale;
   if (ui == 0) sc[row] = scale;
   if (ui >= units) return;
+  const float inv = 1.f / scale;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) y[i] = y[i] / scale;
+  for (int i = 0; i < 16; ++i) {  // y / scale: the product with the reciprocal, corrected by its remainder
+    const float q = y[i] * inv;
+    y[i] = fmaf(fmaf(-q, scale, y[i]), inv, q);
+  }
   uint8_t* o = static_cast<uint8_t*>(key ? g.k_cache : g.v_cache) + row * d;
   *reinterpret_cast<u32x2*>(o + u.lo) = pack_fp8x8(y);
   *reinterpret_cast<u32x2*>(o + u.hi) = pack_fp8x8(y + 8);
@@ -178,13 +180,37 @@ static int append_lanes(int units, bool fp8) {
   return l;
 }
 
-hipError_t launch_append(const AppendGeom& g, hipStream_t st) {
-  const int k_lanes = append_lanes(g.d_k / 16, g.fp8), v_lanes = g.d_v ? append_lanes(g.d_v / 16, g.fp8) : 1;
-  auto blocks = [](int64_t items) { return (items + kAppendThreads - 1) / kAppendThreads; };
-  const int64_t bq = blocks(g.n_tok * g.H * (g.d_k / 16)), bk = blocks(g.n_tok * g.Hkv * k_lanes);
-  const int64_t bv = g.d_v ? blocks(g.n_tok * g.Hkv * v_lanes) : 0;
-  hipLaunchKernelGGL(append_kernel, dim3((unsigned)(bq + bk + bv)), dim3(kAppendThreads), 0, st, g, bq, bk, k_lanes, v_lanes);
-  return hipGetLastError();
+hipError_t launch_append(const AppendGeom& all, hipStream_t st) {
+  AppendGeom g = all;
+  const int q_units = g.H ? g.d_k / 16 : 1, k_lanes = append_lanes(g.d_k / 16, g.fp8), v_lanes = g.d_v ? append_lanes(g.d_v / 16, g.fp8) : 1;
+  g.by_q_units = fast_div((uint32_t)q_units);
+  g.by_q_heads = fast_div((uint32_t)(g.H ? g.H : 1));
+  g.by_kv_heads = fast_div((uint32_t)g.Hkv);
+  g.by_k_lanes = fast_div((uint32_t)k_lanes);
+  g.by_v_lanes = fast_div((uint32_t)v_lanes);
+  g.by_page = fast_div((uint32_t)g.P);
+  // a launch of as many tokens as 31 bits count threads for
+  int64_t most = (int64_t)g.H * q_units;
+  if (most < (int64_t)g.Hkv * k_lanes) most = (int64_t)g.Hkv * k_lanes;
+  if (most < (int64_t)g.Hkv * v_lanes) most = (int64_t)g.Hkv * v_lanes;
+  const int64_t tokens = ((int64_t(1) << 31) - 2 * kAppendThreads) / most;
+  auto blocks = [](int64_t items) { return (int)((items + kAppendThreads - 1) / kAppendThreads); };
+  for (int64_t t0 = 0; t0 < all.n_tok; t0 += tokens) {
+    g.tok0 = (int)t0;
+    g.n_tok = (int)(all.n_tok - t0 < tokens ? all.n_tok - t0 : tokens);
+    if (all.q) g.q = all.q + t0 * g.q_stride;
+    if (all.q_rot) g.q_rot = all.q_rot + t0 * g.q_rot_stride;
+    if (all.q_out) g.q_out = all.q_out + t0 * g.H * g.d_k;
+    g.k = all.k + t0 * g.k_stride;
+    if (all.k_rot) g.k_rot = all.k_rot + t0 * g.k_rot_stride;
+    if (all.v) g.v = all.v + t0 * g.v_stride;
+    const int bq = g.H ? blocks((int64_t)g.n_tok * g.H * q_units) : 0, bk = blocks((int64_t)g.n_tok * g.Hkv * k_lanes);
+    const int bv = g.d_v ? blocks((int64_t)g.n_tok * g.Hkv * v_lanes) : 0;
+    hipLaunchKernelGGL(append_kernel, dim3((unsigned)bq + (unsigned)bk + (unsigned)bv), dim3(kAppendThreads), 0, st, g, bq, bk);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace lsa

@@ -122,9 +122,15 @@ struct AppendGeom {
   void *k_cache, *v_cache;
   float *k_scale, *v_scale;
   int64_t* rows;
-  int64_t n_tok, n_phys;
+  int64_t n_phys;
+  int n_tok;
   int H, Hkv, d_k, d_v, rot_start, rot_dim, interleaved, fp8;
-  int n_seq, rows_per_seq, max_pages, P;
+  int n_seq, max_pages, P;
+  FastDiv by_rows;  // division by rows_per_seq
+  // set by the launcher: first token of the launch (seq, pos, ctx_len and rows are indexed from the call's first), and
+  // divisions by the threads of a head, the heads of a token and P
+  int tok0;
+  FastDiv by_q_units, by_q_heads, by_kv_heads, by_k_lanes, by_v_lanes, by_page;
 };
 hipError_t launch_append(const AppendGeom& g, hipStream_t st);
 

@@ -183,9 +183,6 @@ lsa_status lsa_cache_append(const lsa_append_params* p, const lsa_append_tensors
   LSA_REQUIRE(aligned(t->seq, 4) && aligned(t->pos, 4) && aligned(t->ctx_len, 4) && aligned(t->page_table, 4) &&
                   aligned(t->k_scale, 4) && aligned(t->v_scale, 4) && aligned(t->rows, 8),
               LSA_ERR_INVALID_ARG, "seq, pos, ctx_len, page_table and scales must be 4-byte aligned, rows 8-byte");
-  // a thread per 16 values, in one launch
-  const int64_t threads = n_tok * ((int64_t)p->n_heads * (p->d_k / 16) + (int64_t)p->n_kv_heads * 128);
-  LSA_REQUIRE(threads < (1LL << 38), LSA_ERR_UNSUPPORTED, "the call is too large; append in parts");
 
   lsa::AppendGeom g{};
   g.q = static_cast<const uint16_t*>(t->q);
@@ -210,7 +207,7 @@ lsa_status lsa_cache_append(const lsa_append_params* p, const lsa_append_tensors
   g.k_scale = t->k_scale;
   g.v_scale = t->v_scale;
   g.rows = t->rows;
-  g.n_tok = n_tok;
+  g.n_tok = (int)n_tok;
   g.n_phys = n_phys;
   g.H = p->n_heads;
   g.Hkv = p->n_kv_heads;
@@ -221,7 +218,7 @@ lsa_status lsa_cache_append(const lsa_append_params* p, const lsa_append_tensors
   g.interleaved = p->interleaved;
   g.fp8 = fp8;
   g.n_seq = n_seq;
-  g.rows_per_seq = rows_per_seq;
+  g.by_rows = lsa::fast_div((uint32_t)rows_per_seq);
   g.max_pages = max_pages;
   g.P = kv_page_size;
   const hipError_t e = lsa::launch_append(g, static_cast<hipStream_t>(stream));
