@@ -51,29 +51,20 @@ __device__ __forceinline__ Unit unit_of(const AppendGeom& g, int u) {
   return Unit{g.rot_start + 8 * c, g.rot_start + g.rot_dim / 2 + 8 * c, 8 * c};
 }
 
-// x[0..8) and x[8..16): the values at dims lo and hi, rotated where the unit is.
-__device__ __forceinline__ void load_unit(const AppendGeom& g, const uint16_t* x, int64_t stride, const uint16_t* part,
-                                          int64_t part_stride, int t, int head, const Unit& u, int pos, float* y) {
-  const uint16_t* p;
-  int lo = u.lo, hi = u.hi;
-  if (part == nullptr) {
-    p = x + (int64_t)t * stride + (int64_t)head * g.d_k;
-  } else if (u.pair < 0) {
-    p = x + (int64_t)t * stride + (int64_t)head * (g.d_k - g.rot_dim);
-  } else {
-    p = part + (int64_t)t * part_stride + (int64_t)head * g.rot_dim;
-    lo -= g.rot_start;
-    hi -= g.rot_start;
-  }
-  unpack8(*reinterpret_cast<const u32x4*>(p + lo), y);
-  unpack8(*reinterpret_cast<const u32x4*>(p + hi), y + 8);
-  if (u.pair < 0 || pos < 0) return;
+// The angles of a unit's pairs at a position.
+struct Angles {
+  f32x4 c0, c1, s0, s1;
+};
+__device__ __forceinline__ Angles load_angles(const AppendGeom& g, const Unit& u, int pos) {
   const f32x4* cs = reinterpret_cast<const f32x4*>(g.rope + (int64_t)pos * g.rot_dim + u.pair);
   const f32x4* sn = reinterpret_cast<const f32x4*>(g.rope + (int64_t)pos * g.rot_dim + g.rot_dim / 2 + u.pair);
-  const f32x4 c0 = cs[0], c1 = cs[1], s0 = sn[0], s1 = sn[1];
+  return Angles{cs[0], cs[1], sn[0], sn[1]};
+}
+// y[0..8) and y[8..16) are the values at dims lo and hi.
+__device__ __forceinline__ void rotate(const AppendGeom& g, const Angles& an, float* y) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float c = i < 4 ? c0[i & 3] : c1[i & 3], s = i < 4 ? s0[i & 3] : s1[i & 3];
+    const float c = i < 4 ? an.c0[i & 3] : an.c1[i & 3], s = i < 4 ? an.s0[i & 3] : an.s1[i & 3];
     const float a = g.interleaved ? y[2 * i] : y[i], b = g.interleaved ? y[2 * i + 1] : y[i + 8];
     const float ra = a * c - b * s, rb = b * c + a * s;
     if (g.interleaved) {
@@ -84,6 +75,13 @@ __device__ __forceinline__ void load_unit(const AppendGeom& g, const uint16_t* x
       y[i + 8] = rb;
     }
   }
+}
+// Where a unit of head `head` of token t lies: in x, or with the rotated dims apart in x or `part`.
+__device__ __forceinline__ const uint16_t* unit_base(const AppendGeom& g, const uint16_t* x, int64_t stride, const uint16_t* part,
+                                                     int64_t part_stride, int t, int head, const Unit& u) {
+  if (part == nullptr) return x + (int64_t)t * stride + (int64_t)head * g.d_k;
+  if (u.pair < 0) return x + (int64_t)t * stride + (int64_t)head * (g.d_k - g.rot_dim);
+  return part + (int64_t)t * part_stride + (int64_t)head * g.rot_dim - g.rot_start;
 }
 
 // Eight values as e4m3 codes (round to nearest even; NaN stays NaN; |x| < 464).
@@ -98,6 +96,7 @@ __device__ __forceinline__ u32x2 pack_fp8x8(const float* x) {
 // Blocks [0, bq) rotate queries, [bq, bq + bk) append keys, the rest values. A head's units are dealt to
 // `lanes` neighbouring threads: as many as it has, or for fp8 rows the next power of two, so that the lanes
 // of a row exchange their maximum within one wave.
+template <int HEADS>  // query heads per thread
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendGeom g, int bq, int bk) {
   const int blk = (int)blockIdx.x;
   if (blk < bq) {
@@ -105,15 +104,31 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendGeom g, in
     if (t >= g.n_tok) return;
     const AppendToken tok = append_token(g, t);
     const Unit u = unit_of(g, item - vec * (int)g.by_q_units.d);
-    float y[16];
-    load_unit(g, g.q, g.q_stride, g.q_rot, g.q_rot_stride, t, vec - t * g.H, u, tok.pos, y);
-    if (tok.pos < 0) {
+    const int head = (vec - t * (int)g.by_q_heads.d) * HEADS;
+    u32x4 x[HEADS][2];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) y[i] = 0.f;
+    for (int h = 0; h < HEADS; ++h) {
+      const uint16_t* p = unit_base(g, g.q, g.q_stride, g.q_rot, g.q_rot_stride, t, head + h, u);
+      x[h][0] = *reinterpret_cast<const u32x4*>(p + u.lo);
+      x[h][1] = *reinterpret_cast<const u32x4*>(p + u.hi);
     }
-    uint16_t* o = g.q_out + (int64_t)vec * g.d_k;
-    *reinterpret_cast<u32x4*>(o + u.lo) = pack8(y);
-    *reinterpret_cast<u32x4*>(o + u.hi) = pack8(y + 8);
+    const bool turn = u.pair >= 0 && tok.pos >= 0;
+    Angles an{};
+    if (turn) an = load_angles(g, u, tok.pos);
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h) {
+      float y[16];
+      unpack8(x[h][0], y);
+      unpack8(x[h][1], y + 8);
+      if (turn) rotate(g, an, y);
+      if (tok.pos < 0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[i] = 0.f;
+      }
+      uint16_t* o = g.q_out + ((int64_t)t * g.H + head + h) * g.d_k;
+      *reinterpret_cast<u32x4*>(o + u.lo) = pack8(y);
+      *reinterpret_cast<u32x4*>(o + u.hi) = pack8(y + 8);
+    }
     return;
   }
   const bool key = blk < bq + bk;
@@ -134,14 +149,11 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendGeom g, in
   for (int i = 0; i < 16; ++i) y[i] = 0.f;
   Unit u{16 * ui, 16 * ui + 8, -1};
   if (ui < units) {
-    if (key) {
-      u = unit_of(g, ui);
-      load_unit(g, g.k, g.k_stride, g.k_rot, g.k_rot_stride, t, head, u, tok.pos, y);
-    } else {
-      const uint16_t* p = g.v + (int64_t)t * g.v_stride + head * d;
-      unpack8(*reinterpret_cast<const u32x4*>(p + u.lo), y);
-      unpack8(*reinterpret_cast<const u32x4*>(p + u.hi), y + 8);
-    }
+    if (key) u = unit_of(g, ui);
+    const uint16_t* p = key ? unit_base(g, g.k, g.k_stride, g.k_rot, g.k_rot_stride, t, head, u) : g.v + (int64_t)t * g.v_stride + head * d;
+    unpack8(*reinterpret_cast<const u32x4*>(p + u.lo), y);
+    unpack8(*reinterpret_cast<const u32x4*>(p + u.hi), y + 8);
+    if (u.pair >= 0 && tok.pos >= 0) rotate(g, load_angles(g, u, tok.pos), y);
   }
   const int64_t row = (page * g.Hkv + head) * g.P + off;
   if (!g.fp8) {
@@ -180,11 +192,13 @@ static int append_lanes(int units, bool fp8) {
   return l;
 }
 
+constexpr int64_t kManyUnits = 1 << 18;
 hipError_t launch_append(const AppendGeom& all, hipStream_t st) {
   AppendGeom g = all;
   const int q_units = g.H ? g.d_k / 16 : 1, k_lanes = append_lanes(g.d_k / 16, g.fp8), v_lanes = g.d_v ? append_lanes(g.d_v / 16, g.fp8) : 1;
+  const int heads = g.H % 4 == 0 && all.n_tok * g.H * q_units >= kManyUnits ? 4 : 1;
   g.by_q_units = fast_div((uint32_t)q_units);
-  g.by_q_heads = fast_div((uint32_t)(g.H ? g.H : 1));
+  g.by_q_heads = fast_div((uint32_t)(g.H ? g.H / heads : 1));
   g.by_kv_heads = fast_div((uint32_t)g.Hkv);
   g.by_k_lanes = fast_div((uint32_t)k_lanes);
   g.by_v_lanes = fast_div((uint32_t)v_lanes);
@@ -204,9 +218,10 @@ hipError_t launch_append(const AppendGeom& all, hipStream_t st) {
     g.k = all.k + t0 * g.k_stride;
     if (all.k_rot) g.k_rot = all.k_rot + t0 * g.k_rot_stride;
     if (all.v) g.v = all.v + t0 * g.v_stride;
-    const int bq = g.H ? blocks((int64_t)g.n_tok * g.H * q_units) : 0, bk = blocks((int64_t)g.n_tok * g.Hkv * k_lanes);
+    const int bq = g.H ? blocks((int64_t)g.n_tok * (g.H / heads) * q_units) : 0, bk = blocks((int64_t)g.n_tok * g.Hkv * k_lanes);
     const int bv = g.d_v ? blocks((int64_t)g.n_tok * g.Hkv * v_lanes) : 0;
-    hipLaunchKernelGGL(append_kernel, dim3((unsigned)bq + (unsigned)bk + (unsigned)bv), dim3(kAppendThreads), 0, st, g, bq, bk);
+    hipLaunchKernelGGL(heads == 4 ? append_kernel<4> : append_kernel<1>, dim3((unsigned)bq + (unsigned)bk + (unsigned)bv), dim3(kAppendThreads), 0,
+                       st, g, bq, bk);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -330,3 +330,23 @@ def test_append_refusals():
     with pytest.raises(lsa.LSAError, match="k_rot"):            # the rotated dims are not the last
         call(A(4, 2, 64, 64, 0, 32), k=torch.zeros((n, 2, 32), dtype=torch.bfloat16, device=dev), rope=x["rope"][:, :32].contiguous(),
              k_rot=torch.zeros((n, 2, 32), dtype=torch.bfloat16, device=dev))
+
+
+@pytest.mark.parametrize("prm,kw,n", [(A(32, 8, 128, 128, 0, 64, False, True), dict(fused=True), 2100),
+                                      (A(64, 1, 576, 0, 512, 64, True, False), dict(split=True), 300),
+                                      (A(36, 4, 64, 64, 16, 32, True, False), {}, 4000)], ids=["gqa", "latent", "partial"])
+def test_large_calls_equal_small_ones(prm, kw, n):
+    """A call of many tokens (several query heads per thread) gives the bits of the same tokens in small calls."""
+    s = _setup(prm, [n // 3 + 40, n - n // 3 + 5], [n // 3, n - n // 3], 64, seed=n, **kw)
+    x, rope, table = _dev_inputs(s), s["rope"].to(DEV), _i32(s["table"])
+    pos, seq = _i32(s["pos"]), _i32(s["seq"])
+    seq[5] = 7      # no such sequence: zero queries in both
+    a, b = _caches(prm, s), _caches(prm, s)
+    q, rows = lsa.cache_append(prm, page_table=table, pos=pos, seq=seq, rope=rope, rows=True, **x, **a)
+    for t in range(0, n, 97):
+        part = slice(t, min(n, t + 97))
+        qs, rs = lsa.cache_append(prm, page_table=table, pos=pos[part], seq=seq[part], rope=rope, rows=True,
+                                  **{k: v[part] for k, v in x.items()}, **b)
+        assert torch.equal(qs, q[part]) and torch.equal(rs, rows[part])
+    for name in a:
+        assert torch.equal(a[name], b[name]), name
