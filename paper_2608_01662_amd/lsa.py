@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -48,6 +49,10 @@ class _AppendTensors(ctypes.Structure):
                [("rope", ctypes.c_void_p), ("rope_rows", ctypes.c_int64)] + \
                [(n, ctypes.c_void_p) for n in ("seq", "pos", "ctx_len", "page_table", "q_out", "k_cache", "k_scale",
                                                "v_cache", "v_scale", "rows")]
+
+
+_APPEND_TENSORS = struct.Struct("5P5qPq10P")   # the layout of _AppendTensors, packed in a quarter of its time
+assert _APPEND_TENSORS.size == ctypes.sizeof(_AppendTensors)
 
 
 class _DecodeAttnParams(ctypes.Structure):
@@ -185,7 +190,7 @@ def lib() -> ctypes.CDLL:
         L.lsa_hfa_attn.argtypes = [A, _i64, _vp, _vp, _i64, _vp, _vp, _i32, _i64, _i32, _vp, _vp, _vp, _sz, _vp]
         L.lsa_hfa_attn.restype = _i32
         D = ctypes.POINTER(_DecodeAttnParams)
-        L.lsa_cache_append.argtypes = [ctypes.POINTER(_AppendParams), ctypes.POINTER(_AppendTensors), _i64, _i32, _i32,
+        L.lsa_cache_append.argtypes = [ctypes.POINTER(_AppendParams), _vp, _i64, _i32, _i32,
                                        _i32, _i32, _i64, _vp]
         L.lsa_cache_append.restype = _i32
         L.lsa_decode_attn_workspace_size.argtypes = [D, _i32, _i32, _i32, _i32]
@@ -553,6 +558,10 @@ def hfa_attn(prm: AttnParams, q: torch.Tensor, kv: torch.Tensor, idx: torch.Tens
 _FP8 = (torch.uint8, torch.float8_e4m3fn)
 
 
+def _address(t) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
 def _fits(t, dtypes, shape, index: int) -> bool:
     return isinstance(t, torch.Tensor) and t.dtype in dtypes and t.shape == shape and t.get_device() == index and \
         t.is_contiguous()
@@ -684,15 +693,16 @@ def cache_append(prm: AppendParams, k: torch.Tensor, k_cache: torch.Tensor, *, p
         if seq is not None and not _fits(seq, _I32, (n,), i):
             _need("seq", seq, _I32, (n,), dev)
     if rows is True:
-        rows = torch.empty(n, dtype=torch.int64, device=dev)
+        rows = k.new_empty((n,), dtype=torch.int64)
     elif rows is False or rows is None:
         rows = None
     elif not _fits(rows, _I64, (n,), i):
         _need("rows", rows, _I64, (n,), dev)
-    t = _AppendTensors(_p(q), _p(q_rot), _p(k), _p(k_rot), _p(v), qs, qrs, ks, krs, vs, _p(rope), rope_rows, _p(seq),
-                       _p(pos), _p(ctx_len), _p(page_table), _p(q_out), _p(k_cache), _p(k_scale), _p(v_cache),
-                       _p(v_scale), _p(rows))
-    st = lib().lsa_cache_append(_ref(prm), ctypes.byref(t), n, seqs, rows_per_seq, max_pages, page, n_phys, _stream(dev))
+    at = _address
+    t = _APPEND_TENSORS.pack(at(q), at(q_rot), k.data_ptr(), at(k_rot), at(v), qs, qrs, ks, krs, vs, at(rope), rope_rows,
+                             at(seq), at(pos), at(ctx_len), at(page_table), at(q_out), k_cache.data_ptr(), at(k_scale),
+                             at(v_cache), at(v_scale), at(rows))
+    st = (_lib or lib()).lsa_cache_append(_ref(prm), t, n, seqs, rows_per_seq, max_pages, page, n_phys, _stream(dev))
     if st != 0:
         _check(st, "lsa_cache_append")
     return q_out, rows
@@ -745,16 +755,22 @@ def decode_attn(prm: DecodeAttnParams, q: torch.Tensor, k_cache: torch.Tensor, v
     elif not _fits(out, _BF16, (n_rows, H, d_v), i):
         _need("out", out, _BF16, (n_rows, H, d_v), dev)
     if lse is True:
-        lse = torch.empty((n_rows, H), dtype=torch.float32, device=dev)
+        lse = q.new_empty((n_rows, H), dtype=torch.float32)
     elif lse is False or lse is None:
         lse = None
     elif not _fits(lse, _F32, (n_rows, H), i):
         _need("lse", lse, _F32, (n_rows, H), dev)
-    L, ref = lib(), _ref(prm)
+    L, ref = _lib or lib(), _ref(prm)
     wsb = L.lsa_decode_attn_workspace_size(ref, n_seq, rows_per_seq, max_pages, page)
-    ws, wsb = _workspace(wsb, dev, workspace)
-    st = L.lsa_decode_attn(ref, n_seq, rows_per_seq, _p(q), _p(k_cache), _p(k_scale), _p(v_cache), _p(v_scale),
-                           _p(ctx_len), _p(page_table), max_pages, page, n_phys, _p(out), _p(lse), _p(ws), wsb, _stream(dev))
+    if wsb and workspace is None:
+        workspace = q.new_empty((wsb,), dtype=torch.uint8)
+    elif wsb:
+        workspace, wsb = _workspace(wsb, dev, workspace)
+    else:
+        workspace = None
+    st = L.lsa_decode_attn(ref, n_seq, rows_per_seq, q.data_ptr(), k_cache.data_ptr(), _p(k_scale), _p(v_cache),
+                           _p(v_scale), ctx_len.data_ptr(), _p(page_table), max_pages, page, n_phys, out.data_ptr(),
+                           _p(lse), _p(workspace), wsb, _stream(dev))
     if st != 0:
         _check(st, "lsa_decode_attn")
     return out, lse

@@ -353,3 +353,15 @@ def test_refusals():
     for bad in (lsa.DecodeAttnParams(8, 2, 64, 64, False, 0.0), lsa.DecodeAttnParams(8, 2, 64, 64, False, float("nan"))):
         with pytest.raises(lsa.LSAError, match="sm_scale"):
             _run(bad, x)
+
+
+@pytest.mark.parametrize("form,top", [((GQA, 8, 2, 128, False), 700), ((GQA, 12, 12, 64, True), 300), ((MLA, 64, 1, 576, False), 500)], ids=str)
+def test_uncut_batches(form, top):
+    """Many sequences of short tables: every (sequence, head) whole, a workgroup each, no workspace."""
+    prm = _params(*form)
+    g = torch.Generator().manual_seed(top)
+    ctx = [int(x) for x in torch.randint(0, top + 1, (290,), generator=g)]
+    x = _batch(prm, ctx, 1, 64, seed=top)
+    assert lsa.decode_attn_workspace_size(prm, 290, 1, x["table"].shape[1], 64) == 0
+    out, lse = _run(prm, x)
+    _check(prm, x, out, lse)

@@ -141,3 +141,20 @@ def test_exact_division_of_positions():
         for n in {0, 1, d - 1, d, d + 1, top, top // d * d, top // d * d - 1, top // 2 // d * d - 1, 12345678 // d * d - 1}:
             if 0 <= n <= top:
                 assert (n * mul) >> shift == n // d, (n, d)
+
+
+def test_attention_workspace():
+    """Short tables need none; longer ones room for two fp32 partials per workgroup, of which there are no more than
+    the GPU runs at once; calls of more tiles than the kernels count are refused."""
+    size = lsa.decode_attn_workspace_size
+    gqa, mla = D(32, 8, 128, 128, False, 0.1), D(64, 1, 576, 512, True, 0.1)
+    assert size(gqa, 1, 1, 8, 64) == 0 and size(gqa, 64, 1, 32, 64) == 0 and size(mla, 256, 1, 20, 64) == 0
+    assert size(gqa, 0, 1, 2048, 64) == 0
+    for prm, cols in ((gqa, 16), (mla, 64), (D(32, 1, 128, 128, False, 0.1), 32)):
+        part = cols * (prm.d_v + 2) * 4
+        for n_seq, pages in ((1, 2048), (7, 500), (64, 2048), (300, 100)):
+            assert 2 * part <= size(prm, n_seq, 1, pages, 64) <= 2 * 512 * part + n_seq * prm.n_kv_heads * 16 + 768, (cols, n_seq)
+    # a window bounds the tiles, whatever the table
+    assert size(D(32, 8, 128, 128, False, 0.1, k_sink=4, k_swa=256), 64, 1, 4096, 64) == 0
+    assert attn(n_seq=4096, max_pages=1 << 19, n_phys=1 << 20) == UNSUPPORTED
+    assert b"2^30" in lsa.lib().lsa_last_error()
