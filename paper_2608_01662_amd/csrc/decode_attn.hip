@@ -235,6 +235,7 @@ void gqa_decode_kernel(DecodeGeom g) {
   __shared__ __attribute__((aligned(1024))) uint8_t ring[kGqaWaves][T::kRing];
   __shared__ __attribute__((aligned(16))) float scales[FP8 ? kGqaWaves : 1][FP8 ? NS : 1][64];
   __shared__ int pages[kPageSlots];
+  __shared__ uint32_t seen_bits[kGqaWaves][NS];  // of the tiles in the ring: tokens somebody attends to
   __shared__ float pm[kGqaWaves][16], pl[kGqaWaves][16];
   static_assert(16 * OS * 4 <= T::kRing, "the accumulators are merged in the ring");
   const int lane = threadIdx.x & 63, q4 = lane >> 4, i16 = lane & 15;
@@ -360,8 +361,7 @@ void gqa_decode_kernel(DecodeGeom g) {
           lds_dma16(src + (ld_slot ^ T::swz(t)) * 16, lds_addr(dst + j * 1024));
         }
       };
-      auto issue_k = [&](int i, const Where& w) {
-        const int st = i % NS;
+      auto issue_k = [&](int st, const Where& w) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage's last reads are done
         if constexpr (FP8) {
           const float* sc = lane < 32 ? g.k_scale : g.v_scale;
@@ -370,30 +370,26 @@ void gqa_decode_kernel(DecodeGeom g) {
         }
         issue(g.k, lk + st * T::kBytes, w);
       };
-      auto issue_v = [&](int i, const Where& w) {
+      auto issue_v = [&](int st, const Where& w) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        issue(g.v, lv + (i % NS) * T::kBytes, w);
+        issue(g.v, lv + st * T::kBytes, w);
       };
-      uint32_t seen_bits[NS];
-#pragma unroll
-      for (int i = 0; i < NS; ++i) {
-        seen_bits[i] = 0;
-        if (i < nw) {
-          const Where w = locate(i);
-          seen_bits[i] = w.bits;
-          issue_k(i, w);
-          issue_v(i, w);
-        }
+      // (the stages are not unrolled: eight copies of the body passed the instruction cache)
+#pragma nounroll
+      for (int i = 0; i < NS && i < nw; ++i) {
+        const Where w = locate(i);
+        seen_bits[wv][i] = w.bits;
+        issue_k(i, w);
+        issue_v(i, w);
       }
-      for (int i0 = 0; i0 < nw; i0 += NS) {
-#pragma unroll
-        for (int st = 0; st < NS; ++st) {
-          const int i = i0 + st;
-          if (i >= nw) break;
+      {
+        int st = 0;
+#pragma nounroll
+        for (int i = 0; i < nw; ++i, st = st + 1 == NS ? 0 : st + 1) {
           const bool more = i + NS < nw;  // tile i + NS takes this one's place
+          const uint32_t bits = (uint32_t)uniform((int)seen_bits[wv][st]);
           Where w{};
           if (more) w = locate(i + NS);
-          const uint32_t bits = seen_bits[st];
           // K of tile i has landed: behind it are its V and the other stages' tiles (fewer at the stretch's end)
           if (i + NS <= nw) vm_wait<T::kLoads + (NS - 1) * T::kPair>();
           else vm_wait<0>();
@@ -443,7 +439,7 @@ void gqa_decode_kernel(DecodeGeom g) {
 #pragma unroll
               for (int k = 0; k < 8; ++k) z[nb][k] = s4[k >> 2][nb][k & 3] * g.scale_log2;
           }
-          if (more) issue_k(i + NS, w);
+          if (more) issue_k(st, w);
           const int s0 = tile_pos(i);
           // several new tokens: does the tile reach to where they see different positions?
           const bool uneven = g.R > 1 && (s0 + kTile > sp.c - g.R + 1 || (g.k_swa > 0 && s0 < sp.c - g.k_swa));
@@ -532,8 +528,8 @@ void gqa_decode_kernel(DecodeGeom g) {
             }
           }
           if (more) {
-            seen_bits[st] = w.bits;
-            issue_v(i + NS, w);
+            seen_bits[wv][st] = w.bits;
+            issue_v(st, w);
           }
         }
       }
