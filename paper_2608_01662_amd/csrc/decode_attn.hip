@@ -123,8 +123,8 @@ __device__ __forceinline__ void deal(const DecodeGeom& g, int d, F&& segment) {
       continue;
     }
     const int rel = at - before * M;
-    const int r = M == 1 ? 0 : uniform((int)((uint32_t)rel / (uint32_t)sp.nt)), t0 = rel - r * sp.nt;
-    const int n = end - at < sp.nt - t0 ? end - at : sp.nt - t0;
+    const int r = M == 1 ? 0 : uniform((int)((uint32_t)rel / (uint32_t)sp.nt)), t0 = uniform(rel - r * sp.nt);
+    const int n = uniform(end - at < sp.nt - t0 ? end - at : sp.nt - t0);
     const int slot = 2 * (int)blockIdx.x + (at != start);
     segment(b, r, sp, t0, t0 + n, n == sp.nt, slot);
     if (t0 == 0 && cut && threadIdx.x == 0)  // first workgroup, last one, and the first one's partial
@@ -203,9 +203,9 @@ __device__ __forceinline__ u32x2 tr8(const uint8_t* p) {
 constexpr int kGqaWaves = 4;
 constexpr int kPageSlots = 2048;      // page-table entries staged in LDS at a time
 
-template <int D, bool FP8, int NB>
+template <int D, bool FP8, int NB, bool MULTI>
 struct GqaTile {
-  static constexpr int kPerCu = gqa_per_cu(D, NB);
+  static constexpr int kPerCu = gqa_per_cu(D, NB, MULTI);
   static constexpr int kRing = 32 * 1024 / kPerCu;        // LDS ring bytes per wave
   static constexpr int kRow = D * (FP8 ? 1 : 2);          // bytes of a cache row
   static constexpr int kBytes = kTile * kRow;             // of a K or V tile
@@ -226,18 +226,17 @@ struct GqaTile {
   }
 };
 
-template <int D, bool FP8, int NB>
-__global__ __launch_bounds__(64 * kGqaWaves) __attribute__((amdgpu_waves_per_eu(gqa_per_cu(D, NB), gqa_per_cu(D, NB))))
+template <int D, bool FP8, int NB, bool MULTI>  // MULTI: several new tokens per sequence
+__global__ __launch_bounds__(64 * kGqaWaves) __attribute__((amdgpu_waves_per_eu(gqa_per_cu(D, NB, MULTI), gqa_per_cu(D, NB, MULTI))))
 void gqa_decode_kernel(DecodeGeom g) {
-  using T = GqaTile<D, FP8, NB>;
+  using T = GqaTile<D, FP8, NB, MULTI>;
   constexpr int NS = T::kStages, KS = D / 32, CD = D / 16, COLS = 16 * NB;
-  constexpr int OS = D + 4;  // floats per column of a merged accumulator
   __shared__ __attribute__((aligned(1024))) uint8_t ring[kGqaWaves][T::kRing];
   __shared__ __attribute__((aligned(16))) float scales[FP8 ? kGqaWaves : 1][FP8 ? NS : 1][64];
   __shared__ int pages[kPageSlots];
   __shared__ uint32_t seen_bits[kGqaWaves][NS];  // of the tiles in the ring: tokens somebody attends to
-  __shared__ float pm[kGqaWaves][16], pl[kGqaWaves][16];
-  static_assert(16 * OS * 4 <= T::kRing, "the accumulators are merged in the ring");
+  __shared__ float pm[kGqaWaves][COLS], pl[kGqaWaves][COLS];
+  static_assert(COLS * D * 4 <= T::kRing, "the accumulators are merged in the ring");
   const int lane = threadIdx.x & 63, q4 = lane >> 4, i16 = lane & 15;
   const int wv = uniform((int)(threadIdx.x >> 6));
   uint8_t* const lk = ring[wv];                    // K tiles, then V tiles
@@ -256,6 +255,13 @@ void gqa_decode_kernel(DecodeGeom g) {
   // direct load j: tokens j * 64 / chunks .., lane -> token lane / chunks of them, slot lane % chunks
   constexpr int LT = 64 / T::kChunks;  // tokens per load
   const int ld_t = lane / T::kChunks, ld_slot = lane % T::kChunks;
+
+  // bits of the tokens t8 .. + 7 that a query at position t attends to
+  auto sees8 = [&](int t8, int t) -> uint32_t {
+    auto first = [](int n) { return (1u << (n < 0 ? 0 : n > 8 ? 8 : n)) - 1u; };  // the first n of them
+    const uint32_t window = g.k_swa == 0 ? 0xFFu : ~first(t - g.k_swa + 1 - t8) | first(g.k_sink - t8);
+    return first(t + 1 - t8) & window;
+  };
 
   auto segment = [&](int b, int r, const Span& sp, int t0, int t1, bool whole, int slot) {
     const int kvh = fdiv(g.by_blocks, r), col0 = (r - kvh * cb_n) * COLS;
@@ -386,7 +392,7 @@ void gqa_decode_kernel(DecodeGeom g) {
         int st = 0;
 #pragma nounroll
         for (int i = 0; i < nw; ++i, st = st + 1 == NS ? 0 : st + 1) {
-          const bool more = i + NS < nw;  // tile i + NS takes this one's place
+          const bool more = uniform(i + NS < nw);  // tile i + NS takes this one's place
           const uint32_t bits = (uint32_t)uniform((int)seen_bits[wv][st]);
           Where w{};
           if (more) w = locate(i + NS);
@@ -442,17 +448,14 @@ void gqa_decode_kernel(DecodeGeom g) {
           if (more) issue_k(st, w);
           const int s0 = tile_pos(i);
           // several new tokens: does the tile reach to where they see different positions?
-          const bool uneven = g.R > 1 && (s0 + kTile > sp.c - g.R + 1 || (g.k_swa > 0 && s0 < sp.c - g.k_swa));
-          if (bits != 0xFFFFFFFFu || uneven) {
+          const bool uneven = MULTI && uniform((s0 + kTile > sp.c - g.R + 1 || (g.k_swa > 0 && s0 < sp.c - g.k_swa)));
+          if (bits != ~0u || uneven) {
+            const int t8 = s0 + 8 * q4;  // this lane's first token
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const int s = s0 + 8 * q4 + k;
-              const bool live = (bits >> (8 * q4 + k)) & 1u;
+            for (int nb = 0; nb < NB; ++nb) {
+              const uint32_t own = (bits >> (8 * q4)) & (uneven ? sees8(t8, tcol[nb]) : 0xFFu);
 #pragma unroll
-              for (int nb = 0; nb < NB; ++nb) {
-                const bool own = !uneven || (s <= tcol[nb] && (g.k_swa == 0 || tcol[nb] - s < g.k_swa || s < g.k_sink));
-                z[nb][k] = live && own ? z[nb][k] : -INFINITY;
-              }
+              for (int k = 0; k < 8; ++k) z[nb][k] = (own >> k) & 1u ? z[nb][k] : -INFINITY;
             }
           }
           // ---- online softmax; the reference maximum moves when it grows by more than 2^8
@@ -496,7 +499,18 @@ void gqa_decode_kernel(DecodeGeom g) {
                                vt + v_t1 * T::kRow + (ch ^ T::swz(v_t1)) * 16 + half);
             }
           };
-          if (!uneven) {
+          bool apart = false;
+          if (uneven) {  // (adding 1 to an exponent of ones carries into the sign bit)
+            uint32_t odd = 0;
+#pragma nounroll
+            for (int c = 0; c < CD; ++c) {  // (unrolled, its operands would be held together and spill)
+              const u32x4 a = value(c);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) odd |= (a[k] & 0x7F807F80u) + 0x00800080u;
+            }
+            apart = uniform(__ballot((odd & 0x80008000u) != 0) != 0);
+          }
+          if (!apart) {
 #pragma unroll
             for (int c = 0; c < CD; ++c) {
               const u32x4 a = value(c);
@@ -504,17 +518,14 @@ void gqa_decode_kernel(DecodeGeom g) {
               for (int nb = 0; nb < NB; ++nb) o[nb][c] = mfma16(a, pb[nb], o[nb][c]);
             }
           } else {
-            // a token's row of V reaches only the columns that see it, also if it holds a NaN: one product per new
-            // token, its unseen rows of V zeroed, taken by its own columns
+            // A weight of zero does not silence a NaN or an infinity in a row of V that some of the columns see: one product
+            // per new token, its unseen rows of V zeroed, taken by its own columns.
             for (int j = fdiv(g.by_group, col0); j <= fdiv(g.by_group, col0 + ncols - 1); ++j) {
               const int t = sp.c - g.R + j;
+              const uint32_t own = sees8(s0 + 8 * q4, t);
               u32x4 keep;
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const int s = s0 + 8 * q4 + 2 * k;
-                auto sees = [&](int x) { return x <= t && (g.k_swa == 0 || t - x < g.k_swa || x < g.k_sink); };
-                keep[k] = (sees(s) ? 0xFFFFu : 0u) | (sees(s + 1) ? 0xFFFF0000u : 0u);
-              }
+              for (int k = 0; k < 4; ++k) keep[k] = ((own >> (2 * k)) & 1u ? 0xFFFFu : 0u) | ((own >> (2 * k + 1)) & 1u ? 0xFFFF0000u : 0u);
 #pragma unroll
               for (int c = 0; c < CD; ++c) {
                 const u32x4 a = value(c) & keep;
@@ -522,7 +533,7 @@ void gqa_decode_kernel(DecodeGeom g) {
                 for (int nb = 0; nb < NB; ++nb) {
                   const f32x4 x = mfma16(a, pb[nb], f32x4{});
 #pragma unroll
-                  for (int k = 0; k < 4; ++k) o[nb][c][k] += tcol[nb] == t ? x[k] : 0.f;
+                  for (int k = 0; k < 4; ++k) o[nb][c][k] = tcol[nb] == t ? o[nb][c][k] + x[k] : o[nb][c][k];
                 }
               }
             }
@@ -535,52 +546,51 @@ void gqa_decode_kernel(DecodeGeom g) {
       }
       __syncthreads();  // every wave is done with `pages` and its ring
     }
-    // ---- the waves' results, 16 columns at a time: weighted by 2^(m_w - M) and summed. (The lane is made
-    // opaque, or these offsets are computed before the loop over stretches and spill.)
+    // ---- the waves' results, weighted by 2^(m_w - M) and summed. Column and dims 4 u .. lie in 16-byte slot u ^ column of the
+    // column's row, so that 16 lanes of one u fall on all banks. (The lane is made opaque, or these offsets are computed
+    // before the loop over stretches and spill.)
     int el = lane;
     asm volatile("" : "+v"(el));
     const int e16 = el & 15, e4 = el >> 4;
+    constexpr int U = D / 4;
+    f32x4* const po = reinterpret_cast<f32x4*>(ring[wv]);
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      if (16 * nb >= ncols) break;
-      float* po = reinterpret_cast<float*>(ring[wv]);
 #pragma unroll
-      for (int c = 0; c < CD; ++c) *reinterpret_cast<f32x4*>(po + e16 * OS + 16 * c + 4 * e4) = o[nb][c];
+      for (int c = 0; c < CD; ++c) po[(16 * nb + e16) * U + ((4 * c + e4) ^ e16)] = o[nb][c];
       const float lt = sum4_xor16_32(l[nb]);
       if (e4 == 0) {
-        pm[wv][e16] = m[nb];
-        pl[wv][e16] = lt;
+        pm[wv][16 * nb + e16] = m[nb];
+        pl[wv][16 * nb + e16] = lt;
       }
-      __syncthreads();
-      for (int u = 64 * wv + el; u < 16 * (D / 4); u += 64 * kGqaWaves) {
-        const int col = u / (D / 4), d = 4 * (u % (D / 4));
-        if (16 * nb + col >= ncols) break;
-        float mx = pm[0][col];
-#pragma unroll
-        for (int x = 1; x < kGqaWaves; ++x) mx = fmaxf(mx, pm[x][col]);
-        float sum = 0.f;
-        f32x4 acc = {};
-#pragma unroll
-        for (int x = 0; x < kGqaWaves; ++x) {
-          const float w = fast_exp2(pm[x][col] - mx);
-          sum += pl[x][col] * w;
-          acc += w * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(ring[x]) + col * OS + d);
-        }
-        const int at = col0 + 16 * nb + col;
-        if (whole) {
-          const int j = fdiv(g.by_group, at);
-          const int64_t row = ((int64_t)b * g.R + j) * g.H + kvh * group + at - j * group;
-          const float inv = sum == 0.f ? 0.f : 1.f / sum;
-          *reinterpret_cast<u32x2*>(g.out + row * D + d) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
-          if (g.lse && d == 0) g.lse[row] = sum == 0.f ? -INFINITY : (mx + __log2f(sum)) * kLn2;
-        } else {
-          const int64_t pc = (int64_t)slot * COLS + 16 * nb + col;
-          *reinterpret_cast<f32x4*>(g.part_o + pc * D + d) = acc;
-          if (d == 0) *reinterpret_cast<f32x2*>(g.part_ml + 2 * pc) = f32x2{mx, sum};
-        }
-      }
-      __syncthreads();
     }
+    __syncthreads();
+    for (int x = 64 * wv + el; x < ncols * U; x += 64 * kGqaWaves) {
+      const int col = x / U, u = x % U, d = 4 * u;
+      float mx = pm[0][col];
+#pragma unroll
+      for (int w = 1; w < kGqaWaves; ++w) mx = fmaxf(mx, pm[w][col]);
+      float sum = 0.f;
+      f32x4 acc = {};
+#pragma unroll
+      for (int w = 0; w < kGqaWaves; ++w) {
+        const float f = fast_exp2(pm[w][col] - mx);
+        sum += pl[w][col] * f;
+        acc += f * reinterpret_cast<const f32x4*>(ring[w])[col * U + (u ^ (col & 15))];
+      }
+      if (whole) {
+        const int at = col0 + col, j = fdiv(g.by_group, at);
+        const int64_t row = ((int64_t)b * g.R + j) * g.H + kvh * group + at - j * group;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        *reinterpret_cast<u32x2*>(g.out + row * D + d) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+        if (g.lse && d == 0) g.lse[row] = sum == 0.f ? -INFINITY : (mx + __log2f(sum)) * kLn2;
+      } else {
+        const int64_t pc = (int64_t)slot * COLS + col;
+        *reinterpret_cast<f32x4*>(g.part_o + pc * D + d) = acc;
+        if (d == 0) *reinterpret_cast<f32x2*>(g.part_ml + 2 * pc) = f32x2{mx, sum};
+      }
+    }
+    __syncthreads();
   };
 
   deal(g, D, segment);
@@ -1047,7 +1057,8 @@ __global__ __launch_bounds__(S * T) void latent_join_kernel(DecodeGeom g) {
 constexpr int64_t kJoinFew = 2048;  // workgroups
 template <int D, bool FP8, int NB>
 static hipError_t launch_gqa(const DecodeGeom& g, hipStream_t st) {
-  hipLaunchKernelGGL((gqa_decode_kernel<D, FP8, NB>), dim3((unsigned)g.grid), dim3(64 * kGqaWaves), 0, st, g);
+  const auto kernel = g.R > 1 ? gqa_decode_kernel<D, FP8, NB, true> : gqa_decode_kernel<D, FP8, NB, false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)g.grid), dim3(64 * kGqaWaves), 0, st, g);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.part_o == nullptr) return e;
   const int64_t rows = (int64_t)g.n_seq * g.R * g.H;

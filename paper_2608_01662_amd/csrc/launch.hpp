@@ -173,7 +173,7 @@ __host__ __device__ inline int least_tiles(int64_t total, int step) {
   return t < step ? step : step == 4 ? t & -4 : t;
 }
 // Workgroups of the grouped-head kernel per CU: two where the registers of NB blocks of 16 query rows allow it.
-constexpr int gqa_per_cu(int d, int nb) { return nb * d <= 256 ? 2 : 1; }
+constexpr int gqa_per_cu(int d, int nb, bool multi) { return nb <= 2 || (d == 64 && !multi) ? 2 : 1; }
 hipError_t launch_decode_attn(const DecodeGeom& g, hipStream_t st);
 
 }  // namespace lsa

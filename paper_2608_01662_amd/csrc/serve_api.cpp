@@ -117,7 +117,7 @@ DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t r
   pl.all_tiles = pairs * tiles;
   pl.pairs = pairs;
   const int64_t some = cdiv(pl.all_tiles, lsa::least_tiles(pl.all_tiles, pl.min_tiles)), most = some > pairs ? some : pairs;
-  const int64_t wgs = kCus * (latent ? 1 : lsa::gqa_per_cu(p->d_qk, pl.block_cols / 16));
+  const int64_t wgs = kCus * (latent ? 1 : lsa::gqa_per_cu(p->d_qk, pl.block_cols / 16, rows_per_seq > 1));
   pl.grid = (int)(most < wgs ? most : wgs);
   pl.cut = tiles > whole_tiles(latent, pairs);
   if (!pl.cut) pl.grid = (int)pairs;
