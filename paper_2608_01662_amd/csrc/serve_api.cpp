@@ -84,17 +84,24 @@ constexpr int kTile = 32;          // positions of a tile
 constexpr int kPageSlots = 2048;   // page-table entries a workgroup stages at a time
 constexpr int kLatentPages = 1024; // the same, latent cache
 
-// A (sequence, head) of at most that many tiles is left whole: a workgroup each, no scan of the lengths, no partials and
-// no join. What the host knows is the tables' capacity, so the bound also limits what one long sequence among short
-// ones can cost. us of whole calls, cut / whole, sequences x positions:
-//   32 heads on 8 key heads (about 0.3 us a tile in a workgroup of its own; 128 pairs come near the memory's rate):
-//     1 x 128 7.6 / 5.6, 1 x 500 9.6 / 9.5, 1 x 1001 9.6 / 13.6, 4 x 500 10.3 / 9.6, 4 x 1001 11.6 / 14.8, 16 x 500 15.2 / 11.2,
-//     16 x 2000 34.6 / 30.4, 64 x 1000 53.8 / 51.2, 256 x 1000 196 / 187; a window of 1024 on 33 x 12 heads 27.6 / 22.7
-//   latent, 64 heads (0.95 us a tile): 1 x 128 13.3 / 11.1, 1 x 512 14.8 / 22.1, 16 x 500 25.5 / 22.9, 64 x 500 27.3 / 23.9,
-//     64 x 1000 33.1 / 38.6, 256 x 1000 74.4 / 68.2
-int64_t whole_tiles(bool latent, int64_t pairs) {
-  if (latent) return pairs >= 256 ? 40 : 5 + pairs * 2 / 3 < 20 ? 5 + pairs * 2 / 3 : 20;
-  return pairs >= 128 ? 64 : 16;
+// A (sequence, head, query row block) of at most that many tiles is left whole: a workgroup each, no scan of the lengths, no
+// partials and no join. What the host knows is the tables' capacity, so the bound also limits what one long sequence
+// among short ones can cost. us of whole calls, cut / whole, sequences x positions:
+//   32 heads on 8 key heads (about 0.3 us a tile in a workgroup of its own; 100 of them come near the memory's rate):
+//     1 x 128 7.6 / 5.6, 1 x 1001 9.6 / 13.6, 4 x 500 9.4 / 8.5, 4 x 1001 11.6 / 14.8, 8 x 1000 13.8 / 14.0, 8 x 2000 20.0 / 22.5,
+//     12 x 2000 29.0 / 25.9, 16 x 2000 35.6 / 30.7, 64 x 1000 53.8 / 51.2, 256 x 1000 196 / 187; a window of 1024 on 33 x 12
+//     heads 27.6 / 22.7
+//   64 query rows of a key head: 1 x 500 13.6 / 16.2, 32 x 500 16.8 / 16.7, 32 x 1000 19.8 / 24.0, 69 x 1200 32.7 / 27.8, 69 x 2000
+//     35.7 / 38.1, 150 x 2000 56.9 / 47.4
+//   latent, 64 heads (0.95 us a tile): 1 x 200 12.5 / 13.7, 4 x 300 13.7 / 16.6, 8 x 300 17.0 / 16.6, 16 x 500 25.2 / 22.4, 28 x 700
+//     25.4 / 28.3, 64 x 700 32.1 / 29.0, 64 x 1000 33.1 / 38.6, 128 x 1300 66 / 56, 300 x 1300 139 / 127
+int64_t whole_tiles(const lsa_decode_attn_params* p, int block_cols, int64_t pairs) {
+  if (p->latent) {
+    const int64_t t = pairs <= 16 ? 4 + pairs * 3 / 4 : 12 + pairs / 4;
+    return t < 48 ? t : 48;
+  }
+  const int64_t t = pairs * 3 / 4, least = block_cols == 64 ? 8 : 16;
+  return t < least ? least : t < 64 ? t : 64;
 }
 
 DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq, int32_t max_pages,
@@ -119,7 +126,7 @@ DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t r
   const int64_t some = cdiv(pl.all_tiles, lsa::least_tiles(pl.all_tiles, pl.min_tiles)), most = some > pairs ? some : pairs;
   const int64_t wgs = kCus * (latent ? 1 : lsa::gqa_per_cu(p->d_qk, pl.block_cols / 16, rows_per_seq > 1));
   pl.grid = (int)(most < wgs ? most : wgs);
-  pl.cut = tiles > whole_tiles(latent, pairs);
+  pl.cut = tiles > whole_tiles(p, pl.block_cols, pairs);
   if (!pl.cut) pl.grid = (int)pairs;
   // pages of a pass: tiles * 32 / P, and two more at the ends of each of two parts
   const int64_t pass = (int64_t)((latent ? kLatentPages : kPageSlots) - 4) * kv_page_size / kTile;
