@@ -63,11 +63,12 @@ __device__ __forceinline__ void empty_rows(const DecodeGeom& g, int b, int d) {
     for (int i = (int)threadIdx.x; i < g.R * g.H; i += (int)blockDim.x) g.lse[(int64_t)b * g.R * g.H + i] = -INFINITY;
 }
 
-// Deals this workgroup its stretch of the tiles of all sequences, g.M (head, query row block)s each, one
-// (sequence, head) after the other: an equal share of all, but no fewer tiles than pay for a workgroup. Calls
-// segment(sequence, r in [0, g.M), span, first tile, last tile + 1, whole, slot of the partial), and tells the
-// join about every (sequence, head) whose first tile is here. Then the rows of sequences without a tile, dealt
-// to the workgroups. d: width of an output row. (Tiles of all in all fit 30 bits: the host refuses more.)
+// Deals this workgroup its work. The tiles of all sequences (of one head) stand in one line, and workgroup (y, r) takes
+// stretch y of it, an equal share of all, but no fewer tiles than pay for a workgroup, for r, one of the g.M (head, query row
+// block)s of every sequence; the g.M of a stretch are neighbours in the launch, so that what they share is read at one time. Calls
+// segment(sequence, r, span, first tile, last tile + 1, whole, slot of the partial), and tells the join about every
+// (sequence, r) whose first tile is here. Then the rows of sequences without a tile, dealt to the workgroups. d: width of an output
+// row. (Tiles of all in all fit 30 bits: the host refuses more.)
 //
 // What precedes the first load of a row is a chain of round trips, so the first 64 lengths are loaded once and
 // scanned in registers, and divisions by what the host knows are products.
@@ -75,33 +76,33 @@ template <class F>
 __device__ __forceinline__ void deal(const DecodeGeom& g, int d, F&& segment) {
   const int M = g.M, lane = threadIdx.x & 63;
   const bool cut = g.parts != nullptr;
+  // (together: workgroups i, i + 8, .. run on one XCD, whose L2 then reads the rows that the g.M share once)
+  const int q = g.together ? (int)blockIdx.x >> 3 : (int)blockIdx.x, yq = fdiv(g.by_m, q), r = q - yq * M;
+  const int y = g.together ? 8 * yq + ((int)blockIdx.x & 7) : yq;
   auto length = [&](int b) { return b < g.n_seq ? g.ctx_len[b] : 0; };
   int ctx0 = 0, share = 0;
-  int at = 0, end = 0, b = 0, before = 0;  // tiles [at, end), the sequence of `at`, tiles (of one head) before that sequence
-  if (!cut) {  // a workgroup per (sequence, head); `before` counts from its own sequence
-    b = fdiv(g.by_m, (int)blockIdx.x);
+  int at = 0, end = 0, b = 0, before = 0;  // tiles [at, end), the sequence of `at`, the tiles before that sequence
+  if (!cut) {  // a workgroup per (sequence, r); `before` counts from its own sequence
+    b = y;
     ctx0 = uniform(g.ctx_len[b]);
-    const int nt = span_of(g, ctx0).nt;
-    at = ((int)blockIdx.x - b * M) * nt;
-    end = at + nt;
+    end = span_of(g, ctx0).nt;
   } else {
     ctx0 = length(lane);
     const int inc0 = wave_scan(span_of(g, ctx0).nt);
     int total = __builtin_amdgcn_readlane(inc0, 63);
     for (int b0 = 64; b0 < g.n_seq; b0 += 64) total += __builtin_amdgcn_readlane(wave_scan(span_of(g, length(b0 + lane)).nt), 63);
-    total *= M;
-    share = fdiv(g.by_grid, total + g.grid - 1);
-    int least = least_tiles(total, g.min_tiles);
-    // (where workgroups are idle, one of fewer tiles rather than one for several short (sequence, head)s)
-    const int mean = fdiv(g.by_pairs, total + (int)g.by_pairs.d - 1);
+    share = fdiv(g.by_stretches, total + (int)g.by_stretches.d - 1);
+    int least = least_tiles(total * M, g.min_tiles);
+    // (where workgroups are idle, one of fewer tiles rather than one for several short sequences)
+    const int mean = fdiv(g.by_seqs, total + g.n_seq - 1);
     least = mean < least ? mean : least;
     share = share < least ? least : share;
-    const int64_t first = (int64_t)blockIdx.x * share;
+    const int64_t first = (int64_t)y * share;
     if (first < total) {
       at = (int)first;
       end = total - at < share ? total : at + share;
       for (int inc = inc0, ctx = ctx0;;) {
-        const uint64_t past = __ballot((before + inc) * M > at);
+        const uint64_t past = __ballot(before + inc > at);
         if (past) {
           const int i = __ffsll((unsigned long long)past) - 1;
           before += __builtin_amdgcn_readlane(inc, i) - span_of(g, __builtin_amdgcn_readlane(ctx, i)).nt;
@@ -122,22 +123,20 @@ __device__ __forceinline__ void deal(const DecodeGeom& g, int d, F&& segment) {
       ++b;
       continue;
     }
-    const int rel = at - before * M;
-    const int r = M == 1 ? 0 : uniform((int)((uint32_t)rel / (uint32_t)sp.nt)), t0 = uniform(rel - r * sp.nt);
-    const int n = uniform(end - at < sp.nt - t0 ? end - at : sp.nt - t0);
-    const int slot = 2 * (int)blockIdx.x + (at != start);
+    const int t0 = uniform(at - before), n = uniform(end - at < sp.nt - t0 ? end - at : sp.nt - t0);
+    const int slot = 2 * (y * M + r) + (at != start);
     segment(b, r, sp, t0, t0 + n, n == sp.nt, slot);
-    if (t0 == 0 && cut && threadIdx.x == 0)  // first workgroup, last one, and the first one's partial
-      g.parts[(int64_t)b * M + r] = int4{(int)blockIdx.x, (int)((uint32_t)(at + sp.nt - 1) / (uint32_t)share), slot, 0};
+    if (t0 == 0 && cut && threadIdx.x == 0)  // first stretch and last one, and the first one's partial
+      g.parts[(int64_t)b * M + r] = int4{y, (int)((uint32_t)(at + sp.nt - 1) / (uint32_t)share), slot, r};
     at += n;
-    if (r == M - 1 && t0 + n == sp.nt) {
+    if (t0 + n == sp.nt) {
       before += sp.nt;
       ++b;
     }
   }
   // sequences without a tile
   if (!cut) {
-    if (end == 0 && (int)blockIdx.x == b * M) empty_rows(g, b, d);
+    if (end == 0 && r == 0) empty_rows(g, b, d);
     return;
   }
   for (int e = blockIdx.x; e < g.n_seq; e += g.grid) {
@@ -947,11 +946,11 @@ struct Joined {
   float m, l;
   f32x4 acc;
 };
-// partial v of the parts p: slot of the first workgroup's, then the first slot of each following one
-__device__ __forceinline__ int part_slot(const int4& p, int v) { return v == 0 ? p.z : 2 * (p.x + v); }
+// partial v of the parts p: slot of the first workgroup's, then the first slot of each following stretch's
+__device__ __forceinline__ int part_slot(const int4& p, int v, int M) { return v == 0 ? p.z : 2 * ((p.x + v) * M + p.w); }
 
 template <int S, int U, class ML, class O>  // U partials requested together
-__device__ __forceinline__ Joined join_parts(const int4& p, int sub, ML&& load_ml, O&& load_o) {
+__device__ __forceinline__ Joined join_parts(const int4& p, int M, int sub, ML&& load_ml, O&& load_o) {
   const int n = p.y - p.x + 1;
   Joined r{kNoRef, 0.f, f32x4{}};
   for (int v = sub; v < n; v += S * U) {
@@ -959,7 +958,7 @@ __device__ __forceinline__ Joined join_parts(const int4& p, int sub, ML&& load_m
     f32x4 x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int slot = part_slot(p, v + u * S < n ? v + u * S : v);
+      const int slot = part_slot(p, v + u * S < n ? v + u * S : v, M);
       ml[u] = load_ml(slot);
       x[u] = load_o(slot);
     }
@@ -1024,7 +1023,7 @@ __global__ __launch_bounds__(S * T) void gqa_join_kernel(DecodeGeom g) {
   const int4 p = g.parts[(int64_t)unit * cb_n + col / COLS];
   if (p.x == p.y) return;
   const int d = 4 * (T * (int)blockIdx.y + (int)threadIdx.x % T), cc = col % COLS;
-  Joined r = join_parts<S, 4>(p, threadIdx.x / T, [&](int slot) { return *reinterpret_cast<const f32x2*>(g.part_ml + 2 * ((int64_t)slot * COLS + cc)); },
+  Joined r = join_parts<S, 4>(p, g.M, threadIdx.x / T, [&](int slot) { return *reinterpret_cast<const f32x2*>(g.part_ml + 2 * ((int64_t)slot * COLS + cc)); },
                               [&](int slot) { return *reinterpret_cast<const f32x4*>(g.part_o + ((int64_t)slot * COLS + cc) * D + d); });
   r = join_threads<S, T>(r, lds);
   if ((int)threadIdx.x >= T) return;
@@ -1043,7 +1042,7 @@ __global__ __launch_bounds__(S * T) void latent_join_kernel(DecodeGeom g) {
   const int vec = T * (int)blockIdx.y + (int)threadIdx.x % T;
   const int lane = vec & 63, q = (vec >> 6) & 3, c = (vec >> 8) & 3, hb = (vec >> 10) & 1, w4 = vec >> 11;
   const int lh = 32 * hb + (lane & 31), d = 128 * w4 + 32 * c + 8 * q + 4 * (lane >> 5);
-  Joined r = join_parts<S, (S > 1 ? 8 : 4)>(p, threadIdx.x / T, [&](int slot) { return *reinterpret_cast<const f32x2*>(g.part_ml + 2 * ((int64_t)slot * 64 + lh)); },
+  Joined r = join_parts<S, (S > 1 ? 8 : 4)>(p, g.M, threadIdx.x / T, [&](int slot) { return *reinterpret_cast<const f32x2*>(g.part_ml + 2 * ((int64_t)slot * 64 + lh)); },
                            [&](int slot) { return reinterpret_cast<const f32x4*>(g.part_o)[(int64_t)slot * 8192 + vec]; });
   r = join_threads<S, T>(r, lds);
   if (threadIdx.x >= T) return;
@@ -1064,7 +1063,7 @@ static hipError_t launch_gqa(const DecodeGeom& g, hipStream_t st) {
   const int64_t rows = (int64_t)g.n_seq * g.R * g.H;
   if (rows * (D / 32) <= kJoinFew) {
     // (at most that many partials of a row, if the sequences are alike)
-    if (g.grid / (int)g.by_pairs.d > 32) hipLaunchKernelGGL((gqa_join_kernel<D, 16 * NB, 128, 8>), dim3((unsigned)rows, D / 32), dim3(1024), 0, st, g);
+    if ((int)g.by_stretches.d / g.n_seq > 32) hipLaunchKernelGGL((gqa_join_kernel<D, 16 * NB, 128, 8>), dim3((unsigned)rows, D / 32), dim3(1024), 0, st, g);
     else hipLaunchKernelGGL((gqa_join_kernel<D, 16 * NB, 32, 8>), dim3((unsigned)rows, D / 32), dim3(256), 0, st, g);
   } else {
     hipLaunchKernelGGL((gqa_join_kernel<D, 16 * NB, 1024 / D, D / 4>), dim3((unsigned)rows), dim3(256), 0, st, g);

@@ -158,11 +158,12 @@ struct DecodeGeom {
   int M;              // such blocks of a sequence
   FastDiv by_m;       // by M
   int grid;           // workgroups
-  FastDiv by_grid;    // division by it
-  FastDiv by_pairs;   // by the (sequence, head, query row block)s
+  FastDiv by_stretches;  // division by the stretches the tiles are dealt in (grid = stretches * M)
+  FastDiv by_seqs;    // by n_seq
+  int together;       // the M workgroups of a stretch on one XCD (stretches are a multiple of 8)
   int min_tiles;      // fewest tiles of a workgroup (see least_tiles)
   float *part_o, *part_ml;  // two partials per workgroup: [block_cols, d_v], [block_cols, 2]; nullptr: none is cut
-  int4* parts;        // [n_seq, M]: first and last workgroup of each (sequence, head), slot of the first one's partial
+  int4* parts;        // [n_seq, M]: first and last stretch of each, slot of the first one's partial, r
 };
 // Tiles that pay for a workgroup in a call of `total` tiles: n workgroups take total / n tiles each and leave n partials
 // to be written and joined, and the sum of both is least at n ~ sqrt(total). In steps of `step` (grouped heads: four

@@ -74,9 +74,10 @@ lsa_status check_decode_sizes(const lsa_decode_attn_params* p, int32_t n_seq, in
 
 // How a call is dealt out (decode_attn.hip): `grid` workgroups take equal stretches of all tiles.
 struct DecodePlan {
-  int grid, min_tiles, block_cols, blocks, M, pass_tiles;  // (see DecodeGeom)
+  int grid, stretches, min_tiles, block_cols, blocks, M, pass_tiles;  // (see DecodeGeom)
   bool cut;  // may a stretch end inside a (sequence, head)?
-  int64_t pairs, all_tiles;  // (sequence, head, query row block)s; their tiles at most
+  int64_t all_tiles;  // at most
+  bool together;
   size_t off_ml, off_parts, total;
 };
 constexpr int64_t kCus = 256;
@@ -122,12 +123,14 @@ DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t r
   }
   pl.min_tiles = latent ? 2 : 4;  // (grouped heads: one per wave)
   pl.all_tiles = pairs * tiles;
-  pl.pairs = pairs;
   const int64_t some = cdiv(pl.all_tiles, lsa::least_tiles(pl.all_tiles, pl.min_tiles)), most = some > pairs ? some : pairs;
   const int64_t wgs = kCus * (latent ? 1 : lsa::gqa_per_cu(p->d_qk, pl.block_cols / 16, rows_per_seq > 1));
-  pl.grid = (int)(most < wgs ? most : wgs);
+  const int64_t n = (most < wgs ? most : wgs) / pl.M;
+  pl.stretches = (int)(n > 1 ? n : 1);
+  pl.together = (latent ? pl.M : pl.blocks) > 1 && pl.stretches >= 8;
+  if (pl.together) pl.stretches &= -8;
   pl.cut = tiles > whole_tiles(p, pl.block_cols, pairs);
-  if (!pl.cut) pl.grid = (int)pairs;
+  pl.grid = (int)(pl.cut ? (int64_t)pl.stretches * pl.M : pairs);
   // pages of a pass: tiles * 32 / P, and two more at the ends of each of two parts
   const int64_t pass = (int64_t)((latent ? kLatentPages : kPageSlots) - 4) * kv_page_size / kTile;
   pl.pass_tiles = (int)(pass < (1 << 26) ? pass : (1 << 26));
@@ -305,8 +308,9 @@ lsa_status lsa_decode_attn(const lsa_decode_attn_params* p, int32_t n_seq, int32
   g.M = pl.M;
   g.by_m = lsa::fast_div((uint32_t)pl.M);
   g.grid = pl.grid;
-  g.by_grid = lsa::fast_div((uint32_t)pl.grid);
-  g.by_pairs = lsa::fast_div((uint32_t)pl.pairs);
+  g.by_stretches = lsa::fast_div((uint32_t)pl.stretches);
+  g.together = pl.cut && pl.together;
+  g.by_seqs = lsa::fast_div((uint32_t)n_seq);
   g.min_tiles = pl.min_tiles;
   if (pl.cut) {
     g.part_o = static_cast<float*>(workspace);
