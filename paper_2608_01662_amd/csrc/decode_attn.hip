@@ -199,13 +199,12 @@ __device__ __forceinline__ u32x2 tr8(const uint8_t* p) {
 // blocks per wave); S^T = K Q^T on 16x16x32 products with tokens on the rows, in an order that gives lane
 // (g = lane / 16) the scores of tokens 8 g .. + 7 of its column, which is the layout of the B operand of
 // O^T += V^T P^T: P never leaves the registers.
-constexpr int kGqaWaves = 4;
 constexpr int kPageSlots = 2048;      // page-table entries staged in LDS at a time
 
-template <int D, bool FP8, int NB, bool MULTI>
+template <int D, bool FP8, int NB, bool MULTI, int W>
 struct GqaTile {
-  static constexpr int kPerCu = gqa_per_cu(D, NB, MULTI);
-  static constexpr int kRing = 32 * 1024 / kPerCu;        // LDS ring bytes per wave
+  static constexpr int kPerCu = gqa_per_cu(D, NB, MULTI, W);
+  static constexpr int kRing = 128 * 1024 / (kPerCu * W);  // LDS ring bytes per wave
   static constexpr int kRow = D * (FP8 ? 1 : 2);          // bytes of a cache row
   static constexpr int kBytes = kTile * kRow;             // of a K or V tile
   static constexpr int kChunks = kRow / 16;               // 16-byte chunks of a row
@@ -225,16 +224,16 @@ struct GqaTile {
   }
 };
 
-template <int D, bool FP8, int NB, bool MULTI>  // MULTI: several new tokens per sequence
-__global__ __launch_bounds__(64 * kGqaWaves) __attribute__((amdgpu_waves_per_eu(gqa_per_cu(D, NB, MULTI), gqa_per_cu(D, NB, MULTI))))
+template <int D, bool FP8, int NB, bool MULTI, int W>  // MULTI: several new tokens per sequence; W waves
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(gqa_waves_per_simd(D, NB, MULTI), gqa_waves_per_simd(D, NB, MULTI))))
 void gqa_decode_kernel(DecodeGeom g) {
-  using T = GqaTile<D, FP8, NB, MULTI>;
+  using T = GqaTile<D, FP8, NB, MULTI, W>;
   constexpr int NS = T::kStages, KS = D / 32, CD = D / 16, COLS = 16 * NB;
-  __shared__ __attribute__((aligned(1024))) uint8_t ring[kGqaWaves][T::kRing];
-  __shared__ __attribute__((aligned(16))) float scales[FP8 ? kGqaWaves : 1][FP8 ? NS : 1][64];
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[W][T::kRing];
+  __shared__ __attribute__((aligned(16))) float scales[FP8 ? W : 1][FP8 ? NS : 1][64];
   __shared__ int pages[kPageSlots];
-  __shared__ uint32_t seen_bits[kGqaWaves][NS];  // of the tiles in the ring: tokens somebody attends to
-  __shared__ float pm[kGqaWaves][COLS], pl[kGqaWaves][COLS];
+  __shared__ uint32_t seen_bits[W][NS];  // of the tiles in the ring: tokens somebody attends to
+  __shared__ float pm[W][COLS], pl[W][COLS];
   static_assert(COLS * D * 4 <= T::kRing, "the accumulators are merged in the ring");
   const int lane = threadIdx.x & 63, q4 = lane >> 4, i16 = lane & 15;
   const int wv = uniform((int)(threadIdx.x >> 6));
@@ -307,7 +306,7 @@ void gqa_decode_kernel(DecodeGeom g) {
         const int64_t end = (int64_t)(p1 + sp.skip) * kTile - 1;
         n2 = fdiv(g.by_page, end < sp.c ? (int)end : sp.c - 1) - f2 + 1;
       }
-      for (int i = (int)threadIdx.x; i < n1 + n2; i += 64 * kGqaWaves) {
+      for (int i = (int)threadIdx.x; i < n1 + n2; i += 64 * W) {
         const int pg = i < n1 ? f1 + i : f2 + i - n1;
         const int ph = g.page_table ? g.page_table[(int64_t)b * g.max_pages + pg] : b;
         pages[i] = ph >= 0 && ph < g.n_phys ? ph : -1;
@@ -316,9 +315,9 @@ void gqa_decode_kernel(DecodeGeom g) {
       // not know of those, would wait for all of them together with Q
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
-      const int nw = p1 - p0 > wv ? (p1 - p0 - wv + kGqaWaves - 1) / kGqaWaves : 0;  // this wave's tiles
+      const int nw = p1 - p0 > wv ? (p1 - p0 - wv + W - 1) / W : 0;  // this wave's tiles
       auto tile_pos = [&](int i) {
-        const int t = p0 + wv + kGqaWaves * i;
+        const int t = p0 + wv + W * i;
         return (t < sp.ns ? t : t + sp.skip) * kTile;
       };
       // Where this wave's tile i lies: the cache row of token lane % 32, -1 where nobody attends to it (bits: the tokens
@@ -329,7 +328,7 @@ void gqa_decode_kernel(DecodeGeom g) {
       };
       auto locate = [&](int i) {
         Where w{-1, 0u, 0u};
-        const int t = p0 + wv + kGqaWaves * i, s0 = tile_pos(i), s = s0 + (lane & 31);
+        const int t = p0 + wv + W * i, s0 = tile_pos(i), s = s0 + (lane & 31);
         const bool seen = s < sp.c && (s >= sp.lo || s < g.k_sink);
         const int shift = t < sp.ns ? f1 : f2 - n1;
         if (g.whole_tiles) {
@@ -564,15 +563,15 @@ void gqa_decode_kernel(DecodeGeom g) {
       }
     }
     __syncthreads();
-    for (int x = 64 * wv + el; x < ncols * U; x += 64 * kGqaWaves) {
+    for (int x = 64 * wv + el; x < ncols * U; x += 64 * W) {
       const int col = x / U, u = x % U, d = 4 * u;
       float mx = pm[0][col];
 #pragma unroll
-      for (int w = 1; w < kGqaWaves; ++w) mx = fmaxf(mx, pm[w][col]);
+      for (int w = 1; w < W; ++w) mx = fmaxf(mx, pm[w][col]);
       float sum = 0.f;
       f32x4 acc = {};
 #pragma unroll
-      for (int w = 0; w < kGqaWaves; ++w) {
+      for (int w = 0; w < W; ++w) {
         const float f = fast_exp2(pm[w][col] - mx);
         sum += pl[w][col] * f;
         acc += f * reinterpret_cast<const f32x4*>(ring[w])[col * U + (u ^ (col & 15))];
@@ -1056,8 +1055,10 @@ __global__ __launch_bounds__(S * T) void latent_join_kernel(DecodeGeom g) {
 constexpr int64_t kJoinFew = 2048;  // workgroups
 template <int D, bool FP8, int NB>
 static hipError_t launch_gqa(const DecodeGeom& g, hipStream_t st) {
-  const auto kernel = g.R > 1 ? gqa_decode_kernel<D, FP8, NB, true> : gqa_decode_kernel<D, FP8, NB, false>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)g.grid), dim3(64 * kGqaWaves), 0, st, g);
+  auto kernel = g.R > 1 ? gqa_decode_kernel<D, FP8, NB, true, 4> : gqa_decode_kernel<D, FP8, NB, false, 4>;
+  if constexpr (NB <= 2)
+    if (g.waves == 8) kernel = g.R > 1 ? gqa_decode_kernel<D, FP8, NB, true, 8> : gqa_decode_kernel<D, FP8, NB, false, 8>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)g.grid), dim3(64 * (unsigned)g.waves), 0, st, g);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.part_o == nullptr) return e;
   const int64_t rows = (int64_t)g.n_seq * g.R * g.H;

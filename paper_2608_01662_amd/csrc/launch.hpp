@@ -161,6 +161,7 @@ struct DecodeGeom {
   FastDiv by_stretches;  // division by the stretches the tiles are dealt in (grid = stretches * M)
   FastDiv by_seqs;    // by n_seq
   int together;       // the M workgroups of a stretch on one XCD (stretches are a multiple of 8)
+  int waves;          // of a workgroup (grouped heads)
   int min_tiles;      // fewest tiles of a workgroup (see least_tiles)
   float *part_o, *part_ml;  // two partials per workgroup: [block_cols, d_v], [block_cols, 2]; nullptr: none is cut
   int4* parts;        // [n_seq, M]: first and last stretch of each, slot of the first one's partial, r
@@ -173,8 +174,10 @@ __host__ __device__ inline int least_tiles(int64_t total, int step) {
   const int t = (int)(__builtin_sqrtf((float)total) * 0.25f + 0.5f);
   return t < step ? step : step == 4 ? t & -4 : t;
 }
-// Workgroups of the grouped-head kernel per CU: two where the registers of NB blocks of 16 query rows allow it.
-constexpr int gqa_per_cu(int d, int nb, bool multi) { return nb <= 2 || (d == 64 && !multi) ? 2 : 1; }
+// Waves of the grouped-head kernel per SIMD: two where the registers of nb blocks of 16 query rows allow it; and
+// workgroups of w waves per CU.
+constexpr int gqa_waves_per_simd(int d, int nb, bool multi) { return nb <= 2 || (d == 64 && !multi) ? 2 : 1; }
+constexpr int gqa_per_cu(int d, int nb, bool multi, int w) { return 4 * gqa_waves_per_simd(d, nb, multi) / w; }
 hipError_t launch_decode_attn(const DecodeGeom& g, hipStream_t st);
 
 }  // namespace lsa

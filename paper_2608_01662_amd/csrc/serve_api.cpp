@@ -74,7 +74,7 @@ lsa_status check_decode_sizes(const lsa_decode_attn_params* p, int32_t n_seq, in
 
 // How a call is dealt out (decode_attn.hip): `grid` workgroups take equal stretches of all tiles.
 struct DecodePlan {
-  int grid, stretches, min_tiles, block_cols, blocks, M, pass_tiles;  // (see DecodeGeom)
+  int grid, stretches, waves, min_tiles, block_cols, blocks, M, pass_tiles;  // (see DecodeGeom)
   bool cut;  // may a stretch end inside a (sequence, head)?
   int64_t all_tiles;  // at most
   bool together;
@@ -88,10 +88,11 @@ constexpr int kLatentPages = 1024; // the same, latent cache
 // A (sequence, head, query row block) of at most that many tiles is left whole: a workgroup each, no scan of the lengths, no
 // partials and no join. What the host knows is the tables' capacity, so the bound also limits what one long sequence
 // among short ones can cost. us of whole calls, cut / whole, sequences x positions:
-//   32 heads on 8 key heads (about 0.3 us a tile in a workgroup of its own; 100 of them come near the memory's rate):
-//     1 x 128 7.6 / 5.6, 1 x 1001 9.6 / 13.6, 4 x 500 9.4 / 8.5, 4 x 1001 11.6 / 14.8, 8 x 1000 13.8 / 14.0, 8 x 2000 20.0 / 22.5,
-//     12 x 2000 29.0 / 25.9, 16 x 2000 35.6 / 30.7, 64 x 1000 53.8 / 51.2, 256 x 1000 196 / 187; a window of 1024 on 33 x 12
-//     heads 27.6 / 22.7
+//   32 heads on 8 key heads (about 0.3 us a tile in a workgroup of 4 waves of its own, 0.23 in one of 8; 100 of them come near
+//     the memory's rate): 1 x 128 7.6 / 5.6, 1 x 500 9.0 / 8.0, 1 x 1001 9.1 / 10.5, 2 x 700 11.4 / 9.2, 3 x 1000 11.0 / 11.6, 4 x
+//     1000 12.0 / 11.7, 4 x 2000 16.4 / 16.7, 8 x 1000 14.2 / 12.0, 8 x 2000 20.7 / 17.4, 16 x 2000 34.9 / 29.4, 64 x 1000 53.8 /
+//     51.2, 256 x 1000 196 / 187; fp8 4 x 1000 10.1 / 10.5, 8 x 2000 18.1 / 16.7; a window of 1024 on 33 x 12 heads 27.6 / 22.7
+//   16 heads on one: 32 x 1000 13.8 / 12.2, 69 x 1200 19.4 / 13.8, 69 x 4000 37.6 / 46.7
 //   64 query rows of a key head: 1 x 500 13.6 / 16.2, 32 x 500 16.8 / 16.7, 32 x 1000 19.8 / 24.0, 69 x 1200 32.7 / 27.8, 69 x 2000
 //     35.7 / 38.1, 150 x 2000 56.9 / 47.4
 //   latent, 64 heads (0.95 us a tile): 1 x 200 12.5 / 13.7, 4 x 300 13.7 / 16.6, 8 x 300 17.0 / 16.6, 16 x 500 25.2 / 22.4, 28 x 700
@@ -101,8 +102,8 @@ int64_t whole_tiles(const lsa_decode_attn_params* p, int block_cols, int64_t pai
     const int64_t t = pairs <= 16 ? 4 + pairs * 3 / 4 : 12 + pairs / 4;
     return t < 48 ? t : 48;
   }
-  const int64_t t = pairs * 3 / 4, least = block_cols == 64 ? 8 : 16;
-  return t < least ? least : t < 64 ? t : 64;
+  const int64_t t = block_cols <= 32 ? 16 + pairs * 3 / 4 : pairs < 12 ? 8 : pairs * 3 / 4;
+  return t < 64 ? t : 64;
 }
 
 DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq, int32_t max_pages,
@@ -124,12 +125,16 @@ DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t r
   pl.min_tiles = latent ? 2 : 4;  // (grouped heads: one per wave)
   pl.all_tiles = pairs * tiles;
   const int64_t some = cdiv(pl.all_tiles, lsa::least_tiles(pl.all_tiles, pl.min_tiles)), most = some > pairs ? some : pairs;
-  const int64_t wgs = kCus * (latent ? 1 : lsa::gqa_per_cu(p->d_qk, pl.block_cols / 16, rows_per_seq > 1));
+  const int64_t wgs = kCus * (latent ? 1 : lsa::gqa_per_cu(p->d_qk, pl.block_cols / 16, rows_per_seq > 1, 4));
   const int64_t n = (most < wgs ? most : wgs) / pl.M;
   pl.stretches = (int)(n > 1 ? n : 1);
   pl.together = (latent ? pl.M : pl.blocks) > 1 && pl.stretches >= 8;
   if (pl.together) pl.stretches &= -8;
   pl.cut = tiles > whole_tiles(p, pl.block_cols, pairs);
+  // Left whole, a (sequence, head) has one workgroup: of 8 waves where the workgroups are fewer than the CUs and their tiles
+  // enough for 8. us with 4 / 8 waves, 32 heads on 8: 8 x 2000 22.8 / 17.4, 16 x 1001 15.1 / 15.2, 24 x 1000 19.4 / 20.0, 32 x 1000
+  // 26.5 / 27.0, 1 x 250 6.5 / 6.7, 1 x 500 8.5 / 8.0; 16 heads on one, 69 x 2000 23.3 / 18.1; fp8 24 x 1000 15.5 / 14.2.
+  pl.waves = !latent && !pl.cut && pairs <= kCus * 3 / 4 && tiles > 8 && pl.block_cols <= 32 ? 8 : 4;
   pl.grid = (int)(pl.cut ? (int64_t)pl.stretches * pl.M : pairs);
   // pages of a pass: tiles * 32 / P, and two more at the ends of each of two parts
   const int64_t pass = (int64_t)((latent ? kLatentPages : kPageSlots) - 4) * kv_page_size / kTile;
@@ -311,6 +316,7 @@ lsa_status lsa_decode_attn(const lsa_decode_attn_params* p, int32_t n_seq, int32
   g.by_stretches = lsa::fast_div((uint32_t)pl.stretches);
   g.together = pl.cut && pl.together;
   g.by_seqs = lsa::fast_div((uint32_t)n_seq);
+  g.waves = pl.waves;
   g.min_tiles = pl.min_tiles;
   if (pl.cut) {
     g.part_o = static_cast<float*>(workspace);

@@ -365,3 +365,17 @@ def test_uncut_batches(form, top):
     assert lsa.decode_attn_workspace_size(prm, 290, 1, x["table"].shape[1], 64) == 0
     out, lse = _run(prm, x)
     _check(prm, x, out, lse)
+
+
+@pytest.mark.parametrize("form", FORMS, ids=str)
+@pytest.mark.parametrize("R,ctx,cut", [(1, [0, 1, 31, 257, 2100], True), (5, [2, 64, 2200], True), (1, [0, 3, 299, 480], False),
+                                       (2, [1, 290, 511, 33, 0, 64, 128], False)])
+def test_forms_cut_and_whole(form, R, ctx, cut):
+    """Every head layout and type with the contexts split among workgroups, and each left to one workgroup (of eight waves
+    where few sequences have many tiles)."""
+    prm = _params(*form)
+    x = _batch(prm, ctx, R, 64, seed=21 + R, width=70 if cut else None)
+    if cut:
+        assert lsa.decode_attn_workspace_size(prm, len(ctx), R, x["table"].shape[1], 64) > 0
+    out, lse = _run(prm, x)
+    _check(prm, x, out, lse)
