@@ -44,6 +44,14 @@ __device__ __forceinline__ Span span_of(const DecodeGeom& g, int ctx) {
 // (a wave-uniform value that the compiler cannot know to be: kept in a scalar register)
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
+// 2^(s scale - m), the product rounded as where the maximum m was taken: one rounding for both (an fma) leaves the largest
+// score's exponent at m's rounding error, which overflows from scores of 2^31 on.
+__device__ __forceinline__ float exp2_below(float s, float scale, float m) {
+#pragma clang fp contract(off)
+  const float z = s * scale;
+  return fast_exp2(z - m);
+}
+
 // Inclusive sum over the lanes of a wave.
 __device__ __forceinline__ int wave_scan(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr 1, 2, 4, 8: within rows of 16
@@ -595,10 +603,11 @@ void gqa_decode_kernel(DecodeGeom g) {
 }
 
 // ============================================================================ latent cache
-// One workgroup = eight waves = up to 64 heads of one new token. Two waves per SIMD, split by role as in the
-// sparse attention (attention.hip, whose tile and operand layouts these are): four scorers compute S^T = K Q^T of 16 tokens x 32 heads each, do the online
-// softmax and leave P (bf16) and the reference maximum of their token half in an LDS slot; four value waves,
-// one tile behind, accumulate O^T += V^T P^T for all heads and 128 value columns each, from V operands read a
+// One workgroup = eight waves = 32 HB columns, query rows of a sequence (its new tokens' heads, token by token, so that
+// few heads of several tokens share one pass over the cache). Two waves per SIMD, split by role as in the
+// sparse attention (attention.hip, whose tile and operand layouts these are): four scorers compute S^T = K Q^T of 16 tokens x
+// 16 HB columns each, do the online softmax and leave P (bf16) and the reference maximum of their token half in an LDS slot;
+// four value waves, one tile behind, accumulate O^T += V^T P^T for all columns and 128 value dims each, from V operands read a
 // tile ahead. One barrier per tile.
 //
 // Here the tiles are whole stretches of cache rows, so nothing is gathered through a list: a value wave's lane finds
@@ -609,22 +618,30 @@ constexpr int kLatBufs = 4;
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 constexpr int kLatPages = 1024;  // page-table entries staged in LDS at a time
 
+template <int HB, bool MULTI>  // blocks of 32 query rows; MULTI: of several new tokens
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void latent_decode_kernel(DecodeGeom g) {
+  constexpr int COLS = 32 * HB;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kLatBufs * kMlaTile + 2 * kMlaPSlot];
   __shared__ int pages[kLatPages];
-  __shared__ float fin[2 * 2 * 64];  // per (token half, head): reference maximum and sum
+  __shared__ float fin[2 * 2 * COLS];  // per (token half, column): reference maximum and sum
   const int lane = threadIdx.x & 63, wv = uniform((int)(threadIdx.x >> 6));
   const int i16 = lane & 15, q4 = lane >> 4, w4 = wv & 3;
   const bool scorer = wv < 4;
   uint8_t* const pslots = lds + kLatBufs * kMlaTile;
   const uint8_t* kvb = static_cast<const uint8_t*>(g.k);
-  const int hb_n = (int)g.by_blocks.d;  // 64 heads each, of one new token
 
   auto segment = [&](int b, int r, const Span& sp, int t0, int t1, bool whole, int slot) {
-    const int j = fdiv(g.by_blocks, r), h0 = (r - j * hb_n) * 64, nh = g.H - h0 < 64 ? g.H - h0 : 64;
-    const int tq = sp.c - g.R + j;  // this token's position
-    const int64_t row0 = ((int64_t)b * g.R + j) * g.H + h0;  // output row of head h0
+    // columns: rows col0 .. of the sequence's R * H; positions of the first and the last one's new token
+    const int col0 = r * COLS, ncols = g.R * g.H - col0 < COLS ? g.R * g.H - col0 : COLS;
+    const int tq0 = sp.c - g.R + fdiv(g.by_group, col0);
+    const int tq1 = MULTI ? sp.c - g.R + fdiv(g.by_group, col0 + ncols - 1) : tq0;
+    const int64_t row0 = (int64_t)b * g.R * g.H + col0;  // output row of column 0
+    auto token_of = [&](int col) { return MULTI ? sp.c - g.R + fdiv(g.by_group, col0 + (col < ncols ? col : 0)) : tq0; };
+    auto sees = [&](int s, int t) { return s <= t && (g.k_swa == 0 || t - s < g.k_swa || s < g.k_sink); };
+    // several new tokens: does a tile from position s0 on reach to where they see different positions?
+    auto uneven = [&](int s0) { return MULTI && uniform(tq0 != tq1 && (s0 + kTile > tq0 + 1 || (g.k_swa > 0 && s0 <= tq1 - g.k_swa))); };
+    auto first_pos = [&](int t) { return (t < sp.ns ? t : t + sp.skip) * kTile; };
     // page-table entries of tiles [p0, p1): those before the skipped ones, then the others
     int f1 = 0, n1 = 0, f2 = 0;
     auto stage = [&](int p0, int p1) {
@@ -652,29 +669,36 @@ void latent_decode_kernel(DecodeGeom g) {
         }
       lds_barrier();
     };
-    // cache row of token `tok` of tile t, -1 where this query does not attend to it
+    // cache row of token `tok` of tile t, -1 where no column attends to it
     auto row_of = [&](int t, int tok) {
-      const int s = (t < sp.ns ? t : t + sp.skip) * kTile + tok;
-      if (s < 0 || s > tq || !(g.k_swa == 0 || tq - s < g.k_swa || s < g.k_sink)) return -1;
+      const int s = first_pos(t) + tok;
+      if (s > tq1 || !(g.k_swa == 0 || tq0 - s < g.k_swa || s < g.k_sink)) return -1;
       const int pg = fdiv(g.by_page, s);
       const int ph = pages[t < sp.ns ? pg - f1 : n1 + pg - f2];
       return ph >= 0 ? ph * g.P + (s - pg * g.P) : -1;
     };
     if (scorer) {
-      const int th = w4 & 1, pair = w4 >> 1;  // tokens 16 th .. + 15, heads 32 pair .. + 31
+      const int th = w4 & 1, pair = w4 >> 1;  // tokens 16 th .. + 15, columns 16 HB pair ..
       const int ksw = mla_swz(i16 >> 3, i16 & 7);
       const int k_row = th * kMlaHalf + 9 * (i16 >> 3) * 1024 + 8 * (i16 & 7) * 16;
       const int k_even = k_row + ((0 + q4) ^ ksw) * 16, k_odd = k_row + ((4 + q4) ^ ksw) * 16;
-      u32x4 qb[2][18];  // Q^T as the B operand: column = head 32 pair + 16 nb + i16, k-step s covers dims 32 s + 8 q4 ..
-      float m[2] = {kNoRef, kNoRef}, l[2] = {0.f, 0.f};
+      u32x4 qb[HB][18];  // Q^T as the B operand: column 16 (HB pair + nb) + i16, k-step s covers dims 32 s + 8 q4 ..
+      float m[HB], l[HB];
+      int tcol[HB];  // positions of the columns' new tokens
+#pragma unroll
+      for (int nb = 0; nb < HB; ++nb) {
+        m[nb] = kNoRef;
+        l[nb] = 0.f;
+        tcol[nb] = token_of(16 * (HB * pair + nb) + i16);
+      }
       for (int p0 = t0; p0 < t1; p0 += g.pass_tiles) {
         const int nt = t1 - p0 < g.pass_tiles ? t1 - p0 : g.pass_tiles;
         stage(p0, p0 + nt);
-        if (p0 == t0) {  // Q has landed as two tiles of 32 heads, whose rows lie as a K tile's
+        if (p0 == t0) {  // Q has landed as tiles of 32 columns, whose rows lie as a K tile's
           lds_barrier();
-          const uint8_t* qt = lds + (kLatBufs - 2 + pair) * kMlaTile - th * kMlaHalf;
+          const uint8_t* qt = lds + (kLatBufs - 2) * kMlaTile + pair * (HB == 2 ? kMlaTile : kMlaHalf) - th * kMlaHalf;
 #pragma unroll
-          for (int nb = 0; nb < 2; ++nb)
+          for (int nb = 0; nb < HB; ++nb)
 #pragma unroll
             for (int s = 0; s < 18; ++s) qb[nb][s] = *reinterpret_cast<const u32x4*>(qt + nb * kMlaHalf + ((s & 1) ? k_odd : k_even) + (s >> 1) * 1024);
           lds_barrier();
@@ -691,10 +715,12 @@ void latent_decode_kernel(DecodeGeom g) {
           if (it > 0) {
             const uint8_t* pr = pslots + ((it - 1) & 1) * kMlaPSlot + 64 * kMlaPHead + (1 - th) * 256;
 #pragma unroll
-            for (int nb = 0; nb < 2; ++nb) mp[nb] = *reinterpret_cast<const float*>(pr + 4 * (32 * pair + 16 * nb + i16));
+            for (int nb = 0; nb < HB; ++nb) mp[nb] = *reinterpret_cast<const float*>(pr + 4 * (16 * (HB * pair + nb) + i16));
           }
           constexpr int KB = 3;  // K operands requested ahead of the products
-          f32x4 sacc[2] = {f32x4{}, f32x4{}};
+          f32x4 sacc[HB];
+#pragma unroll
+          for (int nb = 0; nb < HB; ++nb) sacc[nb] = f32x4{};
           u32x4 ka[2][KB];
 #pragma unroll
           for (int s6 = 0; s6 < KB; ++s6) ka[0][s6] = *reinterpret_cast<const u32x4*>(tb + ((s6 & 1) ? k_odd : k_even) + (s6 >> 1) * 1024);
@@ -711,23 +737,30 @@ void latent_decode_kernel(DecodeGeom g) {
 #pragma unroll
             for (int s6 = 0; s6 < KB; ++s6)
 #pragma unroll
-              for (int nb = 0; nb < 2; ++nb) sacc[nb] = mfma16(ka[bt & 1][s6], qb[nb][KB * bt + s6], sacc[nb]);
+              for (int nb = 0; nb < HB; ++nb) sacc[nb] = mfma16(ka[bt & 1][s6], qb[nb][KB * bt + s6], sacc[nb]);
             __builtin_amdgcn_sched_barrier(0);
           }
           const uint32_t hmask = (vmask >> (16 * th)) & 0xFFFFu;
           if (hmask != 0xFFFFu) {
 #pragma unroll
-            for (int nb = 0; nb < 2; ++nb)
+            for (int nb = 0; nb < HB; ++nb)
 #pragma unroll
               for (int k = 0; k < 4; ++k) sacc[nb][k] = ((hmask >> (4 * q4 + k)) & 1u) ? sacc[nb][k] : -INFINITY;
           }
+          if (const int s0 = first_pos(p0 + it); uneven(s0)) {
+#pragma unroll
+            for (int nb = 0; nb < HB; ++nb)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) sacc[nb][k] = sees(s0 + 16 * th + 4 * q4 + k, tcol[nb]) ? sacc[nb][k] : -INFINITY;
+          }
           uint8_t* ps = pslots + (it & 1) * kMlaPSlot;
-          float smx[2];
+          float smx[HB];
 #pragma unroll
-          for (int nb = 0; nb < 2; ++nb) smx[nb] = fmaxf(fmaxf(sacc[nb][0], sacc[nb][1]), fmaxf(sacc[nb][2], sacc[nb][3]));
-          max4_xor16_32_pair(smx[0], smx[1]);
+          for (int nb = 0; nb < HB; ++nb) smx[nb] = fmaxf(fmaxf(sacc[nb][0], sacc[nb][1]), fmaxf(sacc[nb][2], sacc[nb][3]));
+          if constexpr (HB == 2) max4_xor16_32_pair(smx[0], smx[1]);
+          else smx[0] = max4_xor16_32(smx[0]);
 #pragma unroll
-          for (int nb = 0; nb < 2; ++nb) {
+          for (int nb = 0; nb < HB; ++nb) {
             const float mx = smx[nb] * g.scale_log2;
             // the reference moves when the maximum grows by more than 2^8, or to the other half's when that is larger
             float tgt = mx > m[nb] + kLazy ? mx : m[nb];
@@ -740,28 +773,28 @@ void latent_decode_kernel(DecodeGeom g) {
             float p[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              p[k] = fast_exp2(fmaf(sacc[nb][k], g.scale_log2, -m[nb]));  // -inf -> 0
+              p[k] = exp2_below(sacc[nb][k], g.scale_log2, m[nb]);  // -inf -> 0
               l[nb] += p[k];
             }
-            const int lh = 32 * pair + 16 * nb + i16;
+            const int lh = 16 * (HB * pair + nb) + i16;
             *reinterpret_cast<u32x2*>(ps + lh * kMlaPHead + 32 * th + 8 * q4) = u32x2{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])};
             if (q4 == 0) *reinterpret_cast<float*>(ps + 64 * kMlaPHead + th * 256 + 4 * lh) = m[nb];
           }
         }
       }
 #pragma unroll
-      for (int nb = 0; nb < 2; ++nb) {
+      for (int nb = 0; nb < HB; ++nb) {
         const float lt = sum4_xor16_32(l[nb]);
         if (q4 == 0) {
-          const int lh = 32 * pair + 16 * nb + i16;
-          fin[2 * (64 * th + lh)] = m[nb];
-          fin[2 * (64 * th + lh) + 1] = lt;
+          const int lh = 16 * (HB * pair + nb) + i16;
+          fin[2 * (COLS * th + lh)] = m[nb];
+          fin[2 * (COLS * th + lh) + 1] = lt;
         }
       }
       __syncthreads();
       return;
     }
-    // ---- value wave w4: columns 128 w4 .. + 127 of all heads
+    // ---- value wave w4: dims 128 w4 .. + 127 of all columns
     const int G = lane >> 4, sl = lane & 15;
     int v_off[2][2];
 #pragma unroll
@@ -773,18 +806,21 @@ void latent_decode_kernel(DecodeGeom g) {
         v_off[rd][par] = (9 * o8 + 2 * w4) * 1024 + (8 * j8 + (ch ^ mla_swz(o8, j8))) * 16 + (sl & 1) * 8;
       }
     const int oj = lane & 31;
-    f32x16 o[8];  // block 4 hb + c: heads 32 hb .., dims 128 w4 + 32 c ..
+    f32x16 o[4 * HB];  // block 4 hb + c: columns 32 hb .., dims 128 w4 + 32 c ..
 #pragma unroll
-    for (int c = 0; c < 8; ++c) o[c] = f32x16{};
-    float m_o[2] = {-INFINITY, -INFINITY};  // reference maxima of the accumulators
+    for (int c = 0; c < 4 * HB; ++c) o[c] = f32x16{};
+    bool marred = false;  // was a value taken as 0?
+    float m_o[HB];  // reference maxima of the accumulators
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb) m_o[hb] = -INFINITY;
     // this wave loads tokens 8 w4 .. of a tile: lane 8 jj + u takes chunk u ^ swz of token jj of them, nine times
     const int dj = lane >> 3, dma_tok = 8 * w4 + dj;
     const int64_t dma_col = ((lane & 7) ^ mla_swz(w4, dj)) * 16;
-    // Q goes through the last two tile buffers. (Columns past the heads repeat the first and are not stored.)
+    // Q goes through the last tile buffers. (Columns past the last repeat the first and are not stored.)
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < HB; ++t) {
       const int h = 32 * t + dma_tok;
-      lds_dma_row9(reinterpret_cast<const uint8_t*>(g.q) + (row0 + (h < nh ? h : 0)) * 1152 + dma_col,
+      lds_dma_row9(reinterpret_cast<const uint8_t*>(g.q) + (row0 + (h < ncols ? h : 0)) * 1152 + dma_col,
                    lds_addr(lds + (kLatBufs - 2 + t) * kMlaTile + w4 * (kMlaLoads * 1024)));
     }
     for (int p0 = t0; p0 < t1; p0 += g.pass_tiles) {
@@ -839,22 +875,43 @@ void latent_decode_kernel(DecodeGeom g) {
           read_v();
           continue;
         }
-        const uint8_t* ps = pslots + ((it - 1) & 1) * kMlaPSlot;
-        float mA[2], mB[2];
+        if (const int s0 = first_pos(p0 + it - 1); uneven(s0)) {
+          uint32_t odd = 0;  // (adding 1 to an exponent of ones carries into the sign bit)
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb) {
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) odd |= (va[c][ks][k] & 0x7F807F80u) + 0x00800080u;
+          // A weight of zero does not silence a NaN or an infinity in a row of V that only some of the columns see. It is taken
+          // as 0 here, and those that see it get their NaN after the stores.
+          if (uniform(__ballot((odd & 0x80008000u) != 0) != 0)) {
+            marred = true;
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+              for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) va[c][ks][k] &= ~(((((va[c][ks][k] & 0x7F807F80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xFFFFu);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        const uint8_t* ps = pslots + ((it - 1) & 1) * kMlaPSlot;
+        float mA[HB], mB[HB];
+#pragma unroll
+        for (int hb = 0; hb < HB; ++hb) {
           mA[hb] = *reinterpret_cast<const float*>(ps + 64 * kMlaPHead + 4 * (32 * hb + oj));
           mB[hb] = *reinterpret_cast<const float*>(ps + 64 * kMlaPHead + 256 + 4 * (32 * hb + oj));
         }
-        u32x4 pb[2][2];
+        u32x4 pb[HB][2];
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb)
+        for (int hb = 0; hb < HB; ++hb)
 #pragma unroll
           for (int ks = 0; ks < 2; ++ks)
             pb[hb][ks] = *reinterpret_cast<const u32x4*>(ps + (32 * hb + oj) * kMlaPHead + 32 * ks + 16 * (lane >> 5));
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb) {
+        for (int hb = 0; hb < HB; ++hb) {
           const float mn = fmaxf(mA[hb], mB[hb]);  // >= m_o: the references never decrease
           if (__ballot(mA[hb] != mB[hb] || mn > m_o[hb])) {  // rare once the halves agree
             const float alpha = mn > m_o[hb] ? fast_exp2(m_o[hb] - mn) : 1.f;  // m_o = -inf -> 0
@@ -874,7 +931,7 @@ void latent_decode_kernel(DecodeGeom g) {
 #pragma unroll
           for (int c = 0; c < 4; ++c)
 #pragma unroll
-            for (int hb = 0; hb < 2; ++hb) o[4 * hb + c] = mfma32(va[c][ks], pb[hb][ks], o[4 * hb + c]);
+            for (int hb = 0; hb < HB; ++hb) o[4 * hb + c] = mfma32(va[c][ks], pb[hb][ks], o[4 * hb + c]);
         if (it < nt) {
           __builtin_amdgcn_sched_barrier(0);
           read_v();
@@ -882,22 +939,22 @@ void latent_decode_kernel(DecodeGeom g) {
       }
     }
     __syncthreads();  // the scorers' reference maxima and sums
-    float mfin[2], lt[2];
+    float mfin[HB], lt[HB];
 #pragma unroll
-    for (int hb = 0; hb < 2; ++hb) {
+    for (int hb = 0; hb < HB; ++hb) {
       const int lh = 32 * hb + oj;
-      const float ma = fin[2 * lh], la = fin[2 * lh + 1], mb = fin[2 * (64 + lh)], lb = fin[2 * (64 + lh) + 1];
+      const float ma = fin[2 * lh], la = fin[2 * lh + 1], mb = fin[2 * (COLS + lh)], lb = fin[2 * (COLS + lh) + 1];
       mfin[hb] = fmaxf(ma, mb);
       lt[hb] = la * fast_exp2(ma - mfin[hb]) + lb * fast_exp2(mb - mfin[hb]);
-      if (w4 == 0 && lane < 32 && lh < nh) {
+      if (w4 == 0 && lane < 32 && lh < ncols) {
         if (whole) {
           if (g.lse) g.lse[row0 + lh] = lt[hb] == 0.f ? -INFINITY : (mfin[hb] + __log2f(lt[hb])) * kLn2;
         } else {
-          *reinterpret_cast<f32x2*>(g.part_ml + 2 * (slot * 64 + lh)) = f32x2{mfin[hb], lt[hb]};
+          *reinterpret_cast<f32x2*>(g.part_ml + 2 * ((int64_t)slot * COLS + lh)) = f32x2{mfin[hb], lt[hb]};
         }
       }
     }
-    // An output goes head by head through the tile buffers, idle since the barrier, so that a store instruction
+    // An output goes row by row through the tile buffers, idle since the barrier, so that a store instruction
     // writes whole lines.
     // Lane l, register r of block 4 hb + c holds column 32 c + 8 (r / 4) + 4 (l / 32) + r % 4 of head 32 hb + l % 32.
     // (the lane made opaque here, or these offsets are computed before the loop over stretches and spill)
@@ -907,7 +964,7 @@ void latent_decode_kernel(DecodeGeom g) {
     if (whole) {
       uint8_t* ost = lds + w4 * (64 * 272);
 #pragma unroll
-      for (int hb = 0; hb < 2; ++hb) {
+      for (int hb = 0; hb < HB; ++hb) {
         const float inv = lt[hb] == 0.f ? 0.f : 1.f / lt[hb];
 #pragma unroll
         for (int c = 0; c < 4; ++c)
@@ -920,17 +977,38 @@ void latent_decode_kernel(DecodeGeom g) {
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (this wave's own writes)
 #pragma unroll
-      for (int k = 0; k < 16; ++k) {
+      for (int k = 0; k < 8 * HB; ++k) {
         const int hh = 4 * k + (el >> 4);
         const u32x4 v = *reinterpret_cast<const u32x4*>(ost + hh * 272 + 16 * (el & 15));
-        if (hh < nh) *reinterpret_cast<u32x4*>(g.out + (row0 + hh) * 512 + 128 * w4 + 8 * (el & 15)) = v;
+        if (hh < ncols) *reinterpret_cast<u32x4*>(g.out + (row0 + hh) * 512 + 128 * w4 + 8 * (el & 15)) = v;
       }
-    } else {  // a partial in the accumulators' order, whole lines per store: [4 waves][8 blocks][4][64 lanes][4]
-      f32x4* dst = reinterpret_cast<f32x4*>(g.part_o) + (int64_t)slot * 8192 + w4 * 2048 + el;
+    } else {  // a partial in the accumulators' order, whole lines per store: [4 waves][4 HB blocks][4][64 lanes][4]
+      f32x4* dst = reinterpret_cast<f32x4*>(g.part_o) + (int64_t)slot * (4096 * HB) + w4 * (1024 * HB) + el;
 #pragma unroll
-      for (int c = 0; c < 8; ++c)
+      for (int c = 0; c < 4 * HB; ++c)
 #pragma unroll
         for (int q = 0; q < 4; ++q) dst[(4 * c + q) * 64] = f32x4{o[c][4 * q], o[c][4 * q + 1], o[c][4 * q + 2], o[c][4 * q + 3]};
+    }
+    // (A value that is no number or infinite is part of K too: a column that sees it has a score that is none or infinite, so
+    // that all its output is NaN already unless the score is -inf, whose weight of 0 times the value is NaN.)
+    if (MULTI && marred) {
+      for (int t = t0; t < t1; ++t) {
+        const int s0 = first_pos(t);
+        if (!uneven(s0)) continue;
+        for (int s = s0; s < s0 + kTile && s <= tq1; ++s) {
+          const int pg = fdiv(g.by_page, s), ph = g.page_table ? g.page_table[(int64_t)b * g.max_pages + pg] : b;
+          if (ph < 0 || ph >= g.n_phys) continue;
+          const uint16_t* v = reinterpret_cast<const uint16_t*>(kvb + ((int64_t)ph * g.P + (s - pg * g.P)) * 1152) + 128 * w4;
+          for (int d = lane; d < 128; d += 64) {
+            if ((v[d] & 0x7F80u) != 0x7F80u) continue;
+            for (int col = 0; col < ncols; ++col) {
+              if (!sees(s, token_of(col))) continue;
+              if (whole) g.out[(row0 + col) * 512 + 128 * w4 + d] = 0x7FC0;
+              else g.part_o[(((int64_t)slot * 16 * HB + w4 * 4 * HB + 4 * (col / 32) + d / 32) * 4 + (d / 8) % 4) * 256 + (col % 32 + 32 * ((d / 4) % 2)) * 4 + d % 4] = __builtin_nanf("");
+            }
+          }
+        }
+      }
     }
   };
   deal(g, 512, segment);
@@ -1030,23 +1108,23 @@ __global__ __launch_bounds__(S * T) void gqa_join_kernel(DecodeGeom g) {
   join_store(g, r, ((int64_t)b * g.R + j) * g.H + kvh * group + col - j * group, D, d);
 }
 
-// Latent: a workgroup per (new token, 64 heads) and T of the partial's 8192 vectors of four, 64 of which are 32 heads x 8
-// dims in the accumulators' order.
-template <int S, int T>
+// Latent: a workgroup per (sequence, block of columns) and T of the partial's 4096 HB vectors of four, 64 of which are 32
+// columns x 8 dims in the accumulators' order.
+template <int HB, int S, int T>
 __global__ __launch_bounds__(S * T) void latent_join_kernel(DecodeGeom g) {
-  static_assert(T % 64 == 0, "a wave's threads share their partials");
+  static_assert(HB <= 2 && T % 64 == 0, "a wave's threads share their partials");
   __shared__ Joined lds[S * T / 64 * 64];
   const int4 p = g.parts[blockIdx.x];
   if (p.x == p.y) return;
   const int vec = T * (int)blockIdx.y + (int)threadIdx.x % T;
-  const int lane = vec & 63, q = (vec >> 6) & 3, c = (vec >> 8) & 3, hb = (vec >> 10) & 1, w4 = vec >> 11;
+  const int lane = vec & 63, q = (vec >> 6) & 3, c = (vec >> 8) & 3, hb = (vec >> 10) & (HB - 1), w4 = vec >> (9 + HB);
   const int lh = 32 * hb + (lane & 31), d = 128 * w4 + 32 * c + 8 * q + 4 * (lane >> 5);
-  Joined r = join_parts<S, (S > 1 ? 8 : 4)>(p, g.M, threadIdx.x / T, [&](int slot) { return *reinterpret_cast<const f32x2*>(g.part_ml + 2 * ((int64_t)slot * 64 + lh)); },
-                           [&](int slot) { return reinterpret_cast<const f32x4*>(g.part_o)[(int64_t)slot * 8192 + vec]; });
+  Joined r = join_parts<S, (S > 1 ? 8 : 4)>(p, g.M, threadIdx.x / T, [&](int slot) { return *reinterpret_cast<const f32x2*>(g.part_ml + 2 * ((int64_t)slot * (32 * HB) + lh)); },
+                           [&](int slot) { return reinterpret_cast<const f32x4*>(g.part_o)[(int64_t)slot * (4096 * HB) + vec]; });
   r = join_threads<S, T>(r, lds);
   if (threadIdx.x >= T) return;
-  const int hb_n = (int)g.by_blocks.d, row = fdiv(g.by_blocks, (int)blockIdx.x), h = 64 * ((int)blockIdx.x - row * hb_n) + lh;
-  if (h < g.H) join_store(g, r, (int64_t)row * g.H + h, 512, d);
+  const int b = fdiv(g.by_m, (int)blockIdx.x), col = 32 * HB * ((int)blockIdx.x - b * g.M) + lh;
+  if (col < g.R * g.H) join_store(g, r, (int64_t)b * g.R * g.H + col, 512, d);
 }
 
 // ============================================================================ host launchers
@@ -1077,16 +1155,24 @@ static hipError_t launch_gqa(const DecodeGeom& g, hipStream_t st) {
   return nb == 1 ? launch_gqa<D, FP8, 1>(g, st) : nb == 2 ? launch_gqa<D, FP8, 2>(g, st) : launch_gqa<D, FP8, 4>(g, st);
 }
 
+template <int HB>
+static hipError_t launch_latent(const DecodeGeom& g, hipStream_t st) {
+  const auto kernel = g.R > 1 && g.H % (32 * HB) != 0 ? latent_decode_kernel<HB, true> : latent_decode_kernel<HB, false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)g.grid), dim3(512), 0, st, g);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || g.part_o == nullptr) return e;
+  const int64_t units = (int64_t)g.n_seq * g.M;
+  // us with 16 / 4 / 1 threads a vector: 64 heads, 1 x 16K 21.1 / 23.0 / 37.3, 4 x 8000 26.0 / 25.3 / 29.5, 8 x 16K 50.6 / 47.4 /
+  // 50.9, 64 x 1500 70.4 / 49.6 / 45.2; 16 heads, 1 x 64K 27.2 / 35.3 / 76.5, 20 x 4000 33.1 / 29.3 / 30.7
+  const int64_t few = units * 64 * HB;
+  if (few <= 128) hipLaunchKernelGGL((latent_join_kernel<HB, 16, 64>), dim3((unsigned)units, 64 * HB), dim3(1024), 0, st, g);
+  else if (few <= 2048) hipLaunchKernelGGL((latent_join_kernel<HB, 4, 64>), dim3((unsigned)units, 64 * HB), dim3(256), 0, st, g);
+  else hipLaunchKernelGGL((latent_join_kernel<HB, 1, 256>), dim3((unsigned)units, 16 * HB), dim3(256), 0, st, g);
+  return hipGetLastError();
+}
+
 hipError_t launch_decode_attn(const DecodeGeom& g, hipStream_t st) {
-  if (g.latent) {
-    hipLaunchKernelGGL(latent_decode_kernel, dim3((unsigned)g.grid), dim3(512), 0, st, g);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || g.part_o == nullptr) return e;
-    const int64_t units = (int64_t)g.n_seq * g.M;
-    if (units * 128 <= kJoinFew) hipLaunchKernelGGL((latent_join_kernel<16, 64>), dim3((unsigned)units, 128), dim3(1024), 0, st, g);
-    else hipLaunchKernelGGL((latent_join_kernel<1, 256>), dim3((unsigned)units, 32), dim3(256), 0, st, g);
-    return hipGetLastError();
-  }
+  if (g.latent) return g.block_cols == 32 ? launch_latent<1>(g, st) : launch_latent<2>(g, st);
   if (g.d_qk == 64) return g.fp8 ? launch_gqa<64, true>(g, st) : launch_gqa<64, false>(g, st);
   return g.fp8 ? launch_gqa<128, true>(g, st) : launch_gqa<128, false>(g, st);
 }

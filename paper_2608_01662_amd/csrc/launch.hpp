@@ -154,8 +154,8 @@ struct DecodeGeom {
   int pass_tiles;     // tiles whose page-table entries fit the LDS area
   int block_cols;     // query rows of one key/value head that a workgroup takes together
   FastDiv by_group;   // division by H / Hkv
-  FastDiv by_blocks;  // by the blocks of block_cols of a head's query rows (latent: of a new token's heads)
-  int M;              // such blocks of a sequence
+  FastDiv by_blocks;  // by the blocks of block_cols of a head's query rows
+  int M;              // such blocks of a sequence (of all heads)
   FastDiv by_m;       // by M
   int grid;           // workgroups
   FastDiv by_stretches;  // division by the stretches the tiles are dealt in (grid = stretches * M)

@@ -95,9 +95,17 @@ constexpr int kLatentPages = 1024; // the same, latent cache
 //   16 heads on one: 32 x 1000 13.8 / 12.2, 69 x 1200 19.4 / 13.8, 69 x 4000 37.6 / 46.7
 //   64 query rows of a key head: 1 x 500 13.6 / 16.2, 32 x 500 16.8 / 16.7, 32 x 1000 19.8 / 24.0, 69 x 1200 32.7 / 27.8, 69 x 2000
 //     35.7 / 38.1, 150 x 2000 56.9 / 47.4
-//   latent, 64 heads (0.95 us a tile): 1 x 200 12.5 / 13.7, 4 x 300 13.7 / 16.6, 8 x 300 17.0 / 16.6, 16 x 500 25.2 / 22.4, 28 x 700
-//     25.4 / 28.3, 64 x 700 32.1 / 29.0, 64 x 1000 33.1 / 38.6, 128 x 1300 66 / 56, 300 x 1300 139 / 127
-int64_t whole_tiles(const lsa_decode_attn_params* p, int block_cols, int64_t pairs) {
+//   latent, blocks of 64 rows: 8 x 300 17.0 / 16.6, 16 x 500 25.2 / 22.4, 28 x 700 25.4 / 28.3, 64 x 700 32.1 / 29.0, 64 x 1000 33.1 /
+//     38.6, 128 x 1300 66 / 50, 300 x 1300 137 / 122
+//   latent, blocks of 32: 64 heads (two blocks) 1 x 200 10.6 / 10.6, 1 x 400 10.8 / 15.0, 4 x 300 13.5 / 12.8, 8 x 300 14.8 / 12.9, 16
+//     x 500 21.7 / 19.2, 28 x 700 23.4 / 24.4, 64 x 700 30.2 / 25.3, 64 x 1000 30.8 / 32.9; 16 heads 4 x 300 10.3 / 12.7, 8 x 300
+//     11.1 / 12.8, 16 x 500 14.7 / 18.0, 28 x 700 21.1 / 23.8, 64 x 700 23.7 / 24.3, 64 x 1000 26.3 / 32.0, 128 x 1300 54.5 / 45.5,
+//     128 x 2000 73.3 / 65.2, 190 x 1000 61.7 / 44.9
+int64_t whole_tiles(const lsa_decode_attn_params* p, int block_cols, int64_t n_seq, int64_t pairs) {
+  if (p->latent && block_cols == 32) {
+    const int64_t t = pairs <= 16 ? 4 + pairs / 2 : 8 + pairs / 4;
+    return n_seq >= 96 ? 64 : t < 28 ? t : 28;
+  }
   if (p->latent) {
     const int64_t t = pairs <= 16 ? 4 + pairs * 3 / 4 : 12 + pairs / 4;
     return t < 48 ? t : 48;
@@ -109,28 +117,32 @@ int64_t whole_tiles(const lsa_decode_attn_params* p, int block_cols, int64_t pai
 DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq, int32_t max_pages,
                        int32_t kv_page_size) {
   DecodePlan pl{};
-  // grouped heads: the query rows of a key/value head, in blocks; latent: 64 heads of one new token
   const bool latent = p->latent != 0;
-  const int64_t cols = latent ? p->n_heads : (int64_t)rows_per_seq * (p->n_heads / p->n_kv_heads);
-  pl.block_cols = latent ? 64 : cols <= 16 ? 16 : cols <= 32 ? 32 : 64;
-  pl.blocks = (int)cdiv(cols, pl.block_cols);
-  pl.M = (latent ? rows_per_seq : p->n_kv_heads) * pl.blocks;
-  const int64_t pairs = (int64_t)n_seq * pl.M;
   const int64_t cap = (int64_t)max_pages * kv_page_size;
   int64_t tiles = cdiv(cap, kTile);  // of one (sequence, head), at most
   if (p->k_swa > 0) {
     const int64_t window = cdiv(p->k_sink, kTile) + cdiv((int64_t)p->k_swa + rows_per_seq, kTile) + 1;
     tiles = window < tiles ? window : tiles;
   }
+  // The query rows of a key/value head, in blocks. More rows a block read the cache fewer times; latent blocks of 32 go to
+  // twice the workgroups, at 0.6 us a tile instead of 0.95, with half the partials. us of 64 heads in blocks of 32 / 64: 1 x 200
+  // 10.5 / 12.6, 1 x 16K 21.4 / 24.3, 1 x 64K 30.1 / 32.5, 8 x 16K 53.5 / 50.9, 64 x 300 15.6 / 18.2, 64 x 1000 30.8 / 36.2, 128 x 300 20.2 /
+  // 19.3, 128 x 700 33.6 / 31.4.
+  const int64_t cols = (int64_t)rows_per_seq * (p->n_heads / p->n_kv_heads), blocks64 = n_seq * cdiv(cols, 64);
+  if (latent) pl.block_cols = cols <= 32 || (blocks64 <= 96 && blocks64 * tiles <= 2048) ? 32 : 64;
+  else pl.block_cols = cols <= 16 ? 16 : cols <= 32 ? 32 : 64;
+  pl.blocks = (int)cdiv(cols, pl.block_cols);
+  pl.M = p->n_kv_heads * pl.blocks;
+  const int64_t pairs = (int64_t)n_seq * pl.M;
   pl.min_tiles = latent ? 2 : 4;  // (grouped heads: one per wave)
   pl.all_tiles = pairs * tiles;
   const int64_t some = cdiv(pl.all_tiles, lsa::least_tiles(pl.all_tiles, pl.min_tiles)), most = some > pairs ? some : pairs;
   const int64_t wgs = kCus * (latent ? 1 : lsa::gqa_per_cu(p->d_qk, pl.block_cols / 16, rows_per_seq > 1, 4));
   const int64_t n = (most < wgs ? most : wgs) / pl.M;
   pl.stretches = (int)(n > 1 ? n : 1);
-  pl.together = (latent ? pl.M : pl.blocks) > 1 && pl.stretches >= 8;
+  pl.together = pl.blocks > 1 && pl.stretches >= 8;
   if (pl.together) pl.stretches &= -8;
-  pl.cut = tiles > whole_tiles(p, pl.block_cols, pairs);
+  pl.cut = tiles > whole_tiles(p, pl.block_cols, n_seq, pairs);
   // Left whole, a (sequence, head) has one workgroup: of 8 waves where the workgroups are fewer than the CUs and their tiles
   // enough for 8. us with 4 / 8 waves, 32 heads on 8: 8 x 2000 22.8 / 17.4, 16 x 1001 15.1 / 15.2, 24 x 1000 19.4 / 20.0, 32 x 1000
   // 26.5 / 27.0, 1 x 250 6.5 / 6.7, 1 x 500 8.5 / 8.0; 16 heads on one, 69 x 2000 23.3 / 18.1; fp8 24 x 1000 15.5 / 14.2.

@@ -379,3 +379,57 @@ def test_forms_cut_and_whole(form, R, ctx, cut):
         assert lsa.decode_attn_workspace_size(prm, len(ctx), R, x["table"].shape[1], 64) > 0
     out, lse = _run(prm, x)
     _check(prm, x, out, lse)
+
+
+@pytest.mark.parametrize("heads,R", [(20, 3), (16, 2), (64, 2), (40, 4)])
+@pytest.mark.parametrize("ctx,width", [([150, 64, 97], None), ([1500, 33, 700], 40)], ids=["whole", "cut"])
+def test_infinity_of_weight_zero(heads, R, ctx, width):
+    """Latent: a value of -inf in the newest token of every sequence, whose scores it makes -inf. The one row that sees it
+    has NaN in that dim (0 * inf) and nothing else of it; earlier rows, of the same columns' block, have nothing of it."""
+    prm = _params(MLA, heads, 1, 576, False)
+    x = _batch(prm, ctx, R, 64, seed=heads + R, width=width)
+    x["q"][..., 77] = 1.0
+    at = [(int(x["table"][b, (c - 1) // 64]), (c - 1) % 64) for b, c in enumerate(ctx)]
+    for ph, off in at:
+        x["k_cache"][ph, off, 77] = -1e30    # (a weight of zero too, and 0 * 1e30 = 0)
+    ref, ref_l = (y.clone() for y in _run(prm, x))
+    for ph, off in at:
+        x["k_cache"][ph, off, 77] = float("-inf")
+    out, lse = _run(prm, x)
+    last = torch.arange(len(ctx) * R, device=DEV) % R == R - 1
+    assert torch.isfinite(ref).all() and torch.equal(lse, ref_l)
+    assert torch.isnan(out[last][..., 77]).all()
+    out[last, :, 77] = ref[last, :, 77]
+    assert torch.equal(out, ref)
+
+
+@pytest.mark.parametrize("form", [(GQA, 16, 2, 128, False), (GQA, 40, 1, 64, False), (GQA, 64, 1, 128, False), (MLA, 64, 1, 576, False),
+                                  (MLA, 16, 1, 576, False)], ids=str)
+@pytest.mark.parametrize("ctx,width", [([150, 64, 97], None), ([2100, 33, 700], 70)], ids=["whole", "cut"])
+@pytest.mark.parametrize("R", [1, 2])
+def test_huge_scores(form, ctx, width, R):
+    """The newest position with a score of about 1e30 takes all the weight, and of -1e30 none."""
+    prm = _params(*form)
+    x = _batch(prm, ctx, R, 64, seed=3, width=width)
+    x["q"][..., 5] = 1.0
+    at = [(int(x["table"][b, (c - 1) // 64]), (c - 1) % 64) for b, c in enumerate(ctx)]
+    last = torch.arange(len(ctx) * R, device=DEV) % R == R - 1
+    k, v = x["k_cache"], x["v_cache"] if "v_cache" in x else x["k_cache"][..., :512]
+    for ph, off in at:
+        k[ph, ..., off, 5] = 1e30
+    out, lse = _run(prm, x)
+    group = prm.n_heads // prm.n_kv_heads
+    for row, (ph, off) in zip(out[last], at):
+        want = v[ph, ..., off, :].reshape(prm.n_kv_heads, 1, -1).expand(-1, group, -1).reshape(prm.n_heads, -1)
+        assert torch.equal(row, want)
+    assert (lse[last] > 1e28).all()
+    for ph, off in at:
+        k[ph, ..., off, 5] = -1e30
+    out, lse = _run(prm, x)
+    less = dict(x, ctx=x["ctx"] - 1)
+    ref, ref_l = _run(prm, dict(less, q=x["q"].reshape(len(ctx), R, *x["q"].shape[1:])[:, [R - 1] * R].reshape(x["q"].shape)))
+    # (the last row then sees what a row before it would: compared within the rounding of sums in another order)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    assert ((lse[last] - ref_l[last]).abs() <= 2.0 ** -16 * (1 + ref_l[last].abs())).all()
+    d = (out[last].float() - ref[last].float()).abs()
+    assert (d <= 2.0 ** -6 * v.float().abs().clamp(max=10).max()).all()
