@@ -87,7 +87,8 @@ constexpr int kLatentPages = 1024; // the same, latent cache
 
 // A (sequence, head, query row block) of at most that many tiles is left whole: a workgroup each, no scan of the lengths, no
 // partials and no join. What the host knows is the tables' capacity, so the bound also limits what one long sequence
-// among short ones can cost. us of whole calls, cut / whole, sequences x positions:
+// among short ones can cost. (The launch of a join costs the host 4 us besides, so the bound leaves up to 2 us to it.)
+// us of whole calls, cut / whole, sequences x positions:
 //   32 heads on 8 key heads (about 0.3 us a tile in a workgroup of 4 waves of its own, 0.23 in one of 8; 100 of them come near
 //     the memory's rate): 1 x 128 7.6 / 5.6, 1 x 500 9.0 / 8.0, 1 x 1001 9.1 / 10.5, 2 x 700 11.4 / 9.2, 3 x 1000 11.0 / 11.6, 4 x
 //     1000 12.0 / 11.7, 4 x 2000 16.4 / 16.7, 8 x 1000 14.2 / 12.0, 8 x 2000 20.7 / 17.4, 16 x 2000 34.9 / 29.4, 64 x 1000 53.8 /
@@ -110,8 +111,8 @@ int64_t whole_tiles(const lsa_decode_attn_params* p, int block_cols, int64_t n_s
     const int64_t t = pairs <= 16 ? 4 + pairs * 3 / 4 : 12 + pairs / 4;
     return t < 48 ? t : 48;
   }
-  const int64_t t = block_cols <= 32 ? 16 + pairs * 3 / 4 : pairs < 12 ? 8 : pairs * 3 / 4;
-  return t < 64 ? t : 64;
+  const int64_t t = block_cols <= 32 ? 16 + pairs * 3 / 4 : pairs * 3 / 4, least = block_cols <= 32 ? 32 : 8;
+  return t < least ? least : t < 64 ? t : 64;
 }
 
 DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq, int32_t max_pages,
