@@ -29,7 +29,9 @@ HIPCC_FLAGS = [
 # each product chain: keeping them in VGPRs (not AGPRs) saves a register copy per element.
 # The attention kernels never produce a NaN from finite inputs (masked scores are -inf and every
 # difference of two -inf is guarded): without NaN semantics the softmax maxima compile to plain
-# v_max_f32, without the canonicalising v_max_f32 x, x, x in front of each operand.
+# v_max_f32, without the canonicalising v_max_f32 x, x, x in front of each operand. (The decode attention keeps NaN
+# semantics: a masked weight times a NaN is a case of its own there. Its accumulators are rescaled by vector
+# code, so they are kept in VGPRs too.)
 EXTRA_FLAGS = {"indexer.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "attention.hip": ["-fno-honor-nans"],
                "decode_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 

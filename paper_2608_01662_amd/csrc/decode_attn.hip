@@ -197,11 +197,17 @@ __device__ __forceinline__ u32x2 tr8(const uint8_t* p) {
 }
 
 // ============================================================================ grouped heads, 64 or 128 wide
-// One workgroup = four waves that share no tiles: wave w streams tiles w, w + 4, .. of the stretch through a
+// One workgroup = W waves that share no tiles: wave w streams tiles w, w + W, .. of the stretch through a
 // ring in LDS of its own, K and V apart, by direct loads of whole rows, and refills a tile's K as soon as it is
-// scored and its V as soon as it is multiplied, so that about 24 KB per wave are on their way at any time. (A step of the
-// ring needs no barrier, only a count of the wave's own loads.) At the stretch's end the waves' results are
-// merged through LDS.
+// scored and its V as soon as it is multiplied, so that most of its 16 KB (32 where registers leave one wave per
+// SIMD) are on their way at any time, 128 KB per CU. (A step of the ring needs no barrier, only a count of the wave's own
+// loads.) At the stretch's end the waves' results are merged through LDS.
+//
+// Bound by HBM: 64 sequences of up to 16K, 32 heads on 8 in bf16 (mean 2.1 GB) 372 us, 5.8 TB/s; 48 of 4K to 32K in fp8, two
+// new tokens each (1.9 GB) 337 us, 5.5 TB/s; 33 windows of 1024, 12 heads of 64, pages of 20 (104 MB) 22 us; one
+// sequence of 128K, 16 heads on one (67 MB) 21 us, of which the join 5; one of 1001, 32 on 8, 10.5 us, all latency. Two waves per
+// SIMD hide one's softmax behind the other's products: one wave took 402 and 400 us in place of the first two's 356 and 306 at
+// that time. 33 to 64 query rows per key head need the registers of one wave per SIMD and are bound by its issue.
 //
 // The rows of the products are query rows: the heads of the group of all new tokens, in blocks of 16 (NB
 // blocks per wave); S^T = K Q^T on 16x16x32 products with tokens on the rows, in an order that gives lane
@@ -614,6 +620,11 @@ void gqa_decode_kernel(DecodeGeom g) {
 // the row of its token from the staged page-table entries. A call is bound by the cache's bytes, not by the
 // products, so kLatBufs tile buffers keep kLatBufs - 1 tiles on their way while one is scored (at barrier `it`
 // the buffer of tile it - 1 is free: its V operands are in registers).
+//
+// Measured, 64 heads: 64 sequences of 16K to 128K (5.4 GB) 885 us, 6.2 TB/s, bound by HBM; two new tokens on 64 x 16K 345 us,
+// 0.85 PFLOP/s, each row of the cache read by two workgroups of one XCD; 1 x 16K 21.4 us, of which about 5 are the lengths,
+// pages and Q before the first tile, 0.6 a tile, and the partials' way through the join 5 and more. 16 heads: 64 x 16K 220 us, with
+// three new tokens 241 in one pass over the cache (498 with a workgroup per token).
 constexpr int kLatBufs = 4;
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 constexpr int kLatPages = 1024;  // page-table entries staged in LDS at a time
@@ -1018,7 +1029,7 @@ void latent_decode_kernel(DecodeGeom g) {
 // A thread takes four dims of one output row and every S-th of the row's partials, with a running maximum; the
 // S threads of a row and dims meet in LDS. Bound by two round trips to what other XCDs have just written: which
 // workgroups have partials (left there by the first of them), and the partials. Nothing to do where one
-// stretch covered a (sequence, head) whole.
+// stretch covered a (sequence, head) whole. 4 to 6 us for up to 16 MB of partials, 12 for the 42 MB of 64 latent sequences.
 struct Joined {
   float m, l;
   f32x4 acc;
