@@ -202,7 +202,7 @@ constexpr int64_t kManyUnits = 1 << 18;
 hipError_t launch_append(const AppendGeom& all, hipStream_t st) {
   AppendGeom g = all;
   const int q_units = g.H ? g.d_k / 16 : 1, k_lanes = append_lanes(g.d_k / 16, g.fp8), v_lanes = g.d_v ? append_lanes(g.d_v / 16, g.fp8) : 1;
-  const int heads = g.H % 4 == 0 && all.n_tok * g.H * q_units >= kManyUnits ? 4 : 1;
+  const int heads = g.H % 4 == 0 && (int64_t)all.n_tok * g.H * q_units >= kManyUnits ? 4 : 1;
   g.by_q_units = fast_div((uint32_t)q_units);
   g.by_q_heads = fast_div((uint32_t)(g.H ? g.H / heads : 1));
   g.by_kv_heads = fast_div((uint32_t)g.Hkv);
