@@ -14,6 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "liblsa.so")
+SERVE = os.path.join(HERE, "_serve.so")
 SOURCES = ["indexer.hip", "attention.hip", "append.hip", "decode_attn.hip", "lsa_api.cpp", "serve_api.cpp"]
 ARCH = "gfx950"
 
@@ -43,8 +44,22 @@ def _hipcc() -> str:
     return h
 
 
+def _binding_command(out: str) -> list[str]:
+    """The Python module of the serving operators' host side: host code against torch and liblsa.so."""
+    import sysconfig
+    import torch
+    from torch.utils import cpp_extension
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    return [shutil.which("g++") or "c++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f"-I{INCLUDE}",
+            f"-I{sysconfig.get_paths()['include']}", *(f"-isystem{p}" for p in cpp_extension.include_paths()),
+            os.path.join(CSRC, "serve_bind.cpp"), "-o", out, f"-L{HERE}", "-llsa", "-Wl,-rpath,$ORIGIN",
+            f"-L{lib}", "-lc10", "-ltorch_cpu", "-ltorch_python"]
+
+
 def build(verbose: bool = False) -> str:
-    """Compile every source for gfx950 and link liblsa.so next to this file. Always rebuilds."""
+    """Compile every source for gfx950 and link liblsa.so next to this file, and the binding of the serving
+    operators (_serve.so) against it. Always rebuilds."""
     hipcc = _hipcc()
     objdir = os.path.join(HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
@@ -69,6 +84,10 @@ def build(verbose: bool = False) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}{r.stderr}")
     os.replace(tmp, LIB)
+    r = subprocess.run(_binding_command(SERVE + ".tmp"), capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"binding failed:\n{r.stdout}{r.stderr}")
+    os.replace(SERVE + ".tmp", SERVE)
     return LIB
 
 

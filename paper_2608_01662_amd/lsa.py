@@ -7,6 +7,7 @@ first call does, and raises if liblsa.so has not been built (there is no fallbac
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 import struct
 from dataclasses import dataclass
@@ -15,6 +16,7 @@ import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblsa.so")
+SERVE_PATH = os.path.join(_HERE, "_serve.so")
 
 LSA_KEY_BF16 = 0
 LSA_KEY_FP8_E4M3FN = 1
@@ -552,19 +554,30 @@ def hfa_attn(prm: AttnParams, q: torch.Tensor, kv: torch.Tensor, idx: torch.Tens
 
 
 # ---------------------------------------------------------------- serving: appends and dense decode
-# These calls' kernels take a few microseconds at small batches, less than a host that checks every tensor in
-# detail: a tensor as it should be is passed by one expression (_fits), and only what is not goes through the
-# checks that say why (host time of an append 22.5 -> 16.6 us, of an attention 22.3 -> 17.1).
+# These calls' kernels take a few microseconds at small batches, less than a host that looks at every tensor from
+# Python. So good calls are checked, given their outputs and launched by a compiled module (csrc/serve_bind.cpp),
+# which returns None for any other, and the checks below say why.
+_serve = None
+
+
+def _serving():
+    """Load _serve.so (once). Raises when it is missing, as lib() does."""
+    global _serve
+    if _serve is None:
+        lib()   # (the module is linked to it)
+        if not os.path.exists(SERVE_PATH):
+            raise RuntimeError(f"{SERVE_PATH} is missing; build it with `python -m paper_2608_01662_amd.build`")
+        spec = importlib.util.spec_from_file_location(f"{__package__}._serve", SERVE_PATH)
+        _serve = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(_serve)
+    return _serve
+
+
 _FP8 = (torch.uint8, torch.float8_e4m3fn)
 
 
 def _address(t) -> int:
     return 0 if t is None else t.data_ptr()
-
-
-def _fits(t, dtypes, shape, index: int) -> bool:
-    return isinstance(t, torch.Tensor) and t.dtype in dtypes and t.shape == shape and t.get_device() == index and \
-        t.is_contiguous()
 
 
 def _tokens(name: str, t, n_tok, heads: int, width: int, device, index: int) -> int:
@@ -584,7 +597,7 @@ def _tokens(name: str, t, n_tok, heads: int, width: int, device, index: int) -> 
     return s0 if n_tok > 1 else heads * width
 
 
-def _paged_shape(name: str, t, fp8: bool, heads: int, width: int, device, index: int):
+def _paged_shape(name: str, t, fp8: bool, heads: int, width: int, device):
     """(n_phys, page) of a cache [n_phys, heads, page, width], or without the head dimension when there is one
     head."""
     shape = t.shape if isinstance(t, torch.Tensor) else ()
@@ -594,24 +607,20 @@ def _paged_shape(name: str, t, fp8: bool, heads: int, width: int, device, index:
     else:
         n_phys, page = (shape[0], shape[2]) if len(shape) == 4 else (None, None)
         want = (n_phys, heads, page, width)
-    if not _fits(t, _FP8 if fp8 else _BF16, want, index):
-        _need(name, t, _FP8 if fp8 else _BF16, want, device)
+    _need(name, t, _FP8 if fp8 else _BF16, want, device)
     return n_phys, page
 
 
-def _paged_like(name: str, t, fp8: bool, n_phys: int, heads: int, page: int, width: int, device, index: int) -> None:
+def _paged_like(name: str, t, fp8: bool, n_phys: int, heads: int, page: int, width: int, device) -> None:
     """A cache with the pages of another."""
-    dtypes = _FP8 if fp8 else _BF16
-    if _fits(t, dtypes, (n_phys, heads, page, width), index) or (heads == 1 and _fits(t, dtypes, (n_phys, page, width), index)):
-        return
-    got = _paged_shape(name, t, fp8, heads, width, device, index)
-    raise ValueError(f"{name} has {got[0]} pages of {got[1]} rows, expected {n_phys} of {page}")
+    got = _paged_shape(name, t, fp8, heads, width, device)
+    if got != (n_phys, page):
+        raise ValueError(f"{name} has {got[0]} pages of {got[1]} rows, expected {n_phys} of {page}")
 
 
-def _cache_scale(name: str, t, n_phys: int, heads: int, page: int, device, index: int) -> None:
-    if _fits(t, _F32, (n_phys, heads, page), index) or (heads == 1 and _fits(t, _F32, (n_phys, page), index)):
-        return
-    _need(name, t, _F32, (n_phys, heads, page), device)
+def _cache_scale(name: str, t, n_phys: int, heads: int, page: int, device) -> None:
+    flat = heads == 1 and isinstance(t, torch.Tensor) and t.dim() == 2
+    _need(name, t, _F32, (n_phys, page) if flat else (n_phys, heads, page), device)
 
 
 def cache_append(prm: AppendParams, k: torch.Tensor, k_cache: torch.Tensor, *, page_table: torch.Tensor | None = None,
@@ -632,23 +641,27 @@ def cache_append(prm: AppendParams, k: torch.Tensor, k_cache: torch.Tensor, *, p
     [positions, rot_dim] fp32, cosines then sines. page_table None: sequence b has page b alone (n_seq: how many
     there are, else as ctx_len or the cache has). rows: True, or an int64 tensor [n_tok], for the physical cache
     rows (block_keys_update takes them)."""
+    done = (_serve or _serving()).cache_append(prm, k, k_cache, page_table, ctx_len, pos, seq, rows_per_seq, n_seq, rope, k_rot, v,
+                                               v_cache, k_scale, v_scale, q, q_rot, q_out, rows)
+    if done is not None:
+        return done
     nk, nq, d_k, d_v, rot, fp8 = prm.n_kv_heads, prm.n_heads, prm.d_k, prm.d_v, prm.rot_dim, prm.fp8
     is_tensor = isinstance(k, torch.Tensor)
     dev, i = (k.device, k.get_device()) if is_tensor else (None, -1)
     n = k.shape[0] if is_tensor and k.dim() == 3 else None
     ks = _tokens("k", k, n, nk, d_k if k_rot is None else d_k - rot, dev, i)
     krs = 0 if k_rot is None else _tokens("k_rot", k_rot, n, nk, rot, dev, i)
-    n_phys, page = _paged_shape("k_cache", k_cache, fp8, nk, d_k, dev, i)
+    n_phys, page = _paged_shape("k_cache", k_cache, fp8, nk, d_k, dev)
     vs = qs = qrs = rope_rows = 0
     if d_v:
         vs = _tokens("v", v, n, nk, d_v, dev, i)
-        _paged_like("v_cache", v_cache, fp8, n_phys, nk, page, d_v, dev, i)
+        _paged_like("v_cache", v_cache, fp8, n_phys, nk, page, d_v, dev)
     elif v is not None or v_cache is not None or v_scale is not None:
         raise ValueError("v, v_cache and v_scale must be None with d_v = 0")
     if fp8:
-        _cache_scale("k_scale", k_scale, n_phys, nk, page, dev, i)
+        _cache_scale("k_scale", k_scale, n_phys, nk, page, dev)
         if d_v:
-            _cache_scale("v_scale", v_scale, n_phys, nk, page, dev, i)
+            _cache_scale("v_scale", v_scale, n_phys, nk, page, dev)
     elif k_scale is not None or v_scale is not None:
         raise ValueError("k_scale and v_scale must be None for bf16 caches")
     if nq:
@@ -657,14 +670,13 @@ def cache_append(prm: AppendParams, k: torch.Tensor, k_cache: torch.Tensor, *, p
             qrs = _tokens("q_rot", q_rot, n, nq, rot, dev, i)
         if q_out is None:
             q_out = q.new_empty((n, nq, d_k))
-        elif not _fits(q_out, _BF16, (n, nq, d_k), i):
+        else:
             _need("q_out", q_out, _BF16, (n, nq, d_k), dev)
     elif q is not None or q_rot is not None or q_out is not None:
         raise ValueError("q, q_rot and q_out must be None with n_heads = 0")
     if rot:
         rope_rows = rope.shape[0] if isinstance(rope, torch.Tensor) and rope.dim() == 2 else None
-        if not _fits(rope, _F32, (rope_rows, rot), i):
-            _need("rope", rope, _F32, (None, rot), dev)
+        _need("rope", rope, _F32, (None, rot), dev)
     elif rope is not None:
         raise ValueError("rope must be None with rot_dim = 0")
     if (pos is None) == (ctx_len is None):
@@ -672,8 +684,7 @@ def cache_append(prm: AppendParams, k: torch.Tensor, k_cache: torch.Tensor, *, p
     max_pages = 1
     if page_table is not None:
         seqs, max_pages = page_table.shape if isinstance(page_table, torch.Tensor) and page_table.dim() == 2 else (None, None)
-        if not _fits(page_table, _I32, (seqs, max_pages), i):
-            _need("page_table", page_table, _I32, (None, None), dev)
+        _need("page_table", page_table, _I32, (None, None), dev)
     else:
         seqs = n_phys if ctx_len is None else ctx_len.shape[0]
     if n_seq is not None and n_seq != seqs:
@@ -681,22 +692,20 @@ def cache_append(prm: AppendParams, k: torch.Tensor, k_cache: torch.Tensor, *, p
             raise ValueError(f"n_seq is {n_seq}, the page table, ctx_len or cache hold {seqs} sequences")
         seqs = n_seq
     if ctx_len is not None:
-        if not _fits(ctx_len, _I32, (seqs,), i):
-            _need("ctx_len", ctx_len, _I32, (seqs,), dev)
+        _need("ctx_len", ctx_len, _I32, (seqs,), dev)
         if seq is not None:
             raise ValueError("seq must be None with ctx_len")
         if n != seqs * rows_per_seq:
             raise ValueError(f"{n} tokens, but {seqs} sequences of rows_per_seq = {rows_per_seq}")
     else:
-        if not _fits(pos, _I32, (n,), i):
-            _need("pos", pos, _I32, (n,), dev)
-        if seq is not None and not _fits(seq, _I32, (n,), i):
+        _need("pos", pos, _I32, (n,), dev)
+        if seq is not None:
             _need("seq", seq, _I32, (n,), dev)
     if rows is True:
         rows = k.new_empty((n,), dtype=torch.int64)
     elif rows is False or rows is None:
         rows = None
-    elif not _fits(rows, _I64, (n,), i):
+    else:
         _need("rows", rows, _I64, (n,), dev)
     at = _address
     t = _APPEND_TENSORS.pack(at(q), at(q_rot), k.data_ptr(), at(k_rot), at(v), qs, qrs, ks, krs, vs, at(rope), rope_rows,
@@ -723,42 +732,42 @@ def decode_attn(prm: DecodeAttnParams, q: torch.Tensor, k_cache: torch.Tensor, v
 
     Caches as cache_append writes them; v_cache None with a latent cache. page_table None: sequence b has
     page b alone."""
+    done = (_serve or _serving()).decode_attn(prm, q, k_cache, v_cache, ctx_len, page_table, rows_per_seq, k_scale, v_scale, out,
+                                              lse, workspace)
+    if done is not None:
+        return done
     H, nk, d_qk, d_v, fp8 = prm.n_heads, prm.n_kv_heads, prm.d_qk, prm.d_v, prm.fp8
     n_rows = q.shape[0] if isinstance(q, torch.Tensor) and q.dim() == 3 else None
-    i = -1 if n_rows is None else q.get_device()
-    if i < 0 or not _fits(q, _BF16, (n_rows, H, d_qk), i):
-        _need("q", q, _BF16, (None, H, d_qk))
+    _need("q", q, _BF16, (n_rows, H, d_qk))
     dev = q.device
-    n_phys, page = _paged_shape("k_cache", k_cache, fp8, nk, d_qk, dev, i)
+    n_phys, page = _paged_shape("k_cache", k_cache, fp8, nk, d_qk, dev)
     if not prm.latent:
-        _paged_like("v_cache", v_cache, fp8, n_phys, nk, page, d_v, dev, i)
+        _paged_like("v_cache", v_cache, fp8, n_phys, nk, page, d_v, dev)
     elif v_cache is not None:
         raise ValueError("v_cache must be None with a latent cache (V is the first d_v columns of k_cache)")
     if fp8:
-        _cache_scale("k_scale", k_scale, n_phys, nk, page, dev, i)
+        _cache_scale("k_scale", k_scale, n_phys, nk, page, dev)
         if not prm.latent:
-            _cache_scale("v_scale", v_scale, n_phys, nk, page, dev, i)
+            _cache_scale("v_scale", v_scale, n_phys, nk, page, dev)
     elif k_scale is not None or v_scale is not None:
         raise ValueError("k_scale and v_scale must be None for bf16 caches")
     n_seq = ctx_len.shape[0] if isinstance(ctx_len, torch.Tensor) and ctx_len.dim() == 1 else None
-    if not _fits(ctx_len, _I32, (n_seq,), i):
-        _need("ctx_len", ctx_len, _I32, (None,), dev)
+    _need("ctx_len", ctx_len, _I32, (None,), dev)
     if n_rows != n_seq * rows_per_seq:
         raise ValueError(f"q has {n_rows} rows, {n_seq} sequences of rows_per_seq = {rows_per_seq} need {n_seq * rows_per_seq}")
     max_pages = 1
     if page_table is not None:
         max_pages = page_table.shape[1] if isinstance(page_table, torch.Tensor) and page_table.dim() == 2 else None
-        if not _fits(page_table, _I32, (n_seq, max_pages), i):
-            _need("page_table", page_table, _I32, (n_seq, None), dev)
+        _need("page_table", page_table, _I32, (n_seq, None), dev)
     if out is None:
         out = q.new_empty((n_rows, H, d_v))
-    elif not _fits(out, _BF16, (n_rows, H, d_v), i):
+    else:
         _need("out", out, _BF16, (n_rows, H, d_v), dev)
     if lse is True:
         lse = q.new_empty((n_rows, H), dtype=torch.float32)
     elif lse is False or lse is None:
         lse = None
-    elif not _fits(lse, _F32, (n_rows, H), i):
+    else:
         _need("lse", lse, _F32, (n_rows, H), dev)
     L, ref = _lib or lib(), _ref(prm)
     wsb = L.lsa_decode_attn_workspace_size(ref, n_seq, rows_per_seq, max_pages, page)
