@@ -90,10 +90,11 @@ constexpr int kLatentPages = 1024; // the same, latent cache
 // among short ones can cost. (The launch of a join costs the host 4 us besides, so the bound leaves up to 2 us to it.)
 // us of whole calls, cut / whole, sequences x positions:
 //   32 heads on 8 key heads (about 0.3 us a tile in a workgroup of 4 waves of its own, 0.23 in one of 8; 100 of them come near
-//     the memory's rate): 1 x 128 7.6 / 5.6, 1 x 500 9.0 / 8.0, 1 x 1001 9.1 / 10.5, 2 x 700 11.4 / 9.2, 3 x 1000 11.0 / 11.6, 4 x
-//     1000 12.0 / 11.7, 4 x 2000 16.4 / 16.7, 8 x 1000 14.2 / 12.0, 8 x 2000 20.7 / 17.4, 16 x 2000 34.9 / 29.4, 64 x 1000 53.8 /
-//     51.2, 256 x 1000 196 / 187; fp8 4 x 1000 10.1 / 10.5, 8 x 2000 18.1 / 16.7; a window of 1024 on 33 x 12 heads 27.6 / 22.7
-//   16 heads on one: 32 x 1000 13.8 / 12.2, 69 x 1200 19.4 / 13.8, 69 x 4000 37.6 / 46.7
+//     the memory's rate): 1 x 128 7.6 / 5.6, 1 x 500 9.4 / 8.0, 1 x 800 9.5 / 9.0, 1 x 1001 9.7 / 10.5, 2 x 700 11.4 / 9.2, 3 x 1001 9.9 / 10.6, 4
+//     x 1001 10.6 / 10.6, 4 x 1150 12.4 / 11.1, 4 x 2000 16.4 / 16.7, 8 x 1000 11.2 / 11.2, 8 x 2000 20.7 / 17.4, 16 x 2000 34.9 / 29.4, 64 x 1000 53.8 /
+//     51.2, 256 x 1000 196 / 187; fp8 1 x 1001 9.5 / 10.4, 4 x 1150 11.9 / 10.6, 8 x 2000 18.1 / 16.7; a window of 1024 on 33 x 12 heads 27.6 / 22.7
+//   12 heads of 64: 1 x 1001 9.7 / 8.1, fp8 9.6 / 8.6, 3 x 1001 9.8 / 8.2, 5 x 1300 12.2 / 9.4, 32 x 1150 24.9 / 20.8
+//   16 heads on one: 1 x 1001 9.9 / 10.6, 32 x 1000 13.8 / 12.2, 69 x 1200 19.4 / 13.8, 69 x 4000 37.6 / 46.7
 //   64 query rows of a key head: 1 x 500 13.6 / 16.2, 32 x 500 16.8 / 16.7, 32 x 1000 19.8 / 24.0, 69 x 1200 32.7 / 27.8, 69 x 2000
 //     35.7 / 38.1, 150 x 2000 56.9 / 47.4
 //   latent, blocks of 64 rows: 8 x 300 17.0 / 16.6, 16 x 500 25.2 / 22.4, 28 x 700 25.4 / 28.3, 64 x 700 32.1 / 29.0, 64 x 1000 33.1 /
