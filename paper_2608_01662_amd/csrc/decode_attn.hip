@@ -84,8 +84,9 @@ template <class F>
 __device__ __forceinline__ void deal(const DecodeGeom& g, int d, F&& segment) {
   const int M = g.M, lane = threadIdx.x & 63;
   const bool cut = g.parts != nullptr;
-  // (together: workgroups i, i + 8, .. run on one XCD, whose L2 then reads the rows that the g.M share once)
-  const int q = g.together ? (int)blockIdx.x >> 3 : (int)blockIdx.x, yq = fdiv(g.by_m, q), r = q - yq * M;
+  // (together: workgroups i, i + 8, .. run on one XCD, whose L2 then reads the rows that the g.M share once. A call that is cut
+  // has few workgroups, all of one launch.)
+  const int q = g.together ? (int)blockIdx.x >> 3 : g.first + (int)blockIdx.x, yq = fdiv(g.by_m, q), r = q - yq * M;
   const int y = g.together ? 8 * yq + ((int)blockIdx.x & 7) : yq;
   auto length = [&](int b) { return b < g.n_seq ? g.ctx_len[b] : 0; };
   int ctx0 = 0, share = 0;
@@ -1107,7 +1108,7 @@ template <int D, int COLS, int S, int T>
 __global__ __launch_bounds__(S * T) void gqa_join_kernel(DecodeGeom g) {
   __shared__ Joined lds[S * T < 64 ? 1 : S * T / 64 * (T < 64 ? T : 64)];
   const int group = (int)g.by_group.d, cols = g.R * group, cb_n = (int)g.by_blocks.d;
-  const int unit = (int)(blockIdx.x / (uint32_t)cols), col = (int)blockIdx.x - unit * cols;  // (sequence, key/value head)
+  const int nth = g.first + (int)blockIdx.x, unit = (int)((uint32_t)nth / (uint32_t)cols), col = nth - unit * cols;  // (sequence, key/value head)
   const int4 p = g.parts[(int64_t)unit * cb_n + col / COLS];
   if (p.x == p.y) return;
   const int d = 4 * (T * (int)blockIdx.y + (int)threadIdx.x % T), cc = col % COLS;
@@ -1125,7 +1126,8 @@ template <int HB, int S, int T>
 __global__ __launch_bounds__(S * T) void latent_join_kernel(DecodeGeom g) {
   static_assert(HB <= 2 && T % 64 == 0, "a wave's threads share their partials");
   __shared__ Joined lds[S * T / 64 * 64];
-  const int4 p = g.parts[blockIdx.x];
+  const int nth = g.first + (int)blockIdx.x;
+  const int4 p = g.parts[nth];
   if (p.x == p.y) return;
   const int vec = T * (int)blockIdx.y + (int)threadIdx.x % T;
   const int lane = vec & 63, q = (vec >> 6) & 3, c = (vec >> 8) & 3, hb = (vec >> 10) & (HB - 1), w4 = vec >> (9 + HB);
@@ -1134,11 +1136,24 @@ __global__ __launch_bounds__(S * T) void latent_join_kernel(DecodeGeom g) {
                            [&](int slot) { return reinterpret_cast<const f32x4*>(g.part_o)[(int64_t)slot * (4096 * HB) + vec]; });
   r = join_threads<S, T>(r, lds);
   if (threadIdx.x >= T) return;
-  const int b = fdiv(g.by_m, (int)blockIdx.x), col = 32 * HB * ((int)blockIdx.x - b * g.M) + lh;
+  const int b = fdiv(g.by_m, nth), col = 32 * HB * (nth - b * g.M) + lh;
   if (col < g.R * g.H) join_store(g, r, (int64_t)b * g.R * g.H + col, 512, d);
 }
 
 // ============================================================================ host launchers
+// Launches n (times y) workgroups, in as many launches as it takes: the runtime counts the threads of a launch's dimension in 32
+// bits, and a launch of more runs the rest modulo 2^32 without an error.
+static hipError_t launch_all(void (*kernel)(DecodeGeom), DecodeGeom g, int64_t n, unsigned y, unsigned threads, hipStream_t st) {
+  const int64_t most = (int64_t(1) << 31) / threads;
+  for (int64_t at = 0; at < n; at += most) {
+    g.first = (int)at;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(n - at < most ? n - at : most), y), dim3(threads), 0, st, g);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 // Calls of few rows, whose rows have many partials, take few dims per workgroup and share the partials among
 // more threads.
 constexpr int64_t kJoinFew = 2048;  // workgroups
@@ -1147,18 +1162,15 @@ static hipError_t launch_gqa(const DecodeGeom& g, hipStream_t st) {
   auto kernel = g.R > 1 ? gqa_decode_kernel<D, FP8, NB, true, 4> : gqa_decode_kernel<D, FP8, NB, false, 4>;
   if constexpr (NB <= 2)
     if (g.waves == 8) kernel = g.R > 1 ? gqa_decode_kernel<D, FP8, NB, true, 8> : gqa_decode_kernel<D, FP8, NB, false, 8>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)g.grid), dim3(64 * (unsigned)g.waves), 0, st, g);
-  hipError_t e = hipGetLastError();
+  const hipError_t e = launch_all(kernel, g, g.grid, 1, 64 * (unsigned)g.waves, st);
   if (e != hipSuccess || g.part_o == nullptr) return e;
   const int64_t rows = (int64_t)g.n_seq * g.R * g.H;
   if (rows * (D / 32) <= kJoinFew) {
     // (at most that many partials of a row, if the sequences are alike)
-    if ((int)g.by_stretches.d / g.n_seq > 32) hipLaunchKernelGGL((gqa_join_kernel<D, 16 * NB, 128, 8>), dim3((unsigned)rows, D / 32), dim3(1024), 0, st, g);
-    else hipLaunchKernelGGL((gqa_join_kernel<D, 16 * NB, 32, 8>), dim3((unsigned)rows, D / 32), dim3(256), 0, st, g);
-  } else {
-    hipLaunchKernelGGL((gqa_join_kernel<D, 16 * NB, 1024 / D, D / 4>), dim3((unsigned)rows), dim3(256), 0, st, g);
+    if ((int)g.by_stretches.d / g.n_seq > 32) return launch_all(gqa_join_kernel<D, 16 * NB, 128, 8>, g, rows, D / 32, 1024, st);
+    return launch_all(gqa_join_kernel<D, 16 * NB, 32, 8>, g, rows, D / 32, 256, st);
   }
-  return hipGetLastError();
+  return launch_all(gqa_join_kernel<D, 16 * NB, 1024 / D, D / 4>, g, rows, 1, 256, st);
 }
 template <int D, bool FP8>
 static hipError_t launch_gqa(const DecodeGeom& g, hipStream_t st) {
@@ -1169,17 +1181,15 @@ static hipError_t launch_gqa(const DecodeGeom& g, hipStream_t st) {
 template <int HB>
 static hipError_t launch_latent(const DecodeGeom& g, hipStream_t st) {
   const auto kernel = g.R > 1 && g.H % (32 * HB) != 0 ? latent_decode_kernel<HB, true> : latent_decode_kernel<HB, false>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)g.grid), dim3(512), 0, st, g);
-  hipError_t e = hipGetLastError();
+  const hipError_t e = launch_all(kernel, g, g.grid, 1, 512, st);
   if (e != hipSuccess || g.part_o == nullptr) return e;
   const int64_t units = (int64_t)g.n_seq * g.M;
   // us with 16 / 4 / 1 threads a vector: 64 heads, 1 x 16K 21.1 / 23.0 / 37.3, 4 x 8000 26.0 / 25.3 / 29.5, 8 x 16K 50.6 / 47.4 /
   // 50.9, 64 x 1500 70.4 / 49.6 / 45.2; 16 heads, 1 x 64K 27.2 / 35.3 / 76.5, 20 x 4000 33.1 / 29.3 / 30.7
   const int64_t few = units * 64 * HB;
-  if (few <= 128) hipLaunchKernelGGL((latent_join_kernel<HB, 16, 64>), dim3((unsigned)units, 64 * HB), dim3(1024), 0, st, g);
-  else if (few <= 2048) hipLaunchKernelGGL((latent_join_kernel<HB, 4, 64>), dim3((unsigned)units, 64 * HB), dim3(256), 0, st, g);
-  else hipLaunchKernelGGL((latent_join_kernel<HB, 1, 256>), dim3((unsigned)units, 16 * HB), dim3(256), 0, st, g);
-  return hipGetLastError();
+  if (few <= 128) return launch_all(latent_join_kernel<HB, 16, 64>, g, units, 64 * HB, 1024, st);
+  if (few <= 2048) return launch_all(latent_join_kernel<HB, 4, 64>, g, units, 64 * HB, 256, st);
+  return launch_all(latent_join_kernel<HB, 1, 256>, g, units, 16 * HB, 256, st);
 }
 
 hipError_t launch_decode_attn(const DecodeGeom& g, hipStream_t st) {

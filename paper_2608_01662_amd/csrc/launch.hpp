@@ -165,6 +165,7 @@ struct DecodeGeom {
   int min_tiles;      // fewest tiles of a workgroup (see least_tiles)
   float *part_o, *part_ml;  // two partials per workgroup: [block_cols, d_v], [block_cols, 2]; nullptr: none is cut
   int4* parts;        // [n_seq, M]: first and last stretch of each, slot of the first one's partial, r
+  int first;          // set by the launcher: first workgroup of the launch (a large call takes several)
 };
 // Tiles that pay for a workgroup in a call of `total` tiles: n workgroups take total / n tiles each and leave n partials
 // to be written and joined, and the sum of both is least at n ~ sqrt(total). In steps of `step` (grouped heads: four
