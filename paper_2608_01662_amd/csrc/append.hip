@@ -209,11 +209,10 @@ hipError_t launch_append(const AppendGeom& all, hipStream_t st) {
   g.by_k_lanes = fast_div((uint32_t)k_lanes);
   g.by_v_lanes = fast_div((uint32_t)v_lanes);
   g.by_page = fast_div((uint32_t)g.P);
-  // a launch of as many tokens as 31 bits count threads for
-  int64_t most = (int64_t)g.H * q_units;
-  if (most < (int64_t)g.Hkv * k_lanes) most = (int64_t)g.Hkv * k_lanes;
-  if (most < (int64_t)g.Hkv * v_lanes) most = (int64_t)g.Hkv * v_lanes;
-  const int64_t tokens = ((int64_t(1) << 31) - 2 * kAppendThreads) / most;
+  // A launch of as many tokens as 31 bits count threads for, those of queries, keys and values together (each part's last
+  // workgroup is not full): the runtime takes a launch of 2^32 threads or more modulo 2^32, without an error.
+  const int64_t each = (int64_t)g.H * q_units + (int64_t)g.Hkv * (k_lanes + (g.d_v ? v_lanes : 0));
+  const int64_t tokens = ((int64_t(1) << 31) - 3 * kAppendThreads) / each;
   auto blocks = [](int64_t items) { return (int)((items + kAppendThreads - 1) / kAppendThreads); };
   for (int64_t t0 = 0; t0 < all.n_tok; t0 += tokens) {
     g.tok0 = (int)t0;
