@@ -225,9 +225,8 @@ hipError_t launch_append(const AppendGeom& all, hipStream_t st) {
     if (all.v) g.v = all.v + t0 * g.v_stride;
     const int bq = g.H ? blocks((int64_t)g.n_tok * (g.H / heads) * q_units) : 0, bk = blocks((int64_t)g.n_tok * g.Hkv * k_lanes);
     const int bv = g.d_v ? blocks((int64_t)g.n_tok * g.Hkv * v_lanes) : 0;
-    hipLaunchKernelGGL(heads == 4 ? append_kernel<4> : append_kernel<1>, dim3((unsigned)bq + (unsigned)bk + (unsigned)bv), dim3(kAppendThreads), 0,
-                       st, g, bq, bk);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = launch_kernel(heads == 4 ? append_kernel<4> : append_kernel<1>, dim3((unsigned)bq + (unsigned)bk + (unsigned)bv),
+                                       dim3(kAppendThreads), st, g, bq, bk);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

@@ -1147,8 +1147,7 @@ static hipError_t launch_all(void (*kernel)(DecodeGeom), DecodeGeom g, int64_t n
   const int64_t most = (int64_t(1) << 31) / threads;
   for (int64_t at = 0; at < n; at += most) {
     g.first = (int)at;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(n - at < most ? n - at : most), y), dim3(threads), 0, st, g);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = launch_kernel(kernel, dim3((unsigned)(n - at < most ? n - at : most), y), dim3(threads), st, g);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

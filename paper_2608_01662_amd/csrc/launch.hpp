@@ -111,6 +111,16 @@ inline FastDiv fast_div(uint32_t d) {
   return FastDiv{d, shift, (uint64_t(1) << shift) / d + 1};
 }
 
+// Launches a kernel and returns the status of this launch. (hipGetLastError would also return, and clear, an error that an
+// earlier call of the thread left, when the kernel has been enqueued all the same.)
+template <class... A>
+inline hipError_t launch_kernel(void (*kernel)(A...), dim3 grid, dim3 block, hipStream_t st, A... args) {
+  void* at[] = {&args...};
+  const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, at, 0, st);
+  if (e != hipSuccess) (void)hipGetLastError();  // reported by the call, not by the thread's next check
+  return e;
+}
+
 // One cache append (lsa_append_tensors, checked).
 struct AppendGeom {
   const uint16_t *q, *q_rot, *k, *k_rot, *v;

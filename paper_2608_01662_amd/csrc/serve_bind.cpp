@@ -3,7 +3,8 @@
 //
 // A decode step's kernels take 3 to 20 us, as long as a host in Python that looks at a dozen tensors, so the
 // checks that a good call passes, its allocations and the call itself are compiled. What is not as it should be is not explained
-// here: the functions return None, also where the library refuses, and lsa.py says why. us of a call that the
+// here: the functions return None, also where the library refuses, and lsa.py says why. An error of the HIP runtime is
+// raised here (by `check`, a function that lsa.py gives this module), since the call may have run in part. us of a call that the
 // host bounds, with the checks in Python and here: append of one token 12.0, 7.4, of which the launch takes 3.2.
 #include <Python.h>
 
@@ -150,9 +151,21 @@ PyObject* pair_of(const at::Tensor* a, const at::Tensor* b) {
   return r;
 }
 
+// What becomes of a call that the library did not do. Refusals come before its first launch and are left to lsa.py; after an
+// error of the runtime nothing is tried again: an append that rotates queries in place would rotate them twice.
+PyObject* not_done(PyObject* module, lsa_status st, const char* call) {
+  if (st != LSA_ERR_HIP) Py_RETURN_NONE;
+  PyObject* r = PyObject_CallMethod(module, "check", "is", (int)st, call);
+  if (r != nullptr) {
+    Py_DECREF(r);
+    PyErr_Format(PyExc_RuntimeError, "%s: status %d", call, (int)st);
+  }
+  return nullptr;
+}
+
 // cache_append(prm, k, k_cache, page_table, ctx_len, pos, seq, rows_per_seq, n_seq, rope, k_rot, v, v_cache, k_scale, v_scale,
 //              q, q_rot, q_out, rows)
-PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+PyObject* cache_append(PyObject* module, PyObject* const* a, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
   if (n_args != 19) Py_RETURN_NONE;
   int32_t p[8], rows_per_seq, max_pages;
@@ -238,13 +251,13 @@ PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     x.rows = at_of<int64_t>(rows);
     st = lsa_cache_append(&prm, &x, n, (int32_t)seqs, rows_per_seq, max_pages, (int32_t)page, n_phys, stream);
   }
-  if (st != LSA_OK) Py_RETURN_NONE;
+  if (st != LSA_OK) return not_done(module, st, "lsa_cache_append");
   return pair_of(q_out, rows);
   END_HANDLE_TH_ERRORS
 }
 
 // decode_attn(prm, q, k_cache, v_cache, ctx_len, page_table, rows_per_seq, k_scale, v_scale, out, lse, workspace)
-PyObject* decode_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+PyObject* decode_attn(PyObject* module, PyObject* const* a, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
   if (n_args != 12) Py_RETURN_NONE;
   int32_t p[8], rows_per_seq, max_pages;
@@ -309,7 +322,7 @@ PyObject* decode_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                          at_of<int32_t>(ctx_len), at_of<int32_t>(table), max_pages, (int32_t)page, n_phys, at_of(out), at_of<float>(lse),
                          at_of(workspace), workspace == nullptr ? 0 : workspace->nbytes(), stream);
   }
-  if (st != LSA_OK) Py_RETURN_NONE;
+  if (st != LSA_OK) return not_done(module, st, "lsa_decode_attn");
   return pair_of(out, lse);
   END_HANDLE_TH_ERRORS
 }
@@ -318,7 +331,7 @@ PyMethodDef methods[] = {
     {"cache_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_append)), METH_FASTCALL, nullptr},
     {"decode_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(decode_attn)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_serve", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef definition = {PyModuleDef_HEAD_INIT, "_serve", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
@@ -332,5 +345,5 @@ PyMODINIT_FUNC PyInit__serve() {
     if ((append_names[i] = PyUnicode_InternFromString(kAppendNames[i])) == nullptr || (attn_names[i] = PyUnicode_InternFromString(kAttnNames[i])) == nullptr)
       return nullptr;
   if ((sm_scale_name = PyUnicode_InternFromString("sm_scale")) == nullptr) return nullptr;
-  return PyModule_Create(&module);
+  return PyModule_Create(&definition);
 }

@@ -556,7 +556,7 @@ def hfa_attn(prm: AttnParams, q: torch.Tensor, kv: torch.Tensor, idx: torch.Tens
 # ---------------------------------------------------------------- serving: appends and dense decode
 # These calls' kernels take a few microseconds at small batches, less than a host that looks at every tensor from
 # Python. So good calls are checked, given their outputs and launched by a compiled module (csrc/serve_bind.cpp),
-# which returns None for any other, and the checks below say why.
+# which returns None for any other, and the checks below say why. Errors of a launch it raises itself.
 _serve = None
 
 
@@ -570,6 +570,7 @@ def _serving():
         spec = importlib.util.spec_from_file_location(f"{__package__}._serve", SERVE_PATH)
         _serve = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(_serve)
+        _serve.check = _check   # what raises the errors of a launch
     return _serve
 
 
