@@ -313,7 +313,7 @@ void gqa_decode_kernel(DecodeGeom g) {
       int f1 = 0, n1 = 0, f2 = 0, n2 = 0;  // first page and pages of both parts
       if (p0 < e1) {
         f1 = fdiv(g.by_page, p0 * kTile);
-        const int last = e1 * kTile - 1 < sp.c ? e1 * kTile - 1 : sp.c - 1;
+        const int last = e1 <= (sp.c - 1) / kTile ? e1 * kTile - 1 : sp.c - 1;  // (e1 * kTile may be 2^31)
         n1 = fdiv(g.by_page, last) - f1 + 1;
       }
       if (b2 < p1) {
@@ -461,7 +461,7 @@ void gqa_decode_kernel(DecodeGeom g) {
           if (more) issue_k(st, w);
           const int s0 = tile_pos(i);
           // several new tokens: does the tile reach to where they see different positions?
-          const bool uneven = MULTI && uniform((s0 + kTile > sp.c - g.R + 1 || (g.k_swa > 0 && s0 < sp.c - g.k_swa)));
+          const bool uneven = MULTI && uniform((s0 > sp.c - g.R + 1 - kTile || (g.k_swa > 0 && s0 < sp.c - g.k_swa)));
           if (bits != ~0u || uneven) {
             const int t8 = s0 + 8 * q4;  // this lane's first token
 #pragma unroll
@@ -651,8 +651,8 @@ void latent_decode_kernel(DecodeGeom g) {
     const int64_t row0 = (int64_t)b * g.R * g.H + col0;  // output row of column 0
     auto token_of = [&](int col) { return MULTI ? sp.c - g.R + fdiv(g.by_group, col0 + (col < ncols ? col : 0)) : tq0; };
     auto sees = [&](int s, int t) { return s <= t && (g.k_swa == 0 || t - s < g.k_swa || s < g.k_sink); };
-    // several new tokens: does a tile from position s0 on reach to where they see different positions?
-    auto uneven = [&](int s0) { return MULTI && uniform(tq0 != tq1 && (s0 + kTile > tq0 + 1 || (g.k_swa > 0 && s0 <= tq1 - g.k_swa))); };
+    // several new tokens: does a tile from position s0 on reach to where they see different positions? (s0 + kTile may be 2^31)
+    auto uneven = [&](int s0) { return MULTI && uniform(tq0 != tq1 && (s0 > tq0 + 1 - kTile || (g.k_swa > 0 && s0 <= tq1 - g.k_swa))); };
     auto first_pos = [&](int t) { return (t < sp.ns ? t : t + sp.skip) * kTile; };
     // page-table entries of tiles [p0, p1): those before the skipped ones, then the others
     int f1 = 0, n1 = 0, f2 = 0;
@@ -662,7 +662,7 @@ void latent_decode_kernel(DecodeGeom g) {
       f1 = n1 = f2 = 0;
       if (p0 < e1) {
         f1 = fdiv(g.by_page, p0 * kTile);
-        const int last = e1 * kTile - 1 < sp.c ? e1 * kTile - 1 : sp.c - 1;
+        const int last = e1 <= (sp.c - 1) / kTile ? e1 * kTile - 1 : sp.c - 1;  // (e1 * kTile may be 2^31)
         n1 = fdiv(g.by_page, last) - f1 + 1;
       }
       if (b2 < p1) {
@@ -1007,7 +1007,7 @@ void latent_decode_kernel(DecodeGeom g) {
       for (int t = t0; t < t1; ++t) {
         const int s0 = first_pos(t);
         if (!uneven(s0)) continue;
-        for (int s = s0; s < s0 + kTile && s <= tq1; ++s) {
+        for (int s = s0; s - s0 < kTile && s <= tq1; ++s) {
           const int pg = fdiv(g.by_page, s), ph = g.page_table ? g.page_table[(int64_t)b * g.max_pages + pg] : b;
           if (ph < 0 || ph >= g.n_phys) continue;
           const uint16_t* v = reinterpret_cast<const uint16_t*>(kvb + ((int64_t)ph * g.P + (s - pg * g.P)) * 1152) + 128 * w4;
