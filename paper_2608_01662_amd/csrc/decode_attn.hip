@@ -52,6 +52,16 @@ __device__ __forceinline__ float exp2_below(float s, float scale, float m) {
   return fast_exp2(z - m);
 }
 
+// Values over the sum of their weights, 0 where there are none or all are 0 (every score -inf). Selected, since 0 times what a
+// value of a weight of 0 left (a NaN or an infinity times 0) is NaN.
+__device__ __forceinline__ f32x4 average(f32x4 acc, float sum) {
+  const float inv = 1.f / sum;
+  f32x4 y;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) y[k] = sum == 0.f ? 0.f : acc[k] * inv;
+  return y;
+}
+
 // Inclusive sum over the lanes of a wave.
 __device__ __forceinline__ int wave_scan(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr 1, 2, 4, 8: within rows of 16
@@ -594,8 +604,8 @@ void gqa_decode_kernel(DecodeGeom g) {
       if (whole) {
         const int at = col0 + col, j = fdiv(g.by_group, at);
         const int64_t row = ((int64_t)b * g.R + j) * g.H + kvh * group + at - j * group;
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        *reinterpret_cast<u32x2*>(g.out + row * D + d) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+        const f32x4 y = average(acc, sum);
+        *reinterpret_cast<u32x2*>(g.out + row * D + d) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
         if (g.lse && d == 0) g.lse[row] = sum == 0.f ? -INFINITY : (mx + __log2f(sum)) * kLn2;
       } else {
         const int64_t pc = (int64_t)slot * COLS + col;
@@ -977,14 +987,13 @@ void latent_decode_kernel(DecodeGeom g) {
       uint8_t* ost = lds + w4 * (64 * 272);
 #pragma unroll
       for (int hb = 0; hb < HB; ++hb) {
-        const float inv = lt[hb] == 0.f ? 0.f : 1.f / lt[hb];
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const f32x16& ob = o[4 * hb + c];
-            *reinterpret_cast<u32x2*>(ost + (32 * hb + ej) * 272 + (32 * c + 8 * q + 4 * (el >> 5)) * 2) =
-                u32x2{pack_bf16x2(ob[4 * q] * inv, ob[4 * q + 1] * inv), pack_bf16x2(ob[4 * q + 2] * inv, ob[4 * q + 3] * inv)};
+            const f32x4 y = average(f32x4{ob[4 * q], ob[4 * q + 1], ob[4 * q + 2], ob[4 * q + 3]}, lt[hb]);
+            *reinterpret_cast<u32x2*>(ost + (32 * hb + ej) * 272 + (32 * c + 8 * q + 4 * (el >> 5)) * 2) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
           }
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (this wave's own writes)
@@ -1002,7 +1011,8 @@ void latent_decode_kernel(DecodeGeom g) {
         for (int q = 0; q < 4; ++q) dst[(4 * c + q) * 64] = f32x4{o[c][4 * q], o[c][4 * q + 1], o[c][4 * q + 2], o[c][4 * q + 3]};
     }
     // (A value that is no number or infinite is part of K too: a column that sees it has a score that is none or infinite, so
-    // that all its output is NaN already unless the score is -inf, whose weight of 0 times the value is NaN.)
+    // that all its output is NaN already unless the score is -inf, whose weight of 0 times the value is NaN. Columns of no other
+    // score stay 0; a partial's may have other scores elsewhere.)
     if (MULTI && marred) {
       for (int t = t0; t < t1; ++t) {
         const int s0 = first_pos(t);
@@ -1015,6 +1025,7 @@ void latent_decode_kernel(DecodeGeom g) {
             if ((v[d] & 0x7F80u) != 0x7F80u) continue;
             for (int col = 0; col < ncols; ++col) {
               if (!sees(s, token_of(col))) continue;
+              if (whole && fin[2 * col + 1] == 0.f && fin[2 * (COLS + col) + 1] == 0.f) continue;
               if (whole) g.out[(row0 + col) * 512 + 128 * w4 + d] = 0x7FC0;
               else g.part_o[(((int64_t)slot * 16 * HB + w4 * 4 * HB + 4 * (col / 32) + d / 32) * 4 + (d / 8) % 4) * 256 + (col % 32 + 32 * ((d / 4) % 2)) * 4 + d % 4] = __builtin_nanf("");
             }
@@ -1098,8 +1109,8 @@ __device__ __forceinline__ Joined join_threads(Joined r, Joined* lds) {
   return r;
 }
 __device__ __forceinline__ void join_store(const DecodeGeom& g, const Joined& r, int64_t row, int width, int d) {
-  const float inv = r.l == 0.f ? 0.f : 1.f / r.l;
-  *reinterpret_cast<u32x2*>(g.out + row * width + d) = u32x2{pack_bf16x2(r.acc[0] * inv, r.acc[1] * inv), pack_bf16x2(r.acc[2] * inv, r.acc[3] * inv)};
+  const f32x4 y = average(r.acc, r.l);
+  *reinterpret_cast<u32x2*>(g.out + row * width + d) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
   if (g.lse && d == 0) g.lse[row] = r.l == 0.f ? -INFINITY : (r.m + __log2f(r.l)) * kLn2;
 }
 
