@@ -15,7 +15,8 @@
  *   - Tensor pointers are DEVICE pointers owned by the caller, row-major and contiguous, each
  *     aligned to 16 bytes. No call allocates device memory, frees anything, or synchronises the
  *     host: work is enqueued on `stream` (a hipStream_t; NULL = the default stream) and the
- *     caller orders it like any other kernel launch.
+ *     caller orders it like any other kernel launch. The GPU of the tensors and the stream is the calling
+ *     thread's current one (hipSetDevice).
  *   - Positions are 0-based token positions (the paper counts from 1). The query at absolute
  *     position t may see positions 0..t. Sink = [0, k_sink), window = [t-k_swa+1, t], eligible
  *     range E_t = [k_sink, t-k_swa].

@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -233,6 +234,7 @@ PyObject* cache_append(PyObject* module, PyObject* const* a, Py_ssize_t n_args) 
   x.k = at_of(k);
   x.page_table = at_of<int32_t>(table);
   x.ctx_len = at_of<int32_t>(ctx_len);
+  const c10::DeviceGuard guard(c10::Device(c10::kCUDA, ts.device));  // (stream 0 is that of whichever GPU is current)
   void* stream;
   if (!stream_of(ts.device, stream)) return nullptr;
   lsa_status st;
@@ -297,6 +299,7 @@ PyObject* decode_attn(PyObject* module, PyObject* const* a, Py_ssize_t n_args) {
   const at::Tensor* workspace = ts.get(a[11]);
   ts.need(workspace == nullptr || workspace->is_contiguous());
   if (!ts.ok) Py_RETURN_NONE;
+  const c10::DeviceGuard guard(c10::Device(c10::kCUDA, ts.device));  // (stream 0 is that of whichever GPU is current)
   void* stream;
   if (!stream_of(ts.device, stream)) return nullptr;
   lsa_status st;

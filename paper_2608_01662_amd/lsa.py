@@ -556,7 +556,8 @@ def hfa_attn(prm: AttnParams, q: torch.Tensor, kv: torch.Tensor, idx: torch.Tens
 # ---------------------------------------------------------------- serving: appends and dense decode
 # These calls' kernels take a few microseconds at small batches, less than a host that looks at every tensor from
 # Python. So good calls are checked, given their outputs and launched by a compiled module (csrc/serve_bind.cpp),
-# which returns None for any other, and the checks below say why. Errors of a launch it raises itself.
+# which returns None for any other, and the checks below say why. Errors of a launch it raises itself. Both make the
+# tensors' GPU the current one for the call; the calls above are made with it current.
 _serve = None
 
 
@@ -712,7 +713,8 @@ def cache_append(prm: AppendParams, k: torch.Tensor, k_cache: torch.Tensor, *, p
     t = _APPEND_TENSORS.pack(at(q), at(q_rot), k.data_ptr(), at(k_rot), at(v), qs, qrs, ks, krs, vs, at(rope), rope_rows,
                              at(seq), at(pos), at(ctx_len), at(page_table), at(q_out), k_cache.data_ptr(), at(k_scale),
                              at(v_cache), at(v_scale), at(rows))
-    st = (_lib or lib()).lsa_cache_append(_ref(prm), t, n, seqs, rows_per_seq, max_pages, page, n_phys, _stream(dev))
+    with torch.cuda.device(dev):
+        st = (_lib or lib()).lsa_cache_append(_ref(prm), t, n, seqs, rows_per_seq, max_pages, page, n_phys, _stream(dev))
     if st != 0:
         _check(st, "lsa_cache_append")
     return q_out, rows
@@ -778,9 +780,10 @@ def decode_attn(prm: DecodeAttnParams, q: torch.Tensor, k_cache: torch.Tensor, v
         workspace, wsb = _workspace(wsb, dev, workspace)
     else:
         workspace = None
-    st = L.lsa_decode_attn(ref, n_seq, rows_per_seq, q.data_ptr(), k_cache.data_ptr(), _p(k_scale), _p(v_cache),
-                           _p(v_scale), ctx_len.data_ptr(), _p(page_table), max_pages, page, n_phys, out.data_ptr(),
-                           _p(lse), _p(workspace), wsb, _stream(dev))
+    with torch.cuda.device(dev):
+        st = L.lsa_decode_attn(ref, n_seq, rows_per_seq, q.data_ptr(), k_cache.data_ptr(), _p(k_scale), _p(v_cache),
+                               _p(v_scale), ctx_len.data_ptr(), _p(page_table), max_pages, page, n_phys, out.data_ptr(),
+                               _p(lse), _p(workspace), wsb, _stream(dev))
     if st != 0:
         _check(st, "lsa_decode_attn")
     return out, lse
