@@ -86,34 +86,33 @@ constexpr int kPageSlots = 2048;   // page-table entries a workgroup stages at a
 constexpr int kLatentPages = 1024; // the same, latent cache
 
 // A (sequence, head, query row block) of at most that many tiles is left whole: a workgroup each, no scan of the lengths, no
-// partials and no join. What the host knows is the tables' capacity, so the bound also limits what one long sequence
-// among short ones can cost. (The launch of a join costs the host 4 us besides, so the bound leaves up to 2 us to it.)
-// us of whole calls, cut / whole, sequences x positions:
-//   32 heads on 8 key heads (about 0.3 us a tile in a workgroup of 4 waves of its own, 0.23 in one of 8; 100 of them come near
-//     the memory's rate): 1 x 128 7.6 / 5.6, 1 x 500 9.4 / 8.0, 1 x 800 9.5 / 9.0, 1 x 1001 9.7 / 10.5, 2 x 700 11.4 / 9.2, 3 x 1001 9.9 / 10.6, 4
-//     x 1001 10.6 / 10.6, 4 x 1150 12.4 / 11.1, 4 x 2000 16.4 / 16.7, 8 x 1000 11.2 / 11.2, 8 x 2000 20.7 / 17.4, 16 x 2000 34.9 / 29.4, 64 x 1000 53.8 /
-//     51.2, 256 x 1000 196 / 187; fp8 1 x 1001 9.5 / 10.4, 4 x 1150 11.9 / 10.6, 8 x 2000 18.1 / 16.7; a window of 1024 on 33 x 12 heads 27.6 / 22.7
-//   12 heads of 64: 1 x 1001 9.7 / 8.1, fp8 9.6 / 8.6, 3 x 1001 9.8 / 8.2, 5 x 1300 12.2 / 9.4, 32 x 1150 24.9 / 20.8
-//   16 heads on one: 1 x 1001 9.9 / 10.6, 32 x 1000 13.8 / 12.2, 69 x 1200 19.4 / 13.8, 69 x 4000 37.6 / 46.7
-//   64 query rows of a key head: 1 x 500 13.6 / 16.2, 32 x 500 16.8 / 16.7, 32 x 1000 19.8 / 24.0, 69 x 1200 32.7 / 27.8, 69 x 2000
-//     35.7 / 38.1, 150 x 2000 56.9 / 47.4
-//   latent, blocks of 64 rows: 8 x 300 17.0 / 16.6, 16 x 500 25.2 / 22.4, 28 x 700 25.4 / 28.3, 64 x 700 32.1 / 29.0, 64 x 1000 33.1 /
-//     38.6, 128 x 1300 66 / 50, 300 x 1300 137 / 122
-//   latent, blocks of 32: 64 heads (two blocks) 1 x 200 10.6 / 10.6, 1 x 400 10.8 / 15.0, 4 x 300 13.5 / 12.8, 8 x 300 14.8 / 12.9, 16
-//     x 500 21.7 / 19.2, 28 x 700 23.4 / 24.4, 64 x 700 30.2 / 25.3, 64 x 1000 30.8 / 32.9; 16 heads 4 x 300 10.3 / 12.7, 8 x 300
-//     11.1 / 12.8, 16 x 500 14.7 / 18.0, 28 x 700 21.1 / 23.8, 64 x 700 23.7 / 24.3, 64 x 1000 26.3 / 32.0, 128 x 1300 54.5 / 45.5,
-//     128 x 2000 73.3 / 65.2, 190 x 1000 61.7 / 44.9
+// partials and no join. What the host knows is the tables' capacity, so the bound, at most 64 tiles, also limits what one long
+// sequence among short ones can cost. It follows the kernels' time (a cut call costs the host 3 us more, for its second launch; a
+// graph of the step has neither): with few workgroups a whole one is faster for as many tiles as scan, partials and join are
+// worth, `base`, more where stretches of several sequences end inside them, and the more workgroups there are, the fewer can a
+// cut call add. us on the GPU, cut / whole, at capacities around so many tiles, the lengths 0.6 to 1 of them:
+//   lone: 16 rows of 128, 1 head 20 9.2 / 8.9, 24 9.3 / 9.4, 32 9.4 / 11.7; 8 heads 20 9.0 / 8.7, 24 9.0 / 9.2, 32 10.5 / 11.7; fp8 20 8.8 / 8.5, 24 8.6 /
+//     9.2; 32 rows 16 11.1 / 11.0, 24 11.1 / 12.2; 64 wide, 12 heads 28 8.7 / 8.3, 36 8.4 / 8.9; 32 rows 24 8.9 / 8.7, 28 8.8 / 9.8; 33 to 64 rows 8 13.8 /
+//     13.1, 12 13.7 / 15.4, 64 wide 12 10.6 / 10.7; latent 4 10.4 / 9.2, 8 10.5 / 11.2
+//   16 rows of 128, sequences x heads: 2 x 8 28 12.8 / 11.4, 32 11.8 / 11.9, 46 13.1 / 14.1; 4 x 8 40 14.8 / 13.3, 52 15.4 / 15.4; 8 x 8 46 19.2 / 18.5, 52 20.0 /
+//     21.4; 8 x 1 46 14.0 / 14.0; 32 x 1 64 17.9 / 17.9; 12 x 8 52 25.5 / 24.6, 58 26.9 / 26.2; 96 x 1 64 32.5 / 29.8; fp8 8 x 8 64 17.2 / 17.3
+//   32 rows: 8 x 1 40 17.6 / 16.4, 52 17.7 / 18.7; 64 x 1 58 28.1 / 25.9; 64 wide: 2 x 4 36 8.8 / 8.9; 4 x 4 46 10.9 / 11.1; 8 x 4 58 12.8 / 12.7; 32 x 1 64 15.7 / 15.3
+//   33 to 64 rows: 4 x 1 28 21.9 / 23.6; 32 x 1 32 24.7 / 25.2; 64 x 1 46 34.8 / 33.4, 52 36.0 / 37.0; 96 x 1 52 42.1 / 38.6; 64 wide 4 x 1 24 15.2 / 14.4; 32 x 1 32 18.5 /
+//     18.6; 64 x 1 46 24.1 / 23.5; two new tokens 4 x 2 24 25.7 / 25.5; 16 x 2 24 26.8 / 26.3; 32 x 2 32 33.4 / 33.4; 48 x 2 46 44.6 / 44.5; 64 x 2 52 51.1 / 50.1
+//   latent, one block: 4 8 12.1 / 11.3, 12 13.0 / 15.0; 16 12 15.7 / 15.6; 28 16 17.6 / 18.8; 64 20 24.1 / 22.1, 24 25.6 / 24.7, 28 27.8 / 29.3; 80 28 31.4 / 30.8, 32
+//     33.1 / 33.8; 96 32 36.4 / 35.4, 40 41.5 / 42.7; 112 46 49.9 / 45.3, 64 61.4 / 60.2; 128 64 66.6 / 61.5; two blocks: 4 8 13.7 / 11.6, 12 14.4 / 15.3; 32 20 22.9 /
+//     22.4; 64 28 32.9 / 31.1, 36 35.3 / 36.8; blocks of 64: 8 12 19.2 / 19.2; 28 20 25.5 / 26.4; 64 28 36.4 / 37.1; 97 46 57.0 / 54.3, 64 68.9 / 71.9; 128 64 81.5 / 74.8
 int64_t whole_tiles(const lsa_decode_attn_params* p, int block_cols, int64_t n_seq, int64_t pairs) {
-  if (p->latent && block_cols == 32) {
-    const int64_t t = pairs <= 16 ? 4 + pairs / 2 : 8 + pairs / 4;
-    return n_seq >= 96 ? 64 : t < 28 ? t : 28;
+  const bool lone = n_seq == 1;
+  int64_t t;
+  if (p->latent) {  // (the two blocks of 32 rows of a sequence share its rows of the cache and count as one workgroup)
+    const int64_t n = pairs / 2 > n_seq ? pairs / 2 : n_seq;
+    t = (lone ? 6 : 9) + n / 4 + (n > 80 ? (n - 80) * 2 / 3 : 0);
+  } else {
+    const int64_t base = block_cols == 64 ? (lone ? 10 : 22) : !lone ? 36 : p->d_qk == 128 ? 22 : 28;
+    t = base + pairs / 3;
   }
-  if (p->latent) {
-    const int64_t t = pairs <= 16 ? 4 + pairs * 3 / 4 : 12 + pairs / 4;
-    return t < 48 ? t : 48;
-  }
-  const int64_t t = block_cols <= 32 ? 16 + pairs * 3 / 4 : pairs * 3 / 4, least = block_cols <= 32 ? 32 : 8;
-  return t < least ? least : t < 64 ? t : 64;
+  return t < 64 ? t : 64;
 }
 
 DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq, int32_t max_pages,

@@ -25,7 +25,7 @@ def _holes(x, ctx, first, every):
 def test_grouped_heads_whole(form, R, sink, swa):
     """64 tiles in a workgroup, two passes; with a window, tiles of the sink and of the window in one of them."""
     prm = _params(*form, k_sink=sink, k_swa=swa)
-    ctx = [2048, 2047, 1, 0, 2020, 1999, 2017, 33] if not swa else [2918, 2048, 1, 0, 2020, 1999, 3500, 33]
+    ctx = [2048, 2047, 1, 0, 2020, 1999, 2017, 33, 500] if not swa else [2918, 2048, 1, 0, 2020, 1999, 3500, 33, 500]
     x = _batch(prm, ctx, R, 1, seed=31 + R)
     _holes(x, ctx, 2011, 7)
     assert x["table"].shape[1] > 63 * 32 and lsa.decode_attn_workspace_size(prm, len(ctx), R, x["table"].shape[1], 1) == 0
