@@ -166,6 +166,7 @@ struct DecodeGeom {
   FastDiv by_group;   // division by H / Hkv
   FastDiv by_blocks;  // by the blocks of block_cols of a head's query rows
   int M;              // such blocks of a sequence (of all heads)
+  int first;          // set by the launcher: first workgroup of the launch, a large call takes several (read first, with M)
   FastDiv by_m;       // by M
   int grid;           // workgroups
   FastDiv by_stretches;  // division by the stretches the tiles are dealt in (grid = stretches * M)
@@ -175,7 +176,6 @@ struct DecodeGeom {
   int min_tiles;      // fewest tiles of a workgroup (see least_tiles)
   float *part_o, *part_ml;  // two partials per workgroup: [block_cols, d_v], [block_cols, 2]; nullptr: none is cut
   int4* parts;        // [n_seq, M]: first and last stretch of each, slot of the first one's partial, r
-  int first;          // set by the launcher: first workgroup of the launch (a large call takes several)
 };
 // Tiles that pay for a workgroup in a call of `total` tiles: n workgroups take total / n tiles each and leave n partials
 // to be written and joined, and the sum of both is least at n ~ sqrt(total). In steps of `step` (grouped heads: four
