@@ -17,8 +17,6 @@ namespace lsa {
 
 constexpr int kAppendThreads = 256;
 
-__device__ __forceinline__ int fdiv(const FastDiv& f, int n) { return (int)(((uint64_t)(uint32_t)n * f.mul) >> f.shift); }
-
 // What token t of this launch is: its sequence and position (pos < 0: none).
 struct AppendToken {
   int seq, pos;
@@ -198,6 +196,10 @@ static int append_lanes(int units, bool fp8) {
   return l;
 }
 
+// Units of queries from which a thread takes four heads: their position, row and angles are found once, for a quarter of the
+// threads. us of one / four heads a thread: 32 heads of 128, bf16, 64 tokens (2^14 units) 3.4 / 3.8, 512 4.9 / 4.9, 1024 7.5 / 7.2, 4096 19.4 / 18.5, 8192 39.3 /
+// 39.6; with one fp8 indexer key 256 4.1 / 4.0, 1024 6.9 / 6.0, 4096 14.6 / 13.7; 8 heads of 64 2048 (2^16) 4.7 / 5.2, 4096 7.2 / 7.6, 8192 (2^18) 11.7 / 11.4;
+// latent, 64 heads, 64 (2^17) 4.7 / 4.5, 256 10.4 / 10.7, 512 15.9 / 15.1.
 constexpr int64_t kManyUnits = 1 << 18;
 hipError_t launch_append(const AppendGeom& all, hipStream_t st) {
   AppendGeom g = all;

@@ -19,8 +19,6 @@ constexpr int kTile = 32;  // positions of a tile
 // since a weight of zero does not silence a NaN or an infinity in V.
 __device__ __attribute__((aligned(256))) const uint8_t zero_row[1152] = {};
 
-__device__ __forceinline__ int fdiv(const FastDiv& f, int n) { return (int)(((uint64_t)(uint32_t)n * f.mul) >> f.shift); }
-
 // The tiles of a sequence that any of its new tokens attends to: 0 .. ns - 1 (the sink) and then ns + skip ..
 struct Span {
   int c;         // cached positions, 0 where the length is out of range

@@ -110,6 +110,7 @@ inline FastDiv fast_div(uint32_t d) {
   const uint32_t shift = 31 + l;
   return FastDiv{d, shift, (uint64_t(1) << shift) / d + 1};
 }
+__host__ __device__ inline int fdiv(const FastDiv& f, int n) { return (int)(((uint64_t)(uint32_t)n * f.mul) >> f.shift); }
 
 // Launches a kernel and returns the status of this launch. (hipGetLastError would also return, and clear, an error that an
 // earlier call of the thread left, when the kernel has been enqueued all the same.)
