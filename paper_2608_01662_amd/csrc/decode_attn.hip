@@ -502,6 +502,10 @@ void gqa_decode_kernel(DecodeGeom g) {
               l[nb] += p[k];
               if constexpr (FP8) p[k] = z[nb][k] == -INFINITY ? 0.f : p[k] * vs[k];  // (masked: also from a NaN scale)
             }
+            // The weights' one rounding, to the 8 significant bits that a matrix product with bf16 takes (V's codes and values are
+            // exact there; an fp8 row's scale goes into the weight before it). The sum above takes them unrounded. Against 64 bits
+            // the output is off by 2.2e-3 to 2.4e-3 of its norm, 1.7e-3 of which are its own rounding to bf16; weights in two bf16
+            // terms would bring it to that, for twice the value products.
             pb[nb] = u32x4{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])};
           }
           // V of tile i has landed: behind it are the other stages' tiles and the K just requested
@@ -797,6 +801,7 @@ void latent_decode_kernel(DecodeGeom g) {
               l[nb] += p[k];
             }
             const int lh = 16 * (HB * pair + nb) + i16;
+            // (rounded to bf16, what the value products take, which also halves the slot; the sums take them unrounded)
             *reinterpret_cast<u32x2*>(ps + lh * kMlaPHead + 32 * th + 8 * q4) = u32x2{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])};
             if (q4 == 0) *reinterpret_cast<float*>(ps + 64 * kMlaPHead + th * 256 + 4 * lh) = m[nb];
           }
@@ -940,6 +945,8 @@ void latent_decode_kernel(DecodeGeom g) {
 #pragma unroll
               for (int c = 0; c < 4; ++c) o[4 * hb + c] *= alpha;
             }
+            // (a half whose reference is lower: its weights are scaled and rounded to bf16 once more, which leaves them within 2^-8;
+            // from the next tile on both halves have one reference)
             const float fa = mA[hb] == mn ? 1.f : fast_exp2(mA[hb] - mn), fb = mB[hb] == mn ? 1.f : fast_exp2(mB[hb] - mn);
             if (__ballot(fa != 1.f)) pb[hb][0] = scale_bf16x8(pb[hb][0], fa);
             if (__ballot(fb != 1.f)) pb[hb][1] = scale_bf16x8(pb[hb][1], fb);
