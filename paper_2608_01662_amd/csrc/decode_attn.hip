@@ -214,9 +214,11 @@ __device__ __forceinline__ u32x2 tr8(const uint8_t* p) {
 //
 // Bound by HBM: 64 sequences of up to 16K, 32 heads on 8 in bf16 (mean 2.1 GB) 372 us, 5.8 TB/s; 48 of 4K to 32K in fp8, two
 // new tokens each (1.9 GB) 337 us, 5.5 TB/s; 33 windows of 1024, 12 heads of 64, pages of 20 (104 MB) 22 us; one
-// sequence of 128K, 16 heads on one (67 MB) 21 us, of which the join 5; one of 1001, 32 on 8, 10.5 us, all latency. Two waves per
+// sequence of 128K, 16 heads on one (67 MB) 21 us, of which the join 5; one of 1001, 32 on 8, 9.0 us, all latency. Two waves per
 // SIMD hide one's softmax behind the other's products: one wave took 402 and 400 us in place of the first two's 356 and 306 at
-// that time. 33 to 64 query rows per key head need the registers of one wave per SIMD and are bound by its issue.
+// that time. 33 to 64 query rows per key head need the registers of one wave per SIMD: 64 heads on one, 64 x 16K (537 MB) 115 us, 4.7
+// TB/s, but in fp8 97 us, 2.9 TB/s, bound by that wave's issue, as are chunks of new tokens (512 on 16 x 8K, 32 heads on 8, 2.9 ms, 374
+// TFLOP/s), which walk the cache once per 64 query rows.
 //
 // The rows of the products are query rows: the heads of the group of all new tokens, in blocks of 16 (NB
 // blocks per wave); S^T = K Q^T on 16x16x32 products with tokens on the rows, in an order that gives lane
