@@ -9,7 +9,6 @@ from __future__ import annotations
 import ctypes
 import importlib.util
 import os
-import struct
 from dataclasses import dataclass
 
 import torch
@@ -51,10 +50,6 @@ class _AppendTensors(ctypes.Structure):
                [("rope", ctypes.c_void_p), ("rope_rows", ctypes.c_int64)] + \
                [(n, ctypes.c_void_p) for n in ("seq", "pos", "ctx_len", "page_table", "q_out", "k_cache", "k_scale",
                                                "v_cache", "v_scale", "rows")]
-
-
-_APPEND_TENSORS = struct.Struct("5P5qPq10P")   # the layout of _AppendTensors, packed in a quarter of its time
-assert _APPEND_TENSORS.size == ctypes.sizeof(_AppendTensors)
 
 
 class _DecodeAttnParams(ctypes.Structure):
@@ -578,10 +573,6 @@ def _serving():
 _FP8 = (torch.uint8, torch.float8_e4m3fn)
 
 
-def _address(t) -> int:
-    return 0 if t is None else t.data_ptr()
-
-
 def _tokens(name: str, t, n_tok, heads: int, width: int, device, index: int) -> int:
     """A bf16 tensor [n_tok, heads, width] whose tokens may lie any stride apart (a slice of a fused
     projection), their heads one after the other. Returns that stride in elements."""
@@ -709,12 +700,12 @@ def cache_append(prm: AppendParams, k: torch.Tensor, k_cache: torch.Tensor, *, p
         rows = None
     else:
         _need("rows", rows, _I64, (n,), dev)
-    at = _address
-    t = _APPEND_TENSORS.pack(at(q), at(q_rot), k.data_ptr(), at(k_rot), at(v), qs, qrs, ks, krs, vs, at(rope), rope_rows,
-                             at(seq), at(pos), at(ctx_len), at(page_table), at(q_out), k_cache.data_ptr(), at(k_scale),
-                             at(v_cache), at(v_scale), at(rows))
+    at = _p
+    t = _AppendTensors(at(q), at(q_rot), k.data_ptr(), at(k_rot), at(v), qs, qrs, ks, krs, vs, at(rope), rope_rows,
+                       at(seq), at(pos), at(ctx_len), at(page_table), at(q_out), k_cache.data_ptr(), at(k_scale),
+                       at(v_cache), at(v_scale), at(rows))
     with torch.cuda.device(dev):
-        st = (_lib or lib()).lsa_cache_append(_ref(prm), t, n, seqs, rows_per_seq, max_pages, page, n_phys, _stream(dev))
+        st = (_lib or lib()).lsa_cache_append(_ref(prm), ctypes.byref(t), n, seqs, rows_per_seq, max_pages, page, n_phys, _stream(dev))
     if st != 0:
         _check(st, "lsa_cache_append")
     return q_out, rows
