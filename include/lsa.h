@@ -353,7 +353,8 @@ typedef struct lsa_append_tensors {
  * A token is skipped (nothing is cached, rows = -1) when its sequence is outside [0, n_seq), its position
  * is negative, beyond max_pages * P or (with a rotation) beyond rope_rows, or its page-table entry is
  * outside [0, n_phys). The queries of a token without a valid sequence and position are zeros. Two tokens
- * of one call must not share a sequence and position.
+ * of one call must not share a sequence and position. LSA_ERR_HIP, here and from lsa_decode_attn, is an error of
+ * the call's own launches, some of which may have been made (very large calls take several).
  */
 lsa_status lsa_cache_append(const lsa_append_params* p, const lsa_append_tensors* t, int64_t n_tok,
                             int32_t n_seq, int32_t rows_per_seq, int32_t max_pages, int32_t kv_page_size,

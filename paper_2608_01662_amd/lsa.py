@@ -101,6 +101,14 @@ class AttnParams:
         return _AttnParams(self.n_heads, self.d_qk, self.d_v, int(self.latent), self.sm_scale)
 
 
+def _int32(**values):
+    """The values, none of which may need more than the 32 bits that the C interface takes (ctypes would cut it off)."""
+    for name, v in values.items():
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise ValueError(f"{name} = {v} does not fit 32 bits")
+    return values.values()
+
+
 @dataclass(frozen=True)
 class AppendParams:
     """What an append to a paged cache rotates and writes; see lsa_append_params."""
@@ -114,7 +122,8 @@ class AppendParams:
     fp8: bool = False
 
     def c(self) -> _AppendParams:
-        return _AppendParams(self.n_heads, self.n_kv_heads, self.d_k, self.d_v, self.rot_start, self.rot_dim,
+        return _AppendParams(*_int32(n_heads=self.n_heads, n_kv_heads=self.n_kv_heads, d_k=self.d_k, d_v=self.d_v,
+                                     rot_start=self.rot_start, rot_dim=self.rot_dim),
                              int(self.interleaved), LSA_KEY_FP8_E4M3FN if self.fp8 else LSA_KEY_BF16)
 
 
@@ -132,9 +141,9 @@ class DecodeAttnParams:
     k_swa: int = 0           # 0: every position up to the query's; else the last k_swa
 
     def c(self) -> _DecodeAttnParams:
-        return _DecodeAttnParams(self.n_heads, self.n_kv_heads, self.d_qk, self.d_v, int(self.latent),
-                                 LSA_KEY_FP8_E4M3FN if self.fp8 else LSA_KEY_BF16, self.k_sink, self.k_swa,
-                                 self.sm_scale)
+        return _DecodeAttnParams(*_int32(n_heads=self.n_heads, n_kv_heads=self.n_kv_heads, d_qk=self.d_qk, d_v=self.d_v),
+                                 int(self.latent), LSA_KEY_FP8_E4M3FN if self.fp8 else LSA_KEY_BF16,
+                                 *_int32(k_sink=self.k_sink, k_swa=self.k_swa), self.sm_scale)
 
 
 MLA = dict(n_heads=64, d_qk=576, d_v=512, latent=True)
@@ -700,6 +709,7 @@ def cache_append(prm: AppendParams, k: torch.Tensor, k_cache: torch.Tensor, *, p
         rows = None
     else:
         _need("rows", rows, _I64, (n,), dev)
+    _int32(sequences=seqs, rows_per_seq=rows_per_seq, max_pages=max_pages, page=page)
     at = _p
     t = _AppendTensors(at(q), at(q_rot), k.data_ptr(), at(k_rot), at(v), qs, qrs, ks, krs, vs, at(rope), rope_rows,
                        at(seq), at(pos), at(ctx_len), at(page_table), at(q_out), k_cache.data_ptr(), at(k_scale),
@@ -713,6 +723,7 @@ def cache_append(prm: AppendParams, k: torch.Tensor, k_cache: torch.Tensor, *, p
 
 def decode_attn_workspace_size(prm: DecodeAttnParams, n_seq: int, rows_per_seq: int, max_pages: int,
                                kv_page_size: int) -> int:
+    _int32(n_seq=n_seq, rows_per_seq=rows_per_seq, max_pages=max_pages, kv_page_size=kv_page_size)
     return lib().lsa_decode_attn_workspace_size(_ref(prm), n_seq, rows_per_seq, max_pages, kv_page_size)
 
 
@@ -763,6 +774,7 @@ def decode_attn(prm: DecodeAttnParams, q: torch.Tensor, k_cache: torch.Tensor, v
         lse = None
     else:
         _need("lse", lse, _F32, (n_rows, H), dev)
+    _int32(sequences=n_seq, rows_per_seq=rows_per_seq, max_pages=max_pages, page=page)
     L, ref = _lib or lib(), _ref(prm)
     wsb = L.lsa_decode_attn_workspace_size(ref, n_seq, rows_per_seq, max_pages, page)
     if wsb and workspace is None:
