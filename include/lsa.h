@@ -361,6 +361,48 @@ lsa_status lsa_cache_append(const lsa_append_params* p, const lsa_append_tensors
                             int64_t n_phys, void* stream);
 
 /*
+ * lsa_cache_append with norms: each query and key head x of n values is, before its rotation,
+ *   y = x / sqrt(mean(x^2) + eps) * weight   (the squares' sum in fp32, one rounding of each stored value),
+ * where a weight is given, and the keys are written beside the cache as well where k_out is given, for
+ * lsa_prefill_attn over the same tokens. The norm is over the dims of q (k) as they come: of heads whose rotated dims
+ * come apart (q_rot, k_rot), those without them, so that of an MLA latent row the latent alone is normed.
+ */
+typedef struct lsa_append_norm {
+  const void* q_weight; /* [d_k] bf16, or [d_k - rot_dim] with q_rot; NULL: queries are not normed        */
+  const void* k_weight; /* [d_k] bf16, or [d_k - rot_dim] with k_rot; NULL: keys are not normed           */
+  float eps;            /* > 0                                                                            */
+  void* k_out;          /* NULL, or [n_tok, n_kv_heads, d_k] bf16 keys as rotated, contiguous; zeros for a token
+                           without a valid sequence and position; may be k itself when k is contiguous and
+                           k_rot NULL                                                                     */
+} lsa_append_norm;
+lsa_status lsa_norm_append(const lsa_append_params* p, const lsa_append_norm* norm, const lsa_append_tensors* t, int64_t n_tok,
+                           int32_t n_seq, int32_t rows_per_seq, int32_t max_pages, int32_t kv_page_size, int64_t n_phys,
+                           void* stream);
+
+/*
+ * Reading a paged cache back: positions start[b] .. of every sequence as packed bf16 rows (the latent rows that an
+ * up-projection takes, keys and values for lsa_prefill_attn). Row i of the outputs, cu[b] <= i < cu[b + 1], is position
+ * start[b] + i - cu[b] of sequence b, dequantised as bf16(scale * code) from fp8. Rows of positions that are negative or beyond
+ * max_pages * P, or whose page-table entry is outside [0, n_phys), are zeros; rows before cu[0] and from cu[n_seq] on
+ * are not written.
+ */
+typedef struct lsa_cache_read_params {
+  int32_t n_kv_heads; /* >= 1                                             */
+  int32_t d_k, d_v;   /* multiples of 16, <= 1024; d_v = 0: no values     */
+  int32_t key_dtype;  /* lsa_key_dtype of the caches                      */
+} lsa_cache_read_params;
+/*
+ *   k_cache, k_scale, v_cache, v_scale, page_table  as lsa_append_tensors has them
+ *   cu       [n_seq + 1] int32, ascending
+ *   start    [n_seq] int32 first position of each sequence, or NULL: 0
+ *   k_out    [n_tok, n_kv_heads, d_k] bf16; v_out [n_tok, n_kv_heads, d_v] bf16, NULL when d_v = 0
+ */
+lsa_status lsa_cache_read(const lsa_cache_read_params* p, int64_t n_tok, int32_t n_seq, const void* k_cache, const float* k_scale,
+                          const void* v_cache, const float* v_scale, const int32_t* cu, const int32_t* start,
+                          const int32_t* page_table, int32_t max_pages, int32_t kv_page_size, int64_t n_phys, void* k_out,
+                          void* v_out, void* stream);
+
+/*
  * Attention of new tokens over the whole of a paged cache (decode of layers, or of contexts, that have no
  * index list): grouped query heads over keys and values, or the MLA latent cache.
  */

@@ -44,3 +44,8 @@ def decode_attention(q, rows_k, rows_v, seen, sm_scale):
     total = p.sum(1, keepdim=True)
     reach = sm_scale * float((q.abs() @ k.abs().T).max())
     return (p @ v) / total, (total.log() + top)[:, 0], (p @ v.abs()) / total, reach
+
+
+def norm(x, weight, eps):
+    """Heads [.., d] float64 over the root of their mean square, times weight [d]."""
+    return x / torch.sqrt((x * x).mean(-1, keepdim=True) + eps) * weight

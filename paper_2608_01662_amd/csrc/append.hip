@@ -1,9 +1,9 @@
-// Cache append with position rotation (lsa_cache_append) for gfx950: queries and keys rotated, keys and
-// values written to their rows of a paged cache in bf16 or e4m3 with a scale per row.
+// Cache append with position rotation (lsa_cache_append, lsa_norm_append) for gfx950: queries and keys rotated, and before
+// that normed by head where asked, keys and values written to their rows of a paged cache in bf16 or e4m3 with a scale per row.
 //
 // A thread takes 16 values of one head of one token: eight pairs of the rotated part (both halves of each
 // pair, so that every input is loaded once), or 16 neighbours elsewhere. Nothing is shared between threads
-// but the maximum of an fp8 row, an exchange within the lanes that hold the row.
+// but the maximum of an fp8 row and the squares of a normed head, exchanges within the lanes that hold the row.
 //
 // Six flops per rotated pair against 8 bytes: bound by HBM, from a few thousand tokens on; below that by the chain
 // of round trips (position, page-table entry and angles, then rows) and the launch. Measured, GPU time alone: one token of 32
@@ -97,17 +97,43 @@ __device__ __forceinline__ u32x2 pack_fp8x8(const float* x) {
   return u32x2{(uint32_t)lo, (uint32_t)hi};
 }
 
+// y * weight / rms over the head's normed dims: those of the input `x` as it comes (`width` of them), without a rotated part that
+// comes apart. The squares are summed in fp32 over the 16 values of each of the row's lanes, then across the lanes; idle
+// lanes hold zeros. weight: 16 values of this lane, in registers already.
+struct Weight16 {
+  u32x4 lo, hi;
+};
+__device__ __forceinline__ Weight16 load_weight(const uint16_t* w, const Unit& u) {
+  return Weight16{*reinterpret_cast<const u32x4*>(w + u.lo), *reinterpret_cast<const u32x4*>(w + u.hi)};
+}
+__device__ __forceinline__ void norm_head(float* y, bool normed, const Weight16& weight, int lanes, int width, float eps) {
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) sum = fmaf(y[i], y[i], sum);
+  if (!normed) sum = 0.f;
+  for (int o = 1; o < lanes; o <<= 1) sum += __shfl_xor(sum, o);
+  if (!normed) return;
+  const float r = 1.f / sqrtf(sum / (float)width + eps);
+  float w[16];
+  unpack8(weight.lo, w);
+  unpack8(weight.hi, w + 8);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) y[i] = y[i] * r * w[i];
+}
+
 // Blocks [0, bq) rotate queries, [bq, bq + bk) append keys, the rest values. A head's units are dealt to
-// `lanes` neighbouring threads: as many as it has, or for fp8 rows the next power of two, so that the lanes
-// of a row exchange their maximum within one wave.
-template <int HEADS>  // query heads per thread
+// `lanes` neighbouring threads: as many as it has, or for fp8 rows and normed heads the next power of two, so that the
+// lanes of a row exchange their maximum or sum within one wave.
+template <int HEADS, bool NORM>  // query heads per thread; with norms or keys beside the cache (lsa_norm_append)
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendGeom g, int bq, int bk) {
   const int blk = (int)blockIdx.x;
   if (blk < bq) {
     const int item = blk * kAppendThreads + (int)threadIdx.x, vec = fdiv(g.by_q_units, item), t = fdiv(g.by_q_heads, vec);
     if (t >= g.n_tok) return;
     const AppendToken tok = append_token(g, t);
-    const Unit u = unit_of(g, item - vec * (int)g.by_q_units.d);
+    const int ui = item - vec * (int)g.by_q_units.d;
+    const bool live = !NORM || ui < g.d_k / 16;  // (normed heads: lanes beyond the head's units)
+    const Unit u = unit_of(g, live ? ui : 0);
     const int head = (vec - t * (int)g.by_q_heads.d) * HEADS;
     u32x4 x[HEADS][2];
 #pragma unroll
@@ -119,16 +145,21 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendGeom g, in
     const bool turn = u.pair >= 0 && tok.pos >= 0;
     Angles an{};
     if (turn) an = load_angles(g, u, tok.pos);
+    const bool normed = NORM && g.q_weight && live && !(g.q_rot && u.pair >= 0);
+    Weight16 weight{};
+    if (normed) weight = load_weight(g.q_weight, u);
 #pragma unroll
     for (int h = 0; h < HEADS; ++h) {
       float y[16];
       unpack8(x[h][0], y);
       unpack8(x[h][1], y + 8);
+      if (NORM && g.q_weight) norm_head(y, normed, weight, (int)g.by_q_units.d, g.q_rot ? g.d_k - g.rot_dim : g.d_k, g.eps);
       if (turn) rotate(g, an, y);
       if (tok.pos < 0) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) y[i] = 0.f;
       }
+      if (!live) continue;
       uint16_t* o = g.q_out + ((int64_t)t * g.H + head + h) * g.d_k;
       *reinterpret_cast<u32x4*>(o + u.lo) = pack8(y);
       *reinterpret_cast<u32x4*>(o + u.hi) = pack8(y + 8);
@@ -157,7 +188,22 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendGeom g, in
     const uint16_t* p = key ? unit_base(g, g.k, g.k_stride, g.k_rot, g.k_rot_stride, t, head, u) : g.v + (int64_t)t * g.v_stride + head * d;
     unpack8(*reinterpret_cast<const u32x4*>(p + u.lo), y);
     unpack8(*reinterpret_cast<const u32x4*>(p + u.hi), y + 8);
-    if (u.pair >= 0 && tok.pos >= 0) rotate(g, load_angles(g, u, tok.pos), y);
+    if (!NORM && u.pair >= 0 && tok.pos >= 0) rotate(g, load_angles(g, u, tok.pos), y);
+  }
+  if (NORM && key) {
+    const bool live = ui < units, normed = g.k_weight && live && !(g.k_rot && u.pair >= 0);
+    Angles an{};
+    if (live && u.pair >= 0 && tok.pos >= 0) an = load_angles(g, u, tok.pos);
+    Weight16 weight{};
+    if (normed) weight = load_weight(g.k_weight, u);
+    if (g.k_weight) norm_head(y, normed, weight, lanes, g.k_rot ? g.d_k - g.rot_dim : g.d_k, g.eps);
+    if (live && u.pair >= 0 && tok.pos >= 0) rotate(g, an, y);
+    if (g.k_out && live) {
+      uint16_t* o = g.k_out + ((int64_t)t * g.Hkv + head) * g.d_k;
+      const bool valid = tok.pos >= 0;
+      *reinterpret_cast<u32x4*>(o + u.lo) = valid ? pack8(y) : u32x4{};
+      *reinterpret_cast<u32x4*>(o + u.hi) = valid ? pack8(y + 8) : u32x4{};
+    }
   }
   const int64_t row = (page * g.Hkv + head) * g.P + off;
   if (!g.fp8) {
@@ -189,8 +235,8 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendGeom g, in
   *reinterpret_cast<u32x2*>(o + u.hi) = pack_fp8x8(y + 8);
 }
 
-static int append_lanes(int units, bool fp8) {
-  if (!fp8) return units;
+static int append_lanes(int units, bool exchange) {
+  if (!exchange) return units;
   int l = 1;
   while (l < units) l *= 2;
   return l;
@@ -203,7 +249,8 @@ static int append_lanes(int units, bool fp8) {
 constexpr int64_t kManyUnits = 1 << 18;
 hipError_t launch_append(const AppendGeom& all, hipStream_t st) {
   AppendGeom g = all;
-  const int q_units = g.H ? g.d_k / 16 : 1, k_lanes = append_lanes(g.d_k / 16, g.fp8), v_lanes = g.d_v ? append_lanes(g.d_v / 16, g.fp8) : 1;
+  const int q_units = g.H ? append_lanes(g.d_k / 16, g.q_weight != nullptr) : 1;
+  const int k_lanes = append_lanes(g.d_k / 16, g.fp8 || g.k_weight != nullptr), v_lanes = g.d_v ? append_lanes(g.d_v / 16, g.fp8) : 1;
   const int heads = g.H % 4 == 0 && (int64_t)all.n_tok * g.H * q_units >= kManyUnits ? 4 : 1;
   g.by_q_units = fast_div((uint32_t)q_units);
   g.by_q_heads = fast_div((uint32_t)(g.H ? g.H / heads : 1));
@@ -225,9 +272,12 @@ hipError_t launch_append(const AppendGeom& all, hipStream_t st) {
     g.k = all.k + t0 * g.k_stride;
     if (all.k_rot) g.k_rot = all.k_rot + t0 * g.k_rot_stride;
     if (all.v) g.v = all.v + t0 * g.v_stride;
+    if (all.k_out) g.k_out = all.k_out + t0 * g.Hkv * g.d_k;
     const int bq = g.H ? blocks((int64_t)g.n_tok * (g.H / heads) * q_units) : 0, bk = blocks((int64_t)g.n_tok * g.Hkv * k_lanes);
     const int bv = g.d_v ? blocks((int64_t)g.n_tok * g.Hkv * v_lanes) : 0;
-    const hipError_t e = launch_kernel(heads == 4 ? append_kernel<4> : append_kernel<1>, dim3((unsigned)bq + (unsigned)bk + (unsigned)bv),
+    const bool norm = g.q_weight || g.k_weight || g.k_out;
+    auto* kernel = norm ? (heads == 4 ? append_kernel<4, true> : append_kernel<1, true>) : heads == 4 ? append_kernel<4, false> : append_kernel<1, false>;
+    const hipError_t e = launch_kernel(kernel, dim3((unsigned)bq + (unsigned)bk + (unsigned)bv),
                                        dim3(kAppendThreads), st, g, bq, bk);
     if (e != hipSuccess) return e;
   }

@@ -122,9 +122,12 @@ inline hipError_t launch_kernel(void (*kernel)(A...), dim3 grid, dim3 block, hip
   return e;
 }
 
-// One cache append (lsa_append_tensors, checked).
+// One cache append (lsa_append_tensors and lsa_append_norm, checked).
 struct AppendGeom {
   const uint16_t *q, *q_rot, *k, *k_rot, *v;
+  const uint16_t *q_weight, *k_weight;  // of normed heads, or nullptr
+  uint16_t* k_out;                      // the keys beside the cache, or nullptr
+  float eps;
   int64_t q_stride, q_rot_stride, k_stride, k_rot_stride, v_stride;
   const float* rope;
   int64_t rope_rows;
@@ -144,6 +147,20 @@ struct AppendGeom {
   FastDiv by_q_units, by_q_heads, by_kv_heads, by_k_lanes, by_v_lanes, by_page;
 };
 hipError_t launch_append(const AppendGeom& g, hipStream_t st);
+
+// One read of a paged cache (lsa_cache_read, checked).
+struct CacheReadGeom {
+  const void *k, *v;
+  const float *k_scale, *v_scale;
+  const int32_t *cu, *start, *page_table;
+  uint16_t *k_out, *v_out;
+  int64_t n_tok, n_phys;
+  int n_seq, Hkv, d_k, d_v, fp8, max_pages, P;
+  // set by the launcher: rows of a workgroup, and divisions by the 16-value units of a token and of a head, and by P
+  int tokens;
+  FastDiv by_units, by_k_units, by_v_units, by_page;
+};
+hipError_t launch_cache_read(const CacheReadGeom& g, hipStream_t st);
 
 // One call of the attention over the whole cache (lsa_decode_attn, checked).
 struct DecodeGeom {

@@ -159,13 +159,9 @@ DecodePlan plan_decode(const lsa_decode_attn_params* p, int32_t n_seq, int32_t r
   return pl;
 }
 
-}  // namespace
-
-extern "C" {
-
-lsa_status lsa_cache_append(const lsa_append_params* p, const lsa_append_tensors* t, int64_t n_tok, int32_t n_seq,
-                            int32_t rows_per_seq, int32_t max_pages, int32_t kv_page_size, int64_t n_phys,
-                            void* stream) {
+// lsa_cache_append (norm NULL) and lsa_norm_append
+lsa_status append(const lsa_append_params* p, const lsa_append_norm* norm, const lsa_append_tensors* t, int64_t n_tok, int32_t n_seq,
+                  int32_t rows_per_seq, int32_t max_pages, int32_t kv_page_size, int64_t n_phys, void* stream) {
   g_err[0] = 0;
   lsa_status s = check_append_params(p);
   if (s != LSA_OK) return s;
@@ -211,8 +207,22 @@ lsa_status lsa_cache_append(const lsa_append_params* p, const lsa_append_tensors
   LSA_REQUIRE(aligned(t->seq, 4) && aligned(t->pos, 4) && aligned(t->ctx_len, 4) && aligned(t->page_table, 4) &&
                   aligned(t->k_scale, 4) && aligned(t->v_scale, 4) && aligned(t->rows, 8),
               LSA_ERR_INVALID_ARG, "seq, pos, ctx_len, page_table and scales must be 4-byte aligned, rows 8-byte");
+  if (norm != nullptr) {
+    LSA_REQUIRE(norm->eps > 0.f && norm->eps < 1e30f, LSA_ERR_INVALID_ARG, "eps must be positive and finite");
+    LSA_REQUIRE(norm->q_weight == nullptr || p->n_heads > 0, LSA_ERR_INVALID_ARG, "q_weight must be NULL with n_heads = 0");
+    LSA_REQUIRE(aligned(norm->q_weight, 16) && aligned(norm->k_weight, 16) && aligned(norm->k_out, 16), LSA_ERR_INVALID_ARG,
+                "q_weight, k_weight and k_out must be 16-byte aligned");
+    LSA_REQUIRE(norm->k_out == nullptr || norm->k_out != t->k || (t->k_rot == nullptr && t->k_stride == (int64_t)p->n_kv_heads * p->d_k),
+                LSA_ERR_INVALID_ARG, "k_out may be k only when k is contiguous and whole");
+  }
 
   lsa::AppendGeom g{};
+  if (norm != nullptr) {
+    g.q_weight = static_cast<const uint16_t*>(norm->q_weight);
+    g.k_weight = static_cast<const uint16_t*>(norm->k_weight);
+    g.k_out = static_cast<uint16_t*>(norm->k_out);
+    g.eps = norm->eps;
+  }
   g.q = static_cast<const uint16_t*>(t->q);
   g.q_rot = static_cast<const uint16_t*>(t->q_rot);
   g.k = static_cast<const uint16_t*>(t->k);
@@ -252,6 +262,24 @@ lsa_status lsa_cache_append(const lsa_append_params* p, const lsa_append_tensors
   const hipError_t e = lsa::launch_append(g, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "cache append");
   return LSA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+lsa_status lsa_cache_append(const lsa_append_params* p, const lsa_append_tensors* t, int64_t n_tok, int32_t n_seq,
+                            int32_t rows_per_seq, int32_t max_pages, int32_t kv_page_size, int64_t n_phys,
+                            void* stream) {
+  return append(p, nullptr, t, n_tok, n_seq, rows_per_seq, max_pages, kv_page_size, n_phys, stream);
+}
+
+lsa_status lsa_norm_append(const lsa_append_params* p, const lsa_append_norm* norm, const lsa_append_tensors* t, int64_t n_tok,
+                           int32_t n_seq, int32_t rows_per_seq, int32_t max_pages, int32_t kv_page_size, int64_t n_phys,
+                           void* stream) {
+  g_err[0] = 0;
+  LSA_REQUIRE(norm != nullptr, LSA_ERR_INVALID_ARG, "norm is NULL");
+  return append(p, norm, t, n_tok, n_seq, rows_per_seq, max_pages, kv_page_size, n_phys, stream);
 }
 
 size_t lsa_decode_attn_workspace_size(const lsa_decode_attn_params* p, int32_t n_seq, int32_t rows_per_seq,

@@ -1,5 +1,5 @@
-// Python binding of the serving operators (module _serve): the host side of lsa_cache_append and lsa_decode_attn for
-// torch tensors.
+// Python binding of the serving operators (module _serve): the host side of lsa_cache_append, lsa_norm_append and
+// lsa_decode_attn for torch tensors.
 //
 // A decode step's kernels take 3 to 20 us, as long as a host in Python that looks at a dozen tensors, so the
 // checks that a good call passes, its allocations and the call itself are compiled. What is not as it should be is not explained
@@ -143,12 +143,17 @@ bool stream_of(c10::DeviceIndex device, void*& stream) {
   return !PyErr_Occurred();
 }
 
-PyObject* pair_of(const at::Tensor* a, const at::Tensor* b) {
-  auto wrap = [](const at::Tensor* t) { return t == nullptr ? Py_NewRef(Py_None) : THPVariable_Wrap(*t); };
-  PyObject *x = wrap(a), *y = x == nullptr ? nullptr : wrap(b);
-  PyObject* r = y == nullptr ? nullptr : PyTuple_Pack(2, x, y);
-  Py_XDECREF(x);
-  Py_XDECREF(y);
+PyObject* tuple_of(std::initializer_list<const at::Tensor*> ts) {
+  PyObject* r = PyTuple_New((Py_ssize_t)ts.size());
+  Py_ssize_t i = 0;
+  for (const at::Tensor* t : ts) {
+    PyObject* o = r == nullptr ? nullptr : t == nullptr ? Py_NewRef(Py_None) : THPVariable_Wrap(*t);
+    if (o == nullptr) {
+      Py_XDECREF(r);
+      return nullptr;
+    }
+    PyTuple_SET_ITEM(r, i++, o);
+  }
   return r;
 }
 
@@ -165,10 +170,11 @@ PyObject* not_done(PyObject* module, lsa_status st, const char* call) {
 }
 
 // cache_append(prm, k, k_cache, page_table, ctx_len, pos, seq, rows_per_seq, n_seq, rope, k_rot, v, v_cache, k_scale, v_scale,
-//              q, q_rot, q_out, rows)
-PyObject* cache_append(PyObject* module, PyObject* const* a, Py_ssize_t n_args) {
+//              q, q_rot, q_out, rows), and with NORM as norm_append(.., q_weight, k_weight, eps, k_out)
+template <bool NORM>
+PyObject* append(PyObject* module, PyObject* const* a, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
-  if (n_args != 19) Py_RETURN_NONE;
+  if (n_args != (NORM ? 23 : 19)) Py_RETURN_NONE;
   int32_t p[8], rows_per_seq, max_pages;
   for (int i = 0; i < 8; ++i)
     if (!int_attr(a[0], append_names[i], p[i])) Py_RETURN_NONE;
@@ -211,6 +217,19 @@ PyObject* cache_append(PyObject* module, PyObject* const* a, Py_ssize_t n_args) 
     x.rope = at_of<float>(rope);
     x.rope_rows = rope->size(0);
   }
+  lsa_append_norm norm{};
+  const at::Tensor* k_out = nullptr;
+  if constexpr (NORM) {
+    norm.q_weight = at_of(ts.whole(a[19], at::kBFloat16, {a[16] == Py_None ? d_k : d_k - rot}, true));
+    norm.k_weight = at_of(ts.whole(a[20], at::kBFloat16, {a[10] == Py_None ? d_k : d_k - rot}, true));
+    const double eps = PyFloat_AsDouble(a[21]);
+    if (PyErr_Occurred()) {
+      PyErr_Clear();
+      Py_RETURN_NONE;
+    }
+    norm.eps = (float)eps;
+    k_out = a[22] == Py_True || a[22] == Py_False ? nullptr : ts.whole(a[22], at::kBFloat16, {n, nk, d_k}, true);
+  }
   // the tokens' places
   const at::Tensor *table = ts.table(a[3], max_pages), *ctx_len = ts.get(a[4]);
   ts.need((a[4] == Py_None) != (a[5] == Py_None) && (ctx_len == nullptr || ctx_len->dim() == 1));
@@ -238,7 +257,7 @@ PyObject* cache_append(PyObject* module, PyObject* const* a, Py_ssize_t n_args) 
   void* stream;
   if (!stream_of(ts.device, stream)) return nullptr;
   lsa_status st;
-  at::Tensor new_q, new_rows;
+  at::Tensor new_q, new_rows, new_k;
   {
     Unlocked unlocked;
     if (nq != 0 && q_out == nullptr) {
@@ -251,10 +270,19 @@ PyObject* cache_append(PyObject* module, PyObject* const* a, Py_ssize_t n_args) 
     }
     x.q_out = at_of(q_out);
     x.rows = at_of<int64_t>(rows);
-    st = lsa_cache_append(&prm, &x, n, (int32_t)seqs, rows_per_seq, max_pages, (int32_t)page, n_phys, stream);
+    if constexpr (NORM) {
+      if (a[22] == Py_True) {
+        new_k = at::empty({n, nk, d_k}, k->options());
+        k_out = &new_k;
+      }
+      norm.k_out = at_of(k_out);
+      st = lsa_norm_append(&prm, &norm, &x, n, (int32_t)seqs, rows_per_seq, max_pages, (int32_t)page, n_phys, stream);
+    } else {
+      st = lsa_cache_append(&prm, &x, n, (int32_t)seqs, rows_per_seq, max_pages, (int32_t)page, n_phys, stream);
+    }
   }
-  if (st != LSA_OK) return not_done(module, st, "lsa_cache_append");
-  return pair_of(q_out, rows);
+  if (st != LSA_OK) return not_done(module, st, NORM ? "lsa_norm_append" : "lsa_cache_append");
+  return NORM ? tuple_of({q_out, k_out, rows}) : tuple_of({q_out, rows});
   END_HANDLE_TH_ERRORS
 }
 
@@ -326,12 +354,13 @@ PyObject* decode_attn(PyObject* module, PyObject* const* a, Py_ssize_t n_args) {
                          at_of(workspace), workspace == nullptr ? 0 : workspace->nbytes(), stream);
   }
   if (st != LSA_OK) return not_done(module, st, "lsa_decode_attn");
-  return pair_of(out, lse);
+  return tuple_of({out, lse});
   END_HANDLE_TH_ERRORS
 }
 
 PyMethodDef methods[] = {
-    {"cache_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_append)), METH_FASTCALL, nullptr},
+    {"cache_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(append<false>)), METH_FASTCALL, nullptr},
+    {"norm_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(append<true>)), METH_FASTCALL, nullptr},
     {"decode_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(decode_attn)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef definition = {PyModuleDef_HEAD_INIT, "_serve", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -52,6 +52,15 @@ class _AppendTensors(ctypes.Structure):
                                                "v_cache", "v_scale", "rows")]
 
 
+class _AppendNorm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("k_out", ctypes.c_void_p)]
+
+
+class _CacheReadParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_kv_heads", "d_k", "d_v", "key_dtype")]
+
+
 class _DecodeAttnParams(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "n_heads", "n_kv_heads", "d_qk", "d_v", "latent", "key_dtype", "k_sink", "k_swa")] + \
@@ -128,6 +137,19 @@ class AppendParams:
 
 
 @dataclass(frozen=True)
+class CacheReadParams:
+    """The caches of a read; see lsa_cache_read_params."""
+    n_kv_heads: int
+    d_k: int
+    d_v: int = 0             # 0: no values
+    fp8: bool = False
+
+    def c(self) -> _CacheReadParams:
+        return _CacheReadParams(*_int32(n_kv_heads=self.n_kv_heads, d_k=self.d_k, d_v=self.d_v),
+                                LSA_KEY_FP8_E4M3FN if self.fp8 else LSA_KEY_BF16)
+
+
+@dataclass(frozen=True)
 class DecodeAttnParams:
     """Attention of new tokens over a whole paged cache; see lsa_decode_attn_params."""
     n_heads: int
@@ -199,6 +221,12 @@ def lib() -> ctypes.CDLL:
         L.lsa_cache_append.argtypes = [ctypes.POINTER(_AppendParams), _vp, _i64, _i32, _i32,
                                        _i32, _i32, _i64, _vp]
         L.lsa_cache_append.restype = _i32
+        L.lsa_norm_append.argtypes = [ctypes.POINTER(_AppendParams), ctypes.POINTER(_AppendNorm), _vp, _i64, _i32, _i32,
+                                      _i32, _i32, _i64, _vp]
+        L.lsa_norm_append.restype = _i32
+        L.lsa_cache_read.argtypes = [ctypes.POINTER(_CacheReadParams), _i64, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32,
+                                     _i32, _i64, _vp, _vp, _vp]
+        L.lsa_cache_read.restype = _i32
         L.lsa_decode_attn_workspace_size.argtypes = [D, _i32, _i32, _i32, _i32]
         L.lsa_decode_attn_workspace_size.restype = _sz
         L.lsa_decode_attn.argtypes = [D, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i64, _vp, _vp, _vp,
@@ -625,6 +653,22 @@ def _cache_scale(name: str, t, n_phys: int, heads: int, page: int, device) -> No
     _need(name, t, _F32, (n_phys, page) if flat else (n_phys, heads, page), device)
 
 
+def _offsets(name: str, t, device) -> int:
+    """The sequences of offsets [n_seq + 1]."""
+    _need(name, t, _I32, (None,), device)
+    if t.shape[0] < 1:
+        raise ValueError(f"{name} must hold n_seq + 1 offsets")
+    return t.shape[0] - 1
+
+
+def _table_width(t, n_seq: int, device) -> int:
+    """max_pages of a page table [n_seq, max_pages], 1 without one."""
+    if t is None:
+        return 1
+    _need("page_table", t, _I32, (n_seq, None), device)
+    return t.shape[1]
+
+
 def cache_append(prm: AppendParams, k: torch.Tensor, k_cache: torch.Tensor, *, page_table: torch.Tensor | None = None,
                  ctx_len: torch.Tensor | None = None, pos: torch.Tensor | None = None, seq: torch.Tensor | None = None,
                  rows_per_seq: int = 1, n_seq: int | None = None, rope: torch.Tensor | None = None,
@@ -643,10 +687,36 @@ def cache_append(prm: AppendParams, k: torch.Tensor, k_cache: torch.Tensor, *, p
     [positions, rot_dim] fp32, cosines then sines. page_table None: sequence b has page b alone (n_seq: how many
     there are, else as ctx_len or the cache has). rows: True, or an int64 tensor [n_tok], for the physical cache
     rows (block_keys_update takes them)."""
-    done = (_serve or _serving()).cache_append(prm, k, k_cache, page_table, ctx_len, pos, seq, rows_per_seq, n_seq, rope, k_rot, v,
-                                               v_cache, k_scale, v_scale, q, q_rot, q_out, rows)
-    if done is not None:
-        return done
+    args = (prm, k, k_cache, page_table, ctx_len, pos, seq, rows_per_seq, n_seq, rope, k_rot, v, v_cache, k_scale, v_scale, q,
+            q_rot, q_out, rows)
+    done = (_serve or _serving()).cache_append(*args)
+    return _append(*args) if done is None else done
+
+
+def norm_append(prm: AppendParams, k: torch.Tensor, k_cache: torch.Tensor, *, q_weight: torch.Tensor | None = None,
+                k_weight: torch.Tensor | None = None, eps: float = 1e-6, k_out: torch.Tensor | bool = False,
+                page_table: torch.Tensor | None = None, ctx_len: torch.Tensor | None = None,
+                pos: torch.Tensor | None = None, seq: torch.Tensor | None = None, rows_per_seq: int = 1,
+                n_seq: int | None = None, rope: torch.Tensor | None = None, k_rot: torch.Tensor | None = None,
+                v: torch.Tensor | None = None, v_cache: torch.Tensor | None = None, k_scale: torch.Tensor | None = None,
+                v_scale: torch.Tensor | None = None, q: torch.Tensor | None = None, q_rot: torch.Tensor | None = None,
+                q_out: torch.Tensor | None = None, rows: torch.Tensor | bool = False):
+    """cache_append that norms each query and key head (x / rms * weight) before its rotation (lsa_norm_append). Returns
+    (q_out or None, k_out or None, rows or None).
+
+    q_weight, k_weight: bf16, as wide as the heads of q and k as they are given; None: not normed. k_out: True, or a
+    bf16 tensor [n_tok, n_kv_heads, d_k], for the keys beside the cache (prefill_attn takes them). Other arguments as
+    cache_append."""
+    args = (prm, k, k_cache, page_table, ctx_len, pos, seq, rows_per_seq, n_seq, rope, k_rot, v, v_cache, k_scale, v_scale, q,
+            q_rot, q_out, rows)
+    norm = (q_weight, k_weight, eps, k_out)
+    done = (_serve or _serving()).norm_append(*args, *norm)
+    return _append(*args, norm) if done is None else done
+
+
+def _append(prm, k, k_cache, page_table, ctx_len, pos, seq, rows_per_seq, n_seq, rope, k_rot, v, v_cache, k_scale, v_scale, q,
+            q_rot, q_out, rows, norm=None):
+    """The checks of cache_append and norm_append, and the call."""
     nk, nq, d_k, d_v, rot, fp8 = prm.n_kv_heads, prm.n_heads, prm.d_k, prm.d_v, prm.rot_dim, prm.fp8
     is_tensor = isinstance(k, torch.Tensor)
     dev, i = (k.device, k.get_device()) if is_tensor else (None, -1)
@@ -714,11 +784,72 @@ def cache_append(prm: AppendParams, k: torch.Tensor, k_cache: torch.Tensor, *, p
     t = _AppendTensors(at(q), at(q_rot), k.data_ptr(), at(k_rot), at(v), qs, qrs, ks, krs, vs, at(rope), rope_rows,
                        at(seq), at(pos), at(ctx_len), at(page_table), at(q_out), k_cache.data_ptr(), at(k_scale),
                        at(v_cache), at(v_scale), at(rows))
+    where = (n, seqs, rows_per_seq, max_pages, page, n_phys)
+    if norm is None:
+        with torch.cuda.device(dev):
+            st = (_lib or lib()).lsa_cache_append(_ref(prm), ctypes.byref(t), *where, _stream(dev))
+        if st != 0:
+            _check(st, "lsa_cache_append")
+        return q_out, rows
+    q_weight, k_weight, eps, k_out = norm
+    _need_opt("q_weight", q_weight, _BF16, (d_k if q_rot is None else d_k - rot,), dev)
+    _need_opt("k_weight", k_weight, _BF16, (d_k if k_rot is None else d_k - rot,), dev)
+    if k_out is True:
+        k_out = k.new_empty((n, nk, d_k))
+    elif k_out is False or k_out is None:
+        k_out = None
+    else:
+        _need("k_out", k_out, _BF16, (n, nk, d_k), dev)
+    an = _AppendNorm(at(q_weight), at(k_weight), eps, at(k_out))
     with torch.cuda.device(dev):
-        st = (_lib or lib()).lsa_cache_append(_ref(prm), ctypes.byref(t), n, seqs, rows_per_seq, max_pages, page, n_phys, _stream(dev))
+        st = (_lib or lib()).lsa_norm_append(_ref(prm), ctypes.byref(an), ctypes.byref(t), *where, _stream(dev))
     if st != 0:
-        _check(st, "lsa_cache_append")
-    return q_out, rows
+        _check(st, "lsa_norm_append")
+    return q_out, k_out, rows
+
+
+def cache_read(prm: CacheReadParams, k_cache: torch.Tensor, cu: torch.Tensor, n_tok: int, *,
+               page_table: torch.Tensor | None = None, start: torch.Tensor | None = None,
+               v_cache: torch.Tensor | None = None, k_scale: torch.Tensor | None = None,
+               v_scale: torch.Tensor | None = None, k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None):
+    """Read sequences back from a paged cache as packed bf16 rows, dequantised (lsa_cache_read). Returns (k_out [n_tok,
+    n_kv_heads, d_k], v_out [n_tok, n_kv_heads, d_v] or None).
+
+    cu [n_seq + 1] int32: rows cu[b] .. cu[b + 1] - 1 are positions start[b] .. (None: 0 ..) of sequence b; n_tok: rows of the
+    outputs, of which those behind cu[n_seq] are left as they are. Caches as cache_append writes them."""
+    nk, d_k, d_v, fp8 = prm.n_kv_heads, prm.d_k, prm.d_v, prm.fp8
+    dev = k_cache.device if isinstance(k_cache, torch.Tensor) else None
+    n_phys, page = _paged_shape("k_cache", k_cache, fp8, nk, d_k, dev)
+    if d_v:
+        _paged_like("v_cache", v_cache, fp8, n_phys, nk, page, d_v, dev)
+    elif v_cache is not None or v_scale is not None or v_out is not None:
+        raise ValueError("v_cache, v_scale and v_out must be None with d_v = 0")
+    if fp8:
+        _cache_scale("k_scale", k_scale, n_phys, nk, page, dev)
+        if d_v:
+            _cache_scale("v_scale", v_scale, n_phys, nk, page, dev)
+    elif k_scale is not None or v_scale is not None:
+        raise ValueError("k_scale and v_scale must be None for bf16 caches")
+    n_seq = _offsets("cu", cu, dev)
+    _need_opt("start", start, _I32, (n_seq,), dev)
+    max_pages = _table_width(page_table, n_seq, dev)
+    if n_tok < 0:
+        raise ValueError(f"n_tok = {n_tok} < 0")
+    _int32(n_tok=n_tok, sequences=n_seq, max_pages=max_pages, page=page)
+    if k_out is None:
+        k_out = torch.empty((n_tok, nk, d_k), dtype=torch.bfloat16, device=dev)
+    else:
+        _need("k_out", k_out, _BF16, (n_tok, nk, d_k), dev)
+    if d_v and v_out is None:
+        v_out = torch.empty((n_tok, nk, d_v), dtype=torch.bfloat16, device=dev)
+    elif d_v:
+        _need("v_out", v_out, _BF16, (n_tok, nk, d_v), dev)
+    with torch.cuda.device(dev):
+        st = (_lib or lib()).lsa_cache_read(_ref(prm), n_tok, n_seq, _p(k_cache), _p(k_scale), _p(v_cache), _p(v_scale), _p(cu),
+                                            _p(start), _p(page_table), max_pages, page, n_phys, _p(k_out), _p(v_out), _stream(dev))
+    if st != 0:
+        _check(st, "lsa_cache_read")
+    return k_out, v_out
 
 
 def decode_attn_workspace_size(prm: DecodeAttnParams, n_seq: int, rows_per_seq: int, max_pages: int,
