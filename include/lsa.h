@@ -447,6 +447,63 @@ lsa_status lsa_decode_attn(const lsa_decode_attn_params* p, int32_t n_seq, int32
                            int32_t max_pages, int32_t kv_page_size, int64_t n_phys, void* out, float* lse,
                            void* workspace, size_t ws_bytes, void* stream);
 
+/*
+ * Attention of whole prompts, or of the last part of prompts, over keys and values that lie packed in memory (as
+ * lsa_norm_append's k_out, lsa_cache_read or an up-projection leave them): sequences of different lengths one after the
+ * other in one call, grouped query heads.
+ */
+typedef struct lsa_prefill_attn_params {
+  int32_t n_heads;    /* query heads, a multiple of n_kv_heads, <= 1024                                     */
+  int32_t n_kv_heads;
+  int32_t d_qk, d_v;  /* (64, 64), (128, 128), or (192, 128): MLA heads that are not absorbed               */
+  int32_t causal;     /* 1: a query sees the keys up to its own position; 0: all keys of its sequence       */
+  int32_t k_sink;     /* with k_swa > 0: the first k_sink positions are attended as well                    */
+  int32_t k_swa;      /* 0: every position up to the query's; else only the last k_swa (causal only)        */
+  float sm_scale;     /* softmax scale applied to q . k                                                     */
+} lsa_prefill_attn_params;
+
+/* Workspace bytes for lsa_prefill_attn; 0 when no call of these sizes cuts a row's keys into parts. */
+size_t lsa_prefill_attn_workspace_size(const lsa_prefill_attn_params* p, int32_t n_seq, int64_t n_tok, int64_t n_kv);
+
+/*
+ * Sequence b has the query tokens cu_q[b] .. cu_q[b + 1] - 1 and the keys cu_kv[b] .. cu_kv[b + 1] - 1, n_q and n_k of them. Its
+ * queries are its last positions: token j of them is at t = n_k - n_q + j, and attends to
+ *   A = { s < n_k : not causal, or s <= t and (k_swa = 0 or s > t - k_swa or s < k_sink) },
+ *   o = sum_{s in A} softmax_s(sm_scale * q . k_s) v_s,   lse = log sum_{s in A} exp(sm_scale * q . k_s),
+ * head h to key/value head h / (n_heads / n_kv_heads). Where A is empty (t < 0, no keys, or keys out of range), and where every
+ * score is -inf, o = 0 and lse = -inf. Keys and values outside A, NaN and infinities among them, have no effect.
+ *   q           [n_tok, n_heads, d_qk] bf16, tokens q_stride elements apart
+ *   k, v        [n_kv, n_kv_heads, d_qk] and [.., d_v] bf16, rows k_stride and v_stride elements apart. Strides: multiples of 8, less
+ *               than 2^24, so that the slices of a fused projection are taken as they are
+ *   cu_q        [n_seq + 1] int32, ascending; a sequence whose range is not within [0, n_tok] has no tokens. Rows of out and
+ *               lse that belong to no sequence (before cu_q[0], behind cu_q[n_seq]) are not written
+ *   cu_kv       [n_seq + 1] int32, or NULL: cu_q (then n_kv = n_tok); a range not within [0, n_kv] is empty
+ *   out         [n_tok, n_heads, d_v] bf16, contiguous; lse [n_tok, n_heads] fp32 or NULL
+ *   workspace   >= lsa_prefill_attn_workspace_size(...) bytes, 256-byte aligned
+ * The same call gives the same bits; the same sequence in another batch agrees within rounding.
+ */
+lsa_status lsa_prefill_attn(const lsa_prefill_attn_params* p, int32_t n_seq, int64_t n_tok, int64_t n_kv, const void* q,
+                            int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                            const int32_t* cu_q, const int32_t* cu_kv, void* out, float* lse, void* workspace, size_t ws_bytes,
+                            void* stream);
+
+/*
+ * lsa_decode_attn for chunks of prompts: any number of new tokens of every sequence (chunks of some prompts beside the single
+ * tokens of others), packed one after the other, by matrix products over blocks of query rows. Sequence b has the tokens cu_q[b] ..
+ * cu_q[b + 1] - 1, n_b of them, which are its newest: token j is at t = ctx_len[b] - n_b + j. What it attends to, and the rows
+ * that attend to nothing, are as in lsa_decode_attn. p->latent must be 0.
+ *   q           [n_tok, n_heads, d_qk] bf16, contiguous
+ *   cu_q        as in lsa_prefill_attn
+ *   out, lse    [n_tok, n_heads, d_v] bf16; [n_tok, n_heads] fp32 or NULL
+ * Other arguments as in lsa_decode_attn.
+ */
+size_t lsa_chunk_attn_workspace_size(const lsa_decode_attn_params* p, int32_t n_seq, int64_t n_tok, int32_t max_pages,
+                                     int32_t kv_page_size);
+lsa_status lsa_chunk_attn(const lsa_decode_attn_params* p, int32_t n_seq, int64_t n_tok, const void* q, const void* k_cache,
+                          const float* k_scale, const void* v_cache, const float* v_scale, const int32_t* cu_q,
+                          const int32_t* ctx_len, const int32_t* page_table, int32_t max_pages, int32_t kv_page_size,
+                          int64_t n_phys, void* out, float* lse, void* workspace, size_t ws_bytes, void* stream);
+
 /* Human-readable name of a status code (static string). */
 const char* lsa_status_string(int32_t status);
 

@@ -15,8 +15,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "liblsa.so")
 SERVE = os.path.join(HERE, "_serve.so")
-SOURCES = ["indexer.hip", "attention.hip", "append.hip", "cache_read.hip", "decode_attn.hip", "lsa_api.cpp", "serve_api.cpp",
-           "prompt_api.cpp"]
+SOURCES = ["indexer.hip", "attention.hip", "append.hip", "cache_read.hip", "decode_attn.hip", "prompt_attn.hip", "lsa_api.cpp",
+           "serve_api.cpp", "prompt_api.cpp"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [

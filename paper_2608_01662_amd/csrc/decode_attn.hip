@@ -10,14 +10,11 @@
 #include "attn_tile.hpp"
 #include "device.hpp"
 #include "launch.hpp"
+#include "serve_tile.hpp"
 
 namespace lsa {
 
 constexpr int kTile = 32;  // positions of a tile
-
-// What loads of positions that nobody attends to read instead (behind the context, in unmapped pages): zeros,
-// since a weight of zero does not silence a NaN or an infinity in V.
-__device__ __attribute__((aligned(256))) const uint8_t zero_row[1152] = {};
 
 // The tiles of a sequence that any of its new tokens attends to: 0 .. ns - 1 (the sink) and then ns + skip ..
 struct Span {
@@ -39,9 +36,6 @@ __device__ __forceinline__ Span span_of(const DecodeGeom& g, int ctx) {
   return s;
 }
 
-// (a wave-uniform value that the compiler cannot know to be: kept in a scalar register)
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
 // 2^(s scale - m), the product rounded as where the maximum m was taken: one rounding for both (an fma) leaves the largest
 // score's exponent at m's rounding error, which overflows from scores of 2^31 on.
 __device__ __forceinline__ float exp2_below(float s, float scale, float m) {
@@ -58,17 +52,6 @@ __device__ __forceinline__ f32x4 average(f32x4 acc, float sum) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) y[k] = sum == 0.f ? 0.f : acc[k] * inv;
   return y;
-}
-
-// Inclusive sum over the lanes of a wave.
-__device__ __forceinline__ int wave_scan(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr 1, 2, 4, 8: within rows of 16
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast 15: rows 0 and 2 into 1 and 3
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast 31: row 1 into 2 and 3
-  return x;
 }
 
 // The rows of a sequence that attend to nothing (d: width of an output row).
@@ -164,14 +147,6 @@ __device__ __forceinline__ void deal(const DecodeGeom& g, int d, F&& segment) {
 }
 
 // ---------------------------------------------------------------- direct global -> LDS loads
-// 16 (4) bytes per lane from `src` to LDS bytes lds + 16 (4) lane. The compiler does not see these loads, so
-// that it does not drain them before every LDS read; callers wait with explicit vmcnt counts. M0 holds the LDS
-// address and is restored; the s_nop is the wait state before a load may read it.
-__device__ __forceinline__ void lds_dma16(const uint8_t* src, uint32_t lds) {
-  uint32_t save;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
-               : "=&s"(save) : "v"(src), "s"(lds) : "memory");
-}
 // N <= 4 KB of neighbouring cache rows from `base`: load j takes base + 1024 j + off[j] per lane to LDS bytes lds + 1024 j +
 // 16 lane. (The immediate offset counts for both addresses.)
 template <int N>
@@ -184,19 +159,6 @@ __device__ __forceinline__ void lds_dma16_rows(const uint8_t* base, uint32_t off
   else
     asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024\n\ts_mov_b32 m0, %0"
                  : "=&s"(save) : "s"(base), "v"(off), "v"(off ^ x1), "s"(lds) : "memory");
-}
-__device__ __forceinline__ void lds_dma4(const uint8_t* src, uint32_t lds) {
-  uint32_t save;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %1, off\n\ts_mov_b32 m0, %0"
-               : "=&s"(save) : "v"(src), "s"(lds) : "memory");
-}
-
-// eight e4m3 codes -> eight bf16 (exact)
-__device__ __forceinline__ u32x4 fp8x8_bf16(uint32_t lo, uint32_t hi) {
-  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true))};
 }
 typedef __attribute__((ext_vector_type(2))) int i32x2;
 // Transposed read of 8-bit values: in a 16-lane group, source lane s supplies 8 bytes of row s / 2 (columns

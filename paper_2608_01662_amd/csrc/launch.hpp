@@ -162,6 +162,27 @@ struct CacheReadGeom {
 };
 hipError_t launch_cache_read(const CacheReadGeom& g, hipStream_t st);
 
+// One call of the attention of prompts or chunks (lsa_prefill_attn, lsa_chunk_attn, checked).
+struct PromptGeom {
+  const uint16_t* q;  // [n_tok, H, d_qk], tokens q_stride apart
+  const void *k, *v;  // packed rows [n_kv, Hkv, d], k_stride / v_stride apart, or (with ctx_len) caches [n_phys, Hkv, P, d]
+  int64_t q_stride, k_stride, v_stride;
+  const float *k_scale, *v_scale;
+  const int32_t *cu_q, *cu_kv, *ctx_len, *page_table;
+  uint16_t* out;
+  float* lse;  // or nullptr
+  int64_t n_phys;
+  int n_tok, n_kv, n_seq, H, Hkv, d_qk, d_v, fp8, causal;
+  int max_pages, P, cap;
+  int k_sink, k_swa;  // both below the most keys of a sequence, or 0
+  float scale_log2;   // sm_scale * log2(e)
+  FastDiv by_group, by_page;
+  int64_t items;      // blocks of kPromptRows query rows of all heads, at most
+  int first;          // set by the launcher: first item of the launch
+};
+constexpr int kPromptRows = 256;
+hipError_t launch_prompt_attn(const PromptGeom& g, hipStream_t st);
+
 // One call of the attention over the whole cache (lsa_decode_attn, checked).
 struct DecodeGeom {
   const uint16_t* q;  // [n_seq * R, H, d_qk]

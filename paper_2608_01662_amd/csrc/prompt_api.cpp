@@ -1,4 +1,5 @@
-// C-ABI front end of the prompt side of serving: reading a paged cache back. Argument checks (host only, before any HIP
+// C-ABI front end of the prompt side of serving: reading a paged cache back, attention of packed prompts and of chunks of new
+// tokens over a paged cache. Argument checks (host only, before any HIP
 // call) and launches. See include/lsa.h.
 #include "api_common.hpp"
 #include "launch.hpp"
@@ -20,6 +21,70 @@ lsa_status check_pages(const int32_t* page_table, int32_t n_seq, int32_t max_pag
   LSA_REQUIRE(page_table != nullptr || (max_pages == 1 && n_phys >= n_seq), LSA_ERR_INVALID_ARG,
               "without a page table each sequence has one page: max_pages must be 1 and n_phys >= n_seq");
   return LSA_OK;
+}
+
+lsa_status check_heads(int32_t n_heads, int32_t n_kv_heads, int32_t k_sink, int32_t k_swa, float sm_scale) {
+  LSA_REQUIRE(n_heads >= 1 && n_heads <= 1024 && n_kv_heads >= 1 && n_heads % n_kv_heads == 0, LSA_ERR_INVALID_ARG,
+              "n_heads=%d must be a multiple of n_kv_heads=%d and at most 1024", n_heads, n_kv_heads);
+  LSA_REQUIRE(k_sink >= 0 && k_swa >= 0, LSA_ERR_INVALID_ARG, "k_sink=%d / k_swa=%d must be >= 0", k_sink, k_swa);
+  LSA_REQUIRE(sm_scale > 0.f && sm_scale < 1e30f, LSA_ERR_INVALID_ARG, "sm_scale must be positive and finite");
+  return LSA_OK;
+}
+
+lsa_status check_prefill_params(const lsa_prefill_attn_params* p) {
+  LSA_REQUIRE(p != nullptr, LSA_ERR_INVALID_ARG, "params is NULL");
+  LSA_REQUIRE((p->d_qk == 64 && p->d_v == 64) || (p->d_qk == 128 && p->d_v == 128) || (p->d_qk == 192 && p->d_v == 128),
+              LSA_ERR_UNSUPPORTED, "attention shape (d_qk=%d, d_v=%d) not supported; use (64,64), (128,128) or (192,128)", p->d_qk,
+              p->d_v);
+  LSA_REQUIRE(p->causal == 0 || p->causal == 1, LSA_ERR_INVALID_ARG, "causal=%d must be 0 or 1", p->causal);
+  LSA_REQUIRE(p->causal || (p->k_swa == 0 && p->k_sink == 0), LSA_ERR_UNSUPPORTED, "a window and a sink need causal = 1");
+  return check_heads(p->n_heads, p->n_kv_heads, p->k_sink, p->k_swa, p->sm_scale);
+}
+
+lsa_status check_chunk_params(const lsa_decode_attn_params* p) {
+  LSA_REQUIRE(p != nullptr, LSA_ERR_INVALID_ARG, "params is NULL");
+  LSA_REQUIRE(p->latent == 0 || p->latent == 1, LSA_ERR_INVALID_ARG, "latent=%d must be 0 or 1", p->latent);
+  LSA_REQUIRE(p->latent == 0 && (p->d_qk == 64 || p->d_qk == 128) && p->d_v == p->d_qk, LSA_ERR_UNSUPPORTED,
+              "attention shape (d_qk=%d, d_v=%d, latent=%d) not supported; use (64,64) or (128,128), not latent", p->d_qk, p->d_v,
+              p->latent);
+  LSA_REQUIRE(p->key_dtype == LSA_KEY_BF16 || p->key_dtype == LSA_KEY_FP8_E4M3FN, LSA_ERR_INVALID_ARG, "key_dtype=%d unknown",
+              p->key_dtype);
+  return check_heads(p->n_heads, p->n_kv_heads, p->k_sink, p->k_swa, p->sm_scale);
+}
+
+lsa_status check_tokens(int32_t n_seq, int64_t n_tok, int32_t n_heads, int32_t n_kv_heads) {
+  LSA_REQUIRE(n_seq >= 0 && n_tok >= 0, LSA_ERR_INVALID_ARG, "n_seq=%d / n_tok=%lld < 0", n_seq, (long long)n_tok);
+  LSA_REQUIRE(n_tok < (1LL << 30) && n_tok * n_heads < (1LL << 30) && (int64_t)n_seq * n_kv_heads < (1LL << 24), LSA_ERR_UNSUPPORTED,
+              "n_tok * n_heads must be < 2^30 and n_seq * n_kv_heads < 2^24");
+  return LSA_OK;
+}
+
+lsa_status check_rows(const char* name, const void* x, int64_t stride, int64_t heads, int64_t width) {
+  LSA_REQUIRE(x != nullptr, LSA_ERR_INVALID_ARG, "%s is NULL", name);
+  LSA_REQUIRE(aligned(x, 16) && stride % 8 == 0, LSA_ERR_INVALID_ARG,
+              "%s must be 16-byte aligned and its stride (%lld) a multiple of 8", name, (long long)stride);
+  LSA_REQUIRE(stride >= heads * width, LSA_ERR_INVALID_ARG, "%s: a stride of %lld is less than a row's %lld elements", name,
+              (long long)stride, (long long)(heads * width));
+  LSA_REQUIRE(stride < (1LL << 24), LSA_ERR_UNSUPPORTED, "%s: a stride of %lld is not below 2^24", name, (long long)stride);
+  return LSA_OK;
+}
+
+// What both attentions have of their sizes.
+void set_heads(lsa::PromptGeom& g, int32_t n_seq, int64_t n_tok, int32_t n_heads, int32_t n_kv_heads, int32_t d_qk, int32_t d_v,
+               int32_t k_sink, int32_t k_swa, int64_t most_keys, float sm_scale) {
+  g.n_seq = n_seq;
+  g.n_tok = (int)n_tok;
+  g.H = n_heads;
+  g.Hkv = n_kv_heads;
+  g.d_qk = d_qk;
+  g.d_v = d_v;
+  // (a window of all positions is none, and without a window there is no separate sink)
+  g.k_swa = k_swa < most_keys ? k_swa : 0;
+  g.k_sink = g.k_swa == 0 ? 0 : (int)(k_sink < most_keys ? k_sink : most_keys);
+  g.scale_log2 = sm_scale * 1.4426950408889634f;
+  g.by_group = lsa::fast_div((uint32_t)(n_heads / n_kv_heads));
+  // blocks of query rows: a sequence's last one of each head may be partly filled
+  g.items = n_kv_heads * (n_tok * (n_heads / n_kv_heads) / lsa::kPromptRows + (n_seq < n_tok ? n_seq : n_tok));
 }
 
 }  // namespace
@@ -75,6 +140,100 @@ lsa_status lsa_cache_read(const lsa_cache_read_params* p, int64_t n_tok, int32_t
   g.P = kv_page_size;
   const hipError_t e = lsa::launch_cache_read(g, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "cache read");
+  return LSA_OK;
+}
+
+size_t lsa_prefill_attn_workspace_size(const lsa_prefill_attn_params* p, int32_t n_seq, int64_t n_tok, int64_t n_kv) {
+  return 0;
+}
+
+lsa_status lsa_prefill_attn(const lsa_prefill_attn_params* p, int32_t n_seq, int64_t n_tok, int64_t n_kv, const void* q,
+                            int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                            const int32_t* cu_q, const int32_t* cu_kv, void* out, float* lse, void* workspace, size_t ws_bytes,
+                            void* stream) {
+  g_err[0] = 0;
+  lsa_status s = check_prefill_params(p);
+  if (s != LSA_OK) return s;
+  s = check_tokens(n_seq, n_tok, p->n_heads, p->n_kv_heads);
+  if (s != LSA_OK) return s;
+  LSA_REQUIRE(n_kv >= 0, LSA_ERR_INVALID_ARG, "n_kv=%lld < 0", (long long)n_kv);
+  LSA_REQUIRE(n_kv < (1LL << 31), LSA_ERR_UNSUPPORTED, "n_kv must be < 2^31");
+  if (n_tok == 0 || n_seq == 0) return LSA_OK;  // nothing to read or write
+  LSA_REQUIRE(cu_q && out, LSA_ERR_INVALID_ARG, "cu_q and out must be non-NULL");
+  LSA_REQUIRE(cu_kv != nullptr || n_kv == n_tok, LSA_ERR_INVALID_ARG, "without cu_kv the keys are the tokens': n_kv must be n_tok");
+  s = check_rows("q", q, q_stride, p->n_heads, p->d_qk);
+  if (s == LSA_OK && n_kv > 0) s = check_rows("k", k, k_stride, p->n_kv_heads, p->d_qk);
+  if (s == LSA_OK && n_kv > 0) s = check_rows("v", v, v_stride, p->n_kv_heads, p->d_v);
+  if (s != LSA_OK) return s;
+  LSA_REQUIRE(aligned(out, 16) && aligned(cu_q, 4) && aligned(cu_kv, 4) && aligned(lse, 4), LSA_ERR_INVALID_ARG,
+              "out must be 16-byte aligned, cu_q, cu_kv and lse 4-byte");
+  lsa::PromptGeom g{};
+  g.q = static_cast<const uint16_t*>(q);
+  g.k = k;
+  g.v = v;
+  g.q_stride = q_stride;
+  g.k_stride = k_stride;
+  g.v_stride = v_stride;
+  g.cu_q = cu_q;
+  g.cu_kv = cu_kv ? cu_kv : cu_q;
+  g.out = static_cast<uint16_t*>(out);
+  g.lse = lse;
+  g.n_kv = (int)n_kv;
+  g.causal = p->causal;
+  set_heads(g, n_seq, n_tok, p->n_heads, p->n_kv_heads, p->d_qk, p->d_v, p->k_sink, p->k_swa, n_kv, p->sm_scale);
+  const hipError_t e = lsa::launch_prompt_attn(g, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "prefill attention");
+  return LSA_OK;
+}
+
+size_t lsa_chunk_attn_workspace_size(const lsa_decode_attn_params* p, int32_t n_seq, int64_t n_tok, int32_t max_pages,
+                                     int32_t kv_page_size) {
+  return 0;
+}
+
+lsa_status lsa_chunk_attn(const lsa_decode_attn_params* p, int32_t n_seq, int64_t n_tok, const void* q, const void* k_cache,
+                          const float* k_scale, const void* v_cache, const float* v_scale, const int32_t* cu_q,
+                          const int32_t* ctx_len, const int32_t* page_table, int32_t max_pages, int32_t kv_page_size,
+                          int64_t n_phys, void* out, float* lse, void* workspace, size_t ws_bytes, void* stream) {
+  g_err[0] = 0;
+  lsa_status s = check_chunk_params(p);
+  if (s != LSA_OK) return s;
+  s = check_tokens(n_seq, n_tok, p->n_heads, p->n_kv_heads);
+  if (s != LSA_OK) return s;
+  if (n_tok == 0 || n_seq == 0) return LSA_OK;  // nothing to read or write
+  s = check_pages(page_table, n_seq, max_pages, kv_page_size, n_phys, p->n_kv_heads);
+  if (s != LSA_OK) return s;
+  const bool fp8 = p->key_dtype == LSA_KEY_FP8_E4M3FN;
+  LSA_REQUIRE(q && k_cache && v_cache && cu_q && ctx_len && out, LSA_ERR_INVALID_ARG,
+              "q, k_cache, v_cache, cu_q, ctx_len and out must be non-NULL");
+  LSA_REQUIRE(fp8 == (k_scale != nullptr) && fp8 == (v_scale != nullptr), LSA_ERR_INVALID_ARG,
+              "k_scale and v_scale must be given exactly for fp8 caches");
+  LSA_REQUIRE(aligned(q, 16) && aligned(k_cache, 16) && aligned(v_cache, 16) && aligned(out, 16), LSA_ERR_INVALID_ARG,
+              "q, k_cache, v_cache and out must be 16-byte aligned");
+  LSA_REQUIRE(aligned(k_scale, 4) && aligned(v_scale, 4) && aligned(cu_q, 4) && aligned(ctx_len, 4) && aligned(page_table, 4) && aligned(lse, 4),
+              LSA_ERR_INVALID_ARG, "scales, cu_q, ctx_len, page_table and lse must be 4-byte aligned");
+  lsa::PromptGeom g{};
+  g.q = static_cast<const uint16_t*>(q);
+  g.q_stride = (int64_t)p->n_heads * p->d_qk;
+  g.k = k_cache;
+  g.v = v_cache;
+  g.k_scale = k_scale;
+  g.v_scale = v_scale;
+  g.cu_q = cu_q;
+  g.ctx_len = ctx_len;
+  g.page_table = page_table;
+  g.out = static_cast<uint16_t*>(out);
+  g.lse = lse;
+  g.n_phys = n_phys;
+  g.fp8 = fp8;
+  g.causal = 1;
+  g.max_pages = max_pages;
+  g.P = kv_page_size;
+  g.cap = max_pages * kv_page_size;
+  g.by_page = lsa::fast_div((uint32_t)kv_page_size);
+  set_heads(g, n_seq, n_tok, p->n_heads, p->n_kv_heads, p->d_qk, p->d_v, p->k_sink, p->k_swa, g.cap, p->sm_scale);
+  const hipError_t e = lsa::launch_prompt_attn(g, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "chunk attention");
   return LSA_OK;
 }
 

@@ -67,6 +67,11 @@ class _DecodeAttnParams(ctypes.Structure):
                [("sm_scale", ctypes.c_float)]
 
 
+class _PrefillAttnParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_heads", "n_kv_heads", "d_qk", "d_v", "causal", "k_sink", "k_swa")] + \
+               [("sm_scale", ctypes.c_float)]
+
+
 @dataclass(frozen=True)
 class IndexParams:
     """Indexer hyper-parameters (Sec. 3.1 and 3.3 of the paper); see lsa_index_params."""
@@ -150,8 +155,25 @@ class CacheReadParams:
 
 
 @dataclass(frozen=True)
+class PrefillAttnParams:
+    """Attention of packed prompts over packed keys and values; see lsa_prefill_attn_params."""
+    n_heads: int
+    n_kv_heads: int
+    d_qk: int
+    d_v: int
+    sm_scale: float
+    causal: bool = True
+    k_sink: int = 0          # with k_swa > 0: the first positions are attended as well
+    k_swa: int = 0           # 0: every position up to the query's; else the last k_swa
+
+    def c(self) -> _PrefillAttnParams:
+        return _PrefillAttnParams(*_int32(n_heads=self.n_heads, n_kv_heads=self.n_kv_heads, d_qk=self.d_qk, d_v=self.d_v),
+                                  int(self.causal), *_int32(k_sink=self.k_sink, k_swa=self.k_swa), self.sm_scale)
+
+
+@dataclass(frozen=True)
 class DecodeAttnParams:
-    """Attention of new tokens over a whole paged cache; see lsa_decode_attn_params."""
+    """Attention of new tokens over a whole paged cache; see lsa_decode_attn_params (latent: decode_attn only)."""
     n_heads: int
     n_kv_heads: int
     d_qk: int
@@ -232,6 +254,16 @@ def lib() -> ctypes.CDLL:
         L.lsa_decode_attn.argtypes = [D, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i64, _vp, _vp, _vp,
                                       _sz, _vp]
         L.lsa_decode_attn.restype = _i32
+        F = ctypes.POINTER(_PrefillAttnParams)
+        L.lsa_prefill_attn_workspace_size.argtypes = [F, _i32, _i64, _i64]
+        L.lsa_prefill_attn_workspace_size.restype = _sz
+        L.lsa_prefill_attn.argtypes = [F, _i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+        L.lsa_prefill_attn.restype = _i32
+        L.lsa_chunk_attn_workspace_size.argtypes = [D, _i32, _i64, _i32, _i32]
+        L.lsa_chunk_attn_workspace_size.restype = _sz
+        L.lsa_chunk_attn.argtypes = [D, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i64, _vp, _vp, _vp, _sz,
+                                     _vp]
+        L.lsa_chunk_attn.restype = _i32
         L.lsa_status_string.argtypes = [_i32]
         L.lsa_status_string.restype = ctypes.c_char_p
         L.lsa_last_error.argtypes = []
@@ -920,6 +952,99 @@ def decode_attn(prm: DecodeAttnParams, q: torch.Tensor, k_cache: torch.Tensor, v
                                _p(lse), _p(workspace), wsb, _stream(dev))
     if st != 0:
         _check(st, "lsa_decode_attn")
+    return out, lse
+
+
+def _row_outputs(n_rows: int, heads: int, d_v: int, out, lse, device):
+    """out [n_rows, heads, d_v] and lse [n_rows, heads] or None, made where they are not given."""
+    if out is None:
+        out = torch.empty((n_rows, heads, d_v), dtype=torch.bfloat16, device=device)
+    else:
+        _need("out", out, _BF16, (n_rows, heads, d_v), device)
+    if lse is True:
+        lse = torch.empty((n_rows, heads), dtype=torch.float32, device=device)
+    elif lse is False or lse is None:
+        lse = None
+    else:
+        _need("lse", lse, _F32, (n_rows, heads), device)
+    return out, lse
+
+
+def prefill_attn_workspace_size(prm: PrefillAttnParams, n_seq: int, n_tok: int, n_kv: int) -> int:
+    _int32(n_seq=n_seq)
+    return lib().lsa_prefill_attn_workspace_size(_ref(prm), n_seq, n_tok, n_kv)
+
+
+def prefill_attn(prm: PrefillAttnParams, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor,
+                 cu_kv: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                 lse: torch.Tensor | bool | None = True, workspace: torch.Tensor | None = None):
+    """Attention of packed prompts, or of their last parts, over packed keys and values (lsa_prefill_attn). Returns (out
+    [n_tok, H, d_v] bf16, lse [n_tok, H] fp32 or None).
+
+    q [n_tok, H, d_qk], k [n_kv, n_kv_heads, d_qk], v [n_kv, n_kv_heads, d_v]: bf16 with any token stride. Sequence b has the
+    tokens cu_q[b] .. cu_q[b + 1] - 1 and the keys cu_kv[b] .. cu_kv[b + 1] - 1 (None: those of its tokens), the tokens
+    being its last positions. Rows of no sequence are left as they are."""
+    H, nk = prm.n_heads, prm.n_kv_heads
+    is_tensor = isinstance(q, torch.Tensor)
+    dev, i = (q.device, q.get_device()) if is_tensor else (None, -1)
+    n = q.shape[0] if is_tensor and q.dim() == 3 else None
+    qs = _tokens("q", q, n, H, prm.d_qk, dev, i)
+    n_kv = k.shape[0] if isinstance(k, torch.Tensor) and k.dim() == 3 else None
+    ks = _tokens("k", k, n_kv, nk, prm.d_qk, dev, i)
+    vs = _tokens("v", v, n_kv, nk, prm.d_v, dev, i)
+    n_seq = _offsets("cu_q", cu_q, dev)
+    _need_opt("cu_kv", cu_kv, _I32, (n_seq + 1,), dev)
+    if cu_kv is None and n_kv != n:
+        raise ValueError(f"without cu_kv the keys are the tokens', but k has {n_kv} rows and q {n}")
+    out, lse = _row_outputs(n, H, prm.d_v, out, lse, dev)
+    _int32(sequences=n_seq)
+    L, ref = _lib or lib(), _ref(prm)
+    ws, wsb = _workspace(L.lsa_prefill_attn_workspace_size(ref, n_seq, n, n_kv), dev, workspace)
+    with torch.cuda.device(dev):
+        st = L.lsa_prefill_attn(ref, n_seq, n, n_kv, _p(q), qs, _p(k), ks, _p(v), vs, _p(cu_q), _p(cu_kv), _p(out), _p(lse), _p(ws), wsb,
+                                _stream(dev))
+    if st != 0:
+        _check(st, "lsa_prefill_attn")
+    return out, lse
+
+
+def chunk_attn_workspace_size(prm: DecodeAttnParams, n_seq: int, n_tok: int, max_pages: int, kv_page_size: int) -> int:
+    _int32(n_seq=n_seq, max_pages=max_pages, kv_page_size=kv_page_size)
+    return lib().lsa_chunk_attn_workspace_size(_ref(prm), n_seq, n_tok, max_pages, kv_page_size)
+
+
+def chunk_attn(prm: DecodeAttnParams, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, cu_q: torch.Tensor,
+               ctx_len: torch.Tensor, page_table: torch.Tensor | None = None, k_scale: torch.Tensor | None = None,
+               v_scale: torch.Tensor | None = None, out: torch.Tensor | None = None,
+               lse: torch.Tensor | bool | None = True, workspace: torch.Tensor | None = None):
+    """Attention of chunks of new tokens, any number of every sequence, over their cached contexts (lsa_chunk_attn). Returns (out
+    [n_tok, H, d_v] bf16, lse [n_tok, H] fp32 or None).
+
+    Sequence b has the tokens cu_q[b] .. cu_q[b + 1] - 1 of q, the newest of its ctx_len[b]. Caches as cache_append writes them;
+    prm as for decode_attn, not latent. Rows of no sequence are left as they are."""
+    H, nk, d, fp8 = prm.n_heads, prm.n_kv_heads, prm.d_qk, prm.fp8
+    n = q.shape[0] if isinstance(q, torch.Tensor) and q.dim() == 3 else None
+    _need("q", q, _BF16, (n, H, d))
+    dev = q.device
+    n_phys, page = _paged_shape("k_cache", k_cache, fp8, nk, d, dev)
+    _paged_like("v_cache", v_cache, fp8, n_phys, nk, page, prm.d_v, dev)
+    if fp8:
+        _cache_scale("k_scale", k_scale, n_phys, nk, page, dev)
+        _cache_scale("v_scale", v_scale, n_phys, nk, page, dev)
+    elif k_scale is not None or v_scale is not None:
+        raise ValueError("k_scale and v_scale must be None for bf16 caches")
+    n_seq = _offsets("cu_q", cu_q, dev)
+    _need("ctx_len", ctx_len, _I32, (n_seq,), dev)
+    max_pages = _table_width(page_table, n_seq, dev)
+    out, lse = _row_outputs(n, H, prm.d_v, out, lse, dev)
+    _int32(sequences=n_seq, max_pages=max_pages, page=page)
+    L, ref = _lib or lib(), _ref(prm)
+    ws, wsb = _workspace(L.lsa_chunk_attn_workspace_size(ref, n_seq, n, max_pages, page), dev, workspace)
+    with torch.cuda.device(dev):
+        st = L.lsa_chunk_attn(ref, n_seq, n, _p(q), _p(k_cache), _p(k_scale), _p(v_cache), _p(v_scale), _p(cu_q), _p(ctx_len),
+                              _p(page_table), max_pages, page, n_phys, _p(out), _p(lse), _p(ws), wsb, _stream(dev))
+    if st != 0:
+        _check(st, "lsa_chunk_attn")
     return out, lse
 
 
