@@ -177,10 +177,11 @@ struct PromptGeom {
   int k_sink, k_swa;  // both below the most keys of a sequence, or 0
   float scale_log2;   // sm_scale * log2(e)
   FastDiv by_group, by_page;
+  int pass_tiles;     // tiles whose page-table entries fit the LDS area
   int64_t items;      // blocks of kPromptRows query rows of all heads, at most
   int first;          // set by the launcher: first item of the launch
 };
-constexpr int kPromptRows = 256;
+constexpr int kPromptRows = 256, kPromptKeys = 64, kPromptPages = 2048;
 hipError_t launch_prompt_attn(const PromptGeom& g, hipStream_t st);
 
 // One call of the attention over the whole cache (lsa_decode_attn, checked).

@@ -231,6 +231,8 @@ lsa_status lsa_chunk_attn(const lsa_decode_attn_params* p, int32_t n_seq, int64_
   g.P = kv_page_size;
   g.cap = max_pages * kv_page_size;
   g.by_page = lsa::fast_div((uint32_t)kv_page_size);
+  const int64_t pass = (int64_t)(lsa::kPromptPages - 2) * kv_page_size / lsa::kPromptKeys;  // (two pages more at the ends)
+  g.pass_tiles = (int)(pass < (1 << 26) ? pass : (1 << 26));
   set_heads(g, n_seq, n_tok, p->n_heads, p->n_kv_heads, p->d_qk, p->d_v, p->k_sink, p->k_swa, g.cap, p->sm_scale);
   const hipError_t e = lsa::launch_prompt_attn(g, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "chunk attention");

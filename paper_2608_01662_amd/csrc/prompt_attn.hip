@@ -13,8 +13,8 @@
 namespace lsa {
 
 constexpr int kRows = kPromptRows;  // query rows of a workgroup
-constexpr int kKeys = 64;           // keys of a tile
-constexpr int kThreads = 256;
+constexpr int kKeys = kPromptKeys;  // keys of a tile
+constexpr int kPageSlots = kPromptPages;  // page-table entries staged in LDS at a time
 
 // Where 16-byte chunk c of row r of a tile lies: slot c ^ swz(r) of the row. The reads of a product's K operand (16 rows of one
 // chunk at a time) and the transposed reads of V (4 rows of 4 chunks) then fall on all banks alike: rows of 256
@@ -32,7 +32,6 @@ struct Share {
   int n, c;         // new tokens and keys of the sequence
   int64_t q0, kv0;  // its first token, its first key of contiguous ones
   int ns, skip, nt;
-  int clear0, clear1;  // tiles [clear0, clear1) of the span are attended to whole by every row
 };
 
 __device__ __forceinline__ int new_tokens(const PromptGeom& g, int b, int& first) {
@@ -91,220 +90,102 @@ __device__ __forceinline__ float swap32(float x) {  // the value of lane l ^ 32
   return __shfl_xor(x, 32);
 }
 
-template <int DQK, int DV, int KIND>  // KIND 0: contiguous bf16, 1: paged bf16, 2: paged fp8
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void prompt_attn_kernel(PromptGeom g) {
-  constexpr int CK = DQK / 8, CV = DV / 8, KS = DQK / 16, DB = DV / 32, NQ = 2;
-  constexpr bool FP8 = KIND == 2;
-  __shared__ __attribute__((aligned(1024))) uint8_t lk[kKeys * DQK * 2], lv[kKeys * DV * 2];
-  __shared__ __attribute__((aligned(16))) float scales[FP8 ? 2 : 1][FP8 ? kKeys : 1];
-  __shared__ int mapped[kKeys];
-  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5, l32 = lane & 31;
-  Share w;
-  if (!find_share(g, g.first + (int)blockIdx.x, w)) return;
-  const int group = (int)g.by_group.d, wrow = w.row0 + 64 * wave;
-  const bool active = wrow < w.rows;
-
-  u32x4 qf[NQ][KS];
-  int t[NQ];
-#pragma unroll
-  for (int nq = 0; nq < NQ; ++nq) {
-    const int row = wrow + 32 * nq + l32, r = row < w.rows ? row : w.rows - 1, j = fdiv(g.by_group, r);
-    t[nq] = g.causal ? w.c - w.n + j : w.c - 1;
-    const uint16_t* p = g.q + (w.q0 + j) * g.q_stride + (int64_t)(w.head * group + r - j * group) * DQK + 8 * h;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) qf[nq][s] = *reinterpret_cast<const u32x4*>(p + 16 * s);
-  }
-  f32x16 o[DB][NQ];
-  float m[NQ], l[NQ];
-#pragma unroll
-  for (int nq = 0; nq < NQ; ++nq) {
-    m[nq] = kNoRef;
-    l[nq] = 0.f;
-#pragma unroll
-    for (int d = 0; d < DB; ++d) o[d][nq] = f32x16{};
-  }
-  // LDS offsets of this lane's operands
-  int k_off[KS], v_off[2][DB];
-#pragma unroll
-  for (int s = 0; s < KS; ++s) k_off[s] = l32 * DQK * 2 + (((2 * s + h) ^ swz<CK>(l32)) << 4);
-  {
-    const int i = lane & 15, cc = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+// ---------------------------------------------------------------- sizes, LDS layout, operand offsets
+template <int DQK, int DV, int KIND, int NQ_>  // KIND 0: contiguous bf16, 1: paged bf16, 2: paged fp8; blocks of 32 rows of a wave
+struct Prompt {
+  static constexpr bool FP8 = KIND == 2;
+  static constexpr int NQ = NQ_, kWaves = kRows / (32 * NQ), kThreads = 64 * kWaves;
+  static constexpr int CK = DQK / 8, CV = DV / 8, KS = DQK / 16, DB = DV / 32;
+  static constexpr int kK = kKeys * DQK * 2, kV = kKeys * DV * 2;  // bytes of a tile
+  static constexpr int kLoadsK = kK / 1024 / kWaves, kLoadsV = kV / 1024 / kWaves;   // direct loads of a wave
+  // Tile buffers. Step i reads keys i and i + 1 and values i - 1 and i, while tiles up to i + kLead are on their way (of fp8 caches
+  // the last of them in registers): as many as fit.
+  static constexpr int kLead = DQK == 192 ? 2 : 3, kBufsK = FP8 ? 3 : kLead + 1, kBufsV = FP8 ? 4 : kLead + 2;
+  struct Lds {
+    uint8_t k[kBufsK][kK], v[kBufsV][kV];
+    float scales[FP8 ? kBufsV : 1][2][FP8 ? kKeys : 4];  // of keys (times the softmax scale) and of values
+    int pages[KIND ? kPageSlots : 1];
+  };
+  // LDS offsets of this lane's operands in a tile: of K at k-step 0 (at s: ^ 32 s, or by 4 k-steps), of the first four and of the second four values
+  // of a k-step in block 0 (in d: ^ 64 d).
+  int k_off, v_off[2];
+  __device__ __forceinline__ explicit Prompt(int lane) {
+    const int h = lane >> 5, l32 = lane & 31, i = lane & 15, cc = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+    k_off = l32 * DQK * 2 + ((h ^ swz<CK>(l32)) << 4);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const int row = 8 * half + 4 * h + (i >> 2);
-#pragma unroll
-      for (int d = 0; d < DB; ++d) v_off[half][d] = row * DV * 2 + (((4 * d + cc) ^ swz<CV>(row)) << 4) + 8 * (i & 1);
+      v_off[half] = row * DV * 2 + ((cc ^ swz<CV>(row)) << 4) + 8 * (i & 1);
     }
   }
+  // (in a loop over tiles: the operands' addresses are made from these where they are used, one instruction each; kept over the loop,
+  // as the compiler would have them, they take the registers of the accumulators)
+  __device__ __forceinline__ void refresh() { asm volatile("" : "+v"(k_off), "+v"(v_off[0]), "+v"(v_off[1])); }
+  // The K operand of a k-step, and the V operand of a block of 32 dims: `at` is the LDS address of the tile's half (a multiple of
+  // 256, and a row starts at a multiple of what the exclusive or reaches) and for V of the k-step's first key.
+  __device__ __forceinline__ u32x4 k_operand(const uint8_t* at, int s) const {
+    constexpr int X = CK == 16 ? 8 : 4;  // k-steps that the exclusive or of the chunks reaches
+    const uint32_t p = (((uint32_t)(uintptr_t)at + (uint32_t)k_off) ^ (uint32_t)(32 * (s % X))) + 32 * X * (s / X);
+    return *(const __attribute__((address_space(3))) u32x4*)(p);
+  }
+  __device__ __forceinline__ u32x4 v_operand(const uint8_t* at, int ks, int d) const {
+    u32x2 y[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const uint32_t p = (((uint32_t)(uintptr_t)at + (uint32_t)v_off[half]) ^ (uint32_t)(64 * d)) + 16 * ks * DV * 2;
+      y[half] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p)));
+    }
+    return u32x4{y[0].x, y[0].y, y[1].x, y[1].y};
+  }
+};
 
-  for (int i = 0; i < w.nt; ++i) {
-    const int s0 = (i < w.ns ? i : i + w.skip) * kKeys;
-    __syncthreads();
-    // row of the cache (or of the packed keys) of a key, -1: none
-    auto row_of = [&](int key) -> int64_t {
-      const uint32_t s = (uint32_t)s0 + key;
-      if (s >= (uint32_t)w.c) return -1;
-      if constexpr (KIND == 0) return w.kv0 + s;
-      const int pg = fdiv(g.by_page, (int)s);
-      const int64_t ph = g.page_table ? g.page_table[(int64_t)w.b * g.max_pages + pg] : w.b;
-      return ph >= 0 && ph < g.n_phys ? (ph * g.Hkv + w.head) * g.P + ((int)s - pg * g.P) : -1;
-    };
-    auto load = [&](const void* base, int64_t stride, uint8_t* dst, auto width) {
-      constexpr int D = decltype(width)::value, C = D / 8;
-      if constexpr (FP8) {
-        for (int e = (int)threadIdx.x; e < kKeys * (D / 16); e += kThreads) {
-          const int r = e / (D / 16), u = e % (D / 16);
-          const int64_t row = row_of(r);
-          u32x4 x{};
-          if (row >= 0) x = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(base) + row * D + 16 * u);
-          *reinterpret_cast<u32x4*>(dst + r * D * 2 + (((2 * u) ^ swz<C>(r)) << 4)) = fp8x8_bf16(x.x, x.y);
-          *reinterpret_cast<u32x4*>(dst + r * D * 2 + (((2 * u + 1) ^ swz<C>(r)) << 4)) = fp8x8_bf16(x.z, x.w);
-        }
-      } else {
-        for (int e = (int)threadIdx.x; e < kKeys * C; e += kThreads) {
-          const int r = e / C, c = e % C;
-          const int64_t row = row_of(r);
-          u32x4 x{};
-          if (row >= 0) x = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(base) + row * stride + 8 * c);
-          *reinterpret_cast<u32x4*>(dst + r * D * 2 + ((c ^ swz<C>(r)) << 4)) = x;
-        }
-      }
-    };
-    load(KIND ? g.k : static_cast<const void*>(static_cast<const uint16_t*>(g.k) + w.head * DQK), KIND ? DQK : g.k_stride, lk,
-         std::integral_constant<int, DQK>{});
-    load(KIND ? g.v : static_cast<const void*>(static_cast<const uint16_t*>(g.v) + w.head * DV), KIND ? DV : g.v_stride, lv,
-         std::integral_constant<int, DV>{});
-    if (threadIdx.x < kKeys) {
-      const int64_t row = row_of((int)threadIdx.x);
-      mapped[threadIdx.x] = row >= 0;
-      if constexpr (FP8) {
-        scales[0][threadIdx.x] = row >= 0 ? g.k_scale[row] : 0.f;
-        scales[1][threadIdx.x] = row >= 0 ? g.v_scale[row] : 0.f;
-      }
-    }
-    __syncthreads();
-    if (!active) continue;
-    const uint64_t there = __ballot(mapped[lane] != 0);
-    f32x16 s[2][NQ];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int nq = 0; nq < NQ; ++nq) s[kb][nq] = f32x16{};
-#pragma unroll
-    for (int st = 0; st < KS; ++st)
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        const u32x4 a = *reinterpret_cast<const u32x4*>(lk + k_off[st] + kb * 32 * DQK * 2);
-#pragma unroll
-        for (int nq = 0; nq < NQ; ++nq) s[kb][nq] = mfma32(a, qf[nq][st], s[kb][nq]);
-      }
-    u32x4 p[2][2][NQ];      // [key block][k-step of 16]
-    uint32_t live[2][NQ];   // scores that are not -inf
-#pragma unroll
-    for (int nq = 0; nq < NQ; ++nq) {
-      float top = -INFINITY;
-      const int rel = t[nq] - s0, win = g.k_swa > 0 ? rel - g.k_swa : -1, sink = g.k_swa > 0 ? g.k_sink - s0 : 0;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = 32 * kb + 8 * (r >> 2) + 4 * h + (r & 3);
-          const bool seen = key <= rel && (key > win || key < sink) && ((there >> key) & 1);
-          float z = s[kb][nq][r] * g.scale_log2;
-          if constexpr (FP8) z *= scales[0][key];
-          s[kb][nq][r] = seen ? z : -INFINITY;
-          top = fmaxf(top, s[kb][nq][r]);
-        }
-      top = fmaxf(top, swap32(top));
-      const bool grown = top > m[nq] + kLazy;
-      if (__any(grown)) {  // (each row by its own scores, whatever the wave's others do)
-        const float mn = grown ? top : m[nq], al = fast_exp2(m[nq] - mn);
-        m[nq] = mn;
-        l[nq] *= al;
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[d][nq][r] *= al;
-      }
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        live[kb][nq] = 0;
-#pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-          float e[2];
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const float z = s[kb][nq][r + k];
-            const bool in = z != -INFINITY;
-            if (in) live[kb][nq] |= 1u << (r + k);
-            e[k] = fast_exp2(z - m[nq]);
-            l[nq] += e[k];
-            if constexpr (FP8) e[k] = in ? e[k] * scales[1][32 * kb + 8 * (r >> 2) + 4 * h + ((r + k) & 3)] : 0.f;
-          }
-          p[kb][r >> 3][nq][(r & 7) >> 1] = pack_bf16x2(e[0], e[1]);
-        }
-      }
-    }
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          const uint8_t* base = lv + (32 * kb + 16 * ks) * DV * 2;
-          u32x4 a = tr16_pair(base + v_off[0][d], base + v_off[1][d]);
-          // Values that are no finite numbers, of keys that some row attends to and others do not: a weight of 0 does not
-          // silence them, so they are taken out of the product and added where they belong.
-          uint32_t odd = 0;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) odd |= ((a[k] & 0x7F80u) == 0x7F80u) | ((a[k] & 0x7F800000u) == 0x7F800000u);
-          if (__any(odd)) {
-            u32x4 up{}, down{}, fin = a;
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-              for (int half = 0; half < 2; ++half) {
-                const uint32_t v = (a[k] >> (16 * half)) & 0xFFFFu;
-                if ((v & 0x7F80u) == 0x7F80u) {
-                  const bool nan = (v & 0x7Fu) != 0;
-                  fin[k] &= half ? 0xFFFFu : 0xFFFF0000u;
-                  if (nan || !(v & 0x8000u)) up[k] |= 0x3F80u << (16 * half);
-                  if (nan || (v & 0x8000u)) down[k] |= 0x3F80u << (16 * half);
-                }
-              }
-#pragma unroll
-            for (int nq = 0; nq < NQ; ++nq) {
-              u32x4 one;
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const uint32_t bits = live[kb][nq] >> (8 * ks + 2 * k);
-                one[k] = (bits & 1 ? 0x3F80u : 0u) | (bits & 2 ? 0x3F800000u : 0u);
-              }
-              o[d][nq] = mfma32(fin, p[kb][ks][nq], o[d][nq]);
-              const f32x16 plus = mfma32(up, one, f32x16{}), minus = mfma32(down, one, f32x16{});
-#pragma unroll
-              for (int r = 0; r < 16; ++r) {
-                if (plus[r] > 0.f) o[d][nq][r] += INFINITY;
-                if (minus[r] > 0.f) o[d][nq][r] -= INFINITY;
-              }
-            }
-          } else {
-#pragma unroll
-            for (int nq = 0; nq < NQ; ++nq) o[d][nq] = mfma32(a, p[kb][ks][nq], o[d][nq]);
-          }
-        }
-  }
-  if (!active) return;
+// The first n of 32 bits.
+__device__ __forceinline__ uint32_t first_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+
+// This lane's query rows.
+template <int NQ, int KS>
+struct Queries {
+  u32x4 q[NQ][KS];  // B operands: columns are rows, dims of k-step s
+  int t[NQ];        // position of the row's token, -1 and less: none
+};
+template <int NQ, int DQK>
+__device__ __forceinline__ Queries<NQ, DQK / 16> load_queries(const PromptGeom& g, const Share& w, int wrow, int lane) {
+  Queries<NQ, DQK / 16> x;
+  const int group = (int)g.by_group.d;
 #pragma unroll
   for (int nq = 0; nq < NQ; ++nq) {
-    const int row = wrow + 32 * nq + l32;
+    const int row = wrow + 32 * nq + (lane & 31), r = row < w.rows ? row : w.rows - 1, j = fdiv(g.by_group, r);
+    x.t[nq] = g.causal ? w.c - w.n + j : w.c - 1;
+    const uint16_t* p = g.q + (w.q0 + j) * g.q_stride + (int64_t)(w.head * group + r - j * group) * DQK + 8 * (lane >> 5);
+#pragma unroll
+    for (int s = 0; s < DQK / 16; ++s) x.q[nq][s] = *reinterpret_cast<const u32x4*>(p + 16 * s);
+  }
+  return x;
+}
+
+// Which of the 32 keys from s0 on the query at t attends to, of those in `there`.
+__device__ __forceinline__ uint32_t sees32(const PromptGeom& g, int t, int s0, uint32_t there) {
+  const int rel = t - s0;  // (-2^30 and less only where t is: s0 is a position)
+  uint32_t m = first_bits(rel + 1) & there;
+  if (g.k_swa > 0) m &= ~first_bits(rel - g.k_swa + 1) | first_bits(g.k_sink - s0);
+  return m;
+}
+
+// ---------------------------------------------------------------- output
+template <int NQ, int DV>
+__device__ __forceinline__ void store_rows(const PromptGeom& g, const Share& w, int wrow, int lane, const f32x16 (&o)[DV / 32][NQ],
+                                           const float (&m)[NQ], const float (&l)[NQ]) {
+  const int group = (int)g.by_group.d, h = lane >> 5;
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    const int row = wrow + 32 * nq + (lane & 31);
     const float sum = l[nq] + swap32(l[nq]), inv = 1.f / sum;
     if (row >= w.rows) continue;
     const int j = fdiv(g.by_group, row);
     const int64_t at = (w.q0 + j) * g.H + w.head * group + row - j * group;
     if (g.lse && h == 0) g.lse[at] = sum == 0.f ? -INFINITY : (m[nq] + __builtin_amdgcn_logf(sum)) * kLn2;
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+    for (int d = 0; d < DV / 32; ++d)
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
         float y[4];
@@ -315,15 +196,548 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))
   }
 }
 
+// ---------------------------------------------------------------- items with values that are no finite numbers
+// A weight of 0 does not silence a NaN or an infinity in V, and a tile is multiplied whole. So an item whose outputs are not all
+// finite is done again here, a tile at a time, with such values taken out of the product and added to the rows that attend to them
+// (and to no others). Nothing else takes this way: it is written to be right, not fast.
+template <int DQK, int DV, int KIND, int NQ_>
+__device__ __forceinline__ void careful_rows(const PromptGeom& g, const Share& w, int part, typename Prompt<DQK, DV, KIND, NQ_>::Lds& lds) {
+  using T = Prompt<DQK, DV, KIND, NQ_>;
+  constexpr int KS = T::KS, DB = T::DB, NQ = 1;  // (the registers of half a wave's rows)
+  constexpr bool FP8 = T::FP8;
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
+  const int wrow = w.row0 + 32 * (T::NQ * wave + part);
+  const bool active = wrow < w.rows;
+  T f(lane);
+  const Queries<NQ, KS> x = load_queries<NQ, DQK>(g, w, wrow, lane);
+  f32x16 o[DB][NQ];
+  float m[NQ], l[NQ];
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    m[nq] = kNoRef;
+    l[nq] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d][nq] = f32x16{};
+  }
+  uint8_t *lk = lds.k[0], *lv = lds.v[0];
+  for (int i = 0; i < w.nt; ++i) {
+    const int s0 = (i < w.ns ? i : i + w.skip) * kKeys;
+    __syncthreads();
+    // row of the cache (or of the sequence's packed keys) of a key, -1: none
+    auto row_of = [&](int key) -> int64_t {
+      const uint32_t s = (uint32_t)s0 + key;
+      if (s >= (uint32_t)w.c) return -1;
+      if constexpr (KIND == 0) return w.kv0 + s;
+      const int pg = fdiv(g.by_page, (int)s);
+      const int64_t ph = g.page_table ? g.page_table[(int64_t)w.b * g.max_pages + pg] : w.b;
+      return ph >= 0 && ph < g.n_phys ? (ph * g.Hkv + w.head) * g.P + ((int)s - pg * g.P) : -1;
+    };
+    auto load = [&](const void* base, int64_t stride, uint8_t* dst, auto width) {
+      constexpr int D = decltype(width)::value, C = D / 8;
+      for (int e = (int)threadIdx.x; e < kKeys * C; e += T::kThreads) {
+        const int r = e / C, c = e % C;
+        const int64_t row = row_of(r);
+        u32x4 y{};
+        if (row >= 0 && !FP8) y = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(base) + row * stride + 8 * c);
+        if (row >= 0 && FP8) {
+          const u32x2 z = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(base) + row * D + 8 * c);
+          y = fp8x8_bf16(z.x, z.y);
+        }
+        *reinterpret_cast<u32x4*>(dst + r * D * 2 + ((c ^ swz<C>(r)) << 4)) = y;
+      }
+    };
+    load(KIND ? g.k : static_cast<const void*>(static_cast<const uint16_t*>(g.k) + w.head * DQK), KIND ? DQK : g.k_stride, lk,
+         std::integral_constant<int, DQK>{});
+    load(KIND ? g.v : static_cast<const void*>(static_cast<const uint16_t*>(g.v) + w.head * DV), KIND ? DV : g.v_stride, lv,
+         std::integral_constant<int, DV>{});
+    const int64_t own = row_of(lane);
+    if constexpr (FP8) {
+      if (wave == 0) {
+        lds.scales[0][0][lane] = own >= 0 ? g.k_scale[own] * g.scale_log2 : 0.f;
+        lds.scales[0][1][lane] = own >= 0 ? g.v_scale[own] : 0.f;
+      }
+    }
+    __syncthreads();
+    if (!active) continue;
+    const uint64_t there = __ballot(own >= 0);
+#pragma nounroll
+    for (int kb = 0; kb < 2; ++kb) {  // (halves of a tile and sums in the order of the steps below: other rows keep their bits)
+      f.refresh();
+      f32x16 s[NQ];
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) s[nq] = f32x16{};
+#pragma unroll
+      for (int st = 0; st < KS; ++st) {
+        const u32x4 a = f.k_operand(lk + kb * 32 * DQK * 2, st);
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) s[nq] = mfma32(a, x.q[nq][st], s[nq]);
+      }
+      u32x4 p[2][NQ];     // [k-step of 16]
+      uint32_t live[NQ];  // scores that are not -inf
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) {
+        float top = -INFINITY;
+        const uint32_t seen = sees32(g, x.t[nq], s0 + 32 * kb, (uint32_t)(there >> (32 * kb))) >> (4 * h);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = 8 * (r >> 2) + (r & 3);
+          const float z = s[nq][r] * (FP8 ? lds.scales[0][0][32 * kb + 4 * h + key] : g.scale_log2);
+          s[nq][r] = (seen >> key) & 1 ? z : -INFINITY;
+          top = fmaxf(top, s[nq][r]);
+        }
+        top = fmaxf(top, swap32(top));
+        if (top > m[nq] + kLazy) {
+          const float al = fast_exp2(m[nq] - top);
+          m[nq] = top;
+          l[nq] *= al;
+#pragma unroll
+          for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[d][nq][r] *= al;
+        }
+        live[nq] = 0;
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) {
+          float e[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float z = s[nq][r + k];
+            const bool in = z != -INFINITY;
+            if (in) live[nq] |= 1u << (r + k);
+            e[k] = fast_exp2(z - m[nq]);
+            l[nq] += e[k];
+            if constexpr (FP8) e[k] = in ? e[k] * lds.scales[0][1][32 * kb + 8 * (r >> 2) + 4 * h + ((r + k) & 3)] : 0.f;
+          }
+          p[r >> 3][nq][(r & 7) >> 1] = pack_bf16x2(e[0], e[1]);
+        }
+      }
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const u32x4 a = f.v_operand(lv + 32 * kb * DV * 2, ks, d);
+          u32x4 up{}, down{}, fin = a;  // 1 where a value is +inf or NaN, -inf or NaN; the others
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              const uint32_t v = (a[k] >> (16 * half)) & 0xFFFFu, one = 0x3F80u << (16 * half);
+              const bool odd = (v & 0x7F80u) == 0x7F80u, nan = odd && (v & 0x7Fu) != 0;
+              fin[k] &= odd ? (half ? 0xFFFFu : 0xFFFF0000u) : ~0u;
+              up[k] |= nan || (odd && !(v & 0x8000u)) ? one : 0u;
+              down[k] |= nan || (odd && (v & 0x8000u)) ? one : 0u;
+            }
+#pragma unroll
+          for (int nq = 0; nq < NQ; ++nq) {
+            u32x4 one;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t bits = live[nq] >> (8 * ks + 2 * k);
+              one[k] = (bits & 1 ? 0x3F80u : 0u) | (bits & 2 ? 0x3F800000u : 0u);
+            }
+            o[d][nq] = mfma32(fin, p[ks][nq], o[d][nq]);
+            const f32x16 plus = mfma32(up, one, f32x16{}), minus = mfma32(down, one, f32x16{});
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              o[d][nq][r] += plus[r] > 0.f ? INFINITY : 0.f;
+              o[d][nq][r] -= minus[r] > 0.f ? INFINITY : 0.f;
+            }
+          }
+        }
+    }
+  }
+  if (active) store_rows<NQ, DV>(g, w, wrow, lane, o, m, l);
+}
+template <int DQK, int DV, int KIND, int NQ>
+__device__ __forceinline__ void careful_item(const PromptGeom& g, const Share& w, typename Prompt<DQK, DV, KIND, NQ>::Lds& lds) {
+#pragma nounroll
+  for (int part = 0; part < NQ; ++part) careful_rows<DQK, DV, KIND, NQ>(g, w, part, lds);
+}
+
+// ---------------------------------------------------------------- direct loads of tiles
+// N direct loads of a tile's rows: load j takes base + off[j] + 1024 (j % 4) per lane to LDS bytes lds + 1024 j + 16 lane (the
+// immediate offset, less than 4096, counts for both addresses).
+template <int N>
+__device__ __forceinline__ void lds_dma16_tile(const uint8_t* base, const uint32_t* off, uint32_t lds) {
+  if constexpr (N > 4) {
+    lds_dma16_tile<4>(base, off, lds);
+    lds_dma16_tile<N - 4>(base, off + 4, lds + 4096);
+    return;
+  }
+  uint32_t save;
+  if constexpr (N == 4)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024\n\t"
+                 "global_load_lds_dwordx4 %4, %1 offset:2048\n\tglobal_load_lds_dwordx4 %5, %1 offset:3072\n\ts_mov_b32 m0, %0"
+                 : "=&s"(save) : "s"(base), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(lds) : "memory");
+  else if constexpr (N == 3)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024\n\t"
+                 "global_load_lds_dwordx4 %4, %1 offset:2048\n\ts_mov_b32 m0, %0"
+                 : "=&s"(save) : "s"(base), "v"(off[0]), "v"(off[1]), "v"(off[2]), "s"(lds) : "memory");
+  else if constexpr (N == 2)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024\n\ts_mov_b32 m0, %0"
+                 : "=&s"(save) : "s"(base), "v"(off[0]), "v"(off[1]), "s"(lds) : "memory");
+  else if constexpr (N == 1)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\ts_mov_b32 m0, %0"
+                 : "=&s"(save) : "s"(base), "v"(off[0]), "s"(lds) : "memory");
+}
+// Wait until at most N direct loads of this wave are on their way and its LDS reads are done, then join the barrier.
+template <int N>
+__device__ __forceinline__ void tile_barrier() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <int DQK, int DV, int KIND, int NQ>
+__global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves_per_eu(2 / NQ, 2 / NQ))) void prompt_attn_kernel(PromptGeom g) {
+  using T = Prompt<DQK, DV, KIND, NQ>;
+  constexpr int KS = T::KS, DB = T::DB, kThreads = T::kThreads, NK = T::kBufsK, NV = T::kBufsV;
+  constexpr bool FP8 = T::FP8;
+  __shared__ __attribute__((aligned(1024))) typename T::Lds lds;
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
+  Share w;
+  if (!find_share(g, g.first + (int)blockIdx.x, w)) return;
+  const int wrow = w.row0 + 32 * NQ * wave;
+  const bool active = wrow < w.rows;
+  T f(lane);
+  const Queries<NQ, KS> x = load_queries<NQ, DQK>(g, w, wrow, lane);
+  // positions of the wave's first and last token
+  const int wlast = (w.rows - wrow < 32 * NQ ? w.rows : wrow + 32 * NQ) - 1;
+  const int t_first = !active ? -1 : g.causal ? w.c - w.n + fdiv(g.by_group, wrow) : w.c - 1;
+  const int t_last = !active ? -1 : g.causal ? w.c - w.n + fdiv(g.by_group, wlast) : w.c - 1;
+  f32x16 o[DB][NQ];
+  float m[NQ], l[NQ];
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    m[nq] = kNoRef;
+    l[nq] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d][nq] = f32x16{};
+  }
+  // Q has arrived before the first direct load: the compiler, which does not know of those, would wait for all of them with it
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+
+  const bool whole_tiles = KIND == 0 || g.P % kKeys == 0;  // (no tile lies in two pages)
+  const int64_t row_k = KIND ? DQK * (FP8 ? 1 : 2) : g.k_stride * 2, row_v = KIND ? DV * (FP8 ? 1 : 2) : g.v_stride * 2;  // bytes
+  const uint8_t* const base_k = static_cast<const uint8_t*>(g.k) + (KIND ? 0 : w.head * DQK * 2 + w.kv0 * row_k);
+  const uint8_t* const base_v = static_cast<const uint8_t*>(g.v) + (KIND ? 0 : w.head * DV * 2 + w.kv0 * row_v);
+  // direct loads of this wave: load j fills slots 64 (loads wave + j) + lane of the tile
+  uint32_t dma_k[T::kLoadsK], dma_v[T::kLoadsV];
+  if constexpr (!FP8) {
+#pragma unroll
+    for (int j = 0; j < T::kLoadsK; ++j) {
+      const int e = 64 * (T::kLoadsK * wave + j) + lane, r = e / T::CK;
+      dma_k[j] = (uint32_t)(r * (int)row_k + (((e % T::CK) ^ swz<T::CK>(r)) << 4)) - 1024 * (j & 3);
+    }
+#pragma unroll
+    for (int j = 0; j < T::kLoadsV; ++j) {
+      const int e = 64 * (T::kLoadsV * wave + j) + lane, r = e / T::CV;
+      dma_v[j] = (uint32_t)(r * (int)row_v + (((e % T::CV) ^ swz<T::CV>(r)) << 4)) - 1024 * (j & 3);
+    }
+  }
+
+  // Tiles [a, b) of the sequence, the pages of which (from page f1 on) are in LDS.
+  auto run = [&](int a, int b, int f1) {
+    struct Where {
+      bool all;      // every key of the tile is there: rows row0 ..
+      int row0, row; // row of key `lane`, -1: none
+    };
+    auto locate = [&](int tile) {
+      Where p{false, 0, -1};
+      const uint32_t s0 = (uint32_t)tile * kKeys, s = s0 + lane;
+      const bool in = s < (uint32_t)w.c;
+      if constexpr (KIND == 0) {
+        p.row0 = (int)s0;
+        p.all = s0 + kKeys <= (uint32_t)w.c;
+        p.row = in ? (int)s : -1;
+      } else if (whole_tiles) {
+        const int pg = fdiv(g.by_page, (int)s0), ph = uniform(lds.pages[pg - f1]);
+        p.row0 = (ph * g.Hkv + w.head) * g.P + ((int)s0 - pg * g.P);
+        p.all = ph >= 0 && s0 + kKeys <= (uint32_t)w.c;
+        p.row = in && ph >= 0 ? p.row0 + lane : -1;
+      } else if (in) {
+        const int pg = fdiv(g.by_page, (int)s), ph = lds.pages[pg - f1];
+        p.row = ph >= 0 ? (ph * g.Hkv + w.head) * g.P + ((int)s - pg * g.P) : -1;
+      }
+      return p;
+    };
+    uint32_t there = 0;  // bit i % 32: every key of tile a + i is there
+    auto note = [&](int i, bool all) { there = (there & ~(1u << (i & 31))) | (uint32_t)all << (i & 31); };
+
+    // -- bf16: tile a + i by direct loads into its buffers
+    auto issue = [&](int i) {
+      const Where p = locate(a + i);
+      note(i, whole_tiles ? p.all : __ballot(p.row < 0) == 0);
+      uint8_t *dk = lds.k[i % NK] + wave * T::kLoadsK * 1024, *dv = lds.v[i % NV] + wave * T::kLoadsV * 1024;
+      if (whole_tiles && p.all) {
+        const int64_t row0 = (int64_t)(uint32_t)uniform(p.row0);
+        const uint8_t *sk = base_k + row0 * row_k, *sv = base_v + row0 * row_v;
+        lds_dma16_tile<T::kLoadsK>(sk, dma_k, lds_addr(dk));
+        lds_dma16_tile<T::kLoadsV>(sv, dma_v, lds_addr(dv));
+        return;
+      }
+#pragma unroll
+      for (int j = 0; j < T::kLoadsK; ++j) {
+        const int e = 64 * (T::kLoadsK * wave + j) + lane, r = e / T::CK, row = __shfl(p.row, r);
+        lds_dma16((row >= 0 ? base_k + (int64_t)(uint32_t)row * row_k + (((e % T::CK) ^ swz<T::CK>(r)) << 4) : zero_row), lds_addr(dk + j * 1024));
+      }
+#pragma unroll
+      for (int j = 0; j < T::kLoadsV; ++j) {
+        const int e = 64 * (T::kLoadsV * wave + j) + lane, r = e / T::CV, row = __shfl(p.row, r);
+        lds_dma16((row >= 0 ? base_v + (int64_t)(uint32_t)row * row_v + (((e % T::CV) ^ swz<T::CV>(r)) << 4) : zero_row), lds_addr(dv + j * 1024));
+      }
+    };
+    // -- fp8: tile a + i into registers, and from there as bf16 into its buffers
+    constexpr int RK = FP8 ? (kKeys * DQK / 16 + kThreads - 1) / kThreads : 1;
+    const bool loads = !FP8 || kKeys * DQK / 16 >= kThreads || (int)threadIdx.x < kKeys * DQK / 16;  // (a tile of fewer units than threads)
+    struct Regs {
+      u32x4 k[RK], v[RK];
+      float scale;
+    };
+    auto fetch = [&](int i) {
+      const Where p = locate(a + i);
+      note(i, whole_tiles ? p.all : __ballot(p.row < 0) == 0);
+      Regs y{};
+      if (whole_tiles && p.all) {
+        const int64_t at = (int64_t)(uint32_t)uniform(p.row0) * DQK + 16 * threadIdx.x;
+#pragma unroll
+        for (int j = 0; j < RK; ++j) {
+          if (!loads) break;
+          y.k[j] = *reinterpret_cast<const u32x4*>(base_k + at + 16 * kThreads * j);
+          y.v[j] = *reinterpret_cast<const u32x4*>(base_v + at + 16 * kThreads * j);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < RK; ++j) {
+          const int e = (int)threadIdx.x + kThreads * j, row = __shfl(p.row, (e / (DQK / 16)) & 63);
+          if (loads && row >= 0) {
+            y.k[j] = *reinterpret_cast<const u32x4*>(base_k + (int64_t)row * DQK + 16 * (e % (DQK / 16)));
+            y.v[j] = *reinterpret_cast<const u32x4*>(base_v + (int64_t)row * DQK + 16 * (e % (DQK / 16)));
+          }
+        }
+      }
+      if (wave < 2 && p.row >= 0) y.scale = (wave == 0 ? g.k_scale : g.v_scale)[p.row];
+      return y;
+    };
+    auto commit = [&](int i, const Regs& y) {
+#pragma unroll
+      for (int j = 0; j < RK; ++j) {
+        if (!loads) break;
+        const int e = (int)threadIdx.x + kThreads * j, r = e / (DQK / 16), c = 2 * (e % (DQK / 16));
+        uint8_t *dk = lds.k[i % NK] + r * DQK * 2, *dv = lds.v[i % NV] + r * DV * 2;
+        *reinterpret_cast<u32x4*>(dk + ((c ^ swz<T::CK>(r)) << 4)) = fp8x8_bf16(y.k[j].x, y.k[j].y);
+        *reinterpret_cast<u32x4*>(dk + (((c + 1) ^ swz<T::CK>(r)) << 4)) = fp8x8_bf16(y.k[j].z, y.k[j].w);
+        *reinterpret_cast<u32x4*>(dv + ((c ^ swz<T::CV>(r)) << 4)) = fp8x8_bf16(y.v[j].x, y.v[j].y);
+        *reinterpret_cast<u32x4*>(dv + (((c + 1) ^ swz<T::CV>(r)) << 4)) = fp8x8_bf16(y.v[j].z, y.v[j].w);
+      }
+      if (wave < 2) lds.scales[i % NV][wave][lane] = wave == 0 ? y.scale * g.scale_log2 : y.scale;
+    };
+
+    const int nt = b - a;
+    // the tiles that some row of this wave attends to are the first nw
+    const int seen_end = t_last < 0 ? 0 : t_last / kKeys + 1;
+    const int nw = seen_end <= a ? 0 : seen_end < b ? seen_end - a : nt;
+    Regs ahead{};
+
+    // -- the pieces of a step, which takes half a tile: keys 32 kb .. + 31
+    auto scores = [&](int i, int kb, f32x16 (&s)[NQ]) {
+      const uint8_t* lk = lds.k[i % NK] + kb * 32 * DQK * 2;
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) s[nq] = f32x16{};
+#pragma unroll
+      for (int st = 0; st < KS; ++st) {
+        const u32x4 y = f.k_operand(lk, st);
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) s[nq] = mfma32(y, x.q[nq][st], s[nq]);
+      }
+    };
+    u32x4 p[2][NQ];  // weights: B operands of k-steps of 16
+    auto values = [&](int i, int kb) {
+      const uint8_t* lv = lds.v[i % NV] + kb * 32 * DV * 2;
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const u32x4 y = f.v_operand(lv, ks, d);
+#pragma unroll
+          for (int nq = 0; nq < NQ; ++nq) o[d][nq] = mfma32(y, p[ks][nq], o[d][nq]);
+        }
+    };
+    // scores in base-2 units, masked where MASK (keys: those of the half that are there), and their maximum per row
+    auto scale_max = [&](int i, int kb, f32x16 (&s)[NQ], float (&top)[NQ], uint32_t keys, auto mask) {
+      constexpr bool MASK = decltype(mask)::value;
+      f32x4 sc[4];
+      if constexpr (FP8) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sc[k] = *reinterpret_cast<const f32x4*>(&lds.scales[i % NV][0][32 * kb + 8 * k + 4 * h]);
+      }
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) {
+        top[nq] = -INFINITY;
+        uint32_t seen = ~0u;
+        if constexpr (MASK) seen = sees32(g, x.t[nq], (a + i) * kKeys + 32 * kb, keys) >> (4 * h);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          float z = s[nq][r] * (FP8 ? sc[r >> 2][r & 3] : g.scale_log2);
+          if constexpr (MASK) z = (seen >> (8 * (r >> 2) + (r & 3))) & 1 ? z : -INFINITY;
+          s[nq][r] = z;
+          top[nq] = fmaxf(top[nq], z);
+        }
+        top[nq] = fmaxf(top[nq], swap32(top[nq]));
+      }
+    };
+    auto rescale = [&](const float (&top)[NQ]) {
+      bool grown = false;
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) grown |= top[nq] > m[nq] + kLazy;
+      if (__any(grown)) {
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {  // (each row by its own scores, whatever the wave's others do)
+          const float mn = top[nq] > m[nq] + kLazy ? top[nq] : m[nq], al = fast_exp2(m[nq] - mn);
+          m[nq] = mn;
+          l[nq] *= al;
+#pragma unroll
+          for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[d][nq][r] *= al;
+        }
+      }
+    };
+    auto weights = [&](int i, int kb, const f32x16 (&s)[NQ]) {
+      f32x4 sc[4];
+      if constexpr (FP8) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sc[k] = *reinterpret_cast<const f32x4*>(&lds.scales[i % NV][1][32 * kb + 8 * k + 4 * h]);
+      }
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) {
+          float e0 = fast_exp2(s[nq][r] - m[nq]), e1 = fast_exp2(s[nq][r + 1] - m[nq]);
+          l[nq] += e0;
+          l[nq] += e1;
+          if constexpr (FP8) {
+            e0 *= sc[r >> 2][r & 3];
+            e1 *= sc[r >> 2][(r & 3) + 1];
+          }
+          p[r >> 3][nq][(r & 7) >> 1] = pack_bf16x2(e0, e1);
+        }
+    };
+    auto is_clear = [&](int i) {  // every row of the wave attends to every key of tile a + i
+      const int s0 = (a + i) * kKeys;
+      return ((there >> (i & 31)) & 1) && s0 <= t_first - (kKeys - 1) && (g.k_swa == 0 || s0 > t_last - g.k_swa || s0 <= g.k_sink - kKeys);
+    };
+    // start of step i: tile i + 1 has arrived, everyone is done with values i - 2 and keys i - 1; tile i + kLead sets out
+    constexpr int LEAD = T::kLead, G = T::kLoadsK + T::kLoadsV;
+    auto advance = [&](int i) {
+      if constexpr (FP8) {
+        __syncthreads();
+        if (i + 2 < nt) commit(i + 2, ahead);
+        if (i + 3 < nt) ahead = fetch(i + 3);
+      } else {
+        if (i + LEAD - 1 < nt) tile_barrier<(LEAD - 2) * G>();
+        else tile_barrier<0>();
+        if (i + LEAD < nt) issue(i + LEAD);
+      }
+    };
+
+    // -- first tiles
+    if constexpr (FP8) {
+      const Regs y0 = fetch(0), y1 = nt > 1 ? fetch(1) : Regs{};
+      if (nt > 2) ahead = fetch(2);
+      commit(0, y0);
+      if (nt > 1) commit(1, y1);
+      __syncthreads();
+    } else {
+      for (int i = 0; i < LEAD && i < nt; ++i) issue(i);
+      if (nt >= LEAD) tile_barrier<(LEAD - 1) * G>();
+      else tile_barrier<0>();
+    }
+    f32x16 sa[NQ], sb[NQ];
+    if (nw > 0) scores(0, 0, sa);
+    // (before the first half there are no weights: zeros, on values that are there; and after the last one scores of what is left
+    // in the buffers, which nobody reads)
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) p[ks][nq] = u32x4{};
+    auto tile = [&](int i, auto mask) {
+      constexpr bool MASK = decltype(mask)::value;
+      f.refresh();
+      float top[NQ];
+      uint64_t keys = ~0ull;
+      if constexpr (MASK) keys = __ballot(locate(a + i).row >= 0);
+      values(i > 0 ? i - 1 : 0, 1);
+      scale_max(i, 0, sa, top, (uint32_t)keys, mask);
+      rescale(top);
+      scores(i, 1, sb);
+      weights(i, 0, sa);
+      values(i, 0);
+      scale_max(i, 1, sb, top, (uint32_t)(keys >> 32), mask);
+      rescale(top);
+      scores(i + 1, 0, sa);
+      weights(i, 1, sb);
+    };
+    for (int i = 0; i < nt; ++i) {
+      advance(i);
+      if (i < nw) {
+        if (is_clear(i)) tile(i, std::false_type{});
+        else tile(i, std::true_type{});
+      } else if (i == nw && nw > 0) {
+        values(i - 1, 1);
+      }
+    }
+    if (nw == nt) values(nt - 1, 1);
+  };
+
+  // The span's two stretches of tiles, and of a paged cache as many at a time as their pages fit in LDS.
+  for (int part = 0; part < 2; ++part) {
+    const int first = part ? w.ns + w.skip : 0, last = part ? w.nt + w.skip : (w.ns < w.nt ? w.ns : w.nt);
+    for (int a = first; a < last;) {
+      int b = last, f1 = 0;
+      __syncthreads();  // everyone is done with the buffers
+      if constexpr (KIND != 0) {
+        if (b - a > g.pass_tiles) b = a + g.pass_tiles;
+        f1 = fdiv(g.by_page, a * kKeys);
+        const int64_t end = (int64_t)b * kKeys - 1;
+        const int n = fdiv(g.by_page, end < w.c ? (int)end : w.c - 1) - f1 + 1;
+        for (int i = (int)threadIdx.x; i < n; i += kThreads) {
+          const int64_t ph = g.page_table ? g.page_table[(int64_t)w.b * g.max_pages + f1 + i] : w.b;
+          lds.pages[i] = ph >= 0 && ph < g.n_phys ? (int)ph : -1;
+        }
+        __syncthreads();
+      }
+      run(a, b, f1);
+      a = b;
+    }
+  }
+  // (a value that is no finite number leaves every accumulator it was multiplied into so)
+  float odd = 0.f;
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    odd = fmaf(l[nq], 0.f, odd);
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) odd = fmaf(o[d][nq][r], 0.f, odd);
+  }
+  if (__syncthreads_or(odd != 0.f)) {  // (NaN != 0)
+    careful_item<DQK, DV, KIND, NQ>(g, w, lds);
+    return;
+  }
+  if (active) store_rows<NQ, DV>(g, w, wrow, lane, o, m, l);
+}
+
 hipError_t launch_prompt_attn(const PromptGeom& all, hipStream_t st) {
   PromptGeom g = all;
-  auto* kernel = g.ctx_len == nullptr ? (g.d_qk == 64 ? prompt_attn_kernel<64, 64, 0> : g.d_qk == 128 ? prompt_attn_kernel<128, 128, 0> : prompt_attn_kernel<192, 128, 0>)
-                 : g.fp8              ? (g.d_qk == 64 ? prompt_attn_kernel<64, 64, 2> : prompt_attn_kernel<128, 128, 2>)
-                                      : (g.d_qk == 64 ? prompt_attn_kernel<64, 64, 1> : prompt_attn_kernel<128, 128, 1>);
+  constexpr int NQ = 1;
+  auto* kernel = g.ctx_len == nullptr ? (g.d_qk == 64    ? prompt_attn_kernel<64, 64, 0, NQ>
+                                         : g.d_qk == 128 ? prompt_attn_kernel<128, 128, 0, NQ>
+                                                         : prompt_attn_kernel<192, 128, 0, NQ>)
+                 : g.fp8 ? (g.d_qk == 64 ? prompt_attn_kernel<64, 64, 2, NQ> : prompt_attn_kernel<128, 128, 2, NQ>)
+                         : (g.d_qk == 64 ? prompt_attn_kernel<64, 64, 1, NQ> : prompt_attn_kernel<128, 128, 1, NQ>);
   constexpr int64_t kMost = 1 << 22;  // workgroups of a launch (2^32 threads and more are taken modulo 2^32)
   for (int64_t i = 0; i < all.items; i += kMost) {
     g.first = (int)i;
-    const hipError_t e = launch_kernel(kernel, dim3((unsigned)(all.items - i < kMost ? all.items - i : kMost)), dim3(kThreads), st, g);
+    const hipError_t e = launch_kernel(kernel, dim3((unsigned)(all.items - i < kMost ? all.items - i : kMost)), dim3(64 * kRows / (32 * NQ)), st, g);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
