@@ -178,7 +178,8 @@ struct PromptGeom {
   float scale_log2;   // sm_scale * log2(e)
   FastDiv by_group, by_page;
   int pass_tiles;     // tiles whose page-table entries fit the LDS area
-  int64_t items;      // blocks of kPromptRows query rows of all heads, at most
+  int head_classes;   // greatest common divisor of Hkv and 8 (the XCDs)
+  int64_t items;      // workgroups of all blocks of kPromptRows query rows, at most
   int first;          // set by the launcher: first item of the launch
 };
 constexpr int kPromptRows = 256, kPromptKeys = 64, kPromptPages = 2048;

@@ -83,8 +83,11 @@ void set_heads(lsa::PromptGeom& g, int32_t n_seq, int64_t n_tok, int32_t n_heads
   g.k_sink = g.k_swa == 0 ? 0 : (int)(k_sink < most_keys ? k_sink : most_keys);
   g.scale_log2 = sm_scale * 1.4426950408889634f;
   g.by_group = lsa::fast_div((uint32_t)(n_heads / n_kv_heads));
-  // blocks of query rows: a sequence's last one of each head may be partly filled
-  g.items = n_kv_heads * (n_tok * (n_heads / n_kv_heads) / lsa::kPromptRows + (n_seq < n_tok ? n_seq : n_tok));
+  // Of each sequence every XCD takes turns at a class of heads (prompt_attn.hip), as many turns of each head as blocks of rows over
+  // the XCDs that share it, rounded up: the sum of roundings is below the sequences that have tokens.
+  g.head_classes = n_kv_heads % 8 == 0 ? 8 : n_kv_heads % 4 == 0 ? 4 : n_kv_heads % 2 == 0 ? 2 : 1;
+  const int64_t per_turn = (int64_t)lsa::kPromptRows * (8 / g.head_classes), rows = n_tok * (n_heads / n_kv_heads);
+  g.items = 8 * (n_kv_heads / g.head_classes) * (rows / per_turn + (n_seq < n_tok ? n_seq : n_tok));
 }
 
 }  // namespace

@@ -40,27 +40,31 @@ __device__ __forceinline__ int new_tokens(const PromptGeom& g, int b, int& first
   return a >= 0 && e >= a && e <= g.n_tok ? e - a : 0;
 }
 
-// The work item of this workgroup, false when there is none. Items of a sequence: heads outermost, blocks of rows from the last
-// (which has the most keys) to the first.
+// The work item of this workgroup, false when there is none. Workgroups i, i + 8, .. run on one XCD, whose L2 should read the keys
+// that they share once: so with u = gcd(heads, 8) XCD x takes the heads = x mod u, one after the other, and every 8 / u th block of
+// rows of each (which ones, turns with the sequence), from the last, which has the most keys, to the first. Some workgroups at
+// the ends of sequences have nothing to do.
 __device__ __forceinline__ bool find_share(const PromptGeom& g, int item, Share& w) {
-  const int lane = threadIdx.x & 63, group = (int)g.by_group.d;
+  const int lane = threadIdx.x & 63, group = (int)g.by_group.d, u = g.head_classes, step = 8 / u, per_class = g.Hkv / u;
+  const int xcd = item & 7, at = item >> 3;
   int before = 0;
   for (int b0 = 0; b0 < g.n_seq; b0 += 64) {
     const int b = b0 + lane;
     int first = 0;
     const int n = b < g.n_seq ? new_tokens(g, b, first) : 0;
-    const int blocks = (n * group + kRows - 1) / kRows, inc = wave_scan(blocks * g.Hkv);
-    const uint64_t past = __ballot(before + inc > item);
+    const int turns = ((n * group + kRows - 1) / kRows + step - 1) / step, inc = wave_scan(turns * per_class);
+    const uint64_t past = __ballot(before + inc > at);
     if (past) {
       const int i = __ffsll((unsigned long long)past) - 1;
       w.b = b0 + i;
       w.n = __builtin_amdgcn_readlane(n, i);
       w.q0 = __builtin_amdgcn_readlane(first, i);
-      const int nb = __builtin_amdgcn_readlane(blocks, i);
-      const int at = item - (before + __builtin_amdgcn_readlane(inc, i) - nb * g.Hkv);
-      w.head = at / nb;
-      w.row0 = (nb - 1 - (at - w.head * nb)) * kRows;
       w.rows = w.n * group;
+      const int nt = __builtin_amdgcn_readlane(turns, i), k = at - (before + __builtin_amdgcn_readlane(inc, i) - nt * per_class);
+      const int c = k / nt, block = (w.rows + kRows - 1) / kRows - 1 - ((xcd / u + w.b) % step + step * (k - c * nt));
+      if (block < 0) return false;
+      w.head = xcd % u + u * c;
+      w.row0 = block * kRows;
       break;
     }
     before += __builtin_amdgcn_readlane(inc, 63);
