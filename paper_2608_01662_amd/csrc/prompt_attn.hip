@@ -143,6 +143,12 @@ struct Prompt {
   }
 };
 
+// x, made anew here: what is computed from it is not kept in registers over the loop around it.
+__device__ __forceinline__ int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // The first n of 32 bits.
 __device__ __forceinline__ uint32_t first_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
 
@@ -478,14 +484,15 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
         lds_dma16_tile<T::kLoadsV>(sv, dma_v, lds_addr(dv));
         return;
       }
+      const int ln = here(lane);
 #pragma unroll
       for (int j = 0; j < T::kLoadsK; ++j) {
-        const int e = 64 * (T::kLoadsK * wave + j) + lane, r = e / T::CK, row = __shfl(p.row, r);
+        const int e = 64 * (T::kLoadsK * wave + j) + ln, r = e / T::CK, row = __shfl(p.row, r);
         lds_dma16((row >= 0 ? base_k + (int64_t)(uint32_t)row * row_k + (((e % T::CK) ^ swz<T::CK>(r)) << 4) : zero_row), lds_addr(dk + j * 1024));
       }
 #pragma unroll
       for (int j = 0; j < T::kLoadsV; ++j) {
-        const int e = 64 * (T::kLoadsV * wave + j) + lane, r = e / T::CV, row = __shfl(p.row, r);
+        const int e = 64 * (T::kLoadsV * wave + j) + ln, r = e / T::CV, row = __shfl(p.row, r);
         lds_dma16((row >= 0 ? base_v + (int64_t)(uint32_t)row * row_v + (((e % T::CV) ^ swz<T::CV>(r)) << 4) : zero_row), lds_addr(dv + j * 1024));
       }
     };
@@ -511,7 +518,7 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
       } else {
 #pragma unroll
         for (int j = 0; j < RK; ++j) {
-          const int e = (int)threadIdx.x + kThreads * j, row = __shfl(p.row, (e / (DQK / 16)) & 63);
+          const int e = here((int)threadIdx.x) + kThreads * j, row = __shfl(p.row, (e / (DQK / 16)) & 63);
           if (loads && row >= 0) {
             y.k[j] = *reinterpret_cast<const u32x4*>(base_k + (int64_t)row * DQK + 16 * (e % (DQK / 16)));
             y.v[j] = *reinterpret_cast<const u32x4*>(base_v + (int64_t)row * DQK + 16 * (e % (DQK / 16)));
@@ -542,32 +549,44 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
     Regs ahead{};
 
     // -- the pieces of a step, which takes half a tile: keys 32 kb .. + 31
+    // The operands of a product are read from LDS while the one before runs: those of KA k-steps of the scores (all, where the
+    // registers allow it), and all of the values.
+    constexpr int KA = DQK == 192 ? 6 : KS;
+    u32x4 kf[KA], vf[2][DB];
+    auto load_k = [&](int i, int kb) {
+      const uint8_t* lk = lds.k[i % NK] + kb * 32 * DQK * 2;
+#pragma unroll
+      for (int st = 0; st < KA; ++st) kf[st] = f.k_operand(lk, st);
+    };
+    auto load_v = [&](int i, int kb) {
+      const uint8_t* lv = lds.v[i % NV] + kb * 32 * DV * 2;
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int d = 0; d < DB; ++d) vf[ks][d] = f.v_operand(lv, ks, d);
+    };
     auto scores = [&](int i, int kb, f32x16 (&s)[NQ]) {
       const uint8_t* lk = lds.k[i % NK] + kb * 32 * DQK * 2;
 #pragma unroll
       for (int nq = 0; nq < NQ; ++nq) s[nq] = f32x16{};
 #pragma unroll
       for (int st = 0; st < KS; ++st) {
-        const u32x4 y = f.k_operand(lk, st);
+        const u32x4 y = st < KA ? kf[st < KA ? st : 0] : f.k_operand(lk, st);
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) s[nq] = mfma32(y, x.q[nq][st], s[nq]);
       }
     };
     u32x4 p[2][NQ];  // weights: B operands of k-steps of 16
-    auto values = [&](int i, int kb) {
-      const uint8_t* lv = lds.v[i % NV] + kb * 32 * DV * 2;
+    auto values = [&] {
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          const u32x4 y = f.v_operand(lv, ks, d);
+        for (int d = 0; d < DB; ++d)
 #pragma unroll
-          for (int nq = 0; nq < NQ; ++nq) o[d][nq] = mfma32(y, p[ks][nq], o[d][nq]);
-        }
+          for (int nq = 0; nq < NQ; ++nq) o[d][nq] = mfma32(vf[ks][d], p[ks][nq], o[d][nq]);
     };
-    // scores in base-2 units, masked where MASK (keys: those of the half that are there), and their maximum per row
-    auto scale_max = [&](int i, int kb, f32x16 (&s)[NQ], float (&top)[NQ], uint32_t keys, auto mask) {
-      constexpr bool MASK = decltype(mask)::value;
+    // scores in base-2 units and their maximum per row
+    auto scale_max = [&](int i, int kb, f32x16 (&s)[NQ], float (&top)[NQ]) {
       f32x4 sc[4];
       if constexpr (FP8) {
 #pragma unroll
@@ -576,22 +595,34 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
 #pragma unroll
       for (int nq = 0; nq < NQ; ++nq) {
         top[nq] = -INFINITY;
-        uint32_t seen = ~0u;
-        if constexpr (MASK) seen = sees32(g, x.t[nq], (a + i) * kKeys + 32 * kb, keys) >> (4 * h);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          float z = s[nq][r] * (FP8 ? sc[r >> 2][r & 3] : g.scale_log2);
-          if constexpr (MASK) z = (seen >> (8 * (r >> 2) + (r & 3))) & 1 ? z : -INFINITY;
-          s[nq][r] = z;
-          top[nq] = fmaxf(top[nq], z);
+          s[nq][r] *= FP8 ? sc[r >> 2][r & 3] : g.scale_log2;
+          top[nq] = fmaxf(top[nq], s[nq][r]);
         }
-        top[nq] = fmaxf(top[nq], swap32(top[nq]));
       }
     };
-    auto rescale = [&](const float (&top)[NQ]) {
+    // the same of those that the rows attend to (a path of its own beside the products, so that these exist once)
+    auto mask = [&](int i, int kb, f32x16 (&s)[NQ], float (&top)[NQ]) {
+      const uint32_t keys = (uint32_t)(__ballot(locate(a + i).row >= 0) >> (32 * kb));
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) {
+        top[nq] = -INFINITY;
+        const uint32_t seen = sees32(g, x.t[nq], (a + i) * kKeys + 32 * kb, keys) >> (4 * h);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[nq][r] = (seen >> (8 * (r >> 2) + (r & 3))) & 1 ? s[nq][r] : -INFINITY;
+          top[nq] = fmaxf(top[nq], s[nq][r]);
+        }
+      }
+    };
+    auto rescale = [&](float (&top)[NQ]) {
       bool grown = false;
 #pragma unroll
-      for (int nq = 0; nq < NQ; ++nq) grown |= top[nq] > m[nq] + kLazy;
+      for (int nq = 0; nq < NQ; ++nq) {
+        top[nq] = fmaxf(top[nq], swap32(top[nq]));
+        grown |= top[nq] > m[nq] + kLazy;
+      }
       if (__any(grown)) {
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) {  // (each row by its own scores, whatever the wave's others do)
@@ -656,40 +687,41 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
       else tile_barrier<0>();
     }
     f32x16 sa[NQ], sb[NQ];
-    if (nw > 0) scores(0, 0, sa);
+    if (nw > 0) {
+      load_k(0, 0);
+      scores(0, 0, sa);
+      load_v(0, 1);
+    }
     // (before the first half there are no weights: zeros, on values that are there; and after the last one scores of what is left
     // in the buffers, which nobody reads)
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
       for (int nq = 0; nq < NQ; ++nq) p[ks][nq] = u32x4{};
-    auto tile = [&](int i, auto mask) {
-      constexpr bool MASK = decltype(mask)::value;
-      f.refresh();
-      float top[NQ];
-      uint64_t keys = ~0ull;
-      if constexpr (MASK) keys = __ballot(locate(a + i).row >= 0);
-      values(i > 0 ? i - 1 : 0, 1);
-      scale_max(i, 0, sa, top, (uint32_t)keys, mask);
-      rescale(top);
-      scores(i, 1, sb);
-      weights(i, 0, sa);
-      values(i, 0);
-      scale_max(i, 1, sb, top, (uint32_t)(keys >> 32), mask);
-      rescale(top);
-      scores(i + 1, 0, sa);
-      weights(i, 1, sb);
-    };
     for (int i = 0; i < nt; ++i) {
       advance(i);
-      if (i < nw) {
-        if (is_clear(i)) tile(i, std::false_type{});
-        else tile(i, std::true_type{});
-      } else if (i == nw && nw > 0) {
-        values(i - 1, 1);
-      }
+      if (i >= nw) continue;
+      f.refresh();
+      const bool clear = is_clear(i);
+      float top[NQ];
+      load_k(i, 1);
+      values();
+      scale_max(i, 0, sa, top);
+      if (!clear) mask(i, 0, sa, top);
+      rescale(top);
+      load_v(i, 0);
+      scores(i, 1, sb);
+      weights(i, 0, sa);
+      load_k(i + 1, 0);
+      values();
+      scale_max(i, 1, sb, top);
+      if (!clear) mask(i, 1, sb, top);
+      rescale(top);
+      load_v(i, 1);
+      scores(i + 1, 0, sa);
+      weights(i, 1, sb);
     }
-    if (nw == nt) values(nt - 1, 1);
+    if (nw > 0) values();
   };
 
   // The span's two stretches of tiles, and of a paged cache as many at a time as their pages fit in LDS.
@@ -732,7 +764,10 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
 
 hipError_t launch_prompt_attn(const PromptGeom& all, hipStream_t st) {
   PromptGeom g = all;
-  constexpr int NQ = 1;
+#ifndef NQX
+#define NQX 1
+#endif
+  constexpr int NQ = NQX;
   auto* kernel = g.ctx_len == nullptr ? (g.d_qk == 64    ? prompt_attn_kernel<64, 64, 0, NQ>
                                          : g.d_qk == 128 ? prompt_attn_kernel<128, 128, 0, NQ>
                                                          : prompt_attn_kernel<192, 128, 0, NQ>)
