@@ -181,6 +181,12 @@ struct PromptGeom {
   int head_classes;   // greatest common divisor of Hkv and 8 (the XCDs)
   int64_t items;      // workgroups of all blocks of kPromptRows query rows, at most
   int first;          // set by the launcher: first item of the launch
+  // Calls whose blocks' keys are cut into pieces (pieces > 0; about so many, and at most blocks more):
+  int pieces, blocks;          // blocks of kPromptRows query rows of all heads, at most
+  int slot_rows;               // rows of a piece's partial results
+  float *part_o, *part_ml;     // [pieces + blocks, slot_rows, d_v] unnormalised, [.., 2] maximum and sum
+  int4* joins;                 // [blocks, 2]: pieces, first slot, head, row0; rows, first token
+  int32_t* n_joins;
 };
 constexpr int kPromptRows = 256, kPromptKeys = 64, kPromptPages = 2048;
 hipError_t launch_prompt_attn(const PromptGeom& g, hipStream_t st);

@@ -11,6 +11,13 @@ using lsa::hip_fail;
 
 namespace {
 
+#ifndef KMCB
+#define KMCB 512
+#define KPC 512
+#endif
+constexpr int64_t kMostCutBlocks = KMCB, kLeastCutKeys = 16 * lsa::kPromptKeys;
+constexpr int kPieces = KPC;
+
 // The pages of a call's caches
 lsa_status check_pages(const int32_t* page_table, int32_t n_seq, int32_t max_pages, int32_t kv_page_size, int64_t n_phys, int32_t n_kv_heads) {
   LSA_REQUIRE(max_pages >= 1 && kv_page_size >= 1 && n_phys >= 1, LSA_ERR_INVALID_ARG,
@@ -90,6 +97,44 @@ void set_heads(lsa::PromptGeom& g, int32_t n_seq, int64_t n_tok, int32_t n_heads
   g.items = 8 * (n_kv_heads / g.head_classes) * (rows / per_turn + (n_seq < n_tok ? n_seq : n_tok));
 }
 
+// Whether a call's blocks of rows are cut along their keys, and its workspace.
+struct PromptPlan {
+  int pieces, blocks, slot_rows;
+  size_t off_ml, off_joins, off_n, total;
+};
+PromptPlan plan_prompt(int32_t n_seq, int64_t n_tok, int32_t n_heads, int32_t n_kv_heads, int32_t d_v, int32_t k_sink, int32_t k_swa,
+                       int64_t most_keys) {
+  PromptPlan pl{};
+  const int64_t rows = n_tok * (n_heads / n_kv_heads), blocks = n_kv_heads * (rows / lsa::kPromptRows + (n_seq < n_tok ? n_seq : n_tok));
+  int64_t keys = most_keys;
+  if (k_swa > 0 && (int64_t)k_sink + k_swa + lsa::kPromptRows < keys) keys = (int64_t)k_sink + k_swa + lsa::kPromptRows;
+  if (n_tok == 0 || n_seq == 0 || blocks > kMostCutBlocks || keys <= kLeastCutKeys) return pl;
+  pl.pieces = kPieces;
+  pl.blocks = (int)blocks;
+  pl.slot_rows = (int)(rows < lsa::kPromptRows ? rows : lsa::kPromptRows);
+  const size_t slots = (size_t)pl.pieces + pl.blocks;
+  pl.off_ml = lsa::round_up(slots * pl.slot_rows * d_v * 4, 256);
+  pl.off_joins = pl.off_ml + lsa::round_up(slots * pl.slot_rows * 8, 256);
+  pl.off_n = pl.off_joins + lsa::round_up((size_t)blocks * 32, 256);
+  pl.total = pl.off_n + 256;
+  return pl;
+}
+
+lsa_status set_plan(lsa::PromptGeom& g, const PromptPlan& pl, void* workspace, size_t ws_bytes) {
+  if (pl.total == 0) return LSA_OK;
+  LSA_REQUIRE(workspace != nullptr && aligned(workspace, 256), LSA_ERR_WORKSPACE, "workspace must be non-NULL and 256-byte aligned");
+  LSA_REQUIRE(ws_bytes >= pl.total, LSA_ERR_WORKSPACE, "workspace of %zu bytes < %zu needed", ws_bytes, pl.total);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  g.pieces = pl.pieces;
+  g.blocks = pl.blocks;
+  g.slot_rows = pl.slot_rows;
+  g.part_o = reinterpret_cast<float*>(ws);
+  g.part_ml = reinterpret_cast<float*>(ws + pl.off_ml);
+  g.joins = reinterpret_cast<int4*>(ws + pl.off_joins);
+  g.n_joins = reinterpret_cast<int32_t*>(ws + pl.off_n);
+  return LSA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -147,7 +192,9 @@ lsa_status lsa_cache_read(const lsa_cache_read_params* p, int64_t n_tok, int32_t
 }
 
 size_t lsa_prefill_attn_workspace_size(const lsa_prefill_attn_params* p, int32_t n_seq, int64_t n_tok, int64_t n_kv) {
-  return 0;
+  if (check_prefill_params(p) != LSA_OK || check_tokens(n_seq, n_tok, p->n_heads, p->n_kv_heads) != LSA_OK || n_kv < 0 || n_kv >= (1LL << 31))
+    return 0;
+  return plan_prompt(n_seq, n_tok, p->n_heads, p->n_kv_heads, p->d_v, p->k_sink, p->k_swa, n_kv).total;
 }
 
 lsa_status lsa_prefill_attn(const lsa_prefill_attn_params* p, int32_t n_seq, int64_t n_tok, int64_t n_kv, const void* q,
@@ -184,6 +231,8 @@ lsa_status lsa_prefill_attn(const lsa_prefill_attn_params* p, int32_t n_seq, int
   g.n_kv = (int)n_kv;
   g.causal = p->causal;
   set_heads(g, n_seq, n_tok, p->n_heads, p->n_kv_heads, p->d_qk, p->d_v, p->k_sink, p->k_swa, n_kv, p->sm_scale);
+  s = set_plan(g, plan_prompt(n_seq, n_tok, p->n_heads, p->n_kv_heads, p->d_v, p->k_sink, p->k_swa, n_kv), workspace, ws_bytes);
+  if (s != LSA_OK) return s;
   const hipError_t e = lsa::launch_prompt_attn(g, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "prefill attention");
   return LSA_OK;
@@ -191,7 +240,9 @@ lsa_status lsa_prefill_attn(const lsa_prefill_attn_params* p, int32_t n_seq, int
 
 size_t lsa_chunk_attn_workspace_size(const lsa_decode_attn_params* p, int32_t n_seq, int64_t n_tok, int32_t max_pages,
                                      int32_t kv_page_size) {
-  return 0;
+  if (check_chunk_params(p) != LSA_OK || check_tokens(n_seq, n_tok, p->n_heads, p->n_kv_heads) != LSA_OK || max_pages < 1 || kv_page_size < 1)
+    return 0;
+  return plan_prompt(n_seq, n_tok, p->n_heads, p->n_kv_heads, p->d_v, p->k_sink, p->k_swa, (int64_t)max_pages * kv_page_size).total;
 }
 
 lsa_status lsa_chunk_attn(const lsa_decode_attn_params* p, int32_t n_seq, int64_t n_tok, const void* q, const void* k_cache,
@@ -237,6 +288,8 @@ lsa_status lsa_chunk_attn(const lsa_decode_attn_params* p, int32_t n_seq, int64_
   const int64_t pass = (int64_t)(lsa::kPromptPages - 2) * kv_page_size / lsa::kPromptKeys;  // (two pages more at the ends)
   g.pass_tiles = (int)(pass < (1 << 26) ? pass : (1 << 26));
   set_heads(g, n_seq, n_tok, p->n_heads, p->n_kv_heads, p->d_qk, p->d_v, p->k_sink, p->k_swa, g.cap, p->sm_scale);
+  s = set_plan(g, plan_prompt(n_seq, n_tok, p->n_heads, p->n_kv_heads, p->d_v, p->k_sink, p->k_swa, g.cap), workspace, ws_bytes);
+  if (s != LSA_OK) return s;
   const hipError_t e = lsa::launch_prompt_attn(g, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "chunk attention");
   return LSA_OK;

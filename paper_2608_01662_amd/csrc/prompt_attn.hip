@@ -32,6 +32,8 @@ struct Share {
   int n, c;         // new tokens and keys of the sequence
   int64_t q0, kv0;  // its first token, its first key of contiguous ones
   int ns, skip, nt;
+  int p0, p1;       // tiles [p0, p1) of the span are this workgroup's
+  int slot;         // of its partial results, -1: it has all tiles and writes the output
 };
 
 __device__ __forceinline__ int new_tokens(const PromptGeom& g, int b, int& first) {
@@ -40,11 +42,33 @@ __device__ __forceinline__ int new_tokens(const PromptGeom& g, int b, int& first
   return a >= 0 && e >= a && e <= g.n_tok ? e - a : 0;
 }
 
-// The work item of this workgroup, false when there is none. Workgroups i, i + 8, .. run on one XCD, whose L2 should read the keys
-// that they share once: so with u = gcd(heads, 8) XCD x takes the heads = x mod u, one after the other, and every 8 / u th block of
-// rows of each (which ones, turns with the sequence), from the last, which has the most keys, to the first. Some workgroups at
-// the ends of sequences have nothing to do.
-__device__ __forceinline__ bool find_share(const PromptGeom& g, int item, Share& w) {
+// The keys of a block of rows: completes w from its sequence, row0 and rows.
+__device__ __forceinline__ int keys_of(const PromptGeom& g, int b, int& first) {  // keys of sequence b, and the first one's row
+  if (g.ctx_len) {
+    const int c = g.ctx_len[b];
+    first = 0;
+    return c < 0 || c > g.cap ? 0 : c;
+  }
+  const int a = g.cu_kv[b], e = g.cu_kv[b + 1];
+  first = a;
+  return a >= 0 && e >= a && e <= g.n_kv ? e - a : 0;
+}
+__device__ __forceinline__ void span_of(const PromptGeom& g, Share& w) {
+  const int last = (w.rows - w.row0 < kRows ? w.rows : w.row0 + kRows) - 1;
+  const int t_lo = g.causal ? w.c - w.n + fdiv(g.by_group, w.row0) : w.c - 1, t_hi = g.causal ? w.c - w.n + fdiv(g.by_group, last) : w.c - 1;
+  const int end = t_hi + 1 > 0 ? t_hi + 1 : 0, total = (int)(((uint32_t)end + kKeys - 1) / kKeys);  // (t_hi < c)
+  const int lo = g.k_swa > 0 && t_lo >= g.k_swa ? t_lo - g.k_swa + 1 : 0, first = lo / kKeys;
+  const int sink = g.k_sink < end ? g.k_sink : end, st = (int)(((uint32_t)sink + kKeys - 1) / kKeys);
+  w.ns = first <= st ? total : st;
+  w.skip = first <= st ? 0 : first - st;
+  w.nt = total - w.skip;
+}
+
+// The work of workgroup `item` of a call that leaves the keys of a block whole, false when there is none. Workgroups i, i + 8, .. run
+// on one XCD, whose L2 should read the keys that they share once: so with u = gcd(heads, 8) XCD x takes the heads = x mod u, one
+// after the other, and every 8 / u th block of rows of each (which ones, turns with the sequence), from the last, which has the most
+// keys, to the first. Some workgroups at the ends of sequences have nothing to do.
+__device__ __forceinline__ bool find_whole(const PromptGeom& g, int item, Share& w) {
   const int lane = threadIdx.x & 63, group = (int)g.by_group.d, u = g.head_classes, step = 8 / u, per_class = g.Hkv / u;
   const int xcd = item & 7, at = item >> 3;
   int before = 0;
@@ -65,29 +89,94 @@ __device__ __forceinline__ bool find_share(const PromptGeom& g, int item, Share&
       if (block < 0) return false;
       w.head = xcd % u + u * c;
       w.row0 = block * kRows;
-      break;
+      int kv0;
+      w.c = uniform(keys_of(g, w.b, kv0));
+      w.kv0 = uniform(kv0);
+      span_of(g, w);
+      w.p0 = 0;
+      w.p1 = w.nt;
+      w.slot = -1;
+      return true;
     }
     before += __builtin_amdgcn_readlane(inc, 63);
-    if (b0 + 64 >= g.n_seq) return false;
   }
-  if (g.ctx_len) {
-    const int c = uniform(g.ctx_len[w.b]);
-    w.c = c < 0 || c > g.cap ? 0 : c;
-    w.kv0 = 0;
-  } else {
-    const int a = uniform(g.cu_kv[w.b]), e = uniform(g.cu_kv[w.b + 1]);
-    w.c = a >= 0 && e >= a && e <= g.n_kv ? e - a : 0;
-    w.kv0 = a;
+  return false;
+}
+
+// The same of a call that has few blocks of rows: the keys of a sequence's blocks are cut into equal pieces, as many as make the
+// call's pieces about g.pieces, but of no fewer tiles than pay for the partial results of a piece, which the join reads again: 4, and
+// the more the more rows a block has. The first piece of a block tells the join about it.
+__device__ __forceinline__ bool find_piece(const PromptGeom& g, int id, Share& w) {
+  const int lane = threadIdx.x & 63, group = (int)g.by_group.d;
+  struct Seq {
+    int n, q0, c, kv0, blocks, tiles;  // tiles: of its last block, the most
+  };
+  auto load = [&](int b) {
+    Seq s{};
+    if (b >= g.n_seq) return s;
+    s.n = new_tokens(g, b, s.q0);
+    s.c = keys_of(g, b, s.kv0);
+    const int rows = s.n * group;
+    s.blocks = (rows + kRows - 1) / kRows;
+    if (s.blocks > 0) {
+      Share x;
+      x.rows = rows;
+      x.row0 = (s.blocks - 1) * kRows;
+      x.n = s.n;
+      x.c = s.c;
+      span_of(g, x);
+      s.tiles = x.nt;
+    }
+    return s;
+  };
+  Seq s = load(lane);
+  // (tiles of all: in float, they may pass 31 bits)
+  float total = (float)s.tiles * (float)(s.blocks * g.Hkv);
+  for (int b = lane + 64; b < g.n_seq; b += 64) {
+    const Seq y = load(b);
+    total += (float)y.tiles * (float)(y.blocks * g.Hkv);
   }
-  const int last = (w.rows - w.row0 < kRows ? w.rows : w.row0 + kRows) - 1;
-  const int t_lo = g.causal ? w.c - w.n + fdiv(g.by_group, w.row0) : w.c - 1, t_hi = g.causal ? w.c - w.n + fdiv(g.by_group, last) : w.c - 1;
-  const int end = t_hi + 1 > 0 ? t_hi + 1 : 0, total = (int)(((uint32_t)end + kKeys - 1) / kKeys);  // (t_hi < c)
-  const int lo = g.k_swa > 0 && t_lo >= g.k_swa ? t_lo - g.k_swa + 1 : 0, first = lo / kKeys;
-  const int sink = g.k_sink < end ? g.k_sink : end, st = (int)(((uint32_t)sink + kKeys - 1) / kKeys);
-  w.ns = first <= st ? total : st;
-  w.skip = first <= st ? 0 : first - st;
-  w.nt = total - w.skip;
-  return true;
+  for (int k = 32; k >= 1; k >>= 1) total += __shfl_xor(total, k);
+  const float share = total / (float)g.pieces;
+  const int slots = g.pieces + g.blocks;
+  int before = 0, items = 0;
+  for (int b0 = 0; b0 < g.n_seq; b0 += 64) {
+    if (b0 > 0) s = load(b0 + lane);
+    const int rows = s.n * group, least = 4 + 12 * (rows < kRows ? rows : kRows) / kRows;
+    const int each = share > (float)least ? (share < 1e9f ? (int)share + 1 : 1000000000) : least;
+    const int pieces = s.tiles > each ? (s.tiles + each - 1) / each : 1, inc = wave_scan(s.blocks * g.Hkv * pieces);
+    const int inc_items = wave_scan(s.blocks * g.Hkv);
+    const uint64_t past = id < slots ? __ballot(before + inc > id) : 0;
+    if (past) {
+      const int i = __ffsll((unsigned long long)past) - 1;
+      w.b = b0 + i;
+      w.n = __builtin_amdgcn_readlane(s.n, i);
+      w.q0 = __builtin_amdgcn_readlane(s.q0, i);
+      w.c = __builtin_amdgcn_readlane(s.c, i);
+      w.kv0 = __builtin_amdgcn_readlane(s.kv0, i);
+      w.rows = w.n * group;
+      const int np = __builtin_amdgcn_readlane(pieces, i), nb = __builtin_amdgcn_readlane(s.blocks, i);
+      const int k = id - (before + __builtin_amdgcn_readlane(inc, i) - nb * g.Hkv * np), block = k / np, piece = k - block * np;
+      const int item = items + __builtin_amdgcn_readlane(inc_items, i) - nb * g.Hkv + block;
+      if (item >= g.blocks) return false;  // (offsets that are not ascending)
+      w.head = block / nb;
+      w.row0 = (block - w.head * nb) * kRows;
+      span_of(g, w);
+      w.p0 = (int)((int64_t)w.nt * piece / np);
+      w.p1 = (int)((int64_t)w.nt * (piece + 1) / np);
+      w.slot = np > 1 ? id : -1;
+      if (piece == 0 && threadIdx.x == 0) {
+        g.joins[2 * item] = int4{np, id, w.head, w.row0};
+        g.joins[2 * item + 1] = int4{w.rows, (int)w.q0, 0, 0};
+      }
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(inc, 63);
+    items += __builtin_amdgcn_readlane(inc_items, 63);
+  }
+  // the launch has one workgroup more than there can be pieces, which tells the join how many blocks there are
+  if (id == slots && threadIdx.x == 0) *g.n_joins = before <= slots && items <= g.blocks ? items : 0;
+  return false;
 }
 
 __device__ __forceinline__ float swap32(float x) {  // the value of lane l ^ 32
@@ -191,6 +280,16 @@ __device__ __forceinline__ void store_rows(const PromptGeom& g, const Share& w, 
     const int row = wrow + 32 * nq + (lane & 31);
     const float sum = l[nq] + swap32(l[nq]), inv = 1.f / sum;
     if (row >= w.rows) continue;
+    if (w.slot >= 0) {
+      const int64_t at = (int64_t)w.slot * g.slot_rows + row - w.row0;
+      if (h == 0) *reinterpret_cast<f32x2*>(g.part_ml + 2 * at) = f32x2{m[nq], sum};
+#pragma unroll
+      for (int d = 0; d < DV / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+          *reinterpret_cast<f32x4*>(g.part_o + at * DV + 32 * d + 2 * r + 4 * h) = f32x4{o[d][nq][r], o[d][nq][r + 1], o[d][nq][r + 2], o[d][nq][r + 3]};
+      continue;
+    }
     const int j = fdiv(g.by_group, row);
     const int64_t at = (w.q0 + j) * g.H + w.head * group + row - j * group;
     if (g.lse && h == 0) g.lse[at] = sum == 0.f ? -INFINITY : (m[nq] + __builtin_amdgcn_logf(sum)) * kLn2;
@@ -204,6 +303,40 @@ __device__ __forceinline__ void store_rows(const PromptGeom& g, const Share& w, 
         *reinterpret_cast<u32x2*>(g.out + at * DV + 32 * d + 2 * r + 4 * h) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
       }
   }
+}
+
+// The pieces of a block joined: workgroup (y, i) takes rows of block i, DV / 4 threads a row.
+template <int DV>
+__global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g) {
+  constexpr int T = DV / 4, R = 256 / T;
+  const int item = blockIdx.y;
+  if (item >= *g.n_joins) return;
+  const int4 a = g.joins[2 * item], b = g.joins[2 * item + 1];
+  const int np = a.x, row0 = a.w, r = blockIdx.x * R + (int)threadIdx.x / T, row = row0 + r, d = 4 * ((int)threadIdx.x % T);
+  if (np <= 1 || r >= kRows || row >= b.x) return;
+  const int64_t at = (int64_t)a.y * g.slot_rows + r, step = g.slot_rows;
+  const f32x2* ml = reinterpret_cast<const f32x2*>(g.part_ml) + at;
+  float top = kNoRef;
+#pragma unroll 8
+  for (int k = 0; k < np; ++k) top = fmaxf(top, ml[k * step].x);
+  float sum = 0.f;
+  f32x4 y{};
+#pragma unroll 8
+  for (int k = 0; k < np; ++k) {
+    const f32x2 x = ml[k * step];
+    const float f = fast_exp2(x.x - top);
+    sum += f * x.y;
+    const f32x4 o = *reinterpret_cast<const f32x4*>(g.part_o + (at + k * step) * DV + d);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) y[q] += f * o[q];
+  }
+  const int group = (int)g.by_group.d, j = fdiv(g.by_group, row);
+  const int64_t to = ((int64_t)b.y + j) * g.H + a.z * group + row - j * group;
+  if (g.lse && d == 0) g.lse[to] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+  const float inv = 1.f / sum;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) y[q] = sum == 0.f ? 0.f : y[q] * inv;
+  *reinterpret_cast<u32x2*>(g.out + to * DV + d) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
 }
 
 // ---------------------------------------------------------------- items with values that are no finite numbers
@@ -230,7 +363,7 @@ __device__ __forceinline__ void careful_rows(const PromptGeom& g, const Share& w
     for (int d = 0; d < DB; ++d) o[d][nq] = f32x16{};
   }
   uint8_t *lk = lds.k[0], *lv = lds.v[0];
-  for (int i = 0; i < w.nt; ++i) {
+  for (int i = w.p0; i < w.p1; ++i) {
     const int s0 = (i < w.ns ? i : i + w.skip) * kKeys;
     __syncthreads();
     // row of the cache (or of the sequence's packed keys) of a key, -1: none
@@ -404,7 +537,7 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
   __shared__ __attribute__((aligned(1024))) typename T::Lds lds;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
   Share w;
-  if (!find_share(g, g.first + (int)blockIdx.x, w)) return;
+  if (!(g.pieces ? find_piece(g, (int)blockIdx.x, w) : find_whole(g, g.first + (int)blockIdx.x, w))) return;
   const int wrow = w.row0 + 32 * NQ * wave;
   const bool active = wrow < w.rows;
   T f(lane);
@@ -726,7 +859,7 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
 
   // The span's two stretches of tiles, and of a paged cache as many at a time as their pages fit in LDS.
   for (int part = 0; part < 2; ++part) {
-    const int first = part ? w.ns + w.skip : 0, last = part ? w.nt + w.skip : (w.ns < w.nt ? w.ns : w.nt);
+    const int first = part ? (w.p0 > w.ns ? w.p0 : w.ns) + w.skip : w.p0, last = part ? w.p1 + w.skip : (w.ns < w.p1 ? w.ns : w.p1);
     for (int a = first; a < last;) {
       int b = last, f1 = 0;
       __syncthreads();  // everyone is done with the buffers
@@ -773,6 +906,13 @@ hipError_t launch_prompt_attn(const PromptGeom& all, hipStream_t st) {
                                                          : prompt_attn_kernel<192, 128, 0, NQ>)
                  : g.fp8 ? (g.d_qk == 64 ? prompt_attn_kernel<64, 64, 2, NQ> : prompt_attn_kernel<128, 128, 2, NQ>)
                          : (g.d_qk == 64 ? prompt_attn_kernel<64, 64, 1, NQ> : prompt_attn_kernel<128, 128, 1, NQ>);
+  if (g.pieces) {
+    hipError_t e = launch_kernel(kernel, dim3((unsigned)(g.pieces + g.blocks + 1)), dim3(64 * kRows / (32 * NQ)), st, g);
+    if (e != hipSuccess) return e;
+    const int rows = 256 / (g.d_v / 4);  // of a workgroup
+    return launch_kernel(g.d_v == 64 ? prompt_join_kernel<64> : prompt_join_kernel<128>, dim3((unsigned)((g.slot_rows + rows - 1) / rows), (unsigned)g.blocks),
+                         dim3(256), st, g);
+  }
   constexpr int64_t kMost = 1 << 22;  // workgroups of a launch (2^32 threads and more are taken modulo 2^32)
   for (int64_t i = 0; i < all.items; i += kMost) {
     g.first = (int)i;
