@@ -179,8 +179,14 @@ __device__ __forceinline__ bool find_piece(const PromptGeom& g, int id, Share& w
   return false;
 }
 
-__device__ __forceinline__ float swap32(float x) {  // the value of lane l ^ 32
-  return __shfl_xor(x, 32);
+// The maximum and the sum of lanes l and l ^ 32 (see max4_xor16_32).
+__device__ __forceinline__ float max2_xor32(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float sum2_xor32(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
 // ---------------------------------------------------------------- sizes, LDS layout, operand offsets
@@ -238,6 +244,11 @@ __device__ __forceinline__ int here(int x) {
   return x;
 }
 
+__device__ __forceinline__ const uint8_t* uniform_ptr(const uint8_t* p) {
+  const uint64_t x = (uint64_t)(uintptr_t)p;
+  return (const uint8_t*)(uintptr_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+}
+
 // The first n of 32 bits.
 __device__ __forceinline__ uint32_t first_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
 
@@ -259,6 +270,12 @@ __device__ __forceinline__ Queries<NQ, DQK / 16> load_queries(const PromptGeom& 
 #pragma unroll
     for (int s = 0; s < DQK / 16; ++s) x.q[nq][s] = *reinterpret_cast<const u32x4*>(p + 16 * s);
   }
+  // They have arrived here, before the first direct load: the compiler, which does not know of those, would wait for them where it
+  // first uses these, in a loop at every turn.
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+    for (int s = 0; s < DQK / 16; ++s) asm volatile("" : "+v"(x.q[nq][s]));
   return x;
 }
 
@@ -278,7 +295,7 @@ __device__ __forceinline__ void store_rows(const PromptGeom& g, const Share& w, 
 #pragma unroll
   for (int nq = 0; nq < NQ; ++nq) {
     const int row = wrow + 32 * nq + (lane & 31);
-    const float sum = l[nq] + swap32(l[nq]), inv = 1.f / sum;
+    const float sum = sum2_xor32(l[nq]), inv = 1.f / sum;
     if (row >= w.rows) continue;
     if (w.slot >= 0) {
       const int64_t at = (int64_t)w.slot * g.slot_rows + row - w.row0;
@@ -428,7 +445,7 @@ __device__ __forceinline__ void careful_rows(const PromptGeom& g, const Share& w
           s[nq][r] = (seen >> key) & 1 ? z : -INFINITY;
           top = fmaxf(top, s[nq][r]);
         }
-        top = fmaxf(top, swap32(top));
+        top = max2_xor32(top);
         if (top > m[nq] + kLazy) {
           const float al = fast_exp2(m[nq] - top);
           m[nq] = top;
@@ -555,8 +572,6 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d][nq] = f32x16{};
   }
-  // Q has arrived before the first direct load: the compiler, which does not know of those, would wait for all of them with it
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
   const bool whole_tiles = KIND == 0 || g.P % kKeys == 0;  // (no tile lies in two pages)
   const int64_t row_k = KIND ? DQK * (FP8 ? 1 : 2) : g.k_stride * 2, row_v = KIND ? DV * (FP8 ? 1 : 2) : g.v_stride * 2;  // bytes
@@ -611,8 +626,8 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
       note(i, whole_tiles ? p.all : __ballot(p.row < 0) == 0);
       uint8_t *dk = lds.k[i % NK] + wave * T::kLoadsK * 1024, *dv = lds.v[i % NV] + wave * T::kLoadsV * 1024;
       if (whole_tiles && p.all) {
-        const int64_t row0 = (int64_t)(uint32_t)uniform(p.row0);
-        const uint8_t *sk = base_k + row0 * row_k, *sv = base_v + row0 * row_v;
+        const int64_t row0 = (int64_t)(uint32_t)p.row0;
+        const uint8_t *sk = uniform_ptr(base_k + row0 * row_k), *sv = uniform_ptr(base_v + row0 * row_v);
         lds_dma16_tile<T::kLoadsK>(sk, dma_k, lds_addr(dk));
         lds_dma16_tile<T::kLoadsV>(sv, dma_v, lds_addr(dv));
         return;
@@ -753,7 +768,7 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
       bool grown = false;
 #pragma unroll
       for (int nq = 0; nq < NQ; ++nq) {
-        top[nq] = fmaxf(top[nq], swap32(top[nq]));
+        top[nq] = max2_xor32(top[nq]);
         grown |= top[nq] > m[nq] + kLazy;
       }
       if (__any(grown)) {
