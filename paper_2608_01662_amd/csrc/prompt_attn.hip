@@ -76,6 +76,8 @@ __device__ __forceinline__ bool find_whole(const PromptGeom& g, int item, Share&
     const int b = b0 + lane;
     int first = 0;
     const int n = b < g.n_seq ? new_tokens(g, b, first) : 0;
+    int kv0 = 0;
+    const int c = b < g.n_seq ? keys_of(g, b, kv0) : 0;
     const int turns = ((n * group + kRows - 1) / kRows + step - 1) / step, inc = wave_scan(turns * per_class);
     const uint64_t past = __ballot(before + inc > at);
     if (past) {
@@ -85,13 +87,12 @@ __device__ __forceinline__ bool find_whole(const PromptGeom& g, int item, Share&
       w.q0 = __builtin_amdgcn_readlane(first, i);
       w.rows = w.n * group;
       const int nt = __builtin_amdgcn_readlane(turns, i), k = at - (before + __builtin_amdgcn_readlane(inc, i) - nt * per_class);
-      const int c = k / nt, block = (w.rows + kRows - 1) / kRows - 1 - ((xcd / u + w.b) % step + step * (k - c * nt));
+      const int nth = k / nt, block = (w.rows + kRows - 1) / kRows - 1 - ((xcd / u + w.b) % step + step * (k - nth * nt));
       if (block < 0) return false;
-      w.head = xcd % u + u * c;
+      w.head = xcd % u + u * nth;
       w.row0 = block * kRows;
-      int kv0;
-      w.c = uniform(keys_of(g, w.b, kv0));
-      w.kv0 = uniform(kv0);
+      w.c = __builtin_amdgcn_readlane(c, i);
+      w.kv0 = __builtin_amdgcn_readlane(kv0, i);
       span_of(g, w);
       w.p0 = 0;
       w.p1 = w.nt;
@@ -249,8 +250,18 @@ __device__ __forceinline__ const uint8_t* uniform_ptr(const uint8_t* p) {
   return (const uint8_t*)(uintptr_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
 }
 
+// A bf16 cache's weight exponent: s scale - m in one rounding. That leaves the largest score's at m's rounding error, the same for all
+// keys of a row, which cancels; but from scores of 2^28 on it may overflow, and the careful form takes both roundings.
+constexpr float kFarScore = 268435456.f;
+
 // The first n of 32 bits.
 __device__ __forceinline__ uint32_t first_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+
+__device__ __forceinline__ float scaled_below(float s, float scale, float m) {
+#pragma clang fp contract(off)
+  const float z = s * scale;
+  return z - m;
+}
 
 // This lane's query rows.
 template <int NQ, int KS>
@@ -270,8 +281,8 @@ __device__ __forceinline__ Queries<NQ, DQK / 16> load_queries(const PromptGeom& 
 #pragma unroll
     for (int s = 0; s < DQK / 16; ++s) x.q[nq][s] = *reinterpret_cast<const u32x4*>(p + 16 * s);
   }
-  // They have arrived here, before the first direct load: the compiler, which does not know of those, would wait for them where it
-  // first uses these, in a loop at every turn.
+  // They have arrived here: the compiler would wait for them where it first uses them, in a loop at every turn, and for the direct
+  // loads, of which it does not know, with them.
 #pragma unroll
   for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
@@ -296,8 +307,9 @@ __device__ __forceinline__ void store_rows(const PromptGeom& g, const Share& w, 
   for (int nq = 0; nq < NQ; ++nq) {
     const int row = wrow + 32 * nq + (lane & 31);
     const float sum = sum2_xor32(l[nq]), inv = 1.f / sum;
-    if (row >= w.rows) continue;
+    const bool in = row < w.rows;
     if (w.slot >= 0) {
+      if (!in) continue;
       const int64_t at = (int64_t)w.slot * g.slot_rows + row - w.row0;
       if (h == 0) *reinterpret_cast<f32x2*>(g.part_ml + 2 * at) = f32x2{m[nq], sum};
 #pragma unroll
@@ -309,15 +321,18 @@ __device__ __forceinline__ void store_rows(const PromptGeom& g, const Share& w, 
     }
     const int j = fdiv(g.by_group, row);
     const int64_t at = (w.q0 + j) * g.H + w.head * group + row - j * group;
-    if (g.lse && h == 0) g.lse[at] = sum == 0.f ? -INFINITY : (m[nq] + __builtin_amdgcn_logf(sum)) * kLn2;
+    if (g.lse && in && h == 0) g.lse[at] = sum == 0.f ? -INFINITY : (m[nq] + __builtin_amdgcn_logf(sum)) * kLn2;
 #pragma unroll
     for (int d = 0; d < DV / 32; ++d)
 #pragma unroll
-      for (int r = 0; r < 16; r += 4) {
-        float y[4];
+      for (int r = 0; r < 16; r += 8) {
+        // dims 2 r + 4 h and 2 r + 8 + 4 h, four each: swapped with lane l ^ 32 into eight from 2 r + 8 h on
+        uint32_t y[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) y[k] = sum == 0.f ? 0.f : o[d][nq][r + k] * inv;
-        *reinterpret_cast<u32x2*>(g.out + at * DV + 32 * d + 2 * r + 4 * h) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+        for (int k = 0; k < 4; ++k)
+          y[k] = pack_bf16x2(sum == 0.f ? 0.f : o[d][nq][r + 2 * k] * inv, sum == 0.f ? 0.f : o[d][nq][r + 2 * k + 1] * inv);
+        const auto lo = __builtin_amdgcn_permlane32_swap(y[0], y[2], false, false), hi = __builtin_amdgcn_permlane32_swap(y[1], y[3], false, false);
+        if (in) *reinterpret_cast<u32x4*>(g.out + at * DV + 32 * d + 2 * r + 8 * h) = u32x4{lo[0], hi[0], lo[1], hi[1]};
       }
   }
 }
@@ -441,11 +456,11 @@ __device__ __forceinline__ void careful_rows(const PromptGeom& g, const Share& w
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int key = 8 * (r >> 2) + (r & 3);
-          const float z = s[nq][r] * (FP8 ? lds.scales[0][0][32 * kb + 4 * h + key] : g.scale_log2);
-          s[nq][r] = (seen >> key) & 1 ? z : -INFINITY;
+          if constexpr (FP8) s[nq][r] *= lds.scales[0][0][32 * kb + 4 * h + key];
+          s[nq][r] = (seen >> key) & 1 ? s[nq][r] : -INFINITY;
           top = fmaxf(top, s[nq][r]);
         }
-        top = max2_xor32(top);
+        top = max2_xor32(FP8 ? top : top * g.scale_log2);
         if (top > m[nq] + kLazy) {
           const float al = fast_exp2(m[nq] - top);
           m[nq] = top;
@@ -456,6 +471,7 @@ __device__ __forceinline__ void careful_rows(const PromptGeom& g, const Share& w
             for (int r = 0; r < 16; ++r) o[d][nq][r] *= al;
         }
         live[nq] = 0;
+        const bool far = !(fabsf(m[nq]) < kFarScore) && m[nq] != kNoRef;
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
           float e[2];
@@ -464,7 +480,7 @@ __device__ __forceinline__ void careful_rows(const PromptGeom& g, const Share& w
             const float z = s[nq][r + k];
             const bool in = z != -INFINITY;
             if (in) live[nq] |= 1u << (r + k);
-            e[k] = fast_exp2(z - m[nq]);
+            e[k] = fast_exp2(FP8 ? z - m[nq] : far ? scaled_below(z, g.scale_log2, m[nq]) : fmaf(z, g.scale_log2, -m[nq]));
             l[nq] += e[k];
             if constexpr (FP8) e[k] = in ? e[k] * lds.scales[0][1][32 * kb + 8 * (r >> 2) + 4 * h + ((r + k) & 3)] : 0.f;
           }
@@ -558,7 +574,8 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
   const int wrow = w.row0 + 32 * NQ * wave;
   const bool active = wrow < w.rows;
   T f(lane);
-  const Queries<NQ, KS> x = load_queries<NQ, DQK>(g, w, wrow, lane);
+  Queries<NQ, KS> x;  // (loaded with the first tile)
+  bool fresh = true;
   // positions of the wave's first and last token
   const int wlast = (w.rows - wrow < 32 * NQ ? w.rows : wrow + 32 * NQ) - 1;
   const int t_first = !active ? -1 : g.causal ? w.c - w.n + fdiv(g.by_group, wrow) : w.c - 1;
@@ -733,7 +750,7 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
 #pragma unroll
           for (int nq = 0; nq < NQ; ++nq) o[d][nq] = mfma32(vf[ks][d], p[ks][nq], o[d][nq]);
     };
-    // scores in base-2 units and their maximum per row
+    // the scores' maximum per row, in base-2 units (those of an fp8 cache with the keys' scales first)
     auto scale_max = [&](int i, int kb, f32x16 (&s)[NQ], float (&top)[NQ]) {
       f32x4 sc[4];
       if constexpr (FP8) {
@@ -745,7 +762,7 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
         top[nq] = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[nq][r] *= FP8 ? sc[r >> 2][r & 3] : g.scale_log2;
+          if constexpr (FP8) s[nq][r] *= sc[r >> 2][r & 3];
           top[nq] = fmaxf(top[nq], s[nq][r]);
         }
       }
@@ -768,7 +785,7 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
       bool grown = false;
 #pragma unroll
       for (int nq = 0; nq < NQ; ++nq) {
-        top[nq] = max2_xor32(top[nq]);
+        top[nq] = max2_xor32(FP8 ? top[nq] : top[nq] * g.scale_log2);
         grown |= top[nq] > m[nq] + kLazy;
       }
       if (__any(grown)) {
@@ -794,7 +811,8 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
       for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
-          float e0 = fast_exp2(s[nq][r] - m[nq]), e1 = fast_exp2(s[nq][r + 1] - m[nq]);
+          float e0 = fast_exp2(FP8 ? s[nq][r] - m[nq] : fmaf(s[nq][r], g.scale_log2, -m[nq]));
+          float e1 = fast_exp2(FP8 ? s[nq][r + 1] - m[nq] : fmaf(s[nq][r + 1], g.scale_log2, -m[nq]));
           l[nq] += e0;
           l[nq] += e1;
           if constexpr (FP8) {
@@ -825,15 +843,19 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
     // -- first tiles
     if constexpr (FP8) {
       const Regs y0 = fetch(0), y1 = nt > 1 ? fetch(1) : Regs{};
+      if (fresh) x = load_queries<NQ, DQK>(g, w, wrow, lane);
       if (nt > 2) ahead = fetch(2);
       commit(0, y0);
       if (nt > 1) commit(1, y1);
       __syncthreads();
     } else {
-      for (int i = 0; i < LEAD && i < nt; ++i) issue(i);
+      issue(0);
+      if (fresh) x = load_queries<NQ, DQK>(g, w, wrow, lane);
+      for (int i = 1; i < LEAD && i < nt; ++i) issue(i);
       if (nt >= LEAD) tile_barrier<(LEAD - 1) * G>();
       else tile_barrier<0>();
     }
+    fresh = false;
     f32x16 sa[NQ], sb[NQ];
     if (nw > 0) {
       load_k(0, 0);
@@ -894,16 +916,17 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
     }
   }
   // (a value that is no finite number leaves every accumulator it was multiplied into so)
-  float odd = 0.f;
+  float odd[4] = {};
 #pragma unroll
   for (int nq = 0; nq < NQ; ++nq) {
-    odd = fmaf(l[nq], 0.f, odd);
+    odd[0] = fmaf(l[nq], 0.f, odd[0]);
+    if (!FP8 && !(fabsf(m[nq]) < kFarScore) && m[nq] != kNoRef) odd[0] = 1.f;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) odd = fmaf(o[d][nq][r], 0.f, odd);
+      for (int r = 0; r < 16; ++r) odd[r & 3] = fmaf(o[d][nq][r], 0.f, odd[r & 3]);
   }
-  if (__syncthreads_or(odd != 0.f)) {  // (NaN != 0)
+  if (__syncthreads_or((odd[0] + odd[1]) + (odd[2] + odd[3]) != 0.f)) {  // (NaN != 0)
     careful_item<DQK, DV, KIND, NQ>(g, w, lds);
     return;
   }
