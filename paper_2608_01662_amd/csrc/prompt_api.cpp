@@ -13,9 +13,9 @@ namespace {
 
 #ifndef KMCB
 #define KMCB 512
-#define KPC 512
+#define KPC 256
 #endif
-constexpr int64_t kMostCutBlocks = KMCB, kLeastCutKeys = 16 * lsa::kPromptKeys;
+constexpr int64_t kMostCutBlocks = KMCB, kLeastCutKeys = 32 * lsa::kPromptKeys;
 constexpr int kPieces = KPC;
 
 // The pages of a call's caches

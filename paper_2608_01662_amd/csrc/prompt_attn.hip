@@ -105,8 +105,9 @@ __device__ __forceinline__ bool find_whole(const PromptGeom& g, int item, Share&
 }
 
 // The same of a call that has few blocks of rows: the keys of a sequence's blocks are cut into equal pieces, as many as make the
-// call's pieces about g.pieces, but of no fewer tiles than pay for the partial results of a piece, which the join reads again: 4, and
-// the more the more rows a block has. The first piece of a block tells the join about it.
+// call's pieces cost about 1 / g.pieces of all, but of no fewer tiles than pay for the partial results of a piece, which the join
+// reads again: 4, and the more the more rows a block has. (A tile costs 2 with up to 128 rows, a wave per SIMD, and 3 with more.) The
+// largest pieces come first, of up to 64 sequences. The first piece of a block tells the join about it.
 __device__ __forceinline__ bool find_piece(const PromptGeom& g, int id, Share& w) {
   const int lane = threadIdx.x & 63, group = (int)g.by_group.d;
   struct Seq {
@@ -130,13 +131,12 @@ __device__ __forceinline__ bool find_piece(const PromptGeom& g, int id, Share& w
     }
     return s;
   };
+  auto cost = [&](const Seq& s) { return s.n * group <= kRows / 2 ? 2 : 3; };
   Seq s = load(lane);
-  // (tiles of all: in float, they may pass 31 bits)
-  float total = (float)s.tiles * (float)(s.blocks * g.Hkv);
-  for (int b = lane + 64; b < g.n_seq; b += 64) {
-    const Seq y = load(b);
-    total += (float)y.tiles * (float)(y.blocks * g.Hkv);
-  }
+  // (in float: the sum may pass 31 bits)
+  auto all = [&](const Seq& y) { return (float)(cost(y) * y.blocks) * (float)(y.tiles) * (float)g.Hkv; };
+  float total = all(s);
+  for (int b = lane + 64; b < g.n_seq; b += 64) total += all(load(b));
   for (int k = 32; k >= 1; k >>= 1) total += __shfl_xor(total, k);
   const float share = total / (float)g.pieces;
   const int slots = g.pieces + g.blocks;
@@ -144,12 +144,26 @@ __device__ __forceinline__ bool find_piece(const PromptGeom& g, int id, Share& w
   for (int b0 = 0; b0 < g.n_seq; b0 += 64) {
     if (b0 > 0) s = load(b0 + lane);
     const int rows = s.n * group, least = 4 + 12 * (rows < kRows ? rows : kRows) / kRows;
-    const int each = share > (float)least ? (share < 1e9f ? (int)share + 1 : 1000000000) : least;
-    const int pieces = s.tiles > each ? (s.tiles + each - 1) / each : 1, inc = wave_scan(s.blocks * g.Hkv * pieces);
-    const int inc_items = wave_scan(s.blocks * g.Hkv);
+    const float even = share / (float)cost(s);
+    const int each = even > (float)least ? (even < 1e9f ? (int)even + 1 : 1000000000) : least;
+    const int pieces = s.tiles > each ? (s.tiles + each - 1) / each : 1;
+    int count = s.blocks * g.Hkv * pieces, count_items = s.blocks * g.Hkv, from = lane;
+    if (g.n_seq <= 64) {
+      const int size = cost(s) * (s.tiles / pieces);
+      int rank = 0;
+      for (int k = 0; k < g.n_seq; ++k) {
+        const int other = __builtin_amdgcn_readlane(size, k);
+        rank += other > size || (other == size && k < lane);
+      }
+      if (lane >= g.n_seq) rank = lane;
+      count = __builtin_amdgcn_ds_permute(4 * rank, count);
+      count_items = __builtin_amdgcn_ds_permute(4 * rank, count_items);
+      from = __builtin_amdgcn_ds_permute(4 * rank, lane);
+    }
+    const int inc = wave_scan(count), inc_items = wave_scan(count_items);
     const uint64_t past = id < slots ? __ballot(before + inc > id) : 0;
     if (past) {
-      const int i = __ffsll((unsigned long long)past) - 1;
+      const int at = __ffsll((unsigned long long)past) - 1, i = __builtin_amdgcn_readlane(from, at);
       w.b = b0 + i;
       w.n = __builtin_amdgcn_readlane(s.n, i);
       w.q0 = __builtin_amdgcn_readlane(s.q0, i);
@@ -157,8 +171,8 @@ __device__ __forceinline__ bool find_piece(const PromptGeom& g, int id, Share& w
       w.kv0 = __builtin_amdgcn_readlane(s.kv0, i);
       w.rows = w.n * group;
       const int np = __builtin_amdgcn_readlane(pieces, i), nb = __builtin_amdgcn_readlane(s.blocks, i);
-      const int k = id - (before + __builtin_amdgcn_readlane(inc, i) - nb * g.Hkv * np), block = k / np, piece = k - block * np;
-      const int item = items + __builtin_amdgcn_readlane(inc_items, i) - nb * g.Hkv + block;
+      const int k = id - (before + __builtin_amdgcn_readlane(inc, at) - nb * g.Hkv * np), block = k / np, piece = k - block * np;
+      const int item = items + __builtin_amdgcn_readlane(inc_items, at) - nb * g.Hkv + block;
       if (item >= g.blocks) return false;  // (offsets that are not ascending)
       w.head = block / nb;
       w.row0 = (block - w.head * nb) * kRows;
@@ -197,7 +211,7 @@ struct Prompt {
   static constexpr int NQ = NQ_, kWaves = kRows / (32 * NQ), kThreads = 64 * kWaves;
   static constexpr int CK = DQK / 8, CV = DV / 8, KS = DQK / 16, DB = DV / 32;
   static constexpr int kK = kKeys * DQK * 2, kV = kKeys * DV * 2;  // bytes of a tile
-  static constexpr int kLoadsK = kK / 1024 / kWaves, kLoadsV = kV / 1024 / kWaves;   // direct loads of a wave
+  static constexpr int kLoadsK = kK / 512 / kWaves, kLoadsV = kV / 512 / kWaves;   // direct loads of a wave, keys or values
   // Tile buffers. Step i reads keys i and i + 1 and values i - 1 and i, while tiles up to i + kLead are on their way (of fp8 caches
   // the last of them in registers): as many as fit.
   static constexpr int kLead = DQK == 192 ? 2 : 3, kBufsK = FP8 ? 3 : kLead + 1, kBufsV = FP8 ? 4 : kLead + 2;
@@ -223,16 +237,16 @@ struct Prompt {
   __device__ __forceinline__ void refresh() { asm volatile("" : "+v"(k_off), "+v"(v_off[0]), "+v"(v_off[1])); }
   // The K operand of a k-step, and the V operand of a block of 32 dims: `at` is the LDS address of the tile's half (a multiple of
   // 256, and a row starts at a multiple of what the exclusive or reaches) and for V of the k-step's first key.
-  __device__ __forceinline__ u32x4 k_operand(const uint8_t* at, int s) const {
+  __device__ __forceinline__ u32x4 k_operand(uint32_t at, int s) const {
     constexpr int X = CK == 16 ? 8 : 4;  // k-steps that the exclusive or of the chunks reaches
-    const uint32_t p = (((uint32_t)(uintptr_t)at + (uint32_t)k_off) ^ (uint32_t)(32 * (s % X))) + 32 * X * (s / X);
+    const uint32_t p = ((at + (uint32_t)k_off) ^ (uint32_t)(32 * (s % X))) + 32 * X * (s / X);
     return *(const __attribute__((address_space(3))) u32x4*)(p);
   }
-  __device__ __forceinline__ u32x4 v_operand(const uint8_t* at, int ks, int d) const {
+  __device__ __forceinline__ u32x4 v_operand(uint32_t at, int ks, int d) const {
     u32x2 y[2];
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      const uint32_t p = (((uint32_t)(uintptr_t)at + (uint32_t)v_off[half]) ^ (uint32_t)(64 * d)) + 16 * ks * DV * 2;
+      const uint32_t p = ((at + (uint32_t)v_off[half]) ^ (uint32_t)(64 * d)) + 16 * ks * DV * 2;
       y[half] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p)));
     }
     return u32x4{y[0].x, y[0].y, y[1].x, y[1].y};
@@ -337,38 +351,69 @@ __device__ __forceinline__ void store_rows(const PromptGeom& g, const Share& w, 
   }
 }
 
-// The pieces of a block joined: workgroup (y, i) takes rows of block i, DV / 4 threads a row.
+// The pieces of a block joined: workgroup (y, i) takes rows of block i, DV / 4 threads a row and four times as many, each of
+// which joins every fourth piece (a chain of loads of one piece after the other is what few rows of many pieces wait for).
+constexpr int kJoinGroups = 4;
 template <int DV>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g) {
-  constexpr int T = DV / 4, R = 256 / T;
+  constexpr int T = DV / 4, R = 256 / (T * kJoinGroups);
+  __shared__ float part[kJoinGroups][R][2];
+  __shared__ f32x4 part_o[kJoinGroups][R][T];
   const int item = blockIdx.y;
   if (item >= *g.n_joins) return;
   const int4 a = g.joins[2 * item], b = g.joins[2 * item + 1];
-  const int np = a.x, row0 = a.w, r = blockIdx.x * R + (int)threadIdx.x / T, row = row0 + r, d = 4 * ((int)threadIdx.x % T);
-  if (np <= 1 || r >= kRows || row >= b.x) return;
-  const int64_t at = (int64_t)a.y * g.slot_rows + r, step = g.slot_rows;
-  const f32x2* ml = reinterpret_cast<const f32x2*>(g.part_ml) + at;
-  float top = kNoRef;
-#pragma unroll 8
-  for (int k = 0; k < np; ++k) top = fmaxf(top, ml[k * step].x);
-  float sum = 0.f;
-  f32x4 y{};
-#pragma unroll 8
-  for (int k = 0; k < np; ++k) {
-    const f32x2 x = ml[k * step];
-    const float f = fast_exp2(x.x - top);
-    sum += f * x.y;
-    const f32x4 o = *reinterpret_cast<const f32x4*>(g.part_o + (at + k * step) * DV + d);
+  const int x = (int)threadIdx.x % T, grp = (int)threadIdx.x / T % kJoinGroups, lr = (int)threadIdx.x / (T * kJoinGroups);
+  const int np = a.x, row0 = a.w, rows = b.x - row0 < kRows ? b.x - row0 : kRows, d = 4 * x;
+  if (np <= 1) return;
+  const int64_t step = g.slot_rows;
+  const int group = (int)g.by_group.d;
+  for (int r0 = (int)blockIdx.x * R; r0 < rows; r0 += (int)gridDim.x * R) {
+    const int r = r0 + lr, row = row0 + r;
+    const bool in = r < rows;
+    const int64_t at = (int64_t)a.y * g.slot_rows + (in ? r : r0);
+    const f32x2* ml = reinterpret_cast<const f32x2*>(g.part_ml) + at;
+    float top = kNoRef;
+#pragma unroll 4
+    for (int k = grp; k < np; k += kJoinGroups) top = fmaxf(top, ml[k * step].x);
+    float sum = 0.f;
+    f32x4 y{};
+#pragma unroll 4
+    for (int k = grp; k < np; k += kJoinGroups) {
+      const f32x2 z = ml[k * step];
+      const float f = fast_exp2(z.x - top);
+      sum += f * z.y;
+      const f32x4 o = *reinterpret_cast<const f32x4*>(g.part_o + (at + k * step) * DV + d);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) y[q] += f * o[q];
+      for (int q = 0; q < 4; ++q) y[q] += f * o[q];
+    }
+    __syncthreads();  // everyone is done with the rows before
+    if (x == 0) {
+      part[grp][lr][0] = top;
+      part[grp][lr][1] = sum;
+    }
+    part_o[grp][lr][x] = y;
+    __syncthreads();
+    if (grp != 0 || !in) continue;
+#pragma unroll
+    for (int k = 1; k < kJoinGroups; ++k) top = fmaxf(top, part[k][lr][0]);
+    sum = 0.f;
+    y = f32x4{};
+#pragma unroll
+    for (int k = 0; k < kJoinGroups; ++k) {
+      const float f = fast_exp2(part[k][lr][0] - top);
+      sum += f * part[k][lr][1];
+      const f32x4 o = part_o[k][lr][x];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) y[q] += f * o[q];
+    }
+    const int j = fdiv(g.by_group, row);
+    const int64_t to = ((int64_t)b.y + j) * g.H + a.z * group + row - j * group;
+    if (g.lse && x == 0) g.lse[to] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    const float inv = 1.f / sum;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) y[q] = sum == 0.f ? 0.f : y[q] * inv;
+    *reinterpret_cast<u32x2*>(g.out + to * DV + d) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
   }
-  const int group = (int)g.by_group.d, j = fdiv(g.by_group, row);
-  const int64_t to = ((int64_t)b.y + j) * g.H + a.z * group + row - j * group;
-  if (g.lse && d == 0) g.lse[to] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
-  const float inv = 1.f / sum;
-#pragma unroll
-  for (int q = 0; q < 4; ++q) y[q] = sum == 0.f ? 0.f : y[q] * inv;
-  *reinterpret_cast<u32x2*>(g.out + to * DV + d) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
 }
 
 // ---------------------------------------------------------------- items with values that are no finite numbers
@@ -443,7 +488,7 @@ __device__ __forceinline__ void careful_rows(const PromptGeom& g, const Share& w
       for (int nq = 0; nq < NQ; ++nq) s[nq] = f32x16{};
 #pragma unroll
       for (int st = 0; st < KS; ++st) {
-        const u32x4 a = f.k_operand(lk + kb * 32 * DQK * 2, st);
+        const u32x4 a = f.k_operand((uint32_t)(uintptr_t)lk + kb * 32 * DQK * 2, st);
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) s[nq] = mfma32(a, x.q[nq][st], s[nq]);
       }
@@ -491,7 +536,7 @@ __device__ __forceinline__ void careful_rows(const PromptGeom& g, const Share& w
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
-          const u32x4 a = f.v_operand(lv + 32 * kb * DV * 2, ks, d);
+          const u32x4 a = f.v_operand((uint32_t)(uintptr_t)lv + 32 * kb * DV * 2, ks, d);
           u32x4 up{}, down{}, fin = a;  // 1 where a value is +inf or NaN, -inf or NaN; the others
 #pragma unroll
           for (int k = 0; k < 4; ++k)
@@ -594,20 +639,29 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
   const int64_t row_k = KIND ? DQK * (FP8 ? 1 : 2) : g.k_stride * 2, row_v = KIND ? DV * (FP8 ? 1 : 2) : g.v_stride * 2;  // bytes
   const uint8_t* const base_k = static_cast<const uint8_t*>(g.k) + (KIND ? 0 : w.head * DQK * 2 + w.kv0 * row_k);
   const uint8_t* const base_v = static_cast<const uint8_t*>(g.v) + (KIND ? 0 : w.head * DV * 2 + w.kv0 * row_v);
-  // direct loads of this wave: load j fills slots 64 (loads wave + j) + lane of the tile
-  uint32_t dma_k[T::kLoadsK], dma_v[T::kLoadsV];
+  // Direct loads: half the waves load the keys of a tile, half the values; load j of a wave fills slots 64 (loads part + j) + lane.
+  constexpr int LK = T::kLoadsK, LV = T::kLoadsV, LM = LK > LV ? LK : LV;
+  const bool loads_k = wave < T::kWaves / 2;
+  const int part = wave % (T::kWaves / 2);
+  const uint8_t* const base = loads_k ? base_k : base_v;
+  const int64_t row_bytes = loads_k ? row_k : row_v;
+  auto slot_of = [&](int j, int ln, int& r) {  // byte of its row that the slot of load j and lane ln holds
+    const int e = 64 * ((loads_k ? LK : LV) * part + j) + ln;
+    r = loads_k ? e / T::CK : e / T::CV;
+    return loads_k ? ((e % T::CK) ^ swz<T::CK>(r)) << 4 : ((e % T::CV) ^ swz<T::CV>(r)) << 4;
+  };
+  uint32_t dma[LM];
   if constexpr (!FP8) {
 #pragma unroll
-    for (int j = 0; j < T::kLoadsK; ++j) {
-      const int e = 64 * (T::kLoadsK * wave + j) + lane, r = e / T::CK;
-      dma_k[j] = (uint32_t)(r * (int)row_k + (((e % T::CK) ^ swz<T::CK>(r)) << 4)) - 1024 * (j & 3);
-    }
-#pragma unroll
-    for (int j = 0; j < T::kLoadsV; ++j) {
-      const int e = 64 * (T::kLoadsV * wave + j) + lane, r = e / T::CV;
-      dma_v[j] = (uint32_t)(r * (int)row_v + (((e % T::CV) ^ swz<T::CV>(r)) << 4)) - 1024 * (j & 3);
+    for (int j = 0; j < LM; ++j) {
+      int r;
+      const int c = slot_of(j, lane, r);
+      dma[j] = (uint32_t)(r * (int)row_bytes + c) - 1024 * (j & 3);
     }
   }
+  const uint32_t lds_k = (uint32_t)(uintptr_t)&lds.k[0][0], lds_v = (uint32_t)(uintptr_t)&lds.v[0][0];
+  auto next_k = [&](uint32_t at) { return at + T::kK == lds_k + NK * T::kK ? lds_k : at + T::kK; };
+  auto next_v = [&](uint32_t at) { return at + T::kV == lds_v + NV * T::kV ? lds_v : at + T::kV; };
 
   // Tiles [a, b) of the sequence, the pages of which (from page f1 on) are in LDS.
   auto run = [&](int a, int b, int f1) {
@@ -638,27 +692,25 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
     auto note = [&](int i, bool all) { there = (there & ~(1u << (i & 31))) | (uint32_t)all << (i & 31); };
 
     // -- bf16: tile a + i by direct loads into its buffers
+    uint32_t ring = loads_k ? lds_k : lds_v;  // of the next tile to be loaded
     auto issue = [&](int i) {
       const Where p = locate(a + i);
       note(i, whole_tiles ? p.all : __ballot(p.row < 0) == 0);
-      uint8_t *dk = lds.k[i % NK] + wave * T::kLoadsK * 1024, *dv = lds.v[i % NV] + wave * T::kLoadsV * 1024;
+      const uint32_t to = (uint32_t)uniform((int)(ring + part * (loads_k ? LK : LV) * 1024));
+      ring = loads_k ? next_k(ring) : next_v(ring);
       if (whole_tiles && p.all) {
-        const int64_t row0 = (int64_t)(uint32_t)p.row0;
-        const uint8_t *sk = uniform_ptr(base_k + row0 * row_k), *sv = uniform_ptr(base_v + row0 * row_v);
-        lds_dma16_tile<T::kLoadsK>(sk, dma_k, lds_addr(dk));
-        lds_dma16_tile<T::kLoadsV>(sv, dma_v, lds_addr(dv));
+        const uint8_t* from = uniform_ptr(base + (int64_t)(uint32_t)p.row0 * row_bytes);
+        if (LK == LV || loads_k) lds_dma16_tile<LK>(from, dma, to);
+        else lds_dma16_tile<LV>(from, dma, to);
         return;
       }
       const int ln = here(lane);
 #pragma unroll
-      for (int j = 0; j < T::kLoadsK; ++j) {
-        const int e = 64 * (T::kLoadsK * wave + j) + ln, r = e / T::CK, row = __shfl(p.row, r);
-        lds_dma16((row >= 0 ? base_k + (int64_t)(uint32_t)row * row_k + (((e % T::CK) ^ swz<T::CK>(r)) << 4) : zero_row), lds_addr(dk + j * 1024));
-      }
-#pragma unroll
-      for (int j = 0; j < T::kLoadsV; ++j) {
-        const int e = 64 * (T::kLoadsV * wave + j) + ln, r = e / T::CV, row = __shfl(p.row, r);
-        lds_dma16((row >= 0 ? base_v + (int64_t)(uint32_t)row * row_v + (((e % T::CV) ^ swz<T::CV>(r)) << 4) : zero_row), lds_addr(dv + j * 1024));
+      for (int j = 0; j < LM; ++j) {
+        if (j >= (loads_k ? LK : LV)) break;
+        int r;
+        const int c = slot_of(j, ln, r), row = __shfl(p.row, r & 63);
+        lds_dma16(row >= 0 ? base + (int64_t)(uint32_t)row * row_bytes + c : zero_row, to + j * 1024);
       }
     };
     // -- fp8: tile a + i into registers, and from there as bf16 into its buffers
@@ -718,20 +770,17 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
     // registers allow it), and all of the values.
     constexpr int KA = DQK == 192 ? 6 : KS;
     u32x4 kf[KA], vf[2][DB];
-    auto load_k = [&](int i, int kb) {
-      const uint8_t* lk = lds.k[i % NK] + kb * 32 * DQK * 2;
+    auto load_k = [&](uint32_t lk) {
 #pragma unroll
       for (int st = 0; st < KA; ++st) kf[st] = f.k_operand(lk, st);
     };
-    auto load_v = [&](int i, int kb) {
-      const uint8_t* lv = lds.v[i % NV] + kb * 32 * DV * 2;
+    auto load_v = [&](uint32_t lv) {
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
         for (int d = 0; d < DB; ++d) vf[ks][d] = f.v_operand(lv, ks, d);
     };
-    auto scores = [&](int i, int kb, f32x16 (&s)[NQ]) {
-      const uint8_t* lk = lds.k[i % NK] + kb * 32 * DQK * 2;
+    auto scores = [&](uint32_t lk, f32x16 (&s)[NQ]) {
 #pragma unroll
       for (int nq = 0; nq < NQ; ++nq) s[nq] = f32x16{};
 #pragma unroll
@@ -827,15 +876,20 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
       return ((there >> (i & 31)) & 1) && s0 <= t_first - (kKeys - 1) && (g.k_swa == 0 || s0 > t_last - g.k_swa || s0 <= g.k_sink - kKeys);
     };
     // start of step i: tile i + 1 has arrived, everyone is done with values i - 2 and keys i - 1; tile i + kLead sets out
-    constexpr int LEAD = T::kLead, G = T::kLoadsK + T::kLoadsV;
+    constexpr int LEAD = T::kLead;
+    auto wait = [&](auto tiles) {  // until at most so many tiles are on their way
+      constexpr int N = decltype(tiles)::value;
+      if (LK == LV || loads_k) tile_barrier<N * LK>();
+      else tile_barrier<N * LV>();
+    };
     auto advance = [&](int i) {
       if constexpr (FP8) {
         __syncthreads();
         if (i + 2 < nt) commit(i + 2, ahead);
         if (i + 3 < nt) ahead = fetch(i + 3);
       } else {
-        if (i + LEAD - 1 < nt) tile_barrier<(LEAD - 2) * G>();
-        else tile_barrier<0>();
+        if (i + LEAD - 1 < nt) wait(std::integral_constant<int, LEAD - 2>{});
+        else wait(std::integral_constant<int, 0>{});
         if (i + LEAD < nt) issue(i + LEAD);
       }
     };
@@ -852,15 +906,15 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
       issue(0);
       if (fresh) x = load_queries<NQ, DQK>(g, w, wrow, lane);
       for (int i = 1; i < LEAD && i < nt; ++i) issue(i);
-      if (nt >= LEAD) tile_barrier<(LEAD - 1) * G>();
-      else tile_barrier<0>();
+      if (nt >= LEAD) wait(std::integral_constant<int, LEAD - 1>{});
+      else wait(std::integral_constant<int, 0>{});
     }
     fresh = false;
     f32x16 sa[NQ], sb[NQ];
     if (nw > 0) {
-      load_k(0, 0);
-      scores(0, 0, sa);
-      load_v(0, 1);
+      load_k(lds_k);
+      scores(lds_k, sa);
+      load_v(lds_v + 32 * DV * 2);
     }
     // (before the first half there are no weights: zeros, on values that are there; and after the last one scores of what is left
     // in the buffers, which nobody reads)
@@ -868,27 +922,32 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
       for (int nq = 0; nq < NQ; ++nq) p[ks][nq] = u32x4{};
+    constexpr uint32_t HK = 32 * DQK * 2, HV = 32 * DV * 2;  // bytes of half a tile
+    uint32_t kc = lds_k, vc = lds_v;                         // buffers of tile i
     for (int i = 0; i < nt; ++i) {
       advance(i);
+      const uint32_t k = kc, v = vc;
+      kc = next_k(kc);
+      vc = next_v(vc);
       if (i >= nw) continue;
       f.refresh();
       const bool clear = is_clear(i);
       float top[NQ];
-      load_k(i, 1);
+      load_k(k + HK);
       values();
       scale_max(i, 0, sa, top);
       if (!clear) mask(i, 0, sa, top);
       rescale(top);
-      load_v(i, 0);
-      scores(i, 1, sb);
+      load_v(v);
+      scores(k + HK, sb);
       weights(i, 0, sa);
-      load_k(i + 1, 0);
+      load_k(kc);
       values();
       scale_max(i, 1, sb, top);
       if (!clear) mask(i, 1, sb, top);
       rescale(top);
-      load_v(i, 1);
-      scores(i + 1, 0, sa);
+      load_v(v + HV);
+      scores(kc, sa);
       weights(i, 1, sb);
     }
     if (nw > 0) values();
@@ -947,8 +1006,9 @@ hipError_t launch_prompt_attn(const PromptGeom& all, hipStream_t st) {
   if (g.pieces) {
     hipError_t e = launch_kernel(kernel, dim3((unsigned)(g.pieces + g.blocks + 1)), dim3(64 * kRows / (32 * NQ)), st, g);
     if (e != hipSuccess) return e;
-    const int rows = 256 / (g.d_v / 4);  // of a workgroup
-    return launch_kernel(g.d_v == 64 ? prompt_join_kernel<64> : prompt_join_kernel<128>, dim3((unsigned)((g.slot_rows + rows - 1) / rows), (unsigned)g.blocks),
+    // (workgroups of a block: one for as many rows as it takes at a time, but few where there are many blocks, most of them whole)
+    const int rows = 256 / (g.d_v / 4 * kJoinGroups), groups = (g.slot_rows + rows - 1) / rows, most = 8192 / g.blocks > 8 ? 8192 / g.blocks : 8;
+    return launch_kernel(g.d_v == 64 ? prompt_join_kernel<64> : prompt_join_kernel<128>, dim3((unsigned)(groups < most ? groups : most), (unsigned)g.blocks),
                          dim3(256), st, g);
   }
   constexpr int64_t kMost = 1 << 22;  // workgroups of a launch (2^32 threads and more are taken modulo 2^32)
