@@ -1,5 +1,5 @@
-// Python binding of the serving operators (module _serve): the host side of lsa_cache_append, lsa_norm_append and
-// lsa_decode_attn for torch tensors.
+// Python binding of the serving operators (module _serve): the host side of lsa_cache_append, lsa_norm_append, lsa_cache_read,
+// lsa_prefill_attn, lsa_chunk_attn and lsa_decode_attn for torch tensors.
 //
 // A decode step's kernels take 3 to 20 us, as long as a host in Python that looks at a dozen tensors, so the
 // checks that a good call passes, its allocations and the call itself are compiled. What is not as it should be is not explained
@@ -21,7 +21,9 @@ PyObject* raw_stream = nullptr;  // torch._C._cuda_getCurrentRawStream
 
 constexpr const char* kAppendNames[] = {"n_heads", "n_kv_heads", "d_k", "d_v", "rot_start", "rot_dim", "interleaved", "fp8"};
 constexpr const char* kAttnNames[] = {"n_heads", "n_kv_heads", "d_qk", "d_v", "latent", "fp8", "k_sink", "k_swa"};
-PyObject *append_names[8], *attn_names[8], *sm_scale_name;
+constexpr const char* kReadNames[] = {"n_kv_heads", "d_k", "d_v", "fp8"};
+constexpr const char* kPrefillNames[] = {"n_heads", "n_kv_heads", "d_qk", "d_v", "causal", "k_sink", "k_swa"};
+PyObject *append_names[8], *attn_names[8], *read_names[4], *prefill_names[7], *sm_scale_name;
 
 // (bools are ints; anything else that is no int of 32 bits is refused)
 bool to_int(PyObject* o, int32_t& x) {
@@ -43,6 +45,19 @@ bool int_attr(PyObject* o, PyObject* name, int32_t& x) {
   const bool ok = to_int(a, x);
   Py_DECREF(a);
   return ok;
+}
+
+// The softmax scale of an attention's parameters; false where it is no number.
+bool scale_attr(PyObject* o, float& x) {
+  PyObject* scale = PyObject_GetAttr(o, sm_scale_name);
+  const double v = scale == nullptr ? -1.0 : PyFloat_AsDouble(scale);
+  Py_XDECREF(scale);
+  if (PyErr_Occurred()) {
+    PyErr_Clear();
+    return false;
+  }
+  x = (float)v;
+  return true;
 }
 
 // The tensors of a call, all on one GPU.
@@ -106,6 +121,16 @@ struct Tensors {
     if (!ok || t == nullptr) return nullptr;
     need(t->scalar_type() == at::kFloat && t->is_contiguous() &&
          (t->sizes() == at::IntArrayRef({n_phys, heads, page}) || (heads == 1 && t->sizes() == at::IntArrayRef({n_phys, page}))));
+    return t;
+  }
+  // offsets [n_seq + 1] of sequences
+  const at::Tensor* offsets(PyObject* o, int64_t& n_seq) {
+    const at::Tensor* t = get(o);
+    if (t == nullptr) return fail();
+    need(t->scalar_type() == at::kInt && t->dim() == 1 && t->is_contiguous());
+    if (!ok) return nullptr;
+    n_seq = t->size(0) - 1;
+    need(n_seq >= 0 && n_seq <= INT32_MAX);
     return t;
   }
   // A page table [n_seq, max_pages]
@@ -293,17 +318,11 @@ PyObject* decode_attn(PyObject* module, PyObject* const* a, Py_ssize_t n_args) {
   int32_t p[8], rows_per_seq, max_pages;
   for (int i = 0; i < 8; ++i)
     if (!int_attr(a[0], attn_names[i], p[i])) Py_RETURN_NONE;
-  PyObject* scale = PyObject_GetAttr(a[0], sm_scale_name);
-  const double sm_scale = scale == nullptr ? -1.0 : PyFloat_AsDouble(scale);
-  Py_XDECREF(scale);
-  if (PyErr_Occurred()) {
-    PyErr_Clear();
-    Py_RETURN_NONE;
-  }
-  if (!to_int(a[6], rows_per_seq)) Py_RETURN_NONE;
+  float sm_scale;
+  if (!scale_attr(a[0], sm_scale) || !to_int(a[6], rows_per_seq)) Py_RETURN_NONE;
   const int64_t H = p[0], nk = p[1], d_qk = p[2], d_v = p[3];
   const bool latent = p[4] != 0, fp8 = p[5] != 0;
-  lsa_decode_attn_params prm{p[0], p[1], p[2], p[3], p[4], fp8 ? LSA_KEY_FP8_E4M3FN : LSA_KEY_BF16, p[6], p[7], (float)sm_scale};
+  lsa_decode_attn_params prm{p[0], p[1], p[2], p[3], p[4], fp8 ? LSA_KEY_FP8_E4M3FN : LSA_KEY_BF16, p[6], p[7], sm_scale};
   Tensors ts;
   const at::Tensor* q = ts.get(a[1]);
   if (q == nullptr || q->dim() != 3) Py_RETURN_NONE;
@@ -358,9 +377,167 @@ PyObject* decode_attn(PyObject* module, PyObject* const* a, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+// cache_read(prm, k_cache, cu, n_tok, page_table, start, v_cache, k_scale, v_scale, k_out, v_out)
+PyObject* cache_read(PyObject* module, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (n_args != 11) Py_RETURN_NONE;
+  int32_t p[4], n, max_pages;
+  for (int i = 0; i < 4; ++i)
+    if (!int_attr(a[0], read_names[i], p[i])) Py_RETURN_NONE;
+  if (!to_int(a[3], n) || n < 0) Py_RETURN_NONE;
+  const int64_t nk = p[0], d_k = p[1], d_v = p[2];
+  const bool fp8 = p[3] != 0, values = d_v != 0;
+  lsa_cache_read_params prm{p[0], p[1], p[2], fp8 ? LSA_KEY_FP8_E4M3FN : LSA_KEY_BF16};
+  Tensors ts;
+  int64_t n_phys = -1, page = 0, n_seq = 0;
+  const at::Tensor* k = ts.cache(a[1], fp8, nk, d_k, n_phys, page);
+  ts.need(values == (a[6] != Py_None) && (values || a[10] == Py_None));
+  if (!ts.ok) Py_RETURN_NONE;
+  const at::Tensor* v = values ? ts.cache(a[6], fp8, nk, d_v, n_phys, page) : nullptr;
+  const at::Tensor* k_scale = ts.scales(a[7], fp8, n_phys, nk, page);
+  const at::Tensor* v_scale = ts.scales(a[8], fp8 && values, n_phys, nk, page);
+  const at::Tensor* cu = ts.offsets(a[2], n_seq);
+  if (!ts.ok) Py_RETURN_NONE;
+  const at::Tensor* start = ts.whole(a[5], at::kInt, {n_seq}, true);
+  const at::Tensor* table = ts.table(a[4], max_pages);
+  ts.need((table == nullptr || table->size(0) == n_seq) && page <= INT32_MAX);
+  const at::Tensor* k_out = ts.whole(a[9], at::kBFloat16, {n, nk, d_k}, true);
+  const at::Tensor* v_out = values ? ts.whole(a[10], at::kBFloat16, {n, nk, d_v}, true) : nullptr;
+  if (!ts.ok) Py_RETURN_NONE;
+  const c10::DeviceGuard guard(c10::Device(c10::kCUDA, ts.device));
+  void* stream;
+  if (!stream_of(ts.device, stream)) return nullptr;
+  lsa_status st;
+  at::Tensor new_k, new_v;
+  {
+    Unlocked unlocked;
+    const auto options = k->options().dtype(at::kBFloat16);
+    if (k_out == nullptr) {
+      new_k = at::empty({n, nk, d_k}, options);
+      k_out = &new_k;
+    }
+    if (values && v_out == nullptr) {
+      new_v = at::empty({n, nk, d_v}, options);
+      v_out = &new_v;
+    }
+    st = lsa_cache_read(&prm, n, (int32_t)n_seq, at_of(k), at_of<float>(k_scale), at_of(v), at_of<float>(v_scale), at_of<int32_t>(cu),
+                        at_of<int32_t>(start), at_of<int32_t>(table), max_pages, (int32_t)page, n_phys, at_of(k_out), at_of(v_out), stream);
+  }
+  if (st != LSA_OK) return not_done(module, st, "lsa_cache_read");
+  return tuple_of({k_out, v_out});
+  END_HANDLE_TH_ERRORS
+}
+
+// What the attentions of prompts and chunks return and work in: `out`, `lse` (None, True, False or a tensor) and `workspace` as they are given.
+struct Outputs {
+  const at::Tensor *out, *lse, *workspace;
+  at::Tensor made[3];
+  Outputs(Tensors& ts, PyObject* o, PyObject* l, PyObject* w, int64_t n, int64_t H, int64_t d_v) {
+    out = ts.whole(o, at::kBFloat16, {n, H, d_v}, true);
+    lse = l == Py_True || l == Py_False ? nullptr : ts.whole(l, at::kFloat, {n, H}, true);
+    workspace = ts.get(w);
+    ts.need(workspace == nullptr || workspace->is_contiguous());
+  }
+  void make(const at::Tensor* q, bool want_lse, size_t need, int64_t n, int64_t H, int64_t d_v) {
+    if (out == nullptr) out = &(made[0] = at::empty({n, H, d_v}, q->options()));
+    if (want_lse) lse = &(made[1] = at::empty({n, H}, q->options().dtype(at::kFloat)));
+    if (need == 0) workspace = nullptr;
+    else if (workspace == nullptr) workspace = &(made[2] = at::empty({(int64_t)need}, q->options().dtype(at::kByte)));
+  }
+};
+
+// prefill_attn(prm, q, k, v, cu_q, cu_kv, out, lse, workspace)
+PyObject* prefill_attn(PyObject* module, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (n_args != 9) Py_RETURN_NONE;
+  lsa_prefill_attn_params prm{};
+  int32_t p[7];
+  for (int i = 0; i < 7; ++i)
+    if (!int_attr(a[0], prefill_names[i], p[i])) Py_RETURN_NONE;
+  if (!scale_attr(a[0], prm.sm_scale)) Py_RETURN_NONE;
+  prm = lsa_prefill_attn_params{p[0], p[1], p[2], p[3], p[4], p[5], p[6], prm.sm_scale};
+  const int64_t H = p[0], nk = p[1], d_qk = p[2], d_v = p[3];
+  Tensors ts;
+  const at::Tensor *q = ts.get(a[1]), *k = ts.get(a[2]), *v = ts.get(a[3]);
+  if (q == nullptr || k == nullptr || v == nullptr || q->dim() != 3 || k->dim() != 3) Py_RETURN_NONE;
+  const int64_t n = q->size(0), n_kv = k->size(0);
+  int64_t qs = 0, ks = 0, vs = 0, n_seq = 0;
+  ts.tokens(a[1], n, H, d_qk, qs);
+  ts.tokens(a[2], n_kv, nk, d_qk, ks);
+  ts.tokens(a[3], n_kv, nk, d_v, vs);
+  const at::Tensor* cu_q = ts.offsets(a[4], n_seq);
+  if (!ts.ok) Py_RETURN_NONE;
+  const at::Tensor* cu_kv = ts.whole(a[5], at::kInt, {n_seq + 1}, true);
+  ts.need(cu_kv != nullptr || n_kv == n);
+  Outputs y(ts, a[6], a[7], a[8], n, H, d_v);
+  if (!ts.ok) Py_RETURN_NONE;
+  const c10::DeviceGuard guard(c10::Device(c10::kCUDA, ts.device));
+  void* stream;
+  if (!stream_of(ts.device, stream)) return nullptr;
+  lsa_status st;
+  {
+    Unlocked unlocked;
+    y.make(q, a[7] == Py_True, lsa_prefill_attn_workspace_size(&prm, (int32_t)n_seq, n, n_kv), n, H, d_v);
+    st = lsa_prefill_attn(&prm, (int32_t)n_seq, n, n_kv, at_of(q), qs, at_of(k), ks, at_of(v), vs, at_of<int32_t>(cu_q), at_of<int32_t>(cu_kv),
+                          at_of(y.out), at_of<float>(y.lse), at_of(y.workspace), y.workspace == nullptr ? 0 : y.workspace->nbytes(), stream);
+  }
+  if (st != LSA_OK) return not_done(module, st, "lsa_prefill_attn");
+  return tuple_of({y.out, y.lse});
+  END_HANDLE_TH_ERRORS
+}
+
+// chunk_attn(prm, q, k_cache, v_cache, cu_q, ctx_len, page_table, k_scale, v_scale, out, lse, workspace)
+PyObject* chunk_attn(PyObject* module, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (n_args != 12) Py_RETURN_NONE;
+  int32_t p[8], max_pages;
+  float sm_scale;
+  for (int i = 0; i < 8; ++i)
+    if (!int_attr(a[0], attn_names[i], p[i])) Py_RETURN_NONE;
+  if (!scale_attr(a[0], sm_scale)) Py_RETURN_NONE;
+  const int64_t H = p[0], nk = p[1], d_qk = p[2], d_v = p[3];
+  const bool fp8 = p[5] != 0;
+  lsa_decode_attn_params prm{p[0], p[1], p[2], p[3], p[4], fp8 ? LSA_KEY_FP8_E4M3FN : LSA_KEY_BF16, p[6], p[7], sm_scale};
+  Tensors ts;
+  const at::Tensor* q = ts.get(a[1]);
+  if (q == nullptr || q->dim() != 3) Py_RETURN_NONE;
+  const int64_t n = q->size(0);
+  ts.whole(a[1], at::kBFloat16, {n, H, d_qk});
+  int64_t n_phys = -1, page = 0, n_seq = 0;
+  const at::Tensor* k = ts.cache(a[2], fp8, nk, d_qk, n_phys, page);
+  if (!ts.ok) Py_RETURN_NONE;
+  const at::Tensor* v = ts.cache(a[3], fp8, nk, d_v, n_phys, page);
+  const at::Tensor* k_scale = ts.scales(a[7], fp8, n_phys, nk, page);
+  const at::Tensor* v_scale = ts.scales(a[8], fp8, n_phys, nk, page);
+  const at::Tensor* cu_q = ts.offsets(a[4], n_seq);
+  if (!ts.ok) Py_RETURN_NONE;
+  const at::Tensor* ctx_len = ts.whole(a[5], at::kInt, {n_seq});
+  const at::Tensor* table = ts.table(a[6], max_pages);
+  ts.need((table == nullptr || table->size(0) == n_seq) && page <= INT32_MAX);
+  Outputs y(ts, a[9], a[10], a[11], n, H, d_v);
+  if (!ts.ok) Py_RETURN_NONE;
+  const c10::DeviceGuard guard(c10::Device(c10::kCUDA, ts.device));
+  void* stream;
+  if (!stream_of(ts.device, stream)) return nullptr;
+  lsa_status st;
+  {
+    Unlocked unlocked;
+    y.make(q, a[10] == Py_True, lsa_chunk_attn_workspace_size(&prm, (int32_t)n_seq, n, max_pages, (int32_t)page), n, H, d_v);
+    st = lsa_chunk_attn(&prm, (int32_t)n_seq, n, at_of(q), at_of(k), at_of<float>(k_scale), at_of(v), at_of<float>(v_scale), at_of<int32_t>(cu_q),
+                        at_of<int32_t>(ctx_len), at_of<int32_t>(table), max_pages, (int32_t)page, n_phys, at_of(y.out), at_of<float>(y.lse),
+                        at_of(y.workspace), y.workspace == nullptr ? 0 : y.workspace->nbytes(), stream);
+  }
+  if (st != LSA_OK) return not_done(module, st, "lsa_chunk_attn");
+  return tuple_of({y.out, y.lse});
+  END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {
     {"cache_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(append<false>)), METH_FASTCALL, nullptr},
     {"norm_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(append<true>)), METH_FASTCALL, nullptr},
+    {"cache_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_read)), METH_FASTCALL, nullptr},
+    {"prefill_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(prefill_attn)), METH_FASTCALL, nullptr},
+    {"chunk_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(chunk_attn)), METH_FASTCALL, nullptr},
     {"decode_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(decode_attn)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef definition = {PyModuleDef_HEAD_INIT, "_serve", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -373,9 +550,14 @@ PyMODINIT_FUNC PyInit__serve() {
   raw_stream = PyObject_GetAttrString(c, "_cuda_getCurrentRawStream");
   Py_DECREF(c);
   if (raw_stream == nullptr) return nullptr;
-  for (int i = 0; i < 8; ++i)
-    if ((append_names[i] = PyUnicode_InternFromString(kAppendNames[i])) == nullptr || (attn_names[i] = PyUnicode_InternFromString(kAttnNames[i])) == nullptr)
-      return nullptr;
+  auto intern = [](PyObject** to, const char* const* names, int n) {
+    for (int i = 0; i < n; ++i)
+      if ((to[i] = PyUnicode_InternFromString(names[i])) == nullptr) return false;
+    return true;
+  };
+  if (!intern(append_names, kAppendNames, 8) || !intern(attn_names, kAttnNames, 8) || !intern(read_names, kReadNames, 4) ||
+      !intern(prefill_names, kPrefillNames, 7))
+    return nullptr;
   if ((sm_scale_name = PyUnicode_InternFromString("sm_scale")) == nullptr) return nullptr;
   return PyModule_Create(&definition);
 }

@@ -849,6 +849,9 @@ def cache_read(prm: CacheReadParams, k_cache: torch.Tensor, cu: torch.Tensor, n_
 
     cu [n_seq + 1] int32: rows cu[b] .. cu[b + 1] - 1 are positions start[b] .. (None: 0 ..) of sequence b; n_tok: rows of the
     outputs, of which those behind cu[n_seq] are left as they are. Caches as cache_append writes them."""
+    done = (_serve or _serving()).cache_read(prm, k_cache, cu, n_tok, page_table, start, v_cache, k_scale, v_scale, k_out, v_out)
+    if done is not None:
+        return done
     nk, d_k, d_v, fp8 = prm.n_kv_heads, prm.d_k, prm.d_v, prm.fp8
     dev = k_cache.device if isinstance(k_cache, torch.Tensor) else None
     n_phys, page = _paged_shape("k_cache", k_cache, fp8, nk, d_k, dev)
@@ -984,6 +987,9 @@ def prefill_attn(prm: PrefillAttnParams, q: torch.Tensor, k: torch.Tensor, v: to
     q [n_tok, H, d_qk], k [n_kv, n_kv_heads, d_qk], v [n_kv, n_kv_heads, d_v]: bf16 with any token stride. Sequence b has the
     tokens cu_q[b] .. cu_q[b + 1] - 1 and the keys cu_kv[b] .. cu_kv[b + 1] - 1 (None: those of its tokens), the tokens
     being its last positions. Rows of no sequence are left as they are."""
+    done = (_serve or _serving()).prefill_attn(prm, q, k, v, cu_q, cu_kv, out, lse, workspace)
+    if done is not None:
+        return done
     H, nk = prm.n_heads, prm.n_kv_heads
     is_tensor = isinstance(q, torch.Tensor)
     dev, i = (q.device, q.get_device()) if is_tensor else (None, -1)
@@ -1022,6 +1028,9 @@ def chunk_attn(prm: DecodeAttnParams, q: torch.Tensor, k_cache: torch.Tensor, v_
 
     Sequence b has the tokens cu_q[b] .. cu_q[b + 1] - 1 of q, the newest of its ctx_len[b]. Caches as cache_append writes them;
     prm as for decode_attn, not latent. Rows of no sequence are left as they are."""
+    done = (_serve or _serving()).chunk_attn(prm, q, k_cache, v_cache, cu_q, ctx_len, page_table, k_scale, v_scale, out, lse, workspace)
+    if done is not None:
+        return done
     H, nk, d, fp8 = prm.n_heads, prm.n_kv_heads, prm.d_qk, prm.fp8
     n = q.shape[0] if isinstance(q, torch.Tensor) and q.dim() == 3 else None
     _need("q", q, _BF16, (n, H, d))
