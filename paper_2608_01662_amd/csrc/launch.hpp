@@ -185,7 +185,7 @@ struct PromptGeom {
   int pieces, blocks;          // blocks of kPromptRows query rows of all heads, at most
   int slot_rows;               // rows of a piece's partial results
   float *part_o, *part_ml;     // [pieces + blocks, slot_rows, d_v] unnormalised, [.., 2] maximum and sum
-  int4* joins;                 // [blocks, 2]: pieces, first slot, head, row0; rows, first token
+  int4* joins;                 // [blocks, 2]: pieces, slot of the first (of the others Hkv apart), head, row0; rows, first token
   int32_t* n_joins;
 };
 constexpr int kPromptRows = 256, kPromptKeys = 64, kPromptPages = 2048;

@@ -11,12 +11,8 @@ using lsa::hip_fail;
 
 namespace {
 
-#ifndef KMCB
-#define KMCB 512
-#define KPC 256
-#endif
-constexpr int64_t kMostCutBlocks = KMCB, kLeastCutKeys = 32 * lsa::kPromptKeys;
-constexpr int kPieces = KPC;
+constexpr int64_t kMostCutBlocks = 512, kLeastCutKeys = 16 * lsa::kPromptKeys;
+constexpr int kPieces = 256;
 
 // The pages of a call's caches
 lsa_status check_pages(const int32_t* page_table, int32_t n_seq, int32_t max_pages, int32_t kv_page_size, int64_t n_phys, int32_t n_kv_heads) {

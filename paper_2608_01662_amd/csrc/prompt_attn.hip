@@ -171,11 +171,11 @@ __device__ __forceinline__ bool find_piece(const PromptGeom& g, int id, Share& w
       w.kv0 = __builtin_amdgcn_readlane(s.kv0, i);
       w.rows = w.n * group;
       const int np = __builtin_amdgcn_readlane(pieces, i), nb = __builtin_amdgcn_readlane(s.blocks, i);
-      const int k = id - (before + __builtin_amdgcn_readlane(inc, at) - nb * g.Hkv * np), block = k / np, piece = k - block * np;
-      const int item = items + __builtin_amdgcn_readlane(inc_items, at) - nb * g.Hkv + block;
+      const int k = id - (before + __builtin_amdgcn_readlane(inc, at) - nb * g.Hkv * np), rest = k / g.Hkv, nth = rest / np, piece = rest - nth * np;
+      w.head = k - rest * g.Hkv;
+      const int item = items + __builtin_amdgcn_readlane(inc_items, at) - (nb - nth) * g.Hkv + w.head;
       if (item >= g.blocks) return false;  // (offsets that are not ascending)
-      w.head = block / nb;
-      w.row0 = (block - w.head * nb) * kRows;
+      w.row0 = (nb - 1 - nth) * kRows;
       span_of(g, w);
       w.p0 = (int)((int64_t)w.nt * piece / np);
       w.p1 = (int)((int64_t)w.nt * (piece + 1) / np);
@@ -205,19 +205,21 @@ __device__ __forceinline__ float sum2_xor32(float x) {
 }
 
 // ---------------------------------------------------------------- sizes, LDS layout, operand offsets
-template <int DQK, int DV, int KIND, int NQ_>  // KIND 0: contiguous bf16, 1: paged bf16, 2: paged fp8; blocks of 32 rows of a wave
+constexpr int kWaves = kRows / 32, kThreads = 64 * kWaves;  // a wave has 32 rows, the columns of its products
+template <int DQK, int DV, int KIND>  // KIND 0: contiguous bf16, 1: paged bf16, 2: paged fp8
 struct Prompt {
   static constexpr bool FP8 = KIND == 2;
-  static constexpr int NQ = NQ_, kWaves = kRows / (32 * NQ), kThreads = 64 * kWaves;
   static constexpr int CK = DQK / 8, CV = DV / 8, KS = DQK / 16, DB = DV / 32;
   static constexpr int kK = kKeys * DQK * 2, kV = kKeys * DV * 2;  // bytes of a tile
   static constexpr int kLoadsK = kK / 512 / kWaves, kLoadsV = kV / 512 / kWaves;   // direct loads of a wave, keys or values
-  // Tile buffers. Step i reads keys i and i + 1 and values i - 1 and i, while tiles up to i + kLead are on their way (of fp8 caches
-  // the last of them in registers): as many as fit.
-  static constexpr int kLead = DQK == 192 ? 2 : 3, kBufsK = FP8 ? 3 : kLead + 1, kBufsV = FP8 ? 4 : kLead + 2;
+  // Tile buffers. Step i reads keys i and i + 1 and values i, while tiles up to i + kLead are on their way: as many as fit. Of fp8
+  // caches tile i + 2 is written in bf16 meanwhile, from the kRaw buffers that the tiles up to i + 2 + kRaw come into.
+  static constexpr int kLead = FP8 || DQK == 192 ? 2 : 3, kBufs = kLead + 1, kRaw = 3;
   struct Lds {
-    uint8_t k[kBufsK][kK], v[kBufsV][kV];
-    float scales[FP8 ? kBufsV : 1][2][FP8 ? kKeys : 4];  // of keys (times the softmax scale) and of values
+    uint8_t k[kBufs][kK], v[kBufs][kV];
+    uint8_t raw[FP8 ? kRaw : 1][FP8 ? kK : 16];  // of fp8 tiles the keys, then the values
+    float raw_scales[FP8 ? kRaw : 1][2][FP8 ? kKeys : 4];
+    float scales[FP8 ? kBufs : 1][2][FP8 ? kKeys : 4];  // of keys (times the softmax scale) and of values
     int pages[KIND ? kPageSlots : 1];
   };
   // LDS offsets of this lane's operands in a tile: of K at k-step 0 (at s: ^ 32 s, or by 4 k-steps), of the first four and of the second four values
@@ -277,30 +279,25 @@ __device__ __forceinline__ float scaled_below(float s, float scale, float m) {
   return z - m;
 }
 
-// This lane's query rows.
-template <int NQ, int KS>
-struct Queries {
-  u32x4 q[NQ][KS];  // B operands: columns are rows, dims of k-step s
-  int t[NQ];        // position of the row's token, -1 and less: none
+// This lane's query row.
+template <int KS>
+struct Query {
+  u32x4 q[KS];  // B operands: columns are rows, dims of k-step s
+  int t;        // position of the row's token, -1 and less: none
 };
-template <int NQ, int DQK>
-__device__ __forceinline__ Queries<NQ, DQK / 16> load_queries(const PromptGeom& g, const Share& w, int wrow, int lane) {
-  Queries<NQ, DQK / 16> x;
+template <int DQK>
+__device__ __forceinline__ Query<DQK / 16> load_query(const PromptGeom& g, const Share& w, int wrow, int lane) {
+  Query<DQK / 16> x;
   const int group = (int)g.by_group.d;
+  const int row = wrow + (lane & 31), r = row < w.rows ? row : w.rows - 1, j = fdiv(g.by_group, r);
+  x.t = g.causal ? w.c - w.n + j : w.c - 1;
+  const uint16_t* p = g.q + (w.q0 + j) * g.q_stride + (int64_t)(w.head * group + r - j * group) * DQK + 8 * (lane >> 5);
 #pragma unroll
-  for (int nq = 0; nq < NQ; ++nq) {
-    const int row = wrow + 32 * nq + (lane & 31), r = row < w.rows ? row : w.rows - 1, j = fdiv(g.by_group, r);
-    x.t[nq] = g.causal ? w.c - w.n + j : w.c - 1;
-    const uint16_t* p = g.q + (w.q0 + j) * g.q_stride + (int64_t)(w.head * group + r - j * group) * DQK + 8 * (lane >> 5);
-#pragma unroll
-    for (int s = 0; s < DQK / 16; ++s) x.q[nq][s] = *reinterpret_cast<const u32x4*>(p + 16 * s);
-  }
+  for (int s = 0; s < DQK / 16; ++s) x.q[s] = *reinterpret_cast<const u32x4*>(p + 16 * s);
   // They have arrived here: the compiler would wait for them where it first uses them, in a loop at every turn, and for the direct
   // loads, of which it does not know, with them.
 #pragma unroll
-  for (int nq = 0; nq < NQ; ++nq)
-#pragma unroll
-    for (int s = 0; s < DQK / 16; ++s) asm volatile("" : "+v"(x.q[nq][s]));
+  for (int s = 0; s < DQK / 16; ++s) asm volatile("" : "+v"(x.q[s]));
   return x;
 }
 
@@ -313,42 +310,38 @@ __device__ __forceinline__ uint32_t sees32(const PromptGeom& g, int t, int s0, u
 }
 
 // ---------------------------------------------------------------- output
-template <int NQ, int DV>
-__device__ __forceinline__ void store_rows(const PromptGeom& g, const Share& w, int wrow, int lane, const f32x16 (&o)[DV / 32][NQ],
-                                           const float (&m)[NQ], const float (&l)[NQ]) {
+template <int DV>
+__device__ __forceinline__ void store_row(const PromptGeom& g, const Share& w, int wrow, int lane, const f32x16 (&o)[DV / 32], float m, float l) {
   const int group = (int)g.by_group.d, h = lane >> 5;
-#pragma unroll
-  for (int nq = 0; nq < NQ; ++nq) {
-    const int row = wrow + 32 * nq + (lane & 31);
-    const float sum = sum2_xor32(l[nq]), inv = 1.f / sum;
-    const bool in = row < w.rows;
-    if (w.slot >= 0) {
-      if (!in) continue;
-      const int64_t at = (int64_t)w.slot * g.slot_rows + row - w.row0;
-      if (h == 0) *reinterpret_cast<f32x2*>(g.part_ml + 2 * at) = f32x2{m[nq], sum};
-#pragma unroll
-      for (int d = 0; d < DV / 32; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4)
-          *reinterpret_cast<f32x4*>(g.part_o + at * DV + 32 * d + 2 * r + 4 * h) = f32x4{o[d][nq][r], o[d][nq][r + 1], o[d][nq][r + 2], o[d][nq][r + 3]};
-      continue;
-    }
-    const int j = fdiv(g.by_group, row);
-    const int64_t at = (w.q0 + j) * g.H + w.head * group + row - j * group;
-    if (g.lse && in && h == 0) g.lse[at] = sum == 0.f ? -INFINITY : (m[nq] + __builtin_amdgcn_logf(sum)) * kLn2;
+  const int row = wrow + (lane & 31);
+  const float sum = sum2_xor32(l), inv = 1.f / sum;
+  const bool in = row < w.rows;
+  if (w.slot >= 0) {
+    if (!in) return;
+    const int64_t at = (int64_t)w.slot * g.slot_rows + row - w.row0;
+    if (h == 0) *reinterpret_cast<f32x2*>(g.part_ml + 2 * at) = f32x2{m, sum};
 #pragma unroll
     for (int d = 0; d < DV / 32; ++d)
 #pragma unroll
-      for (int r = 0; r < 16; r += 8) {
-        // dims 2 r + 4 h and 2 r + 8 + 4 h, four each: swapped with lane l ^ 32 into eight from 2 r + 8 h on
-        uint32_t y[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          y[k] = pack_bf16x2(sum == 0.f ? 0.f : o[d][nq][r + 2 * k] * inv, sum == 0.f ? 0.f : o[d][nq][r + 2 * k + 1] * inv);
-        const auto lo = __builtin_amdgcn_permlane32_swap(y[0], y[2], false, false), hi = __builtin_amdgcn_permlane32_swap(y[1], y[3], false, false);
-        if (in) *reinterpret_cast<u32x4*>(g.out + at * DV + 32 * d + 2 * r + 8 * h) = u32x4{lo[0], hi[0], lo[1], hi[1]};
-      }
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<f32x4*>(g.part_o + at * DV + 32 * d + 2 * r + 4 * h) = f32x4{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
+    return;
   }
+  const int j = fdiv(g.by_group, row);
+  const int64_t at = (w.q0 + j) * g.H + w.head * group + row - j * group;
+  if (g.lse && in && h == 0) g.lse[at] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+#pragma unroll
+  for (int d = 0; d < DV / 32; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; r += 8) {
+      // dims 2 r + 4 h and 2 r + 8 + 4 h, four each: swapped with lane l ^ 32 into eight from 2 r + 8 h on
+      uint32_t y[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        y[k] = pack_bf16x2(sum == 0.f ? 0.f : o[d][r + 2 * k] * inv, sum == 0.f ? 0.f : o[d][r + 2 * k + 1] * inv);
+      const auto lo = __builtin_amdgcn_permlane32_swap(y[0], y[2], false, false), hi = __builtin_amdgcn_permlane32_swap(y[1], y[3], false, false);
+      if (in) *reinterpret_cast<u32x4*>(g.out + at * DV + 32 * d + 2 * r + 8 * h) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+    }
 }
 
 // The pieces of a block joined: workgroup (y, i) takes rows of block i, DV / 4 threads a row and four times as many, each of
@@ -365,7 +358,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g) {
   const int x = (int)threadIdx.x % T, grp = (int)threadIdx.x / T % kJoinGroups, lr = (int)threadIdx.x / (T * kJoinGroups);
   const int np = a.x, row0 = a.w, rows = b.x - row0 < kRows ? b.x - row0 : kRows, d = 4 * x;
   if (np <= 1) return;
-  const int64_t step = g.slot_rows;
+  const int64_t step = (int64_t)g.slot_rows * g.Hkv;  // from a piece to the next
   const int group = (int)g.by_group.d;
   for (int r0 = (int)blockIdx.x * R; r0 < rows; r0 += (int)gridDim.x * R) {
     const int r = r0 + lr, row = row0 + r;
@@ -420,25 +413,20 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g) {
 // A weight of 0 does not silence a NaN or an infinity in V, and a tile is multiplied whole. So an item whose outputs are not all
 // finite is done again here, a tile at a time, with such values taken out of the product and added to the rows that attend to them
 // (and to no others). Nothing else takes this way: it is written to be right, not fast.
-template <int DQK, int DV, int KIND, int NQ_>
-__device__ __forceinline__ void careful_rows(const PromptGeom& g, const Share& w, int part, typename Prompt<DQK, DV, KIND, NQ_>::Lds& lds) {
-  using T = Prompt<DQK, DV, KIND, NQ_>;
-  constexpr int KS = T::KS, DB = T::DB, NQ = 1;  // (the registers of half a wave's rows)
+template <int DQK, int DV, int KIND>
+__device__ __forceinline__ void careful_item(const PromptGeom& g, const Share& w, typename Prompt<DQK, DV, KIND>::Lds& lds) {
+  using T = Prompt<DQK, DV, KIND>;
+  constexpr int KS = T::KS, DB = T::DB;
   constexpr bool FP8 = T::FP8;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
-  const int wrow = w.row0 + 32 * (T::NQ * wave + part);
+  const int wrow = w.row0 + 32 * wave;
   const bool active = wrow < w.rows;
   T f(lane);
-  const Queries<NQ, KS> x = load_queries<NQ, DQK>(g, w, wrow, lane);
-  f32x16 o[DB][NQ];
-  float m[NQ], l[NQ];
+  const Query<KS> x = load_query<DQK>(g, w, wrow, lane);
+  f32x16 o[DB];
+  float m = kNoRef, l = 0.f;
 #pragma unroll
-  for (int nq = 0; nq < NQ; ++nq) {
-    m[nq] = kNoRef;
-    l[nq] = 0.f;
-#pragma unroll
-    for (int d = 0; d < DB; ++d) o[d][nq] = f32x16{};
-  }
+  for (int d = 0; d < DB; ++d) o[d] = f32x16{};
   uint8_t *lk = lds.k[0], *lv = lds.v[0];
   for (int i = w.p0; i < w.p1; ++i) {
     const int s0 = (i < w.ns ? i : i + w.skip) * kKeys;
@@ -454,7 +442,7 @@ __device__ __forceinline__ void careful_rows(const PromptGeom& g, const Share& w
     };
     auto load = [&](const void* base, int64_t stride, uint8_t* dst, auto width) {
       constexpr int D = decltype(width)::value, C = D / 8;
-      for (int e = (int)threadIdx.x; e < kKeys * C; e += T::kThreads) {
+      for (int e = (int)threadIdx.x; e < kKeys * C; e += kThreads) {
         const int r = e / C, c = e % C;
         const int64_t row = row_of(r);
         u32x4 y{};
@@ -483,54 +471,47 @@ __device__ __forceinline__ void careful_rows(const PromptGeom& g, const Share& w
 #pragma nounroll
     for (int kb = 0; kb < 2; ++kb) {  // (halves of a tile and sums in the order of the steps below: other rows keep their bits)
       f.refresh();
-      f32x16 s[NQ];
-#pragma unroll
-      for (int nq = 0; nq < NQ; ++nq) s[nq] = f32x16{};
+      f32x16 s{};
 #pragma unroll
       for (int st = 0; st < KS; ++st) {
         const u32x4 a = f.k_operand((uint32_t)(uintptr_t)lk + kb * 32 * DQK * 2, st);
-#pragma unroll
-        for (int nq = 0; nq < NQ; ++nq) s[nq] = mfma32(a, x.q[nq][st], s[nq]);
+        s = mfma32(a, x.q[st], s);
       }
-      u32x4 p[2][NQ];     // [k-step of 16]
-      uint32_t live[NQ];  // scores that are not -inf
+      u32x4 p[2];     // [k-step of 16]
+      float top = -INFINITY;
+      const uint32_t seen = sees32(g, x.t, s0 + 32 * kb, (uint32_t)(there >> (32 * kb))) >> (4 * h);
 #pragma unroll
-      for (int nq = 0; nq < NQ; ++nq) {
-        float top = -INFINITY;
-        const uint32_t seen = sees32(g, x.t[nq], s0 + 32 * kb, (uint32_t)(there >> (32 * kb))) >> (4 * h);
+      for (int r = 0; r < 16; ++r) {
+        const int key = 8 * (r >> 2) + (r & 3);
+        if constexpr (FP8) s[r] *= lds.scales[0][0][32 * kb + 4 * h + key];
+        s[r] = (seen >> key) & 1 ? s[r] : -INFINITY;
+        top = fmaxf(top, s[r]);
+      }
+      top = max2_xor32(FP8 ? top : top * g.scale_log2);
+      if (top > m + kLazy) {
+        const float al = fast_exp2(m - top);
+        m = top;
+        l *= al;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = 8 * (r >> 2) + (r & 3);
-          if constexpr (FP8) s[nq][r] *= lds.scales[0][0][32 * kb + 4 * h + key];
-          s[nq][r] = (seen >> key) & 1 ? s[nq][r] : -INFINITY;
-          top = fmaxf(top, s[nq][r]);
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[d][r] *= al;
+      }
+      uint32_t live = 0;  // scores that are not -inf
+      const bool far = !(fabsf(m) < kFarScore) && m != kNoRef;
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) {
+        float e[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const float z = s[r + k];
+          const bool in = z != -INFINITY;
+          if (in) live |= 1u << (r + k);
+          e[k] = fast_exp2(FP8 ? z - m : far ? scaled_below(z, g.scale_log2, m) : fmaf(z, g.scale_log2, -m));
+          l += e[k];
+          if constexpr (FP8) e[k] = in ? e[k] * lds.scales[0][1][32 * kb + 8 * (r >> 2) + 4 * h + ((r + k) & 3)] : 0.f;
         }
-        top = max2_xor32(FP8 ? top : top * g.scale_log2);
-        if (top > m[nq] + kLazy) {
-          const float al = fast_exp2(m[nq] - top);
-          m[nq] = top;
-          l[nq] *= al;
-#pragma unroll
-          for (int d = 0; d < DB; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[d][nq][r] *= al;
-        }
-        live[nq] = 0;
-        const bool far = !(fabsf(m[nq]) < kFarScore) && m[nq] != kNoRef;
-#pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-          float e[2];
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const float z = s[nq][r + k];
-            const bool in = z != -INFINITY;
-            if (in) live[nq] |= 1u << (r + k);
-            e[k] = fast_exp2(FP8 ? z - m[nq] : far ? scaled_below(z, g.scale_log2, m[nq]) : fmaf(z, g.scale_log2, -m[nq]));
-            l[nq] += e[k];
-            if constexpr (FP8) e[k] = in ? e[k] * lds.scales[0][1][32 * kb + 8 * (r >> 2) + 4 * h + ((r + k) & 3)] : 0.f;
-          }
-          p[r >> 3][nq][(r & 7) >> 1] = pack_bf16x2(e[0], e[1]);
-        }
+        p[r >> 3][(r & 7) >> 1] = pack_bf16x2(e[0], e[1]);
       }
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
@@ -548,31 +529,23 @@ __device__ __forceinline__ void careful_rows(const PromptGeom& g, const Share& w
               up[k] |= nan || (odd && !(v & 0x8000u)) ? one : 0u;
               down[k] |= nan || (odd && (v & 0x8000u)) ? one : 0u;
             }
+          u32x4 one;
 #pragma unroll
-          for (int nq = 0; nq < NQ; ++nq) {
-            u32x4 one;
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t bits = live >> (8 * ks + 2 * k);
+            one[k] = (bits & 1 ? 0x3F80u : 0u) | (bits & 2 ? 0x3F800000u : 0u);
+          }
+          o[d] = mfma32(fin, p[ks], o[d]);
+          const f32x16 plus = mfma32(up, one, f32x16{}), minus = mfma32(down, one, f32x16{});
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t bits = live[nq] >> (8 * ks + 2 * k);
-              one[k] = (bits & 1 ? 0x3F80u : 0u) | (bits & 2 ? 0x3F800000u : 0u);
-            }
-            o[d][nq] = mfma32(fin, p[ks][nq], o[d][nq]);
-            const f32x16 plus = mfma32(up, one, f32x16{}), minus = mfma32(down, one, f32x16{});
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              o[d][nq][r] += plus[r] > 0.f ? INFINITY : 0.f;
-              o[d][nq][r] -= minus[r] > 0.f ? INFINITY : 0.f;
-            }
+          for (int r = 0; r < 16; ++r) {
+            o[d][r] += plus[r] > 0.f ? INFINITY : 0.f;
+            o[d][r] -= minus[r] > 0.f ? INFINITY : 0.f;
           }
         }
     }
   }
-  if (active) store_rows<NQ, DV>(g, w, wrow, lane, o, m, l);
-}
-template <int DQK, int DV, int KIND, int NQ>
-__device__ __forceinline__ void careful_item(const PromptGeom& g, const Share& w, typename Prompt<DQK, DV, KIND, NQ>::Lds& lds) {
-#pragma nounroll
-  for (int part = 0; part < NQ; ++part) careful_rows<DQK, DV, KIND, NQ>(g, w, part, lds);
+  if (active) store_row<DV>(g, w, wrow, lane, o, m, l);
 }
 
 // ---------------------------------------------------------------- direct loads of tiles
@@ -607,33 +580,28 @@ __device__ __forceinline__ void tile_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-template <int DQK, int DV, int KIND, int NQ>
-__global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves_per_eu(2 / NQ, 2 / NQ))) void prompt_attn_kernel(PromptGeom g) {
-  using T = Prompt<DQK, DV, KIND, NQ>;
-  constexpr int KS = T::KS, DB = T::DB, kThreads = T::kThreads, NK = T::kBufsK, NV = T::kBufsV;
+template <int DQK, int DV, int KIND>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_attn_kernel(PromptGeom g) {
+  using T = Prompt<DQK, DV, KIND>;
+  constexpr int KS = T::KS, DB = T::DB, NB = T::kBufs, NR = T::kRaw;
   constexpr bool FP8 = T::FP8;
   __shared__ __attribute__((aligned(1024))) typename T::Lds lds;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
   Share w;
   if (!(g.pieces ? find_piece(g, (int)blockIdx.x, w) : find_whole(g, g.first + (int)blockIdx.x, w))) return;
-  const int wrow = w.row0 + 32 * NQ * wave;
+  const int wrow = w.row0 + 32 * wave;
   const bool active = wrow < w.rows;
   T f(lane);
-  Queries<NQ, KS> x;  // (loaded with the first tile)
+  Query<KS> x;  // (loaded with the first tile)
   bool fresh = true;
   // positions of the wave's first and last token
-  const int wlast = (w.rows - wrow < 32 * NQ ? w.rows : wrow + 32 * NQ) - 1;
+  const int wlast = (w.rows - wrow < 32 ? w.rows : wrow + 32) - 1;
   const int t_first = !active ? -1 : g.causal ? w.c - w.n + fdiv(g.by_group, wrow) : w.c - 1;
   const int t_last = !active ? -1 : g.causal ? w.c - w.n + fdiv(g.by_group, wlast) : w.c - 1;
-  f32x16 o[DB][NQ];
-  float m[NQ], l[NQ];
+  f32x16 o[DB];
+  float m = kNoRef, l = 0.f;
 #pragma unroll
-  for (int nq = 0; nq < NQ; ++nq) {
-    m[nq] = kNoRef;
-    l[nq] = 0.f;
-#pragma unroll
-    for (int d = 0; d < DB; ++d) o[d][nq] = f32x16{};
-  }
+  for (int d = 0; d < DB; ++d) o[d] = f32x16{};
 
   const bool whole_tiles = KIND == 0 || g.P % kKeys == 0;  // (no tile lies in two pages)
   const int64_t row_k = KIND ? DQK * (FP8 ? 1 : 2) : g.k_stride * 2, row_v = KIND ? DV * (FP8 ? 1 : 2) : g.v_stride * 2;  // bytes
@@ -641,8 +609,8 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
   const uint8_t* const base_v = static_cast<const uint8_t*>(g.v) + (KIND ? 0 : w.head * DV * 2 + w.kv0 * row_v);
   // Direct loads: half the waves load the keys of a tile, half the values; load j of a wave fills slots 64 (loads part + j) + lane.
   constexpr int LK = T::kLoadsK, LV = T::kLoadsV, LM = LK > LV ? LK : LV;
-  const bool loads_k = wave < T::kWaves / 2;
-  const int part = wave % (T::kWaves / 2);
+  const bool loads_k = wave < kWaves / 2;
+  const int part = wave % (kWaves / 2);
   const uint8_t* const base = loads_k ? base_k : base_v;
   const int64_t row_bytes = loads_k ? row_k : row_v;
   auto slot_of = [&](int j, int ln, int& r) {  // byte of its row that the slot of load j and lane ln holds
@@ -660,8 +628,8 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
     }
   }
   const uint32_t lds_k = (uint32_t)(uintptr_t)&lds.k[0][0], lds_v = (uint32_t)(uintptr_t)&lds.v[0][0];
-  auto next_k = [&](uint32_t at) { return at + T::kK == lds_k + NK * T::kK ? lds_k : at + T::kK; };
-  auto next_v = [&](uint32_t at) { return at + T::kV == lds_v + NV * T::kV ? lds_v : at + T::kV; };
+  auto next_k = [&](uint32_t at) { return at + T::kK == lds_k + NB * T::kK ? lds_k : at + T::kK; };
+  auto next_v = [&](uint32_t at) { return at + T::kV == lds_v + NB * T::kV ? lds_v : at + T::kV; };
 
   // Tiles [a, b) of the sequence, the pages of which (from page f1 on) are in LDS.
   auto run = [&](int a, int b, int f1) {
@@ -713,57 +681,57 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
         lds_dma16(row >= 0 ? base + (int64_t)(uint32_t)row * row_bytes + c : zero_row, to + j * 1024);
       }
     };
-    // -- fp8: tile a + i into registers, and from there as bf16 into its buffers
-    constexpr int RK = FP8 ? (kKeys * DQK / 16 + kThreads - 1) / kThreads : 1;
-    const bool loads = !FP8 || kKeys * DQK / 16 >= kThreads || (int)threadIdx.x < kKeys * DQK / 16;  // (a tile of fewer units than threads)
-    struct Regs {
-      u32x4 k[RK], v[RK];
-      float scale;
+    // -- fp8: tile a + i by direct loads as it is, and from there in bf16 into its buffers; a thread converts what it has loaded itself
+    constexpr int kUnits = kKeys * DQK / 16, RL = FP8 ? 2 * kUnits / kThreads : 1;  // 16-byte units of a tile's keys or values; loads of a wave
+    static_assert(!FP8 || RL * kThreads == 2 * kUnits, "whole loads");
+    auto unit_of = [&](int j, bool& keys) {
+      const int e = kThreads * j + (int)threadIdx.x;
+      keys = RL == 2 ? j == 0 : wave < kWaves / 2;
+      return e % kUnits;
     };
     auto fetch = [&](int i) {
       const Where p = locate(a + i);
       note(i, whole_tiles ? p.all : __ballot(p.row < 0) == 0);
-      Regs y{};
-      if (whole_tiles && p.all) {
-        const int64_t at = (int64_t)(uint32_t)uniform(p.row0) * DQK + 16 * threadIdx.x;
+      const int slot = i % NR;
+      const uint32_t to = (uint32_t)uniform((int)((uint32_t)(uintptr_t)&lds.raw[slot][0] + 1024 * wave));
 #pragma unroll
-        for (int j = 0; j < RK; ++j) {
-          if (!loads) break;
-          y.k[j] = *reinterpret_cast<const u32x4*>(base_k + at + 16 * kThreads * j);
-          y.v[j] = *reinterpret_cast<const u32x4*>(base_v + at + 16 * kThreads * j);
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < RK; ++j) {
-          const int e = here((int)threadIdx.x) + kThreads * j, row = __shfl(p.row, (e / (DQK / 16)) & 63);
-          if (loads && row >= 0) {
-            y.k[j] = *reinterpret_cast<const u32x4*>(base_k + (int64_t)row * DQK + 16 * (e % (DQK / 16)));
-            y.v[j] = *reinterpret_cast<const u32x4*>(base_v + (int64_t)row * DQK + 16 * (e % (DQK / 16)));
-          }
+      for (int j = 0; j < RL; ++j) {
+        bool keys;
+        const int u = unit_of(j, keys);
+        const uint8_t* const from = keys ? base_k : base_v;
+        if (whole_tiles && p.all) {
+          const uint32_t off = 16 * u;
+          lds_dma16_tile<1>(uniform_ptr(from + (int64_t)(uint32_t)uniform(p.row0) * DQK), &off, to + 1024 * kWaves * j);
+        } else {
+          const int row = __shfl(p.row, u / (DQK / 16));
+          lds_dma16(row >= 0 ? from + (int64_t)row * DQK + 16 * (u % (DQK / 16)) : zero_row, to + 1024 * kWaves * j);
         }
       }
-      if (wave < 2 && p.row >= 0) y.scale = (wave == 0 ? g.k_scale : g.v_scale)[p.row];
-      return y;
+      if (wave < 2)
+        lds_dma4(p.row >= 0 ? reinterpret_cast<const uint8_t*>((wave == 0 ? g.k_scale : g.v_scale) + p.row) : zero_row,
+                 (uint32_t)uniform((int)(uint32_t)(uintptr_t)&lds.raw_scales[slot][wave & 1][0]));
     };
-    auto commit = [&](int i, const Regs& y) {
+    auto commit = [&](int i) {
+      const int slot = i % NR;
 #pragma unroll
-      for (int j = 0; j < RK; ++j) {
-        if (!loads) break;
-        const int e = (int)threadIdx.x + kThreads * j, r = e / (DQK / 16), c = 2 * (e % (DQK / 16));
-        uint8_t *dk = lds.k[i % NK] + r * DQK * 2, *dv = lds.v[i % NV] + r * DV * 2;
-        *reinterpret_cast<u32x4*>(dk + ((c ^ swz<T::CK>(r)) << 4)) = fp8x8_bf16(y.k[j].x, y.k[j].y);
-        *reinterpret_cast<u32x4*>(dk + (((c + 1) ^ swz<T::CK>(r)) << 4)) = fp8x8_bf16(y.k[j].z, y.k[j].w);
-        *reinterpret_cast<u32x4*>(dv + ((c ^ swz<T::CV>(r)) << 4)) = fp8x8_bf16(y.v[j].x, y.v[j].y);
-        *reinterpret_cast<u32x4*>(dv + (((c + 1) ^ swz<T::CV>(r)) << 4)) = fp8x8_bf16(y.v[j].z, y.v[j].w);
+      for (int j = 0; j < RL; ++j) {
+        bool keys;
+        const int u = unit_of(j, keys), r = u / (DQK / 16), c = 2 * (u % (DQK / 16));
+        const u32x4 y = *reinterpret_cast<const u32x4*>(&lds.raw[slot][16 * (kThreads * j + (int)threadIdx.x)]);
+        uint8_t* const to = (keys ? lds.k[i % NB] : lds.v[i % NB]) + r * DQK * 2;
+        *reinterpret_cast<u32x4*>(to + ((c ^ swz<T::CK>(r)) << 4)) = fp8x8_bf16(y.x, y.y);
+        *reinterpret_cast<u32x4*>(to + (((c + 1) ^ swz<T::CK>(r)) << 4)) = fp8x8_bf16(y.z, y.w);
       }
-      if (wave < 2) lds.scales[i % NV][wave][lane] = wave == 0 ? y.scale * g.scale_log2 : y.scale;
+      if (wave < 2) {
+        const float y = lds.raw_scales[slot][wave][lane];
+        lds.scales[i % NB][wave][lane] = wave == 0 ? y * g.scale_log2 : y;
+      }
     };
 
     const int nt = b - a;
     // the tiles that some row of this wave attends to are the first nw
     const int seen_end = t_last < 0 ? 0 : t_last / kKeys + 1;
     const int nw = seen_end <= a ? 0 : seen_end < b ? seen_end - a : nt;
-    Regs ahead{};
 
     // -- the pieces of a step, which takes half a tile: keys 32 kb .. + 31
     // The operands of a product are read from LDS while the one before runs: those of KA k-steps of the scores (all, where the
@@ -780,113 +748,100 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
 #pragma unroll
         for (int d = 0; d < DB; ++d) vf[ks][d] = f.v_operand(lv, ks, d);
     };
-    auto scores = [&](uint32_t lk, f32x16 (&s)[NQ]) {
-#pragma unroll
-      for (int nq = 0; nq < NQ; ++nq) s[nq] = f32x16{};
+    auto scores = [&](uint32_t lk, f32x16& s) {
+      s = f32x16{};
 #pragma unroll
       for (int st = 0; st < KS; ++st) {
         const u32x4 y = st < KA ? kf[st < KA ? st : 0] : f.k_operand(lk, st);
-#pragma unroll
-        for (int nq = 0; nq < NQ; ++nq) s[nq] = mfma32(y, x.q[nq][st], s[nq]);
+        s = mfma32(y, x.q[st], s);
       }
     };
-    u32x4 p[2][NQ];  // weights: B operands of k-steps of 16
+    u32x4 p[2];  // weights: B operands of k-steps of 16
     auto values = [&] {
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
         for (int d = 0; d < DB; ++d)
-#pragma unroll
-          for (int nq = 0; nq < NQ; ++nq) o[d][nq] = mfma32(vf[ks][d], p[ks][nq], o[d][nq]);
+          o[d] = mfma32(vf[ks][d], p[ks], o[d]);
     };
     // the scores' maximum per row, in base-2 units (those of an fp8 cache with the keys' scales first)
-    auto scale_max = [&](int i, int kb, f32x16 (&s)[NQ], float (&top)[NQ]) {
+    auto scale_max = [&](int i, int kb, f32x16& s, float& top) {
       f32x4 sc[4];
       if constexpr (FP8) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) sc[k] = *reinterpret_cast<const f32x4*>(&lds.scales[i % NV][0][32 * kb + 8 * k + 4 * h]);
+        for (int k = 0; k < 4; ++k) sc[k] = *reinterpret_cast<const f32x4*>(&lds.scales[i % NB][0][32 * kb + 8 * k + 4 * h]);
       }
+      top = -INFINITY;
 #pragma unroll
-      for (int nq = 0; nq < NQ; ++nq) {
-        top[nq] = -INFINITY;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          if constexpr (FP8) s[nq][r] *= sc[r >> 2][r & 3];
-          top[nq] = fmaxf(top[nq], s[nq][r]);
-        }
+      for (int r = 0; r < 16; ++r) {
+        if constexpr (FP8) s[r] *= sc[r >> 2][r & 3];
+        top = fmaxf(top, s[r]);
       }
     };
     // the same of those that the rows attend to (a path of its own beside the products, so that these exist once)
-    auto mask = [&](int i, int kb, f32x16 (&s)[NQ], float (&top)[NQ]) {
+    auto mask = [&](int i, int kb, f32x16& s, float& top) {
       const uint32_t keys = (uint32_t)(__ballot(locate(a + i).row >= 0) >> (32 * kb));
+      top = -INFINITY;
+      const uint32_t seen = sees32(g, x.t, (a + i) * kKeys + 32 * kb, keys) >> (4 * h);
 #pragma unroll
-      for (int nq = 0; nq < NQ; ++nq) {
-        top[nq] = -INFINITY;
-        const uint32_t seen = sees32(g, x.t[nq], (a + i) * kKeys + 32 * kb, keys) >> (4 * h);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[nq][r] = (seen >> (8 * (r >> 2) + (r & 3))) & 1 ? s[nq][r] : -INFINITY;
-          top[nq] = fmaxf(top[nq], s[nq][r]);
-        }
+      for (int r = 0; r < 16; ++r) {
+        s[r] = (seen >> (8 * (r >> 2) + (r & 3))) & 1 ? s[r] : -INFINITY;
+        top = fmaxf(top, s[r]);
       }
     };
-    auto rescale = [&](float (&top)[NQ]) {
-      bool grown = false;
-#pragma unroll
-      for (int nq = 0; nq < NQ; ++nq) {
-        top[nq] = max2_xor32(FP8 ? top[nq] : top[nq] * g.scale_log2);
-        grown |= top[nq] > m[nq] + kLazy;
-      }
+    auto rescale = [&](float& top) {
+      top = max2_xor32(FP8 ? top : top * g.scale_log2);
+      const bool grown = top > m + kLazy;
       if (__any(grown)) {
+        // (each row by its own scores, whatever the wave's others do)
+        const float mn = grown ? top : m, al = fast_exp2(m - mn);
+        m = mn;
+        l *= al;
 #pragma unroll
-        for (int nq = 0; nq < NQ; ++nq) {  // (each row by its own scores, whatever the wave's others do)
-          const float mn = top[nq] > m[nq] + kLazy ? top[nq] : m[nq], al = fast_exp2(m[nq] - mn);
-          m[nq] = mn;
-          l[nq] *= al;
+        for (int d = 0; d < DB; ++d)
 #pragma unroll
-          for (int d = 0; d < DB; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[d][nq][r] *= al;
-        }
+          for (int r = 0; r < 16; ++r) o[d][r] *= al;
       }
     };
-    auto weights = [&](int i, int kb, const f32x16 (&s)[NQ]) {
+    auto weights = [&](int i, int kb, const f32x16& s) {
       f32x4 sc[4];
       if constexpr (FP8) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) sc[k] = *reinterpret_cast<const f32x4*>(&lds.scales[i % NV][1][32 * kb + 8 * k + 4 * h]);
+        for (int k = 0; k < 4; ++k) sc[k] = *reinterpret_cast<const f32x4*>(&lds.scales[i % NB][1][32 * kb + 8 * k + 4 * h]);
       }
 #pragma unroll
-      for (int nq = 0; nq < NQ; ++nq)
-#pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-          float e0 = fast_exp2(FP8 ? s[nq][r] - m[nq] : fmaf(s[nq][r], g.scale_log2, -m[nq]));
-          float e1 = fast_exp2(FP8 ? s[nq][r + 1] - m[nq] : fmaf(s[nq][r + 1], g.scale_log2, -m[nq]));
-          l[nq] += e0;
-          l[nq] += e1;
-          if constexpr (FP8) {
-            e0 *= sc[r >> 2][r & 3];
-            e1 *= sc[r >> 2][(r & 3) + 1];
-          }
-          p[r >> 3][nq][(r & 7) >> 1] = pack_bf16x2(e0, e1);
+      for (int r = 0; r < 16; r += 2) {
+        float e0 = fast_exp2(FP8 ? s[r] - m : fmaf(s[r], g.scale_log2, -m));
+        float e1 = fast_exp2(FP8 ? s[r + 1] - m : fmaf(s[r + 1], g.scale_log2, -m));
+        l += e0;
+        l += e1;
+        if constexpr (FP8) {
+          e0 *= sc[r >> 2][r & 3];
+          e1 *= sc[r >> 2][(r & 3) + 1];
         }
+        p[r >> 3][(r & 7) >> 1] = pack_bf16x2(e0, e1);
+      }
     };
     auto is_clear = [&](int i) {  // every row of the wave attends to every key of tile a + i
       const int s0 = (a + i) * kKeys;
       return ((there >> (i & 31)) & 1) && s0 <= t_first - (kKeys - 1) && (g.k_swa == 0 || s0 > t_last - g.k_swa || s0 <= g.k_sink - kKeys);
     };
-    // start of step i: tile i + 1 has arrived, everyone is done with values i - 2 and keys i - 1; tile i + kLead sets out
+    // start of step i: tile i + 1 has arrived, everyone is done with tile i - 1 (and the first half of keys i); tile i + kLead sets out
     constexpr int LEAD = T::kLead;
     auto wait = [&](auto tiles) {  // until at most so many tiles are on their way
       constexpr int N = decltype(tiles)::value;
-      if (LK == LV || loads_k) tile_barrier<N * LK>();
+      if constexpr (FP8) {  // (and tile i + 2 as it is)
+        if (wave < 2) tile_barrier<N * (RL + 1)>();
+        else tile_barrier<N * RL>();
+      } else if (LK == LV || loads_k) tile_barrier<N * LK>();
       else tile_barrier<N * LV>();
     };
     auto advance = [&](int i) {
       if constexpr (FP8) {
-        __syncthreads();
-        if (i + 2 < nt) commit(i + 2, ahead);
-        if (i + 3 < nt) ahead = fetch(i + 3);
+        if (i + 1 + NR < nt) wait(std::integral_constant<int, NR - 1>{});
+        else wait(std::integral_constant<int, 0>{});
+        if (i + 2 < nt) commit(i + 2);
+        if (i + 2 + NR < nt) fetch(i + 2 + NR);
       } else {
         if (i + LEAD - 1 < nt) wait(std::integral_constant<int, LEAD - 2>{});
         else wait(std::integral_constant<int, 0>{});
@@ -896,21 +851,25 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
 
     // -- first tiles
     if constexpr (FP8) {
-      const Regs y0 = fetch(0), y1 = nt > 1 ? fetch(1) : Regs{};
-      if (fresh) x = load_queries<NQ, DQK>(g, w, wrow, lane);
-      if (nt > 2) ahead = fetch(2);
-      commit(0, y0);
-      if (nt > 1) commit(1, y1);
-      __syncthreads();
+      fetch(0);
+      if (fresh) x = load_query<DQK>(g, w, wrow, lane);
+      for (int i = 1; i < NR && i < nt; ++i) fetch(i);
+      if (nt >= NR) wait(std::integral_constant<int, NR - 2>{});
+      else wait(std::integral_constant<int, 0>{});
+      for (int i = 0; i < 2 && i < nt; ++i) {
+        commit(i);
+        if (i + NR < nt) fetch(i + NR);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     } else {
       issue(0);
-      if (fresh) x = load_queries<NQ, DQK>(g, w, wrow, lane);
+      if (fresh) x = load_query<DQK>(g, w, wrow, lane);
       for (int i = 1; i < LEAD && i < nt; ++i) issue(i);
       if (nt >= LEAD) wait(std::integral_constant<int, LEAD - 1>{});
       else wait(std::integral_constant<int, 0>{});
     }
     fresh = false;
-    f32x16 sa[NQ], sb[NQ];
+    f32x16 sa, sb;
     if (nw > 0) {
       load_k(lds_k);
       scores(lds_k, sa);
@@ -920,8 +879,7 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
     // in the buffers, which nobody reads)
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-      for (int nq = 0; nq < NQ; ++nq) p[ks][nq] = u32x4{};
+      p[ks] = u32x4{};
     constexpr uint32_t HK = 32 * DQK * 2, HV = 32 * DV * 2;  // bytes of half a tile
     uint32_t kc = lds_k, vc = lds_v;                         // buffers of tile i
     for (int i = 0; i < nt; ++i) {
@@ -932,7 +890,7 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
       if (i >= nw) continue;
       f.refresh();
       const bool clear = is_clear(i);
-      float top[NQ];
+      float top;
       load_k(k + HK);
       values();
       scale_max(i, 0, sa, top);
@@ -976,35 +934,28 @@ __global__ __launch_bounds__(64 * kRows / (32 * NQ)) __attribute__((amdgpu_waves
   }
   // (a value that is no finite number leaves every accumulator it was multiplied into so)
   float odd[4] = {};
+  odd[0] = fmaf(l, 0.f, odd[0]);
+  if (!FP8 && !(fabsf(m) < kFarScore) && m != kNoRef) odd[0] = 1.f;
 #pragma unroll
-  for (int nq = 0; nq < NQ; ++nq) {
-    odd[0] = fmaf(l[nq], 0.f, odd[0]);
-    if (!FP8 && !(fabsf(m[nq]) < kFarScore) && m[nq] != kNoRef) odd[0] = 1.f;
+  for (int d = 0; d < DB; ++d)
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) odd[r & 3] = fmaf(o[d][nq][r], 0.f, odd[r & 3]);
-  }
+    for (int r = 0; r < 16; ++r) odd[r & 3] = fmaf(o[d][r], 0.f, odd[r & 3]);
   if (__syncthreads_or((odd[0] + odd[1]) + (odd[2] + odd[3]) != 0.f)) {  // (NaN != 0)
-    careful_item<DQK, DV, KIND, NQ>(g, w, lds);
+    careful_item<DQK, DV, KIND>(g, w, lds);
     return;
   }
-  if (active) store_rows<NQ, DV>(g, w, wrow, lane, o, m, l);
+  if (active) store_row<DV>(g, w, wrow, lane, o, m, l);
 }
 
 hipError_t launch_prompt_attn(const PromptGeom& all, hipStream_t st) {
   PromptGeom g = all;
-#ifndef NQX
-#define NQX 1
-#endif
-  constexpr int NQ = NQX;
-  auto* kernel = g.ctx_len == nullptr ? (g.d_qk == 64    ? prompt_attn_kernel<64, 64, 0, NQ>
-                                         : g.d_qk == 128 ? prompt_attn_kernel<128, 128, 0, NQ>
-                                                         : prompt_attn_kernel<192, 128, 0, NQ>)
-                 : g.fp8 ? (g.d_qk == 64 ? prompt_attn_kernel<64, 64, 2, NQ> : prompt_attn_kernel<128, 128, 2, NQ>)
-                         : (g.d_qk == 64 ? prompt_attn_kernel<64, 64, 1, NQ> : prompt_attn_kernel<128, 128, 1, NQ>);
+  auto* kernel = g.ctx_len == nullptr ? (g.d_qk == 64    ? prompt_attn_kernel<64, 64, 0>
+                                         : g.d_qk == 128 ? prompt_attn_kernel<128, 128, 0>
+                                                         : prompt_attn_kernel<192, 128, 0>)
+                 : g.fp8 ? (g.d_qk == 64 ? prompt_attn_kernel<64, 64, 2> : prompt_attn_kernel<128, 128, 2>)
+                         : (g.d_qk == 64 ? prompt_attn_kernel<64, 64, 1> : prompt_attn_kernel<128, 128, 1>);
   if (g.pieces) {
-    hipError_t e = launch_kernel(kernel, dim3((unsigned)(g.pieces + g.blocks + 1)), dim3(64 * kRows / (32 * NQ)), st, g);
+    hipError_t e = launch_kernel(kernel, dim3((unsigned)(g.pieces + g.blocks + 1)), dim3(kThreads), st, g);
     if (e != hipSuccess) return e;
     // (workgroups of a block: one for as many rows as it takes at a time, but few where there are many blocks, most of them whole)
     const int rows = 256 / (g.d_v / 4 * kJoinGroups), groups = (g.slot_rows + rows - 1) / rows, most = 8192 / g.blocks > 8 ? 8192 / g.blocks : 8;
@@ -1014,7 +965,7 @@ hipError_t launch_prompt_attn(const PromptGeom& all, hipStream_t st) {
   constexpr int64_t kMost = 1 << 22;  // workgroups of a launch (2^32 threads and more are taken modulo 2^32)
   for (int64_t i = 0; i < all.items; i += kMost) {
     g.first = (int)i;
-    const hipError_t e = launch_kernel(kernel, dim3((unsigned)(all.items - i < kMost ? all.items - i : kMost)), dim3(64 * kRows / (32 * NQ)), st, g);
+    const hipError_t e = launch_kernel(kernel, dim3((unsigned)(all.items - i < kMost ? all.items - i : kMost)), dim3(kThreads), st, g);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
