@@ -294,11 +294,14 @@ __device__ __forceinline__ Query<DQK / 16> load_query(const PromptGeom& g, const
   const uint16_t* p = g.q + (w.q0 + j) * g.q_stride + (int64_t)(w.head * group + r - j * group) * DQK + 8 * (lane >> 5);
 #pragma unroll
   for (int s = 0; s < DQK / 16; ++s) x.q[s] = *reinterpret_cast<const u32x4*>(p + 16 * s);
-  // They have arrived here: the compiler would wait for them where it first uses them, in a loop at every turn, and for the direct
-  // loads, of which it does not know, with them.
-#pragma unroll
-  for (int s = 0; s < DQK / 16; ++s) asm volatile("" : "+v"(x.q[s]));
   return x;
+}
+// They have arrived here: the compiler would wait for them where it first uses them, in a loop at every turn, and for the direct
+// loads, of which it does not know, with them.
+template <int KS>
+__device__ __forceinline__ void arrived(Query<KS>& x) {
+#pragma unroll
+  for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(x.q[s]));
 }
 
 // Which of the 32 keys from s0 on the query at t attends to, of those in `there`.
@@ -346,15 +349,15 @@ __device__ __forceinline__ void store_row(const PromptGeom& g, const Share& w, i
 
 // The pieces of a block joined: workgroup (y, i) takes rows of block i, DV / 4 threads a row and four times as many, each of
 // which joins every fourth piece (a chain of loads of one piece after the other is what few rows of many pieces wait for).
-constexpr int kJoinGroups = 4;
+constexpr int kJoinGroups = 4, kJoinAhead = 4;  // (pieces that a thread loads at a time)
 template <int DV>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g) {
   constexpr int T = DV / 4, R = 256 / (T * kJoinGroups);
   __shared__ float part[kJoinGroups][R][2];
   __shared__ f32x4 part_o[kJoinGroups][R][T];
-  const int item = blockIdx.y;
-  if (item >= *g.n_joins) return;
-  const int4 a = g.joins[2 * item], b = g.joins[2 * item + 1];
+  const int item = blockIdx.y, n = *g.n_joins;
+  const int4 a = g.joins[2 * item], b = g.joins[2 * item + 1];  // (of an item that is none: whatever was there)
+  if (item >= n) return;
   const int x = (int)threadIdx.x % T, grp = (int)threadIdx.x / T % kJoinGroups, lr = (int)threadIdx.x / (T * kJoinGroups);
   const int np = a.x, row0 = a.w, rows = b.x - row0 < kRows ? b.x - row0 : kRows, d = 4 * x;
   if (np <= 1) return;
@@ -365,19 +368,36 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g) {
     const bool in = r < rows;
     const int64_t at = (int64_t)a.y * g.slot_rows + (in ? r : r0);
     const f32x2* ml = reinterpret_cast<const f32x2*>(g.part_ml) + at;
-    float top = kNoRef;
-#pragma unroll 4
-    for (int k = grp; k < np; k += kJoinGroups) top = fmaxf(top, ml[k * step].x);
-    float sum = 0.f;
+    float top = kNoRef, sum = 0.f;
     f32x4 y{};
-#pragma unroll 4
-    for (int k = grp; k < np; k += kJoinGroups) {
-      const f32x2 z = ml[k * step];
-      const float f = fast_exp2(z.x - top);
-      sum += f * z.y;
-      const f32x4 o = *reinterpret_cast<const f32x4*>(g.part_o + (at + k * step) * DV + d);
+    for (int k0 = grp; k0 < np; k0 += kJoinGroups * kJoinAhead) {
+      f32x2 z[kJoinAhead];
+      f32x4 o[kJoinAhead];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) y[q] += f * o[q];
+      for (int e = 0; e < kJoinAhead; ++e) {
+        const int k = k0 + kJoinGroups * e;
+        z[e] = f32x2{kNoRef, 0.f};
+        o[e] = f32x4{};
+        if (k < np) {
+          z[e] = ml[k * step];
+          o[e] = *reinterpret_cast<const f32x4*>(g.part_o + (at + k * step) * DV + d);
+        }
+      }
+      float tn = top;
+#pragma unroll
+      for (int e = 0; e < kJoinAhead; ++e) tn = fmaxf(tn, z[e].x);
+      const float f0 = fast_exp2(top - tn);
+      top = tn;
+      sum *= f0;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) y[q] *= f0;
+#pragma unroll
+      for (int e = 0; e < kJoinAhead; ++e) {
+        const float f = fast_exp2(z[e].x - top);
+        sum += f * z[e].y;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y[q] += f * o[e][q];
+      }
     }
     __syncthreads();  // everyone is done with the rows before
     if (x == 0) {
@@ -592,7 +612,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int wrow = w.row0 + 32 * wave;
   const bool active = wrow < w.rows;
   T f(lane);
-  Query<KS> x;  // (loaded with the first tile)
+  Query<KS> x;
   bool fresh = true;
   // positions of the wave's first and last token
   const int wlast = (w.rows - wrow < 32 ? w.rows : wrow + 32) - 1;
@@ -631,53 +651,52 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   auto next_k = [&](uint32_t at) { return at + T::kK == lds_k + NB * T::kK ? lds_k : at + T::kK; };
   auto next_v = [&](uint32_t at) { return at + T::kV == lds_v + NB * T::kV ? lds_v : at + T::kV; };
 
-  // Tiles [a, b) of the sequence, the pages of which (from page f1 on) are in LDS.
-  auto run = [&](int a, int b, int f1) {
-    struct Where {
-      bool all;      // every key of the tile is there: rows row0 ..
-      int row0, row; // row of key `lane`, -1: none
+  // Tiles [a, b) of the sequence, the pages of which (from page f1 on) are in LDS; mapped: none of them is missing.
+  auto run = [&](int a, int b, int f1, bool mapped) {
+    auto row_of = [&](int tile) {  // row of key `lane` of a tile, -1: none
+      const uint32_t s = (uint32_t)tile * kKeys + lane;
+      if (s >= (uint32_t)w.c) return -1;
+      if constexpr (KIND == 0) return (int)s;
+      const int pg = fdiv(g.by_page, (int)s), ph = lds.pages[pg - f1];
+      return ph >= 0 ? (ph * g.Hkv + w.head) * g.P + ((int)s - pg * g.P) : -1;
     };
-    auto locate = [&](int tile) {
-      Where p{false, 0, -1};
-      const uint32_t s0 = (uint32_t)tile * kKeys, s = s0 + lane;
-      const bool in = s < (uint32_t)w.c;
-      if constexpr (KIND == 0) {
-        p.row0 = (int)s0;
-        p.all = s0 + kKeys <= (uint32_t)w.c;
-        p.row = in ? (int)s : -1;
-      } else if (whole_tiles) {
-        const int pg = fdiv(g.by_page, (int)s0), ph = uniform(lds.pages[pg - f1]);
-        p.row0 = (ph * g.Hkv + w.head) * g.P + ((int)s0 - pg * g.P);
-        p.all = ph >= 0 && s0 + kKeys <= (uint32_t)w.c;
-        p.row = in && ph >= 0 ? p.row0 + lane : -1;
-      } else if (in) {
-        const int pg = fdiv(g.by_page, (int)s), ph = lds.pages[pg - f1];
-        p.row = ph >= 0 ? (ph * g.Hkv + w.head) * g.P + ((int)s - pg * g.P) : -1;
+    // The tile to be loaded next, where tiles do not lie in two pages and every page is mapped: it starts at row `off` of page `ph`
+    // (read a step before it is used).
+    const int start = a * kKeys, pg0 = KIND ? fdiv(g.by_page, start) : 0;
+    int off = KIND ? start - pg0 * g.P : start, entry = pg0 - f1, ph = KIND ? lds.pages[entry] : 0;
+    // the first row of tile a + i, which is next; -1: its rows are to be looked up one by one
+    auto next_rows = [&](int i) {
+      int row = -1;
+      if (whole_tiles) {
+        if (mapped && (uint32_t)(a + i + 1) * kKeys <= (uint32_t)w.c) row = KIND ? (uniform(ph) * g.Hkv + w.head) * g.P + off : off;
+        off += kKeys;
+        if (KIND != 0 && off == g.P) {
+          off = 0;
+          ++entry;
+        }
+        if constexpr (KIND != 0) ph = lds.pages[entry];  // (behind the last tile: an entry that is not used)
       }
-      return p;
+      return row;
     };
-    uint32_t there = 0;  // bit i % 32: every key of tile a + i is there
-    auto note = [&](int i, bool all) { there = (there & ~(1u << (i & 31))) | (uint32_t)all << (i & 31); };
 
     // -- bf16: tile a + i by direct loads into its buffers
     uint32_t ring = loads_k ? lds_k : lds_v;  // of the next tile to be loaded
     auto issue = [&](int i) {
-      const Where p = locate(a + i);
-      note(i, whole_tiles ? p.all : __ballot(p.row < 0) == 0);
+      const int row0 = next_rows(i);
       const uint32_t to = (uint32_t)uniform((int)(ring + part * (loads_k ? LK : LV) * 1024));
       ring = loads_k ? next_k(ring) : next_v(ring);
-      if (whole_tiles && p.all) {
-        const uint8_t* from = uniform_ptr(base + (int64_t)(uint32_t)p.row0 * row_bytes);
+      if (row0 >= 0) {
+        const uint8_t* from = uniform_ptr(base + (int64_t)row0 * row_bytes);
         if (LK == LV || loads_k) lds_dma16_tile<LK>(from, dma, to);
         else lds_dma16_tile<LV>(from, dma, to);
         return;
       }
-      const int ln = here(lane);
+      const int ln = here(lane), own = row_of(a + i);
 #pragma unroll
       for (int j = 0; j < LM; ++j) {
         if (j >= (loads_k ? LK : LV)) break;
         int r;
-        const int c = slot_of(j, ln, r), row = __shfl(p.row, r & 63);
+        const int c = slot_of(j, ln, r), row = __shfl(own, r & 63);
         lds_dma16(row >= 0 ? base + (int64_t)(uint32_t)row * row_bytes + c : zero_row, to + j * 1024);
       }
     };
@@ -690,8 +709,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       return e % kUnits;
     };
     auto fetch = [&](int i) {
-      const Where p = locate(a + i);
-      note(i, whole_tiles ? p.all : __ballot(p.row < 0) == 0);
+      const int row0 = next_rows(i), own = row0 >= 0 ? row0 + lane : row_of(a + i);
       const int slot = i % NR;
       const uint32_t to = (uint32_t)uniform((int)((uint32_t)(uintptr_t)&lds.raw[slot][0] + 1024 * wave));
 #pragma unroll
@@ -699,16 +717,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         bool keys;
         const int u = unit_of(j, keys);
         const uint8_t* const from = keys ? base_k : base_v;
-        if (whole_tiles && p.all) {
-          const uint32_t off = 16 * u;
-          lds_dma16_tile<1>(uniform_ptr(from + (int64_t)(uint32_t)uniform(p.row0) * DQK), &off, to + 1024 * kWaves * j);
+        if (row0 >= 0) {
+          const uint32_t byte = 16 * u;
+          lds_dma16_tile<1>(uniform_ptr(from + (int64_t)row0 * DQK), &byte, to + 1024 * kWaves * j);
         } else {
-          const int row = __shfl(p.row, u / (DQK / 16));
+          const int row = __shfl(own, u / (DQK / 16));
           lds_dma16(row >= 0 ? from + (int64_t)row * DQK + 16 * (u % (DQK / 16)) : zero_row, to + 1024 * kWaves * j);
         }
       }
       if (wave < 2)
-        lds_dma4(p.row >= 0 ? reinterpret_cast<const uint8_t*>((wave == 0 ? g.k_scale : g.v_scale) + p.row) : zero_row,
+        lds_dma4(own >= 0 ? reinterpret_cast<const uint8_t*>((wave == 0 ? g.k_scale : g.v_scale) + own) : zero_row,
                  (uint32_t)uniform((int)(uint32_t)(uintptr_t)&lds.raw_scales[slot][wave & 1][0]));
     };
     auto commit = [&](int i) {
@@ -780,7 +798,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     };
     // the same of those that the rows attend to (a path of its own beside the products, so that these exist once)
     auto mask = [&](int i, int kb, f32x16& s, float& top) {
-      const uint32_t keys = (uint32_t)(__ballot(locate(a + i).row >= 0) >> (32 * kb));
+      const uint32_t keys = (uint32_t)(__ballot(row_of(a + i) >= 0) >> (32 * kb));
       top = -INFINITY;
       const uint32_t seen = sees32(g, x.t, (a + i) * kKeys + 32 * kb, keys) >> (4 * h);
 #pragma unroll
@@ -824,7 +842,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     };
     auto is_clear = [&](int i) {  // every row of the wave attends to every key of tile a + i
       const int s0 = (a + i) * kKeys;
-      return ((there >> (i & 31)) & 1) && s0 <= t_first - (kKeys - 1) && (g.k_swa == 0 || s0 > t_last - g.k_swa || s0 <= g.k_sink - kKeys);
+      return mapped && s0 <= t_first - (kKeys - 1) && (g.k_swa == 0 || s0 > t_last - g.k_swa || s0 <= g.k_sink - kKeys);
     };
     // start of step i: tile i + 1 has arrived, everyone is done with tile i - 1 (and the first half of keys i); tile i + kLead sets out
     constexpr int LEAD = T::kLead;
@@ -849,11 +867,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       }
     };
 
-    // -- first tiles
+    // -- first tiles (the queries of a paged cache's call have set out with the first page table entries)
+    if (KIND != 0 && fresh) arrived(x);
     if constexpr (FP8) {
-      fetch(0);
-      if (fresh) x = load_query<DQK>(g, w, wrow, lane);
-      for (int i = 1; i < NR && i < nt; ++i) fetch(i);
+      for (int i = 0; i < NR && i < nt; ++i) fetch(i);
       if (nt >= NR) wait(std::integral_constant<int, NR - 2>{});
       else wait(std::integral_constant<int, 0>{});
       for (int i = 0; i < 2 && i < nt; ++i) {
@@ -863,7 +880,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     } else {
       issue(0);
-      if (fresh) x = load_query<DQK>(g, w, wrow, lane);
+      if (KIND == 0 && fresh) {
+        x = load_query<DQK>(g, w, wrow, lane);
+        arrived(x);
+      }
       for (int i = 1; i < LEAD && i < nt; ++i) issue(i);
       if (nt >= LEAD) wait(std::integral_constant<int, LEAD - 1>{});
       else wait(std::integral_constant<int, 0>{});
@@ -911,24 +931,29 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     if (nw > 0) values();
   };
 
+  if constexpr (KIND != 0) x = load_query<DQK>(g, w, wrow, lane);
   // The span's two stretches of tiles, and of a paged cache as many at a time as their pages fit in LDS.
   for (int part = 0; part < 2; ++part) {
     const int first = part ? (w.p0 > w.ns ? w.p0 : w.ns) + w.skip : w.p0, last = part ? w.p1 + w.skip : (w.ns < w.p1 ? w.ns : w.p1);
     for (int a = first; a < last;) {
       int b = last, f1 = 0;
+      bool mapped = true;
       __syncthreads();  // everyone is done with the buffers
       if constexpr (KIND != 0) {
         if (b - a > g.pass_tiles) b = a + g.pass_tiles;
         f1 = fdiv(g.by_page, a * kKeys);
         const int64_t end = (int64_t)b * kKeys - 1;
         const int n = fdiv(g.by_page, end < w.c ? (int)end : w.c - 1) - f1 + 1;
+        bool missing = false;
         for (int i = (int)threadIdx.x; i < n; i += kThreads) {
           const int64_t ph = g.page_table ? g.page_table[(int64_t)w.b * g.max_pages + f1 + i] : w.b;
-          lds.pages[i] = ph >= 0 && ph < g.n_phys ? (int)ph : -1;
+          const bool there = ph >= 0 && ph < g.n_phys;
+          missing |= !there;
+          lds.pages[i] = there ? (int)ph : -1;
         }
-        __syncthreads();
+        mapped = !__syncthreads_or(missing);
       }
-      run(a, b, f1);
+      run(a, b, f1, mapped);
       a = b;
     }
   }
