@@ -11,6 +11,12 @@ using lsa::hip_fail;
 
 namespace {
 
+// Calls of at most so many blocks of rows, and of more keys than so many, are cut along their keys into about so many pieces: one per CU.
+// us of 32 heads on 8 of 128, with the limit of blocks at 0 / 256 / 512 / 1024: 16 tokens behind 32K (8 blocks) in fp8 872 / 47 / 47 / 47;
+// 1024 behind 7K (136) 226 / 162 / 159 / 159; 24 sequences, 2048 tokens (456) 238 / 231 / 207 / 203, in fp8 309 / 304 / 237 / 237; 2048 behind 6K (264)
+// 256 / 260 / 264 / 264; 3900 behind 4K (496) 393 / 401 / 407 / 406. With 128 / 256 / 512 pieces: 16 behind 32K in fp8 69 / 47 / 56, 512 behind 8K 144 /
+// 102 / 121, 24 sequences 239 / 207 / 222. With keys from 512 / 1024 / 2048 on: 16 behind 1.5K 19 / 19 / 34, behind 2K 21 / 21 / 43, 128 behind 2K 46 / 46 /
+// 64; prompts of 1024 tokens, which gain nothing, 41.6 / 38.2 / 38.2.
 constexpr int64_t kMostCutBlocks = 512, kLeastCutKeys = 16 * lsa::kPromptKeys;
 constexpr int kPieces = 256;
 

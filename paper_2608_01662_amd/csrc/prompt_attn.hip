@@ -1,10 +1,21 @@
 // Attention of packed prompts over their own keys and values (lsa_prefill_attn) and of ragged chunks of new tokens over a
 // paged cache (lsa_chunk_attn) for gfx950.
 //
-// The query rows of a key/value head are the heads of its group of all new tokens of a sequence, token after token. A
-// workgroup takes 256 of them, four waves of 64, and walks the tiles of 64 keys that any of them attends to, with the running
-// maximum and sum of an online softmax. S^T = K Q^T on 32x32x16 products: a lane holds the scores of one query row,
-// which are, rounded to bf16, the B operand of O^T += V^T P^T as they lie, so that P never leaves the registers.
+// The query rows of a key/value head are the heads of its group of all new tokens of a sequence, token after token: a row of
+// them attends to o = sum_j 2^(z_j - m) v_j / l with z_j = scale log2(e) q.k_j, m the largest z_j, l = sum_j 2^(z_j - m). A workgroup takes
+// 256 rows, eight waves of 32, and walks the tiles of 64 keys that any of them attends to, each tile once through LDS for all, in
+// halves of 32 keys, with a running m (moved when a row's grew by more than 2^8, by the row's own scores) and l in fp32.
+// S^T = K Q^T on 32x32x16 products: a lane holds 16 scores of one row and half, which are, rounded to bf16, the B operand of
+// O^T += V^T P^T as they lie, so that P never leaves the registers; V^T comes from LDS by transposed reads. Queries and accumulators
+// stay in registers (two waves per SIMD, 256 each). The scores of the next half and the values of the last run on the matrix
+// cores while this half's weights are computed.
+//
+// What bounds it: long calls the matrix cores with the softmax between them, and the clock that the chip holds under them. 32 heads
+// on 8, 8192 x 8192 keys without a mask: 1125 us, 977 TFLOP/s, where a large matrix product reaches 1224 (192/128 wide 1006, 64 wide, whose
+// softmax is twice as much per product, 725). A wave's products of a tile take 1024 cycles (64 wide 512) and two waves of a SIMD need about 3900
+// for a tile each. Calls of few rows: the bytes of K and V, and the way to the first tile. Measured and not kept: 64 rows of a wave, one
+// wave per SIMD (1333 us against 1190 at the time); scores weighed before the maximum is known, in one block with the products (1309
+// against 1151); the instructions' order by hand or by groups (1318 against 1151); wave priorities (no change).
 #include "attn_tile.hpp"
 #include "device.hpp"
 #include "launch.hpp"
@@ -107,7 +118,10 @@ __device__ __forceinline__ bool find_whole(const PromptGeom& g, int item, Share&
 // The same of a call that has few blocks of rows: the keys of a sequence's blocks are cut into equal pieces, as many as make the
 // call's pieces cost about 1 / g.pieces of all, but of no fewer tiles than pay for the partial results of a piece, which the join
 // reads again: 4, and the more the more rows a block has. (A tile costs 2 with up to 128 rows, a wave per SIMD, and 3 with more.) The
-// largest pieces come first, of up to 64 sequences. The first piece of a block tells the join about it.
+// largest pieces come first, of up to 64 sequences (24 of 1 to 342 tokens behind 1389 to 8423: 202 us, in the sequences' order and by equal
+// tiles 231). Of a sequence the heads come one after the other, so that an XCD keeps to a class of them, and a block's pieces lie Hkv
+// apart; the last block, which has the most keys, first (3900 tokens behind 4292, 32 heads on 8: 407 us, blocks of a head from the first on 470,
+// not cut at all 393). The first piece of a block tells the join about it.
 __device__ __forceinline__ bool find_piece(const PromptGeom& g, int id, Share& w) {
   const int lane = threadIdx.x & 63, group = (int)g.by_group.d;
   struct Seq {
@@ -347,8 +361,11 @@ __device__ __forceinline__ void store_row(const PromptGeom& g, const Share& w, i
     }
 }
 
-// The pieces of a block joined: workgroup (y, i) takes rows of block i, DV / 4 threads a row and four times as many, each of
-// which joins every fourth piece (a chain of loads of one piece after the other is what few rows of many pieces wait for).
+// The pieces of a block joined: o = sum_k 2^(m_k - m) o_k / sum_k 2^(m_k - m) l_k. Workgroup (i, y) takes rows of block y, DV / 4 threads
+// a row and four times as many, each of which joins every fourth piece, kJoinAhead of them at a time: what few rows of many pieces
+// wait for is the chain of loads (16 tokens behind 32K, 31 pieces: 3.4 us from its start to its end, one group of threads and one piece after the
+// other 5 and more). With 8 pieces at a time 4 tokens behind 100K, 256 pieces, 30.7 against 33.4 us in all, but 512 behind 8K, few pieces
+// of many rows, 106 against 97.
 constexpr int kJoinGroups = 4, kJoinAhead = 4;  // (pieces that a thread loads at a time)
 template <int DV>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g) {
