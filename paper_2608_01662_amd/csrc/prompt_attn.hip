@@ -7,12 +7,12 @@
 // halves of 32 keys, with a running m (moved when a row's grew by more than 2^8, by the row's own scores) and l in fp32.
 // S^T = K Q^T on 32x32x16 products: a lane holds 16 scores of one row and half, which are, rounded to bf16, the B operand of
 // O^T += V^T P^T as they lie, so that P never leaves the registers; V^T comes from LDS by transposed reads. Queries and accumulators
-// stay in registers (two waves per SIMD, 256 each). The scores of the next half and the values of the last run on the matrix
+// stay in registers (two waves per SIMD, 256 each; see waves_per_simd). The scores of the next half and the values of the last run on the matrix
 // cores while this half's weights are computed.
 //
 // What bounds it: long calls the matrix cores with the softmax between them, and the clock that the chip holds under them. 32 heads
-// on 8, 8192 x 8192 keys without a mask: 1125 us, 977 TFLOP/s, where a large matrix product reaches 1224 (192/128 wide 1006, 64 wide, whose
-// softmax is twice as much per product, 725). A wave's products of a tile take 1024 cycles (64 wide 512) and two waves of a SIMD need about 3900
+// on 8, 8192 x 8192 keys without a mask: 1125 us, 977 TFLOP/s, where a large matrix product reaches 1224 to 1407 (192/128 wide 1006, 64 wide, whose
+// softmax is twice as much per product, 811). A wave's products of a tile take 1024 cycles (64 wide 512) and two waves of a SIMD need about 3900
 // for a tile each. Calls of few rows: the bytes of K and V, and the way to the first tile. Measured and not kept: 64 rows of a wave, one
 // wave per SIMD (1333 us against 1190 at the time); scores weighed before the maximum is known, in one block with the products (1309
 // against 1151); the instructions' order by hand or by groups (1318 against 1151); wave priorities (no change).
@@ -617,8 +617,12 @@ __device__ __forceinline__ void tile_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+// Heads of 64 have registers for two workgroups per CU, the careful form's spilled; not those of fp8 caches, whose loop would be. us with two
+// waves per SIMD and with four: 12 heads, 8192 x 8192 keys 771, 678, window of 1024 81, 68; 32 on 8, 24 sequences mixed 132, 125, in fp8 181, 472; 2048
+// behind 6K 169, 176, 16 behind 32K 28.5, 30.0.
+constexpr int waves_per_simd(int d_qk, int kind) { return d_qk == 64 && kind != 2 ? 4 : 2; }
 template <int DQK, int DV, int KIND>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_attn_kernel(PromptGeom g) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_per_simd(DQK, KIND), waves_per_simd(DQK, KIND)))) void prompt_attn_kernel(PromptGeom g) {
   using T = Prompt<DQK, DV, KIND>;
   constexpr int KS = T::KS, DB = T::DB, NB = T::kBufs, NR = T::kRaw;
   constexpr bool FP8 = T::FP8;
