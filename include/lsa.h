@@ -462,7 +462,8 @@ typedef struct lsa_prefill_attn_params {
   float sm_scale;     /* softmax scale applied to q . k                                                     */
 } lsa_prefill_attn_params;
 
-/* Workspace bytes for lsa_prefill_attn; 0 when no call of these sizes cuts a row's keys into parts. */
+/* Workspace bytes for lsa_prefill_attn; 0 when no call of these sizes cuts a row's keys into parts. What a workspace holds before a
+ * call has no effect; it serves one call at a time (calls that may run at once, on two streams or in two graphs, need one each). */
 size_t lsa_prefill_attn_workspace_size(const lsa_prefill_attn_params* p, int32_t n_seq, int64_t n_tok, int64_t n_kv);
 
 /*

@@ -362,21 +362,22 @@ __device__ __forceinline__ void store_row(const PromptGeom& g, const Share& w, i
 }
 
 // The pieces of a block joined: o = sum_k 2^(m_k - m) o_k / sum_k 2^(m_k - m) l_k. Workgroup (i, y) takes rows of block y, DV / 4 threads
-// a row and four times as many, each of which joins every fourth piece, kJoinAhead of them at a time: what few rows of many pieces
-// wait for is the chain of loads (16 tokens behind 32K, 31 pieces: 3.4 us from its start to its end, one group of threads and one piece after the
+// a row of few pieces, and four times as many a row of more, each of which joins every fourth piece, kJoinAhead of them at a time: what few
+// rows of many pieces wait for is the chain of loads (16 tokens behind 32K, 31 pieces: 3.4 us from its start to its end, one group of threads and one piece after the
 // other 5 and more). With 8 pieces at a time 4 tokens behind 100K, 256 pieces, 30.7 against 33.4 us in all, but 512 behind 8K, few pieces
 // of many rows, 106 against 97.
 constexpr int kJoinGroups = 4, kJoinAhead = 4;  // (pieces that a thread loads at a time)
 template <int DV>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g) {
-  constexpr int T = DV / 4, R = 256 / (T * kJoinGroups);
-  __shared__ float part[kJoinGroups][R][2];
-  __shared__ f32x4 part_o[kJoinGroups][R][T];
+  constexpr int T = DV / 4, kR = 256 / (T * kJoinGroups);
+  __shared__ float part[kJoinGroups][kR][2];
+  __shared__ f32x4 part_o[kJoinGroups][kR][T];
   const int item = blockIdx.y, n = *g.n_joins;
   const int4 a = g.joins[2 * item], b = g.joins[2 * item + 1];  // (of an item that is none: whatever was there)
   if (item >= n) return;
-  const int x = (int)threadIdx.x % T, grp = (int)threadIdx.x / T % kJoinGroups, lr = (int)threadIdx.x / (T * kJoinGroups);
-  const int np = a.x, row0 = a.w, rows = b.x - row0 < kRows ? b.x - row0 : kRows, d = 4 * x;
+  const int np = a.x, groups = np <= kJoinAhead ? 1 : kJoinGroups, R = kR * kJoinGroups / groups;  // (rows at a time)
+  const int x = (int)threadIdx.x % T, grp = (int)threadIdx.x / T & (groups - 1), lr = (int)threadIdx.x / (T * groups);
+  const int row0 = a.w, rows = b.x - row0 < kRows ? b.x - row0 : kRows, d = 4 * x;
   if (np <= 1) return;
   const int64_t step = (int64_t)g.slot_rows * g.Hkv;  // from a piece to the next
   const int group = (int)g.by_group.d;
@@ -387,12 +388,12 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g) {
     const f32x2* ml = reinterpret_cast<const f32x2*>(g.part_ml) + at;
     float top = kNoRef, sum = 0.f;
     f32x4 y{};
-    for (int k0 = grp; k0 < np; k0 += kJoinGroups * kJoinAhead) {
+    for (int k0 = grp; k0 < np; k0 += groups * kJoinAhead) {
       f32x2 z[kJoinAhead];
       f32x4 o[kJoinAhead];
 #pragma unroll
       for (int e = 0; e < kJoinAhead; ++e) {
-        const int k = k0 + kJoinGroups * e;
+        const int k = k0 + groups * e;
         z[e] = f32x2{kNoRef, 0.f};
         o[e] = f32x4{};
         if (k < np) {
@@ -416,26 +417,29 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g) {
         for (int q = 0; q < 4; ++q) y[q] += f * o[e][q];
       }
     }
-    __syncthreads();  // everyone is done with the rows before
-    if (x == 0) {
-      part[grp][lr][0] = top;
-      part[grp][lr][1] = sum;
+    if (groups > 1) {
+      __syncthreads();  // everyone is done with the rows before
+      if (x == 0) {
+        part[grp][lr][0] = top;
+        part[grp][lr][1] = sum;
+      }
+      part_o[grp][lr][x] = y;
+      __syncthreads();
+      if (grp != 0) continue;
+#pragma unroll
+      for (int k = 1; k < kJoinGroups; ++k) top = fmaxf(top, part[k][lr][0]);
+      sum = 0.f;
+      y = f32x4{};
+#pragma unroll
+      for (int k = 0; k < kJoinGroups; ++k) {
+        const float f = fast_exp2(part[k][lr][0] - top);
+        sum += f * part[k][lr][1];
+        const f32x4 o = part_o[k][lr][x];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y[q] += f * o[q];
+      }
     }
-    part_o[grp][lr][x] = y;
-    __syncthreads();
-    if (grp != 0 || !in) continue;
-#pragma unroll
-    for (int k = 1; k < kJoinGroups; ++k) top = fmaxf(top, part[k][lr][0]);
-    sum = 0.f;
-    y = f32x4{};
-#pragma unroll
-    for (int k = 0; k < kJoinGroups; ++k) {
-      const float f = fast_exp2(part[k][lr][0] - top);
-      sum += f * part[k][lr][1];
-      const f32x4 o = part_o[k][lr][x];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) y[q] += f * o[q];
-    }
+    if (!in) continue;
     const int j = fdiv(g.by_group, row);
     const int64_t to = ((int64_t)b.y + j) * g.H + a.z * group + row - j * group;
     if (g.lse && x == 0) g.lse[to] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
@@ -1003,8 +1007,9 @@ hipError_t launch_prompt_attn(const PromptGeom& all, hipStream_t st) {
   if (g.pieces) {
     hipError_t e = launch_kernel(kernel, dim3((unsigned)(g.pieces + g.blocks + 1)), dim3(kThreads), st, g);
     if (e != hipSuccess) return e;
-    // (workgroups of a block: one for as many rows as it takes at a time, but few where there are many blocks, most of them whole)
-    const int rows = 256 / (g.d_v / 4 * kJoinGroups), groups = (g.slot_rows + rows - 1) / rows, most = 8192 / g.blocks > 8 ? 8192 / g.blocks : 8;
+    // (workgroups of a block: one for as many rows as it takes at a time, but few where there are many blocks, most of them whole. With 4096 / 8192 /
+    // 32768 in all, us: prompts of 2048, none cut, 68.3 / 70.0 / 75.3, 24 sequences mixed 207 / 205 / 209)
+    const int rows = 256 / (g.d_v / 4 * kJoinGroups), groups = (g.slot_rows + rows - 1) / rows, most = 4096 / g.blocks > 8 ? 4096 / g.blocks : 8;
     return launch_kernel(g.d_v == 64 ? prompt_join_kernel<64> : prompt_join_kernel<128>, dim3((unsigned)(groups < most ? groups : most), (unsigned)g.blocks),
                          dim3(256), st, g);
   }

@@ -135,6 +135,28 @@ def test_two_graphs_with_workspaces_of_their_own():
             assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
 
 
+def test_two_graphs_that_share_a_workspace():
+    """Two captured calls of other sizes with one workspace, replayed one after the other, each against its eager result."""
+    prm = C(8, 2)
+    calls = []
+    xs = [chunks(prm, new, ctx, 64, seed=seed) for seed, new, ctx in ((1, [3, 40], [6000, 4000]), (2, [64, 1, 1], [9000, 500, 3000]))]
+    ws = torch.empty(max(lsa.chunk_attn_workspace_size(prm, len(x["new"]), sum(x["new"]), x["table"].shape[1], 64) for x in xs), dtype=torch.uint8, device=DEV)
+    for x in xs:
+        out, lse = run_chunks(prm, x)
+        want = out.clone(), lse.clone()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            lsa.chunk_attn(prm, x["q"], x["k_cache"], x["v_cache"], x["cu"], x["ctx"], page_table=x["table"], out=out, lse=lse, workspace=ws)
+        calls.append((graph, out, lse, want))
+    for i in (0, 1, 1, 0, 0, 1):
+        graph, out, lse, want = calls[i]
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
 def test_a_workspace_that_held_something_else():
     """What the workspace holds before a call has no effect."""
     prm = C(8, 2)
