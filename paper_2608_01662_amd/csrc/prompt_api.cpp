@@ -11,14 +11,17 @@ using lsa::hip_fail;
 
 namespace {
 
-// Calls of at most so many blocks of rows, and of more keys than so many, are cut along their keys into about so many pieces: one per CU.
-// us of 32 heads on 8 of 128, with the limit of blocks at 0 / 256 / 512 / 1024: 16 tokens behind 32K (8 blocks) in fp8 872 / 47 / 47 / 47;
-// 1024 behind 7K (136) 226 / 162 / 159 / 159; 24 sequences, 2048 tokens (456) 238 / 231 / 207 / 203, in fp8 309 / 304 / 237 / 237; 2048 behind 6K (264)
-// 256 / 260 / 264 / 264; 3900 behind 4K (496) 393 / 401 / 407 / 406. With 128 / 256 / 512 pieces: 16 behind 32K in fp8 69 / 47 / 56, 512 behind 8K 144 /
-// 102 / 121, 24 sequences 239 / 207 / 222. With keys from 512 / 1024 / 2048 on: 16 behind 1.5K 19 / 19 / 34, behind 2K 21 / 21 / 43, 128 behind 2K 46 / 46 /
-// 64; prompts of 1024 tokens, which gain nothing, 41.6 / 38.2 / 38.2.
-constexpr int64_t kMostCutBlocks = 512, kLeastCutKeys = 16 * lsa::kPromptKeys;
+// Calls of at most so many blocks of rows are cut along their keys into about so many pieces, one per CU. us of 32 heads on 8 of 128, with the limit
+// of blocks at 0 / 256 / 512 / 1024: 16 tokens behind 32K (8 blocks) in fp8 872 / 47 / 47 / 47; 1024 behind 7K (136) 226 / 162 / 159 / 159; 24 sequences,
+// 2048 tokens (456) 238 / 231 / 207 / 203, in fp8 309 / 304 / 237 / 237; 2048 behind 6K (264) 256 / 260 / 264 / 264; 3900 behind 4K (496) 393 / 401 / 407
+// / 406. With 128 / 256 / 512 pieces: 16 behind 32K in fp8 69 / 47 / 56, 512 behind 8K 144 / 102 / 121, 24 sequences 239 / 207 / 222.
+constexpr int64_t kMostCutBlocks = 512;
 constexpr int kPieces = 256;
+// They have to have more than so many keys: the more blocks, the more CUs are busy with them whole, and the more partial results there are. us whole
+// and cut: 16 tokens of 500 keys (8 blocks) 17.4, 15.6, of 900 23.3, 16.6, of 2K 43, 16.4; 200 of 900 (32) 34.0, 27.8; 16 heads on one,
+// prompts of 700 (45) 27.3, 28.0; 12 heads of 64, 900 (48) 23.4, 22.3; 32 on 8, 300 (40) 17.1, 24.2, 700 (88) 28.4, 37, 1024 (136) 37, 41,
+// 1500 (192) 67, 55.
+constexpr int64_t least_cut_keys(int64_t blocks) { return lsa::kPromptKeys * (blocks < 32 ? 8 : blocks > 64 ? 16 : blocks / 4); }
 
 // The pages of a call's caches
 lsa_status check_pages(const int32_t* page_table, int32_t n_seq, int32_t max_pages, int32_t kv_page_size, int64_t n_phys, int32_t n_kv_heads) {
@@ -110,7 +113,7 @@ PromptPlan plan_prompt(int32_t n_seq, int64_t n_tok, int32_t n_heads, int32_t n_
   const int64_t rows = n_tok * (n_heads / n_kv_heads), blocks = n_kv_heads * (rows / lsa::kPromptRows + (n_seq < n_tok ? n_seq : n_tok));
   int64_t keys = most_keys;
   if (k_swa > 0 && (int64_t)k_sink + k_swa + lsa::kPromptRows < keys) keys = (int64_t)k_sink + k_swa + lsa::kPromptRows;
-  if (n_tok == 0 || n_seq == 0 || blocks > kMostCutBlocks || keys <= kLeastCutKeys) return pl;
+  if (n_tok == 0 || n_seq == 0 || blocks > kMostCutBlocks || keys <= least_cut_keys(blocks)) return pl;
   pl.pieces = kPieces;
   pl.blocks = (int)blocks;
   pl.slot_rows = (int)(rows < lsa::kPromptRows ? rows : lsa::kPromptRows);

@@ -116,12 +116,14 @@ __device__ __forceinline__ bool find_whole(const PromptGeom& g, int item, Share&
 }
 
 // The same of a call that has few blocks of rows: the keys of a sequence's blocks are cut into equal pieces, as many as make the
-// call's pieces cost about 1 / g.pieces of all, but of no fewer tiles than pay for the partial results of a piece, which the join
-// reads again: 4, and the more the more rows a block has. (A tile costs 2 with up to 128 rows, a wave per SIMD, and 3 with more.) The
-// largest pieces come first, of up to 64 sequences (24 of 1 to 342 tokens behind 1389 to 8423: 202 us, in the sequences' order and by equal
-// tiles 231). Of a sequence the heads come one after the other, so that an XCD keeps to a class of them, and a block's pieces lie Hkv
+// call's pieces cost about 1 / g.pieces of all, but of kLeastTiles at least: a piece's way to its first tile and its partial results, which
+// the join reads again, take as long as some tiles. (us with 4 tiles, and with 4 to 16 that go with the rows: 64 tokens behind 8K 33.5, 42.4; 128
+// behind 2K 29.9, 42.4; 16 behind 2K 16.4, 20.7, with 2 to 6 15.9.) A tile costs 2 with up to 128 rows, a wave per SIMD, and 3 with more (1 and 2: 24
+// sequences 212 for 202). The largest pieces come first, of up to 64 sequences (24 of 1 to 342 tokens behind 1389 to 8423: 202 us, in the
+// sequences' order and by equal tiles 231). Of a sequence the heads come one after the other, so that an XCD keeps to a class of them, and a block's pieces lie Hkv
 // apart; the last block, which has the most keys, first (3900 tokens behind 4292, 32 heads on 8: 407 us, blocks of a head from the first on 470,
 // not cut at all 393). The first piece of a block tells the join about it.
+constexpr int kLeastTiles = 4;
 __device__ __forceinline__ bool find_piece(const PromptGeom& g, int id, Share& w) {
   const int lane = threadIdx.x & 63, group = (int)g.by_group.d;
   struct Seq {
@@ -157,9 +159,8 @@ __device__ __forceinline__ bool find_piece(const PromptGeom& g, int id, Share& w
   int before = 0, items = 0;
   for (int b0 = 0; b0 < g.n_seq; b0 += 64) {
     if (b0 > 0) s = load(b0 + lane);
-    const int rows = s.n * group, least = 4 + 12 * (rows < kRows ? rows : kRows) / kRows;
-    const float even = share / (float)cost(s);
-    const int each = even > (float)least ? (even < 1e9f ? (int)even + 1 : 1000000000) : least;
+        const float even = share / (float)cost(s);
+    const int each = even > (float)kLeastTiles ? (even < 1e9f ? (int)even + 1 : 1000000000) : kLeastTiles;
     const int pieces = s.tiles > each ? (s.tiles + each - 1) / each : 1;
     int count = s.blocks * g.Hkv * pieces, count_items = s.blocks * g.Hkv, from = lane;
     if (g.n_seq <= 64) {
