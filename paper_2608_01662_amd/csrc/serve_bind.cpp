@@ -5,7 +5,8 @@
 // checks that a good call passes, its allocations and the call itself are compiled. What is not as it should be is not explained
 // here: the functions return None, also where the library refuses, and lsa.py says why. An error of the HIP runtime is
 // raised here (by `check`, a function that lsa.py gives this module), since the call may have run in part. us of a call that the
-// host bounds, with the checks in Python and here: append of one token 12.0, 7.4, of which the launch takes 3.2.
+// host bounds, with the checks in Python and here: append of one token 12.0, 7.4, of which the launch takes 3.2;
+// 1001 rows of a cache read back 15.3, 6.2.
 #include <Python.h>
 
 #include <ATen/ATen.h>
