@@ -23,6 +23,11 @@ constexpr int kPieces = 256;
 // 1500 (192) 67, 55.
 constexpr int64_t least_cut_keys(int64_t blocks) { return lsa::kPromptKeys * (blocks < 32 ? 8 : blocks > 64 ? 16 : blocks / 4); }
 
+// Every workgroup looks through the sequences, 64 at a time, so that a call's time grows with their square (figures beside lsa_chunk_attn in lsa.h;
+// 2^21 sequences would hold the GPU for minutes). And with at most so many the device's sums over sequences (pieces of calls that are cut: per sequence
+// kMostCutBlocks blocks and Hkv more) stay below 2^31 whatever the offsets hold, also where they do not ascend.
+constexpr int32_t kMostSequences = 1 << 16;
+
 // The pages of a call's caches
 lsa_status check_pages(const int32_t* page_table, int32_t n_seq, int32_t max_pages, int32_t kv_page_size, int64_t n_phys, int32_t n_kv_heads) {
   LSA_REQUIRE(max_pages >= 1 && kv_page_size >= 1 && n_phys >= 1, LSA_ERR_INVALID_ARG,
@@ -66,6 +71,7 @@ lsa_status check_chunk_params(const lsa_decode_attn_params* p) {
 
 lsa_status check_tokens(int32_t n_seq, int64_t n_tok, int32_t n_heads, int32_t n_kv_heads) {
   LSA_REQUIRE(n_seq >= 0 && n_tok >= 0, LSA_ERR_INVALID_ARG, "n_seq=%d / n_tok=%lld < 0", n_seq, (long long)n_tok);
+  LSA_REQUIRE(n_seq <= kMostSequences, LSA_ERR_UNSUPPORTED, "n_seq=%d must be at most %d per call", n_seq, kMostSequences);
   LSA_REQUIRE(n_tok < (1LL << 30) && n_tok * n_heads < (1LL << 30) && (int64_t)n_seq * n_kv_heads < (1LL << 24), LSA_ERR_UNSUPPORTED,
               "n_tok * n_heads must be < 2^30 and n_seq * n_kv_heads < 2^24");
   return LSA_OK;
