@@ -246,7 +246,9 @@ static int append_lanes(int units, bool exchange) {
 // Units of queries from which a thread takes four heads: their position, row and angles are found once, for a quarter of the
 // threads. us of one / four heads a thread: 32 heads of 128, bf16, 64 tokens (2^14 units) 3.4 / 3.8, 512 4.9 / 4.9, 1024 7.5 / 7.2, 4096 19.4 / 18.5, 8192 39.3 /
 // 39.6; with one fp8 indexer key 256 4.1 / 4.0, 1024 6.9 / 6.0, 4096 14.6 / 13.7; 8 heads of 64 2048 (2^16) 4.7 / 5.2, 4096 7.2 / 7.6, 8192 (2^18) 11.7 / 11.4;
-// latent, 64 heads, 64 (2^17) 4.7 / 4.5, 256 10.4 / 10.7, 512 15.9 / 15.1.
+// latent, 64 heads, 64 (2^17) 4.7 / 4.5, 256 10.4 / 10.7, 512 15.9 / 15.1. With norms, 32 heads on 8 of 128, bf16, the keys beside the cache: 256 4.5 / 6.2, 512
+// 5.6 / 6.8, 1024 (2^18) 7.5 / 8.0, 2048 12.6 / 12.6, 4096 21.2 / 19.7, 8192 39.2 / 36.6, in fp8 8192 37.6 / 35.8; latent, the latent normed, 64 5.4 / 4.8, 256 10.3 /
+// 9.7, 512 17.0 / 14.8, 8192 229 / 225.
 constexpr int64_t kManyUnits = 1 << 18;
 hipError_t launch_append(const AppendGeom& all, hipStream_t st) {
   AppendGeom g = all;

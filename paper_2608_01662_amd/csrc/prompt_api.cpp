@@ -14,7 +14,10 @@ namespace {
 // Calls of at most so many blocks of rows are cut along their keys into about so many pieces, one per CU. us of 32 heads on 8 of 128, with the limit
 // of blocks at 0 / 256 / 512 / 1024: 16 tokens behind 32K (8 blocks) in fp8 872 / 47 / 47 / 47; 1024 behind 7K (136) 226 / 162 / 159 / 159; 24 sequences,
 // 2048 tokens (456) 238 / 231 / 207 / 203, in fp8 309 / 304 / 237 / 237; 2048 behind 6K (264) 256 / 260 / 264 / 264; 3900 behind 4K (496) 393 / 401 / 407
-// / 406. With 128 / 256 / 512 pieces: 16 behind 32K in fp8 69 / 47 / 56, 512 behind 8K 144 / 102 / 121, 24 sequences 239 / 207 / 222.
+// / 406. From 256 blocks on it is blocks of unequal lengths that gain; equal ones lose 1 to 4%, but the host has the sizes alone and cannot tell them apart. For
+// the same reason calls are planned as cut whose blocks then stay whole (short prompts, of which only the sum of keys is known, and windows), and
+// pay for the join's launch: 16 prompts of 100 28.5, 25.2 without the plan; window of 1024, 12 heads of 64, 8192 tokens 66.7, 62.5, 2048 of 32 on 8 51.4, 48.2, 24
+// sequences 96, 92. With 128 / 256 / 512 pieces: 16 behind 32K in fp8 69 / 47 / 56, 512 behind 8K 144 / 102 / 121, 24 sequences 239 / 207 / 222.
 constexpr int64_t kMostCutBlocks = 512;
 constexpr int kPieces = 256;
 // They have to have more than so many keys: the more blocks, the more CUs are busy with them whole, and the more partial results there are. us whole

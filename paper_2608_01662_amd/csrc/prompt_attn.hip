@@ -10,10 +10,10 @@
 // stay in registers (two waves per SIMD, 256 each; see waves_per_simd). The scores of the next half and the values of the last run on the matrix
 // cores while this half's weights are computed.
 //
-// What bounds it: long calls the matrix cores with the softmax between them, and the clock that the chip holds under them. 32 heads
-// on 8, 8192 x 8192 keys without a mask: 1125 us, 977 TFLOP/s, where a large matrix product reaches 1224 to 1407 (192/128 wide 1006, 64 wide, whose
-// softmax is twice as much per product, 811). A wave's products of a tile take 1024 cycles (64 wide 512) and two waves of a SIMD need about 3900
-// for a tile each. Calls of few rows: the bytes of K and V, and the way to the first tile. Measured and not kept: 64 rows of a wave, one
+// What bounds it: long calls neither the matrix cores (busy 0.39 to 0.43 of the cycles) nor the vector unit (0.29 to 0.48 beside the products), but that they
+// take turns, and the clock, which falls under them. 32 heads on 8, 8192 x 8192 keys without a mask: 1125 us, 977 TFLOP/s, where a large matrix product reaches
+// 1224 to 1407 (192/128 wide 1006, 64 wide, whose softmax is twice as much per product, 811). A wave's products of a tile take 1024 cycles (64 wide 512) and two
+// waves of a SIMD need about 3900 for a tile each. Calls of few rows: the bytes of K and V, and the way to the first tile. Measured and not kept: 64 rows of a wave, one
 // wave per SIMD (1333 us against 1190 at the time); scores weighed before the maximum is known, in one block with the products (1309
 // against 1151); the instructions' order by hand or by groups (1318 against 1151); wave priorities (no change).
 #include "attn_tile.hpp"
@@ -53,8 +53,8 @@ __device__ __forceinline__ int new_tokens(const PromptGeom& g, int b, int& first
   return a >= 0 && e >= a && e <= g.n_tok ? e - a : 0;
 }
 
-// The keys of a block of rows: completes w from its sequence, row0 and rows.
-__device__ __forceinline__ int keys_of(const PromptGeom& g, int b, int& first) {  // keys of sequence b, and the first one's row
+// The keys of sequence b, and the first one's row.
+__device__ __forceinline__ int keys_of(const PromptGeom& g, int b, int& first) {
   if (g.ctx_len) {
     const int c = g.ctx_len[b];
     first = 0;
@@ -64,6 +64,7 @@ __device__ __forceinline__ int keys_of(const PromptGeom& g, int b, int& first) {
   first = a;
   return a >= 0 && e >= a && e <= g.n_kv ? e - a : 0;
 }
+// The tiles of a block of rows: completes w from its sequence, row0 and rows.
 __device__ __forceinline__ void span_of(const PromptGeom& g, Share& w) {
   const int last = (w.rows - w.row0 < kRows ? w.rows : w.row0 + kRows) - 1;
   const int t_lo = g.causal ? w.c - w.n + fdiv(g.by_group, w.row0) : w.c - 1, t_hi = g.causal ? w.c - w.n + fdiv(g.by_group, last) : w.c - 1;
@@ -159,7 +160,7 @@ __device__ __forceinline__ bool find_piece(const PromptGeom& g, int id, Share& w
   int before = 0, items = 0;
   for (int b0 = 0; b0 < g.n_seq; b0 += 64) {
     if (b0 > 0) s = load(b0 + lane);
-        const float even = share / (float)cost(s);
+    const float even = share / (float)cost(s);
     const int each = even > (float)kLeastTiles ? (even < 1e9f ? (int)even + 1 : 1000000000) : kLeastTiles;
     const int pieces = s.tiles > each ? (s.tiles + each - 1) / each : 1;
     int count = s.blocks * g.Hkv * pieces, count_items = s.blocks * g.Hkv, from = lane;
@@ -622,9 +623,11 @@ __device__ __forceinline__ void tile_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// Heads of 64 have registers for two workgroups per CU, the careful form's spilled; not those of fp8 caches, whose loop would be. us with two
-// waves per SIMD and with four: 12 heads, 8192 x 8192 keys 771, 678, window of 1024 81, 68; 32 on 8, 24 sequences mixed 132, 125, in fp8 181, 472; 2048
-// behind 6K 169, 176, 16 behind 32K 28.5, 30.0.
+// Heads of 64 in bf16 run two workgroups per CU, four waves per SIMD. What does not fit their 128 registers is spilled: of the careful form, and over a paged
+// cache also a few addresses of the load path and one register of the masked tiles; not those of fp8 caches, whose products' operands would be. us with two waves
+// per SIMD and with four. Packed: 12 heads, 8192 x 8192 keys 771, 678, window of 1024 81, 68. Paged, 32 heads on 8: 24 sequences mixed 137, 129; 8192 behind 8K
+// 984, 870; 4096 behind 60K 2500, 2260; 4096 of four behind 16K 215, 205; 8 of one token behind 16K 106, 65; 2048 behind 6K 178, 178; 512 behind 4K 42, 44; 16
+// behind 32K 28.7, 29.8; 300 alone 13.3, 14.6; 12 on 12, 8192 alone 169, 177. In fp8, 24 mixed: 181, 472.
 constexpr int waves_per_simd(int d_qk, int kind) { return d_qk == 64 && kind != 2 ? 4 : 2; }
 template <int DQK, int DV, int KIND>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_per_simd(DQK, KIND), waves_per_simd(DQK, KIND)))) void prompt_attn_kernel(PromptGeom g) {
@@ -847,6 +850,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
           for (int r = 0; r < 16; ++r) o[d][r] *= al;
       }
     };
+    // The weights, rounded to bf16 for the product with V (half a step, 2^-8, of each; their sum l takes them as they are in fp32): one product in place of the
+    // two that their high and low halves would need. It moves an output's relative error from 1.7e-3, which its own rounding makes, to 2.2e-3. Those of an fp8
+    // cache are multiplied by the values' scales first, so that there is one rounding too.
     auto weights = [&](int i, int kb, const f32x16& s) {
       f32x4 sc[4];
       if constexpr (FP8) {
