@@ -472,7 +472,8 @@ size_t lsa_prefill_attn_workspace_size(const lsa_prefill_attn_params* p, int32_t
  *   A = { s < n_k : not causal, or s <= t and (k_swa = 0 or s > t - k_swa or s < k_sink) },
  *   o = sum_{s in A} softmax_s(sm_scale * q . k_s) v_s,   lse = log sum_{s in A} exp(sm_scale * q . k_s),
  * head h to key/value head h / (n_heads / n_kv_heads). Where A is empty (t < 0, no keys, or keys out of range), and where every
- * score is -inf, o = 0 and lse = -inf. Keys and values outside A, NaN and infinities among them, have no effect.
+ * score is -inf, o = 0 and lse = -inf. Keys and values outside A, NaN and infinities among them, have no effect. A value in A that is
+ * not finite leaves its dimension of o not finite: infinite, or NaN where its weight is below what fp32 holds.
  *   q           [n_tok, n_heads, d_qk] bf16, tokens q_stride elements apart
  *   k, v        [n_kv, n_kv_heads, d_qk] and [.., d_v] bf16, rows k_stride and v_stride elements apart. Strides: multiples of 8, less
  *               than 2^24, so that the slices of a fused projection are taken as they are

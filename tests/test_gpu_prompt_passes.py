@@ -134,3 +134,22 @@ def test_a_prompt_of_a_whole_call_in_a_cut_one(d):
     check_prompts(prm, x, *whole)
     check_prompts(prm, y, *cut)
     _agree((whole[0][4500:], whole[1][4500:]), cut, y["v"])
+
+
+@pytest.mark.parametrize("d", [64, 128, 192])
+@pytest.mark.parametrize("n,c,top", [(130, 130, 70), (16, 5000, 4000), (16, 5000, 20)], ids=["whole", "cut", "cut, before"])
+def test_an_infinite_value_of_no_weight(d, n, c, top):
+    """One key whose score is hundreds above all others: its value is the output, but for the dimensions in which a value attended to is not finite."""
+    prm = lsa.PrefillAttnParams(2, 1, d, min(d, 128), 0.125)
+    assert (lsa.prefill_attn_workspace_size(prm, 1, n, c) > 0) == (c == 5000)
+    x = prompts(prm, [n], [c], seed=d)
+    x["q"].fill_(8)
+    x["k"].zero_()
+    x["k"][top] = 8
+    x["v"][10, 0, 5], x["v"][30, 0, 6], x["v"][31, 0, 7] = float("inf"), float("-inf"), float("nan")
+    out, _ = run_prompts(prm, x)
+    rows = out[top + 1:] if c == n else out
+    finite = torch.ones(prm.d_v, dtype=torch.bool, device=DEV)
+    finite[5:8] = False
+    assert not torch.isfinite(rows[..., ~finite]).any()
+    assert torch.equal(rows[..., finite], x["v"][top].expand(rows.shape)[..., finite])
